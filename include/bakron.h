@@ -491,6 +491,192 @@ bakron_status bakron_mlp_local_factors_iter(const float *x, const float *g, cons
                                             float *A, float *B, void *work, size_t *work_bytes,
                                             hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Operators around a quantised layer: what feeds it, runs it, calibrates it
+ * and tells what the rounding cost.
+ *
+ * Conventions of this group (in addition to those at the top):
+ *   - matrices are row-major with a leading dimension (entries from one row to
+ *     the next, at least the row's length) where one is given, else contiguous;
+ *     any element alignment is accepted, rows of 16-byte multiples at 16-byte
+ *     addresses are read faster;
+ *   - T is the number of rows (tokens), 0 <= T <= 2^31 - 1; T = 0 does nothing;
+ *   - sums, norms, softmax statistics and products are accumulated in 32 bits
+ *     and rounded once when they are stored, except where a call says otherwise;
+ *   - the summation order is fixed for a given device and shape: repeated calls
+ *     give bitwise the same result;
+ *   - asynchronous on `stream`, no device allocation, no host synchronisation,
+ *     capturable into a graph; error messages via bakron_last_error();
+ *   - workspaces by the protocol of the factor construction: with work == NULL
+ *     the call stores the bytes it needs (possibly 0) in *work_bytes and does
+ *     nothing else.  Where the need is 0 any non-NULL work is accepted.
+ * ------------------------------------------------------------------------ */
+
+typedef enum {
+    BAKRON_F32 = 0,
+    BAKRON_F16 = 1,
+    BAKRON_BF16 = 2
+} bakron_dtype;
+
+typedef enum {
+    BAKRON_ACT_NONE = 0,
+    BAKRON_ACT_SILU = 1,   /* z / (1 + exp(-z))          */
+    BAKRON_ACT_GELU = 2    /* z (1 + erf(z / sqrt 2)) / 2 */
+} bakron_act;
+
+typedef enum {
+    BAKRON_COMBINE_NONE = 0,
+    BAKRON_COMBINE_ADD = 1,   /* a residual              */
+    BAKRON_COMBINE_MUL = 2    /* a gated layer's factor  */
+} bakron_combine;
+
+/* Packed rows of codes, and the rows of 8-bit values that meet them, are padded
+ * to a multiple of this many columns. */
+#define BAKRON_PACK_COLUMNS 128
+
+/*
+ * bakron_rmsnorm_quant -- residual addition, RMS norm and 8-bit output with
+ * one scale a row:
+ *   h = x + residual
+ *   y = normalise ? weight (.) h / sqrt(mean(h^2) + eps) : weight (.) h
+ *   scale = max |y| / 127,   q = rint(y / scale)   (ties to even)
+ * A row of zeros has scale 0 and q 0; a row with a NaN or infinite y has scale
+ * NaN and q 0.  The norm sees the unrounded h.
+ *   x, residual   device, T x d of dtype (bakron_dtype); residual may be NULL
+ *   weight        device, d floats, or NULL for 1.  A quantiser's per-column
+ *                 factors (bakron_quantizer.col_scale) belong in here
+ *   eps           >= 0, finite
+ *   sum           device output of dtype, h rounded once, or NULL; may be x or
+ *                 residual with the same leading dimension
+ *   y             device output of dtype, y rounded once, or NULL
+ *   q             device output int8, or NULL.  ldq >= d; columns d up to
+ *                 min(ldq, d rounded up to BAKRON_PACK_COLUMNS) are set to 0
+ *   scale         device output, T floats; NULL exactly when q is
+ * 1 <= d <= 65536.  One launch.
+ */
+bakron_status bakron_rmsnorm_quant(const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                                   int32_t dtype, int64_t T, int64_t d, const float *weight,
+                                   float eps, int32_t normalise, void *sum, int64_t lds, void *y,
+                                   int64_t ldy, int8_t *q, int64_t ldq, float *scale,
+                                   hipStream_t stream);
+
+/*
+ * bakron_pack_codes -- lays out a layer's codes for bakron_linear, once per
+ * layer: rows padded with zeros to np = n rounded up to BAKRON_PACK_COLUMNS;
+ * in 4 bits, byte i of every 4 bytes holds code i of 8 in its low half and code
+ * i + 4 in its high half (two's complement).
+ *   codes   device, m x n int8 as bakron_solve writes them
+ *   width   4 (codes in [-8, 7]; others lose their upper bits) or 8
+ *   packed  device output, m * np * width / 8 bytes, 16-byte aligned
+ * 1 <= n <= 2^17, 1 <= m <= 2^20.  One launch.
+ */
+bakron_status bakron_pack_codes(const int8_t *codes, int64_t m, int64_t n, int32_t width,
+                                void *packed, hipStream_t stream);
+
+/*
+ * bakron_linear -- 8-bit rows times a quantised layer:
+ *   z_ti = q_scale_t * sum_j s_ij q_tj c_ij + bias_i
+ *   y_ti = act(z_ti) {alone | + other_ti | * other_ti}
+ * with s_ij = scale[i], or scale[i * ceil(n / group_size) + j / group_size].
+ * The products of 8-bit values are summed exactly, over the row or the group.
+ *   q         device, T x n int8 in [-127, 127] (-128 is accepted for
+ *             n <= 65536), as bakron_rmsnorm_quant writes it: ldq >= n rounded up to
+ *             BAKRON_PACK_COLUMNS, a multiple of 16, q 16-byte aligned; the
+ *             padding columns are read (and count for nothing)
+ *   q_scale   device, T floats, or NULL for 1
+ *   packed    from bakron_pack_codes with this n, m and width
+ *   group_size  0 or a multiple of 64
+ *   bias      device, m of dtype, or NULL
+ *   other     device, T x m of dtype; NULL exactly when combine is NONE.  May be
+ *             y with the same leading dimension
+ *   y         device output, T x m of dtype
+ * Workspace as above.
+ */
+bakron_status bakron_linear(const int8_t *q, int64_t ldq, const float *q_scale, int64_t T,
+                            int64_t n, const void *packed, int32_t width, int64_t m,
+                            const float *scale, int64_t group_size, const void *bias, int32_t act,
+                            const void *other, int64_t ldo, int32_t combine, void *y, int64_t ldy,
+                            int32_t dtype, void *work, size_t *work_bytes, hipStream_t stream);
+
+/*
+ * bakron_gated_mlp -- the hidden layer of a gated MLP, both projections, the
+ * activation and the product in one kernel (the first half of App. A's
+ * MLP(x) = W_down (W_up x (.) sigma(W_gate x))):
+ *   G = x W_gate^T,  U = x W_up^T,  h = act(G) (.) U
+ *   x             device, T x d of dtype BAKRON_F16 or BAKRON_BF16
+ *   w_gate, w_up  device, f x d of dtype, the same leading dimension ldw
+ *   act           BAKRON_ACT_SILU or BAKRON_ACT_GELU
+ *   h             device output, T x f of dtype, or NULL
+ *   feat_up       device output, T x f fp32, act(G): the features g that
+ *                 bakron_mlp_local_factors takes for W_up; or NULL
+ *   feat_gate     device output, T x f fp32, act'(G) (.) U: the features f it
+ *                 takes for W_gate; or NULL
+ * 1 <= d, f <= 2^17; ceil(T / 64) * (max(d, 2 f) / 32 + 2) < 2^23 (or
+ * BAKRON_EINVAL).  Workspace as above.
+ */
+bakron_status bakron_gated_mlp(const void *x, int64_t ldx, int64_t T, int64_t d,
+                               const void *w_gate, const void *w_up, int64_t ldw, int64_t f,
+                               int32_t dtype, int32_t act, void *h, int64_t ldh, float *feat_up,
+                               float *feat_gate, void *work, size_t *work_bytes,
+                               hipStream_t stream);
+
+/*
+ * bakron_gated_mlp_backward -- gradients of bakron_gated_mlp from dh, the
+ * gradient with respect to h (G and U are computed again, nothing is kept from
+ * the forward call):
+ *   dG = dh (.) U (.) act'(G),  dU = dh (.) act(G)       (rounded to dtype)
+ *   dx = dG W_gate + dU W_up,  dw_gate = dG^T x,  dw_up = dU^T x
+ *   dx            device output, T x d of dtype, or NULL
+ *   dw_gate, dw_up  device outputs, f x d of dtype, leading dimension lddw;
+ *                 both or neither NULL.  T = 0 gives zeros
+ * Other arguments as bakron_gated_mlp.
+ */
+bakron_status bakron_gated_mlp_backward(const void *dh, int64_t lddh, const void *x, int64_t ldx,
+                                        int64_t T, int64_t d, const void *w_gate, const void *w_up,
+                                        int64_t ldw, int64_t f, int32_t dtype, int32_t act,
+                                        void *dx, int64_t lddx, void *dw_gate, void *dw_up,
+                                        int64_t lddw, void *work, size_t *work_bytes,
+                                        hipStream_t stream);
+
+/*
+ * bakron_token_logprobs -- log probabilities of given tokens, with entropy and
+ * top alternatives, in one pass over the logits:
+ *   lse_t = log sum_j exp(z_tj),   logprob_t = z_t,target - lse_t,
+ *   entropy_t = -sum_j p_tj log p_tj,   p = exp(z - lse)
+ *   logits     device, T x V of dtype.  -inf masks a token.  A row of -inf
+ *              throughout has lse -inf, entropy 0 and log probabilities -inf; a
+ *              row with a NaN or +inf has NaN in every output but top_index
+ *   target     device, T token numbers, or NULL (then logprob must be NULL).  One
+ *              outside [0, V) asks for nothing: logprob 0
+ *   top        number of alternatives, 0 .. min(32, V)
+ *   logprob, entropy, lse   device outputs, T floats each, or NULL
+ *   top_index, top_logprob  device outputs, T x top, by falling logit, equal ones by
+ *              rising index (NaN before all); NULL exactly when top is 0
+ * 1 <= V <= 2^20, T * ceil(V / 16384) <= 2^22 (or BAKRON_EINVAL).  Workspace as above.
+ */
+bakron_status bakron_token_logprobs(const void *logits, int64_t ld, int32_t dtype, int64_t T,
+                                    int64_t V, const int64_t *target, int32_t top, float *logprob,
+                                    float *entropy, float *lse, float *top_logprob,
+                                    int64_t *top_index, void *work, size_t *work_bytes,
+                                    hipStream_t stream);
+
+/*
+ * bakron_token_logprobs_backward -- the gradient with respect to the logits:
+ *   d_tj = g_logprob_t (1[j = target_t] - p_tj) - g_entropy_t p_tj (log p_tj + entropy_t)
+ * A target outside [0, V) has no first term; a row of -inf throughout has d = 0.
+ *   lse, entropy  from bakron_token_logprobs (entropy may be NULL without
+ *                 g_entropy)
+ *   g_logprob, g_entropy  device, T floats, or NULL for 0; target may be NULL
+ *                 without g_logprob
+ *   d             device output, T x V of dtype; may be logits with ldd = ld
+ * T * ceil(V / 4096) <= 2^23 (or BAKRON_EINVAL).  One launch.
+ */
+bakron_status bakron_token_logprobs_backward(const void *logits, int64_t ld, int32_t dtype,
+                                             int64_t T, int64_t V, const int64_t *target,
+                                             const float *lse, const float *entropy,
+                                             const float *g_logprob, const float *g_entropy,
+                                             void *d, int64_t ldd, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,4 +9,7 @@ from ._lib import (BAKRON_EHIP, BAKRON_EINVAL, BAKRON_ENOMEM, BAKRON_ENOTSPD, BA
                    gram_workspace_bytes, mse_scales,
                    kron_factors, load, mlp_local_factors, quadform_weights, sample_weights, solve,
                    solve_antidiag, solve_noalloc,
-                   status_string)
+                   status_string,
+                   MlpFeatures, NormQuant, PackedCodes, TokenLogprobs, gated_mlp,
+                   gated_mlp_backward, linear, pack_codes, rmsnorm_quant, token_logprobs,
+                   token_logprobs_backward)

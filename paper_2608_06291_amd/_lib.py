@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbakron.so")
@@ -20,7 +21,9 @@ EXPORTED = ("bakron_factor", "bakron_solve", "bakron_solve_debug", "bakron_facto
             "bakron_solve_check", "bakron_solve_antidiag", "bakron_gram",
             "bakron_sample_weights", "bakron_kron_factors", "bakron_mlp_local_factors",
             "bakron_mse_scales", "bakron_factor_blockdiag", "bakron_quadform_weights",
-            "bakron_kron_factors_iter", "bakron_mlp_local_factors_iter", "bakron_solve_noalloc")
+            "bakron_kron_factors_iter", "bakron_mlp_local_factors_iter", "bakron_solve_noalloc",
+            "bakron_rmsnorm_quant", "bakron_pack_codes", "bakron_linear", "bakron_gated_mlp",
+            "bakron_gated_mlp_backward", "bakron_token_logprobs", "bakron_token_logprobs_backward")
 
 ALPHABETS = {"sym": 0, "asym": 1}
 
@@ -113,6 +116,23 @@ def load(path: str = LIB_PATH):
     lib.bakron_mlp_local_factors.restype = ctypes.c_int
     lib.bakron_mlp_local_factors.argtypes = [vp, vp, vp, i64, i64, i64, ctypes.c_int32, vp, vp, vp,
                                              szp, vp]
+    i32, f32 = ctypes.c_int32, ctypes.c_float
+    for name, args in (
+            ("bakron_rmsnorm_quant", [vp, i64, vp, i64, i32, i64, i64, vp, f32, i32, vp, i64, vp, i64,
+                                      vp, i64, vp, vp]),
+            ("bakron_pack_codes", [vp, i64, i64, i32, vp, vp]),
+            ("bakron_linear", [vp, i64, vp, i64, i64, vp, i32, i64, vp, i64, vp, i32, vp, i64, i32, vp,
+                               i64, i32, vp, szp, vp]),
+            ("bakron_gated_mlp", [vp, i64, i64, i64, vp, vp, i64, i64, i32, i32, vp, i64, vp, vp, vp,
+                                  szp, vp]),
+            ("bakron_gated_mlp_backward", [vp, i64, vp, i64, i64, i64, vp, vp, i64, i64, i32, i32, vp,
+                                           i64, vp, vp, i64, vp, szp, vp]),
+            ("bakron_token_logprobs", [vp, i64, i32, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp, szp,
+                                       vp]),
+            ("bakron_token_logprobs_backward", [vp, i64, i32, i64, i64, vp, vp, vp, vp, vp, vp, i64,
+                                                vp])):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
     _lib = lib
     return lib
 
@@ -530,3 +550,297 @@ def mlp_local_factors(x, g, D, style: str = "kfac", iters: int = 1):
                                                                 dff, STYLES[style], _ptr(A),
                                                                 _ptr(B), wk, nb, st), x.device)
     return A, B
+
+
+# ---------------------------------------------------------------- operators around a quantised layer
+ACTS = {"none": 0, "silu": 1, "gelu": 2}
+COMBINES = {"none": 0, "add": 1, "mul": 2}
+PACK_COLUMNS = 128   # BAKRON_PACK_COLUMNS
+_DTYPES = None
+
+
+def _dtype_code(dtype):
+    """bakron_dtype of a torch dtype."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+    try:
+        return _DTYPES[dtype]
+    except KeyError:
+        raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}") from None
+
+
+def _rows_of(t, name, shape=None, dtype=None, device=None):
+    """A 2-d tensor whose rows are contiguous (any distance between rows, none
+    overlapping): its address and leading dimension."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must have shape {shape or '(rows, columns)'}, got {tuple(t.shape)}")
+    rows, cols = t.shape
+    ld, inner = t.stride()
+    if cols > 1 and inner != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if rows <= 1:
+        return t.data_ptr(), cols if rows == 0 or ld < cols else ld
+    if ld < cols:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    return t.data_ptr(), ld
+
+
+def _vector(t, name, n, dtype, device):
+    """A contiguous 1-d tensor of n entries, or None: its address."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.device != device:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with {n} entries")
+    return t.data_ptr()
+
+
+def _run_op(fn, args, device, work=None):
+    """Call a workspace-protocol operator; allocates its workspace unless given."""
+    import torch
+    st = torch.cuda.current_stream(device).cuda_stream
+    if work is None:
+        need = ctypes.c_size_t(0)
+        _raise_last(fn(*args, None, ctypes.byref(need), st))
+        if need.value == 0:
+            work_ptr = 256   # not read
+        else:
+            work = torch.empty(need.value, dtype=torch.uint8, device=device)
+    if work is not None:
+        need = ctypes.c_size_t(work.numel() * work.element_size())
+        work_ptr = work.data_ptr()
+    _raise_last(fn(*args, work_ptr, ctypes.byref(need), st))
+
+
+class NormQuant(NamedTuple):
+    """What rmsnorm_quant returns: 8-bit rows (a view of rows padded to a multiple
+    of 128 columns), their scales, and h and y where asked for."""
+    q: object
+    scale: object
+    sum: object = None
+    y: object = None
+
+
+def rmsnorm_quant(x, weight=None, residual=None, eps: float = 1e-5, normalise: bool = True,
+                  quantise: bool = True, with_sum: bool | None = None, with_y: bool = False,
+                  sum_out=None):
+    """bakron_rmsnorm_quant on the current stream: h = x + residual, y = weight *
+    h / rms(h) (normalise=False: weight * h), q = rint(y / scale), scale = max |y| / 127
+    per row.  x: T x d fp32, fp16 or bf16; weight: d fp32.  `sum` is returned where
+    there is a residual, unless with_sum says otherwise; sum_out (e.g. residual
+    itself) receives it."""
+    import torch
+    lib = load()
+    xp, ldx = _rows_of(x, "x")
+    T, d = x.shape
+    code = _dtype_code(x.dtype)
+    dev = x.device
+    rp, ldr = (None, d) if residual is None else _rows_of(residual, "residual", (T, d), x.dtype, dev)
+    wp = _vector(weight, "weight", d, torch.float32, dev)
+    if with_sum is None:
+        with_sum = residual is not None or sum_out is not None
+    hs = ys = q = scale = None
+    sp = yp = qp = cp = None
+    lds = ldy = ldq = d
+    if with_sum:
+        hs = torch.empty((T, d), dtype=x.dtype, device=dev) if sum_out is None else sum_out
+        sp, lds = _rows_of(hs, "sum_out", (T, d), x.dtype, dev)
+    if with_y:
+        ys = torch.empty((T, d), dtype=x.dtype, device=dev)
+        yp, ldy = ys.data_ptr(), d
+    if quantise:
+        ldq = -(-d // PACK_COLUMNS) * PACK_COLUMNS
+        q = torch.empty((T, ldq), dtype=torch.int8, device=dev)
+        scale = torch.empty((T,), dtype=torch.float32, device=dev)
+        qp, cp = q.data_ptr(), scale.data_ptr()
+        if ldq != d:
+            q = q[:, :d]
+    _raise_last(lib.bakron_rmsnorm_quant(
+        xp, ldx, rp, ldr, code, T, d, wp, float(eps), 1 if normalise else 0, sp, lds, yp, ldy, qp, ldq,
+        cp, torch.cuda.current_stream(dev).cuda_stream))
+    return NormQuant(q, scale, hs, ys)
+
+
+class PackedCodes(NamedTuple):
+    """A layer's codes as bakron_linear reads them (bakron_pack_codes): `data` is
+    m x bytes of a padded row, uint8; n columns of `width` bits."""
+    data: object
+    n: int
+    width: int
+
+
+def pack_codes(codes, width: int = 4) -> PackedCodes:
+    """bakron_pack_codes: lays out codes (m x n int8, e.g. of solve) once per layer.
+    width 4 holds codes in [-8, 7]."""
+    import torch
+    _check_dev(codes, "codes", torch.int8)
+    if codes.dim() != 2:
+        raise ValueError("codes must be m x n")
+    m, n = codes.shape
+    padded = -(-n // PACK_COLUMNS) * PACK_COLUMNS
+    data = torch.empty((m, padded * int(width) // 8), dtype=torch.uint8, device=codes.device)
+    _raise_last(load().bakron_pack_codes(codes.data_ptr(), m, n, int(width), data.data_ptr(),
+                                         torch.cuda.current_stream(codes.device).cuda_stream))
+    return PackedCodes(data, n, int(width))
+
+
+def linear(q, q_scale, w: PackedCodes, scale, group_size: int = 0, bias=None, act: str = "none",
+           other=None, combine: str | None = None, dtype=None, out=None, work=None):
+    """bakron_linear on the current stream: act(q_scale * (q (scale * codes)^T) + bias),
+    plus `other` (combine "add", the default where there is one) or times it ("mul").
+    q, q_scale: as rmsnorm_quant returns them (T x n int8, T); scale: m, or m x
+    ceil(n / group_size).  Returns T x m of dtype (default bf16)."""
+    import torch
+    lib = load()
+    qp, ldq = _rows_of(q, "q", None, torch.int8)
+    dev = q.device
+    T, n = q.shape
+    if n != w.n:
+        raise ValueError(f"q has {n} columns, the codes {w.n}")
+    padded = -(-n // PACK_COLUMNS) * PACK_COLUMNS
+    m, row_bytes = w.data.shape
+    if row_bytes * 8 != padded * w.width or not w.data.is_contiguous() or w.data.device != dev:
+        raise ValueError("w.data must be m x padded row bytes, contiguous, on q's device")
+    if T <= 1:
+        # the one row may be a view of any stride: what counts is what follows it
+        ldq = padded
+    if (q.storage_offset() + (T - 1) * ldq + padded if T else 0) > q.untyped_storage().nbytes():
+        raise ValueError("q needs rows padded to a multiple of 128 columns (as rmsnorm_quant leaves them)")
+    g = int(group_size)
+    groups = -(-n // g) if g > 0 else 1
+    if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.device != dev or \
+            scale.numel() != m * groups:
+        raise ValueError(f"scale must be contiguous fp32 with {m * groups} entries")
+    sp = _vector(q_scale, "q_scale", T, torch.float32, dev)
+    if out is None:
+        out = torch.empty((T, m), dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
+    yp, ldy = _rows_of(out, "out", (T, m), dtype, dev)
+    code = _dtype_code(out.dtype)
+    bp = _vector(bias, "bias", m, out.dtype, dev)
+    op, ldo = (None, m) if other is None else _rows_of(other, "other", (T, m), out.dtype, dev)
+    if combine is None:
+        combine = "none" if other is None else "add"
+    _run_op(lib.bakron_linear,
+            (qp, ldq, sp, T, n, w.data.data_ptr(), w.width, m, scale.data_ptr(), g, bp, ACTS[act], op,
+             ldo, COMBINES[combine], yp, ldy, code), dev, work)
+    return out
+
+
+def _mlp_operands(x, w_gate, w_up):
+    xp, ldx = _rows_of(x, "x")
+    T, d = x.shape
+    gp, ldw = _rows_of(w_gate, "w_gate", None, x.dtype, x.device)
+    f = w_gate.shape[0]
+    up, ldu = _rows_of(w_up, "w_up", (f, d), x.dtype, x.device)
+    if w_gate.shape[1] != d or ldu != ldw:
+        raise ValueError("w_gate and w_up must be f x d with the same distance between rows")
+    return xp, ldx, T, d, gp, up, ldw, f, _dtype_code(x.dtype)
+
+
+class MlpFeatures(NamedTuple):
+    """What gated_mlp returns with features=True: the output and the fp32 features
+    that mlp_local_factors takes for W_up and for W_gate."""
+    h: object
+    up: object
+    gate: object
+
+
+def gated_mlp(x, w_gate, w_up, act: str = "silu", features: bool = False, out=None, work=None):
+    """bakron_gated_mlp on the current stream: act(x w_gate^T) * (x w_up^T) in one
+    kernel.  x: T x d, w_gate, w_up: f x d, all fp16 or all bf16.  features=True
+    also returns act(G) and act'(G) * U in fp32."""
+    import torch
+    lib = load()
+    xp, ldx, T, d, gp, up, ldw, f, code = _mlp_operands(x, w_gate, w_up)
+    if out is None:
+        out = torch.empty((T, f), dtype=x.dtype, device=x.device)
+    hp, ldh = _rows_of(out, "out", (T, f), x.dtype, x.device)
+    fu = fg = None
+    if features:
+        fu, fg = (torch.empty((T, f), dtype=torch.float32, device=x.device) for _ in range(2))
+    _run_op(lib.bakron_gated_mlp,
+            (xp, ldx, T, d, gp, up, ldw, f, code, ACTS[act], hp, ldh,
+             fu.data_ptr() if features else None, fg.data_ptr() if features else None), x.device, work)
+    return MlpFeatures(out, fu, fg) if features else out
+
+
+def gated_mlp_backward(dh, x, w_gate, w_up, act: str = "silu", need_dx: bool = True,
+                       need_dw: bool = True, work=None):
+    """bakron_gated_mlp_backward: (dx, dw_gate, dw_up) from dh, the gradient with
+    respect to gated_mlp's output; None for what is not needed."""
+    import torch
+    lib = load()
+    xp, ldx, T, d, gp, up, ldw, f, code = _mlp_operands(x, w_gate, w_up)
+    hp, ldh = _rows_of(dh, "dh", (T, f), x.dtype, x.device)
+    dx = torch.empty((T, d), dtype=x.dtype, device=x.device) if need_dx else None
+    dg, du = (torch.empty((f, d), dtype=x.dtype, device=x.device) if need_dw else None for _ in range(2))
+    _run_op(lib.bakron_gated_mlp_backward,
+            (hp, ldh, xp, ldx, T, d, gp, up, ldw, f, code, ACTS[act], dx.data_ptr() if need_dx else None,
+             d, dg.data_ptr() if need_dw else None, du.data_ptr() if need_dw else None, d), x.device, work)
+    return dx, dg, du
+
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs returns (logprob None without targets, the top
+    alternatives None without `top`)."""
+    logprob: object
+    entropy: object
+    lse: object
+    top_logprob: object = None
+    top_index: object = None
+
+
+def token_logprobs(logits, target=None, top: int = 0, work=None) -> TokenLogprobs:
+    """bakron_token_logprobs on the current stream.  logits: T x V fp32, fp16 or
+    bf16; target: T int64 (outside [0, V): ignored, 0) or None; top: number of
+    alternatives, at most 32."""
+    import torch
+    lib = load()
+    zp, ld = _rows_of(logits, "logits")
+    T, V = logits.shape
+    dev = logits.device
+    tp = _vector(target, "target", T, torch.int64, dev)
+    stats = torch.empty((3, T), dtype=torch.float32, device=dev)
+    logprob, entropy, lse = stats.unbind(0)
+    top = int(top)
+    tl = ti = None
+    if top > 0:
+        tl = torch.empty((T, top), dtype=torch.float32, device=dev)
+        ti = torch.empty((T, top), dtype=torch.int64, device=dev)
+    _run_op(lib.bakron_token_logprobs,
+            (zp, ld, _dtype_code(logits.dtype), T, V, tp, top, None if tp is None else logprob.data_ptr(),
+             entropy.data_ptr(), lse.data_ptr(), None if tl is None else tl.data_ptr(),
+             None if ti is None else ti.data_ptr()), dev, work)
+    return TokenLogprobs(None if tp is None else logprob, entropy, lse, tl, ti)
+
+
+def token_logprobs_backward(logits, target, lse, entropy=None, g_logprob=None, g_entropy=None, out=None):
+    """bakron_token_logprobs_backward: the gradient with respect to the logits, T x V
+    in their dtype (out may be logits itself), from the gradients with respect to
+    token_logprobs' logprob and entropy (None for 0)."""
+    import torch
+    lib = load()
+    zp, ld = _rows_of(logits, "logits")
+    T, V = logits.shape
+    dev = logits.device
+    if out is None:
+        out = torch.empty((T, V), dtype=logits.dtype, device=dev)
+    dp, ldd = _rows_of(out, "out", (T, V), logits.dtype, dev)
+    f32 = torch.float32
+    _raise_last(lib.bakron_token_logprobs_backward(
+        zp, ld, _dtype_code(logits.dtype), T, V, _vector(target, "target", T, torch.int64, dev),
+        _vector(lse, "lse", T, f32, dev), _vector(entropy, "entropy", T, f32, dev),
+        _vector(g_logprob, "g_logprob", T, f32, dev), _vector(g_entropy, "g_entropy", T, f32, dev), dp,
+        ldd, torch.cuda.current_stream(dev).cuda_stream))
+    return out

@@ -1,11 +1,14 @@
 """Build libbakron.so (hand-written HIP for gfx950) in-tree with hipcc."""
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["csrc/api.hip", "csrc/factor.hip", "csrc/solve.hip", "csrc/antidiag.hip",
-           "csrc/hessian.hip", "csrc/quant.hip", "csrc/gptq.hip"]
+           "csrc/hessian.hip", "csrc/quant.hip", "csrc/gptq.hip", "csrc/norm.hip", "csrc/linear.hip",
+           "csrc/mlp.hip", "csrc/logprob.hip"]
 LIB = os.path.join(HERE, "libbakron.so")
 
 HIPCC_FLAGS = [
@@ -20,13 +23,22 @@ def build(verbose: bool = False) -> str:
     """Compile every HIP source into paper_2608_06291_amd/libbakron.so."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp"
-    cmd = [hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
-           "-o", tmp, *[os.path.join(HERE, s) for s in SOURCES]]
-    if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    inc = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
+
+    # one object per source, side by side, then one link
+    with tempfile.TemporaryDirectory() as obj, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        objects = [os.path.join(obj, os.path.basename(s) + ".o") for s in SOURCES]
+        list(pool.map(run, [[hipcc, *flags, *inc, "-c", os.path.join(HERE, s), "-o", o]
+                            for s, o in zip(SOURCES, objects)]))
+        run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *objects])
     os.replace(tmp, LIB)
     return LIB
 

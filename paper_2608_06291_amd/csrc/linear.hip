@@ -1,0 +1,207 @@
+// 8-bit rows times a quantised layer's integer codes, with everything that follows in
+// the epilogue:
+//   z_ti = q_scale_t * sum_j s_ij q_tj c_ij + bias_i,   y = act(z) {alone | + other | * other}
+// The products of 8-bit values run on the integer matrix cores and are summed exactly:
+// |16 c q| <= 128 * 127 and n <= 2^17 keep the sum below 2^31.
+#include "tile.h"
+
+namespace bk {
+
+struct LinearArgs {
+    const int8_t* q;
+    const char* w;           // packed codes
+    const float* q_scale;
+    const float* scale;
+    const void* bias;
+    const void* other;
+    void* y;
+    int64_t ldq, ldw, ldo, ldy;
+    int64_t T, m;
+    int chunks;              // of 128 codes
+    int gsteps, ngroups;     // group_size / 64; groups of a row
+    int act, combine, dtype;
+    int ni, nt;              // tiles
+};
+
+// y_t,i..i+3 from the four sums z (scales applied).
+template <typename E>
+__device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, float (&z)[4]) {
+    const int64_t valid = a.m - i;
+    float v[4];
+    if (a.bias) {
+        load4(static_cast<const E*>(a.bias) + i, v, valid);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] += v[j];
+    }
+    if (a.act != BAKRON_ACT_NONE) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = act_value(z[j], a.act);
+    }
+    if (a.combine != BAKRON_COMBINE_NONE) {
+        load4(static_cast<const E*>(a.other) + t * a.ldo + i, v, valid);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = a.combine == BAKRON_COMBINE_ADD ? z[j] + v[j] : z[j] * v[j];
+    }
+    store4(static_cast<E*>(a.y) + t * a.ldy + i, z, valid);
+}
+
+template <typename M, bool GROUPED, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_linear(LinearArgs a) {
+    typedef Tile<M, BM, BN, WM, WN> Tl;
+    __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+    int ti, tt;
+    tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
+    const int64_t i0 = (int64_t)ti * BM, t0 = (int64_t)tt * BN;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = wave / WN, wn = wave % WN;
+    const int r4 = (lane >> 4) * 4;
+    constexpr int X = Tl::X, Y = Tl::Y;
+    constexpr float UNIT = M::A_BYTES == CHUNK_BYTES ? 1.0f : 1.0f / 16.0f;
+
+    i32x4 acc[X][Y] = {};
+    f32x4 sum[GROUPED ? X : 1][GROUPED ? Y : 1] = {};
+    const int last = 2 * a.chunks - 1;
+    int left = a.gsteps, g = 0;
+    auto after = [&](int step, i32x4 (&acc)[X][Y]) {
+        if constexpr (GROUPED) {
+            if (--left > 0 && step != last) return;
+            left = a.gsteps;
+            if (g < a.ngroups) {   // (past them only padding, whose sums are 0)
+#pragma unroll
+                for (int x = 0; x < X; ++x) {
+                    f32x4 s;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int64_t i = min(i0 + wm * Tl::TM + x * 16 + r4 + j, a.m - 1);
+                        s[j] = a.scale[i * a.ngroups + g];
+                    }
+#pragma unroll
+                    for (int y = 0; y < Y; ++y)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            sum[x][y][j] = fmaf((float)acc[x][y][j], s[j], sum[x][y][j]);
+                            acc[x][y][j] = 0;
+                        }
+                }
+            }
+            ++g;
+        }
+    };
+    Tl::run(
+        lds, [&](int r) { return a.w + min(i0 + r, a.m - 1) * a.ldw; },
+        [&](int r) { return reinterpret_cast<const char*>(a.q) + min(t0 + r, a.T - 1) * a.ldq; },
+        a.ldw, (int64_t)a.chunks * CHUNK_BYTES, a.chunks, acc, after);
+
+#pragma unroll
+    for (int y = 0; y < Y; ++y) {
+        const int64_t t = t0 + wn * Tl::TN + y * 16 + (lane & 15);
+        if (t >= a.T) continue;
+        const float qs = (a.q_scale ? a.q_scale[t] : 1.0f) * UNIT;
+#pragma unroll
+        for (int x = 0; x < X; ++x) {
+            const int64_t i = i0 + wm * Tl::TM + x * 16 + r4;
+            if (i >= a.m) continue;
+            float z[4];
+            if constexpr (GROUPED) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] = sum[x][y][j] * qs;
+            } else {
+                float s[4];
+                load4(a.scale + i, s, a.m - i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] = (float)acc[x][y][j] * (qs * s[j]);
+            }
+            if (a.dtype == BAKRON_F32)
+                linear_store<float>(a, t, i, z);
+            else if (a.dtype == BAKRON_F16)
+                linear_store<f16_t>(a, t, i, z);
+            else
+                linear_store<bf16_t>(a, t, i, z);
+        }
+    }
+}
+
+template <typename M, bool GROUPED, int BM, int BN, int WM, int WN>
+static void launch_linear_tile(LinearArgs a, hipStream_t st) {
+    a.ni = (int)((a.m + BM - 1) / BM);
+    a.nt = (int)((a.T + BN - 1) / BN);
+    hipLaunchKernelGGL((k_linear<M, GROUPED, BM, BN, WM, WN>), dim3((unsigned)(a.ni * a.nt)),
+                       dim3(64 * WM * WN), 0, st, a);
+}
+
+template <typename M, bool GROUPED>
+static void launch_linear(const LinearArgs& a, hipStream_t st) {
+    auto tiles = [&](int64_t b) { return ((a.m + b - 1) / b) * ((a.T + b - 1) / b); };
+    const int ncu = op_cus();
+    if constexpr (!GROUPED) {
+        if (tiles(256) >= ncu) return launch_linear_tile<M, GROUPED, 256, 256, 2, 4>(a, st);
+    }
+    if (tiles(128) >= ncu) return launch_linear_tile<M, GROUPED, 128, 128, 2, 2>(a, st);
+    launch_linear_tile<M, GROUPED, 64, 64, 2, 2>(a, st);
+}
+
+}  // namespace bk
+
+extern "C" bakron_status bakron_linear(const int8_t* q, int64_t ldq, const float* q_scale,
+                                       int64_t T, int64_t n, const void* packed, int32_t width,
+                                       int64_t m, const float* scale, int64_t group_size,
+                                       const void* bias, int32_t act, const void* other,
+                                       int64_t ldo, int32_t combine, void* y, int64_t ldy,
+                                       int32_t dtype, void* work, size_t* work_bytes,
+                                       hipStream_t stream) {
+    static const char who[] = "bakron_linear";
+    bk::set_last_error("");
+    if (T < 0 || T > bk::OP_T_MAX || n < 1 || m < 1 || n > ((int64_t)1 << 17) ||
+        m > ((int64_t)1 << 20))
+        return bk::op_fail(who, "bad size");
+    if (width != 4 && width != 8) return bk::op_fail(who, "width must be 4 or 8");
+    if (group_size < 0 || group_size % 64) return bk::op_fail(who, "group_size must be a multiple of 64");
+    if (act < BAKRON_ACT_NONE || act > BAKRON_ACT_GELU) return bk::op_fail(who, "bad act");
+    if (combine < BAKRON_COMBINE_NONE || combine > BAKRON_COMBINE_MUL)
+        return bk::op_fail(who, "bad combine");
+    if (dtype != BAKRON_F32 && dtype != BAKRON_F16 && dtype != BAKRON_BF16)
+        return bk::op_fail(who, "bad dtype");
+    bool query;
+    const bakron_status st = bk::op_workspace(who, work, work_bytes, 0, &query);
+    if (st != BAKRON_OK || query) return st;
+    const int64_t np = (n + BAKRON_PACK_COLUMNS - 1) / BAKRON_PACK_COLUMNS * BAKRON_PACK_COLUMNS;
+    if (ldq < np || ldq % 16) return bk::op_fail(who, "ldq must be a multiple of 16, at least n padded");
+    if (ldy < m || (other && ldo < m)) return bk::op_fail(who, "leading dimension below m");
+    if ((combine != BAKRON_COMBINE_NONE) != (other != nullptr))
+        return bk::op_fail(who, "other goes with combine");
+    if (other && other == y && ldo != ldy)
+        return bk::op_fail(who, "other in place needs the same leading dimension");
+    if (T == 0) return BAKRON_OK;
+    if (!q || !packed || !scale || !y) return bk::op_fail(who, "null pointer");
+    if (((uintptr_t)q & 15) || ((uintptr_t)packed & 15))
+        return bk::op_fail(who, "q and packed must be 16-byte aligned");
+    if (((T + 63) / 64) * ((m + 63) / 64) > ((int64_t)1 << 24) - 1)
+        return bk::op_fail(who, "too large for one call");
+    bk::LinearArgs a{};
+    a.q = q;
+    a.w = static_cast<const char*>(packed);
+    a.q_scale = q_scale;
+    a.scale = scale;
+    a.bias = bias;
+    a.other = other;
+    a.y = y;
+    a.ldq = ldq;
+    a.ldw = np * width / 8;
+    a.ldo = ldo;
+    a.ldy = ldy;
+    a.T = T;
+    a.m = m;
+    a.chunks = (int)(np / BAKRON_PACK_COLUMNS);
+    a.gsteps = (int)(group_size / 64);
+    a.ngroups = group_size ? (int)((n + group_size - 1) / group_size) : 1;
+    a.act = act;
+    a.combine = combine;
+    a.dtype = dtype;
+    if (width == 4)
+        group_size ? bk::launch_linear<bk::MmaI4, true>(a, stream)
+                   : bk::launch_linear<bk::MmaI4, false>(a, stream);
+    else
+        group_size ? bk::launch_linear<bk::MmaI8, true>(a, stream)
+                   : bk::launch_linear<bk::MmaI8, false>(a, stream);
+    return bk::op_launched(who);
+}

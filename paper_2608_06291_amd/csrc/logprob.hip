@@ -1,0 +1,457 @@
+// Log probabilities of given tokens with entropy and top alternatives, and their
+// gradient.
+//
+// For a row z:  m = max z,  s = sum exp(z - m),  s1 = sum exp(z - m) (z - m),
+//   lse = m + log s,   logprob = z_target - lse,   entropy = log s - s1 / s.
+// Parts of a row join by rescaling to the larger m:
+//   s = s_a e^(m_a - m) + s_b e^(m_b - m),
+//   s1 = (s1_a + (m_a - m) s_a) e^(m_a - m) + (s1_b + (m_b - m) s_b) e^(m_b - m).
+//
+// Top k without sorting: a workgroup holds its part of the row in registers, cuts
+// its threads into 32 groups and takes the k-th largest group maximum as a bound.
+// At least k entries are not below it, and of a row in random order only about
+// 32 (H_32 - H_(32-k)) (31 for k = 20) are, so the candidates are ranked by counting.
+#include "ops.h"
+
+namespace bk {
+
+constexpr int LP_THREADS = 512;
+constexpr int LP_WAVES = LP_THREADS / 64;
+constexpr int LP_REGS = 32;           // 32-bit registers of logits a thread holds at most
+constexpr int LP_TOP = 32;            // alternatives at most
+constexpr int LP_CAND = 1024;         // candidates that are ranked by counting
+constexpr int LP_PARTS = 64;          // parts of a row at most
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LN2 = 0.69314718055994530942f;
+
+// What a part of a row leaves for the join.
+struct LpPart {
+    float m, s, s1, pad;
+};
+
+struct LpArgs {
+    const void* z;
+    int64_t ld;
+    const int64_t* target;
+    int64_t T;
+    int V, part_len, parts, top;
+    float *logprob, *entropy, *lse, *top_logprob;
+    int64_t* top_index;
+    LpPart* part;              // T x parts
+    uint64_t* cand;            // T x parts x top, sorted
+};
+
+// Order of the alternatives: larger logit first (NaN before all, -0 = +0), then
+// smaller index.  Never 0, which stands for none.
+__device__ inline uint32_t lp_key(float v) {
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return v != v ? 0xffffffffu : (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ inline float lp_unkey(uint32_t k) {
+    return k == 0xffffffffu ? NAN : __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
+}
+__device__ inline uint64_t lp_rank(float v, int index) {
+    return ((uint64_t)lp_key(v) << 32) | (uint32_t)(0x7fffffff - index);
+}
+__device__ inline int lp_index(uint64_t r) { return 0x7fffffff - (int)(uint32_t)r; }
+
+__device__ inline uint64_t wave_max_u64(uint64_t v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        const uint32_t lo = __shfl_xor((uint32_t)v, off, 64);
+        const uint32_t hi = __shfl_xor((uint32_t)(v >> 32), off, 64);
+        const uint64_t o = ((uint64_t)hi << 32) | lo;
+        if (o > v) v = o;
+    }
+    return v;
+}
+
+// Writes what a row's statistics give.
+__device__ inline void lp_store(const LpArgs& a, int64_t row, float m, float s, float s1, float zt,
+                                bool asked) {
+    const bool empty = m == -INFINITY;
+    const float lse = empty ? -INFINITY : m + logf(s);
+    if (a.lse) a.lse[row] = lse;
+    if (a.logprob) a.logprob[row] = !asked ? 0.0f : empty ? -INFINITY : zt - lse;
+    if (a.entropy) a.entropy[row] = empty ? 0.0f : logf(s) - s1 / s;
+}
+
+// One workgroup takes one part of one row.  NV: 16-byte vectors a thread holds.
+template <typename E, int NV, bool TOP>
+__global__ __launch_bounds__(LP_THREADS) void k_logprob(LpArgs a) {
+    constexpr int VEC = 16 / sizeof(E);
+    __shared__ float red[3][LP_WAVES];
+    __shared__ float group_max[32];
+    __shared__ float bound;
+    __shared__ int count;
+    __shared__ uint64_t cand[LP_CAND];
+    __shared__ uint64_t best[LP_WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = (int64_t)blockIdx.x / a.parts;
+    const int p = (int)((int64_t)blockIdx.x % a.parts);
+    const E* const z = static_cast<const E*>(a.z) + row * a.ld;
+    const int lo = p * a.part_len, hi = min(a.V, lo + a.part_len);
+
+    Pack<E, VEC> r[NV];
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = lo + (i * LP_THREADS + tid) * VEC;
+        if (c + VEC <= hi) {
+            r[i] = load_pack<E, VEC>(z + c);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) r[i].v[j] = c + j < hi ? z[c + j] : (E)-INFINITY;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) m = max_nan(m, (float)r[i].v[j]);
+    if constexpr (TOP) {   // maxima of 32 groups of 16 threads
+        float g = m;
+#pragma unroll
+        for (int off = 8; off >= 1; off >>= 1) g = max_nan(g, __shfl_xor(g, off, 64));
+        if ((lane & 15) == 0) group_max[wave * 4 + (lane >> 4)] = g;
+        if (tid == 0) count = 0;
+    }
+    m = group_reduce(m, MaxNan(), red[0], wave, lane, LP_WAVES);
+    const float ms = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            // (the bound keeps 0 * -inf out of s1; exp is 0 there)
+            const float d = max_nan((float)r[i].v[j] - ms, -200.0f);
+            const float e = __builtin_amdgcn_exp2f(d * LOG2E);
+            s += e;
+            s1 = fmaf(e, d, s1);
+        }
+    s = wave_reduce(s, Add());
+    s1 = wave_reduce(s1, Add());
+    if (lane == 0) {
+        red[1][wave] = s;
+        red[2][wave] = s1;
+    }
+    if constexpr (TOP) {
+        if (tid < 64) {   // the k-th largest of the 32 group maxima
+            const float g = group_max[tid & 31];
+            const uint64_t k = lp_rank(g, tid & 31);
+            int above = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) above += lp_rank(group_max[i], i) > k;
+            if (tid < 32 && above == a.top - 1) bound = g;
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        s = red[1][0];
+        s1 = red[2][0];
+        for (int w = 1; w < LP_WAVES; ++w) {
+            s += red[1][w];
+            s1 += red[2][w];
+        }
+        if (a.parts == 1) {
+            const int64_t t = a.target ? a.target[row] : -1;
+            const bool asked = t >= 0 && t < a.V;
+            lp_store(a, row, m, s, s1, asked ? (float)z[t] : 0.0f, asked);
+            red[0][0] = m == -INFINITY ? 0.0f : m + logf(s);
+        } else {
+            a.part[row * a.parts + p] = LpPart{m, s, s1, 0.0f};
+        }
+    }
+    if constexpr (TOP) {
+        const float b = bound;
+        // (a thread whose own maximum is below the bound has no candidate; !(x < b)
+        // keeps NaN)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = lo + (i * LP_THREADS + tid) * VEC;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float v = (float)r[i].v[j];
+                if (!(v < b) && c + j < hi) {
+                    const int at = atomicAdd(&count, 1);
+                    if (at < LP_CAND) cand[at] = lp_rank(v, c + j);
+                }
+            }
+        }
+        __syncthreads();
+        const int n = count;
+        const float base = red[0][0];
+        const int64_t part = row * a.parts + p;
+        auto put = [&](int k, uint64_t v) {
+            if (a.parts == 1) {
+                a.top_index[row * a.top + k] = lp_index(v);
+                a.top_logprob[row * a.top + k] = lp_unkey((uint32_t)(v >> 32)) - base;
+            } else {
+                a.cand[part * a.top + k] = v;
+            }
+        };
+        if (n <= LP_CAND) {
+            // every slot of the list has its own rank, whatever order it was filled in
+            for (int i = tid; i < n; i += LP_THREADS) {
+                const uint64_t v = cand[i];
+                int above = 0;
+                for (int k = 0; k < n; ++k) above += cand[k] > v;
+                if (above < a.top) put(above, v);
+            }
+            for (int k = n + tid; k < a.top; k += LP_THREADS) put(k, 0);   // (part shorter than top)
+        } else {
+            // many equal logits (masked rows): the largest one, top times
+            auto own_best = [&](uint64_t below) {
+                uint64_t v = 0;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = lo + (i * LP_THREADS + tid) * VEC;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const uint64_t k = lp_rank((float)r[i].v[j], c + j);
+                        if (c + j < hi && k < below && k > v) v = k;
+                    }
+                }
+                return v;
+            };
+            uint64_t mine = own_best(~0ull);
+            for (int k = 0; k < a.top; ++k) {
+                uint64_t v = wave_max_u64(mine);
+                if (lane == 0) best[wave] = v;
+                __syncthreads();
+                v = best[0];
+                for (int w = 1; w < LP_WAVES; ++w) v = best[w] > v ? best[w] : v;
+                __syncthreads();
+                if (tid == 0) put(k, v);
+                if (v != 0 && mine == v) mine = own_best(v);
+            }
+        }
+    }
+}
+
+// One wave joins the parts of a row: lane l holds part l and the head of its sorted
+// candidates.
+template <typename E>
+__global__ __launch_bounds__(64) void k_logprob_join(LpArgs a) {
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    LpPart q{-INFINITY, 0.0f, 0.0f, 0.0f};
+    const uint64_t* const mine = a.cand + (row * a.parts + lane) * a.top;
+    uint64_t head = 0;
+    if (lane < a.parts) {
+        q = a.part[row * a.parts + lane];
+        if (a.top) head = mine[0];
+    }
+    const float m = wave_reduce(q.m, MaxNan());
+    const float ms = m == -INFINITY ? 0.0f : m;
+    const float d = max_nan(q.m - ms, -200.0f);
+    const float e = __builtin_amdgcn_exp2f(d * LOG2E);
+    const float s = wave_reduce(q.s * e, Add());
+    const float s1 = wave_reduce(fmaf(d, q.s, q.s1) * e, Add());
+    if (lane == 0) {
+        const int64_t t = a.target ? a.target[row] : -1;
+        const bool asked = t >= 0 && t < a.V;
+        lp_store(a, row, m, s, s1,
+                 asked ? (float)(static_cast<const E*>(a.z) + row * a.ld)[t] : 0.0f, asked);
+    }
+    const float base = m == -INFINITY ? 0.0f : m + logf(s);
+    int at = 0;
+    for (int k = 0; k < a.top; ++k) {
+        const uint64_t v = wave_max_u64(head);
+        if (v == head) {   // keys are distinct: one lane
+            a.top_index[row * a.top + k] = lp_index(v);
+            a.top_logprob[row * a.top + k] = lp_unkey((uint32_t)(v >> 32)) - base;
+            ++at;
+            head = at < a.top ? mine[at] : 0;
+        }
+    }
+}
+
+struct LpGradArgs {
+    const void* z;
+    int64_t ld;
+    const int64_t* target;
+    const float *lse, *entropy, *g_logprob, *g_entropy;
+    void* d;
+    int64_t ldd;
+    int V, pieces;
+};
+
+constexpr int LPG_NV = 4;   // vectors a thread has in flight
+
+template <typename E, bool ENT>
+__global__ __launch_bounds__(256) void k_logprob_grad(LpGradArgs a) {
+    constexpr int VEC = 16 / sizeof(E);
+    const int64_t row = (int64_t)blockIdx.x / a.pieces;
+    const int lo = (int)((int64_t)blockIdx.x % a.pieces) * (256 * LPG_NV * VEC);
+    const E* const z = static_cast<const E*>(a.z) + row * a.ld;
+    E* const out = static_cast<E*>(a.d) + row * a.ldd;
+    Pack<E, VEC> r[LPG_NV];
+    const int c0 = lo + (int)threadIdx.x * VEC;
+#pragma unroll
+    for (int i = 0; i < LPG_NV; ++i) {
+        const int c = c0 + i * 256 * VEC;
+        if (c + VEC <= a.V) {
+            r[i] = load_pack<E, VEC>(z + c);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) r[i].v[j] = c + j < a.V ? z[c + j] : (E)0.0f;
+        }
+    }
+    float lse = a.lse[row];
+    const bool empty = lse == -INFINITY;
+    if (empty) lse = INFINITY;   // every p is then exp(-inf) = 0
+    const int64_t t64 = a.target ? a.target[row] : -1;
+    const bool asked = t64 >= 0 && t64 < a.V && !empty;
+    const int t = asked ? (int)t64 : -1;
+    const float gl = asked && a.g_logprob ? a.g_logprob[row] : 0.0f;
+    const float gh = ENT ? a.g_entropy[row] : 0.0f, H = ENT ? a.entropy[row] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < LPG_NV; ++i) {
+        const int c = c0 + i * 256 * VEC;
+        Pack<E, VEC> o;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float lp = (float)r[i].v[j] - lse;
+            const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
+            float g = gl;
+            if (ENT) g = fmaf(gh, max_nan(lp, -1e4f) + H, gl);   // (0 * -inf stays out)
+            float v = -p * g;
+            if (c + j == t) v += gl;
+            o.v[j] = (E)v;
+        }
+        if (c + VEC <= a.V) {
+            store_pack(out + c, o);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (c + j < a.V) out[c + j] = o.v[j];
+        }
+    }
+}
+
+// Parts of a row: as long as the registers allow with many rows; with few, so many
+// that every CU has a workgroup, down to one vector a thread.
+struct LpGeom {
+    int parts, len, nv;
+};
+static LpGeom lp_geom(int64_t T, int64_t V, int esize) {
+    const int64_t vec = 16 / esize, least = LP_THREADS * vec, most = LP_THREADS * LP_REGS * 4 / esize;
+    int64_t parts = (V + most - 1) / most;
+    const int64_t fill = (2 * 256 + T - 1) / T;   // two workgroups a CU
+    if (parts < fill) parts = std::min<int64_t>(fill, (V + least - 1) / least);
+    parts = std::min<int64_t>(parts, LP_PARTS);
+    // (parts <= LP_PARTS always holds `most` entries a part at V <= 2^20)
+    int64_t len = (V + parts - 1) / parts;
+    len = (len + vec - 1) / vec * vec;
+    LpGeom g;
+    g.parts = (int)((V + len - 1) / len);
+    g.len = (int)len;
+    g.nv = (int)((len + least - 1) / least);
+    return g;
+}
+
+template <typename E, int NV>
+static void launch_logprob_nv(const LpArgs& a, hipStream_t st) {
+    const dim3 grid((unsigned)(a.T * a.parts));
+    if (a.top)
+        hipLaunchKernelGGL((k_logprob<E, NV, true>), grid, dim3(LP_THREADS), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_logprob<E, NV, false>), grid, dim3(LP_THREADS), 0, st, a);
+}
+
+template <typename E>
+static void launch_logprob(const LpArgs& a, int nv, hipStream_t st) {
+    if (nv <= 1)
+        launch_logprob_nv<E, 1>(a, st);
+    else if (nv <= 2)
+        launch_logprob_nv<E, 2>(a, st);
+    else if (nv <= 4)
+        launch_logprob_nv<E, 4>(a, st);
+    else
+        launch_logprob_nv<E, 8>(a, st);
+    if (a.parts > 1)
+        hipLaunchKernelGGL(k_logprob_join<E>, dim3((unsigned)a.T), dim3(64), 0, st, a);
+}
+
+template <typename E>
+static void launch_logprob_grad(LpGradArgs a, int64_t T, hipStream_t st) {
+    const int per = 256 * LPG_NV * 16 / (int)sizeof(E);
+    a.pieces = (a.V + per - 1) / per;
+    const dim3 grid((unsigned)(T * a.pieces));
+    if (a.g_entropy)
+        hipLaunchKernelGGL((k_logprob_grad<E, true>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_logprob_grad<E, false>), grid, dim3(256), 0, st, a);
+}
+
+}  // namespace bk
+
+static bakron_status logprob_sizes(const char* who, int32_t dtype, int64_t T, int64_t V, int64_t ld) {
+    if (dtype != BAKRON_F32 && dtype != BAKRON_F16 && dtype != BAKRON_BF16)
+        return bk::op_fail(who, "bad dtype");
+    if (T < 0 || T > bk::OP_T_MAX || V < 1 || V > ((int64_t)1 << 20) || ld < V) return bk::op_fail(who, "bad size");
+    return BAKRON_OK;
+}
+
+extern "C" bakron_status bakron_token_logprobs(const void* logits, int64_t ld, int32_t dtype,
+                                               int64_t T, int64_t V, const int64_t* target,
+                                               int32_t top, float* logprob, float* entropy,
+                                               float* lse, float* top_logprob, int64_t* top_index,
+                                               void* work, size_t* work_bytes, hipStream_t stream) {
+    static const char who[] = "bakron_token_logprobs";
+    bk::set_last_error("");
+    bakron_status st = logprob_sizes(who, dtype, T, V, ld);
+    if (st != BAKRON_OK) return st;
+    if (top < 0 || top > bk::LP_TOP || top > V) return bk::op_fail(who, "bad number of alternatives");
+    const int esize = dtype == BAKRON_F32 ? 4 : 2;
+    const bk::LpGeom g = bk::lp_geom(T ? T : 1, V, esize);
+    if (T > bk::OP_LAUNCH_MAX / bk::LP_THREADS / g.parts)
+        return bk::op_fail(who, "too many rows for one call");
+    const size_t stats = (size_t)T * g.parts * sizeof(bk::LpPart);
+    const size_t need = g.parts > 1 ? stats + (size_t)T * g.parts * top * sizeof(uint64_t) : 0;
+    bool query;
+    st = bk::op_workspace(who, work, work_bytes, need, &query);
+    if (st != BAKRON_OK || query) return st;
+    if (logprob && !target) return bk::op_fail(who, "logprob needs targets");
+    if ((top > 0) != (top_logprob != nullptr) || (top > 0) != (top_index != nullptr))
+        return bk::op_fail(who, "top outputs go with top");
+    if (T == 0) return BAKRON_OK;
+    if (!logits) return bk::op_fail(who, "null pointer");
+    bk::LpArgs a{logits, ld, target, T, (int)V, g.len, g.parts, top, logprob, entropy, lse,
+                 top_logprob, top_index, static_cast<bk::LpPart*>(work),
+                 reinterpret_cast<uint64_t*>(static_cast<char*>(work) + stats)};
+    if (dtype == BAKRON_F32)
+        bk::launch_logprob<float>(a, g.nv, stream);
+    else if (dtype == BAKRON_F16)
+        bk::launch_logprob<bk::f16_t>(a, g.nv, stream);
+    else
+        bk::launch_logprob<bk::bf16_t>(a, g.nv, stream);
+    return bk::op_launched(who);
+}
+
+extern "C" bakron_status bakron_token_logprobs_backward(
+    const void* logits, int64_t ld, int32_t dtype, int64_t T, int64_t V, const int64_t* target,
+    const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy, void* d,
+    int64_t ldd, hipStream_t stream) {
+    static const char who[] = "bakron_token_logprobs_backward";
+    bk::set_last_error("");
+    bakron_status st = logprob_sizes(who, dtype, T, V, ld);
+    if (st != BAKRON_OK) return st;
+    if (ldd < V) return bk::op_fail(who, "bad size");
+    const int64_t per = 256 * bk::LPG_NV * 16 / (dtype == BAKRON_F32 ? 4 : 2);
+    if (T > bk::OP_LAUNCH_MAX / 256 / ((V + per - 1) / per))
+        return bk::op_fail(who, "too many rows for one call");
+    if (d == logits && ldd != ld) return bk::op_fail(who, "in place needs ldd = ld");
+    if (g_logprob && !target) return bk::op_fail(who, "g_logprob needs targets");
+    if (g_entropy && !entropy) return bk::op_fail(who, "g_entropy needs the entropies");
+    if (T == 0) return BAKRON_OK;
+    if (!logits || !lse || !d) return bk::op_fail(who, "null pointer");
+    bk::LpGradArgs a{logits, ld, target, lse, entropy, g_logprob, g_entropy, d, ldd, (int)V, 0};
+    if (dtype == BAKRON_F32)
+        bk::launch_logprob_grad<float>(a, T, stream);
+    else if (dtype == BAKRON_F16)
+        bk::launch_logprob_grad<bk::f16_t>(a, T, stream);
+    else
+        bk::launch_logprob_grad<bk::bf16_t>(a, T, stream);
+    return bk::op_launched(who);
+}

@@ -1,0 +1,272 @@
+// Residual addition, RMS norm and 8-bit rows with one scale each.
+//
+//   h = x + r,   y = w (.) h / sqrt(mean(h^2) + eps),   s = max |y| / 127,   q = rint(y / s)
+//
+// Every entry is read once and stays in registers over the two reductions of its
+// row (the sum of squares, then the largest |y|, which needs the first), so the
+// kernel moves what it must: x and r in, h and q out.  Bound by memory.
+#include "ops.h"
+
+namespace bk {
+
+struct NormArgs {
+    const void* x;
+    const void* res;
+    const float* w;
+    void* sum;
+    void* y;
+    int8_t* q;
+    float* scale;
+    int64_t ldx, ldr, lds, ldy, ldq;
+    int64_t T;
+    int d;
+    int dpad;        // q columns written: d rounded up, within ldq
+    float eps;
+    int normalise;
+};
+
+// A row belongs to blockDim.x threads (one wave, with blockDim.y rows in the
+// workgroup, or the whole workgroup); thread t holds the vectors t, t + blockDim.x, ..
+// of VEC entries, NV of them.
+template <typename E, int NV>
+__global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
+    constexpr int VEC = 16 / sizeof(E);
+    __shared__ float red[2][16];
+    const int tid = threadIdx.x, tpr = blockDim.x, lane = tid & 63, wave = tid >> 6;
+    const int waves = tpr >> 6;
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (row >= a.T) return;   // (a whole wave, and never one of several in a row)
+    const E* const x = static_cast<const E*>(a.x) + row * a.ldx;
+    const E* const res = a.res ? static_cast<const E*>(a.res) + row * a.ldr : nullptr;
+
+    float h[NV][VEC];
+    float ssq = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * tpr + tid) * VEC;
+        if (c + VEC <= a.d) {
+            const auto px = load_pack<E, VEC>(x + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) h[i][j] = (float)px.v[j];
+            if (res) {
+                const auto pr = load_pack<E, VEC>(res + c);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) h[i][j] += (float)pr.v[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                h[i][j] = 0.0f;
+                if (c + j < a.d) h[i][j] = (float)x[c + j] + (res ? (float)res[c + j] : 0.0f);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) ssq = fmaf(h[i][j], h[i][j], ssq);
+    if (a.sum) {
+        E* const out = static_cast<E*>(a.sum) + row * a.lds;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * tpr + tid) * VEC;
+            if (c + VEC <= a.d) {
+                Pack<E, VEC> p;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) p.v[j] = (E)h[i][j];
+                store_pack(out + c, p);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+                    if (c + j < a.d) out[c + j] = (E)h[i][j];
+            }
+        }
+    }
+    float r = 1.0f;
+    if (a.normalise) {
+        ssq = group_reduce(ssq, Add(), red[0], wave, lane, waves);
+        const float v = ssq / (float)a.d + a.eps;
+        r = v == 0.0f ? 0.0f : 1.0f / sqrtf(v);
+        if (!(v < INFINITY)) r = NAN;   // squares beyond fp32: not silently 0
+    }
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * tpr + tid) * VEC;
+        if (c + VEC <= a.d) {
+            if (a.w) {
+                const auto pw = load_pack<float, VEC>(a.w + c);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) h[i][j] = h[i][j] * r * pw.v[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) h[i][j] *= r;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (c + j < a.d) h[i][j] = h[i][j] * r * (a.w ? a.w[c + j] : 1.0f);
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) top = max_nan(top, fabsf(h[i][j]));
+    }
+    if (a.y) {
+        E* const out = static_cast<E*>(a.y) + row * a.ldy;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * tpr + tid) * VEC;
+            if (c + VEC <= a.d) {
+                Pack<E, VEC> p;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) p.v[j] = (E)h[i][j];
+                store_pack(out + c, p);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+                    if (c + j < a.d) out[c + j] = (E)h[i][j];
+            }
+        }
+    }
+    if (!a.q) return;
+    top = group_reduce(top, MaxNan(), red[1], wave, lane, waves);
+    const bool finite = top < INFINITY;
+    const float s = finite ? top / 127.0f : NAN;
+    if (tid == 0) a.scale[row] = s;
+    // y / s as a product where 1 / s exists, so a division only for rows below 2^-119
+    const bool tiny = top < 1.5e-36f;
+    const float inv = finite && !tiny ? 127.0f / top : 0.0f;
+    int8_t* const out = a.q + row * a.ldq;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * tpr + tid) * VEC;
+        Pack<int8_t, VEC> p;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            float v = h[i][j] * inv;
+            if (tiny) v = s > 0.0f ? h[i][j] / s : 0.0f;
+            p.v[j] = finite && c + j < a.d ? (int8_t)(int)rintf(v) : (int8_t)0;
+        }
+        if (c + VEC <= a.dpad) {
+            store_pack(out + c, p);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (c + j < a.dpad) out[c + j] = p.v[j];
+        }
+    }
+}
+
+// Codes to packed rows: a thread writes 16 bytes (32 codes of 4 bits, 16 of 8).
+template <int WIDTH>
+__global__ __launch_bounds__(256) void k_pack(const int8_t* __restrict__ codes, int64_t m, int64_t n,
+                                              int64_t np, uint32_t* __restrict__ packed) {
+    constexpr int PER = 128 / WIDTH;
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, per_row = np / PER;
+    if (e >= m * per_row) return;
+    const int64_t i = e / per_row, c = e % per_row * PER;
+    const int8_t* const src = codes + i * n;
+    uint32_t out[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const uint32_t v = c + j < n ? (uint32_t)(uint8_t)src[c + j] : 0u;
+        if (WIDTH == 8)
+            out[j / 4] |= v << (8 * (j % 4));
+        else
+            out[j / 8] |= (v & 15u) << (8 * (j % 4) + (j % 8 >= 4 ? 4 : 0));
+    }
+    uint32_t* const dst = packed + e * 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dst[j] = out[j];
+}
+
+template <typename E>
+static void launch_norm(const NormArgs& a, hipStream_t st) {
+    constexpr int VEC = 16 / sizeof(E);
+    // (the padding of q is written by the threads of the vectors past d)
+    const int vecs = (std::max(a.d, a.q ? a.dpad : 0) + VEC - 1) / VEC;
+    constexpr int NV_MAX = 64 / VEC;
+    // Threads a row: one vector a thread with few rows, where the latency of the
+    // row counts; two with many.
+    int nv = a.T < 1024 ? 1 : 2, tpr = 64;
+    while (tpr < 1024 && tpr * nv < vecs) tpr *= 2;
+    while (nv < NV_MAX && tpr * nv < vecs) nv *= 2;
+    const int rows = tpr == 64 ? 4 : 1;
+    if (a.T * tpr > OP_LAUNCH_MAX) {   // more threads than one launch takes
+        NormArgs b = a;
+        b.T = OP_LAUNCH_MAX / tpr;
+        launch_norm<E>(b, st);
+        b.T = a.T - OP_LAUNCH_MAX / tpr;
+        const int64_t r = OP_LAUNCH_MAX / tpr;
+        b.x = static_cast<const E*>(a.x) + r * a.ldx;
+        if (a.res) b.res = static_cast<const E*>(a.res) + r * a.ldr;
+        if (a.sum) b.sum = static_cast<E*>(a.sum) + r * a.lds;
+        if (a.y) b.y = static_cast<E*>(a.y) + r * a.ldy;
+        if (a.q) {
+            b.q = a.q + r * a.ldq;
+            b.scale = a.scale + r;
+        }
+        return launch_norm<E>(b, st);
+    }
+    const dim3 grid((unsigned)((a.T + rows - 1) / rows)), block(tpr, rows);
+    switch (nv) {
+        case 1: hipLaunchKernelGGL((k_norm<E, 1>), grid, block, 0, st, a); break;
+        case 2: hipLaunchKernelGGL((k_norm<E, 2>), grid, block, 0, st, a); break;
+        case 4: hipLaunchKernelGGL((k_norm<E, 4>), grid, block, 0, st, a); break;
+        case 8: hipLaunchKernelGGL((k_norm<E, 8>), grid, block, 0, st, a); break;
+        default: hipLaunchKernelGGL((k_norm<E, NV_MAX>), grid, block, 0, st, a); break;
+    }
+}
+
+}  // namespace bk
+
+extern "C" bakron_status bakron_rmsnorm_quant(const void* x, int64_t ldx, const void* residual,
+                                              int64_t ldr, int32_t dtype, int64_t T, int64_t d,
+                                              const float* weight, float eps, int32_t normalise,
+                                              void* sum, int64_t lds, void* y, int64_t ldy,
+                                              int8_t* q, int64_t ldq, float* scale,
+                                              hipStream_t stream) {
+    static const char who[] = "bakron_rmsnorm_quant";
+    bk::set_last_error("");
+    if (T < 0 || T > bk::OP_T_MAX || d < 1 || d > 65536) return bk::op_fail(who, "bad size");
+    if (dtype != BAKRON_F32 && dtype != BAKRON_F16 && dtype != BAKRON_BF16)
+        return bk::op_fail(who, "bad dtype");
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return bk::op_fail(who, "bad eps");
+    if (!q != !scale) return bk::op_fail(who, "q and scale go together");
+    if (ldx < d || (residual && ldr < d) || (sum && lds < d) || (y && ldy < d) || (q && ldq < d))
+        return bk::op_fail(who, "leading dimension below d");
+    if (((sum && sum == x) && lds != ldx) || ((sum && sum == residual) && lds != ldr))
+        return bk::op_fail(who, "sum in place needs the same leading dimension");
+    if (T == 0) return BAKRON_OK;
+    if (!x) return bk::op_fail(who, "null pointer");
+    const int64_t up = (d + BAKRON_PACK_COLUMNS - 1) / BAKRON_PACK_COLUMNS * BAKRON_PACK_COLUMNS;
+    bk::NormArgs a{x, residual, weight, sum, y, q, scale, ldx, ldr, lds, ldy, ldq, T, (int)d,
+                   (int)(ldq < up ? ldq : up), eps, normalise != 0};
+    if (dtype == BAKRON_F32)
+        bk::launch_norm<float>(a, stream);
+    else if (dtype == BAKRON_F16)
+        bk::launch_norm<bk::f16_t>(a, stream);
+    else
+        bk::launch_norm<bk::bf16_t>(a, stream);
+    return bk::op_launched(who);
+}
+
+extern "C" bakron_status bakron_pack_codes(const int8_t* codes, int64_t m, int64_t n, int32_t width,
+                                           void* packed, hipStream_t stream) {
+    static const char who[] = "bakron_pack_codes";
+    bk::set_last_error("");
+    if (m < 1 || n < 1 || m > ((int64_t)1 << 20) || n > ((int64_t)1 << 17))
+        return bk::op_fail(who, "bad size");
+    if (width != 4 && width != 8) return bk::op_fail(who, "width must be 4 or 8");
+    if (!codes || !packed) return bk::op_fail(who, "null pointer");
+    if ((uintptr_t)packed & 15) return bk::op_fail(who, "packed must be 16-byte aligned");
+    const int64_t np = (n + BAKRON_PACK_COLUMNS - 1) / BAKRON_PACK_COLUMNS * BAKRON_PACK_COLUMNS;
+    const int64_t pieces = m * np * width / 128;
+    const dim3 grid((unsigned)((pieces + 255) / 256));
+    if (width == 4)
+        hipLaunchKernelGGL(bk::k_pack<4>, grid, dim3(256), 0, stream, codes, m, n, np,
+                           static_cast<uint32_t*>(packed));
+    else
+        hipLaunchKernelGGL(bk::k_pack<8>, grid, dim3(256), 0, stream, codes, m, n, np,
+                           static_cast<uint32_t*>(packed));
+    return bk::op_launched(who);
+}
