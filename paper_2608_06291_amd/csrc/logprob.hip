@@ -55,15 +55,12 @@ __device__ inline uint64_t lp_rank(float v, int index) {
 }
 __device__ inline int lp_index(uint64_t r) { return 0x7fffffff - (int)(uint32_t)r; }
 
+// The largest of the wave: by the upper halves, then by the lower ones among equals.
 __device__ inline uint64_t wave_max_u64(uint64_t v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        const uint32_t lo = __shfl_xor((uint32_t)v, off, 64);
-        const uint32_t hi = __shfl_xor((uint32_t)(v >> 32), off, 64);
-        const uint64_t o = ((uint64_t)hi << 32) | lo;
-        if (o > v) v = o;
-    }
-    return v;
+    const uint32_t hi = (uint32_t)(v >> 32);
+    const uint32_t top = wave_reduce(hi, MaxU32());
+    const uint32_t lo = wave_reduce(hi == top ? (uint32_t)v : 0u, MaxU32());
+    return ((uint64_t)top << 32) | lo;
 }
 
 // Writes what a row's statistics give.
@@ -78,7 +75,7 @@ __device__ inline void lp_store(const LpArgs& a, int64_t row, float m, float s, 
 
 // One workgroup takes one part of one row.  NV: 16-byte vectors a thread holds.
 template <typename E, int NV, bool TOP>
-__global__ __launch_bounds__(LP_THREADS) void k_logprob(LpArgs a) {
+__global__ __launch_bounds__(LP_THREADS, 6) void k_logprob(LpArgs a) {
     constexpr int VEC = 16 / sizeof(E);
     __shared__ float red[3][LP_WAVES];
     __shared__ float group_max[32];
@@ -87,99 +84,86 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprob(LpArgs a) {
     __shared__ uint64_t cand[LP_CAND];
     __shared__ uint64_t best[LP_WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = (int64_t)blockIdx.x / a.parts;
-    const int p = (int)((int64_t)blockIdx.x % a.parts);
+    const int64_t row = blockIdx.x / (uint32_t)a.parts;
+    const int p = (int)(blockIdx.x % (uint32_t)a.parts);
     const E* const z = static_cast<const E*>(a.z) + row * a.ld;
     const int lo = p * a.part_len, hi = min(a.V, lo + a.part_len);
 
-    Pack<E, VEC> r[NV];
-    float m = -INFINITY;
+    // The part's whole vectors; what is left of it, less than one, goes one entry a thread.
+    const int whole = (hi - lo) / VEC;
+    u32x4 r[NV];
+    if (whole > 0) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = lo + (i * LP_THREADS + tid) * VEC;
-        if (c + VEC <= hi) {
-            r[i] = load_pack<E, VEC>(z + c);
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) r[i].v[j] = c + j < hi ? z[c + j] : (E)-INFINITY;
-        }
+        for (int i = 0; i < NV; ++i)
+            r[i] = load_words(z + lo + min(i * LP_THREADS + tid, whole - 1) * VEC);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
+        if (i * LP_THREADS + tid >= whole) r[i] = u32x4(minus_infinity<E>());
+    const int left = lo + whole * VEC + tid;
+    const float extra = left < hi ? (float)z[left] : -INFINITY;
+    float m = extra;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) m = max_nan(m, (float)r[i].v[j]);
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) m = max_nan(m, entry<E>(r[i], j));
     if constexpr (TOP) {   // maxima of 32 groups of 16 threads
-        float g = m;
-#pragma unroll
-        for (int off = 8; off >= 1; off >>= 1) g = max_nan(g, __shfl_xor(g, off, 64));
+        const float g = row_reduce(m, MaxNan());
         if ((lane & 15) == 0) group_max[wave * 4 + (lane >> 4)] = g;
         if (tid == 0) count = 0;
     }
     m = group_reduce(m, MaxNan(), red[0], wave, lane, LP_WAVES);
+    if constexpr (TOP) {
+        // the k-th largest of the group maxima: a wave ranks four of them, 16 lanes each
+        const int g = wave * 4 + (lane >> 4), l = lane & 15;
+        const uint64_t own = lp_rank(group_max[g], g);
+        const uint64_t b0 = __ballot(lp_rank(group_max[l], l) > own);
+        const uint64_t b1 = __ballot(lp_rank(group_max[l + 16], l + 16) > own);
+        const int sh = lane & 48;
+        const int above = __popc((uint32_t)(b0 >> sh) & 0xffffu) + __popc((uint32_t)(b1 >> sh) & 0xffffu);
+        if (l == 0 && above == a.top - 1) bound = group_max[g];
+    }
     const float ms = m == -INFINITY ? 0.0f : m;
     float s = 0.0f, s1 = 0.0f;
+    auto add = [&](float x) {
+        // (the bound keeps 0 * -inf out of s1; exp is 0 there)
+        const float d = max_nan(x - ms, -200.0f);
+        const float e = __builtin_amdgcn_exp2f(d * LOG2E);
+        s += e;
+        s1 = fmaf(e, d, s1);
+    };
+    add(extra);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+        forget(r[i]);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            // (the bound keeps 0 * -inf out of s1; exp is 0 there)
-            const float d = max_nan((float)r[i].v[j] - ms, -200.0f);
-            const float e = __builtin_amdgcn_exp2f(d * LOG2E);
-            s += e;
-            s1 = fmaf(e, d, s1);
-        }
+        for (int j = 0; j < VEC; ++j) add(entry<E>(r[i], j));
+    }
     s = wave_reduce(s, Add());
     s1 = wave_reduce(s1, Add());
     if (lane == 0) {
         red[1][wave] = s;
         red[2][wave] = s1;
     }
-    if constexpr (TOP) {
-        if (tid < 64) {   // the k-th largest of the 32 group maxima
-            const float g = group_max[tid & 31];
-            const uint64_t k = lp_rank(g, tid & 31);
-            int above = 0;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) above += lp_rank(group_max[i], i) > k;
-            if (tid < 32 && above == a.top - 1) bound = g;
-        }
-    }
     __syncthreads();
+    s = red[1][0];
+    s1 = red[2][0];
+#pragma unroll
+    for (int w = 1; w < LP_WAVES; ++w) {
+        s += red[1][w];
+        s1 += red[2][w];
+    }
     if (tid == 0) {
-        s = red[1][0];
-        s1 = red[2][0];
-        for (int w = 1; w < LP_WAVES; ++w) {
-            s += red[1][w];
-            s1 += red[2][w];
-        }
         if (a.parts == 1) {
             const int64_t t = a.target ? a.target[row] : -1;
             const bool asked = t >= 0 && t < a.V;
             lp_store(a, row, m, s, s1, asked ? (float)z[t] : 0.0f, asked);
-            red[0][0] = m == -INFINITY ? 0.0f : m + logf(s);
         } else {
             a.part[row * a.parts + p] = LpPart{m, s, s1, 0.0f};
         }
     }
     if constexpr (TOP) {
-        const float b = bound;
-        // (a thread whose own maximum is below the bound has no candidate; !(x < b)
-        // keeps NaN)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = lo + (i * LP_THREADS + tid) * VEC;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float v = (float)r[i].v[j];
-                if (!(v < b) && c + j < hi) {
-                    const int at = atomicAdd(&count, 1);
-                    if (at < LP_CAND) cand[at] = lp_rank(v, c + j);
-                }
-            }
-        }
-        __syncthreads();
-        const int n = count;
-        const float base = red[0][0];
+        const float base = m == -INFINITY ? 0.0f : m + logf(s);
         const int64_t part = row * a.parts + p;
         auto put = [&](int k, uint64_t v) {
             if (a.parts == 1) {
@@ -189,80 +173,133 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprob(LpArgs a) {
                 a.cand[part * a.top + k] = v;
             }
         };
-        if (n <= LP_CAND) {
-            // every slot of the list has its own rank, whatever order it was filled in
+        // Every entry of the list has its own rank, whatever order it was filled in.
+        auto rank = [&](int n) {
             for (int i = tid; i < n; i += LP_THREADS) {
                 const uint64_t v = cand[i];
                 int above = 0;
                 for (int k = 0; k < n; ++k) above += cand[k] > v;
                 if (above < a.top) put(above, v);
             }
+        };
+        const float b = bound;
+        // Lists the entries not below b (NaN among them); or, where those are too many,
+        // the ones above b alone: masked rows have thousands of -inf.
+        int ties = b == -INFINITY, n;
+        for (;;) {
+            auto below = [&](float v) { return v < b || (ties && v == b); };
+            auto offer = [&](float v, int c) {
+                if (below(v)) return;
+                const int at = atomicAdd(&count, 1);
+                if (at < LP_CAND) cand[at] = lp_rank(v, c);
+            };
+            if (left < hi) offer(extra, left);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                forget(r[i]);
+                float top = entry<E>(r[i], 0);
+#pragma unroll
+                for (int j = 1; j < VEC; ++j) top = max_nan(top, entry<E>(r[i], j));
+                const int v = i * LP_THREADS + tid;
+                if (below(top) || v >= whole) continue;
+                int c = lo + v * VEC;
+                asm volatile("" : "+v"(c));   // (computed here, not kept for every vector)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) offer(entry<E>(r[i], j), c + j);
+            }
+            __syncthreads();
+            n = count;
+            if (ties || n <= LP_CAND) break;
+            __syncthreads();
+            if (tid == 0) count = 0;
+            __syncthreads();
+            ties = 1;
+        }
+        if (n <= LP_CAND) {
+            // every entry of the list has its own rank, whatever order it was filled in
+            for (int i = tid; i < n; i += LP_THREADS) {
+                const uint64_t v = cand[i];
+                int above = 0;
+                for (int k = 0; k < n; ++k) above += cand[k] > v;
+                if (above < a.top) put(above, v);
+            }
+            // then the first entries equal to b, in the order of their indices
+            for (int c0 = lo; ties && n < a.top && c0 < hi; c0 += LP_THREADS) {
+                const bool is = c0 + tid < hi && (float)z[c0 + tid] == b;
+                const uint64_t mask = __ballot(is);
+                __syncthreads();
+                if (lane == 0) best[wave] = __popcll(mask);
+                __syncthreads();
+                int at = n + __popcll(mask & ((1ull << lane) - 1));
+                for (int w = 0; w < LP_WAVES; ++w) {
+                    if (w < wave) at += (int)best[w];
+                    n += (int)best[w];
+                }
+                if (is && at < a.top) put(at, lp_rank(b, c0 + tid));
+            }
             for (int k = n + tid; k < a.top; k += LP_THREADS) put(k, 0);   // (part shorter than top)
         } else {
-            // many equal logits (masked rows): the largest one, top times
-            auto own_best = [&](uint64_t below) {
-                uint64_t v = 0;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int c = lo + (i * LP_THREADS + tid) * VEC;
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const uint64_t k = lp_rank((float)r[i].v[j], c + j);
-                        if (c + j < hi && k < below && k > v) v = k;
+            // a row in an order that defeats the bound (one group of threads far below the
+            // others): the largest entry below the last one, top times
+            uint64_t mine = 0, v = ~0ull;
+            for (int k = 0; k < a.top; ++k) {
+                if (k == 0 || mine == v) {
+                    mine = 0;
+                    for (int c = lo + tid; c < hi; c += LP_THREADS) {
+                        const uint64_t o = lp_rank((float)z[c], c);
+                        if (o < v && o > mine) mine = o;
                     }
                 }
-                return v;
-            };
-            uint64_t mine = own_best(~0ull);
-            for (int k = 0; k < a.top; ++k) {
-                uint64_t v = wave_max_u64(mine);
+                v = wave_max_u64(mine);
                 if (lane == 0) best[wave] = v;
                 __syncthreads();
                 v = best[0];
                 for (int w = 1; w < LP_WAVES; ++w) v = best[w] > v ? best[w] : v;
                 __syncthreads();
                 if (tid == 0) put(k, v);
-                if (v != 0 && mine == v) mine = own_best(v);
             }
         }
     }
 }
 
 // One wave joins the parts of a row: lane l holds part l and the head of its sorted
-// candidates.
+// candidates, which wait in LDS.
 template <typename E>
 __global__ __launch_bounds__(64) void k_logprob_join(LpArgs a) {
+    __shared__ uint64_t lists[LP_PARTS * LP_TOP];
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
+    const uint64_t* const cand = a.cand + row * a.parts * a.top;
+    for (int i = lane; i < a.parts * a.top; i += 64) lists[i] = cand[i];
     LpPart q{-INFINITY, 0.0f, 0.0f, 0.0f};
-    const uint64_t* const mine = a.cand + (row * a.parts + lane) * a.top;
-    uint64_t head = 0;
-    if (lane < a.parts) {
-        q = a.part[row * a.parts + lane];
-        if (a.top) head = mine[0];
-    }
+    if (lane < a.parts) q = a.part[row * a.parts + lane];
+    const int64_t t = a.target ? a.target[row] : -1;
+    const bool asked = t >= 0 && t < a.V;
+    const float zt = asked ? (float)(static_cast<const E*>(a.z) + row * a.ld)[t] : 0.0f;
     const float m = wave_reduce(q.m, MaxNan());
     const float ms = m == -INFINITY ? 0.0f : m;
     const float d = max_nan(q.m - ms, -200.0f);
     const float e = __builtin_amdgcn_exp2f(d * LOG2E);
     const float s = wave_reduce(q.s * e, Add());
     const float s1 = wave_reduce(fmaf(d, q.s, q.s1) * e, Add());
-    if (lane == 0) {
-        const int64_t t = a.target ? a.target[row] : -1;
-        const bool asked = t >= 0 && t < a.V;
-        lp_store(a, row, m, s, s1,
-                 asked ? (float)(static_cast<const E*>(a.z) + row * a.ld)[t] : 0.0f, asked);
-    }
+    if (lane == 0) lp_store(a, row, m, s, s1, zt, asked);
+    if (a.top == 0) return;
     const float base = m == -INFINITY ? 0.0f : m + logf(s);
-    int at = 0;
+    __syncthreads();
+    int at = lane * a.top;
+    const int end = lane < a.parts ? at + a.top : at;
+    uint64_t head = at < end ? lists[at] : 0, mine = 0;
     for (int k = 0; k < a.top; ++k) {
         const uint64_t v = wave_max_u64(head);
+        if (lane == k) mine = v;
         if (v == head) {   // keys are distinct: one lane
-            a.top_index[row * a.top + k] = lp_index(v);
-            a.top_logprob[row * a.top + k] = lp_unkey((uint32_t)(v >> 32)) - base;
             ++at;
-            head = at < a.top ? mine[at] : 0;
+            head = at < end ? lists[at] : 0;
         }
+    }
+    if (lane < a.top) {
+        a.top_index[row * a.top + lane] = lp_index(mine);
+        a.top_logprob[row * a.top + lane] = lp_unkey((uint32_t)(mine >> 32)) - base;
     }
 }
 
@@ -281,21 +318,18 @@ constexpr int LPG_NV = 4;   // vectors a thread has in flight
 template <typename E, bool ENT>
 __global__ __launch_bounds__(256) void k_logprob_grad(LpGradArgs a) {
     constexpr int VEC = 16 / sizeof(E);
-    const int64_t row = (int64_t)blockIdx.x / a.pieces;
-    const int lo = (int)((int64_t)blockIdx.x % a.pieces) * (256 * LPG_NV * VEC);
+    const int64_t row = blockIdx.x / (uint32_t)a.pieces;
+    const int lo = (int)(blockIdx.x % (uint32_t)a.pieces) * (256 * LPG_NV * VEC);
     const E* const z = static_cast<const E*>(a.z) + row * a.ld;
     E* const out = static_cast<E*>(a.d) + row * a.ldd;
-    Pack<E, VEC> r[LPG_NV];
-    const int c0 = lo + (int)threadIdx.x * VEC;
+    // The piece's whole vectors; what is left of the row, less than one, goes one entry a
+    // thread of the last piece.
+    const int hi = min(a.V, lo + 256 * LPG_NV * VEC), whole = (hi - lo) / VEC;
+    u32x4 r[LPG_NV];
+    if (whole > 0) {
 #pragma unroll
-    for (int i = 0; i < LPG_NV; ++i) {
-        const int c = c0 + i * 256 * VEC;
-        if (c + VEC <= a.V) {
-            r[i] = load_pack<E, VEC>(z + c);
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) r[i].v[j] = c + j < a.V ? z[c + j] : (E)0.0f;
-        }
+        for (int i = 0; i < LPG_NV; ++i)
+            r[i] = load_words(z + lo + min(i * 256 + (int)threadIdx.x, whole - 1) * VEC);
     }
     float lse = a.lse[row];
     const bool empty = lse == -INFINITY;
@@ -305,28 +339,25 @@ __global__ __launch_bounds__(256) void k_logprob_grad(LpGradArgs a) {
     const int t = asked ? (int)t64 : -1;
     const float gl = asked && a.g_logprob ? a.g_logprob[row] : 0.0f;
     const float gh = ENT ? a.g_entropy[row] : 0.0f, H = ENT ? a.entropy[row] : 0.0f;
+    auto grad = [&](float x, int c) {
+        const float lp = x - lse;
+        const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
+        float g = gl;
+        if (ENT) g = fmaf(gh, max_nan(lp, -1e4f) + H, gl);   // (0 * -inf stays out)
+        const float v = -p * g;
+        return c == t ? v + gl : v;
+    };
 #pragma unroll
     for (int i = 0; i < LPG_NV; ++i) {
-        const int c = c0 + i * 256 * VEC;
+        const int v = i * 256 + (int)threadIdx.x;
+        if (v >= whole) break;
         Pack<E, VEC> o;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const float lp = (float)r[i].v[j] - lse;
-            const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
-            float g = gl;
-            if (ENT) g = fmaf(gh, max_nan(lp, -1e4f) + H, gl);   // (0 * -inf stays out)
-            float v = -p * g;
-            if (c + j == t) v += gl;
-            o.v[j] = (E)v;
-        }
-        if (c + VEC <= a.V) {
-            store_pack(out + c, o);
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (c + j < a.V) out[c + j] = o.v[j];
-        }
+        for (int j = 0; j < VEC; ++j) o.v[j] = (E)grad(entry<E>(r[i], j), lo + v * VEC + j);
+        store_pack(out + lo + v * VEC, o);
     }
+    const int left = lo + whole * VEC + (int)threadIdx.x;
+    if (left < hi) out[left] = (E)grad((float)z[left], left);
 }
 
 // Parts of a row: as long as the registers allow with many rows; with few, so many

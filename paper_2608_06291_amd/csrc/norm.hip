@@ -26,8 +26,8 @@ struct NormArgs {
 };
 
 // A row belongs to blockDim.x threads (one wave, with blockDim.y rows in the
-// workgroup, or the whole workgroup); thread t holds the vectors t, t + blockDim.x, ..
-// of VEC entries, NV of them.
+// workgroup, or the whole workgroup); thread t holds the whole vectors t, t + blockDim.x, ..
+// of VEC entries, NV of them, and one entry of what is left of the row.
 template <typename E, int NV>
 __global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
     constexpr int VEC = 16 / sizeof(E);
@@ -38,50 +38,59 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
     if (row >= a.T) return;   // (a whole wave, and never one of several in a row)
     const E* const x = static_cast<const E*>(a.x) + row * a.ldx;
     const E* const res = a.res ? static_cast<const E*>(a.res) + row * a.ldr : nullptr;
+    const int whole = a.d / VEC, left = whole * VEC + tid;
 
-    float h[NV][VEC];
-    float ssq = 0.0f;
+    // Vectors read at once: not so many that both operands wait in registers of their own.
+    constexpr int STEP = NV * VEC <= 32 ? NV : 32 / VEC;
+    constexpr bool EARLY = NV * VEC <= 16;   // the weights, too, before the first reduction
+    float h[NV][VEC], hx = 0.0f, ssq = 0.0f;
+    Pack<float, VEC> pw[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * tpr + tid) * VEC;
-        if (c + VEC <= a.d) {
-            const auto px = load_pack<E, VEC>(x + c);
+    for (int i0 = 0; i0 < NV; i0 += STEP) {
+        u32x4 rx[STEP], rr[STEP];
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) h[i][j] = (float)px.v[j];
+        for (int i = 0; i < STEP; ++i) rx[i] = rr[i] = u32x4(0);
+        if (whole > 0) {   // (past the row its last vector, not used)
+#pragma unroll
+            for (int i = 0; i < STEP; ++i)
+                rx[i] = load_words(x + min((i0 + i) * tpr + tid, whole - 1) * VEC);
             if (res) {
-                const auto pr = load_pack<E, VEC>(res + c);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) h[i][j] += (float)pr.v[j];
+                for (int i = 0; i < STEP; ++i)
+                    rr[i] = load_words(res + min((i0 + i) * tpr + tid, whole - 1) * VEC);
             }
-        } else {
+            if (EARLY && a.w) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    pw[i] = load_pack<float, VEC>(a.w + min(i * tpr + tid, whole - 1) * VEC);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+            const bool in = (i0 + i) * tpr + tid < whole;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                h[i][j] = 0.0f;
-                if (c + j < a.d) h[i][j] = (float)x[c + j] + (res ? (float)res[c + j] : 0.0f);
+                const float v = entry<E>(rx[i], j) + entry<E>(rr[i], j);
+                h[i0 + i][j] = in ? v : 0.0f;
+                ssq = fmaf(h[i0 + i][j], h[i0 + i][j], ssq);
             }
         }
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) ssq = fmaf(h[i][j], h[i][j], ssq);
-    if (a.sum) {
-        E* const out = static_cast<E*>(a.sum) + row * a.lds;
+    if (left < a.d) hx = (float)x[left] + (res ? (float)res[left] : 0.0f);
+    ssq = fmaf(hx, hx, ssq);
+    auto store = [&](void* base, int64_t ld) {   // h, rounded once
+        E* const out = static_cast<E*>(base) + row * ld;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * tpr + tid) * VEC;
-            if (c + VEC <= a.d) {
-                Pack<E, VEC> p;
+            const int v = i * tpr + tid;
+            Pack<E, VEC> p;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) p.v[j] = (E)h[i][j];
-                store_pack(out + c, p);
-            } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (c + j < a.d) out[c + j] = (E)h[i][j];
-            }
+            for (int j = 0; j < VEC; ++j) p.v[j] = (E)h[i][j];
+            if (v < whole) store_pack(out + v * VEC, p);
         }
-    }
+        if (left < a.d) out[left] = (E)hx;
+    };
+    if (a.sum) store(a.sum, a.lds);
     float r = 1.0f;
     if (a.normalise) {
         ssq = group_reduce(ssq, Add(), red[0], wave, lane, waves);
@@ -89,44 +98,22 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
         r = v == 0.0f ? 0.0f : 1.0f / sqrtf(v);
         if (!(v < INFINITY)) r = NAN;   // squares beyond fp32: not silently 0
     }
-    float top = 0.0f;
+    hx *= r;
+    if (a.w && left < a.d) hx *= a.w[left];
+    float top = fabsf(hx);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * tpr + tid) * VEC;
-        if (c + VEC <= a.d) {
-            if (a.w) {
-                const auto pw = load_pack<float, VEC>(a.w + c);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) h[i][j] = h[i][j] * r * pw.v[j];
-            } else {
+        for (int j = 0; j < VEC; ++j) h[i][j] *= r;
+        if (a.w && whole > 0) {
+            if (!EARLY) pw[i] = load_pack<float, VEC>(a.w + min(i * tpr + tid, whole - 1) * VEC);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) h[i][j] *= r;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (c + j < a.d) h[i][j] = h[i][j] * r * (a.w ? a.w[c + j] : 1.0f);
+            for (int j = 0; j < VEC; ++j) h[i][j] *= pw[i].v[j];
         }
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) top = max_nan(top, fabsf(h[i][j]));
+        for (int j = 0; j < VEC; ++j) top = max_nan(top, i * tpr + tid < whole ? fabsf(h[i][j]) : 0.0f);
     }
-    if (a.y) {
-        E* const out = static_cast<E*>(a.y) + row * a.ldy;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * tpr + tid) * VEC;
-            if (c + VEC <= a.d) {
-                Pack<E, VEC> p;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) p.v[j] = (E)h[i][j];
-                store_pack(out + c, p);
-            } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (c + j < a.d) out[c + j] = (E)h[i][j];
-            }
-        }
-    }
+    if (a.y) store(a.y, a.ldy);
     if (!a.q) return;
     top = group_reduce(top, MaxNan(), red[1], wave, lane, waves);
     const bool finite = top < INFINITY;
@@ -135,25 +122,22 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
     // y / s as a product where 1 / s exists, so a division only for rows below 2^-119
     const bool tiny = top < 1.5e-36f;
     const float inv = finite && !tiny ? 127.0f / top : 0.0f;
+    auto code = [&](float v) {
+        float c = v * inv;
+        if (tiny) c = s > 0.0f ? v / s : 0.0f;
+        return finite ? (int8_t)(int)rintf(c) : (int8_t)0;
+    };
     int8_t* const out = a.q + row * a.ldq;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * tpr + tid) * VEC;
+        const int v = i * tpr + tid;
         Pack<int8_t, VEC> p;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            float v = h[i][j] * inv;
-            if (tiny) v = s > 0.0f ? h[i][j] / s : 0.0f;
-            p.v[j] = finite && c + j < a.d ? (int8_t)(int)rintf(v) : (int8_t)0;
-        }
-        if (c + VEC <= a.dpad) {
-            store_pack(out + c, p);
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (c + j < a.dpad) out[c + j] = p.v[j];
-        }
+        for (int j = 0; j < VEC; ++j) p.v[j] = code(h[i][j]);
+        if (v < whole) store_pack(out + v * VEC, p);
     }
+    if (left < a.d) out[left] = code(hx);
+    for (int c = a.d + tid; c < a.dpad; c += tpr) out[c] = 0;
 }
 
 // Codes to packed rows: a thread writes 16 bytes (32 codes of 4 bits, 16 of 8).
@@ -182,8 +166,7 @@ __global__ __launch_bounds__(256) void k_pack(const int8_t* __restrict__ codes, 
 template <typename E>
 static void launch_norm(const NormArgs& a, hipStream_t st) {
     constexpr int VEC = 16 / sizeof(E);
-    // (the padding of q is written by the threads of the vectors past d)
-    const int vecs = (std::max(a.d, a.q ? a.dpad : 0) + VEC - 1) / VEC;
+    const int vecs = (a.d + VEC - 1) / VEC;
     constexpr int NV_MAX = 64 / VEC;
     // Threads a row: one vector a thread with few rows, where the latency of the
     // row counts; two with many.

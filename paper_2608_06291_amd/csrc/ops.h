@@ -3,6 +3,7 @@
 #pragma once
 #include <cmath>
 #include <cstdio>
+#include <type_traits>
 
 #include "bakron.h"
 #include "common.h"
@@ -29,23 +30,80 @@ __device__ inline void store_pack(E* p, const Pack<E, N>& r) {
     __builtin_memcpy(p, &r, sizeof(r));
 }
 
+// A 16-byte vector of E as four registers: whole until an entry is asked for, so that
+// neither a branch around a load nor a second use makes the compiler take it apart.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename E>
+__device__ inline u32x4 load_words(const E* p) {
+    u32x4 u;
+    __builtin_memcpy(&u, p, 16);
+    return u;
+}
+template <typename E>
+__device__ inline float entry(const u32x4& u, int j) {
+    if constexpr (sizeof(E) == 4) {
+        return __uint_as_float(u[j]);
+    } else if constexpr (std::is_same<E, bf16_t>::value) {
+        return __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
+    } else {
+        return (float)__builtin_bit_cast(f16_t, (uint16_t)(u[j >> 1] >> (16 * (j & 1))));
+    }
+}
+// -infinity in every entry.
+template <typename E>
+__device__ inline uint32_t minus_infinity() {
+    return sizeof(E) == 4 ? 0xff800000u : std::is_same<E, bf16_t>::value ? 0xff80ff80u : 0xfc00fc00u;
+}
+// Makes the compiler forget what it knows of a vector, so that values derived from it
+// (its entries in fp32, twice the registers) are not kept from one use to the next.
+__device__ inline void forget(u32x4& u) {
+    asm volatile("" : "+v"(u));
+}
+
 // max that keeps a NaN from either side (v_maximum3_f32).
 __device__ inline float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 struct MaxNan {
     __device__ float operator()(float a, float b) const { return max_nan(a, b); }
 };
+struct MaxU32 {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
+};
 struct Add {
     __device__ float operator()(float a, float b) const { return a + b; }
 };
 
-// Butterfly over the wave: every lane has the result, in an order that does
-// not depend on the lane.
-template <typename Op>
-__device__ inline float wave_reduce(float v, Op op) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v = op(v, __shfl_xor(v, off, 64));
-    return v;
+// The value that a lane permutation inside rows of 16 lanes (a DPP control) brings.
+template <int CTRL>
+__device__ inline uint32_t dpp(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+}
+template <int CTRL>
+__device__ inline float dpp(float v) {
+    return __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
+}
+constexpr int DPP_XOR1 = 0xb1, DPP_XOR2 = 0x4e, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
+
+// Over the 16 lanes of a row, every lane having the result: neighbours, then (all of a
+// quad, of an eight being equal) mirrored.  One operation a step, no trip through LDS.
+template <typename V, typename Op>
+__device__ inline V row_reduce(V v, Op op) {
+    v = op(v, dpp<DPP_XOR1>(v));
+    v = op(v, dpp<DPP_XOR2>(v));
+    v = op(v, dpp<DPP_HALF_MIRROR>(v));
+    return op(v, dpp<DPP_MIRROR>(v));
+}
+__device__ inline float lane_value(float v, int lane) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane));
+}
+__device__ inline uint32_t lane_value(uint32_t v, int lane) {
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+// Over the wave, in a fixed order.  All lanes have to be active.
+template <typename V, typename Op>
+__device__ inline V wave_reduce(V v, Op op) {
+    v = row_reduce(v, op);
+    return op(op(lane_value(v, 0), lane_value(v, 16)), op(lane_value(v, 32), lane_value(v, 48)));
 }
 
 // Over `waves` waves of a workgroup; `red` holds one float a wave and may be used

@@ -548,6 +548,26 @@ def test_token_logprobs_ties(dtype, V):
     assert abs(float(r.entropy[0]) - math.log(V)) < 1e-4
 
 
+def test_token_logprobs_uneven_rows():
+    """Rows whose large logits sit together, so that a bound from a few places of the row
+    is far below the largest ones: rising, falling, one block low."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("logprob uneven")
+    V = 32768
+    z = torch.rand((5, V), generator=_gen(1)).float()
+    z[0] = z[0].sort().values
+    z[1] = z[1].sort(descending=True).values
+    z[2].view(-1, 4096)[:, :128] -= 50          # what 16 neighbouring threads hold
+    z[3].view(-1, 2048)[:, 64:128] -= 50
+    z[4, :30000] = -math.inf
+    for dt in (torch.float32, torch.float16):
+        y = z.to(dt)
+        r = pk.token_logprobs(y.to("cuda:0"), None, top=32)
+        idx = _logprob64(y, torch.zeros(5, dtype=torch.int64), 32)[3]
+        assert torch.equal(r.top_index.cpu(), idx), dt
+
+
 @pytest.mark.parametrize("V", [300, 70000])
 def test_token_logprobs_non_finite(V):
     import paper_2608_06291_amd as pk
