@@ -606,21 +606,33 @@ def _vector(t, name, n, dtype, device):
     return t.data_ptr()
 
 
-def _run_op(fn, args, device, work=None):
-    """Call a workspace-protocol operator; allocates its workspace unless given."""
+def _raw_stream(device):
+    """The current stream's handle (no Stream object: small calls are bound by the host)."""
     import torch
-    st = torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+_work_sizes = {}
+
+
+def _run_op(fn, args, device, work=None, key=None):
+    """Call a workspace-protocol operator; allocates its workspace unless given.  `key`
+    holds everything its size depends on, so that it is asked for once."""
+    import torch
+    st = _raw_stream(device)
     if work is None:
-        need = ctypes.c_size_t(0)
-        _raise_last(fn(*args, None, ctypes.byref(need), st))
-        if need.value == 0:
-            work_ptr = 256   # not read
-        else:
-            work = torch.empty(need.value, dtype=torch.uint8, device=device)
-    if work is not None:
-        need = ctypes.c_size_t(work.numel() * work.element_size())
-        work_ptr = work.data_ptr()
-    _raise_last(fn(*args, work_ptr, ctypes.byref(need), st))
+        need = _work_sizes.get(key) if key is not None else None
+        if need is None:
+            size = ctypes.c_size_t(0)
+            if key is None and fn(*args, 256, ctypes.byref(size), st) == BAKRON_OK:
+                return   # needs none
+            _raise_last(fn(*args, None, ctypes.byref(size), st))
+            need = size.value
+            if key is not None:
+                _work_sizes[key] = need
+        work = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+    size = ctypes.c_size_t(work.numel() * work.element_size())
+    _raise_last(fn(*args, work.data_ptr(), ctypes.byref(size), st))
 
 
 class NormQuant(NamedTuple):
@@ -668,7 +680,7 @@ def rmsnorm_quant(x, weight=None, residual=None, eps: float = 1e-5, normalise: b
             q = q[:, :d]
     _raise_last(lib.bakron_rmsnorm_quant(
         xp, ldx, rp, ldr, code, T, d, wp, float(eps), 1 if normalise else 0, sp, lds, yp, ldy, qp, ldq,
-        cp, torch.cuda.current_stream(dev).cuda_stream))
+        cp, _raw_stream(dev)))
     return NormQuant(q, scale, hs, ys)
 
 
@@ -691,7 +703,7 @@ def pack_codes(codes, width: int = 4) -> PackedCodes:
     padded = -(-n // PACK_COLUMNS) * PACK_COLUMNS
     data = torch.empty((m, padded * int(width) // 8), dtype=torch.uint8, device=codes.device)
     _raise_last(load().bakron_pack_codes(codes.data_ptr(), m, n, int(width), data.data_ptr(),
-                                         torch.cuda.current_stream(codes.device).cuda_stream))
+                                         _raw_stream(codes.device)))
     return PackedCodes(data, n, int(width))
 
 
@@ -821,7 +833,8 @@ def token_logprobs(logits, target=None, top: int = 0, work=None) -> TokenLogprob
     _run_op(lib.bakron_token_logprobs,
             (zp, ld, _dtype_code(logits.dtype), T, V, tp, top, None if tp is None else logprob.data_ptr(),
              entropy.data_ptr(), lse.data_ptr(), None if tl is None else tl.data_ptr(),
-             None if ti is None else ti.data_ptr()), dev, work)
+             None if ti is None else ti.data_ptr()), dev, work,
+            ("token_logprobs", T, V, top, logits.dtype))
     return TokenLogprobs(None if tp is None else logprob, entropy, lse, tl, ti)
 
 
@@ -842,5 +855,5 @@ def token_logprobs_backward(logits, target, lse, entropy=None, g_logprob=None, g
         zp, ld, _dtype_code(logits.dtype), T, V, _vector(target, "target", T, torch.int64, dev),
         _vector(lse, "lse", T, f32, dev), _vector(entropy, "entropy", T, f32, dev),
         _vector(g_logprob, "g_logprob", T, f32, dev), _vector(g_entropy, "g_entropy", T, f32, dev), dp,
-        ldd, torch.cuda.current_stream(dev).cuda_stream))
+        ldd, _raw_stream(dev)))
     return out

@@ -45,61 +45,70 @@ __device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, f
     store4(static_cast<E*>(a.y) + t * a.ldy + i, z, valid);
 }
 
-template <typename M, bool GROUPED, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_linear(LinearArgs a) {
-    typedef Tile<M, BM, BN, WM, WN> Tl;
+template <typename Tl, bool GROUPED>
+__global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
+    typedef typename Tl::Mma M;
     __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
     int ti, tt;
     tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
-    const int64_t i0 = (int64_t)ti * BM, t0 = (int64_t)tt * BN;
+    const int64_t i0 = (int64_t)ti * Tl::ROWS, t0 = (int64_t)tt * Tl::COLS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = wave / WN, wn = wave % WN;
-    const int r4 = (lane >> 4) * 4;
-    constexpr int X = Tl::X, Y = Tl::Y;
+    const int64_t iw = i0 + Tl::a0(wave) + (lane >> 4) * 4, tw = t0 + Tl::b0(wave) + (lane & 15);
     constexpr float UNIT = M::A_BYTES == CHUNK_BYTES ? 1.0f : 1.0f / 16.0f;
 
-    i32x4 acc[X][Y] = {};
-    f32x4 sum[GROUPED ? X : 1][GROUPED ? Y : 1] = {};
-    const int last = 2 * a.chunks - 1;
-    int left = a.gsteps, g = 0;
-    auto after = [&](int step, i32x4 (&acc)[X][Y]) {
-        if constexpr (GROUPED) {
+    typename Tl::Accs acc = {};
+    f32x4 sum[GROUPED ? Tl::UA : 1][GROUPED ? Tl::UB : 1] = {};
+    const int64_t end_w = a.ldw, end_q = (int64_t)a.chunks * CHUNK_BYTES;
+    const char* const q = reinterpret_cast<const char*>(a.q);
+    if constexpr (GROUPED) {
+        const int last = 2 * a.chunks - 1;
+        int left = a.gsteps, g = 0;
+        auto after = [&](int step, typename Tl::Accs& acc) {
             if (--left > 0 && step != last) return;
             left = a.gsteps;
             if (g < a.ngroups) {   // (past them only padding, whose sums are 0)
 #pragma unroll
-                for (int x = 0; x < X; ++x) {
+                for (int x = 0; x < Tl::UA; ++x) {
                     f32x4 s;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int64_t i = min(i0 + wm * Tl::TM + x * 16 + r4 + j, a.m - 1);
-                        s[j] = a.scale[i * a.ngroups + g];
+                    for (int j = 0; j < 4; ++j)
+                        s[j] = a.scale[min(iw + x * 16 + j, a.m - 1) * a.ngroups + g];
+#pragma unroll
+                    for (int y = 0; y < Tl::UB; ++y) {
+                        i32x4& p = Tl::at(acc, x, y);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            sum[x][y][j] = fmaf((float)p[j], s[j], sum[x][y][j]);
+                        p = i32x4{0, 0, 0, 0};
                     }
-#pragma unroll
-                    for (int y = 0; y < Y; ++y)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            sum[x][y][j] = fmaf((float)acc[x][y][j], s[j], sum[x][y][j]);
-                            acc[x][y][j] = 0;
-                        }
                 }
             }
             ++g;
-        }
-    };
-    Tl::run(
-        lds, [&](int r) { return a.w + min(i0 + r, a.m - 1) * a.ldw; },
-        [&](int r) { return reinterpret_cast<const char*>(a.q) + min(t0 + r, a.T - 1) * a.ldq; },
-        a.ldw, (int64_t)a.chunks * CHUNK_BYTES, a.chunks, acc, after);
+        };
+        Tl::run(
+            lds, [&](int r) { return a.w + min(i0 + r, a.m - 1) * a.ldw; },
+            [&](int r) { return q + min(t0 + r, a.T - 1) * a.ldq; }, end_w, end_q, a.chunks, acc, after);
+    } else if constexpr (Tl::THREADS == 512) {
+        Tl::run(
+            lds, a.w + i0 * a.ldw, q + t0 * a.ldq,
+            [&](int r) { return (uint32_t)(min((int64_t)r, a.m - 1 - i0) * a.ldw); },
+            [&](int r) { return (uint32_t)(min((int64_t)r, a.T - 1 - t0) * a.ldq); }, end_w, end_q,
+            a.chunks, acc, [](int, typename Tl::Accs&) {});
+    } else {
+        Tl::run(
+            lds, [&](int r) { return a.w + min(i0 + r, a.m - 1) * a.ldw; },
+            [&](int r) { return q + min(t0 + r, a.T - 1) * a.ldq; }, end_w, end_q, a.chunks, acc,
+            [](int, typename Tl::Accs&) {});
+    }
 
 #pragma unroll
-    for (int y = 0; y < Y; ++y) {
-        const int64_t t = t0 + wn * Tl::TN + y * 16 + (lane & 15);
+    for (int y = 0; y < Tl::UB; ++y) {
+        const int64_t t = tw + y * 16;
         if (t >= a.T) continue;
         const float qs = (a.q_scale ? a.q_scale[t] : 1.0f) * UNIT;
 #pragma unroll
-        for (int x = 0; x < X; ++x) {
-            const int64_t i = i0 + wm * Tl::TM + x * 16 + r4;
+        for (int x = 0; x < Tl::UA; ++x) {
+            const int64_t i = iw + x * 16;
             if (i >= a.m) continue;
             float z[4];
             if constexpr (GROUPED) {
@@ -109,7 +118,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear(LinearArgs a) {
                 float s[4];
                 load4(a.scale + i, s, a.m - i);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) z[j] = (float)acc[x][y][j] * (qs * s[j]);
+                for (int j = 0; j < 4; ++j) z[j] = (float)Tl::at(acc, x, y)[j] * (qs * s[j]);
             }
             if (a.dtype == BAKRON_F32)
                 linear_store<float>(a, t, i, z);
@@ -121,12 +130,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear(LinearArgs a) {
     }
 }
 
-template <typename M, bool GROUPED, int BM, int BN, int WM, int WN>
+template <typename Tl, bool GROUPED>
 static void launch_linear_tile(LinearArgs a, hipStream_t st) {
-    a.ni = (int)((a.m + BM - 1) / BM);
-    a.nt = (int)((a.T + BN - 1) / BN);
-    hipLaunchKernelGGL((k_linear<M, GROUPED, BM, BN, WM, WN>), dim3((unsigned)(a.ni * a.nt)),
-                       dim3(64 * WM * WN), 0, st, a);
+    a.ni = (int)((a.m + Tl::ROWS - 1) / Tl::ROWS);
+    a.nt = (int)((a.T + Tl::COLS - 1) / Tl::COLS);
+    hipLaunchKernelGGL((k_linear<Tl, GROUPED>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
 }
 
 template <typename M, bool GROUPED>
@@ -134,10 +142,10 @@ static void launch_linear(const LinearArgs& a, hipStream_t st) {
     auto tiles = [&](int64_t b) { return ((a.m + b - 1) / b) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
     if constexpr (!GROUPED) {
-        if (tiles(256) >= ncu) return launch_linear_tile<M, GROUPED, 256, 256, 2, 4>(a, st);
+        if (tiles(256) >= ncu && a.ldq < TILE_LD_MAX) return launch_linear_tile<BigTile<M>, GROUPED>(a, st);
     }
-    if (tiles(128) >= ncu) return launch_linear_tile<M, GROUPED, 128, 128, 2, 2>(a, st);
-    launch_linear_tile<M, GROUPED, 64, 64, 2, 2>(a, st);
+    if (tiles(128) >= ncu) return launch_linear_tile<Tile<M, 128, 128, 2, 2>, GROUPED>(a, st);
+    launch_linear_tile<Tile<M, 64, 64, 2, 2>, GROUPED>(a, st);
 }
 
 }  // namespace bk

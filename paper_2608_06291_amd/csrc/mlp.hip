@@ -29,35 +29,43 @@ struct GatedArgs {
     int64_t fp, Tp;
 };
 
-template <typename M, bool BWD, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_gated(GatedArgs a) {
-    typedef Tile<M, BM, BN, WM, WN> Tl;
-    typedef typename M::Elem E;
+template <typename Tl, bool BWD>
+__global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
+    typedef typename Tl::Mma::Elem E;
     __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
     int ti, tt;
     tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
-    const int64_t f0 = (int64_t)ti * (BM / 2), t0 = (int64_t)tt * BN;
+    const int64_t f0 = (int64_t)ti * (Tl::ROWS / 2), t0 = (int64_t)tt * Tl::COLS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = wave / WN, wn = wave % WN;
-    constexpr int X = Tl::X, Y = Tl::Y;
-    static_assert(X % 2 == 0, "gate and up rows in one wave");
+    static_assert(Tl::UA % 2 == 0, "gate and up rows in one wave");
 
-    f32x4 acc[X][Y] = {};
-    Tl::run(
-        lds,
-        [&](int r) {
-            const int64_t j = min(f0 + (r >> 5) * 16 + (r & 15), a.f - 1);
-            return ((r >> 4) & 1 ? a.wu : a.wg) + j * a.ldw;
-        },
-        [&](int r) { return a.x + min(t0 + r, a.T - 1) * a.ldx; }, a.kbytes, a.kbytes, a.chunks, acc,
-        [](int, f32x4 (&)[X][Y]) {});
+    typename Tl::Accs acc = {};
+    auto none = [](int, typename Tl::Accs&) {};
+    auto feature = [](int r) { return (int64_t)((r >> 5) * 16 + (r & 15)); };   // of tile row r
+    if constexpr (Tl::THREADS == 512) {
+        // (the rows that a wave loads are all of one matrix)
+        const int w = __builtin_amdgcn_readfirstlane(wave);
+        const bool up = (Tl::load_row_a(0, 0, w) >> 4) & 1;
+        Tl::run(
+            lds, (up ? a.wu : a.wg) + f0 * a.ldw, a.x + t0 * a.ldx,
+            [&](int r) { return (uint32_t)(min(feature(r), a.f - 1 - f0) * a.ldw); },
+            [&](int r) { return (uint32_t)(min((int64_t)r, a.T - 1 - t0) * a.ldx); }, a.kbytes, a.kbytes,
+            a.chunks, acc, none);
+    } else {
+        Tl::run(
+            lds,
+            [&](int r) { return ((r >> 4) & 1 ? a.wu : a.wg) + min(f0 + feature(r), a.f - 1) * a.ldw; },
+            [&](int r) { return a.x + min(t0 + r, a.T - 1) * a.ldx; }, a.kbytes, a.kbytes, a.chunks, acc,
+            none);
+    }
 
 #pragma unroll
-    for (int y = 0; y < Y; ++y) {
-        const int64_t t = t0 + wn * Tl::TN + y * 16 + (lane & 15);
+    for (int y = 0; y < Tl::UB; ++y) {
+        const int64_t t = t0 + Tl::b0(wave) + y * 16 + (lane & 15);
 #pragma unroll
-        for (int x = 0; x < X; x += 2) {
-            const int64_t j = f0 + (wm * Tl::TM + x * 16) / 2 + (lane >> 4) * 4;
+        for (int x = 0; x < Tl::UA; x += 2) {
+            const f32x4 G = Tl::at(acc, x, y), U = Tl::at(acc, x + 1, y);
+            const int64_t j = f0 + (Tl::a0(wave) + x * 16) / 2 + (lane >> 4) * 4;
             const int64_t valid = a.f - j;
             if constexpr (!BWD) {
                 if (t >= a.T || valid <= 0) continue;
@@ -65,18 +73,18 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gated(GatedArgs a) {
                 if (a.feat_gate) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        act_both(acc[x][y][r], a.act, &v[r], &s[r]);
-                        s[r] *= acc[x + 1][y][r];
+                        act_both(G[r], a.act, &v[r], &s[r]);
+                        s[r] *= U[r];
                     }
                     store4(a.feat_gate + t * a.f + j, s, valid);
                 } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = act_value(acc[x][y][r], a.act);
+                    for (int r = 0; r < 4; ++r) v[r] = act_value(G[r], a.act);
                 }
                 if (a.feat_up) store4(a.feat_up + t * a.f + j, v, valid);
                 if (a.h) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) h[r] = v[r] * acc[x + 1][y][r];
+                    for (int r = 0; r < 4; ++r) h[r] = v[r] * U[r];
                     store4(static_cast<E*>(a.h) + t * a.ldh + j, h, valid);
                 }
             } else {
@@ -89,9 +97,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gated(GatedArgs a) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         float v, s;
-                        act_both(acc[x][y][r], a.act, &v, &s);
+                        act_both(G[r], a.act, &v, &s);
                         if (r < valid) {
-                            dg[r] = dh[r] * acc[x + 1][y][r] * s;
+                            dg[r] = dh[r] * U[r] * s;
                             du[r] = dh[r] * v;
                         }
                     }
@@ -123,35 +131,40 @@ struct ProdArgs {
     int64_t ldo, split, split2;
 };
 
-template <typename M, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_prod(ProdArgs a) {
-    typedef Tile<M, BM, BN, WM, WN> Tl;
-    typedef typename M::Elem E;
+template <typename Tl>
+__global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
+    typedef typename Tl::Mma::Elem E;
     __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
     int ti, tt;
     tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
-    const int64_t i0 = (int64_t)ti * BM, t0 = (int64_t)tt * BN;
+    const int64_t i0 = (int64_t)ti * Tl::ROWS, t0 = (int64_t)tt * Tl::COLS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = wave / WN, wn = wave % WN;
-    constexpr int X = Tl::X, Y = Tl::Y;
 
-    f32x4 acc[X][Y] = {};
-    Tl::run(
-        lds, [&](int r) { return a.a + min(i0 + r, a.ni_rows - 1) * a.lda; },
-        [&](int r) { return a.b + min(t0 + r, a.nt_rows - 1) * a.ldb; }, a.kbytes, a.kbytes, a.chunks,
-        acc, [](int, f32x4 (&)[X][Y]) {});
+    typename Tl::Accs acc = {};
+    auto none = [](int, typename Tl::Accs&) {};
+    if constexpr (Tl::THREADS == 512)
+        Tl::run(
+            lds, a.a + i0 * a.lda, a.b + t0 * a.ldb,
+            [&](int r) { return (uint32_t)(min((int64_t)r, a.ni_rows - 1 - i0) * a.lda); },
+            [&](int r) { return (uint32_t)(min((int64_t)r, a.nt_rows - 1 - t0) * a.ldb); }, a.kbytes,
+            a.kbytes, a.chunks, acc, none);
+    else
+        Tl::run(
+            lds, [&](int r) { return a.a + min(i0 + r, a.ni_rows - 1) * a.lda; },
+            [&](int r) { return a.b + min(t0 + r, a.nt_rows - 1) * a.ldb; }, a.kbytes, a.kbytes,
+            a.chunks, acc, none);
 #pragma unroll
-    for (int y = 0; y < Y; ++y) {
-        const int64_t t = t0 + wn * Tl::TN + y * 16 + (lane & 15);
+    for (int y = 0; y < Tl::UB; ++y) {
+        const int64_t t = t0 + Tl::b0(wave) + y * 16 + (lane & 15);
         if (t >= a.nt_rows || (t >= a.split && t < a.split2)) continue;
         E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
                                    : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
 #pragma unroll
-        for (int x = 0; x < X; ++x) {
-            const int64_t i = i0 + wm * Tl::TM + x * 16 + (lane >> 4) * 4;
+        for (int x = 0; x < Tl::UA; ++x) {
+            const int64_t i = i0 + Tl::a0(wave) + x * 16 + (lane >> 4) * 4;
             float v[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = acc[x][y][r];
+            for (int r = 0; r < 4; ++r) v[r] = Tl::at(acc, x, y)[r];
             if (i < a.ni_rows) store4(row + i, v, a.ni_rows - i);
         }
     }
@@ -212,38 +225,38 @@ static bool direct_rows(const void* p, int64_t ld, int64_t cols) {
 
 template <typename M, bool BWD>
 static void launch_gated(GatedArgs a, hipStream_t st) {
-    auto tiles = [&](int64_t bm, int64_t bn) {
-        return ((a.f + bm / 2 - 1) / (bm / 2)) * ((a.T + bn - 1) / bn);
-    };
+    auto tiles = [&](int64_t b) { return ((a.f + b / 2 - 1) / (b / 2)) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
-    auto go = [&](auto kernel, int bm, int bn, int threads) {
-        a.ni = (int)((a.f + bm / 2 - 1) / (bm / 2));
-        a.nt = (int)((a.T + bn - 1) / bn);
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.ni * a.nt)), dim3(threads), 0, st, a);
+    auto go = [&](auto tile) {
+        typedef decltype(tile) Tl;
+        a.ni = (int)((a.f + Tl::ROWS / 2 - 1) / (Tl::ROWS / 2));
+        a.nt = (int)((a.T + Tl::COLS - 1) / Tl::COLS);
+        hipLaunchKernelGGL((k_gated<Tl, BWD>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
     };
-    if (tiles(256, 256) >= ncu)
-        go(k_gated<M, BWD, 256, 256, 2, 4>, 256, 256, 512);
-    else if (tiles(128, 128) >= ncu)
-        go(k_gated<M, BWD, 128, 128, 2, 2>, 128, 128, 256);
+    if (tiles(256) >= ncu && std::max(a.ldx, a.ldw) < TILE_LD_MAX)
+        go(BigTile<M>());
+    else if (tiles(128) >= ncu)
+        go(Tile<M, 128, 128, 2, 2>());
     else
-        go(k_gated<M, BWD, 64, 64, 2, 2>, 64, 64, 256);
+        go(Tile<M, 64, 64, 2, 2>());
 }
 
 template <typename M>
 static void launch_prod(ProdArgs a, hipStream_t st) {
     auto tiles = [&](int64_t b) { return ((a.ni_rows + b - 1) / b) * ((a.nt_rows + b - 1) / b); };
     const int ncu = op_cus();
-    auto go = [&](auto kernel, int b, int threads) {
-        a.ni = (int)((a.ni_rows + b - 1) / b);
-        a.nt = (int)((a.nt_rows + b - 1) / b);
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.ni * a.nt)), dim3(threads), 0, st, a);
+    auto go = [&](auto tile) {
+        typedef decltype(tile) Tl;
+        a.ni = (int)((a.ni_rows + Tl::ROWS - 1) / Tl::ROWS);
+        a.nt = (int)((a.nt_rows + Tl::COLS - 1) / Tl::COLS);
+        hipLaunchKernelGGL((k_prod<Tl>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
     };
-    if (tiles(256) >= ncu)
-        go(k_prod<M, 256, 256, 2, 4>, 256, 512);
+    if (tiles(256) >= ncu && std::max(a.lda, a.ldb) < TILE_LD_MAX)
+        go(BigTile<M>());
     else if (tiles(128) >= ncu)
-        go(k_prod<M, 128, 128, 2, 2>, 128, 256);
+        go(Tile<M, 128, 128, 2, 2>());
     else
-        go(k_prod<M, 64, 64, 2, 2>, 64, 256);
+        go(Tile<M, 64, 64, 2, 2>());
 }
 
 // Padded copies of operands that cannot be staged as they are.

@@ -346,7 +346,8 @@ def _mlp_errors(x, wg, wu, act):
 
 
 MLP = [(1, 1, 1), (1, 64, 32), (1, 1000, 333), (2, 8, 100), (5, 130, 257), (16, 512, 512), (17, 72, 40),
-       (64, 264, 130), (129, 200, 1000), (257, 1000, 270), (700, 96, 1500), (2100, 40, 2200)]
+       (64, 264, 130), (129, 200, 1000), (257, 1000, 270), (700, 96, 1500), (2100, 40, 2200),
+       (4100, 40, 2200), (40, 4100, 2200), (4200, 4104, 70)]
 
 
 @pytest.mark.parametrize("T,d,f", MLP)
