@@ -581,7 +581,7 @@ bakron_status bakron_pack_codes(const int8_t *codes, int64_t m, int64_t n, int32
  * The products of 8-bit values are summed exactly, over the row or the group.
  *   q         device, T x n int8 in [-127, 127] (-128 is accepted for
  *             n <= 65536), as bakron_rmsnorm_quant writes it: ldq >= n rounded up to
- *             BAKRON_PACK_COLUMNS, a multiple of 16, q 16-byte aligned; the
+ *             BAKRON_PACK_COLUMNS, a multiple of 16 below 2^23, q 16-byte aligned; the
  *             padding columns are read (and count for nothing)
  *   q_scale   device, T floats, or NULL for 1
  *   packed    from bakron_pack_codes with this n, m and width

@@ -23,26 +23,26 @@ struct LinearArgs {
     int ni, nt;              // tiles
 };
 
-// y_t,i..i+3 from the four sums z (scales applied).
+// y_t,i..i+7 from the sums z (scales applied) and the bias.
 template <typename E>
-__device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, float (&z)[4]) {
+__device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, float (&z)[8]) {
     const int64_t valid = a.m - i;
-    float v[4];
+    float v[8];
     if (a.bias) {
-        load4(static_cast<const E*>(a.bias) + i, v, valid);
+        load8(static_cast<const E*>(a.bias) + i, v, valid);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] += v[j];
+        for (int j = 0; j < 8; ++j) z[j] += v[j];
     }
     if (a.act != BAKRON_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = act_value(z[j], a.act);
+        for (int j = 0; j < 8; ++j) z[j] = act_value(z[j], a.act);
     }
     if (a.combine != BAKRON_COMBINE_NONE) {
-        load4(static_cast<const E*>(a.other) + t * a.ldo + i, v, valid);
+        load8(static_cast<const E*>(a.other) + t * a.ldo + i, v, valid);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = a.combine == BAKRON_COMBINE_ADD ? z[j] + v[j] : z[j] * v[j];
+        for (int j = 0; j < 8; ++j) z[j] = a.combine == BAKRON_COMBINE_ADD ? z[j] + v[j] : z[j] * v[j];
     }
-    store4(static_cast<E*>(a.y) + t * a.ldy + i, z, valid);
+    store8(static_cast<E*>(a.y) + t * a.ldy + i, z, valid);
 }
 
 template <typename Tl, bool GROUPED>
@@ -53,14 +53,16 @@ __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
     tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
     const int64_t i0 = (int64_t)ti * Tl::ROWS, t0 = (int64_t)tt * Tl::COLS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t iw = i0 + Tl::a0(wave) + (lane >> 4) * 4, tw = t0 + Tl::b0(wave) + (lane & 15);
     constexpr float UNIT = M::A_BYTES == CHUNK_BYTES ? 1.0f : 1.0f / 16.0f;
 
     typename Tl::Accs acc = {};
     f32x4 sum[GROUPED ? Tl::UA : 1][GROUPED ? Tl::UB : 1] = {};
-    const int64_t end_w = a.ldw, end_q = (int64_t)a.chunks * CHUNK_BYTES;
-    const char* const q = reinterpret_cast<const char*>(a.q);
+    const Operand w{a.w, nullptr, a.ldw, a.m, a.ldw, 0};
+    const Operand q{reinterpret_cast<const char*>(a.q), nullptr, a.ldq, a.T,
+                    (int64_t)a.chunks * CHUNK_BYTES, 0};
+    auto same = [](int r) { return r; };
     if constexpr (GROUPED) {
+        const int64_t iw = i0 + Tl::a0(wave) + (lane >> 4) * 4;
         const int last = 2 * a.chunks - 1;
         int left = a.gsteps, g = 0;
         auto after = [&](int step, typename Tl::Accs& acc) {
@@ -85,41 +87,39 @@ __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
             }
             ++g;
         };
-        Tl::run(
-            lds, [&](int r) { return a.w + min(i0 + r, a.m - 1) * a.ldw; },
-            [&](int r) { return q + min(t0 + r, a.T - 1) * a.ldq; }, end_w, end_q, a.chunks, acc, after);
+        Tl::run(lds, w, i0, q, t0, a.chunks, acc, same, after);
     } else if constexpr (Tl::THREADS == 512) {
-        Tl::run(
-            lds, a.w + i0 * a.ldw, q + t0 * a.ldq,
-            [&](int r) { return (uint32_t)(min((int64_t)r, a.m - 1 - i0) * a.ldw); },
-            [&](int r) { return (uint32_t)(min((int64_t)r, a.T - 1 - t0) * a.ldq); }, end_w, end_q,
-            a.chunks, acc, [](int, typename Tl::Accs&) {});
+        Tl::run(lds, w, i0, q, t0, a.chunks, acc, same);
     } else {
-        Tl::run(
-            lds, [&](int r) { return a.w + min(i0 + r, a.m - 1) * a.ldw; },
-            [&](int r) { return q + min(t0 + r, a.T - 1) * a.ldq; }, end_w, end_q, a.chunks, acc,
-            [](int, typename Tl::Accs&) {});
+        Tl::run(lds, w, i0, q, t0, a.chunks, acc, same, [](int, typename Tl::Accs&) {});
     }
 
+    auto get = [&](int x, int y) {
+        if constexpr (GROUPED) {
+            return sum[x][y];
+        } else {
+            const i32x4 p = Tl::at(acc, x, y);
+            return f32x4{(float)p[0], (float)p[1], (float)p[2], (float)p[3]};
+        }
+    };
+    const auto rows = handover<Tl>(lds, wave, lane, get);
+    constexpr int PER = Tl::UA * 2;   // lanes a row
+    const int p = lane % PER;
+    const int64_t i = i0 + Tl::a0(wave) + p * 8;
+    float s[8];
+    if (!GROUPED) load8(a.scale + min(i, a.m), s, a.m - i);
 #pragma unroll
     for (int y = 0; y < Tl::UB; ++y) {
-        const int64_t t = tw + y * 16;
-        if (t >= a.T) continue;
-        const float qs = (a.q_scale ? a.q_scale[t] : 1.0f) * UNIT;
+        rows.put(y);
 #pragma unroll
-        for (int x = 0; x < Tl::UA; ++x) {
-            const int64_t i = iw + x * 16;
-            if (i >= a.m) continue;
-            float z[4];
-            if constexpr (GROUPED) {
+        for (int tl = lane / PER; tl < 16; tl += 64 / PER) {
+            const int64_t t = t0 + Tl::b0(wave) + y * 16 + tl;
+            float z[8];
+            rows.take(tl, p, z);
+            if (t >= a.T || i >= a.m) continue;
+            const float qs = (a.q_scale ? a.q_scale[t] : 1.0f) * UNIT;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) z[j] = sum[x][y][j] * qs;
-            } else {
-                float s[4];
-                load4(a.scale + i, s, a.m - i);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) z[j] = (float)Tl::at(acc, x, y)[j] * (qs * s[j]);
-            }
+            for (int j = 0; j < 8; ++j) z[j] = GROUPED ? z[j] * qs : z[j] * (qs * s[j]);
             if (a.dtype == BAKRON_F32)
                 linear_store<float>(a, t, i, z);
             else if (a.dtype == BAKRON_F16)
@@ -142,7 +142,7 @@ static void launch_linear(const LinearArgs& a, hipStream_t st) {
     auto tiles = [&](int64_t b) { return ((a.m + b - 1) / b) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
     if constexpr (!GROUPED) {
-        if (tiles(256) >= ncu && a.ldq < TILE_LD_MAX) return launch_linear_tile<BigTile<M>, GROUPED>(a, st);
+        if (tiles(256) >= ncu) return launch_linear_tile<BigTile<M>, GROUPED>(a, st);
     }
     if (tiles(128) >= ncu) return launch_linear_tile<Tile<M, 128, 128, 2, 2>, GROUPED>(a, st);
     launch_linear_tile<Tile<M, 64, 64, 2, 2>, GROUPED>(a, st);
@@ -174,6 +174,7 @@ extern "C" bakron_status bakron_linear(const int8_t* q, int64_t ldq, const float
     if (st != BAKRON_OK || query) return st;
     const int64_t np = (n + BAKRON_PACK_COLUMNS - 1) / BAKRON_PACK_COLUMNS * BAKRON_PACK_COLUMNS;
     if (ldq < np || ldq % 16) return bk::op_fail(who, "ldq must be a multiple of 16, at least n padded");
+    if (ldq >= bk::TILE_LD_MAX) return bk::op_fail(who, "ldq too large");
     if (ldy < m || (other && ldo < m)) return bk::op_fail(who, "leading dimension below m");
     if ((combine != BAKRON_COMBINE_NONE) != (other != nullptr))
         return bk::op_fail(who, "other goes with combine");

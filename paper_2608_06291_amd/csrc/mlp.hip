@@ -11,9 +11,7 @@
 namespace bk {
 
 struct GatedArgs {
-    const char *x, *wg, *wu;       // rows of 16-byte multiples
-    int64_t ldx, ldw;              // bytes
-    int64_t kbytes;                // d in bytes
+    Operand x, w;                  // w: rows of Wg at base, of Wu at base2
     int64_t T, f;
     int chunks, act;
     int ni, nt;
@@ -24,9 +22,8 @@ struct GatedArgs {
     // backward
     const void* dh;
     int64_t lddh;
-    void* dgu;                     // T x 2 fp: dG | dU
-    void* dgut;                    // 2 fp x Tp: its transpose
-    int64_t fp, Tp;
+    void* dgu;                     // T x 2 fp: dG | dU, zeros in the padding of each
+    int64_t fp;
 };
 
 template <typename Tl, bool BWD>
@@ -36,99 +33,81 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
     int ti, tt;
     tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
     const int64_t f0 = (int64_t)ti * (Tl::ROWS / 2), t0 = (int64_t)tt * Tl::COLS;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     static_assert(Tl::UA % 2 == 0, "gate and up rows in one wave");
 
     typename Tl::Accs acc = {};
-    auto none = [](int, typename Tl::Accs&) {};
-    auto feature = [](int r) { return (int64_t)((r >> 5) * 16 + (r & 15)); };   // of tile row r
-    if constexpr (Tl::THREADS == 512) {
-        // (the rows that a wave loads are all of one matrix)
-        const int w = __builtin_amdgcn_readfirstlane(wave);
-        const bool up = (Tl::load_row_a(0, 0, w) >> 4) & 1;
-        Tl::run(
-            lds, (up ? a.wu : a.wg) + f0 * a.ldw, a.x + t0 * a.ldx,
-            [&](int r) { return (uint32_t)(min(feature(r), a.f - 1 - f0) * a.ldw); },
-            [&](int r) { return (uint32_t)(min((int64_t)r, a.T - 1 - t0) * a.ldx); }, a.kbytes, a.kbytes,
-            a.chunks, acc, none);
-    } else {
-        Tl::run(
-            lds,
-            [&](int r) { return ((r >> 4) & 1 ? a.wu : a.wg) + min(f0 + feature(r), a.f - 1) * a.ldw; },
-            [&](int r) { return a.x + min(t0 + r, a.T - 1) * a.ldx; }, a.kbytes, a.kbytes, a.chunks, acc,
-            none);
-    }
+    // Tile row r: gate and up in turn, 16 and 16.  The rows that a wave loads are all of
+    // one matrix: 8 at a time, multiples of 32 (or 64) apart.
+    const bool up = Tl::THREADS == 512 ? (wave >> 1) & 1 : (wave * 8 >> 4) & 1;
+    Operand w = a.w;
+    if (up) w.base = a.w.base2;
+    const int64_t first = min(f0, a.f - 1);
+    auto feature = [](int r) { return (r >> 5) * 16 + (r & 15); };
+    if constexpr (Tl::THREADS == 512)
+        Tl::run(lds, w, first, a.x, t0, a.chunks, acc, feature);
+    else
+        Tl::run(lds, w, first, a.x, t0, a.chunks, acc, feature, [](int, typename Tl::Accs&) {});
 
+    const auto rows =
+        handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
+    constexpr int PER = Tl::UA;   // lanes a row: 8 features each
+    const int p = lane % PER;
+    const int64_t j = f0 + Tl::a0(wave) / 2 + p * 8, valid = a.f - j;
 #pragma unroll
     for (int y = 0; y < Tl::UB; ++y) {
-        const int64_t t = t0 + Tl::b0(wave) + y * 16 + (lane & 15);
+        rows.put(y);
+        const int tl = lane / PER;
+        const int64_t t = t0 + Tl::b0(wave) + y * 16 + tl;
+        if (tl >= 16) continue;
+        float G[8], U[8];
+        rows.take(tl, (p >> 1) * 4 + (p & 1), G);
+        rows.take(tl, (p >> 1) * 4 + (p & 1) + 2, U);
+        if (t >= a.T) continue;
+        if constexpr (!BWD) {
+            if (valid <= 0) continue;
+            float v[8], s[8];
+            if (a.feat_gate) {
 #pragma unroll
-        for (int x = 0; x < Tl::UA; x += 2) {
-            const f32x4 G = Tl::at(acc, x, y), U = Tl::at(acc, x + 1, y);
-            const int64_t j = f0 + (Tl::a0(wave) + x * 16) / 2 + (lane >> 4) * 4;
-            const int64_t valid = a.f - j;
-            if constexpr (!BWD) {
-                if (t >= a.T || valid <= 0) continue;
-                float h[4], v[4], s[4];
-                if (a.feat_gate) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        act_both(G[r], a.act, &v[r], &s[r]);
-                        s[r] *= U[r];
-                    }
-                    store4(a.feat_gate + t * a.f + j, s, valid);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = act_value(G[r], a.act);
+                for (int r = 0; r < 8; ++r) {
+                    act_both(G[r], a.act, &v[r], &s[r]);
+                    s[r] *= U[r];
                 }
-                if (a.feat_up) store4(a.feat_up + t * a.f + j, v, valid);
-                if (a.h) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) h[r] = v[r] * U[r];
-                    store4(static_cast<E*>(a.h) + t * a.ldh + j, h, valid);
-                }
+                store8(a.feat_gate + t * a.f + j, s, valid);
             } else {
-                // zeros in the padding of both layouts, which the products read
-                if (j >= a.fp) continue;
-                float dg[4] = {0.0f, 0.0f, 0.0f, 0.0f}, du[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (t < a.T && valid > 0) {
-                    float dh[4];
-                    load4(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, valid);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float v, s;
-                        act_both(G[r], a.act, &v, &s);
-                        if (r < valid) {
-                            dg[r] = dh[r] * U[r] * s;
-                            du[r] = dh[r] * v;
-                        }
-                    }
-                }
-                if (t < a.T && a.dgu) {
-                    E* const row = static_cast<E*>(a.dgu) + t * (2 * a.fp) + j;
-                    store4(row, dg, 4);
-                    store4(row + a.fp, du, 4);
-                }
-                if (t < a.Tp && a.dgut) {
-                    E* const col = static_cast<E*>(a.dgut) + j * a.Tp + t;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        col[r * a.Tp] = (E)dg[r];
-                        col[(a.fp + r) * a.Tp] = (E)du[r];
-                    }
-                }
+                for (int r = 0; r < 8; ++r) v[r] = act_value(G[r], a.act);
             }
+            if (a.feat_up) store8(a.feat_up + t * a.f + j, v, valid);
+            if (a.h) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] *= U[r];
+                store8(static_cast<E*>(a.h) + t * a.ldh + j, v, valid);
+            }
+        } else {
+            if (j >= a.fp) continue;
+            float dh[8] = {}, dg[8], du[8];
+            if (valid > 0) load8(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, valid);
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                float v, s;
+                act_both(G[r], a.act, &v, &s);
+                dg[r] = r < valid ? dh[r] * U[r] * s : 0.0f;   // (0 in the padding, whatever G is)
+                du[r] = r < valid ? dh[r] * v : 0.0f;
+            }
+            E* const row = static_cast<E*>(a.dgu) + t * (2 * a.fp) + j;
+            store8(row, dg, 8);
+            store8(row + a.fp, du, 8);
         }
     }
 }
 
 struct ProdArgs {
-    const char *a, *b;             // D[i][t] = sum_k a[i][k] b[t][k]
-    int64_t lda, ldb, kbytes;      // bytes
-    int64_t ni_rows, nt_rows;
+    Operand a, b;                  // D[i][t] = sum_k a[i][k] b[t][k]
     int chunks, ni, nt;
-    void *out, *out2;              // rows t < split of out; from split2 on, of out2
-    int64_t ldo, split, split2;
+    int64_t d;                     // columns of the output
+    void *out, *out2;              // rows t < split of out; split2 <= t < end, of out2
+    int64_t ldo, split, split2, end;
 };
 
 template <typename Tl>
@@ -141,31 +120,29 @@ __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 
     typename Tl::Accs acc = {};
-    auto none = [](int, typename Tl::Accs&) {};
+    auto same = [](int r) { return r; };
     if constexpr (Tl::THREADS == 512)
-        Tl::run(
-            lds, a.a + i0 * a.lda, a.b + t0 * a.ldb,
-            [&](int r) { return (uint32_t)(min((int64_t)r, a.ni_rows - 1 - i0) * a.lda); },
-            [&](int r) { return (uint32_t)(min((int64_t)r, a.nt_rows - 1 - t0) * a.ldb); }, a.kbytes,
-            a.kbytes, a.chunks, acc, none);
+        Tl::run(lds, a.a, i0, a.b, t0, a.chunks, acc, same);
     else
-        Tl::run(
-            lds, [&](int r) { return a.a + min(i0 + r, a.ni_rows - 1) * a.lda; },
-            [&](int r) { return a.b + min(t0 + r, a.nt_rows - 1) * a.ldb; }, a.kbytes, a.kbytes,
-            a.chunks, acc, none);
+        Tl::run(lds, a.a, i0, a.b, t0, a.chunks, acc, same, [](int, typename Tl::Accs&) {});
+
+    const auto rows =
+        handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
+    constexpr int PER = Tl::UA * 2;   // lanes a row
+    const int p = lane % PER;
+    const int64_t i = i0 + Tl::a0(wave) + p * 8;
 #pragma unroll
     for (int y = 0; y < Tl::UB; ++y) {
-        const int64_t t = t0 + Tl::b0(wave) + y * 16 + (lane & 15);
-        if (t >= a.nt_rows || (t >= a.split && t < a.split2)) continue;
-        E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
-                                   : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
+        rows.put(y);
 #pragma unroll
-        for (int x = 0; x < Tl::UA; ++x) {
-            const int64_t i = i0 + Tl::a0(wave) + x * 16 + (lane >> 4) * 4;
-            float v[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = Tl::at(acc, x, y)[r];
-            if (i < a.ni_rows) store4(row + i, v, a.ni_rows - i);
+        for (int tl = lane / PER; tl < 16; tl += 64 / PER) {
+            const int64_t t = t0 + Tl::b0(wave) + y * 16 + tl;
+            float v[8];
+            rows.take(tl, p, v);
+            if (i >= a.d || t >= a.end || (t >= a.split && t < a.split2)) continue;
+            E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
+                                       : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
+            store8(row + i, v, a.d - i);
         }
     }
 }
@@ -187,53 +164,31 @@ __global__ __launch_bounds__(256) void k_pad_rows(const uint16_t* __restrict__ s
     store_pack(dst + e * 8, v);
 }
 
-// dst[c][r] = src[r][c] for r < rows, 0 for rows <= r < rows_p; 16-bit entries, one
-// 64 x 64 block a workgroup.
-__global__ __launch_bounds__(256) void k_transpose(const uint16_t* __restrict__ src, int64_t ld,
-                                                   int64_t rows, int64_t cols, int64_t rows_p,
-                                                   uint16_t* __restrict__ dst, int64_t ldd) {
-    __shared__ uint16_t s[64][66];
-    const int64_t nb = (cols + 63) / 64;
-    const int64_t r0 = (int64_t)blockIdx.x / nb * 64, c0 = (int64_t)blockIdx.x % nb * 64;
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int64_t r = r0 + k * 4 + y, c = c0 + x;
-        s[k * 4 + y][x] = r < rows && c < cols ? src[r * ld + c] : (uint16_t)0;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int64_t c = c0 + k * 4 + y, r = r0 + x;
-        if (c < cols && r < rows_p) dst[c * ldd + r] = s[x][k * 4 + y];
-    }
-}
-
 __global__ __launch_bounds__(256) void k_zero_rows(uint16_t* p, int64_t ld, int64_t rows, int64_t cols) {
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
         for (int64_t c = threadIdx.x; c < cols; c += 256) p[r * ld + c] = 0;
 }
 
-static inline int64_t up64(int64_t v) { return (v + 63) / 64 * 64; }
 static inline size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 static inline dim3 grid256(int64_t n) { return dim3((unsigned)((n + 255) / 256)); }
 
 // Whether rows can be staged as they are: 16-byte pieces at 16-byte addresses.
 static bool direct_rows(const void* p, int64_t ld, int64_t cols) {
-    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0;
+    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && 2 * ld < TILE_LD_MAX;
 }
 
 template <typename M, bool BWD>
 static void launch_gated(GatedArgs a, hipStream_t st) {
-    auto tiles = [&](int64_t b) { return ((a.f + b / 2 - 1) / (b / 2)) * ((a.T + b - 1) / b); };
+    const int64_t f = BWD ? a.fp : a.f;   // (the padding is written, too)
+    auto tiles = [&](int64_t b) { return ((f + b / 2 - 1) / (b / 2)) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
     auto go = [&](auto tile) {
         typedef decltype(tile) Tl;
-        a.ni = (int)((a.f + Tl::ROWS / 2 - 1) / (Tl::ROWS / 2));
+        a.ni = (int)((f + Tl::ROWS / 2 - 1) / (Tl::ROWS / 2));
         a.nt = (int)((a.T + Tl::COLS - 1) / Tl::COLS);
         hipLaunchKernelGGL((k_gated<Tl, BWD>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
     };
-    if (tiles(256) >= ncu && std::max(a.ldx, a.ldw) < TILE_LD_MAX)
+    if (tiles(256) >= ncu)
         go(BigTile<M>());
     else if (tiles(128) >= ncu)
         go(Tile<M, 128, 128, 2, 2>());
@@ -241,22 +196,22 @@ static void launch_gated(GatedArgs a, hipStream_t st) {
         go(Tile<M, 64, 64, 2, 2>());
 }
 
-template <typename M>
+template <typename M, bool ACOLS, bool BCOLS>
 static void launch_prod(ProdArgs a, hipStream_t st) {
-    auto tiles = [&](int64_t b) { return ((a.ni_rows + b - 1) / b) * ((a.nt_rows + b - 1) / b); };
+    auto tiles = [&](int64_t b) { return ((a.a.n + b - 1) / b) * ((a.b.n + b - 1) / b); };
     const int ncu = op_cus();
     auto go = [&](auto tile) {
         typedef decltype(tile) Tl;
-        a.ni = (int)((a.ni_rows + Tl::ROWS - 1) / Tl::ROWS);
-        a.nt = (int)((a.nt_rows + Tl::COLS - 1) / Tl::COLS);
+        a.ni = (int)((a.a.n + Tl::ROWS - 1) / Tl::ROWS);
+        a.nt = (int)((a.b.n + Tl::COLS - 1) / Tl::COLS);
         hipLaunchKernelGGL((k_prod<Tl>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
     };
-    if (tiles(256) >= ncu && std::max(a.lda, a.ldb) < TILE_LD_MAX)
-        go(BigTile<M>());
+    if (tiles(256) >= ncu)
+        go(BigTile<M, ACOLS, BCOLS>());
     else if (tiles(128) >= ncu)
-        go(Tile<M, 128, 128, 2, 2>());
+        go(Tile<M, 128, 128, 2, 2, ACOLS, BCOLS>());
     else
-        go(Tile<M, 64, 64, 2, 2>());
+        go(Tile<M, 64, 64, 2, 2, ACOLS, BCOLS>());
 }
 
 // Padded copies of operands that cannot be staged as they are.
@@ -268,7 +223,7 @@ struct PadPlan {
 static PadPlan pad_plan(const void* x, int64_t ldx, const void* wg, const void* wu, int64_t ldw,
                         int64_t T, int64_t d, int64_t f) {
     PadPlan p;
-    p.dp = up64(d);
+    p.dp = (d + 63) / 64 * 64;
     p.x = !direct_rows(x, ldx, d);
     p.w = !direct_rows(wg, ldw, d) || !direct_rows(wu, ldw, d);
     p.xbytes = p.x ? up256((size_t)T * p.dp * 2) : 0;
@@ -282,39 +237,65 @@ static void pad_copy(const void* src, int64_t ld, int64_t rows, int64_t cols, in
                        static_cast<const uint16_t*>(src), ld, rows, cols, cols_p,
                        static_cast<uint16_t*>(dst));
 }
-static void transpose(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t rows_p,
-                      void* dst, int64_t ldd, hipStream_t st) {
-    hipLaunchKernelGGL(k_transpose, dim3((unsigned)((rows_p + 63) / 64 * ((cols + 63) / 64))),
-                       dim3(256), 0, st, static_cast<const uint16_t*>(src), ld, rows, cols, rows_p,
-                       static_cast<uint16_t*>(dst), ldd);
-}
 
-// Puts x and the weights into `a`, through padded copies at `*at` where needed.
+// x and the weights as operands of the gated product, through padded copies at `*at`
+// where needed.
 static void gated_operands(GatedArgs& a, const PadPlan& p, const void* x, int64_t ldx,
                            const void* wg, const void* wu, int64_t ldw, int64_t d, char** at,
                            hipStream_t st) {
-    a.x = static_cast<const char*>(x);
-    a.ldx = 2 * ldx;
+    // (a copy's padding is zeros; without copies what lies past d reads as zeros)
+    const int64_t kbytes = p.x && p.w ? 2 * p.dp : 2 * ((d + 7) / 8 * 8);
+    a.x = operand(x, 2 * ldx, a.T, kbytes);
     if (p.x) {
         pad_copy(x, ldx, a.T, d, p.dp, *at, st);
-        a.x = *at;
-        a.ldx = 2 * p.dp;
+        a.x = operand(*at, 2 * p.dp, a.T, kbytes);
         *at += p.xbytes;
     }
-    a.wg = static_cast<const char*>(wg);
-    a.wu = static_cast<const char*>(wu);
-    a.ldw = 2 * ldw;
+    a.w = operand(wg, 2 * ldw, a.f, kbytes);
+    a.w.base2 = static_cast<const char*>(wu);
     if (p.w) {
         pad_copy(wg, ldw, a.f, d, p.dp, *at, st);
         pad_copy(wu, ldw, a.f, d, p.dp, *at + p.wbytes, st);
-        a.wg = *at;
-        a.wu = *at + p.wbytes;
-        a.ldw = 2 * p.dp;
+        a.w = operand(*at, 2 * p.dp, a.f, kbytes);
+        a.w.base2 = *at + p.wbytes;
         *at += 2 * p.wbytes;
     }
-    // (a copy's padding is zeros; without copies the pieces past d are)
-    a.kbytes = p.x && p.w ? 2 * p.dp : 2 * ((d + 7) / 8 * 8);
-    a.chunks = (int)((a.kbytes + CHUNK_BYTES - 1) / CHUNK_BYTES);
+    a.chunks = (int)((kbytes + CHUNK_BYTES - 1) / CHUNK_BYTES);
+}
+
+template <typename M>
+static void run_backward(const GatedArgs& a, int64_t d, void* dx, int64_t lddx, void* dw_gate,
+                         void* dw_up, int64_t lddw, hipStream_t st) {
+    launch_gated<M, true>(a, st);
+    const int64_t ldg = 4 * a.fp;
+    const int64_t cols = (d + 7) / 8 * 8;   // (of x and the weights, as they are or padded)
+    if (dx) {   // over the features: those of Wg, then those of Wu
+        ProdArgs g{};
+        g.a = operand(a.w.base, a.w.ld, cols, a.f);
+        g.a.base2 = a.w.base2;
+        g.a.split = (int)(a.fp / 64);
+        g.b = operand(a.dgu, ldg, a.T, ldg);
+        g.chunks = 2 * g.a.split;
+        g.out = dx;
+        g.ldo = lddx;
+        g.split = g.split2 = g.end = a.T;
+        g.d = d;
+        launch_prod<M, true, false>(g, st);
+    }
+    if (dw_gate) {   // over the tokens
+        ProdArgs g{};
+        g.a = operand(a.x.base, a.x.ld, cols, a.T);
+        g.b = operand(a.dgu, ldg, 2 * a.fp, a.T);
+        g.chunks = (int)((a.T + 63) / 64);
+        g.out = dw_gate;
+        g.out2 = dw_up;
+        g.ldo = lddw;
+        g.split = a.f;
+        g.split2 = a.fp;
+        g.end = a.fp + a.f;
+        g.d = d;
+        launch_prod<M, true, true>(g, st);
+    }
 }
 
 }  // namespace bk
@@ -381,12 +362,10 @@ extern "C" bakron_status bakron_gated_mlp_backward(const void* dh, int64_t lddh,
     if (lddh < f || (dx && lddx < d) || (dw_gate && lddw < d))
         return bk::op_fail(who, "leading dimension too small");
     const bk::PadPlan p = bk::pad_plan(x, ldx, w_gate, w_up, ldw, T, d, f);
-    // (every tile of the gated product covers the padding it has to clear)
-    const int64_t fp = (f + 31) / 32 * 32, Tp = bk::up64(T);
-    const size_t dgu = bk::up256((size_t)T * 2 * fp * 2), dgut = bk::up256((size_t)Tp * 2 * fp * 2);
-    const size_t wt = bk::up256((size_t)d * 2 * fp * 2), xt = bk::up256((size_t)d * Tp * 2);
+    const int64_t fp = (f + 63) / 64 * 64;
+    const size_t dgu = bk::up256((size_t)T * 2 * fp * 2);
     bool query;
-    st = bk::op_workspace(who, work, work_bytes, p.xbytes + 2 * p.wbytes + dgu + dgut + wt + xt, &query);
+    st = bk::op_workspace(who, work, work_bytes, p.xbytes + 2 * p.wbytes + dgu, &query);
     if (st != BAKRON_OK || query) return st;
     if (!dw_gate != !dw_up) return bk::op_fail(who, "dw_gate and dw_up go together");
     if (!dx && !dw_gate) return bk::op_fail(who, "null pointer");
@@ -405,50 +384,10 @@ extern "C" bakron_status bakron_gated_mlp_backward(const void* dh, int64_t lddh,
     a.dh = dh;
     a.lddh = lddh;
     a.fp = fp;
-    a.Tp = Tp;
     char* at = static_cast<char*>(work);
     bk::gated_operands(a, p, x, ldx, w_gate, w_up, ldw, d, &at, stream);
-    char* const dgu_at = at;
-    char* const dgut_at = dgu_at + dgu;
-    char* const wt_at = dgut_at + dgut;
-    char* const xt_at = wt_at + wt;
-    a.dgu = dx ? dgu_at : nullptr;
-    a.dgut = dw_gate ? dgut_at : nullptr;
-    const bool bf16 = dtype == BAKRON_BF16;
-    bf16 ? bk::launch_gated<bk::MmaBF16, true>(a, stream) : bk::launch_gated<bk::MmaF16, true>(a, stream);
-    if (dx) {
-        bk::transpose(w_gate, ldw, f, d, fp, wt_at, 2 * fp, stream);
-        bk::transpose(w_up, ldw, f, d, fp, wt_at + 2 * fp, 2 * fp, stream);
-        bk::ProdArgs g{};
-        g.a = wt_at;
-        g.b = dgu_at;
-        g.lda = g.ldb = 4 * fp;
-        g.kbytes = 4 * fp;
-        g.ni_rows = d;
-        g.nt_rows = T;
-        g.chunks = (int)(g.kbytes / bk::CHUNK_BYTES);
-        g.out = dx;
-        g.ldo = lddx;
-        g.split = T;
-        g.split2 = T;
-        bf16 ? bk::launch_prod<bk::MmaBF16>(g, stream) : bk::launch_prod<bk::MmaF16>(g, stream);
-    }
-    if (dw_gate) {
-        bk::transpose(x, ldx, T, d, Tp, xt_at, Tp, stream);
-        bk::ProdArgs g{};
-        g.a = xt_at;
-        g.b = dgut_at;
-        g.lda = g.ldb = 2 * Tp;
-        g.kbytes = 2 * Tp;
-        g.ni_rows = d;
-        g.nt_rows = fp + f;   // (the rest of dU^T is padding)
-        g.chunks = (int)(g.kbytes / bk::CHUNK_BYTES);
-        g.out = dw_gate;
-        g.out2 = dw_up;
-        g.ldo = lddw;
-        g.split = f;
-        g.split2 = fp;
-        bf16 ? bk::launch_prod<bk::MmaBF16>(g, stream) : bk::launch_prod<bk::MmaF16>(g, stream);
-    }
+    a.dgu = at;
+    dtype == BAKRON_BF16 ? bk::run_backward<bk::MmaBF16>(a, d, dx, lddx, dw_gate, dw_up, lddw, stream)
+                         : bk::run_backward<bk::MmaF16>(a, d, dx, lddx, dw_gate, dw_up, lddw, stream);
     return bk::op_launched(who);
 }

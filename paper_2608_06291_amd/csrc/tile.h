@@ -1,11 +1,12 @@
-// Products of two matrices whose rows are contiguous along the summed axis, on the
-// matrix cores:  D[i][t] = sum_k A[i][k] B[t][k]  for 16-bit floats and 8-bit integers.
+// Products on the matrix cores:  D[i][t] = sum_k A[i][k] B[t][k]  for 16-bit floats and
+// 8-bit integers.
 //
-// A workgroup computes BM x BN of D from chunks of 128 bytes of k (64 16-bit or 128
-// 8-bit entries) of BM rows of A and BN rows of B, double-buffered in LDS and written
-// there by direct global loads.  A lane's 16-byte piece of a row is what one MFMA of 16 x 16
-// takes, for either type.  The pieces of a row are permuted by the row (by address, on
-// the way in), so that the 16 rows of a fragment read meet different banks.
+// A workgroup computes a tile of D from chunks of 128 bytes of k (64 16-bit or 128 8-bit
+// entries), double-buffered in LDS and written there by direct global loads.  Either
+// operand is held in memory with k contiguous (rows), or, in 16 bits, with i or t
+// contiguous (columns; the fragments are then read with the transposing LDS read).  The
+// pieces of a staged row are permuted by the row, by address on the way in, so that the
+// rows of a fragment read meet different banks.
 #pragma once
 #include "ops.h"
 
@@ -17,7 +18,7 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int CHUNK_BYTES = 128;
-// BigTile's 32-bit offsets reach 256 rows of fewer bytes than this.
+// 32-bit offsets reach 256 rows of fewer bytes than this.
 constexpr int64_t TILE_LD_MAX = (int64_t)1 << 23;
 
 // Operand types: what a 16-byte piece holds, the accumulator, bytes of A a chunk.
@@ -67,123 +68,47 @@ __device__ inline i32x4 unpack_codes(i32x2 p) {
 // 16 bytes of zeros: where a lane whose piece lies past the end of k reads.
 static __device__ const uint4 tile_zeros = {0, 0, 0, 0};
 
-// One operand: `row(r)` gives the address of row r of the tile.
-// Stages chunk bytes [off, off + BYTES) of ROWS rows; pieces at or past `end` are zeros.
-template <int ROWS, int BYTES, int WAVES>
-struct Stager {
-    static constexpr int PER_ROW = BYTES / 16;            // 16-byte pieces of a row
-    static constexpr int ROWS_PER = 64 / PER_ROW;         // rows a wave writes at once
-    static constexpr int N = ROWS / ROWS_PER / WAVES;     // loads a wave issues
-    static_assert(N >= 1 && N * ROWS_PER * WAVES == ROWS, "tile rows");
+// How an operand lies in LDS, for UNITS units of 16 of its rows (or columns) a chunk.
+//
+// Rows (k contiguous): a row of BYTES bytes is cut into 16-byte pieces; slot s of row r
+// holds piece s ^ (r & 7), or s ^ ((r >> 2) & 3) in rows of 64 bytes.  A lane's 16 (or 8,
+// packed) bytes of a fragment are one read.
+//
+// Columns (k outside): row k holds UNITS units of 16 entries (32 bytes); unit u of row k lies at
+// u ^ f(k), f(k) from the bits of k that differ between the 16 rows that a transposing read
+// touches (k = 8 q + 4 e + r: q and r, for 16 lanes of rows r and 4 x 4 entries each).
+template <int BYTES>
+__device__ inline int row_piece(int r, int slot) {
+    return BYTES == 128 ? slot ^ (r & 7) : slot ^ ((r >> 2) & 3);
+}
+template <int UNITS>
+__device__ inline int col_twist(int k) {
+    return UNITS >= 8 ? (k & 3) | ((k >> 3) & 1) << 2 : ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
+}
+typedef int16_t i16x4 __attribute__((ext_vector_type(4)));
+__device__ inline i32x2 read_transposed(const char* p) {
+    return __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         (__attribute__((address_space(3))) i16x4*)p));
+}
 
-    const char* src[N];   // this lane's piece of chunk 0
-    int piece;            // its byte offset in the chunk
-
-    // Piece held in slot `slot` of LDS row r.
-    static __device__ inline int permuted(int r, int slot) {
-        return BYTES == 128 ? slot ^ (r & 7) : slot ^ ((r >> 2) & 3);
-    }
-    template <typename RowFn>
-    __device__ inline void init(RowFn row, int wave, int lane) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int r = (i * WAVES + wave) * ROWS_PER + lane / PER_ROW;
-            piece = permuted(r, lane % PER_ROW) * 16;
-            src[i] = row(r) + piece;
-        }
-    }
-    // (the permutation has period 8 or 16 in r, and r steps by multiples of WAVES *
-    // ROWS_PER, so `piece` is the same for every i)
-    static_assert((WAVES * ROWS_PER) % (BYTES == 128 ? 8 : 16) == 0, "one piece a lane");
-
-    __device__ inline void load(char* lds, int64_t off, int64_t end, int wave) const {
-        const bool out = off + piece >= end;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const char* p = out ? reinterpret_cast<const char*>(&tile_zeros) : src[i] + off;
-            __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void*)p,
-                (__attribute__((address_space(3))) void*)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
-        }
-    }
+// An operand in memory.  Rows: row(r) is r rows of `ld` bytes on, r < n; k runs over
+// [0, k_end) bytes of it.  Columns: k rows of `ld` bytes, k < k_end, of n entries (n a
+// multiple of 8).  With `split` > 0 the chunks from `split` on start over at base2.  Past its
+// end an operand reads as zeros; past n (never used) as some entry before it.
+struct Operand {
+    const char* base;
+    const char* base2;
+    int64_t ld, n, k_end;
+    int split;
 };
+inline Operand operand(const void* base, int64_t ld, int64_t n, int64_t k_end) {
+    return Operand{static_cast<const char*>(base), nullptr, ld, n, k_end, 0};
+}
 
-// The tile's main loop.  acc[x][y] gets rows x, columns y of 16 of the wave's part;
-// lane l of it holds D[4 (l / 16) + 0..3][l % 16].
-template <typename M, int BM, int BN, int WM, int WN>
-struct Tile {
-    static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
-    static constexpr int TM = BM / WM, TN = BN / WN;      // a wave's part
-    static constexpr int X = TM / 16, Y = TN / 16;
-    static constexpr int A_LDS = BM * M::A_BYTES, B_LDS = BN * CHUNK_BYTES;
-    static constexpr int LDS = 2 * (A_LDS + B_LDS);
-    static constexpr int ROWS = BM, COLS = BN;
-    typedef M Mma;
-    typedef typename M::Acc Acc;
-    typedef Acc Accs[X][Y];
-    // Units of 16 rows of A and of 16 rows of B in a wave's part, and where they begin.
-    static constexpr int UA = X, UB = Y;
-    static __device__ inline int a0(int wave) { return wave / WN * TM; }
-    static __device__ inline int b0(int wave) { return wave % WN * TN; }
-    static __device__ inline Acc& at(Accs& acc, int a, int b) { return acc[a][b]; }
-
-    // `after(c, acc)` runs when chunk c has been added.
-    template <typename RowA, typename RowB, typename After>
-    static __device__ inline void run(char* lds, RowA row_a, RowB row_b, int64_t a_end, int64_t b_end,
-                                      int chunks, Acc (&acc)[X][Y], After after) {
-        const int tid = threadIdx.x, lane = tid & 63;
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int wm = wave / WN, wn = wave % WN;
-        Stager<BM, M::A_BYTES, WAVES> sa;
-        Stager<BN, CHUNK_BYTES, WAVES> sb;
-        sa.init(row_a, wave, lane);
-        sb.init(row_b, wave, lane);
-        const int r16 = lane & 15, kq = lane >> 4;
-        if (chunks > 0) {
-            sa.load(lds, 0, a_end, wave);
-            sb.load(lds + A_LDS, 0, b_end, wave);
-        }
-        for (int c = 0; c < chunks; ++c) {
-            char* const cur = lds + (c & 1) * (A_LDS + B_LDS);
-            char* const nxt = lds + ((c + 1) & 1) * (A_LDS + B_LDS);
-            __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's direct loads landed
-            __syncthreads();                      // everybody's, and the other buffer is free
-            if (c + 1 < chunks) {
-                sa.load(nxt, (int64_t)(c + 1) * M::A_BYTES, a_end, wave);
-                sb.load(nxt + A_LDS, (int64_t)(c + 1) * CHUNK_BYTES, b_end, wave);
-            }
-            const char* const A = cur + wm * TM * M::A_BYTES;
-            const char* const B = cur + A_LDS + wn * TN * CHUNK_BYTES;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                i32x4 b[Y];
-#pragma unroll
-                for (int y = 0; y < Y; ++y) {
-                    const int r = y * 16 + r16;
-                    b[y] = *reinterpret_cast<const i32x4*>(B + r * CHUNK_BYTES +
-                                                           (((s * 4 + kq) ^ (r & 7)) << 4));
-                }
-#pragma unroll
-                for (int x = 0; x < X; ++x) {
-                    const int r = x * 16 + r16;
-                    i32x4 a;
-                    if constexpr (M::A_BYTES == CHUNK_BYTES) {
-                        a = *reinterpret_cast<const i32x4*>(A + r * CHUNK_BYTES +
-                                                            (((s * 4 + kq) ^ (r & 7)) << 4));
-                    } else {
-                        const int k8 = s * 4 + kq;   // 8-byte piece
-                        a = unpack_codes(*reinterpret_cast<const i32x2*>(
-                            A + r * M::A_BYTES + ((((k8 >> 1) ^ ((r >> 2) & 3)) << 4) | ((k8 & 1) << 3))));
-                    }
-#pragma unroll
-                    for (int y = 0; y < Y; ++y) acc[x][y] = M::mma(a, b[y], acc[x][y]);
-                }
-                after(2 * c + s, acc);
-            }
-        }
-    }
-};
-
+__device__ inline void load_lds(const char* p, char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
 template <int N>
 __device__ inline void wait_loads() {   // all but the last N of this wave's
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -198,6 +123,162 @@ __device__ inline void bare_barrier() {
     asm volatile("" ::: "memory");
 }
 
+// N loads of a wave from one operand: each lane's pieces as 32-bit offsets from a base
+// that moves on with the chunks.
+template <bool COLS, int BYTES, int N>
+struct Source {
+    const char *base, *base2;
+    int64_t step;        // bytes from chunk to chunk
+    int split, last;
+    uint32_t off[N];
+    int at[N];           // Columns: row in the chunk; rows: at[0] the piece's byte
+    int64_t end;         // k_end
+
+    __device__ inline void load(int i, int chunk, char* to) const {
+        int c = min(chunk, last);   // (past the last chunk: that one again, not used)
+        const char* b = base;
+        if (split > 0 && c >= split) {
+            b = base2;
+            c -= split;
+        }
+        const char* p = b + c * step + off[i];
+        if constexpr (COLS) {
+            if ((int64_t)(c + 1) * 64 > end && (int64_t)c * 64 + at[i] >= end)
+                p = reinterpret_cast<const char*>(&tile_zeros);
+        } else {
+            if ((int64_t)(c + 1) * BYTES > end && (int64_t)c * BYTES + at[0] >= end)
+                p = reinterpret_cast<const char*>(&tile_zeros);
+        }
+        load_lds(p, to);
+    }
+    __device__ inline void init(const Operand& o, int64_t first, int chunks) {
+        base = o.base + (COLS ? 2 * first : first * o.ld);
+        base2 = o.base2 + (COLS ? 2 * first : first * o.ld);
+        step = COLS ? 64 * o.ld : BYTES;
+        split = o.split;
+        last = chunks - 1;
+        end = o.k_end;
+    }
+    // The lane's piece of load i: slot `slot` of LDS row r; `local` maps the row (or the
+    // first of 8 columns) of the half's layout to the tile's.
+    __device__ inline void set_row(int i, const Operand& o, int64_t first, int tile_row, int piece) {
+        at[0] = piece;
+        off[i] = (uint32_t)(min((int64_t)tile_row, o.n - 1 - first) * o.ld) + piece;
+    }
+    __device__ inline void set_col(int i, const Operand& o, int64_t first, int k, int tile_col) {
+        at[i] = k;
+        off[i] = (uint32_t)(k * o.ld) + (first + tile_col < o.n ? 2 * tile_col : 0);
+    }
+};
+
+// The small tile: WM x WN waves, two buffers, one barrier a chunk.
+template <typename M, int BM, int BN, int WM, int WN, bool ACOLS = false, bool BCOLS = false>
+struct Tile {
+    static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int ROWS = BM, COLS = BN;
+    static constexpr int TM = BM / WM, TN = BN / WN;      // a wave's part
+    static constexpr int UA = TM / 16, UB = TN / 16;      // in units of 16
+    static constexpr int A_LDS = BM * M::A_BYTES, B_LDS = BN * CHUNK_BYTES;
+    static constexpr int LDS = 2 * (A_LDS + B_LDS);
+    typedef M Mma;
+    typedef typename M::Acc Acc;
+    typedef Acc Accs[UA][UB];
+    static __device__ inline int a0(int wave) { return wave / WN * TM; }
+    static __device__ inline int b0(int wave) { return wave % WN * TN; }
+    static __device__ inline Acc& at(Accs& acc, int a, int b) { return acc[a][b]; }
+
+    // All loads of one operand of R rows (columns).
+    template <bool C, int R, int BYTES>
+    struct Loads {
+        static constexpr int PIECES = C ? R / 8 : BYTES / 16;   // of an LDS row
+        static constexpr int PER = 64 / PIECES;                 // LDS rows a load writes
+        static constexpr int N = (C ? 64 : R) / PER / WAVES;
+        static_assert(N >= 1, "every wave loads");
+        Source<C, BYTES, N> s;
+        template <typename RowFn>
+        __device__ inline void init(const Operand& o, int64_t first, int chunks, int wave, int lane,
+                                    RowFn row) {
+            s.init(o, first, chunks);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int r = (i * WAVES + wave) * PER + lane / PIECES, slot = lane % PIECES;
+                if constexpr (C) {
+                    const int unit = (slot >> 1) ^ col_twist<R / 16>(r);
+                    s.set_col(i, o, first, r, unit * 16 + (slot & 1) * 8);
+                } else {
+                    // (row_piece has a period that divides the rows between two loads)
+                    s.set_row(i, o, first, row(r), row_piece<BYTES>(r, slot) * 16);
+                }
+            }
+        }
+        __device__ inline void load(int chunk, char* lds, int wave) const {
+#pragma unroll
+            for (int i = 0; i < N; ++i) s.load(i, chunk, lds + (i * WAVES + wave) * 1024);
+        }
+    };
+    // A fragment: unit u of R / 16, step s.
+    template <bool C, int R, int BYTES>
+    static __device__ inline i32x4 fragment(const char* lds, int u, int s, int lane) {
+        const int r16 = lane & 15, kq = lane >> 4;
+        if constexpr (C) {
+            const int k = s * 32 + kq * 8 + (r16 >> 2);
+            const char* const p = lds + k * (2 * R) + ((u ^ col_twist<R / 16>(k)) << 5) + (r16 & 3) * 8;
+            const i32x2 x = read_transposed(p), y = read_transposed(p + 4 * 2 * R);
+            return i32x4{x[0], x[1], y[0], y[1]};
+        } else {
+            const int r = u * 16 + r16, k = s * 4 + kq;
+            if constexpr (BYTES == CHUNK_BYTES)
+                return *reinterpret_cast<const i32x4*>(lds + r * BYTES + (row_piece<BYTES>(r, k) << 4));
+            else
+                return unpack_codes(*reinterpret_cast<const i32x2*>(
+                    lds + r * BYTES + (row_piece<BYTES>(r, k >> 1) << 4) + ((k & 1) << 3)));
+        }
+    }
+
+    // The tile that begins at row `ia` of A and row `ib` of B; row_a maps rows of the tile to
+    // rows of the operand, counted from ia.  `after(step, acc)` runs when step `step` (half a
+    // chunk) has been added.  LDS is free to use again on return.
+    template <typename RowA, typename After>
+    static __device__ inline void run(char* lds, const Operand& oa, int64_t ia, const Operand& ob,
+                                      int64_t ib, int chunks, Accs& acc, RowA row_a, After after) {
+        const int tid = threadIdx.x, lane = tid & 63;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        Loads<ACOLS, BM, M::A_BYTES> la;
+        Loads<BCOLS, BN, CHUNK_BYTES> lb;
+        la.init(oa, ia, chunks, wave, lane, row_a);
+        lb.init(ob, ib, chunks, wave, lane, [](int r) { return r; });
+        if (chunks > 0) {
+            la.load(0, lds, wave);
+            lb.load(0, lds + A_LDS, wave);
+        }
+        for (int c = 0; c < chunks; ++c) {
+            char* const cur = lds + (c & 1) * (A_LDS + B_LDS);
+            char* const nxt = lds + ((c + 1) & 1) * (A_LDS + B_LDS);
+            wait_loads<0>();
+            __syncthreads();   // everybody's loads landed, and the other buffer is free
+            if (c + 1 < chunks) {
+                la.load(c + 1, nxt, wave);
+                lb.load(c + 1, nxt + A_LDS, wave);
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                i32x4 b[UB];
+#pragma unroll
+                for (int y = 0; y < UB; ++y)
+                    b[y] = fragment<BCOLS, BN, CHUNK_BYTES>(cur + A_LDS, b0(wave) / 16 + y, s, lane);
+#pragma unroll
+                for (int x = 0; x < UA; ++x) {
+                    const i32x4 a = fragment<ACOLS, BM, M::A_BYTES>(cur, a0(wave) / 16 + x, s, lane);
+#pragma unroll
+                    for (int y = 0; y < UB; ++y) acc[x][y] = M::mma(a, b[y], acc[x][y]);
+                }
+                after(2 * c + s, acc);
+            }
+        }
+        __syncthreads();
+    }
+};
+
 // The same product for many tiles: 256 x 256, eight waves in two groups of four, one of
 // each group on every SIMD, half a phase apart.  While the waves of one group feed the matrix cores
 // (16 MFMAs a phase, at raised priority), those of the other read the fragments of
@@ -209,10 +290,11 @@ __device__ inline void bare_barrier() {
 // read it, and the same half of the chunk after next is loaded over it: B0 in phase 1, A0 and A1 in
 // phase 2, B1 in phase 3, five phases or more before they are read.  Loads past the last
 // chunk read it again, so that the waits can count.
-template <typename M>
+template <typename M, bool ACOLS = false, bool BCOLS = false>
 struct BigTile {
     static constexpr int THREADS = 512, ROWS = 256, COLS = 256;
     static constexpr int A_LDS = ROWS * M::A_BYTES, B_LDS = COLS * CHUNK_BYTES;
+    static constexpr int A_HALF = A_LDS / 2, B_HALF = B_LDS / 2;
     static constexpr int LDS = 2 * (A_LDS + B_LDS);
     static constexpr int NA = M::A_BYTES / 64;   // loads of a half of A by a wave (of B: 2)
     typedef M Mma;
@@ -223,110 +305,109 @@ struct BigTile {
     static __device__ inline int b0(int wave) { return (wave >> 2) * 128; }
     static __device__ inline Acc& at(Accs& acc, int a, int b) { return acc[b][a]; }
 
-    // One operand's loads: 32-bit offsets of this lane's pieces from a base that moves
-    // on with the chunks.
-    template <int BYTES, int N>
-    struct Source {
-        const char* base;
-        uint32_t off[2][N];   // [half][load]
-        int piece;
+    // A half of an operand, in LDS 128 rows (or 64 rows of 128 columns): G groups of
+    // 128 / G of them, those of half h being at 256 / G * g + 128 / G * h in the tile.
+    template <bool C, int BYTES, int G, int N>
+    struct Half {
+        Source<C, BYTES, N> s[2];
+        static __device__ inline int tile_index(int h, int j) {   // j of the half's 128
+            return j / (128 / G) * (256 / G) + h * (128 / G) + j % (128 / G);
+        }
+        template <typename RowFn>
+        __device__ inline void init(const Operand& o, int64_t first, int chunks, int wave, int lane,
+                                    RowFn row) {
+            constexpr int PIECES = C ? 16 : BYTES / 16, PER = 64 / PIECES;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                s[h].init(o, first, chunks);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int r = (i * 8 + wave) * PER + lane / PIECES, slot = lane % PIECES;
+                    if constexpr (C) {
+                        const int unit = (slot >> 1) ^ col_twist<8>(r);
+                        s[h].set_col(i, o, first, r, tile_index(h, unit * 16) + (slot & 1) * 8);
+                    } else {
+                        s[h].set_row(i, o, first, row(tile_index(h, r)), row_piece<BYTES>(r, slot) * 16);
+                    }
+                }
+            }
+        }
+        __device__ inline void load(int h, int chunk, char* lds, int wave) const {
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[h].load(i, chunk, lds + (i * 8 + wave) * 1024);
+        }
     };
-    static __device__ inline int load_row_b(int half, int i, int wave) {   // first of 8 rows
-        return i * 128 + half * 64 + wave * 8;
-    }
-    static __device__ inline int load_row_a(int half, int i, int wave) {   // of 8, or of 16 of 64 bytes
-        return M::A_BYTES == CHUNK_BYTES ? i * 128 + wave / 4 * 64 + half * 32 + wave % 4 * 8
-                                         : wave / 2 * 64 + half * 32 + wave % 2 * 16;
-    }
-    template <int BYTES, int N>
-    static __device__ inline void load(const Source<BYTES, N>& s, int half, char* lds, int row_of_load,
-                                       int i, int chunk, int last, int64_t end) {
-        char* const to = lds + row_of_load * BYTES;
-        const int c = min(chunk, last);
-        const char* base = s.base + (int64_t)c * BYTES;
-        const char* p = base + s.off[half][i];
-        if ((int64_t)(c + 1) * BYTES > end && (int64_t)c * BYTES + s.piece >= end)
-            p = reinterpret_cast<const char*>(&tile_zeros);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                         (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-    }
+    // Byte offsets in a half of this lane's reads: rows, per step; columns, per unit.
+    template <bool C, int BYTES, int U>
+    struct Reads {
+        int at[C ? U : 2];
+        __device__ inline void init(int unit0, int lane) {   // the wave's first unit of the half
+            const int r16 = lane & 15, kq = lane >> 4;
+            if constexpr (C) {
+                const int k = kq * 8 + (r16 >> 2);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    at[u] = k * 256 + (((unit0 + u) ^ col_twist<8>(k)) << 5) + (r16 & 3) * 8;
+            } else {
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const int k = st * 4 + kq;
+                    at[st] = (unit0 * 16 + r16) * BYTES +
+                             (BYTES == CHUNK_BYTES
+                                  ? row_piece<BYTES>(r16, k) << 4
+                                  : (row_piece<BYTES>(r16, k >> 1) << 4) + ((k & 1) << 3));
+                }
+            }
+        }
+        __device__ inline i32x4 get(const char* half, int u, int st) const {
+            if constexpr (C) {
+                const char* const p = half + at[u] + st * (32 * 256);
+                const i32x2 x = read_transposed(p), y = read_transposed(p + 4 * 256);
+                return i32x4{x[0], x[1], y[0], y[1]};
+            } else {
+                const char* const p = half + at[st] + u * 16 * BYTES;
+                if constexpr (BYTES == CHUNK_BYTES)
+                    return *reinterpret_cast<const i32x4*>(p);
+                else
+                    return unpack_codes(*reinterpret_cast<const i32x2*>(p));
+            }
+        }
+    };
 
-    // base_a, base_b: where the tile's rows begin; off_a(r), off_b(r): bytes from there to
-    // row r (rows of one load share base_a).  All rows are read up to a_end, b_end bytes.
-    template <typename OffA, typename OffB, typename After>
-    static __device__ inline void run(char* lds, const char* base_a, const char* base_b, OffA off_a,
-                                      OffB off_b, int64_t a_end, int64_t b_end, int chunks, Accs& acc,
-                                      After after) {
+    // Arguments as of Tile::run (without `after`).  The 8 or 16 rows of A that one load
+    // stages have to lie in one matrix: row_a may choose oa.base by the wave.
+    template <typename RowA>
+    static __device__ inline void run(char* lds, const Operand& oa, int64_t ia, const Operand& ob,
+                                      int64_t ib, int chunks, Accs& acc, RowA row_a) {
         const int tid = threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int group = wave >> 2;
         constexpr int BUF = A_LDS + B_LDS;
-        Source<M::A_BYTES, NA> sa;
-        Source<CHUNK_BYTES, 2> sb;
-        sa.base = base_a;
-        sb.base = base_b;
-        {
-            constexpr int PR = M::A_BYTES / 16;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < NA; ++i) {
-                    const int r = load_row_a(h, i, wave) + lane / PR;
-                    sa.piece = Stager<256, M::A_BYTES, 8>::permuted(r, lane % PR) * 16;
-                    sa.off[h][i] = off_a(r) + sa.piece;
-                }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = load_row_b(h, i, wave) + lane / 8;
-                    sb.piece = Stager<256, CHUNK_BYTES, 8>::permuted(r, lane % 8) * 16;
-                    sb.off[h][i] = off_b(r) + sb.piece;
-                }
-        }
-        const int last = chunks - 1;
+        Half<ACOLS, M::A_BYTES, 4, NA> ha;
+        Half<BCOLS, CHUNK_BYTES, 2, 2> hb;
+        ha.init(oa, ia, chunks, wave, lane, row_a);
+        hb.init(ob, ib, chunks, wave, lane, [](int r) { return r; });
+        Reads<ACOLS, M::A_BYTES, 2> ra;
+        Reads<BCOLS, CHUNK_BYTES, 4> rb;
+        ra.init((wave & 3) * 2, lane);
+        rb.init(group * 4, lane);
         auto load_a = [&](int half, int c) {
-            char* const to = lds + (c & 1) * BUF;
-#pragma unroll
-            for (int i = 0; i < NA; ++i)
-                load(sa, half, to, load_row_a(half, i, wave), i, c, last, a_end);
+            ha.load(half, c, lds + (c & 1) * BUF + half * A_HALF, wave);
         };
         auto load_b = [&](int half, int c) {
-            char* const to = lds + (c & 1) * BUF + A_LDS;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                load(sb, half, to, load_row_b(half, i, wave), i, c, last, b_end);
+            hb.load(half, c, lds + (c & 1) * BUF + A_LDS + half * B_HALF, wave);
         };
-        const int r16 = lane & 15, kq = lane >> 4;
-        // byte offsets of the fragments of the two steps of a chunk in a row
-        int fa[2], fb[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int k = s * 4 + kq;
-            fb[s] = A_LDS + (b0(wave) + r16) * CHUNK_BYTES + ((k ^ (r16 & 7)) << 4);
-            fa[s] = (a0(wave) + r16) * M::A_BYTES +
-                    (M::A_BYTES == CHUNK_BYTES
-                         ? (k ^ (r16 & 7)) << 4
-                         : (((k >> 1) ^ ((r16 >> 2) & 3)) << 4) | ((k & 1) << 3));
-        }
         auto read_a = [&](int half, const char* buf, i32x4 (&a)[2][2]) {
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const char* const p = buf + fa[s] + (half * 2 + y) * 16 * M::A_BYTES;
-                    if constexpr (M::A_BYTES == CHUNK_BYTES)
-                        a[y][s] = *reinterpret_cast<const i32x4*>(p);
-                    else
-                        a[y][s] = unpack_codes(*reinterpret_cast<const i32x2*>(p));
-                }
+                for (int s = 0; s < 2; ++s) a[y][s] = ra.get(buf + half * A_HALF, y, s);
         };
         auto read_b = [&](int half, const char* buf, i32x4 (&b)[4][2]) {
 #pragma unroll
             for (int x = 0; x < 4; ++x)
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
-                    b[x][s] = *reinterpret_cast<const i32x4*>(buf + fb[s] + (half * 4 + x) * 16 * CHUNK_BYTES);
+                for (int s = 0; s < 2; ++s) b[x][s] = rb.get(buf + A_LDS + half * B_HALF, x, s);
         };
         i32x4 a_0[2][2], a_1[2][2], b_[4][2];
         auto products = [&](const i32x4 (&a)[2][2], int ha, int hb) {
@@ -383,7 +464,6 @@ struct BigTile {
             wait_lds();
             bare_barrier();
             products(a_0, 0, 1);
-            after(c, acc);
             bare_barrier();
 #pragma unroll
             for (int y = 0; y < 2; ++y)
@@ -391,9 +471,43 @@ struct BigTile {
                 for (int s = 0; s < 2; ++s) a_0[y][s] = a_n[y][s];
         }
         if (group == 0) bare_barrier();
-        wait_loads<0>();   // none may land after the workgroup has gone
+        wait_loads<0>();   // the loads past the last chunk
+        __syncthreads();
     }
 };
+
+// Hands a wave's part of D on in rows: the four consecutive i of one t that a lane holds
+// go through LDS (4 KiB a wave, permuted like the operands), and come back eight at a
+// time, neighbouring lanes holding neighbouring ones, so that global memory is read and
+// written in whole lines.  get(a, b): the accumulator of units a, b as fp32.
+template <typename Tl, typename Get>
+struct Handover {
+    static constexpr int SLOTS = Tl::UA * 4;   // 16-byte slots of a t
+    char* lds;
+    int lane;
+    Get get;
+    __device__ inline void put(int b) const {
+        const int t = lane & 15;
+#pragma unroll
+        for (int a = 0; a < Tl::UA; ++a)
+            *reinterpret_cast<f32x4*>(lds + t * (SLOTS * 16) + (((a * 4 + (lane >> 4)) ^ (t & (SLOTS - 1))) << 4)) =
+                get(a, b);
+    }
+    // i = 8 p .. 8 p + 7 of row t of the unit put last
+    __device__ inline void take(int t, int p, float (&v)[8]) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(
+                lds + t * (SLOTS * 16) + (((2 * p + h) ^ (t & (SLOTS - 1))) << 4));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * h + j] = x[j];
+        }
+    }
+};
+template <typename Tl, typename Get>
+__device__ inline Handover<Tl, Get> handover(char* lds, int wave, int lane, Get get) {
+    return Handover<Tl, Get>{lds + wave * (Tl::UA * 1024), lane, get};
+}
 
 // Workgroup v runs on XCD v mod 8, each with an L2 of its own: every XCD takes a
 // contiguous range of the tiles, which go down strips `strip` tiles wide.
@@ -407,47 +521,52 @@ __device__ inline void tile_of(int v, int ni, int nt, int strip, int* i, int* t)
     *t = in / w;
 }
 
-// Four consecutive outputs, `valid` of them inside the row.
+// Eight consecutive entries, `valid` of them inside the row.
 template <typename E>
-__device__ inline void store4(E* p, const float (&v)[4], int64_t valid) {
-    if (valid >= 4) {
-        Pack<E, 4> o;
+__device__ inline void store8(E* p, const float (&v)[8], int64_t valid) {
+    if (valid >= 8) {
+        Pack<E, 8> o;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o.v[j] = (E)v[j];
+        for (int j = 0; j < 8; ++j) o.v[j] = (E)v[j];
         store_pack(p, o);
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 8; ++j)
             if (j < valid) p[j] = (E)v[j];
     }
 }
 template <typename E>
-__device__ inline void load4(const E* p, float (&v)[4], int64_t valid) {
-    if (valid >= 4) {
-        const auto o = load_pack<E, 4>(p);
+__device__ inline void load8(const E* p, float (&v)[8], int64_t valid) {
+    if (valid >= 8) {
+        const auto o = load_pack<E, 8>(p);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = (float)o.v[j];
+        for (int j = 0; j < 8; ++j) v[j] = (float)o.v[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = j < valid ? (float)p[j] : 0.0f;
+        for (int j = 0; j < 8; ++j) v[j] = j < valid ? (float)p[j] : 0.0f;
     }
 }
 
-// Activations and their slopes in fp32, with the library's exp and erf.
+// Activations and their slopes in fp32: the hardware's exp2 and reciprocal (1 ulp each), the
+// library's erf.
+__device__ inline float sigmoid(float z) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896340736f));
+}
 __device__ inline float act_value(float z, int act) {
-    if (act == BAKRON_ACT_SILU) return z / (1.0f + expf(-z));
+    if (act == BAKRON_ACT_SILU) return z * sigmoid(z);
     if (act == BAKRON_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
     return z;
 }
 __device__ inline void act_both(float z, int act, float* value, float* slope) {
     if (act == BAKRON_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-z));
+        const float s = sigmoid(z);
         *value = z * s;
         *slope = s * (1.0f + z * (1.0f - s));
     } else {
         const float c = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
         *value = z * c;
-        *slope = c + z * 0.39894228040143268f * expf(-0.5f * z * z);
+        *slope = c + z * 0.39894228040143268f *
+                         __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.44269504088896340736f));
     }
 }
 
