@@ -105,9 +105,18 @@ inline Operand operand(const void* base, int64_t ld, int64_t n, int64_t k_end) {
     return Operand{static_cast<const char*>(base), nullptr, ld, n, k_end, 0};
 }
 
-__device__ inline void load_lds(const char* p, char* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+__device__ inline uint32_t lds_address(char* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)p;
+}
+// 16 bytes a lane from p to LDS address `to` (the same in all lanes) + 16 * lane.  In
+// assembly because the compiler waits for every load of its own before a transposing LDS
+// read, which it cannot tell from the place being loaded; all waits are wait_loads().  It
+// writes no register.
+__device__ inline void load_lds(const char* p, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(
+                     __builtin_amdgcn_readfirstlane(to)),
+                 "v"(p)
+                 : "memory", "m0");
 }
 template <int N>
 __device__ inline void wait_loads() {   // all but the last N of this wave's
@@ -134,7 +143,7 @@ struct Source {
     int at[N];           // Columns: row in the chunk; rows: at[0] the piece's byte
     int64_t end;         // k_end
 
-    __device__ inline void load(int i, int chunk, char* to) const {
+    __device__ inline void load(int i, int chunk, uint32_t to) const {
         int c = min(chunk, last);   // (past the last chunk: that one again, not used)
         const char* b = base;
         if (split > 0 && c >= split) {
@@ -211,7 +220,7 @@ struct Tile {
                 }
             }
         }
-        __device__ inline void load(int chunk, char* lds, int wave) const {
+        __device__ inline void load(int chunk, uint32_t lds, int wave) const {
 #pragma unroll
             for (int i = 0; i < N; ++i) s.load(i, chunk, lds + (i * WAVES + wave) * 1024);
         }
@@ -247,13 +256,14 @@ struct Tile {
         Loads<BCOLS, BN, CHUNK_BYTES> lb;
         la.init(oa, ia, chunks, wave, lane, row_a);
         lb.init(ob, ib, chunks, wave, lane, [](int r) { return r; });
+        const uint32_t base = lds_address(lds);
         if (chunks > 0) {
-            la.load(0, lds, wave);
-            lb.load(0, lds + A_LDS, wave);
+            la.load(0, base, wave);
+            lb.load(0, base + A_LDS, wave);
         }
         for (int c = 0; c < chunks; ++c) {
-            char* const cur = lds + (c & 1) * (A_LDS + B_LDS);
-            char* const nxt = lds + ((c + 1) & 1) * (A_LDS + B_LDS);
+            const char* const cur = lds + (c & 1) * (A_LDS + B_LDS);
+            const uint32_t nxt = base + ((c + 1) & 1) * (A_LDS + B_LDS);
             wait_loads<0>();
             __syncthreads();   // everybody's loads landed, and the other buffer is free
             if (c + 1 < chunks) {
@@ -332,7 +342,7 @@ struct BigTile {
                 }
             }
         }
-        __device__ inline void load(int h, int chunk, char* lds, int wave) const {
+        __device__ inline void load(int h, int chunk, uint32_t lds, int wave) const {
 #pragma unroll
             for (int i = 0; i < N; ++i) s[h].load(i, chunk, lds + (i * 8 + wave) * 1024);
         }
@@ -391,11 +401,12 @@ struct BigTile {
         Reads<BCOLS, CHUNK_BYTES, 4> rb;
         ra.init((wave & 3) * 2, lane);
         rb.init(group * 4, lane);
+        const uint32_t base = lds_address(lds);
         auto load_a = [&](int half, int c) {
-            ha.load(half, c, lds + (c & 1) * BUF + half * A_HALF, wave);
+            ha.load(half, c, base + (c & 1) * BUF + half * A_HALF, wave);
         };
         auto load_b = [&](int half, int c) {
-            hb.load(half, c, lds + (c & 1) * BUF + A_LDS + half * B_HALF, wave);
+            hb.load(half, c, base + (c & 1) * BUF + A_LDS + half * B_HALF, wave);
         };
         auto read_a = [&](int half, const char* buf, i32x4 (&a)[2][2]) {
 #pragma unroll
