@@ -23,30 +23,34 @@ struct LinearArgs {
     int ni, nt;              // tiles
 };
 
-// y_t,i..i+7 from the sums z (scales applied) and the bias.
-template <typename E>
-__device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, float (&z)[8]) {
+// Rows up to which a product is taken as one of few rows.
+constexpr int64_t FEW_ROWS = 64;
+
+// y_t,i..i+N-1 from the sums z (scales applied).
+template <typename E, int N>
+__device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, float (&z)[N]) {
     const int64_t valid = a.m - i;
-    float v[8];
+    float v[N];
     if (a.bias) {
-        load8(static_cast<const E*>(a.bias) + i, v, valid);
+        load_n(static_cast<const E*>(a.bias) + i, v, valid);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] += v[j];
+        for (int j = 0; j < N; ++j) z[j] += v[j];
     }
     if (a.act != BAKRON_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = act_value(z[j], a.act);
+        for (int j = 0; j < N; ++j) z[j] = act_value(z[j], a.act);
     }
     if (a.combine != BAKRON_COMBINE_NONE) {
-        load8(static_cast<const E*>(a.other) + t * a.ldo + i, v, valid);
+        load_n(static_cast<const E*>(a.other) + t * a.ldo + i, v, valid);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = a.combine == BAKRON_COMBINE_ADD ? z[j] + v[j] : z[j] * v[j];
+        for (int j = 0; j < N; ++j) z[j] = a.combine == BAKRON_COMBINE_ADD ? z[j] + v[j] : z[j] * v[j];
     }
-    store8(static_cast<E*>(a.y) + t * a.ldy + i, z, valid);
+    store_n(static_cast<E*>(a.y) + t * a.ldy + i, z, valid);
 }
 
-template <typename Tl, bool GROUPED>
+template <typename Tl, int FLUSH>
 __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
+    constexpr bool GROUPED = FLUSH > 0;
     typedef typename Tl::Mma M;
     __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
     int ti, tt;
@@ -61,38 +65,14 @@ __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
     const Operand q{reinterpret_cast<const char*>(a.q), nullptr, a.ldq, a.T,
                     (int64_t)a.chunks * CHUNK_BYTES, 0};
     auto same = [](int r) { return r; };
-    if constexpr (GROUPED) {
-        const int64_t iw = i0 + Tl::a0(wave) + (lane >> 4) * 4;
-        const int last = 2 * a.chunks - 1;
-        int left = a.gsteps, g = 0;
-        auto after = [&](int step, typename Tl::Accs& acc) {
-            if (--left > 0 && step != last) return;
-            left = a.gsteps;
-            if (g < a.ngroups) {   // (past them only padding, whose sums are 0)
-#pragma unroll
-                for (int x = 0; x < Tl::UA; ++x) {
-                    f32x4 s;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        s[j] = a.scale[min(iw + x * 16 + j, a.m - 1) * a.ngroups + g];
-#pragma unroll
-                    for (int y = 0; y < Tl::UB; ++y) {
-                        i32x4& p = Tl::at(acc, x, y);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            sum[x][y][j] = fmaf((float)p[j], s[j], sum[x][y][j]);
-                        p = i32x4{0, 0, 0, 0};
-                    }
-                }
-            }
-            ++g;
-        };
-        Tl::run(lds, w, i0, q, t0, a.chunks, acc, same, after);
-    } else if constexpr (Tl::THREADS == 512) {
+    if constexpr (GROUPED)
+        Tl::run(lds, w, i0, q, t0, a.chunks, acc, same, sum, [&](int r, int c, int k) {
+            // (groups past the last one hold only padding, whose sums are 0)
+            const int g = min((2 * c + k * FLUSH) / a.gsteps, a.ngroups - 1);
+            return a.scale + min(i0 + r, a.m - 1) * a.ngroups + g;
+        });
+    else
         Tl::run(lds, w, i0, q, t0, a.chunks, acc, same);
-    } else {
-        Tl::run(lds, w, i0, q, t0, a.chunks, acc, same, [](int, typename Tl::Accs&) {});
-    }
 
     auto get = [&](int x, int y) {
         if constexpr (GROUPED) {
@@ -107,7 +87,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
     const int p = lane % PER;
     const int64_t i = i0 + Tl::a0(wave) + p * 8;
     float s[8];
-    if (!GROUPED) load8(a.scale + min(i, a.m), s, a.m - i);
+    if (!GROUPED) load_n(a.scale + min(i, a.m), s, a.m - i);
 #pragma unroll
     for (int y = 0; y < Tl::UB; ++y) {
         rows.put(y);
@@ -130,22 +110,191 @@ __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
     }
 }
 
-template <typename Tl, bool GROUPED>
+// Few rows (a decoding step): bound by reading the codes once, so no tile is staged.  A
+// workgroup takes R units of 16 rows of codes and Y of 16 rows of q; its waves share the row's
+// steps of 64 codes, U at a time in turn, every fragment straight from memory into
+// registers, the next U steps' before the products of these.  The partial sums meet in LDS.
+template <typename M, bool GROUPED, int R, int Y, int U>
+__global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
+    constexpr int STEP = M::A_BYTES / 2;      // bytes of codes a step
+    constexpr bool NARROW = M::A_BYTES != CHUNK_BYTES;
+    constexpr float UNIT = NARROW ? 1.0f / 16.0f : 1.0f;
+    extern __shared__ __attribute__((aligned(16))) char few_lds[];
+    // scales as [group][row], then the partial sums as [wave][r][y][lane]
+    float* const scales = reinterpret_cast<float*>(few_lds);
+    const int nscales = GROUPED ? a.ngroups * R * 16 : 0;
+    const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, kq = lane >> 4;
+    const int64_t i0 = (int64_t)blockIdx.x * (R * 16);
+    const int64_t t0 = (int64_t)blockIdx.y * (Y * 16);
+    const int nsteps = 2 * a.chunks;
+
+    const char* w[R];
+    const char* q[Y];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        w[r] = a.w + min(i0 + r * 16 + r16, a.m - 1) * a.ldw + kq * (STEP / 4);
+#pragma unroll
+    for (int y = 0; y < Y; ++y)
+        q[y] = reinterpret_cast<const char*>(a.q) + min(t0 + y * 16 + r16, a.T - 1) * a.ldq + kq * 16;
+
+    typedef typename std::conditional<NARROW, i32x2, i32x4>::type Codes;
+    struct Block {
+        Codes w[U][R];
+        i32x4 q[U][Y];
+    };
+    auto load = [&](Block& b, int first) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = min(first + u, nsteps - 1);
+#pragma unroll
+            for (int r = 0; r < R; ++r) b.w[u][r] = *reinterpret_cast<const Codes*>(w[r] + s * STEP);
+#pragma unroll
+            for (int y = 0; y < Y; ++y) b.q[u][y] = *reinterpret_cast<const i32x4*>(q[y] + s * 64);
+        }
+    };
+    // (scales first: they are waited for first)
+    constexpr int SC = 4;
+    float sc[SC];
+    if constexpr (GROUPED) {
+#pragma unroll
+        for (int k = 0; k < SC; ++k) {
+            const int e = min(tid + k * (int)blockDim.x, nscales - 1);
+            sc[k] = a.scale[min(i0 + e / a.ngroups, a.m - 1) * a.ngroups + e % a.ngroups];
+        }
+    }
+    Block b;
+    load(b, wave * U);
+    if constexpr (GROUPED) {
+#pragma unroll
+        for (int k = 0; k < SC; ++k) {
+            const int e = tid + k * (int)blockDim.x;
+            if (e < nscales) scales[e % a.ngroups * (R * 16) + e / a.ngroups] = sc[k];
+        }
+        for (int e = tid + SC * blockDim.x; e < nscales; e += blockDim.x)
+            scales[e % a.ngroups * (R * 16) + e / a.ngroups] =
+                a.scale[min(i0 + e / a.ngroups, a.m - 1) * a.ngroups + e % a.ngroups];
+        wait_lds();
+        bare_barrier();
+    }
+    i32x4 acc[R][Y] = {};
+    f32x4 sum[R][Y] = {};
+    for (int first = wave * U; first < nsteps; first += waves * U) {
+        Block n;
+        load(n, first + waves * U);   // (past the end the last step again, not used)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (first + u >= nsteps) break;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                i32x4 c;
+                if constexpr (NARROW)
+                    c = unpack_codes(b.w[u][r]);
+                else
+                    c = b.w[u][r];
+                f32x4 s;
+                if constexpr (GROUPED)
+                    s = *reinterpret_cast<const f32x4*>(
+                        scales + min((first + u) / a.gsteps, a.ngroups - 1) * (R * 16) + r * 16 + kq * 4);
+#pragma unroll
+                for (int y = 0; y < Y; ++y) {
+                    if constexpr (GROUPED) {
+                        const i32x4 p = M::mma(c, b.q[u][y], i32x4{0, 0, 0, 0});
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sum[r][y][j] = fmaf((float)p[j], s[j], sum[r][y][j]);
+                    } else {
+                        acc[r][y] = M::mma(c, b.q[u][y], acc[r][y]);
+                    }
+                }
+            }
+        }
+        b = n;
+    }
+    char* const parts = few_lds + (nscales * 4 + 15) / 16 * 16;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int y = 0; y < Y; ++y) {
+            i32x4 v = acc[r][y];
+            if constexpr (GROUPED) v = __builtin_bit_cast(i32x4, sum[r][y]);
+            *reinterpret_cast<i32x4*>(parts + (((wave * R + r) * Y + y) * 64 + lane) * 16) = v;
+        }
+    __syncthreads();
+    for (int u = wave; u < R * Y; u += waves) {   // a wave joins one unit
+        const int r = u / Y, y = u % Y;
+        i32x4 p = {0, 0, 0, 0};
+        f32x4 f = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < waves; ++k) {
+            const i32x4 v = *reinterpret_cast<const i32x4*>(parts + ((k * R * Y + u) * 64 + lane) * 16);
+            if constexpr (GROUPED)
+                f += __builtin_bit_cast(f32x4, v);
+            else
+                p += v;
+        }
+        const int64_t t = t0 + y * 16 + r16, i = i0 + r * 16 + kq * 4;
+        if (t >= a.T || i >= a.m) continue;
+        const float qs = (a.q_scale ? a.q_scale[t] : 1.0f) * UNIT;
+        float z[4];
+        if constexpr (GROUPED) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] = f[j] * qs;
+        } else {
+            float s[4];
+            load_n(a.scale + i, s, a.m - i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] = (float)p[j] * (qs * s[j]);
+        }
+        if (a.dtype == BAKRON_F32)
+            linear_store<float>(a, t, i, z);
+        else if (a.dtype == BAKRON_F16)
+            linear_store<f16_t>(a, t, i, z);
+        else
+            linear_store<bf16_t>(a, t, i, z);
+    }
+}
+
+template <typename Tl, int FLUSH>
 static void launch_linear_tile(LinearArgs a, hipStream_t st) {
     a.ni = (int)((a.m + Tl::ROWS - 1) / Tl::ROWS);
     a.nt = (int)((a.T + Tl::COLS - 1) / Tl::COLS);
-    hipLaunchKernelGGL((k_linear<Tl, GROUPED>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
+    hipLaunchKernelGGL((k_linear<Tl, FLUSH>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
+}
+
+template <typename M, bool GROUPED, int R, int Y, int U>
+static void launch_linear_few(const LinearArgs& a, hipStream_t st) {
+    const dim3 grid((unsigned)((a.m + R * 16 - 1) / (R * 16)), (unsigned)((a.T + Y * 16 - 1) / (Y * 16)));
+    // as many waves as have work, 8 at most (4 with 8 units: 64 KiB of LDS)
+    const int blocks = (2 * a.chunks + U - 1) / U;
+    const int waves = blocks >= 8 && R * Y < 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
+    const int scales = GROUPED ? (a.ngroups * R * 16 * 4 + 15) / 16 * 16 : 0;
+    hipLaunchKernelGGL((k_linear_few<M, GROUPED, R, Y, U>), grid, dim3(64 * waves),
+                       scales + waves * R * Y * 1024, st, a);
 }
 
 template <typename M, bool GROUPED>
 static void launch_linear(const LinearArgs& a, hipStream_t st) {
     auto tiles = [&](int64_t b) { return ((a.m + b - 1) / b) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
-    if constexpr (!GROUPED) {
-        if (tiles(256) >= ncu) return launch_linear_tile<BigTile<M>, GROUPED>(a, st);
+    // (a row's scales have to fit beside the partial sums)
+    if (a.T <= FEW_ROWS && (!GROUPED || a.ngroups <= 256)) {
+        if (a.T <= 16) return launch_linear_few<M, GROUPED, 1, 1, 4>(a, st);
+        if (a.T <= 32) return launch_linear_few<M, GROUPED, 1, 2, 2>(a, st);
+        return launch_linear_few<M, GROUPED, 2, 4, 2>(a, st);
     }
-    if (tiles(128) >= ncu) return launch_linear_tile<Tile<M, 128, 128, 2, 2>, GROUPED>(a, st);
-    launch_linear_tile<Tile<M, 64, 64, 2, 2>, GROUPED>(a, st);
+    if constexpr (!GROUPED) {
+        if (tiles(256) >= ncu) return launch_linear_tile<BigTile<M>, 0>(a, st);
+        if (tiles(128) >= ncu) return launch_linear_tile<Tile<M, 128, 128, 2, 2, 3>, 0>(a, st);
+        return launch_linear_tile<Tile<M, 64, 64, 2, 2, 4>, 0>(a, st);
+    } else if (a.gsteps % 2 == 0) {   // a chunk of 128 codes is in one group
+        if (tiles(128) >= ncu)
+            return launch_linear_tile<Tile<M, 128, 128, 2, 4, 3, false, false, 2>, 2>(a, st);
+        launch_linear_tile<Tile<M, 64, 64, 2, 2, 4, false, false, 2>, 2>(a, st);
+    } else {
+        if (tiles(128) >= ncu)
+            return launch_linear_tile<Tile<M, 128, 128, 2, 4, 3, false, false, 1>, 1>(a, st);
+        launch_linear_tile<Tile<M, 64, 64, 2, 2, 4, false, false, 1>, 1>(a, st);
+    }
 }
 
 }  // namespace bk

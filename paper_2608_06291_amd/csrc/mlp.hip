@@ -39,15 +39,12 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
     typename Tl::Accs acc = {};
     // Tile row r: gate and up in turn, 16 and 16.  The rows that a wave loads are all of
     // one matrix: 8 at a time, multiples of 32 (or 64) apart.
-    const bool up = Tl::THREADS == 512 ? (wave >> 1) & 1 : (wave * 8 >> 4) & 1;
+    const bool up = (wave >> 1) & 1;
     Operand w = a.w;
     if (up) w.base = a.w.base2;
     const int64_t first = min(f0, a.f - 1);
     auto feature = [](int r) { return (r >> 5) * 16 + (r & 15); };
-    if constexpr (Tl::THREADS == 512)
-        Tl::run(lds, w, first, a.x, t0, a.chunks, acc, feature);
-    else
-        Tl::run(lds, w, first, a.x, t0, a.chunks, acc, feature, [](int, typename Tl::Accs&) {});
+    Tl::run(lds, w, first, a.x, t0, a.chunks, acc, feature);
 
     const auto rows =
         handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
@@ -73,21 +70,21 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
                     act_both(G[r], a.act, &v[r], &s[r]);
                     s[r] *= U[r];
                 }
-                store8(a.feat_gate + t * a.f + j, s, valid);
+                store_n(a.feat_gate + t * a.f + j, s, valid);
             } else {
 #pragma unroll
                 for (int r = 0; r < 8; ++r) v[r] = act_value(G[r], a.act);
             }
-            if (a.feat_up) store8(a.feat_up + t * a.f + j, v, valid);
+            if (a.feat_up) store_n(a.feat_up + t * a.f + j, v, valid);
             if (a.h) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r) v[r] *= U[r];
-                store8(static_cast<E*>(a.h) + t * a.ldh + j, v, valid);
+                store_n(static_cast<E*>(a.h) + t * a.ldh + j, v, valid);
             }
         } else {
             if (j >= a.fp) continue;
             float dh[8] = {}, dg[8], du[8];
-            if (valid > 0) load8(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, valid);
+            if (valid > 0) load_n(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, valid);
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
                 float v, s;
@@ -96,8 +93,8 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
                 du[r] = r < valid ? dh[r] * v : 0.0f;
             }
             E* const row = static_cast<E*>(a.dgu) + t * (2 * a.fp) + j;
-            store8(row, dg, 8);
-            store8(row + a.fp, du, 8);
+            store_n(row, dg, 8);
+            store_n(row + a.fp, du, 8);
         }
     }
 }
@@ -120,11 +117,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 
     typename Tl::Accs acc = {};
-    auto same = [](int r) { return r; };
-    if constexpr (Tl::THREADS == 512)
-        Tl::run(lds, a.a, i0, a.b, t0, a.chunks, acc, same);
-    else
-        Tl::run(lds, a.a, i0, a.b, t0, a.chunks, acc, same, [](int, typename Tl::Accs&) {});
+    Tl::run(lds, a.a, i0, a.b, t0, a.chunks, acc, [](int r) { return r; });
 
     const auto rows =
         handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
@@ -142,7 +135,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
             if (i >= a.d || t >= a.end || (t >= a.split && t < a.split2)) continue;
             E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
                                        : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
-            store8(row + i, v, a.d - i);
+            store_n(row + i, v, a.d - i);
         }
     }
 }
@@ -191,9 +184,9 @@ static void launch_gated(GatedArgs a, hipStream_t st) {
     if (tiles(256) >= ncu)
         go(BigTile<M>());
     else if (tiles(128) >= ncu)
-        go(Tile<M, 128, 128, 2, 2>());
+        go(Tile<M, 128, 128, 2, 2, 2>());
     else
-        go(Tile<M, 64, 64, 2, 2>());
+        go(Tile<M, 64, 64, 2, 2, 4>());
 }
 
 template <typename M, bool ACOLS, bool BCOLS>
@@ -209,9 +202,9 @@ static void launch_prod(ProdArgs a, hipStream_t st) {
     if (tiles(256) >= ncu)
         go(BigTile<M, ACOLS, BCOLS>());
     else if (tiles(128) >= ncu)
-        go(Tile<M, 128, 128, 2, 2, ACOLS, BCOLS>());
+        go(Tile<M, 128, 128, 2, 2, 2, ACOLS, BCOLS>());
     else
-        go(Tile<M, 64, 64, 2, 2, ACOLS, BCOLS>());
+        go(Tile<M, 64, 64, 2, 2, 4, ACOLS, BCOLS>());
 }
 
 // Padded copies of operands that cannot be staged as they are.

@@ -118,6 +118,13 @@ __device__ inline void load_lds(const char* p, uint32_t to) {
                  "v"(p)
                  : "memory", "m0");
 }
+// The same for 4 bytes a lane.
+__device__ inline void load_lds_word(const float* p, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(
+                     __builtin_amdgcn_readfirstlane(to)),
+                 "v"(p)
+                 : "memory", "m0");
+}
 template <int N>
 __device__ inline void wait_loads() {   // all but the last N of this wave's
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -180,15 +187,22 @@ struct Source {
     }
 };
 
-// The small tile: WM x WN waves, two buffers, one barrier a chunk.
-template <typename M, int BM, int BN, int WM, int WN, bool ACOLS = false, bool BCOLS = false>
+// The small tile: WM x WN waves, BUFS buffers, so that BUFS - 1 chunks are on their way
+// while one is multiplied, and one barrier a chunk.  FLUSH > 0: the sums of every FLUSH steps
+// (half chunks) are handed to `flush` and begin at zero again.
+template <typename M, int BM, int BN, int WM, int WN, int BUFS, bool ACOLS = false, bool BCOLS = false,
+          int FLUSH = 0>
 struct Tile {
+    static constexpr bool BIG = false;
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int ROWS = BM, COLS = BN;
     static constexpr int TM = BM / WM, TN = BN / WN;      // a wave's part
     static constexpr int UA = TM / 16, UB = TN / 16;      // in units of 16
     static constexpr int A_LDS = BM * M::A_BYTES, B_LDS = BN * CHUNK_BYTES;
-    static constexpr int LDS = 2 * (A_LDS + B_LDS);
+    // the scales of the chunk's 2 / FLUSH groups for every row of A
+    static constexpr int S_LDS = FLUSH ? 2 / FLUSH * BM * 4 : 0;
+    static constexpr int BUF = A_LDS + B_LDS + S_LDS;
+    static constexpr int LDS = BUFS * BUF;
     typedef M Mma;
     typedef typename M::Acc Acc;
     typedef Acc Accs[UA][UB];
@@ -245,11 +259,13 @@ struct Tile {
     }
 
     // The tile that begins at row `ia` of A and row `ib` of B; row_a maps rows of the tile to
-    // rows of the operand, counted from ia.  `after(step, acc)` runs when step `step` (half a
-    // chunk) has been added.  LDS is free to use again on return.
-    template <typename RowA, typename After>
+    // rows of the operand, counted from ia.  With FLUSH, scale(row, c, k) is the address of
+    // the scale of tile row `row` for the k-th FLUSH steps of chunk c, and what is flushed is
+    // sum[x][y] += acc * scale.  LDS is free to use again on return.
+    template <typename RowA, typename Scale>
     static __device__ inline void run(char* lds, const Operand& oa, int64_t ia, const Operand& ob,
-                                      int64_t ib, int chunks, Accs& acc, RowA row_a, After after) {
+                                      int64_t ib, int chunks, Accs& acc, RowA row_a,
+                                      f32x4 (&sum)[FLUSH ? UA : 1][FLUSH ? UB : 1], Scale scale) {
         const int tid = threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         Loads<ACOLS, BM, M::A_BYTES> la;
@@ -257,19 +273,31 @@ struct Tile {
         la.init(oa, ia, chunks, wave, lane, row_a);
         lb.init(ob, ib, chunks, wave, lane, [](int r) { return r; });
         const uint32_t base = lds_address(lds);
-        if (chunks > 0) {
-            la.load(0, base, wave);
-            lb.load(0, base + A_LDS, wave);
-        }
-        for (int c = 0; c < chunks; ++c) {
-            const char* const cur = lds + (c & 1) * (A_LDS + B_LDS);
-            const uint32_t nxt = base + ((c + 1) & 1) * (A_LDS + B_LDS);
-            wait_loads<0>();
-            __syncthreads();   // everybody's loads landed, and the other buffer is free
-            if (c + 1 < chunks) {
-                la.load(c + 1, nxt, wave);
-                lb.load(c + 1, nxt + A_LDS, wave);
+        constexpr int S_LOADS = FLUSH ? (2 / FLUSH * BM + THREADS - 1) / THREADS : 0;
+        constexpr int LOADS = la.N + lb.N + S_LOADS;   // of a chunk
+        auto load = [&](int c, int buf) {
+            const uint32_t to = base + buf * BUF;
+            la.load(c, to, wave);
+            lb.load(c, to + A_LDS, wave);
+            if constexpr (FLUSH > 0) {
+                // (with fewer scales than threads the waves past them load the same again)
+#pragma unroll
+                for (int i = 0; i < S_LOADS; ++i) {
+                    const int e = (i * WAVES + wave) * 64 % (2 / FLUSH * BM);
+                    load_lds_word(scale((e + lane) % BM, min(c, chunks - 1), e / BM),
+                                  to + A_LDS + B_LDS + e * 4);
+                }
             }
+        };
+#pragma unroll
+        for (int c = 0; c < BUFS - 1; ++c) load(c, c);   // (chunks past the last read it again)
+        int buf = 0;
+        for (int c = 0; c < chunks; ++c) {
+            const char* const cur = lds + buf * BUF;
+            wait_loads<(BUFS - 2) * LOADS>();
+            bare_barrier();   // everybody's loads of this chunk landed, and the buffer before is free
+            load(c + BUFS - 1, buf == 0 ? BUFS - 1 : buf - 1);
+            buf = buf == BUFS - 1 ? 0 : buf + 1;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 i32x4 b[UB];
@@ -279,13 +307,37 @@ struct Tile {
 #pragma unroll
                 for (int x = 0; x < UA; ++x) {
                     const i32x4 a = fragment<ACOLS, BM, M::A_BYTES>(cur, a0(wave) / 16 + x, s, lane);
+                    if constexpr (FLUSH > 0) {
+                        constexpr bool FIRST_ONLY = FLUSH == 1;
 #pragma unroll
-                    for (int y = 0; y < UB; ++y) acc[x][y] = M::mma(a, b[y], acc[x][y]);
+                        for (int y = 0; y < UB; ++y)
+                            acc[x][y] = M::mma(a, b[y], FIRST_ONLY || s == 0 ? Acc{} : acc[x][y]);
+                        if (FLUSH == 1 || s == 1) {
+                            const f32x4 sc = *reinterpret_cast<const f32x4*>(
+                                cur + A_LDS + B_LDS +
+                                ((FLUSH == 1 ? s * BM : 0) + a0(wave) + x * 16 + (lane >> 4) * 4) * 4);
+#pragma unroll
+                            for (int y = 0; y < UB; ++y)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    sum[x][y][j] = fmaf((float)acc[x][y][j], sc[j], sum[x][y][j]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int y = 0; y < UB; ++y) acc[x][y] = M::mma(a, b[y], acc[x][y]);
+                    }
                 }
-                after(2 * c + s, acc);
             }
         }
+        wait_loads<0>();   // the loads past the last chunk
         __syncthreads();
+    }
+    template <typename RowA>
+    static __device__ inline void run(char* lds, const Operand& oa, int64_t ia, const Operand& ob,
+                                      int64_t ib, int chunks, Accs& acc, RowA row_a) {
+        static_assert(FLUSH == 0, "scales missing");
+        f32x4 none[1][1];
+        run(lds, oa, ia, ob, ib, chunks, acc, row_a, none, [](int, int, int) { return (const float*)nullptr; });
     }
 };
 
@@ -302,6 +354,7 @@ struct Tile {
 // chunk read it again, so that the waits can count.
 template <typename M, bool ACOLS = false, bool BCOLS = false>
 struct BigTile {
+    static constexpr bool BIG = true;
     static constexpr int THREADS = 512, ROWS = 256, COLS = 256;
     static constexpr int A_LDS = ROWS * M::A_BYTES, B_LDS = COLS * CHUNK_BYTES;
     static constexpr int A_HALF = A_LDS / 2, B_HALF = B_LDS / 2;
@@ -384,7 +437,7 @@ struct BigTile {
         }
     };
 
-    // Arguments as of Tile::run (without `after`).  The 8 or 16 rows of A that one load
+    // Arguments as of Tile::run.  The 8 or 16 rows of A that one load
     // stages have to lie in one matrix: row_a may choose oa.base by the wave.
     template <typename RowA>
     static __device__ inline void run(char* lds, const Operand& oa, int64_t ia, const Operand& ob,
@@ -532,29 +585,29 @@ __device__ inline void tile_of(int v, int ni, int nt, int strip, int* i, int* t)
     *t = in / w;
 }
 
-// Eight consecutive entries, `valid` of them inside the row.
-template <typename E>
-__device__ inline void store8(E* p, const float (&v)[8], int64_t valid) {
-    if (valid >= 8) {
-        Pack<E, 8> o;
+// N consecutive entries, `valid` of them inside the row.
+template <typename E, int N>
+__device__ inline void store_n(E* p, const float (&v)[N], int64_t valid) {
+    if (valid >= N) {
+        Pack<E, N> o;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o.v[j] = (E)v[j];
+        for (int j = 0; j < N; ++j) o.v[j] = (E)v[j];
         store_pack(p, o);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < N; ++j)
             if (j < valid) p[j] = (E)v[j];
     }
 }
-template <typename E>
-__device__ inline void load8(const E* p, float (&v)[8], int64_t valid) {
-    if (valid >= 8) {
-        const auto o = load_pack<E, 8>(p);
+template <typename E, int N>
+__device__ inline void load_n(const E* p, float (&v)[N], int64_t valid) {
+    if (valid >= N) {
+        const auto o = load_pack<E, N>(p);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (float)o.v[j];
+        for (int j = 0; j < N; ++j) v[j] = (float)o.v[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < valid ? (float)p[j] : 0.0f;
+        for (int j = 0; j < N; ++j) v[j] = j < valid ? (float)p[j] : 0.0f;
     }
 }
 
