@@ -509,7 +509,9 @@ bakron_status bakron_mlp_local_factors_iter(const float *x, const float *g, cons
  *     capturable into a graph; error messages via bakron_last_error();
  *   - workspaces by the protocol of the factor construction: with work == NULL
  *     the call stores the bytes it needs (possibly 0) in *work_bytes and does
- *     nothing else.  Where the need is 0 any non-NULL work is accepted.
+ *     nothing else (it depends on the alignment of the operands and on which are
+ *     NULL, so ask with those of the call).  Where the need is 0 any non-NULL work is
+ *     accepted.
  * ------------------------------------------------------------------------ */
 
 typedef enum {

@@ -66,13 +66,13 @@ __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
                     (int64_t)a.chunks * CHUNK_BYTES, 0};
     auto same = [](int r) { return r; };
     if constexpr (GROUPED)
-        Tl::run(lds, w, i0, q, t0, a.chunks, acc, same, sum, [&](int r, int c, int k) {
+        Tl::run(lds, w, i0, q, t0, 0, a.chunks, acc, same, sum, [&](int r, int c, int k) {
             // (groups past the last one hold only padding, whose sums are 0)
             const int g = min((2 * c + k * FLUSH) / a.gsteps, a.ngroups - 1);
             return a.scale + min(i0 + r, a.m - 1) * a.ngroups + g;
         });
     else
-        Tl::run(lds, w, i0, q, t0, a.chunks, acc, same);
+        Tl::run(lds, w, i0, q, t0, 0, a.chunks, acc, same);
 
     auto get = [&](int x, int y) {
         if constexpr (GROUPED) {

@@ -26,6 +26,55 @@ struct GatedArgs {
     int64_t fp;
 };
 
+// What few rows need beside that: x and the weights as they are, in entries.
+struct FewArgs {
+    const void *x, *wg, *wu;
+    int64_t ldx, ldw;
+    int d;
+};
+
+// Row t, features j .. j + N - 1, from G and U.
+template <typename E, bool BWD, int N>
+__device__ inline void gated_finish(const GatedArgs& a, int64_t t, int64_t j, const float (&G)[N],
+                                    const float (&U)[N]) {
+    const int64_t valid = a.f - j;
+    if constexpr (!BWD) {
+        if (valid <= 0) return;
+        float v[N], s[N];
+        if (a.feat_gate) {
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                act_both(G[r], a.act, &v[r], &s[r]);
+                s[r] *= U[r];
+            }
+            store_n(a.feat_gate + t * a.f + j, s, valid);
+        } else {
+#pragma unroll
+            for (int r = 0; r < N; ++r) v[r] = act_value(G[r], a.act);
+        }
+        if (a.feat_up) store_n(a.feat_up + t * a.f + j, v, valid);
+        if (a.h) {
+#pragma unroll
+            for (int r = 0; r < N; ++r) v[r] *= U[r];
+            store_n(static_cast<E*>(a.h) + t * a.ldh + j, v, valid);
+        }
+    } else {
+        if (j >= a.fp) return;
+        float dh[N] = {}, dg[N], du[N];
+        if (valid > 0) load_n(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, valid);
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            float v, s;
+            act_both(G[r], a.act, &v, &s);
+            dg[r] = r < valid ? dh[r] * U[r] * s : 0.0f;   // (0 in the padding, whatever G is)
+            du[r] = r < valid ? dh[r] * v : 0.0f;
+        }
+        E* const row = static_cast<E*>(a.dgu) + t * (2 * a.fp) + j;
+        store_n(row, dg, N);
+        store_n(row + a.fp, du, N);
+    }
+}
+
 template <typename Tl, bool BWD>
 __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
     typedef typename Tl::Mma::Elem E;
@@ -44,13 +93,13 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
     if (up) w.base = a.w.base2;
     const int64_t first = min(f0, a.f - 1);
     auto feature = [](int r) { return (r >> 5) * 16 + (r & 15); };
-    Tl::run(lds, w, first, a.x, t0, a.chunks, acc, feature);
+    Tl::run(lds, w, first, a.x, t0, 0, a.chunks, acc, feature);
 
     const auto rows =
         handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
     constexpr int PER = Tl::UA;   // lanes a row: 8 features each
     const int p = lane % PER;
-    const int64_t j = f0 + Tl::a0(wave) / 2 + p * 8, valid = a.f - j;
+    const int64_t j = f0 + Tl::a0(wave) / 2 + p * 8;
 #pragma unroll
     for (int y = 0; y < Tl::UB; ++y) {
         rows.put(y);
@@ -61,41 +110,101 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
         rows.take(tl, (p >> 1) * 4 + (p & 1), G);
         rows.take(tl, (p >> 1) * 4 + (p & 1) + 2, U);
         if (t >= a.T) continue;
-        if constexpr (!BWD) {
-            if (valid <= 0) continue;
-            float v[8], s[8];
-            if (a.feat_gate) {
+        gated_finish<E, BWD>(a, t, j, G, U);
+    }
+}
+
+// Few rows (a decoding step): bound by reading the weights once.  A workgroup takes 16
+// features and Y units of 16 rows; its waves share the summed axis, U steps of 32 at a time in
+// turn, every fragment straight from memory (at any alignment) into registers, the next U steps'
+// before the products of these.  The partial sums meet in LDS.
+template <typename M, bool BWD, int Y, int U>
+__global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
+    typedef typename M::Elem E;
+    extern __shared__ __attribute__((aligned(16))) char few_lds[];
+    const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, kq = lane >> 4;
+    const int64_t j0 = (int64_t)blockIdx.x * 16, t0 = (int64_t)blockIdx.y * (Y * 16);
+    const int64_t jr = min(j0 + r16, a.f - 1);
+    const E* const wg = static_cast<const E*>(f.wg) + jr * f.ldw + kq * 8;
+    const E* const wu = static_cast<const E*>(f.wu) + jr * f.ldw + kq * 8;
+    const E* x[Y];
 #pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    act_both(G[r], a.act, &v[r], &s[r]);
-                    s[r] *= U[r];
-                }
-                store_n(a.feat_gate + t * a.f + j, s, valid);
-            } else {
+    for (int y = 0; y < Y; ++y)
+        x[y] = static_cast<const E*>(f.x) + min(t0 + y * 16 + r16, a.T - 1) * f.ldx + kq * 8;
+    const int nsteps = f.d / 32;   // whole ones; what is left goes to the last wave
+
+    struct Block {
+        u32x4 g[U], u[U], x[U][Y];
+    };
+    auto load = [&](Block& b, int first) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] = act_value(G[r], a.act);
-            }
-            if (a.feat_up) store_n(a.feat_up + t * a.f + j, v, valid);
-            if (a.h) {
+        for (int i = 0; i < U; ++i) {
+            const int k = min(first + i, nsteps - 1) * 32;   // (past the end the last step, not used)
+            b.g[i] = load_words(wg + k);
+            b.u[i] = load_words(wu + k);
 #pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] *= U[r];
-                store_n(static_cast<E*>(a.h) + t * a.ldh + j, v, valid);
-            }
-        } else {
-            if (j >= a.fp) continue;
-            float dh[8] = {}, dg[8], du[8];
-            if (valid > 0) load_n(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, valid);
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                float v, s;
-                act_both(G[r], a.act, &v, &s);
-                dg[r] = r < valid ? dh[r] * U[r] * s : 0.0f;   // (0 in the padding, whatever G is)
-                du[r] = r < valid ? dh[r] * v : 0.0f;
-            }
-            E* const row = static_cast<E*>(a.dgu) + t * (2 * a.fp) + j;
-            store_n(row, dg, 8);
-            store_n(row + a.fp, du, 8);
+            for (int y = 0; y < Y; ++y) b.x[i][y] = load_words(x[y] + k);
         }
+    };
+    f32x4 G[Y] = {}, Up[Y] = {};
+    auto add = [&](u32x4 g, u32x4 u, const u32x4 (&v)[Y]) {
+#pragma unroll
+        for (int y = 0; y < Y; ++y) {
+            const i32x4 b = __builtin_bit_cast(i32x4, v[y]);
+            G[y] = M::mma(__builtin_bit_cast(i32x4, g), b, G[y]);
+            Up[y] = M::mma(__builtin_bit_cast(i32x4, u), b, Up[y]);
+        }
+    };
+    int first = wave * U;
+    if (first < nsteps) {
+        Block b;
+        load(b, first);
+        for (; first < nsteps; first += waves * U) {
+            Block n;
+            load(n, first + waves * U);
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                if (first + i >= nsteps) break;
+                add(b.g[i], b.u[i], b.x[i]);
+            }
+            b = n;
+        }
+    }
+    if (f.d % 32 != 0 && wave == waves - 1) {
+        const int k = nsteps * 32, left = f.d - k - kq * 8;   // entries of this lane's pieces
+        auto part = [&](const E* p) {
+            uint16_t v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = e < left ? __builtin_bit_cast(uint16_t, p[k + e]) : (uint16_t)0;
+            u32x4 r;
+            __builtin_memcpy(&r, v, 16);
+            return r;
+        };
+        u32x4 v[Y];
+#pragma unroll
+        for (int y = 0; y < Y; ++y) v[y] = part(x[y]);
+        add(part(wg), part(wu), v);
+    }
+#pragma unroll
+    for (int y = 0; y < Y; ++y) {
+        *reinterpret_cast<f32x4*>(few_lds + ((wave * Y + y) * 128 + lane) * 16) = G[y];
+        *reinterpret_cast<f32x4*>(few_lds + ((wave * Y + y) * 128 + 64 + lane) * 16) = Up[y];
+    }
+    __syncthreads();
+    for (int y = wave; y < Y; y += waves) {   // a wave joins one unit of rows
+        f32x4 g = {0.0f, 0.0f, 0.0f, 0.0f}, u = g;
+        for (int k = 0; k < waves; ++k) {
+            g += *reinterpret_cast<const f32x4*>(few_lds + ((k * Y + y) * 128 + lane) * 16);
+            u += *reinterpret_cast<const f32x4*>(few_lds + ((k * Y + y) * 128 + 64 + lane) * 16);
+        }
+        const int64_t t = t0 + y * 16 + r16;
+        float gv[4], uv[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) gv[r] = g[r], uv[r] = u[r];
+        if (t < a.T) gated_finish<E, BWD>(a, t, j0 + kq * 4, gv, uv);
     }
 }
 
@@ -105,19 +214,36 @@ struct ProdArgs {
     int64_t d;                     // columns of the output
     void *out, *out2;              // rows t < split of out; split2 <= t < end, of out2
     int64_t ldo, split, split2, end;
+    int parts, part_chunks;        // the summed axis in parts of so many chunks
+    float* partial;                // parts x end x dp, where there are several
+    int64_t dp;
 };
+
+template <typename E>
+__device__ inline void prod_store(const ProdArgs& a, int64_t t, int64_t i, const float (&v)[8]) {
+    if (t >= a.end || (t >= a.split && t < a.split2)) return;
+    E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
+                               : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
+    store_n(row + i, v, a.d - i);
+}
 
 template <typename Tl>
 __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
     typedef typename Tl::Mma::Elem E;
     __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
-    int ti, tt;
-    tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
+    int ti, tt, part = 0, chunks = a.chunks;
+    if (a.parts > 1) {
+        part = blockIdx.x % (uint32_t)a.parts;
+        tile_of(blockIdx.x / (uint32_t)a.parts, a.ni, a.nt, 8, &ti, &tt);
+        chunks = min(a.part_chunks, a.chunks - part * a.part_chunks);
+    } else {
+        tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
+    }
     const int64_t i0 = (int64_t)ti * Tl::ROWS, t0 = (int64_t)tt * Tl::COLS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 
     typename Tl::Accs acc = {};
-    Tl::run(lds, a.a, i0, a.b, t0, a.chunks, acc, [](int r) { return r; });
+    Tl::run(lds, a.a, i0, a.b, t0, part * a.part_chunks, chunks, acc, [](int r) { return r; });
 
     const auto rows =
         handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
@@ -132,12 +258,29 @@ __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
             const int64_t t = t0 + Tl::b0(wave) + y * 16 + tl;
             float v[8];
             rows.take(tl, p, v);
-            if (i >= a.d || t >= a.end || (t >= a.split && t < a.split2)) continue;
-            E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
-                                       : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
-            store_n(row + i, v, a.d - i);
+            if (i >= a.d || t >= a.end) continue;
+            if (a.parts > 1)
+                store_n(a.partial + (part * a.end + t) * a.dp + i, v, 8);
+            else
+                prod_store<E>(a, t, i, v);
         }
     }
+}
+
+// Sums the parts, in their order.
+template <typename E>
+__global__ __launch_bounds__(256) void k_prod_join(ProdArgs a) {
+    const int64_t per = a.dp / 8, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= a.end * per) return;
+    const int64_t t = e / per, i = e % per * 8;
+    if (i >= a.d) return;
+    float v[8] = {};
+    for (int p = 0; p < a.parts; ++p) {
+        const auto x = load_pack<float, 8>(a.partial + (p * a.end + t) * a.dp + i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += x.v[j];
+    }
+    prod_store<E>(a, t, i, v);
 }
 
 // dst[r][0 .. cols_p) = src[r][0 .. cols), zeros behind; 16-bit entries.
@@ -170,8 +313,22 @@ static bool direct_rows(const void* p, int64_t ld, int64_t cols) {
     return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && 2 * ld < TILE_LD_MAX;
 }
 
+// Rows up to which the gated product is taken as one of few rows.
+constexpr int64_t FEW_ROWS = 64;
+
+template <typename M, bool BWD, int Y, int U>
+static void launch_gated_few(const FewArgs& f, const GatedArgs& a, hipStream_t st) {
+    const dim3 grid((unsigned)(((BWD ? a.fp : a.f) + 15) / 16), (unsigned)((a.T + Y * 16 - 1) / (Y * 16)));
+    const int blocks = (f.d / 32 + U - 1) / U;   // as many waves as have work, 8 at most
+    const int waves = blocks >= 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
+    hipLaunchKernelGGL((k_gated_few<M, BWD, Y, U>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
+}
+
 template <typename M, bool BWD>
-static void launch_gated(GatedArgs a, hipStream_t st) {
+static void launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
+    if (a.T <= 16) return launch_gated_few<M, BWD, 1, 4>(few, a, st);
+    if (a.T <= 32) return launch_gated_few<M, BWD, 2, 2>(few, a, st);
+    if (a.T <= FEW_ROWS) return launch_gated_few<M, BWD, 4, 2>(few, a, st);
     const int64_t f = BWD ? a.fp : a.f;   // (the padding is written, too)
     auto tiles = [&](int64_t b) { return ((f + b / 2 - 1) / (b / 2)) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
@@ -189,22 +346,46 @@ static void launch_gated(GatedArgs a, hipStream_t st) {
         go(Tile<M, 64, 64, 2, 2, 4>());
 }
 
+// How a product is cut: tile edge, and parts of the summed axis where the tiles alone
+// leave CUs idle (each part of 8 chunks at least).
+struct ProdPlan {
+    int tile, parts, part_chunks;
+    size_t bytes;   // of the partial sums
+};
+static ProdPlan prod_plan(int64_t i, int64_t t, int chunks, int ncu) {
+    auto tiles = [&](int64_t b) { return ((i + b - 1) / b) * ((t + b - 1) / b); };
+    ProdPlan p{256, 1, chunks, 0};
+    if (tiles(256) >= ncu) return p;
+    p.tile = tiles(128) * std::max(1, chunks / 8) >= ncu ? 128 : 64;
+    const int64_t want = (ncu + tiles(p.tile) - 1) / tiles(p.tile);
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, chunks / 8));
+    p.part_chunks = (chunks + parts - 1) / parts;
+    p.parts = (chunks + p.part_chunks - 1) / p.part_chunks;
+    if (p.parts > 1) p.bytes = up256((size_t)p.parts * t * ((i + 7) / 8 * 8) * sizeof(float));
+    return p;
+}
+
 template <typename M, bool ACOLS, bool BCOLS>
-static void launch_prod(ProdArgs a, hipStream_t st) {
-    auto tiles = [&](int64_t b) { return ((a.a.n + b - 1) / b) * ((a.b.n + b - 1) / b); };
-    const int ncu = op_cus();
+static void launch_prod(ProdArgs a, const ProdPlan& p, void* partial, hipStream_t st) {
+    a.parts = p.parts;
+    a.part_chunks = p.part_chunks;
+    a.partial = static_cast<float*>(partial);
+    a.dp = (a.d + 7) / 8 * 8;
     auto go = [&](auto tile) {
         typedef decltype(tile) Tl;
         a.ni = (int)((a.a.n + Tl::ROWS - 1) / Tl::ROWS);
         a.nt = (int)((a.b.n + Tl::COLS - 1) / Tl::COLS);
-        hipLaunchKernelGGL((k_prod<Tl>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
+        hipLaunchKernelGGL((k_prod<Tl>), dim3((unsigned)(a.ni * a.nt * a.parts)), dim3(Tl::THREADS), 0, st,
+                           a);
     };
-    if (tiles(256) >= ncu)
+    if (p.tile == 256)
         go(BigTile<M, ACOLS, BCOLS>());
-    else if (tiles(128) >= ncu)
+    else if (p.tile == 128)
         go(Tile<M, 128, 128, 2, 2, 2, ACOLS, BCOLS>());
     else
         go(Tile<M, 64, 64, 2, 2, 4, ACOLS, BCOLS>());
+    if (a.parts > 1)
+        hipLaunchKernelGGL(k_prod_join<typename M::Elem>, grid256(a.end * (a.dp / 8)), dim3(256), 0, st, a);
 }
 
 // Padded copies of operands that cannot be staged as they are.
@@ -214,11 +395,11 @@ struct PadPlan {
     size_t xbytes, wbytes;   // of one copy
 };
 static PadPlan pad_plan(const void* x, int64_t ldx, const void* wg, const void* wu, int64_t ldw,
-                        int64_t T, int64_t d, int64_t f) {
+                        int64_t T, int64_t d, int64_t f, bool need_x, bool need_w) {
     PadPlan p;
     p.dp = (d + 63) / 64 * 64;
-    p.x = !direct_rows(x, ldx, d);
-    p.w = !direct_rows(wg, ldw, d) || !direct_rows(wu, ldw, d);
+    p.x = need_x && !direct_rows(x, ldx, d);
+    p.w = need_w && (!direct_rows(wg, ldw, d) || !direct_rows(wu, ldw, d));
     p.xbytes = p.x ? up256((size_t)T * p.dp * 2) : 0;
     p.wbytes = p.w ? up256((size_t)f * p.dp * 2) : 0;
     return p;
@@ -256,38 +437,56 @@ static void gated_operands(GatedArgs& a, const PadPlan& p, const void* x, int64_
     a.chunks = (int)((kbytes + CHUNK_BYTES - 1) / CHUNK_BYTES);
 }
 
+// The two products of the backward pass: dx over the features (those of Wg, then those of Wu), dW over
+// the tokens.
+struct BackwardPlan {
+    int64_t fp;
+    ProdPlan dx, dw;
+    size_t dgu, partial;
+};
+static BackwardPlan backward_plan(int64_t T, int64_t d, int64_t f, bool dx, bool dw, int ncu) {
+    BackwardPlan p{};
+    p.fp = (f + 63) / 64 * 64;
+    p.dgu = up256((size_t)T * 2 * p.fp * 2);
+    if (dx) p.dx = prod_plan(d, T, (int)(2 * p.fp / 64), ncu);
+    if (dw) p.dw = prod_plan(d, 2 * p.fp, (int)((T + 63) / 64), ncu);
+    p.partial = std::max(p.dx.bytes, p.dw.bytes);
+    return p;
+}
+
 template <typename M>
-static void run_backward(const GatedArgs& a, int64_t d, void* dx, int64_t lddx, void* dw_gate,
-                         void* dw_up, int64_t lddw, hipStream_t st) {
-    launch_gated<M, true>(a, st);
+static void run_backward(const FewArgs& few, const GatedArgs& a, const BackwardPlan& p, int64_t d,
+                         void* dx, int64_t lddx, void* dw_gate, void* dw_up, int64_t lddw,
+                         void* partial, hipStream_t st) {
+    launch_gated<M, true>(few, a, st);
     const int64_t ldg = 4 * a.fp;
     const int64_t cols = (d + 7) / 8 * 8;   // (of x and the weights, as they are or padded)
-    if (dx) {   // over the features: those of Wg, then those of Wu
+    if (dx) {
         ProdArgs g{};
         g.a = operand(a.w.base, a.w.ld, cols, a.f);
         g.a.base2 = a.w.base2;
         g.a.split = (int)(a.fp / 64);
         g.b = operand(a.dgu, ldg, a.T, ldg);
         g.chunks = 2 * g.a.split;
+        g.d = d;
         g.out = dx;
         g.ldo = lddx;
         g.split = g.split2 = g.end = a.T;
-        g.d = d;
-        launch_prod<M, true, false>(g, st);
+        launch_prod<M, true, false>(g, p.dx, partial, st);
     }
-    if (dw_gate) {   // over the tokens
+    if (dw_gate) {
         ProdArgs g{};
         g.a = operand(a.x.base, a.x.ld, cols, a.T);
         g.b = operand(a.dgu, ldg, 2 * a.fp, a.T);
         g.chunks = (int)((a.T + 63) / 64);
+        g.d = d;
         g.out = dw_gate;
         g.out2 = dw_up;
         g.ldo = lddw;
         g.split = a.f;
         g.split2 = a.fp;
         g.end = a.fp + a.f;
-        g.d = d;
-        launch_prod<M, true, true>(g, st);
+        launch_prod<M, true, true>(g, p.dw, partial, st);
     }
 }
 
@@ -316,7 +515,8 @@ extern "C" bakron_status bakron_gated_mlp(const void* x, int64_t ldx, int64_t T,
     bakron_status st = mlp_sizes(who, ldx, T, d, ldw, f, dtype, act);
     if (st != BAKRON_OK) return st;
     if (h && ldh < f) return bk::op_fail(who, "leading dimension below f");
-    const bk::PadPlan p = bk::pad_plan(x, ldx, w_gate, w_up, ldw, T, d, f);
+    const bool many = T > bk::FEW_ROWS;
+    const bk::PadPlan p = bk::pad_plan(x, ldx, w_gate, w_up, ldw, T, d, f, many, many);
     bool query;
     st = bk::op_workspace(who, work, work_bytes, p.xbytes + 2 * p.wbytes, &query);
     if (st != BAKRON_OK || query) return st;
@@ -333,10 +533,11 @@ extern "C" bakron_status bakron_gated_mlp(const void* x, int64_t ldx, int64_t T,
     a.feat_gate = feat_gate;
     char* at = static_cast<char*>(work);
     bk::gated_operands(a, p, x, ldx, w_gate, w_up, ldw, d, &at, stream);
+    const bk::FewArgs few{x, w_gate, w_up, ldx, ldw, (int)d};
     if (dtype == BAKRON_BF16)
-        bk::launch_gated<bk::MmaBF16, false>(a, stream);
+        bk::launch_gated<bk::MmaBF16, false>(few, a, stream);
     else
-        bk::launch_gated<bk::MmaF16, false>(a, stream);
+        bk::launch_gated<bk::MmaF16, false>(few, a, stream);
     return bk::op_launched(who);
 }
 
@@ -354,11 +555,12 @@ extern "C" bakron_status bakron_gated_mlp_backward(const void* dh, int64_t lddh,
     if (st != BAKRON_OK) return st;
     if (lddh < f || (dx && lddx < d) || (dw_gate && lddw < d))
         return bk::op_fail(who, "leading dimension too small");
-    const bk::PadPlan p = bk::pad_plan(x, ldx, w_gate, w_up, ldw, T, d, f);
-    const int64_t fp = (f + 63) / 64 * 64;
-    const size_t dgu = bk::up256((size_t)T * 2 * fp * 2);
+    const bool many = T > bk::FEW_ROWS;
+    const bk::PadPlan p = bk::pad_plan(x, ldx, w_gate, w_up, ldw, T, d, f, many || dw_gate, many || dx);
+    const bk::BackwardPlan b =
+        bk::backward_plan(std::max<int64_t>(T, 1), d, f, dx != nullptr, dw_gate != nullptr, bk::op_cus());
     bool query;
-    st = bk::op_workspace(who, work, work_bytes, p.xbytes + 2 * p.wbytes + dgu, &query);
+    st = bk::op_workspace(who, work, work_bytes, p.xbytes + 2 * p.wbytes + b.dgu + b.partial, &query);
     if (st != BAKRON_OK || query) return st;
     if (!dw_gate != !dw_up) return bk::op_fail(who, "dw_gate and dw_up go together");
     if (!dx && !dw_gate) return bk::op_fail(who, "null pointer");
@@ -376,11 +578,15 @@ extern "C" bakron_status bakron_gated_mlp_backward(const void* dh, int64_t lddh,
     a.act = act;
     a.dh = dh;
     a.lddh = lddh;
-    a.fp = fp;
+    a.fp = b.fp;
     char* at = static_cast<char*>(work);
     bk::gated_operands(a, p, x, ldx, w_gate, w_up, ldw, d, &at, stream);
     a.dgu = at;
-    dtype == BAKRON_BF16 ? bk::run_backward<bk::MmaBF16>(a, d, dx, lddx, dw_gate, dw_up, lddw, stream)
-                         : bk::run_backward<bk::MmaF16>(a, d, dx, lddx, dw_gate, dw_up, lddw, stream);
+    char* const partial = at + b.dgu;
+    const bk::FewArgs few{x, w_gate, w_up, ldx, ldw, (int)d};
+    if (dtype == BAKRON_BF16)
+        bk::run_backward<bk::MmaBF16>(few, a, b, d, dx, lddx, dw_gate, dw_up, lddw, partial, stream);
+    else
+        bk::run_backward<bk::MmaF16>(few, a, b, d, dx, lddx, dw_gate, dw_up, lddw, partial, stream);
     return bk::op_launched(who);
 }

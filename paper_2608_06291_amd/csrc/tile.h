@@ -167,12 +167,12 @@ struct Source {
         }
         load_lds(p, to);
     }
-    __device__ inline void init(const Operand& o, int64_t first, int chunks) {
+    __device__ inline void init(const Operand& o, int64_t first, int end_chunk) {
         base = o.base + (COLS ? 2 * first : first * o.ld);
         base2 = o.base2 + (COLS ? 2 * first : first * o.ld);
         step = COLS ? 64 * o.ld : BYTES;
         split = o.split;
-        last = chunks - 1;
+        last = end_chunk - 1;
         end = o.k_end;
     }
     // The lane's piece of load i: slot `slot` of LDS row r; `local` maps the row (or the
@@ -219,9 +219,9 @@ struct Tile {
         static_assert(N >= 1, "every wave loads");
         Source<C, BYTES, N> s;
         template <typename RowFn>
-        __device__ inline void init(const Operand& o, int64_t first, int chunks, int wave, int lane,
+        __device__ inline void init(const Operand& o, int64_t first, int end_chunk, int wave, int lane,
                                     RowFn row) {
-            s.init(o, first, chunks);
+            s.init(o, first, end_chunk);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int r = (i * WAVES + wave) * PER + lane / PIECES, slot = lane % PIECES;
@@ -258,33 +258,34 @@ struct Tile {
         }
     }
 
-    // The tile that begins at row `ia` of A and row `ib` of B; row_a maps rows of the tile to
+    // Chunks c0 .. c0 + chunks - 1 of the tile that begins at row `ia` of A and row `ib` of
+    // B; row_a maps rows of the tile to
     // rows of the operand, counted from ia.  With FLUSH, scale(row, c, k) is the address of
     // the scale of tile row `row` for the k-th FLUSH steps of chunk c, and what is flushed is
     // sum[x][y] += acc * scale.  LDS is free to use again on return.
     template <typename RowA, typename Scale>
     static __device__ inline void run(char* lds, const Operand& oa, int64_t ia, const Operand& ob,
-                                      int64_t ib, int chunks, Accs& acc, RowA row_a,
+                                      int64_t ib, int c0, int chunks, Accs& acc, RowA row_a,
                                       f32x4 (&sum)[FLUSH ? UA : 1][FLUSH ? UB : 1], Scale scale) {
         const int tid = threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         Loads<ACOLS, BM, M::A_BYTES> la;
         Loads<BCOLS, BN, CHUNK_BYTES> lb;
-        la.init(oa, ia, chunks, wave, lane, row_a);
-        lb.init(ob, ib, chunks, wave, lane, [](int r) { return r; });
+        la.init(oa, ia, c0 + chunks, wave, lane, row_a);
+        lb.init(ob, ib, c0 + chunks, wave, lane, [](int r) { return r; });
         const uint32_t base = lds_address(lds);
         constexpr int S_LOADS = FLUSH ? (2 / FLUSH * BM + THREADS - 1) / THREADS : 0;
         constexpr int LOADS = la.N + lb.N + S_LOADS;   // of a chunk
         auto load = [&](int c, int buf) {
             const uint32_t to = base + buf * BUF;
-            la.load(c, to, wave);
-            lb.load(c, to + A_LDS, wave);
+            la.load(c0 + c, to, wave);
+            lb.load(c0 + c, to + A_LDS, wave);
             if constexpr (FLUSH > 0) {
                 // (with fewer scales than threads the waves past them load the same again)
 #pragma unroll
                 for (int i = 0; i < S_LOADS; ++i) {
                     const int e = (i * WAVES + wave) * 64 % (2 / FLUSH * BM);
-                    load_lds_word(scale((e + lane) % BM, min(c, chunks - 1), e / BM),
+                    load_lds_word(scale((e + lane) % BM, c0 + min(c, chunks - 1), e / BM),
                                   to + A_LDS + B_LDS + e * 4);
                 }
             }
@@ -334,10 +335,10 @@ struct Tile {
     }
     template <typename RowA>
     static __device__ inline void run(char* lds, const Operand& oa, int64_t ia, const Operand& ob,
-                                      int64_t ib, int chunks, Accs& acc, RowA row_a) {
+                                      int64_t ib, int c0, int chunks, Accs& acc, RowA row_a) {
         static_assert(FLUSH == 0, "scales missing");
         f32x4 none[1][1];
-        run(lds, oa, ia, ob, ib, chunks, acc, row_a, none, [](int, int, int) { return (const float*)nullptr; });
+        run(lds, oa, ia, ob, ib, c0, chunks, acc, row_a, none, [](int, int, int) { return (const float*)nullptr; });
     }
 };
 
@@ -377,12 +378,12 @@ struct BigTile {
             return j / (128 / G) * (256 / G) + h * (128 / G) + j % (128 / G);
         }
         template <typename RowFn>
-        __device__ inline void init(const Operand& o, int64_t first, int chunks, int wave, int lane,
+        __device__ inline void init(const Operand& o, int64_t first, int end_chunk, int wave, int lane,
                                     RowFn row) {
             constexpr int PIECES = C ? 16 : BYTES / 16, PER = 64 / PIECES;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                s[h].init(o, first, chunks);
+                s[h].init(o, first, end_chunk);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const int r = (i * 8 + wave) * PER + lane / PIECES, slot = lane % PIECES;
@@ -441,25 +442,25 @@ struct BigTile {
     // stages have to lie in one matrix: row_a may choose oa.base by the wave.
     template <typename RowA>
     static __device__ inline void run(char* lds, const Operand& oa, int64_t ia, const Operand& ob,
-                                      int64_t ib, int chunks, Accs& acc, RowA row_a) {
+                                      int64_t ib, int c0, int chunks, Accs& acc, RowA row_a) {
         const int tid = threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int group = wave >> 2;
         constexpr int BUF = A_LDS + B_LDS;
         Half<ACOLS, M::A_BYTES, 4, NA> ha;
         Half<BCOLS, CHUNK_BYTES, 2, 2> hb;
-        ha.init(oa, ia, chunks, wave, lane, row_a);
-        hb.init(ob, ib, chunks, wave, lane, [](int r) { return r; });
+        ha.init(oa, ia, c0 + chunks, wave, lane, row_a);
+        hb.init(ob, ib, c0 + chunks, wave, lane, [](int r) { return r; });
         Reads<ACOLS, M::A_BYTES, 2> ra;
         Reads<BCOLS, CHUNK_BYTES, 4> rb;
         ra.init((wave & 3) * 2, lane);
         rb.init(group * 4, lane);
         const uint32_t base = lds_address(lds);
         auto load_a = [&](int half, int c) {
-            ha.load(half, c, base + (c & 1) * BUF + half * A_HALF, wave);
+            ha.load(half, c0 + c, base + (c & 1) * BUF + half * A_HALF, wave);
         };
         auto load_b = [&](int half, int c) {
-            hb.load(half, c, base + (c & 1) * BUF + A_LDS + half * B_HALF, wave);
+            hb.load(half, c0 + c, base + (c & 1) * BUF + A_LDS + half * B_HALF, wave);
         };
         auto read_a = [&](int half, const char* buf, i32x4 (&a)[2][2]) {
 #pragma unroll
