@@ -19,12 +19,14 @@ struct LinearArgs {
     int64_t T, m;
     int chunks;              // of 128 codes
     int gsteps, ngroups;     // group_size / 64; groups of a row
+    int gshift;              // log2 gsteps, or -1
     int act, combine, dtype;
     int ni, nt;              // tiles
 };
 
-// Rows up to which a product is taken as one of few rows.
-constexpr int64_t FEW_ROWS = 64;
+// Rows up to which a product is taken as one of few rows: 4096 x 11008 with 128-column groups, 32
+// rows 14.5 us against 15.7 in 64 x 64 tiles, 64 rows 24.4 against 18.9.
+constexpr int64_t FEW_ROWS = 32;
 
 // y_t,i..i+N-1 from the sums z (scales applied).
 template <typename E, int N>
@@ -112,11 +114,16 @@ __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
 
 // Few rows (a decoding step): bound by reading the codes once, so no tile is staged.  A
 // workgroup takes R units of 16 rows of codes and Y of 16 rows of q; its waves share the row's
-// steps of 64 codes, U at a time in turn, every fragment straight from memory into
-// registers, the next U steps' before the products of these.  The partial sums meet in LDS.
-template <typename M, bool GROUPED, int R, int Y, int U>
+// chunks of 128 codes in turn, every fragment straight from memory into registers, several
+// chunks asked for at once.  The partial sums meet in LDS.
+//
+// FLUSH as in the tiles: sums are scaled once a chunk (2, or 0: at the end), or every 64 codes
+// (1: groups that end inside a chunk).  In the first two cases a lane reads the 32 codes at
+// 32 (lane / 16) of the chunk at once and takes them 16 and 16 (the order of the summed axis
+// is free as long as q follows it): 64 or 128 bytes of a row side by side, not 32.
+template <typename M, int FLUSH, int R, int Y>
 __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
-    constexpr int STEP = M::A_BYTES / 2;      // bytes of codes a step
+    constexpr bool GROUPED = FLUSH > 0, WIDE = FLUSH != 1;
     constexpr bool NARROW = M::A_BYTES != CHUNK_BYTES;
     constexpr float UNIT = NARROW ? 1.0f / 16.0f : 1.0f;
     extern __shared__ __attribute__((aligned(16))) char few_lds[];
@@ -128,88 +135,105 @@ __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
     const int r16 = lane & 15, kq = lane >> 4;
     const int64_t i0 = (int64_t)blockIdx.x * (R * 16);
     const int64_t t0 = (int64_t)blockIdx.y * (Y * 16);
-    const int nsteps = 2 * a.chunks;
 
+    // byte of a chunk where this lane's first 16 entries begin, and from there to its second
+    constexpr int Q_LANE = WIDE ? 32 : 16, Q_NEXT = WIDE ? 16 : 64;
+    constexpr int W_LANE = NARROW ? Q_LANE / 2 : Q_LANE, W_NEXT = NARROW ? Q_NEXT / 2 : Q_NEXT;
     const char* w[R];
     const char* q[Y];
 #pragma unroll
     for (int r = 0; r < R; ++r)
-        w[r] = a.w + min(i0 + r * 16 + r16, a.m - 1) * a.ldw + kq * (STEP / 4);
+        w[r] = a.w + min(i0 + r * 16 + r16, a.m - 1) * a.ldw + kq * W_LANE;
 #pragma unroll
     for (int y = 0; y < Y; ++y)
-        q[y] = reinterpret_cast<const char*>(a.q) + min(t0 + y * 16 + r16, a.T - 1) * a.ldq + kq * 16;
+        q[y] = reinterpret_cast<const char*>(a.q) + min(t0 + y * 16 + r16, a.T - 1) * a.ldq + kq * Q_LANE;
 
-    typedef typename std::conditional<NARROW, i32x2, i32x4>::type Codes;
-    struct Block {
-        Codes w[U][R];
-        i32x4 q[U][Y];
+    struct Block {   // a chunk
+        i32x4 w[NARROW ? 1 : 2][R];
+        i32x4 q[2][Y];
     };
-    auto load = [&](Block& b, int first) {
+    auto load = [&](Block& b, int c) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int s = min(first + u, nsteps - 1);
-#pragma unroll
-            for (int r = 0; r < R; ++r) b.w[u][r] = *reinterpret_cast<const Codes*>(w[r] + s * STEP);
-#pragma unroll
-            for (int y = 0; y < Y; ++y) b.q[u][y] = *reinterpret_cast<const i32x4*>(q[y] + s * 64);
+        for (int r = 0; r < R; ++r) {
+            const char* const p = w[r] + c * M::A_BYTES;
+            if constexpr (NARROW && WIDE) {
+                b.w[0][r] = *reinterpret_cast<const i32x4*>(p);
+            } else if constexpr (NARROW) {
+                const i32x2 x = *reinterpret_cast<const i32x2*>(p), y = *reinterpret_cast<const i32x2*>(p + W_NEXT);
+                b.w[0][r] = i32x4{x[0], x[1], y[0], y[1]};
+            } else {
+                b.w[0][r] = *reinterpret_cast<const i32x4*>(p);
+                b.w[NARROW ? 0 : 1][r] = *reinterpret_cast<const i32x4*>(p + W_NEXT);
+            }
         }
+#pragma unroll
+        for (int y = 0; y < Y; ++y)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                b.q[u][y] = *reinterpret_cast<const i32x4*>(q[y] + c * CHUNK_BYTES + u * Q_NEXT);
     };
-    // (scales first: they are waited for first)
-    constexpr int SC = 4;
-    float sc[SC];
+    // A thread's first scale (32 groups of a row side by side) is asked for before the codes.
+    const int sg = tid & 31, srow = tid >> 5, srows = blockDim.x >> 5;
+    float sc = 0.0f;
+    auto scale_at = [&](int row, int g) { return a.scale + min(i0 + row, a.m - 1) * a.ngroups + g; };
     if constexpr (GROUPED) {
-#pragma unroll
-        for (int k = 0; k < SC; ++k) {
-            const int e = min(tid + k * (int)blockDim.x, nscales - 1);
-            sc[k] = a.scale[min(i0 + e / a.ngroups, a.m - 1) * a.ngroups + e % a.ngroups];
-        }
+        if (sg < a.ngroups) sc = *scale_at(min(srow, R * 16 - 1), sg);
     }
-    Block b;
-    load(b, wave * U);
-    if constexpr (GROUPED) {
+    // D chunks of this wave are asked for at once (4: 5% slower).
+    constexpr int D = 2;
+    Block b[D];
+    auto load_all = [&](int c) {
 #pragma unroll
-        for (int k = 0; k < SC; ++k) {
-            const int e = tid + k * (int)blockDim.x;
-            if (e < nscales) scales[e % a.ngroups * (R * 16) + e / a.ngroups] = sc[k];
-        }
-        for (int e = tid + SC * blockDim.x; e < nscales; e += blockDim.x)
-            scales[e % a.ngroups * (R * 16) + e / a.ngroups] =
-                a.scale[min(i0 + e / a.ngroups, a.m - 1) * a.ngroups + e % a.ngroups];
+        for (int k = 0; k < D; ++k)
+            if (c + k * waves < a.chunks) load(b[k], c + k * waves);
+    };
+    load_all(wave);
+    if constexpr (GROUPED) {
+        for (int row = srow; row < R * 16; row += srows)
+            for (int g = sg; g < a.ngroups; g += 32)
+                scales[g * (R * 16) + row] = row == srow && g == sg ? sc : *scale_at(row, g);
         wait_lds();
         bare_barrier();
     }
     i32x4 acc[R][Y] = {};
     f32x4 sum[R][Y] = {};
-    for (int first = wave * U; first < nsteps; first += waves * U) {
-        Block n;
-        load(n, first + waves * U);   // (past the end the last step again, not used)
+    auto add = [&](const Block& b, int c) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (first + u >= nsteps) break;
+        for (int r = 0; r < R; ++r) {
+            i32x4 p[Y];
+            f32x4 s;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                i32x4 c;
-                if constexpr (NARROW)
-                    c = unpack_codes(b.w[u][r]);
-                else
-                    c = b.w[u][r];
-                f32x4 s;
-                if constexpr (GROUPED)
-                    s = *reinterpret_cast<const f32x4*>(
-                        scales + min((first + u) / a.gsteps, a.ngroups - 1) * (R * 16) + r * 16 + kq * 4);
-#pragma unroll
-                for (int y = 0; y < Y; ++y) {
-                    if constexpr (GROUPED) {
-                        const i32x4 p = M::mma(c, b.q[u][y], i32x4{0, 0, 0, 0});
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) sum[r][y][j] = fmaf((float)p[j], s[j], sum[r][y][j]);
-                    } else {
-                        acc[r][y] = M::mma(c, b.q[u][y], acc[r][y]);
+            for (int u = 0; u < 2; ++u) {
+                i32x4 w = b.w[NARROW ? 0 : u][r];
+                if constexpr (NARROW) w = unpack_codes(i32x2{w[2 * u], w[2 * u + 1]});
+                if constexpr (GROUPED) {
+                    if (FLUSH == 1 || u == 0) {
+                        const int step = 2 * c + u;
+                        const int g = a.gshift >= 0 ? step >> a.gshift : step / a.gsteps;
+                        s = *reinterpret_cast<const f32x4*>(scales + min(g, a.ngroups - 1) * (R * 16) +
+                                                            r * 16 + kq * 4);
                     }
+#pragma unroll
+                    for (int y = 0; y < Y; ++y) {
+                        p[y] = M::mma(w, b.q[u][y], FLUSH == 1 || u == 0 ? i32x4{0, 0, 0, 0} : p[y]);
+                        if (FLUSH == 1 || u == 1) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                sum[r][y][j] = fmaf((float)p[y][j], s[j], sum[r][y][j]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int y = 0; y < Y; ++y) acc[r][y] = M::mma(w, b.q[u][y], acc[r][y]);
                 }
             }
         }
-        b = n;
+    };
+    for (int c = wave; c < a.chunks; c += waves * D) {
+        if (c != wave) load_all(c);
+#pragma unroll
+        for (int k = 0; k < D; ++k)
+            if (c + k * waves < a.chunks) add(b[k], c + k * waves);
     }
     char* const parts = few_lds + (nscales * 4 + 15) / 16 * 16;
 #pragma unroll
@@ -261,40 +285,45 @@ static void launch_linear_tile(LinearArgs a, hipStream_t st) {
     hipLaunchKernelGGL((k_linear<Tl, FLUSH>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
 }
 
-template <typename M, bool GROUPED, int R, int Y, int U>
+template <typename M, int FLUSH, int R, int Y>
 static void launch_linear_few(const LinearArgs& a, hipStream_t st) {
     const dim3 grid((unsigned)((a.m + R * 16 - 1) / (R * 16)), (unsigned)((a.T + Y * 16 - 1) / (Y * 16)));
-    // as many waves as have work, 8 at most (4 with 8 units: 64 KiB of LDS)
-    const int blocks = (2 * a.chunks + U - 1) / U;
-    const int waves = blocks >= 8 && R * Y < 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
-    const int scales = GROUPED ? (a.ngroups * R * 16 * 4 + 15) / 16 * 16 : 0;
-    hipLaunchKernelGGL((k_linear_few<M, GROUPED, R, Y, U>), grid, dim3(64 * waves),
+    // as many waves as have work, 8 at most
+    const int blocks = a.chunks;
+    const int waves = blocks >= 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
+    const int scales = FLUSH > 0 ? (a.ngroups * R * 16 * 4 + 15) / 16 * 16 : 0;
+    hipLaunchKernelGGL((k_linear_few<M, FLUSH, R, Y>), grid, dim3(64 * waves),
                        scales + waves * R * Y * 1024, st, a);
 }
 
-template <typename M, bool GROUPED>
+// FLUSH: 0 one scale a row, 2 groups of whole chunks of 128 codes, 1 other multiples of 64.
+template <typename M, int FLUSH>
 static void launch_linear(const LinearArgs& a, hipStream_t st) {
     auto tiles = [&](int64_t b) { return ((a.m + b - 1) / b) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
     // (a row's scales have to fit beside the partial sums)
-    if (a.T <= FEW_ROWS && (!GROUPED || a.ngroups <= 256)) {
-        if (a.T <= 16) return launch_linear_few<M, GROUPED, 1, 1, 4>(a, st);
-        if (a.T <= 32) return launch_linear_few<M, GROUPED, 1, 2, 2>(a, st);
-        return launch_linear_few<M, GROUPED, 2, 4, 2>(a, st);
+    if (a.T <= FEW_ROWS && (FLUSH == 0 || a.ngroups <= 256)) {
+        if (a.T <= 16) return launch_linear_few<M, FLUSH, 1, 1>(a, st);
+        return launch_linear_few<M, FLUSH, 2, 2>(a, st);
     }
-    if constexpr (!GROUPED) {
+    if constexpr (FLUSH == 0) {
         if (tiles(256) >= ncu) return launch_linear_tile<BigTile<M>, 0>(a, st);
         if (tiles(128) >= ncu) return launch_linear_tile<Tile<M, 128, 128, 2, 2, 3>, 0>(a, st);
-        return launch_linear_tile<Tile<M, 64, 64, 2, 2, 4>, 0>(a, st);
-    } else if (a.gsteps % 2 == 0) {   // a chunk of 128 codes is in one group
-        if (tiles(128) >= ncu)
-            return launch_linear_tile<Tile<M, 128, 128, 2, 4, 3, false, false, 2>, 2>(a, st);
-        launch_linear_tile<Tile<M, 64, 64, 2, 2, 4, false, false, 2>, 2>(a, st);
+        launch_linear_tile<Tile<M, 64, 64, 2, 2, 4>, 0>(a, st);
     } else {
         if (tiles(128) >= ncu)
-            return launch_linear_tile<Tile<M, 128, 128, 2, 4, 3, false, false, 1>, 1>(a, st);
-        launch_linear_tile<Tile<M, 64, 64, 2, 2, 4, false, false, 1>, 1>(a, st);
+            return launch_linear_tile<Tile<M, 128, 128, 2, 4, 3, false, false, FLUSH>, FLUSH>(a, st);
+        launch_linear_tile<Tile<M, 64, 64, 2, 2, 4, false, false, FLUSH>, FLUSH>(a, st);
     }
+}
+template <typename M>
+static void launch_linear(const LinearArgs& a, hipStream_t st) {
+    if (a.gsteps == 0)
+        launch_linear<M, 0>(a, st);
+    else if (a.gsteps % 2 == 0)
+        launch_linear<M, 2>(a, st);
+    else
+        launch_linear<M, 1>(a, st);
 }
 
 }  // namespace bk
@@ -351,15 +380,11 @@ extern "C" bakron_status bakron_linear(const int8_t* q, int64_t ldq, const float
     a.m = m;
     a.chunks = (int)(np / BAKRON_PACK_COLUMNS);
     a.gsteps = (int)(group_size / 64);
+    a.gshift = a.gsteps > 0 && (a.gsteps & (a.gsteps - 1)) == 0 ? __builtin_ctz(a.gsteps) : -1;
     a.ngroups = group_size ? (int)((n + group_size - 1) / group_size) : 1;
     a.act = act;
     a.combine = combine;
     a.dtype = dtype;
-    if (width == 4)
-        group_size ? bk::launch_linear<bk::MmaI4, true>(a, stream)
-                   : bk::launch_linear<bk::MmaI4, false>(a, stream);
-    else
-        group_size ? bk::launch_linear<bk::MmaI8, true>(a, stream)
-                   : bk::launch_linear<bk::MmaI8, false>(a, stream);
+    width == 4 ? bk::launch_linear<bk::MmaI4>(a, stream) : bk::launch_linear<bk::MmaI8>(a, stream);
     return bk::op_launched(who);
 }

@@ -115,9 +115,9 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
 }
 
 // Few rows (a decoding step): bound by reading the weights once.  A workgroup takes 16
-// features and Y units of 16 rows; its waves share the summed axis, U steps of 32 at a time in
-// turn, every fragment straight from memory (at any alignment) into registers, the next U steps'
-// before the products of these.  The partial sums meet in LDS.
+// features and Y units of 16 rows; its waves share the summed axis, blocks of U steps of 32 in
+// turn, every fragment straight from memory (at any alignment) into registers, two blocks asked
+// for at once.  The partial sums meet in LDS.
 template <typename M, bool BWD, int Y, int U>
 __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
     typedef typename M::Elem E;
@@ -133,20 +133,20 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
 #pragma unroll
     for (int y = 0; y < Y; ++y)
         x[y] = static_cast<const E*>(f.x) + min(t0 + y * 16 + r16, a.T - 1) * f.ldx + kq * 8;
-    const int nsteps = f.d / 32;   // whole ones; what is left goes to the last wave
+    const int nblocks = f.d / (32 * U), nsteps = f.d / 32;   // what is left goes to the last wave
 
     struct Block {
         u32x4 g[U], u[U], x[U][Y];
     };
-    auto load = [&](Block& b, int first) {
+    auto load = [&](Block& b, int k) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int k = min(first + i, nsteps - 1) * 32;   // (past the end the last step, not used)
-            b.g[i] = load_words(wg + k);
-            b.u[i] = load_words(wu + k);
+        for (int i = 0; i < U; ++i) b.g[i] = load_words(wg + k + i * 32);
 #pragma unroll
-            for (int y = 0; y < Y; ++y) b.x[i][y] = load_words(x[y] + k);
-        }
+        for (int i = 0; i < U; ++i) b.u[i] = load_words(wu + k + i * 32);
+#pragma unroll
+        for (int y = 0; y < Y; ++y)
+#pragma unroll
+            for (int i = 0; i < U; ++i) b.x[i][y] = load_words(x[y] + k + i * 32);
     };
     f32x4 G[Y] = {}, Up[Y] = {};
     auto add = [&](u32x4 g, u32x4 u, const u32x4 (&v)[Y]) {
@@ -157,19 +157,25 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
             Up[y] = M::mma(__builtin_bit_cast(i32x4, u), b, Up[y]);
         }
     };
-    int first = wave * U;
-    if (first < nsteps) {
-        Block b;
-        load(b, first);
-        for (; first < nsteps; first += waves * U) {
-            Block n;
-            load(n, first + waves * U);
+    // two blocks of this wave are asked for at once
+    for (int c = wave; c < nblocks; c += waves * 2) {
+        Block b[2];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                if (first + i >= nsteps) break;
-                add(b.g[i], b.u[i], b.x[i]);
-            }
-            b = n;
+        for (int k = 0; k < 2; ++k)
+            if (c + k * waves < nblocks) load(b[k], (c + k * waves) * (32 * U));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (c + k * waves >= nblocks) break;
+#pragma unroll
+            for (int i = 0; i < U; ++i) add(b[k].g[i], b[k].u[i], b[k].x[i]);
+        }
+    }
+    if (wave == waves - 1) {
+        for (int s = nblocks * U; s < nsteps; ++s) {
+            u32x4 v[Y];
+#pragma unroll
+            for (int y = 0; y < Y; ++y) v[y] = load_words(x[y] + s * 32);
+            add(load_words(wg + s * 32), load_words(wu + s * 32), v);
         }
     }
     if (f.d % 32 != 0 && wave == waves - 1) {
@@ -313,13 +319,15 @@ static bool direct_rows(const void* p, int64_t ld, int64_t cols) {
     return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && 2 * ld < TILE_LD_MAX;
 }
 
-// Rows up to which the gated product is taken as one of few rows.
-constexpr int64_t FEW_ROWS = 64;
+// Rows up to which the gated product is taken as one of few rows: 4096 -> 11008, 32 rows 52 us
+// (64 x 64 tiles: 50, and two copies more for rows that are no 16-byte multiples), 64 rows
+// 73 against 50.
+constexpr int64_t FEW_ROWS = 32;
 
 template <typename M, bool BWD, int Y, int U>
 static void launch_gated_few(const FewArgs& f, const GatedArgs& a, hipStream_t st) {
     const dim3 grid((unsigned)(((BWD ? a.fp : a.f) + 15) / 16), (unsigned)((a.T + Y * 16 - 1) / (Y * 16)));
-    const int blocks = (f.d / 32 + U - 1) / U;   // as many waves as have work, 8 at most
+    const int blocks = f.d / (32 * U);   // as many waves as have work, 8 at most
     const int waves = blocks >= 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
     hipLaunchKernelGGL((k_gated_few<M, BWD, Y, U>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
 }
@@ -327,8 +335,7 @@ static void launch_gated_few(const FewArgs& f, const GatedArgs& a, hipStream_t s
 template <typename M, bool BWD>
 static void launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
     if (a.T <= 16) return launch_gated_few<M, BWD, 1, 4>(few, a, st);
-    if (a.T <= 32) return launch_gated_few<M, BWD, 2, 2>(few, a, st);
-    if (a.T <= FEW_ROWS) return launch_gated_few<M, BWD, 4, 2>(few, a, st);
+    if (a.T <= FEW_ROWS) return launch_gated_few<M, BWD, 2, 2>(few, a, st);
     const int64_t f = BWD ? a.fp : a.f;   // (the padding is written, too)
     auto tiles = [&](int64_t b) { return ((f + b / 2 - 1) / (b / 2)) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
