@@ -556,15 +556,21 @@ def mlp_local_factors(x, g, D, style: str = "kfac", iters: int = 1):
 ACTS = {"none": 0, "silu": 1, "gelu": 2}
 COMBINES = {"none": 0, "add": 1, "mul": 2}
 PACK_COLUMNS = 128   # BAKRON_PACK_COLUMNS
-_DTYPES = None
+_torch = None
+_DTYPES = {}
+
+
+def _import_torch():
+    """torch, kept by name: small calls are bound by the host."""
+    global _torch
+    import torch
+    _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    _torch = torch
+    return torch
 
 
 def _dtype_code(dtype):
     """bakron_dtype of a torch dtype."""
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
     try:
         return _DTYPES[dtype]
     except KeyError:
@@ -608,8 +614,7 @@ def _vector(t, name, n, dtype, device):
 
 def _raw_stream(device):
     """The current stream's handle (no Stream object: small calls are bound by the host)."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(device.index)
+    return (_torch or _import_torch())._C._cuda_getCurrentRawStream(device.index)
 
 
 _work_sizes = {}
@@ -618,13 +623,13 @@ _work_sizes = {}
 def _run_op(fn, args, device, work=None, key=None):
     """Call a workspace-protocol operator; allocates its workspace unless given.  `key`
     holds everything its size depends on, so that it is asked for once."""
-    import torch
+    torch = _torch or _import_torch()
     st = _raw_stream(device)
     if work is None:
         need = _work_sizes.get(key) if key is not None else None
         if need is None:
             size = ctypes.c_size_t(0)
-            if key is None and fn(*args, 256, ctypes.byref(size), st) == BAKRON_OK:
+            if key is None and fn(*args, 256, size, st) == BAKRON_OK:
                 return   # needs none
             _raise_last(fn(*args, None, ctypes.byref(size), st))
             need = size.value
@@ -652,7 +657,7 @@ def rmsnorm_quant(x, weight=None, residual=None, eps: float = 1e-5, normalise: b
     per row.  x: T x d fp32, fp16 or bf16; weight: d fp32.  `sum` is returned where
     there is a residual, unless with_sum says otherwise; sum_out (e.g. residual
     itself) receives it."""
-    import torch
+    torch = _torch or _import_torch()
     lib = load()
     xp, ldx = _rows_of(x, "x")
     T, d = x.shape
@@ -695,7 +700,7 @@ class PackedCodes(NamedTuple):
 def pack_codes(codes, width: int = 4) -> PackedCodes:
     """bakron_pack_codes: lays out codes (m x n int8, e.g. of solve) once per layer.
     width 4 holds codes in [-8, 7]."""
-    import torch
+    torch = _torch or _import_torch()
     _check_dev(codes, "codes", torch.int8)
     if codes.dim() != 2:
         raise ValueError("codes must be m x n")
@@ -713,7 +718,7 @@ def linear(q, q_scale, w: PackedCodes, scale, group_size: int = 0, bias=None, ac
     plus `other` (combine "add", the default where there is one) or times it ("mul").
     q, q_scale: as rmsnorm_quant returns them (T x n int8, T); scale: m, or m x
     ceil(n / group_size).  Returns T x m of dtype (default bf16)."""
-    import torch
+    torch = _torch or _import_torch()
     lib = load()
     qp, ldq = _rows_of(q, "q", None, torch.int8)
     dev = q.device
@@ -772,7 +777,7 @@ def gated_mlp(x, w_gate, w_up, act: str = "silu", features: bool = False, out=No
     """bakron_gated_mlp on the current stream: act(x w_gate^T) * (x w_up^T) in one
     kernel.  x: T x d, w_gate, w_up: f x d, all fp16 or all bf16.  features=True
     also returns act(G) and act'(G) * U in fp32."""
-    import torch
+    torch = _torch or _import_torch()
     lib = load()
     xp, ldx, T, d, gp, up, ldw, f, code = _mlp_operands(x, w_gate, w_up)
     if out is None:
@@ -791,7 +796,7 @@ def gated_mlp_backward(dh, x, w_gate, w_up, act: str = "silu", need_dx: bool = T
                        need_dw: bool = True, work=None):
     """bakron_gated_mlp_backward: (dx, dw_gate, dw_up) from dh, the gradient with
     respect to gated_mlp's output; None for what is not needed."""
-    import torch
+    torch = _torch or _import_torch()
     lib = load()
     xp, ldx, T, d, gp, up, ldw, f, code = _mlp_operands(x, w_gate, w_up)
     hp, ldh = _rows_of(dh, "dh", (T, f), x.dtype, x.device)
@@ -817,7 +822,7 @@ def token_logprobs(logits, target=None, top: int = 0, work=None) -> TokenLogprob
     """bakron_token_logprobs on the current stream.  logits: T x V fp32, fp16 or
     bf16; target: T int64 (outside [0, V): ignored, 0) or None; top: number of
     alternatives, at most 32."""
-    import torch
+    torch = _torch or _import_torch()
     lib = load()
     zp, ld = _rows_of(logits, "logits")
     T, V = logits.shape
@@ -842,7 +847,7 @@ def token_logprobs_backward(logits, target, lse, entropy=None, g_logprob=None, g
     """bakron_token_logprobs_backward: the gradient with respect to the logits, T x V
     in their dtype (out may be logits itself), from the gradients with respect to
     token_logprobs' logprob and entropy (None for 0)."""
-    import torch
+    torch = _torch or _import_torch()
     lib = load()
     zp, ld = _rows_of(logits, "logits")
     T, V = logits.shape

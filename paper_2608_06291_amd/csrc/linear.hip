@@ -308,11 +308,11 @@ static void launch_linear(const LinearArgs& a, hipStream_t st) {
     }
     if constexpr (FLUSH == 0) {
         if (tiles(256) >= ncu) return launch_linear_tile<BigTile<M>, 0>(a, st);
-        if (tiles(128) >= ncu) return launch_linear_tile<Tile<M, 128, 128, 2, 2, 3>, 0>(a, st);
+        if (tiles(128) >= ncu) return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2>, 0>(a, st);
         launch_linear_tile<Tile<M, 64, 64, 2, 2, 4>, 0>(a, st);
     } else {
         if (tiles(128) >= ncu)
-            return launch_linear_tile<Tile<M, 128, 128, 2, 4, 3, false, false, FLUSH>, FLUSH>(a, st);
+            return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2, false, false, FLUSH>, FLUSH>(a, st);
         launch_linear_tile<Tile<M, 64, 64, 2, 2, 4, false, false, FLUSH>, FLUSH>(a, st);
     }
 }

@@ -21,6 +21,7 @@ constexpr int LP_REGS = 32;           // 32-bit registers of logits a thread hol
 constexpr int LP_TOP = 32;            // alternatives at most
 constexpr int LP_CAND = 1024;         // candidates that are ranked by counting
 constexpr int LP_PARTS = 64;          // parts of a row at most
+constexpr int LP_JOIN = 256;          // candidates that the join ranks by counting
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float LN2 = 0.69314718055994530942f;
 
@@ -262,11 +263,16 @@ __global__ __launch_bounds__(LP_THREADS, 6) void k_logprob(LpArgs a) {
     }
 }
 
-// One wave joins the parts of a row: lane l holds part l and the head of its sorted
-// candidates, which wait in LDS.
+// One wave joins the parts of a row, lane l holding part l.  The parts' sorted candidates
+// wait in LDS.  With c the least number of candidates a part that makes `top` in all, the
+// q-th largest (q = ceil(top / c)) of the parts' c-th candidates has q c >= top candidates at
+// or above it: those, few more than `top` as a rule, are ranked by counting.  Where they are
+// many (masked rows) the largest head of all lists is taken `top` times instead, 0.25 us each.
 template <typename E>
 __global__ __launch_bounds__(64) void k_logprob_join(LpArgs a) {
     __shared__ uint64_t lists[LP_PARTS * LP_TOP];
+    __shared__ uint64_t chosen[LP_JOIN];
+    __shared__ int count;
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
     const uint64_t* const cand = a.cand + row * a.parts * a.top;
@@ -285,7 +291,38 @@ __global__ __launch_bounds__(64) void k_logprob_join(LpArgs a) {
     if (lane == 0) lp_store(a, row, m, s, s1, zt, asked);
     if (a.top == 0) return;
     const float base = m == -INFINITY ? 0.0f : m + logf(s);
+    if (lane == 0) count = 0;
     __syncthreads();
+    const int c = (a.top + a.parts - 1) / a.parts, q_th = (a.top + c - 1) / c;
+    const uint64_t mark = lane < a.parts ? lists[lane * a.top + c - 1] : 0;
+    int higher = 0;
+    for (int i = 0; i < a.parts; ++i) higher += lists[i * a.top + c - 1] > mark;
+    const uint64_t who = __ballot(mark != 0 && higher == q_th - 1);   // marks are distinct, but for 0
+    const int from = who ? __ffsll((unsigned long long)who) - 1 : 0;
+    const uint64_t bound =
+        who ? ((uint64_t)lane_value((uint32_t)(mark >> 32), from) << 32) | lane_value((uint32_t)mark, from) : 1;
+    for (int i = lane; i < a.parts * a.top; i += 64) {
+        const uint64_t v = lists[i];
+        if (v >= bound) {
+            const int k = atomicAdd(&count, 1);
+            if (k < LP_JOIN) chosen[k] = v;
+        }
+    }
+    __syncthreads();
+    const int n = count;
+    auto put = [&](int k, uint64_t v) {
+        a.top_index[row * a.top + k] = lp_index(v);
+        a.top_logprob[row * a.top + k] = lp_unkey((uint32_t)(v >> 32)) - base;
+    };
+    if (n <= LP_JOIN) {
+        for (int i = lane; i < n; i += 64) {
+            const uint64_t v = chosen[i];
+            int above = 0;
+            for (int k = 0; k < n; ++k) above += chosen[k] > v;
+            if (above < a.top) put(above, v);
+        }
+        return;
+    }
     int at = lane * a.top;
     const int end = lane < a.parts ? at + a.top : at;
     uint64_t head = at < end ? lists[at] : 0, mine = 0;
@@ -297,10 +334,7 @@ __global__ __launch_bounds__(64) void k_logprob_join(LpArgs a) {
             head = at < end ? lists[at] : 0;
         }
     }
-    if (lane < a.top) {
-        a.top_index[row * a.top + lane] = lp_index(mine);
-        a.top_logprob[row * a.top + lane] = lp_unkey((uint32_t)(mine >> 32)) - base;
-    }
+    if (lane < a.top) put(lane, mine);
 }
 
 struct LpGradArgs {

@@ -348,7 +348,7 @@ static void launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
     if (tiles(256) >= ncu)
         go(BigTile<M>());
     else if (tiles(128) >= ncu)
-        go(Tile<M, 128, 128, 2, 2, 2>());
+        go(Tile<M, 128, 128, 2, 4, 2>());
     else
         go(Tile<M, 64, 64, 2, 2, 4>());
 }
@@ -388,7 +388,7 @@ static void launch_prod(ProdArgs a, const ProdPlan& p, void* partial, hipStream_
     if (p.tile == 256)
         go(BigTile<M, ACOLS, BCOLS>());
     else if (p.tile == 128)
-        go(Tile<M, 128, 128, 2, 2, 2, ACOLS, BCOLS>());
+        go(Tile<M, 128, 128, 2, 4, 2, ACOLS, BCOLS>());
     else
         go(Tile<M, 64, 64, 2, 2, 4, ACOLS, BCOLS>());
     if (a.parts > 1)

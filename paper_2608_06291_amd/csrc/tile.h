@@ -118,7 +118,14 @@ __device__ inline void load_lds(const char* p, uint32_t to) {
                  "v"(p)
                  : "memory", "m0");
 }
-// The same for 4 bytes a lane.
+// The same from base (the same in all lanes) + off.
+__device__ inline void load_lds(const char* base, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(
+                     __builtin_amdgcn_readfirstlane(to)),
+                 "v"(off), "s"(base)
+                 : "memory", "m0");
+}
+// 4 bytes a lane.
 __device__ inline void load_lds_word(const float* p, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(
                      __builtin_amdgcn_readfirstlane(to)),
@@ -140,7 +147,7 @@ __device__ inline void bare_barrier() {
 }
 
 // N loads of a wave from one operand: each lane's pieces as 32-bit offsets from a base
-// that moves on with the chunks.
+// that moves on with the chunks (a scalar: a load takes no vector arithmetic).
 template <bool COLS, int BYTES, int N>
 struct Source {
     const char *base, *base2;
@@ -150,23 +157,6 @@ struct Source {
     int at[N];           // Columns: row in the chunk; rows: at[0] the piece's byte
     int64_t end;         // k_end
 
-    __device__ inline void load(int i, int chunk, uint32_t to) const {
-        int c = min(chunk, last);   // (past the last chunk: that one again, not used)
-        const char* b = base;
-        if (split > 0 && c >= split) {
-            b = base2;
-            c -= split;
-        }
-        const char* p = b + c * step + off[i];
-        if constexpr (COLS) {
-            if ((int64_t)(c + 1) * 64 > end && (int64_t)c * 64 + at[i] >= end)
-                p = reinterpret_cast<const char*>(&tile_zeros);
-        } else {
-            if ((int64_t)(c + 1) * BYTES > end && (int64_t)c * BYTES + at[0] >= end)
-                p = reinterpret_cast<const char*>(&tile_zeros);
-        }
-        load_lds(p, to);
-    }
     __device__ inline void init(const Operand& o, int64_t first, int end_chunk) {
         base = o.base + (COLS ? 2 * first : first * o.ld);
         base2 = o.base2 + (COLS ? 2 * first : first * o.ld);
@@ -175,8 +165,7 @@ struct Source {
         last = end_chunk - 1;
         end = o.k_end;
     }
-    // The lane's piece of load i: slot `slot` of LDS row r; `local` maps the row (or the
-    // first of 8 columns) of the half's layout to the tile's.
+    // Load i: the lane's piece of tile row `tile_row`, or the 8 columns at `tile_col` of row k.
     __device__ inline void set_row(int i, const Operand& o, int64_t first, int tile_row, int piece) {
         at[0] = piece;
         off[i] = (uint32_t)(min((int64_t)tile_row, o.n - 1 - first) * o.ld) + piece;
@@ -184,6 +173,27 @@ struct Source {
     __device__ inline void set_col(int i, const Operand& o, int64_t first, int k, int tile_col) {
         at[i] = k;
         off[i] = (uint32_t)(k * o.ld) + (first + tile_col < o.n ? 2 * tile_col : 0);
+    }
+    // All loads of a chunk, number i to to + i * stride.
+    __device__ inline void load(int chunk, uint32_t to, int stride) const {
+        constexpr int UNIT = COLS ? 64 : BYTES;
+        int c = min(chunk, last);   // (past the last chunk: that one again, not used)
+        const char* b = base;
+        if (split > 0 && c >= split) {
+            b = base2;
+            c -= split;
+        }
+        b += c * step;
+        if ((int64_t)(c + 1) * UNIT <= end) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_lds(b, off[i], to + i * stride);
+        } else {   // the operand ends in this chunk: zeros from there on
+            const int64_t left = end - (int64_t)c * UNIT;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                load_lds(at[COLS ? i : 0] < left ? b + off[i] : reinterpret_cast<const char*>(&tile_zeros),
+                         to + i * stride);
+        }
     }
 };
 
@@ -235,8 +245,7 @@ struct Tile {
             }
         }
         __device__ inline void load(int chunk, uint32_t lds, int wave) const {
-#pragma unroll
-            for (int i = 0; i < N; ++i) s.load(i, chunk, lds + (i * WAVES + wave) * 1024);
+            s.load(chunk, lds + wave * 1024, WAVES * 1024);
         }
     };
     // A fragment: unit u of R / 16, step s.
@@ -397,8 +406,7 @@ struct BigTile {
             }
         }
         __device__ inline void load(int h, int chunk, uint32_t lds, int wave) const {
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[h].load(i, chunk, lds + (i * 8 + wave) * 1024);
+            s[h].load(chunk, lds + wave * 1024, 8 * 1024);
         }
     };
     // Byte offsets in a half of this lane's reads: rows, per step; columns, per unit.
