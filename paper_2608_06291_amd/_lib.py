@@ -631,13 +631,15 @@ def _run_op(fn, args, device, work=None, key=None):
             size = ctypes.c_size_t(0)
             if key is None and fn(*args, 256, size, st) == BAKRON_OK:
                 return   # needs none
-            _raise_last(fn(*args, None, ctypes.byref(size), st))
+            _raise_last(fn(*args, None, size, st))
             need = size.value
             if key is not None:
                 _work_sizes[key] = need
-        work = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
-    size = ctypes.c_size_t(work.numel() * work.element_size())
-    _raise_last(fn(*args, work.data_ptr(), ctypes.byref(size), st))
+        if need == 0:
+            _raise_last(fn(*args, 256, ctypes.c_size_t(0), st))
+            return
+        work = torch.empty(need, dtype=torch.uint8, device=device)
+    _raise_last(fn(*args, work.data_ptr(), ctypes.c_size_t(work.numel() * work.element_size()), st))
 
 
 class NormQuant(NamedTuple):
@@ -671,15 +673,15 @@ def rmsnorm_quant(x, weight=None, residual=None, eps: float = 1e-5, normalise: b
     sp = yp = qp = cp = None
     lds = ldy = ldq = d
     if with_sum:
-        hs = torch.empty((T, d), dtype=x.dtype, device=dev) if sum_out is None else sum_out
+        hs = torch.empty(T, d, dtype=x.dtype, device=dev) if sum_out is None else sum_out
         sp, lds = _rows_of(hs, "sum_out", (T, d), x.dtype, dev)
     if with_y:
-        ys = torch.empty((T, d), dtype=x.dtype, device=dev)
+        ys = torch.empty(T, d, dtype=x.dtype, device=dev)
         yp, ldy = ys.data_ptr(), d
     if quantise:
         ldq = -(-d // PACK_COLUMNS) * PACK_COLUMNS
-        q = torch.empty((T, ldq), dtype=torch.int8, device=dev)
-        scale = torch.empty((T,), dtype=torch.float32, device=dev)
+        q = torch.empty(T, ldq, dtype=torch.int8, device=dev)
+        scale = torch.empty(T, dtype=torch.float32, device=dev)
         qp, cp = q.data_ptr(), scale.data_ptr()
         if ldq != d:
             q = q[:, :d]
@@ -741,7 +743,7 @@ def linear(q, q_scale, w: PackedCodes, scale, group_size: int = 0, bias=None, ac
         raise ValueError(f"scale must be contiguous fp32 with {m * groups} entries")
     sp = _vector(q_scale, "q_scale", T, torch.float32, dev)
     if out is None:
-        out = torch.empty((T, m), dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
+        out = torch.empty(T, m, dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
     yp, ldy = _rows_of(out, "out", (T, m), dtype, dev)
     code = _dtype_code(out.dtype)
     bp = _vector(bias, "bias", m, out.dtype, dev)
@@ -781,11 +783,11 @@ def gated_mlp(x, w_gate, w_up, act: str = "silu", features: bool = False, out=No
     lib = load()
     xp, ldx, T, d, gp, up, ldw, f, code = _mlp_operands(x, w_gate, w_up)
     if out is None:
-        out = torch.empty((T, f), dtype=x.dtype, device=x.device)
+        out = torch.empty(T, f, dtype=x.dtype, device=x.device)
     hp, ldh = _rows_of(out, "out", (T, f), x.dtype, x.device)
     fu = fg = None
     if features:
-        fu, fg = (torch.empty((T, f), dtype=torch.float32, device=x.device) for _ in range(2))
+        fu, fg = (torch.empty(T, f, dtype=torch.float32, device=x.device) for _ in range(2))
     _run_op(lib.bakron_gated_mlp,
             (xp, ldx, T, d, gp, up, ldw, f, code, ACTS[act], hp, ldh,
              fu.data_ptr() if features else None, fg.data_ptr() if features else None), x.device, work)
@@ -800,8 +802,8 @@ def gated_mlp_backward(dh, x, w_gate, w_up, act: str = "silu", need_dx: bool = T
     lib = load()
     xp, ldx, T, d, gp, up, ldw, f, code = _mlp_operands(x, w_gate, w_up)
     hp, ldh = _rows_of(dh, "dh", (T, f), x.dtype, x.device)
-    dx = torch.empty((T, d), dtype=x.dtype, device=x.device) if need_dx else None
-    dg, du = (torch.empty((f, d), dtype=x.dtype, device=x.device) if need_dw else None for _ in range(2))
+    dx = torch.empty(T, d, dtype=x.dtype, device=x.device) if need_dx else None
+    dg, du = (torch.empty(f, d, dtype=x.dtype, device=x.device) if need_dw else None for _ in range(2))
     _run_op(lib.bakron_gated_mlp_backward,
             (hp, ldh, xp, ldx, T, d, gp, up, ldw, f, code, ACTS[act], dx.data_ptr() if need_dx else None,
              d, dg.data_ptr() if need_dw else None, du.data_ptr() if need_dw else None, d), x.device, work)
@@ -828,13 +830,13 @@ def token_logprobs(logits, target=None, top: int = 0, work=None) -> TokenLogprob
     T, V = logits.shape
     dev = logits.device
     tp = _vector(target, "target", T, torch.int64, dev)
-    stats = torch.empty((3, T), dtype=torch.float32, device=dev)
+    stats = torch.empty(3, T, dtype=torch.float32, device=dev)
     logprob, entropy, lse = stats.unbind(0)
     top = int(top)
     tl = ti = None
     if top > 0:
-        tl = torch.empty((T, top), dtype=torch.float32, device=dev)
-        ti = torch.empty((T, top), dtype=torch.int64, device=dev)
+        tl = torch.empty(T, top, dtype=torch.float32, device=dev)
+        ti = torch.empty(T, top, dtype=torch.int64, device=dev)
     _run_op(lib.bakron_token_logprobs,
             (zp, ld, _dtype_code(logits.dtype), T, V, tp, top, None if tp is None else logprob.data_ptr(),
              entropy.data_ptr(), lse.data_ptr(), None if tl is None else tl.data_ptr(),
@@ -853,7 +855,7 @@ def token_logprobs_backward(logits, target, lse, entropy=None, g_logprob=None, g
     T, V = logits.shape
     dev = logits.device
     if out is None:
-        out = torch.empty((T, V), dtype=logits.dtype, device=dev)
+        out = torch.empty(T, V, dtype=logits.dtype, device=dev)
     dp, ldd = _rows_of(out, "out", (T, V), logits.dtype, dev)
     f32 = torch.float32
     _raise_last(lib.bakron_token_logprobs_backward(

@@ -1,6 +1,7 @@
 // Shared by the operators around a quantised layer: element types, vector
 // access at any alignment, reductions over a workgroup, argument checks.
 #pragma once
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <type_traits>
@@ -155,11 +156,15 @@ constexpr int64_t OP_T_MAX = ((int64_t)1 << 31) - 1;
 // Threads of one launch (the runtime takes below 2^32).
 constexpr int64_t OP_LAUNCH_MAX = (int64_t)1 << 31;
 
+// CUs of the current device (asked for once a device).
 inline int op_cus() {
+    static std::atomic<int> known[16];
     int dev = 0, ncu = 0;
     if (hipGetDevice(&dev) != hipSuccess) return 256;
+    if (dev >= 0 && dev < 16 && (ncu = known[dev].load(std::memory_order_relaxed)) > 0) return ncu;
     if (hipDeviceGetAttribute(&ncu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
         return 256;
+    if (dev >= 0 && dev < 16) known[dev].store(ncu, std::memory_order_relaxed);
     return ncu;
 }
 
