@@ -27,6 +27,9 @@ struct LinearArgs {
 // Rows up to which a product is taken as one of few rows: 4096 x 11008 with 128-column groups, 32
 // rows 14.5 us against 15.7 in 64 x 64 tiles, 64 rows 24.4 against 18.9.
 constexpr int64_t FEW_ROWS = 32;
+// And with few tiles (by 64 x 64) a CU: 7008 x 152 with 64-column groups, 2315 rows (less than half) 26.7 us
+// against 35; 4096 x 160, 127 rows 8.2 against 15.2.
+constexpr int64_t FEW_TILES = 2;
 
 // y_t,i..i+N-1 from the sums z (scales applied).
 template <typename E, int N>
@@ -299,19 +302,21 @@ static void launch_linear_few(const LinearArgs& a, hipStream_t st) {
 // FLUSH: 0 one scale a row, 2 groups of whole chunks of 128 codes, 1 other multiples of 64.
 template <typename M, int FLUSH>
 static void launch_linear(const LinearArgs& a, hipStream_t st) {
-    auto tiles = [&](int64_t b) { return ((a.m + b - 1) / b) * ((a.T + b - 1) / b); };
     const int ncu = op_cus();
     // (a row's scales have to fit beside the partial sums)
-    if (a.T <= FEW_ROWS && (FLUSH == 0 || a.ngroups <= 256)) {
-        if (a.T <= 16) return launch_linear_few<M, FLUSH, 1, 1>(a, st);
+    const bool fits = FLUSH == 0 || a.ngroups <= 256;
+    if (a.T <= 16 && fits) return launch_linear_few<M, FLUSH, 1, 1>(a, st);
+    if (a.T <= FEW_ROWS && fits) return launch_linear_few<M, FLUSH, 2, 2>(a, st);
+    // Few tiles with a long way to sum: cut that way among the waves, too.
+    if (fits && ((a.m + 63) / 64) * ((a.T + 63) / 64) * FEW_TILES <= ncu && a.chunks >= 8)
         return launch_linear_few<M, FLUSH, 2, 2>(a, st);
-    }
+    const int tile = pick_tile(a.m, a.T, ncu, FLUSH == 0);
     if constexpr (FLUSH == 0) {
-        if (tiles(256) >= ncu) return launch_linear_tile<BigTile<M>, 0>(a, st);
-        if (tiles(128) >= ncu) return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2>, 0>(a, st);
+        if (tile == 256) return launch_linear_tile<BigTile<M>, 0>(a, st);
+        if (tile == 128) return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2>, 0>(a, st);
         launch_linear_tile<Tile<M, 64, 64, 2, 2, 4>, 0>(a, st);
     } else {
-        if (tiles(128) >= ncu)
+        if (tile == 128)
             return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2, false, false, FLUSH>, FLUSH>(a, st);
         launch_linear_tile<Tile<M, 64, 64, 2, 2, 4, false, false, FLUSH>, FLUSH>(a, st);
     }

@@ -114,11 +114,43 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
     }
 }
 
+// 8 entries on their way; see SHIFT below.
+template <bool SHIFT>
+struct FewPiece {
+    u32x4 w;
+    uint32_t next;
+    template <typename E>
+    __device__ inline void load(const E* p) {
+        if constexpr (SHIFT) {
+            const uintptr_t at = (uintptr_t)p & ~(uintptr_t)3;
+            __builtin_memcpy(&w, (const void*)at, 16);
+            __builtin_memcpy(&next, (const void*)(at + ((uintptr_t)p & 2 ? 16 : 12)), 4);
+        } else {
+            w = load_words(p);
+        }
+    }
+    // `row`: any address of the same row's parity
+    template <typename E>
+    __device__ inline u32x4 get(const E* row) const {
+        if constexpr (SHIFT) {
+            if ((uintptr_t)row & 2)
+                return u32x4{__builtin_amdgcn_alignbit(w[1], w[0], 16), __builtin_amdgcn_alignbit(w[2], w[1], 16),
+                             __builtin_amdgcn_alignbit(w[3], w[2], 16), __builtin_amdgcn_alignbit(next, w[3], 16)};
+        }
+        return w;
+    }
+};
+
 // Few rows (a decoding step): bound by reading the weights once.  A workgroup takes 16
 // features and Y units of 16 rows; its waves share the summed axis, blocks of U steps of 32 in
 // turn, every fragment straight from memory (at any alignment) into registers, two blocks asked
 // for at once.  The partial sums meet in LDS.
-template <typename M, bool BWD, int Y, int U>
+//
+// SHIFT: rows of an odd number of entries, every other of them 2 bytes off a word.  16-byte reads
+// there are several times slower (4097 -> 11008, one row 79 us, 36 with this), so a lane
+// reads the words around its piece and shifts; the host makes sure that those words hold an
+// entry of the matrix (launch_gated).
+template <typename M, bool BWD, int Y, int U, bool SHIFT>
 __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
     typedef typename M::Elem E;
     extern __shared__ __attribute__((aligned(16))) char few_lds[];
@@ -136,17 +168,17 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
     const int nblocks = f.d / (32 * U), nsteps = f.d / 32;   // what is left goes to the last wave
 
     struct Block {
-        u32x4 g[U], u[U], x[U][Y];
+        FewPiece<SHIFT> g[U], u[U], x[U][Y];
     };
     auto load = [&](Block& b, int k) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) b.g[i] = load_words(wg + k + i * 32);
+        for (int i = 0; i < U; ++i) b.g[i].load(wg + k + i * 32);
 #pragma unroll
-        for (int i = 0; i < U; ++i) b.u[i] = load_words(wu + k + i * 32);
+        for (int i = 0; i < U; ++i) b.u[i].load(wu + k + i * 32);
 #pragma unroll
         for (int y = 0; y < Y; ++y)
 #pragma unroll
-            for (int i = 0; i < U; ++i) b.x[i][y] = load_words(x[y] + k + i * 32);
+            for (int i = 0; i < U; ++i) b.x[i][y].load(x[y] + k + i * 32);
     };
     f32x4 G[Y] = {}, Up[Y] = {};
     auto add = [&](u32x4 g, u32x4 u, const u32x4 (&v)[Y]) {
@@ -167,26 +199,41 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
         for (int k = 0; k < 2; ++k) {
             if (c + k * waves >= nblocks) break;
 #pragma unroll
-            for (int i = 0; i < U; ++i) add(b[k].g[i], b[k].u[i], b[k].x[i]);
-        }
-    }
-    if (wave == waves - 1) {
-        for (int s = nblocks * U; s < nsteps; ++s) {
-            u32x4 v[Y];
+            for (int i = 0; i < U; ++i) {
+                u32x4 v[Y];
 #pragma unroll
-            for (int y = 0; y < Y; ++y) v[y] = load_words(x[y] + s * 32);
-            add(load_words(wg + s * 32), load_words(wu + s * 32), v);
+                for (int y = 0; y < Y; ++y) v[y] = b[k].x[i][y].get(x[y]);
+                add(b[k].g[i].get(wg), b[k].u[i].get(wu), v);
+            }
         }
     }
-    if (f.d % 32 != 0 && wave == waves - 1) {
+    // What is left: whole steps one a wave, then the piece of a step.
+    for (int s = nblocks * U + wave; s < nsteps; s += waves) {
+        u32x4 v[Y];
+#pragma unroll
+        for (int y = 0; y < Y; ++y) v[y] = load_words(x[y] + s * 32);
+        add(load_words(wg + s * 32), load_words(wu + s * 32), v);
+    }
+    if (f.d % 32 != 0 && wave == (nsteps - nblocks * U) % waves) {
         const int k = nsteps * 32, left = f.d - k - kq * 8;   // entries of this lane's pieces
+        // 8 entries from p + k, zeros past the row: its last 8 entries moved down
         auto part = [&](const E* p) {
-            uint16_t v[8];
+            u32x4 r = u32x4(0);
+            if (left >= 8) {
+                r = load_words(p + k);
+            } else if (left > 0 && f.d >= 8) {
+                unsigned __int128 v;
+                const u32x4 last = load_words(p + k + left - 8);
+                __builtin_memcpy(&v, &last, 16);
+                v >>= 16 * (8 - left);
+                __builtin_memcpy(&r, &v, 16);
+            } else if (left > 0) {
+                uint16_t v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] = e < left ? __builtin_bit_cast(uint16_t, p[k + e]) : (uint16_t)0;
-            u32x4 r;
-            __builtin_memcpy(&r, v, 16);
+                for (int e = 0; e < 8; ++e)
+                    v[e] = e < left ? __builtin_bit_cast(uint16_t, p[k + e]) : (uint16_t)0;
+                __builtin_memcpy(&r, v, 16);
+            }
             return r;
         };
         u32x4 v[Y];
@@ -289,19 +336,29 @@ __global__ __launch_bounds__(256) void k_prod_join(ProdArgs a) {
     prod_store<E>(a, t, i, v);
 }
 
-// dst[r][0 .. cols_p) = src[r][0 .. cols), zeros behind; 16-bit entries.
-__global__ __launch_bounds__(256) void k_pad_rows(const uint16_t* __restrict__ src, int64_t ld,
-                                                  int64_t rows, int64_t cols, int64_t cols_p,
-                                                  uint16_t* __restrict__ dst) {
-    const int64_t per = cols_p / 8, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= rows * per) return;
-    const int64_t r = e / per, c = e % per * 8;
+// Up to three matrices of the same width copied into rows of cols_p, zeros behind;
+// 16-bit entries.
+struct PadArgs {
+    const uint16_t* src[3];
+    uint16_t* dst[3];
+    int64_t ld[3], end[3];   // end: 8-entry pieces up to and with this one
+    int64_t cols, cols_p;
+};
+__global__ __launch_bounds__(256) void k_pad_rows(PadArgs a) {
+    int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= a.end[2]) return;
+    const int i = e < a.end[0] ? 0 : e < a.end[1] ? 1 : 2;
+    if (i > 0) e -= a.end[i - 1];
+    const int64_t per = a.cols_p / 8, r = e / per, c = e % per * 8;
+    const uint16_t* const src = i == 0 ? a.src[0] : i == 1 ? a.src[1] : a.src[2];
+    uint16_t* const dst = i == 0 ? a.dst[0] : i == 1 ? a.dst[1] : a.dst[2];
+    const uint16_t* const row = src + r * (i == 0 ? a.ld[0] : i == 1 ? a.ld[1] : a.ld[2]);
     Pack<uint16_t, 8> v;
-    if (c + 8 <= cols) {
-        v = load_pack<uint16_t, 8>(src + r * ld + c);
+    if (c + 8 <= a.cols) {
+        v = load_pack<uint16_t, 8>(row + c);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.v[j] = c + j < cols ? src[r * ld + c + j] : (uint16_t)0;
+        for (int j = 0; j < 8; ++j) v.v[j] = c + j < a.cols ? row[c + j] : (uint16_t)0;
     }
     store_pack(dst + e * 8, v);
 }
@@ -321,55 +378,80 @@ static bool direct_rows(const void* p, int64_t ld, int64_t cols) {
 
 // Rows up to which the gated product is taken as one of few rows: 4096 -> 11008, 32 rows 52 us
 // (64 x 64 tiles: 50, and two copies more for rows that are no 16-byte multiples), 64 rows
-// 73 against 50.
+// 73 against 50.  And with few tiles (by 64 x 64) a CU: 2048 -> 512, 200 rows (a quarter) 10.7 us
+// against 14.3, 500 rows (half) 17.5 against 14.2.
 constexpr int64_t FEW_ROWS = 32;
+constexpr int64_t FEW_TILES = 4;
 
 template <typename M, bool BWD, int Y, int U>
 static void launch_gated_few(const FewArgs& f, const GatedArgs& a, hipStream_t st) {
+    // Words around the pieces of odd rows: the first row of each matrix begins on a word, and whole steps
+    // end before the row does, so an entry before and one behind each piece are in the matrix.
+    const bool shift = (f.ldx % 2 != 0 || f.ldw % 2 != 0) && f.d % 32 != 0 && (uintptr_t)f.x % 4 == 0 &&
+                       (uintptr_t)f.wg % 4 == 0 && (uintptr_t)f.wu % 4 == 0;
     const dim3 grid((unsigned)(((BWD ? a.fp : a.f) + 15) / 16), (unsigned)((a.T + Y * 16 - 1) / (Y * 16)));
-    const int blocks = f.d / (32 * U);   // as many waves as have work, 8 at most
+    constexpr int US = 2;   // (steps at a time with SHIFT, which takes more registers)
+    const int blocks = f.d / (32 * (shift ? US : U));   // as many waves as have work, 8 at most
     const int waves = blocks >= 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
-    hipLaunchKernelGGL((k_gated_few<M, BWD, Y, U>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
+    if (shift)
+        hipLaunchKernelGGL((k_gated_few<M, BWD, Y, US, true>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
+    else
+        hipLaunchKernelGGL((k_gated_few<M, BWD, Y, U, false>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
+}
+
+// Whether the kernel for few rows takes it: few rows, or few tiles with a long way to sum.
+static bool gated_few_rows(int64_t T, int64_t f, int64_t d) {
+    if (T <= FEW_ROWS) return true;
+    return ((f + 31) / 32) * ((T + 63) / 64) * FEW_TILES <= op_cus() && d >= 512;
 }
 
 template <typename M, bool BWD>
 static void launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
-    if (a.T <= 16) return launch_gated_few<M, BWD, 1, 4>(few, a, st);
-    if (a.T <= FEW_ROWS) return launch_gated_few<M, BWD, 2, 2>(few, a, st);
+    if (gated_few_rows(a.T, a.f, few.d))
+        return a.T <= 16 ? launch_gated_few<M, BWD, 1, 4>(few, a, st)
+                         : launch_gated_few<M, BWD, 2, 2>(few, a, st);
     const int64_t f = BWD ? a.fp : a.f;   // (the padding is written, too)
-    auto tiles = [&](int64_t b) { return ((f + b / 2 - 1) / (b / 2)) * ((a.T + b - 1) / b); };
-    const int ncu = op_cus();
     auto go = [&](auto tile) {
         typedef decltype(tile) Tl;
         a.ni = (int)((f + Tl::ROWS / 2 - 1) / (Tl::ROWS / 2));
         a.nt = (int)((a.T + Tl::COLS - 1) / Tl::COLS);
         hipLaunchKernelGGL((k_gated<Tl, BWD>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
     };
-    if (tiles(256) >= ncu)
+    const int tile = pick_tile(2 * f, a.T, op_cus(), true);
+    if (tile == 256)
         go(BigTile<M>());
-    else if (tiles(128) >= ncu)
+    else if (tile == 128)
         go(Tile<M, 128, 128, 2, 4, 2>());
     else
         go(Tile<M, 64, 64, 2, 2, 4>());
 }
 
-// How a product is cut: tile edge, and parts of the summed axis where the tiles alone
-// leave CUs idle (each part of 8 chunks at least).
+// How a product is cut: tile edge, and parts of the summed axis (of 4 chunks at least),
+// by the least time: 1.55 us for a chunk's round of 256 x 256, the partial sums written and read
+// at 4 TB/s, 4 us for the launch that joins them.
 struct ProdPlan {
     int tile, parts, part_chunks;
     size_t bytes;   // of the partial sums
 };
 static ProdPlan prod_plan(int64_t i, int64_t t, int chunks, int ncu) {
-    auto tiles = [&](int64_t b) { return ((i + b - 1) / b) * ((t + b - 1) / b); };
-    ProdPlan p{256, 1, chunks, 0};
-    if (tiles(256) >= ncu) return p;
-    p.tile = tiles(128) * std::max(1, chunks / 8) >= ncu ? 128 : 64;
-    const int64_t want = (ncu + tiles(p.tile) - 1) / tiles(p.tile);
-    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, chunks / 8));
-    p.part_chunks = (chunks + parts - 1) / parts;
-    p.parts = (chunks + p.part_chunks - 1) / p.part_chunks;
-    if (p.parts > 1) p.bytes = up256((size_t)p.parts * t * ((i + 7) / 8 * 8) * sizeof(float));
-    return p;
+    ProdPlan best{64, 1, chunks, 0};
+    double least = 1e30;
+    for (int tile : {256, 128, 64}) {
+        const int64_t tiles = ((i + tile - 1) / tile) * ((t + tile - 1) / tile);
+        for (int parts = 1; parts <= 32 && (parts == 1 || chunks / parts >= 4); ++parts) {
+            const int each = (chunks + parts - 1) / parts, n = (chunks + each - 1) / each;
+            if (n != parts) continue;
+            const double us = tile_rounds(tile, tiles * n, ncu) * (each * 1.55 + 6.0) +
+                              (n > 1 ? 8.0 * n * i * t / 4e6 + 4.0 : 0.0);
+            if (us < least) {
+                least = us;
+                best = ProdPlan{tile, n, each, 0};
+            }
+        }
+    }
+    if (best.parts > 1)
+        best.bytes = up256((size_t)best.parts * t * ((i + 7) / 8 * 8) * sizeof(float));
+    return best;
 }
 
 template <typename M, bool ACOLS, bool BCOLS>
@@ -412,13 +494,6 @@ static PadPlan pad_plan(const void* x, int64_t ldx, const void* wg, const void* 
     return p;
 }
 
-static void pad_copy(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t cols_p,
-                     void* dst, hipStream_t st) {
-    hipLaunchKernelGGL(k_pad_rows, grid256(rows * (cols_p / 8)), dim3(256), 0, st,
-                       static_cast<const uint16_t*>(src), ld, rows, cols, cols_p,
-                       static_cast<uint16_t*>(dst));
-}
-
 // x and the weights as operands of the gated product, through padded copies at `*at`
 // where needed.
 static void gated_operands(GatedArgs& a, const PadPlan& p, const void* x, int64_t ldx,
@@ -427,19 +502,31 @@ static void gated_operands(GatedArgs& a, const PadPlan& p, const void* x, int64_
     // (a copy's padding is zeros; without copies what lies past d reads as zeros)
     const int64_t kbytes = p.x && p.w ? 2 * p.dp : 2 * ((d + 7) / 8 * 8);
     a.x = operand(x, 2 * ldx, a.T, kbytes);
-    if (p.x) {
-        pad_copy(x, ldx, a.T, d, p.dp, *at, st);
-        a.x = operand(*at, 2 * p.dp, a.T, kbytes);
-        *at += p.xbytes;
-    }
     a.w = operand(wg, 2 * ldw, a.f, kbytes);
     a.w.base2 = static_cast<const char*>(wu);
+    PadArgs c{};
+    int n = 0;
+    int64_t pieces = 0;
+    auto copy = [&](const void* src, int64_t ld, int64_t rows, size_t bytes) {
+        char* const to = *at;
+        c.src[n] = static_cast<const uint16_t*>(src);
+        c.dst[n] = reinterpret_cast<uint16_t*>(to);
+        c.ld[n] = ld;
+        pieces += rows * (p.dp / 8);
+        for (int i = n; i < 3; ++i) c.end[i] = pieces;
+        ++n;
+        *at += bytes;
+        return to;
+    };
+    if (p.x) a.x = operand(copy(x, ldx, a.T, p.xbytes), 2 * p.dp, a.T, kbytes);
     if (p.w) {
-        pad_copy(wg, ldw, a.f, d, p.dp, *at, st);
-        pad_copy(wu, ldw, a.f, d, p.dp, *at + p.wbytes, st);
-        a.w = operand(*at, 2 * p.dp, a.f, kbytes);
-        a.w.base2 = *at + p.wbytes;
-        *at += 2 * p.wbytes;
+        a.w = operand(copy(wg, ldw, a.f, p.wbytes), 2 * p.dp, a.f, kbytes);
+        a.w.base2 = copy(wu, ldw, a.f, p.wbytes);
+    }
+    if (n > 0) {
+        c.cols = d;
+        c.cols_p = p.dp;
+        hipLaunchKernelGGL(k_pad_rows, grid256(pieces), dim3(256), 0, st, c);
     }
     a.chunks = (int)((kbytes + CHUNK_BYTES - 1) / CHUNK_BYTES);
 }
@@ -522,7 +609,7 @@ extern "C" bakron_status bakron_gated_mlp(const void* x, int64_t ldx, int64_t T,
     bakron_status st = mlp_sizes(who, ldx, T, d, ldw, f, dtype, act);
     if (st != BAKRON_OK) return st;
     if (h && ldh < f) return bk::op_fail(who, "leading dimension below f");
-    const bool many = T > bk::FEW_ROWS;
+    const bool many = !bk::gated_few_rows(T, f, d);
     const bk::PadPlan p = bk::pad_plan(x, ldx, w_gate, w_up, ldw, T, d, f, many, many);
     bool query;
     st = bk::op_workspace(who, work, work_bytes, p.xbytes + 2 * p.wbytes, &query);
@@ -562,7 +649,7 @@ extern "C" bakron_status bakron_gated_mlp_backward(const void* dh, int64_t lddh,
     if (st != BAKRON_OK) return st;
     if (lddh < f || (dx && lddx < d) || (dw_gate && lddw < d))
         return bk::op_fail(who, "leading dimension too small");
-    const bool many = T > bk::FEW_ROWS;
+    const bool many = !bk::gated_few_rows(T, f, d);
     const bk::PadPlan p = bk::pad_plan(x, ldx, w_gate, w_up, ldw, T, d, f, many || dw_gate, many || dx);
     const bk::BackwardPlan b =
         bk::backward_plan(std::max<int64_t>(T, 1), d, f, dx != nullptr, dw_gate != nullptr, bk::op_cus());

@@ -594,6 +594,29 @@ __device__ inline void tile_of(int v, int ni, int nt, int strip, int* i, int* t)
     *t = in / w;
 }
 
+// Which tile, by the rounds of workgroups that n of them take: a round of 256 x 256 (one a
+// CU) is the unit; 128 x 128 takes 0.63 of it with two a CU and 0.42 with one, 64 x 64 0.30
+// and 0.20; a round that leaves half of the CUs idle 0.8 (16-bit product 1024 to 8192 x 4096 x 4096
+// to 11008 with each tile forced: 256 x 256 ahead by 20% on full rounds, 12% behind at half a
+// round).
+inline double tile_rounds(int tile, int64_t n, int ncu) {
+    if (tile == 256) {
+        const int64_t rest = n % ncu;
+        return (double)(n / ncu) + (rest == 0 ? 0.0 : 2 * rest <= ncu ? 0.8 : 1.0);
+    }
+    const double two = tile == 128 ? 0.63 : 0.30, one = tile == 128 ? 0.42 : 0.20;
+    const int64_t rest = n % (2 * ncu);
+    return (double)(n / (2 * ncu)) * two + (rest == 0 ? 0.0 : rest <= ncu ? one : two);
+}
+// The tile of least rounds for i x t outputs; `big`: 256 x 256 can be had.
+inline int pick_tile(int64_t i, int64_t t, int ncu, bool big) {
+    auto rounds = [&](int b) { return tile_rounds(b, ((i + b - 1) / b) * ((t + b - 1) / b), ncu); };
+    int best = 64;
+    if (rounds(128) <= rounds(64)) best = 128;
+    if (big && rounds(256) <= rounds(best)) best = 256;
+    return best;
+}
+
 // N consecutive entries, `valid` of them inside the row.
 template <typename E, int N>
 __device__ inline void store_n(E* p, const float (&v)[N], int64_t valid) {

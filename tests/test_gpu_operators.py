@@ -225,6 +225,10 @@ LINEAR = [
     (2050, 200, 2100, 4, 64, False, "none", None, "f32"),
     (4100, 256, 4200, 4, 0, False, "none", "add", "bf16"),
     (4100, 130, 4200, 8, 0, True, "none", None, "f16"),
+    # few tiles, a long way to sum
+    (70, 3000, 40, 8, 128, True, "gelu", "mul", "f32"),
+    (300, 2100, 150, 4, 64, False, "none", None, "bf16"),
+    (129, 1500, 33, 4, 0, False, "silu", "add", "f16"),
 ]
 
 
@@ -347,7 +351,9 @@ def _mlp_errors(x, wg, wu, act):
 
 MLP = [(1, 1, 1), (1, 64, 32), (1, 1000, 333), (2, 8, 100), (5, 130, 257), (16, 512, 512), (17, 72, 40),
        (64, 264, 130), (129, 200, 1000), (257, 1000, 270), (700, 96, 1500), (2100, 40, 2200),
-       (4100, 40, 2200), (40, 4100, 2200), (4200, 4104, 70)]
+       (4100, 40, 2200), (40, 4100, 2200), (4200, 4104, 70),
+       # odd rows read a word at a time; whole steps that end with the row
+       (3, 97, 33), (30, 1001, 65), (16, 33, 40), (90, 1025, 48), (200, 513, 96)]
 
 
 @pytest.mark.parametrize("T,d,f", MLP)
@@ -432,6 +438,30 @@ def test_gated_mlp_gradient_against_differences(act):
         diff = (value(1e-5) - value(-1e-5)) / 2e-5
         size = float((grads[k].abs() * v.abs()).sum())
         assert abs(diff - float((grads[k] * v).sum())) <= 3 * _u(dtype) * size + 1e-6, k
+
+
+@pytest.mark.parametrize("d,ld,shift", [(64, 65, 0), (96, 97, 1), (65, 65, 1), (100, 101, 2), (31, 33, 0)])
+def test_gated_mlp_odd_rows(d, ld, shift):
+    """Weights and tokens in rows an odd number of entries apart, beginning on a word or off
+    one, the last row ending where the buffer ends."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("mlp odd rows", d, ld, shift)
+    T, f = 5, 37
+
+    def odd(t):
+        rows = t.shape[0]
+        buf = torch.full(((rows - 1) * ld + d + shift,), 3.0, dtype=t.dtype, device="cuda:0")
+        v = buf[shift:].as_strided((rows, d), (ld, 1))
+        v.copy_(t)
+        return v
+    x, wg, wu, dh = _mlp_inputs(T, d, f, "bf16", 71)
+    want = pk.gated_mlp(*(t.to("cuda:0") for t in (x, wg, wu)))
+    assert torch.equal(pk.gated_mlp(odd(x), odd(wg), odd(wu)), want)
+    a = pk.gated_mlp_backward(*(t.to("cuda:0") for t in (dh, x, wg, wu)))
+    b = pk.gated_mlp_backward(dh.to("cuda:0"), odd(x), odd(wg), odd(wu))
+    for p, q in zip(a, b):
+        assert torch.equal(p, q)
 
 
 def test_gated_mlp_no_rows():
