@@ -500,6 +500,7 @@ bakron_status bakron_mlp_local_factors_iter(const float *x, const float *g, cons
  *     the next, at least the row's length) where one is given, else contiguous;
  *     any element alignment is accepted, rows of 16-byte multiples at 16-byte
  *     addresses are read faster;
+ *   - outputs overlap no input or other output, except where a call says so;
  *   - T is the number of rows (tokens), 0 <= T <= 2^31 - 1; T = 0 does nothing;
  *   - sums, norms, softmax statistics and products are accumulated in 32 bits
  *     and rounded once when they are stored, except where a call says otherwise;

@@ -72,7 +72,10 @@ static __device__ const uint4 tile_zeros = {0, 0, 0, 0};
 //
 // Rows (k contiguous): a row of BYTES bytes is cut into 16-byte pieces; slot s of row r
 // holds piece s ^ (r & 7), or s ^ ((r >> 2) & 3) in rows of 64 bytes.  A lane's 16 (or 8,
-// packed) bytes of a fragment are one read.
+// packed) bytes of a fragment are one read.  Packed rows are read 16 bytes (32 codes) a lane, for
+// both steps of a chunk: lane q = lane / 16 has codes 32 q .. 32 q + 31, 16 for each step, and
+// the other operand's pieces follow (the order of the summed axis is free).  Only where sums end every
+// 64 codes (FLUSH = 1) the steps are the chunk's halves.
 //
 // Columns (k outside): row k holds UNITS units of 16 entries (32 bytes); unit u of row k lies at
 // u ^ f(k), f(k) from the bits of k that differ between the 16 rows that a transposing read
@@ -248,6 +251,7 @@ struct Tile {
             s.load(chunk, lds + wave * 1024, WAVES * 1024);
         }
     };
+    static constexpr bool PAIRED = M::A_BYTES != CHUNK_BYTES && FLUSH != 1;
     // A fragment: unit u of R / 16, step s.
     template <bool C, int R, int BYTES>
     static __device__ inline i32x4 fragment(const char* lds, int u, int s, int lane) {
@@ -258,10 +262,14 @@ struct Tile {
             const i32x2 x = read_transposed(p), y = read_transposed(p + 4 * 2 * R);
             return i32x4{x[0], x[1], y[0], y[1]};
         } else {
-            const int r = u * 16 + r16, k = s * 4 + kq;
-            if constexpr (BYTES == CHUNK_BYTES)
+            const int r = u * 16 + r16, k = PAIRED ? 2 * kq + s : s * 4 + kq;
+            if constexpr (BYTES == CHUNK_BYTES) {
                 return *reinterpret_cast<const i32x4*>(lds + r * BYTES + (row_piece<BYTES>(r, k) << 4));
-            else
+            } else if constexpr (PAIRED) {
+                const i32x4 w =
+                    *reinterpret_cast<const i32x4*>(lds + r * BYTES + (row_piece<BYTES>(r, kq) << 4));
+                return unpack_codes(i32x2{w[2 * s], w[2 * s + 1]});
+            } else
                 return unpack_codes(*reinterpret_cast<const i32x2*>(
                     lds + r * BYTES + (row_piece<BYTES>(r, k >> 1) << 4) + ((k & 1) << 3)));
         }
@@ -369,6 +377,7 @@ struct BigTile {
     static constexpr int A_LDS = ROWS * M::A_BYTES, B_LDS = COLS * CHUNK_BYTES;
     static constexpr int A_HALF = A_LDS / 2, B_HALF = B_LDS / 2;
     static constexpr int LDS = 2 * (A_LDS + B_LDS);
+    static constexpr bool PAIRED = M::A_BYTES != CHUNK_BYTES;
     static constexpr int NA = M::A_BYTES / 64;   // loads of a half of A by a wave (of B: 2)
     typedef M Mma;
     typedef typename M::Acc Acc;
@@ -422,13 +431,12 @@ struct BigTile {
                     at[u] = k * 256 + (((unit0 + u) ^ col_twist<8>(k)) << 5) + (r16 & 3) * 8;
             } else {
 #pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    const int k = st * 4 + kq;
+                for (int st = 0; st < 2; ++st)
                     at[st] = (unit0 * 16 + r16) * BYTES +
-                             (BYTES == CHUNK_BYTES
-                                  ? row_piece<BYTES>(r16, k) << 4
-                                  : (row_piece<BYTES>(r16, k >> 1) << 4) + ((k & 1) << 3));
-                }
+                             (row_piece<BYTES>(r16, BYTES != CHUNK_BYTES ? kq
+                                                    : PAIRED             ? 2 * kq + st
+                                                                         : st * 4 + kq)
+                              << 4);
             }
         }
         __device__ inline i32x4 get(const char* half, int u, int st) const {
@@ -438,10 +446,11 @@ struct BigTile {
                 return i32x4{x[0], x[1], y[0], y[1]};
             } else {
                 const char* const p = half + at[st] + u * 16 * BYTES;
+                const i32x4 w = *reinterpret_cast<const i32x4*>(p);
                 if constexpr (BYTES == CHUNK_BYTES)
-                    return *reinterpret_cast<const i32x4*>(p);
+                    return w;
                 else
-                    return unpack_codes(*reinterpret_cast<const i32x2*>(p));
+                    return unpack_codes(i32x2{w[2 * st], w[2 * st + 1]});
             }
         }
     };

@@ -680,6 +680,94 @@ def test_token_logprobs_gradient_against_differences():
     assert abs(diff - float((d * v).sum())) <= 1e-7 + 600 * U32 * float((d.abs() * v.abs()).sum())
 
 
+# ---------------------------------------------------------------- offsets beyond 32 bits
+def test_logprobs_beyond_32_bits():
+    """More than 2^31 logits: the last rows, forward and backward."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("logprob large")
+    T, V = 16500, 131072
+    z = torch.empty((T, V), dtype=torch.bfloat16, device="cuda:0")
+    z.zero_()
+    tail = _logits(3, V, "bf16", 131, False)
+    z[-3:] = tail.to("cuda:0")
+    target = torch.arange(T, dtype=torch.int64)
+    r = pk.token_logprobs(z, target.to("cuda:0"), top=3)
+    lse, H, lp, idx, _, logp, p = _logprob64(tail, target[-3:], 3)
+    _within(r.lse[-3:], lse, 300 * U32 * (1 + lse.abs()), "lse")
+    _within(r.logprob[-3:], lp, 300 * U32 * (1 + lp.abs()), "logprob")
+    assert torch.equal(r.top_index[-3:].cpu(), idx)
+    assert abs(float(r.lse[7]) - math.log(V)) < 1e-4
+    pk.token_logprobs_backward(z, target.to("cuda:0"), r.lse, g_logprob=torch.ones(T, device="cuda:0"), out=z)
+    one = (torch.arange(V)[None] == target[-3:, None]).double()
+    _within(z[-3:], one - p, 2.0 ** -8 * (one - p).abs() + 300 * U32 * (p + one), "d")
+
+
+def test_linear_beyond_32_bits():
+    """More than 2^31 outputs."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("linear large")
+    T, n, m = 66000, 128, 32768
+    q = torch.randint(-127, 128, (T, n), generator=_gen(1), dtype=torch.int8)
+    c = _codes(m, n, 4, 2)
+    y = pk.linear(q.to("cuda:0"), None, pk.pack_codes(c.to("cuda:0")), torch.full((m,), 1e-3, device="cuda:0"))
+    for rows in (slice(0, 2), slice(T - 3, T)):
+        want = q[rows].double() @ c.double().t() * float(torch.tensor(1e-3, dtype=torch.float32))
+        _within(y[rows], want, (2.0 ** -8 + 4 * U32) * want.abs(), "y")
+
+
+# ---------------------------------------------------------------- refusals of the binding
+def test_binding_refuses_what_does_not_fit():
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    dev = "cuda:0"
+    bf = dict(dtype=torch.bfloat16, device=dev)
+    x, w = torch.zeros((4, 64), **bf), torch.zeros((8, 64), **bf)
+    with pytest.raises(ValueError):
+        pk.gated_mlp(x, w, w[:4])
+    with pytest.raises(ValueError):
+        pk.gated_mlp(x, w[:, :32], w[:, :32])
+    with pytest.raises(TypeError):
+        pk.gated_mlp(x, w.float(), w)
+    with pytest.raises(ValueError):
+        pk.gated_mlp(x.t(), w, w)
+    with pytest.raises(pk.BakronError):
+        pk.gated_mlp(x.float(), w.float(), w.float())
+    with pytest.raises(KeyError):
+        pk.gated_mlp(x, w, w, act="tanh")
+    with pytest.raises(ValueError):
+        pk.gated_mlp(x[:1].expand(4, 64), w, w)               # rows that overlap
+    with pytest.raises(ValueError):
+        pk.gated_mlp_backward(x, x, w, w)
+    q = torch.zeros((4, 100), dtype=torch.int8, device=dev)    # rows that are not padded
+    codes = pk.pack_codes(torch.zeros((8, 100), dtype=torch.int8, device=dev))
+    with pytest.raises((ValueError, pk.BakronError)):
+        pk.linear(q, None, codes, torch.ones(8, device=dev))
+    good = _padded_rows(q.cpu())
+    with pytest.raises(ValueError):
+        pk.linear(good, None, codes, torch.ones(9, device=dev))
+    with pytest.raises(ValueError):
+        pk.linear(good, torch.ones(5, device=dev), codes, torch.ones(8, device=dev))
+    with pytest.raises(TypeError):
+        pk.linear(good.float(), None, codes, torch.ones(8, device=dev))
+    with pytest.raises(pk.BakronError):
+        pk.linear(good, None, codes, torch.ones((8, 4), device=dev), group_size=32)
+    with pytest.raises(ValueError):
+        pk.linear(good, None, codes, torch.ones(8, device=dev), other=torch.zeros((4, 7), **bf))
+    z = torch.zeros((4, 50), device=dev)
+    with pytest.raises(TypeError):
+        pk.token_logprobs(z, torch.zeros(4, dtype=torch.int32, device=dev))
+    with pytest.raises(pk.BakronError):
+        pk.token_logprobs(z, None, top=51)
+    with pytest.raises(TypeError):
+        pk.token_logprobs(z.double())
+    with pytest.raises(ValueError):
+        pk.rmsnorm_quant(x, weight=torch.ones(63, device=dev))
+    with pytest.raises(pk.BakronError):
+        pk.rmsnorm_quant(x, eps=-1.0)
+
+
 # ---------------------------------------------------------------- capture into graphs
 def test_operators_replay_from_a_graph():
     """All operators in one graph, replayed three times on changed inputs with eager
