@@ -31,26 +31,70 @@ constexpr int64_t FEW_ROWS = 32;
 // against 35; 4096 x 160, 127 rows 8.2 against 15.2.
 constexpr int64_t FEW_TILES = 2;
 
-// y_t,i..i+N-1 from the sums z (scales applied).
+// y_t,i..i+N-1 from the sums z (scales applied), the bias and the entries of `other`.
 template <typename E, int N>
-__device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, float (&z)[N]) {
+__device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, float (&z)[N],
+                                    const float (&bias)[N], const float (&other)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        float v = act_value(z[j] + bias[j], a.act);
+        if (a.combine == BAKRON_COMBINE_ADD) v += other[j];
+        if (a.combine == BAKRON_COMBINE_MUL) v *= other[j];
+        z[j] = v;
+    }
+    store_n(static_cast<E*>(a.y) + t * a.ldy + i, z, a.m - i);
+}
+
+// Everything after the sums, for a tile: z(j) gives the 8 sums of this lane's row in turn
+// j.  The stores of one row may alias what the next ones read as far as the compiler
+// knows, so the operands of a batch of rows are asked for before its first store (2048 x 8192 x 28672
+// with a factor: 18 us less a round of tiles).
+template <typename E, int TURNS, typename Row, typename Sums>
+__device__ inline void linear_rows(const LinearArgs& a, int64_t i, float unit, bool scaled, Row row,
+                                   Sums sums) {
+    constexpr int BATCH = TURNS < 4 ? TURNS : 32 / (4 * (int)sizeof(E));   // 32 registers of `other`
     const int64_t valid = a.m - i;
-    float v[N];
-    if (a.bias) {
-        load_n(static_cast<const E*>(a.bias) + i, v, valid);
+    float bias[8] = {}, s[8];
 #pragma unroll
-        for (int j = 0; j < N; ++j) z[j] += v[j];
+    for (int j = 0; j < 8; ++j) s[j] = 1.0f;
+    if (valid > 0) {
+        if (a.bias) load_n(static_cast<const E*>(a.bias) + i, bias, valid);
+        if (!scaled) load_n(a.scale + i, s, valid);
     }
-    if (a.act != BAKRON_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) z[j] = act_value(z[j], a.act);
-    }
-    if (a.combine != BAKRON_COMBINE_NONE) {
-        load_n(static_cast<const E*>(a.other) + t * a.ldo + i, v, valid);
+    for (int j0 = 0; j0 < TURNS; j0 += BATCH) {
+        float qs[BATCH];
+        Pack<E, 8> other[BATCH];
 #pragma unroll
-        for (int j = 0; j < N; ++j) z[j] = a.combine == BAKRON_COMBINE_ADD ? z[j] + v[j] : z[j] * v[j];
+        for (int b = 0; b < BATCH; ++b) {
+            const int64_t t = row(j0 + b);
+            qs[b] = t < a.T && a.q_scale ? a.q_scale[t] : 1.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) other[b].v[j] = (E)0.0f;
+            if (a.other && t < a.T && valid > 0) {
+                const E* const p = static_cast<const E*>(a.other) + t * a.ldo + i;
+                if (valid >= 8) {
+                    other[b] = load_pack<E, 8>(p);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < valid) other[b].v[j] = p[j];
+                }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            float z[8], o[8];
+            sums(j0 + b, z);
+            const int64_t t = row(j0 + b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                z[j] *= qs[b] * unit * s[j];
+                o[j] = (float)other[b].v[j];
+            }
+            if (t < a.T && valid > 0) linear_store<E>(a, t, i, z, bias, o);
+        }
     }
-    store_n(static_cast<E*>(a.y) + t * a.ldy + i, z, valid);
 }
 
 template <typename Tl, int FLUSH>
@@ -88,31 +132,21 @@ __global__ __launch_bounds__(Tl::THREADS) void k_linear(LinearArgs a) {
         }
     };
     const auto rows = handover<Tl>(lds, wave, lane, get);
-    constexpr int PER = Tl::UA * 2;   // lanes a row
+    constexpr int PER = Tl::UA * 2, EACH = 64 / PER;   // lanes a row, rows at a time
+    constexpr int TURNS = Tl::UB * 16 / EACH;
     const int p = lane % PER;
-    const int64_t i = i0 + Tl::a0(wave) + p * 8;
-    float s[8];
-    if (!GROUPED) load_n(a.scale + min(i, a.m), s, a.m - i);
-#pragma unroll
-    for (int y = 0; y < Tl::UB; ++y) {
-        rows.put(y);
-#pragma unroll
-        for (int tl = lane / PER; tl < 16; tl += 64 / PER) {
-            const int64_t t = t0 + Tl::b0(wave) + y * 16 + tl;
-            float z[8];
-            rows.take(tl, p, z);
-            if (t >= a.T || i >= a.m) continue;
-            const float qs = (a.q_scale ? a.q_scale[t] : 1.0f) * UNIT;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = GROUPED ? z[j] * qs : z[j] * (qs * s[j]);
-            if (a.dtype == BAKRON_F32)
-                linear_store<float>(a, t, i, z);
-            else if (a.dtype == BAKRON_F16)
-                linear_store<f16_t>(a, t, i, z);
-            else
-                linear_store<bf16_t>(a, t, i, z);
-        }
-    }
+    const int64_t i = i0 + Tl::a0(wave) + p * 8, tw = t0 + Tl::b0(wave) + lane / PER;
+    auto row = [&](int j) { return tw + j * EACH; };
+    auto sums = [&](int j, float (&z)[8]) {
+        if (j * EACH % 16 == 0) rows.put(j * EACH / 16);
+        rows.take(j * EACH % 16 + lane / PER, p, z);
+    };
+    if (a.dtype == BAKRON_F32)
+        linear_rows<float, TURNS>(a, i, UNIT, GROUPED, row, sums);
+    else if (a.dtype == BAKRON_F16)
+        linear_rows<f16_t, TURNS>(a, i, UNIT, GROUPED, row, sums);
+    else
+        linear_rows<bf16_t, TURNS>(a, i, UNIT, GROUPED, row, sums);
 }
 
 // Few rows (a decoding step): bound by reading the codes once, so no tile is staged.  A
@@ -272,12 +306,19 @@ __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) z[j] = (float)p[j] * (qs * s[j]);
         }
+        auto finish = [&](auto e) {
+            typedef decltype(e) E;
+            float bias[4] = {}, other[4] = {};
+            if (a.bias) load_n(static_cast<const E*>(a.bias) + i, bias, a.m - i);
+            if (a.other) load_n(static_cast<const E*>(a.other) + t * a.ldo + i, other, a.m - i);
+            linear_store<E>(a, t, i, z, bias, other);
+        };
         if (a.dtype == BAKRON_F32)
-            linear_store<float>(a, t, i, z);
+            finish(0.0f);
         else if (a.dtype == BAKRON_F16)
-            linear_store<f16_t>(a, t, i, z);
+            finish(f16_t());
         else
-            linear_store<bf16_t>(a, t, i, z);
+            finish(bf16_t());
     }
 }
 

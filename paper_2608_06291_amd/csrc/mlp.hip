@@ -36,7 +36,7 @@ struct FewArgs {
 // Row t, features j .. j + N - 1, from G and U.
 template <typename E, bool BWD, int N>
 __device__ inline void gated_finish(const GatedArgs& a, int64_t t, int64_t j, const float (&G)[N],
-                                    const float (&U)[N]) {
+                                    const float (&U)[N], const float (&dh)[N]) {
     const int64_t valid = a.f - j;
     if constexpr (!BWD) {
         if (valid <= 0) return;
@@ -60,8 +60,7 @@ __device__ inline void gated_finish(const GatedArgs& a, int64_t t, int64_t j, co
         }
     } else {
         if (j >= a.fp) return;
-        float dh[N] = {}, dg[N], du[N];
-        if (valid > 0) load_n(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, valid);
+        float dg[N], du[N];
 #pragma unroll
         for (int r = 0; r < N; ++r) {
             float v, s;
@@ -100,17 +99,37 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
     constexpr int PER = Tl::UA;   // lanes a row: 8 features each
     const int p = lane % PER;
     const int64_t j = f0 + Tl::a0(wave) / 2 + p * 8;
+    const int tl = lane / PER;
+    const int64_t tw = t0 + Tl::b0(wave) + tl;
+    // (all of dh before the first store, which may alias it as far as the compiler knows)
+    u32x4 dh[BWD ? Tl::UB : 1];
+    if constexpr (BWD) {
+#pragma unroll
+        for (int y = 0; y < Tl::UB; ++y) {
+            dh[y] = u32x4(0);
+            const E* const p = static_cast<const E*>(a.dh) + (tw + y * 16) * a.lddh + j;
+            if (tl < 16 && tw + y * 16 < a.T && j + 8 <= a.f) {
+                dh[y] = load_words(p);
+            } else if (tl < 16 && tw + y * 16 < a.T && j < a.f) {
+                float v[8];
+                load_n(p, v, a.f - j);
+                Pack<E, 8> e;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) e.v[r] = (E)v[r];
+                __builtin_memcpy(&dh[y], &e, 16);
+            }
+        }
+    }
 #pragma unroll
     for (int y = 0; y < Tl::UB; ++y) {
         rows.put(y);
-        const int tl = lane / PER;
-        const int64_t t = t0 + Tl::b0(wave) + y * 16 + tl;
-        if (tl >= 16) continue;
-        float G[8], U[8];
-        rows.take(tl, (p >> 1) * 4 + (p & 1), G);
-        rows.take(tl, (p >> 1) * 4 + (p & 1) + 2, U);
-        if (t >= a.T) continue;
-        gated_finish<E, BWD>(a, t, j, G, U);
+        const int64_t t = tw + y * 16;
+        float G[8], U[8], d[8];
+        rows.take(tl & 15, (p >> 1) * 4 + (p & 1), G);
+        rows.take(tl & 15, (p >> 1) * 4 + (p & 1) + 2, U);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) d[r] = BWD ? entry<E>(dh[BWD ? y : 0], r) : 0.0f;
+        if (tl < 16 && t < a.T) gated_finish<E, BWD>(a, t, j, G, U, d);
     }
 }
 
@@ -257,7 +276,10 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
         float gv[4], uv[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) gv[r] = g[r], uv[r] = u[r];
-        if (t < a.T) gated_finish<E, BWD>(a, t, j0 + kq * 4, gv, uv);
+        float dh[4] = {};
+        const int64_t j = j0 + kq * 4;
+        if (BWD && t < a.T && j < a.f) load_n(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, a.f - j);
+        if (t < a.T) gated_finish<E, BWD>(a, t, j, gv, uv, dh);
     }
 }
 
@@ -307,15 +329,17 @@ __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
     for (int y = 0; y < Tl::UB; ++y) {
         rows.put(y);
 #pragma unroll
-        for (int tl = lane / PER; tl < 16; tl += 64 / PER) {
+        for (int k = 0; k < 16 * PER / 64; ++k) {
+            const int tl = k * (64 / PER) + lane / PER;
             const int64_t t = t0 + Tl::b0(wave) + y * 16 + tl;
             float v[8];
             rows.take(tl, p, v);
-            if (i >= a.d || t >= a.end) continue;
-            if (a.parts > 1)
-                store_n(a.partial + (part * a.end + t) * a.dp + i, v, 8);
-            else
-                prod_store<E>(a, t, i, v);
+            if (i < a.d && t < a.end) {
+                if (a.parts > 1)
+                    store_n(a.partial + (part * a.end + t) * a.dp + i, v, 8);
+                else
+                    prod_store<E>(a, t, i, v);
+            }
         }
     }
 }

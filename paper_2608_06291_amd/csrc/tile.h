@@ -562,6 +562,11 @@ struct BigTile {
 // go through LDS (4 KiB a wave, permuted like the operands), and come back eight at a
 // time, neighbouring lanes holding neighbouring ones, so that global memory is read and
 // written in whole lines.  get(a, b): the accumulator of units a, b as fp32.
+//
+// One lane reads what others wrote, with no workgroup barrier between: every lane of the wave
+// has to come through put() and take() together.  The wave barriers keep the compiler from
+// letting lanes with nothing to store run ahead to the next put(); callers put their conditions
+// around the stores alone.
 template <typename Tl, typename Get>
 struct Handover {
     static constexpr int SLOTS = Tl::UA * 4;   // 16-byte slots of a t
@@ -570,10 +575,12 @@ struct Handover {
     Get get;
     __device__ inline void put(int b) const {
         const int t = lane & 15;
+        __builtin_amdgcn_wave_barrier();   // the last take() is over
 #pragma unroll
         for (int a = 0; a < Tl::UA; ++a)
             *reinterpret_cast<f32x4*>(lds + t * (SLOTS * 16) + (((a * 4 + (lane >> 4)) ^ (t & (SLOTS - 1))) << 4)) =
                 get(a, b);
+        __builtin_amdgcn_wave_barrier();
     }
     // i = 8 p .. 8 p + 7 of row t of the unit put last
     __device__ inline void take(int t, int p, float (&v)[8]) const {
