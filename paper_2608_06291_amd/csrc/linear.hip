@@ -47,8 +47,7 @@ __device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, f
 
 // Everything after the sums, for a tile: z(j) gives the 8 sums of this lane's row in turn
 // j.  The stores of one row may alias what the next ones read as far as the compiler
-// knows, so the operands of a batch of rows are asked for before its first store (2048 x 8192 x 28672
-// with a factor: 18 us less a round of tiles).
+// knows, so the operands of a batch of rows are asked for before its first store.
 template <typename E, int TURNS, typename Row, typename Sums>
 __device__ inline void linear_rows(const LinearArgs& a, int64_t i, float unit, bool scaled, Row row,
                                    Sums sums) {

@@ -659,14 +659,30 @@ __device__ inline void load_n(const E* p, float (&v)[N], int64_t valid) {
     }
 }
 
-// Activations and their slopes in fp32: the hardware's exp2 and reciprocal (1 ulp each), the
-// library's erf.
+// Activations and their slopes in fp32, from the hardware's exp2 and reciprocal (1 ulp
+// each).  The normal distribution function of GELU is Abramowitz and Stegun's 7.1.26,
+//   erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2) + e,  t = 1 / (1 + p x),  |e| <= 1.5e-7,
+// whose exponential the slope needs, too; with the library's erf a tile's epilogue takes four times
+// as long (2048 x 8192 x 28672: 489 us, 449 with this, 427 without activation).
 __device__ inline float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896340736f));
 }
+__device__ inline float normal_cdf(float z, float* gauss) {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    const float g = __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.44269504088896340736f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float tail = 0.5f * p * t * g;
+    *gauss = g;
+    return z > 0.0f ? 1.0f - tail : tail;
+}
 __device__ inline float act_value(float z, int act) {
     if (act == BAKRON_ACT_SILU) return z * sigmoid(z);
-    if (act == BAKRON_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    float g;
+    if (act == BAKRON_ACT_GELU) return z * normal_cdf(z, &g);
     return z;
 }
 __device__ inline void act_both(float z, int act, float* value, float* slope) {
@@ -675,10 +691,10 @@ __device__ inline void act_both(float z, int act, float* value, float* slope) {
         *value = z * s;
         *slope = s * (1.0f + z * (1.0f - s));
     } else {
-        const float c = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+        float g;
+        const float c = normal_cdf(z, &g);
         *value = z * c;
-        *slope = c + z * 0.39894228040143268f *
-                         __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.44269504088896340736f));
+        *slope = fmaf(z * 0.39894228040143268f, g, c);
     }
 }
 
