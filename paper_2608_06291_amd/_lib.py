@@ -620,16 +620,17 @@ def _raw_stream(device):
 _work_sizes = {}
 
 
-def _run_op(fn, args, device, work=None, key=None):
+def _run_op(fn, args, device, work=None, key=None, maybe_none=True):
     """Call a workspace-protocol operator; allocates its workspace unless given.  `key`
-    holds everything its size depends on, so that it is asked for once."""
+    holds everything its size depends on, so that it is asked for once; maybe_none: it may
+    need none, so try that first."""
     torch = _torch or _import_torch()
     st = _raw_stream(device)
     if work is None:
         need = _work_sizes.get(key) if key is not None else None
         if need is None:
             size = ctypes.c_size_t(0)
-            if key is None and fn(*args, 256, size, st) == BAKRON_OK:
+            if key is None and maybe_none and fn(*args, 256, size, st) == BAKRON_OK:
                 return   # needs none
             _raise_last(fn(*args, None, size, st))
             need = size.value
@@ -806,7 +807,8 @@ def gated_mlp_backward(dh, x, w_gate, w_up, act: str = "silu", need_dx: bool = T
     dg, du = (torch.empty(f, d, dtype=x.dtype, device=x.device) if need_dw else None for _ in range(2))
     _run_op(lib.bakron_gated_mlp_backward,
             (hp, ldh, xp, ldx, T, d, gp, up, ldw, f, code, ACTS[act], dx.data_ptr() if need_dx else None,
-             d, dg.data_ptr() if need_dw else None, du.data_ptr() if need_dw else None, d), x.device, work)
+             d, dg.data_ptr() if need_dw else None, du.data_ptr() if need_dw else None, d), x.device, work,
+            maybe_none=False)
     return dx, dg, du
 
 

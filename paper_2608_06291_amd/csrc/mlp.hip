@@ -6,6 +6,18 @@
 // that the same lane ends with G and U of the same entries and the activation and the
 // product happen on its registers.  The gradients come from the same product, with dG and
 // dU (rounded to 16 bits, as operands of the products that follow) in its epilogue.
+//
+// G and U are computed again in the backward pass (a sixth of its products more than keeping
+// them would need, and 4 T f bytes less to keep).  dG and dU are rounded to 16 bits, as the
+// products that follow take them: one rounding more than fp32 arithmetic, so dx and the
+// weights' gradients are off by 2.4e-3 of their norm in bf16 where a single rounding gives 1.7e-3.
+// The gradients' products read the weights, x, dG and dU as they lie (columns, see
+// tile.h), with no transposed copies.
+//
+// Measured (bf16, 4096 -> 11008): 8192 rows 1085 to 1220 us by the box, 1210 to 1364 TFLOP/s (the
+// library's product of that size: 1312), matrix cores 67% busy; backward of 4096 rows 1820 to
+// 1910 us: gated product 603, dx 522, dW 665; the first and last take 5.4 rounds of tiles in the
+// time of 6.  One row 35 us: the weights' 180 MB at 5.2 TB/s.
 #include "tile.h"
 
 namespace bk {

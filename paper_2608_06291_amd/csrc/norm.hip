@@ -4,7 +4,11 @@
 //
 // Every entry is read once and stays in registers over the two reductions of its
 // row (the sum of squares, then the largest |y|, which needs the first), so the
-// kernel moves what it must: x and r in, h and q out.  Bound by memory.
+// kernel moves what it must: x and r in, h and q out.  Bound by memory: 4096 x 8192 bf16
+// with a residual 40 us, 5.9 TB/s of 235 MB (a large copy here: 5.2); one row of 4096 3.5 us, all
+// latency.  A row per workgroup of one or two vectors a thread; loads are whole vectors at
+// clamped addresses, issued together (with a branch around each they went one after
+// the other: 47.5 us).
 #include "ops.h"
 
 namespace bk {

@@ -370,6 +370,13 @@ struct Tile {
 // read it, and the same half of the chunk after next is loaded over it: B0 in phase 1, A0 and A1 in
 // phase 2, B1 in phase 3, five phases or more before they are read.  Loads past the last
 // chunk read it again, so that the waits can count.
+//
+// 4096 x 4096 x 22016 bf16: 522 us, 1415 TFLOP/s (the library's product: 1326), 630 with the same
+// tile, two buffers and one barrier a chunk.  Bound by power and issue: matrix cores 67%
+// busy at that rate, LDS 26% of the cycles and no bank conflicts.  Two steps that mattered: loads from a
+// scalar base (vector addresses: 572 us) and loads in assembly (the compiler's own waits before
+// transposing reads: 674).  One workgroup a CU, so a tile's prologue and epilogue overlap nothing: 15
+// to 25 us a round.
 template <typename M, bool ACOLS = false, bool BCOLS = false>
 struct BigTile {
     static constexpr bool BIG = true;
