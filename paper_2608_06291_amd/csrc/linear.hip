@@ -360,13 +360,20 @@ static void launch_linear(const LinearArgs& a, hipStream_t st) {
     if (fits && ((a.m + 63) / 64) * ((a.T + 63) / 64) * FEW_TILES <= ncu && a.chunks >= 8)
         return launch_linear_few<M, FLUSH, 2, 2>(a, st);
     const int tile = pick_tile(a.m, a.T, ncu, FLUSH == 0);
+    // Three buffers of 4-bit rows leave room for two workgroups a CU, those of 8-bit rows do not.
+    const bool deep = M::A_BYTES < CHUNK_BYTES || one_a_cu(128, a.m, a.T);
     if constexpr (FLUSH == 0) {
         if (tile == 256) return launch_linear_tile<BigTile<M>, 0>(a, st);
-        if (tile == 128) return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2>, 0>(a, st);
+        if (tile == 128 && deep) return launch_linear_tile<Tile<M, 128, 128, 4, 2, 3>, 0>(a, st);
+        if constexpr (M::A_BYTES == CHUNK_BYTES)
+            if (tile == 128) return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2>, 0>(a, st);
         launch_linear_tile<Tile<M, 64, 64, 2, 2, 4>, 0>(a, st);
     } else {
-        if (tile == 128)
-            return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2, false, false, FLUSH>, FLUSH>(a, st);
+        if (tile == 128 && deep)
+            return launch_linear_tile<Tile<M, 128, 128, 4, 2, 3, false, false, FLUSH>, FLUSH>(a, st);
+        if constexpr (M::A_BYTES == CHUNK_BYTES)
+            if (tile == 128)
+                return launch_linear_tile<Tile<M, 128, 128, 4, 2, 2, false, false, FLUSH>, FLUSH>(a, st);
         launch_linear_tile<Tile<M, 64, 64, 2, 2, 4, false, false, FLUSH>, FLUSH>(a, st);
     }
 }

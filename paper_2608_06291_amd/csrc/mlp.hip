@@ -456,6 +456,8 @@ static void launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
     const int tile = pick_tile(2 * f, a.T, op_cus(), true);
     if (tile == 256)
         go(BigTile<M>());
+    else if (tile == 128 && one_a_cu(128, 2 * f, a.T))
+        go(Tile<M, 128, 128, 2, 4, 3>());
     else if (tile == 128)
         go(Tile<M, 128, 128, 2, 4, 2>());
     else
@@ -505,6 +507,8 @@ static void launch_prod(ProdArgs a, const ProdPlan& p, void* partial, hipStream_
     };
     if (p.tile == 256)
         go(BigTile<M, ACOLS, BCOLS>());
+    else if (p.tile == 128 && one_a_cu(128, a.a.n, a.b.n, p.parts))
+        go(Tile<M, 128, 128, 2, 4, 3, ACOLS, BCOLS>());
     else if (p.tile == 128)
         go(Tile<M, 128, 128, 2, 4, 2, ACOLS, BCOLS>());
     else

@@ -639,6 +639,13 @@ inline int pick_tile(int64_t i, int64_t t, int ncu, bool big) {
     if (big && rounds(256) <= rounds(best)) best = 256;
     return best;
 }
+// Tiles that leave every CU with one workgroup at most have its LDS to themselves: a third buffer
+// puts two chunks on their way (16-bit product 512 x 4096 x 4096: 50.6 -> 48.6 us, 441 x 2944 x 3304:
+// 49.7 -> 39.0; 8-bit rows 1001 x 4096 x 4096: 27.6 -> 23.7; a fourth adds nothing).  More tiles are
+// better off as two workgroups of two buffers a CU (1111 x 1000 x 2731: 24.4 us, 28.1 with three).
+inline bool one_a_cu(int tile, int64_t i, int64_t t, int parts = 1) {
+    return ((i + tile - 1) / tile) * ((t + tile - 1) / tile) * parts <= op_cus();
+}
 
 // N consecutive entries, `valid` of them inside the row.
 template <typename E, int N>

@@ -229,6 +229,13 @@ LINEAR = [
     (70, 3000, 40, 8, 128, True, "gelu", "mul", "f32"),
     (300, 2100, 150, 4, 64, False, "none", None, "bf16"),
     (129, 1500, 33, 4, 0, False, "silu", "add", "f16"),
+    # one round of tiles, and more
+    (1050, 1100, 2050, 8, 0, True, "none", "add", "bf16"),
+    (1050, 900, 2050, 8, 128, False, "silu", None, "f16"),
+    (1050, 700, 2050, 8, 64, False, "none", None, "f32"),
+    (1050, 1300, 2050, 4, 0, False, "gelu", None, "f16"),
+    (2050, 500, 2300, 8, 128, True, "none", None, "bf16"),
+    (2050, 500, 2300, 8, 192, False, "none", "mul", "f16"),
 ]
 
 
@@ -353,7 +360,9 @@ MLP = [(1, 1, 1), (1, 64, 32), (1, 1000, 333), (2, 8, 100), (5, 130, 257), (16, 
        (64, 264, 130), (129, 200, 1000), (257, 1000, 270), (700, 96, 1500), (2100, 40, 2200),
        (4100, 40, 2200), (40, 4100, 2200), (4200, 4104, 70),
        # odd rows read a word at a time; whole steps that end with the row
-       (3, 97, 33), (30, 1001, 65), (16, 33, 40), (90, 1025, 48), (200, 513, 96)]
+       (3, 97, 33), (30, 1001, 65), (16, 33, 40), (90, 1025, 48), (200, 513, 96),
+       # one round of tiles
+       (1030, 1100, 1030), (1030, 2050, 300)]
 
 
 @pytest.mark.parametrize("T,d,f", MLP)
