@@ -153,9 +153,11 @@ __device__ inline void bare_barrier() {
 // that moves on with the chunks (a scalar: a load takes no vector arithmetic).
 template <bool COLS, int BYTES, int N>
 struct Source {
+    static constexpr int UNIT = COLS ? 64 : BYTES;   // of k in a chunk
     const char *base, *base2;
     int64_t step;        // bytes from chunk to chunk
     int split, last;
+    int whole;           // chunks before the one in which the operand ends
     uint32_t off[N];
     int at[N];           // Columns: row in the chunk; rows: at[0] the piece's byte
     int64_t end;         // k_end
@@ -167,6 +169,7 @@ struct Source {
         split = o.split;
         last = end_chunk - 1;
         end = o.k_end;
+        whole = (int)(end / UNIT);
     }
     // Load i: the lane's piece of tile row `tile_row`, or the 8 columns at `tile_col` of row k.
     __device__ inline void set_row(int i, const Operand& o, int64_t first, int tile_row, int piece) {
@@ -177,27 +180,35 @@ struct Source {
         at[i] = k;
         off[i] = (uint32_t)(k * o.ld) + (first + tile_col < o.n ? 2 * tile_col : 0);
     }
-    // All loads of a chunk, number i to to + i * stride.
-    __device__ inline void load(int chunk, uint32_t to, int stride) const {
-        constexpr int UNIT = COLS ? 64 : BYTES;
-        int c = min(chunk, last);   // (past the last chunk: that one again, not used)
+    // Where a chunk lies: worked out before the barrier that its loads come after, because nothing
+    // runs beside scalar arithmetic that all waves do at once behind one.
+    struct Chunk {
+        const char* b;
+        int number;   // in its part
+    };
+    __device__ inline Chunk chunk(int number) const {
+        int c = min(number, last);   // (past the last chunk: that one again, not used)
         const char* b = base;
         if (split > 0 && c >= split) {
             b = base2;
             c -= split;
         }
-        b += c * step;
-        if ((int64_t)(c + 1) * UNIT <= end) {
+        return Chunk{b + c * step, c};
+    }
+    // All loads of a chunk, number i to to + i * stride.
+    __device__ inline void load(const Chunk& c, uint32_t to, int stride) const {
+        if (c.number < whole) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) load_lds(b, off[i], to + i * stride);
+            for (int i = 0; i < N; ++i) load_lds(c.b, off[i], to + i * stride);
         } else {   // the operand ends in this chunk: zeros from there on
-            const int64_t left = end - (int64_t)c * UNIT;
+            const int64_t left = end - (int64_t)c.number * UNIT;
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                load_lds(at[COLS ? i : 0] < left ? b + off[i] : reinterpret_cast<const char*>(&tile_zeros),
+                load_lds(at[COLS ? i : 0] < left ? c.b + off[i] : reinterpret_cast<const char*>(&tile_zeros),
                          to + i * stride);
         }
     }
+    __device__ inline void load(int number, uint32_t to, int stride) const { load(chunk(number), to, stride); }
 };
 
 // The small tile: WM x WN waves, BUFS buffers, so that BUFS - 1 chunks are on their way
@@ -247,7 +258,8 @@ struct Tile {
                 }
             }
         }
-        __device__ inline void load(int chunk, uint32_t lds, int wave) const {
+        typedef typename Source<C, BYTES, N>::Chunk Chunk;
+        __device__ inline void load(const Chunk& chunk, uint32_t lds, int wave) const {
             s.load(chunk, lds + wave * 1024, WAVES * 1024);
         }
     };
@@ -293,28 +305,45 @@ struct Tile {
         const uint32_t base = lds_address(lds);
         constexpr int S_LOADS = FLUSH ? (2 / FLUSH * BM + THREADS - 1) / THREADS : 0;
         constexpr int LOADS = la.N + lb.N + S_LOADS;   // of a chunk
-        auto load = [&](int c, int buf) {
-            const uint32_t to = base + buf * BUF;
-            la.load(c0 + c, to, wave);
-            lb.load(c0 + c, to + A_LDS, wave);
+        // What the loads of a chunk start from.
+        struct Ahead {
+            typename decltype(la)::Chunk a;
+            typename decltype(lb)::Chunk b;
+            const float* scale[FLUSH ? S_LOADS : 1];
+        };
+        auto ahead = [&](int c) {
+            Ahead h{la.s.chunk(c0 + c), lb.s.chunk(c0 + c), {}};
             if constexpr (FLUSH > 0) {
                 // (with fewer scales than threads the waves past them load the same again)
 #pragma unroll
                 for (int i = 0; i < S_LOADS; ++i) {
                     const int e = (i * WAVES + wave) * 64 % (2 / FLUSH * BM);
-                    load_lds_word(scale((e + lane) % BM, c0 + min(c, chunks - 1), e / BM),
-                                  to + A_LDS + B_LDS + e * 4);
+                    h.scale[i] = scale((e + lane) % BM, c0 + min(c, chunks - 1), e / BM);
                 }
+            }
+            return h;
+        };
+        auto load = [&](const Ahead& h, int buf) {
+            const uint32_t to = base + buf * BUF;
+            la.load(h.a, to, wave);
+            lb.load(h.b, to + A_LDS, wave);
+            if constexpr (FLUSH > 0) {
+#pragma unroll
+                for (int i = 0; i < S_LOADS; ++i)
+                    load_lds_word(h.scale[i],
+                                  to + A_LDS + B_LDS + (i * WAVES + wave) * 64 % (2 / FLUSH * BM) * 4);
             }
         };
 #pragma unroll
-        for (int c = 0; c < BUFS - 1; ++c) load(c, c);   // (chunks past the last read it again)
+        for (int c = 0; c < BUFS - 1; ++c) load(ahead(c), c);   // (chunks past the last read it again)
+        Ahead next = ahead(BUFS - 1);
         int buf = 0;
         for (int c = 0; c < chunks; ++c) {
             const char* const cur = lds + buf * BUF;
             wait_loads<(BUFS - 2) * LOADS>();
             bare_barrier();   // everybody's loads of this chunk landed, and the buffer before is free
-            load(c + BUFS - 1, buf == 0 ? BUFS - 1 : buf - 1);
+            load(next, buf == 0 ? BUFS - 1 : buf - 1);
+            next = ahead(c + BUFS);
             buf = buf == BUFS - 1 ? 0 : buf + 1;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
