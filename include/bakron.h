@@ -627,7 +627,9 @@ bakron_status bakron_gated_mlp(const void *x, int64_t ldx, int64_t T, int64_t d,
  * bakron_gated_mlp_backward -- gradients of bakron_gated_mlp from dh, the
  * gradient with respect to h (G and U are computed again, nothing is kept from
  * the forward call):
- *   dG = dh (.) U (.) act'(G),  dU = dh (.) act(G)       (rounded to dtype)
+ *   dG = dh (.) U (.) act'(G),  dU = dh (.) act(G)
+ * (rounded to dtype; where few tokens, features or weights make up a result, to
+ * two numbers of dtype, so that the result is as good as rounded once)
  *   dx = dG W_gate + dU W_up,  dw_gate = dG^T x,  dw_up = dU^T x
  *   dx            device output, T x d of dtype, or NULL
  *   dw_gate, dw_up  device outputs, f x d of dtype, leading dimension lddw;

@@ -4,7 +4,7 @@
 // The products of 8-bit values run on the integer matrix cores and are summed exactly:
 // |16 c q| <= 128 * 127 and n <= 2^17 keep the sum below 2^31.
 //
-// Many rows: the tiles of tile.h.  2048 x 8192 x 28672 in 4 bits 428 us, 2250 TOPS (the library's
+// Many rows: the tiles of tile.h.  2048 x 8192 x 28672 in 4 bits 412 to 428 us, 2250 to 2330 TOPS (the library's
 // 8-bit product of 8192^3: 2202), 483 with SiLU and a factor, whose 117 MB are read and multiplied
 // while no tile is; 4096^3 62 us; with a scale for 128 columns 102 us, 1001 rows of
 // it 35: there each chunk's sums are scaled in fp32, two vector operations an accumulator

@@ -7,17 +7,18 @@
 // product happen on its registers.  The gradients come from the same product, with dG and
 // dU (rounded to 16 bits, as operands of the products that follow) in its epilogue.
 //
-// G and U are computed again in the backward pass (a sixth of its products more than keeping
-// them would need, and 4 T f bytes less to keep).  dG and dU are rounded to 16 bits, as the
-// products that follow take them: one rounding more than fp32 arithmetic, so dx and the
-// weights' gradients are off by 2.4e-3 of their norm in bf16 where a single rounding gives 1.7e-3.
+// G and U are computed again in the backward pass (two of its six products, and 4 T f bytes less
+// to keep).  dG and dU are rounded to 16 bits, as the products that follow take them: one
+// rounding more than fp32 arithmetic, so dx and the weights' gradients are off by 2.4e-3 of their
+// norm in bf16 where a single rounding gives 1.7e-3, except where few entries make up a result
+// (backward_plan).
 // The gradients' products read the weights, x, dG and dU as they lie (columns, see
 // tile.h), with no transposed copies.
 //
 // Measured (bf16, 4096 -> 11008): 8192 rows 1085 to 1220 us by the box, 1210 to 1364 TFLOP/s (the
-// library's product of that size: 1312), matrix cores 67% busy; backward of 4096 rows 1820 to
+// library's product of that size: 1312), matrix cores 70% busy; backward of 4096 rows 1806 to
 // 1910 us: gated product 603, dx 522, dW 665; the first and last take 5.4 rounds of tiles in the
-// time of 6.  One row 35 us: the weights' 180 MB at 5.2 TB/s.
+// time of 6.  One row 34 us: the weights' 180 MB at 5.2 TB/s.
 #include "tile.h"
 
 namespace bk {
@@ -34,8 +35,8 @@ struct GatedArgs {
     // backward
     const void* dh;
     int64_t lddh;
-    void* dgu;                     // T x 2 fp: dG | dU, zeros in the padding of each
-    int64_t fp;
+    void* dgu;                     // T rows: dG | dU (fp each, zeros in the padding), then their rests
+    int64_t fp, ldg;               // ldg: 2 fp entries, or 4 fp with the rests
 };
 
 // What few rows need beside that: x and the weights as they are, in entries.
@@ -80,9 +81,19 @@ __device__ inline void gated_finish(const GatedArgs& a, int64_t t, int64_t j, co
             dg[r] = r < valid ? dh[r] * U[r] * s : 0.0f;   // (0 in the padding, whatever G is)
             du[r] = r < valid ? dh[r] * v : 0.0f;
         }
-        E* const row = static_cast<E*>(a.dgu) + t * (2 * a.fp) + j;
+        E* const row = static_cast<E*>(a.dgu) + t * a.ldg + j;
         store_n(row, dg, N);
         store_n(row + a.fp, du, N);
+        if (a.ldg > 2 * a.fp) {   // what the rounding took (nothing beside what is not finite)
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                const float g = (float)(E)dg[r], u = (float)(E)du[r];
+                dg[r] = __builtin_isfinite(g) ? dg[r] - g : 0.0f;
+                du[r] = __builtin_isfinite(u) ? du[r] - u : 0.0f;
+            }
+            store_n(row + 2 * a.fp, dg, N);
+            store_n(row + 3 * a.fp, du, N);
+        }
     }
 }
 
@@ -573,17 +584,29 @@ static void gated_operands(GatedArgs& a, const PadPlan& p, const void* x, int64_
 
 // The two products of the backward pass: dx over the features (those of Wg, then those of Wu), dW over
 // the tokens.
+//
+// Both take dG and dU in 16 bits.  Where many tokens, features and outputs count, the errors of
+// that average out to as much as the result's own rounding (together 1.4 times one rounding's
+// norm).  Where few do they may not (1.6 times), so there the sums go on over the rests that the
+// rounding took, in 16 bits, too, and the result is as good as rounded once: for dW with one chunk
+// of tokens and few features, or few weights; for dx with one chunk of tokens and few features or
+// weights.  16 x 4096 x 1024: 31.5 -> 36.3 us, 1 x 1024 x 1024: 17.9 -> 20.4, 2752 x 65 x 128:
+// 21.5 -> 25.7; with more features 1 x 4096 x 11008 would take 147 us instead of 133 for nothing.
 struct BackwardPlan {
-    int64_t fp;
+    int64_t fp, ldg;
+    bool rests_x, rests_w;
     ProdPlan dx, dw;
     size_t dgu, partial;
 };
 static BackwardPlan backward_plan(int64_t T, int64_t d, int64_t f, bool dx, bool dw, int ncu) {
     BackwardPlan p{};
     p.fp = (f + 63) / 64 * 64;
-    p.dgu = up256((size_t)T * 2 * p.fp * 2);
-    if (dx) p.dx = prod_plan(d, T, (int)(2 * p.fp / 64), ncu);
-    if (dw) p.dw = prod_plan(d, 2 * p.fp, (int)((T + 63) / 64), ncu);
+    p.rests_w = dw && ((T <= 64 && f <= 4096) || d * f <= (1 << 17));
+    p.rests_x = dx && T <= 64 && (f <= 1024 || d * f <= (1 << 21));
+    p.ldg = (p.rests_w || p.rests_x ? 4 : 2) * p.fp;
+    p.dgu = up256((size_t)T * p.ldg * 2);
+    if (dx) p.dx = prod_plan(d, T, (int)((p.rests_x ? 4 : 2) * p.fp / 64), ncu);
+    if (dw) p.dw = prod_plan(d, 2 * p.fp, (int)((p.rests_w ? 2 : 1) * ((T + 63) / 64)), ncu);
     p.partial = std::max(p.dx.bytes, p.dw.bytes);
     return p;
 }
@@ -593,15 +616,15 @@ static void run_backward(const FewArgs& few, const GatedArgs& a, const BackwardP
                          void* dx, int64_t lddx, void* dw_gate, void* dw_up, int64_t lddw,
                          void* partial, hipStream_t st) {
     launch_gated<M, true>(few, a, st);
-    const int64_t ldg = 4 * a.fp;
+    const int64_t ldg = 2 * a.ldg;   // in bytes
     const int64_t cols = (d + 7) / 8 * 8;   // (of x and the weights, as they are or padded)
     if (dx) {
         ProdArgs g{};
         g.a = operand(a.w.base, a.w.ld, cols, a.f);
         g.a.base2 = a.w.base2;
         g.a.split = (int)(a.fp / 64);
-        g.b = operand(a.dgu, ldg, a.T, ldg);
-        g.chunks = 2 * g.a.split;
+        g.chunks = (p.rests_x ? 4 : 2) * g.a.split;
+        g.b = operand(a.dgu, ldg, a.T, (int64_t)g.chunks * CHUNK_BYTES);
         g.d = d;
         g.out = dx;
         g.ldo = lddx;
@@ -613,6 +636,12 @@ static void run_backward(const FewArgs& few, const GatedArgs& a, const BackwardP
         g.a = operand(a.x.base, a.x.ld, cols, a.T);
         g.b = operand(a.dgu, ldg, 2 * a.fp, a.T);
         g.chunks = (int)((a.T + 63) / 64);
+        if (p.rests_w) {   // the same x again, beside the rests
+            g.a.split = g.b.split = g.chunks;
+            g.a.base2 = g.a.base;
+            g.b.base2 = g.b.base + 4 * a.fp;
+            g.chunks *= 2;
+        }
         g.d = d;
         g.out = dw_gate;
         g.out2 = dw_up;
@@ -713,6 +742,7 @@ extern "C" bakron_status bakron_gated_mlp_backward(const void* dh, int64_t lddh,
     a.dh = dh;
     a.lddh = lddh;
     a.fp = b.fp;
+    a.ldg = b.ldg;
     char* at = static_cast<char*>(work);
     bk::gated_operands(a, p, x, ldx, w_gate, w_up, ldw, d, &at, stream);
     a.dgu = at;

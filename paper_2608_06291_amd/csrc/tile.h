@@ -96,8 +96,9 @@ __device__ inline i32x2 read_transposed(const char* p) {
 
 // An operand in memory.  Rows: row(r) is r rows of `ld` bytes on, r < n; k runs over
 // [0, k_end) bytes of it.  Columns: k rows of `ld` bytes, k < k_end, of n entries (n a
-// multiple of 8).  With `split` > 0 the chunks from `split` on start over at base2.  Past its
-// end an operand reads as zeros; past n (never used) as some entry before it.
+// multiple of 8).  With `split` > 0 the chunks from `split` on start over at base2, those from
+// 2 * split on at base again (and may be as many as before).  Past its end an operand reads as
+// zeros; past n (never used) as some entry before it.
 struct Operand {
     const char* base;
     const char* base2;
@@ -189,9 +190,12 @@ struct Source {
     __device__ inline Chunk chunk(int number) const {
         int c = min(number, last);   // (past the last chunk: that one again, not used)
         const char* b = base;
-        if (split > 0 && c >= split) {
-            b = base2;
-            c -= split;
+        if (split > 0) {
+            if (c >= 2 * split) c -= 2 * split;
+            if (c >= split) {
+                b = base2;
+                c -= split;
+            }
         }
         return Chunk{b + c * step, c};
     }

@@ -426,6 +426,53 @@ def test_gated_mlp_backward(T, d, f, dtype, act):
     assert only[0] is None and torch.equal(only[1], dwg) and torch.equal(only[2], dwu)
 
 
+@pytest.mark.parametrize("T,d,f", [(1, 64, 1), (1, 264, 66), (2, 100, 500), (5, 65, 1024), (33, 72, 70),
+                                   (64, 130, 300), (3, 128, 1025), (4, 2048, 1025), (130, 65, 128), (1000, 72, 300)])
+@pytest.mark.parametrize("dtype,act", [("bf16", "silu"), ("f16", "gelu")])
+def test_gated_mlp_backward_few_tokens(T, d, f, dtype, act):
+    """Over few tokens (and features or weights, for dx) or for few weights the gradients are off by no more than their own
+    rounding: the norm of the error is that of rounding the 64-bit result, to 5%.  What is
+    left of rounding dG and dU is u^2 of them, the fp32 sums and activations a few 1e-6 or
+    less; both add in squares to the result's u / 2.5."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("mlp backward, few tokens", T, d, f, dtype, act)
+    x, wg, wu, dh = _mlp_inputs(T, d, f, dtype, 91)
+    got = pk.gated_mlp_backward(*(t.to("cuda:0") for t in (dh, x, wg, wu)), act=act)
+    dt = x.dtype
+    x, wg, wu, dh = x.double(), wg.double(), wu.double(), dh.double()
+    G, U = x @ wg.t(), x @ wu.t()
+    dG, dU = dh * U * _slope64(G, act), dh * _act64(G, act)
+    for label, g, want in (("dx", got[0], dG @ wg + dU @ wu), ("dw_gate", got[1], dG.t() @ x),
+                           ("dw_up", got[2], dU.t() @ x)):
+        if label == "dx" and (T > 64 or (f > 1024 and d * f > 1 << 21)):
+            continue
+        once = float((want.to(dt).double() - want).norm())
+        assert float((g.cpu().double() - want).norm()) <= 1.05 * once + 3e-6 * float(want.norm()), label
+
+
+@pytest.mark.parametrize("T", [2, 40])
+def test_gated_mlp_backward_overflow(T):
+    """Gradients of the hidden layer beyond half precision: infinite where they meet one token,
+    as without the rests of their rounding."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("mlp backward, overflow", T)
+    d, f = 32, 40
+    x, wg, wu, dh = (torch.ones(s, dtype=torch.float16, device="cuda:0")
+                     for s in ((T, d), (f, d), (f, d), (T, f)))
+    x[1:] = 0
+    x[1:, 0] = 1
+    dh[0, 3] = 60000.0   # dU = 60000 * silu(32), dG = 60000 * 32
+    dx, dwg, dwu = pk.gated_mlp_backward(dh, x, wg, wu, act="silu")
+    torch.cuda.synchronize()
+    assert bool(torch.isposinf(dx[0]).all()) and bool(torch.isfinite(dx[1:]).all())
+    for w in (dwg, dwu):
+        assert bool(torch.isposinf(w[3]).all())
+        rows = torch.arange(f, device="cuda:0") != 3
+        assert bool(torch.isfinite(w[rows]).all())
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 def test_gated_mlp_gradient_against_differences(act):
     """The directional derivative of sum(h * dh), from differences of the 64-bit
