@@ -123,12 +123,13 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
     const bool finite = top < INFINITY;
     const float s = finite ? top / 127.0f : NAN;
     if (tid == 0) a.scale[row] = s;
-    // y / s as a product where 1 / s exists, so a division only for rows below 2^-119
+    // y / s as a product where 1 / s exists, so a division only for rows below 2^-119, whose scale may
+    // be a few steps of the smallest number: rounded down, it takes y / s beyond 127
     const bool tiny = top < 1.5e-36f;
     const float inv = finite && !tiny ? 127.0f / top : 0.0f;
     auto code = [&](float v) {
         float c = v * inv;
-        if (tiny) c = s > 0.0f ? v / s : 0.0f;
+        if (tiny) c = s > 0.0f ? fminf(fmaxf(v / s, -127.0f), 127.0f) : 0.0f;
         return finite ? (int8_t)(int)rintf(c) : (int8_t)0;
     };
     int8_t* const out = a.q + row * a.ldq;
