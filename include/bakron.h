@@ -629,7 +629,9 @@ bakron_status bakron_gated_mlp(const void *x, int64_t ldx, int64_t T, int64_t d,
  * the forward call):
  *   dG = dh (.) U (.) act'(G),  dU = dh (.) act(G)
  * (rounded to dtype; where few tokens, features or weights make up a result, to
- * two numbers of dtype, so that the result is as good as rounded once)
+ * two numbers of dtype, so that the result is as good as rounded once; in
+ * BAKRON_F16 times a power of two, undone at the end, where the largest of them
+ * is below 1 or beyond 65504, so that neither small nor large ones are lost)
  *   dx = dG W_gate + dU W_up,  dw_gate = dG^T x,  dw_up = dU^T x
  *   dx            device output, T x d of dtype, or NULL
  *   dw_gate, dw_up  device outputs, f x d of dtype, leading dimension lddw;

@@ -12,6 +12,7 @@
 // rounding more than fp32 arithmetic, so dx and the weights' gradients are off by 2.4e-3 of their
 // norm in bf16 where a single rounding gives 1.7e-3, except where few entries make up a result
 // (backward_plan).
+// In half precision their range counts, too: see GradScale.
 // The gradients' products read the weights, x, dG and dU as they lie (columns, see
 // tile.h), with no transposed copies.
 //
@@ -37,7 +38,32 @@ struct GatedArgs {
     int64_t lddh;
     void* dgu;                     // T rows: dG | dU (fp each, zeros in the padding), then their rests
     int64_t fp, ldg;               // ldg: 2 fp entries, or 4 fp with the rests
+    float* top;                    // half precision: the largest |dG|, |dU| of every wave
+    const float* factor;           // .. and what this second run takes them times (1: not needed)
 };
+
+// Half precision holds 6e-8 to 65504, eleven bits from 6e-5 on.  dG and dU of a loss that is a mean over
+// many tokens lie below that, and large ones beyond it, where dx and dW need not.  So the gated product
+// leaves the largest of them that is finite; where that is below 1 or beyond 65504 a second run of it takes
+// all of them times the power of two that puts the largest at 2^14 to 2^15, and the products that
+// follow undo it (in fp32).  Then no number down to 2^-29 of the largest loses a bit.  The second run is
+// launched in any case and ends at once where there is nothing to do: 5 us.
+struct GradScale {
+    float factor, undo;
+};
+template <typename E>
+constexpr bool narrow_range = std::is_same<E, f16_t>::value;
+__global__ __launch_bounds__(1024) void k_grad_scale(const float* __restrict__ top, int64_t n, GradScale* out) {
+    __shared__ float red[16];
+    float m = 0.0f;
+    for (int64_t i = threadIdx.x; i < n; i += 1024) m = fmaxf(m, top[i]);
+    m = group_reduce(m, MaxNan(), red, threadIdx.x >> 6, threadIdx.x & 63, 16);
+    if (threadIdx.x != 0) return;
+    int e = 15;
+    if (m > 0.0f && (m < 1.0f || m > 65504.0f)) frexpf(m, &e);   // m < 2^e
+    e = max(e, 15 - 126);                                        // (both powers are normal numbers)
+    *out = GradScale{ldexpf(1.0f, 15 - e), ldexpf(1.0f, e - 15)};
+}
 
 // What few rows need beside that: x and the weights as they are, in entries.
 struct FewArgs {
@@ -46,10 +72,10 @@ struct FewArgs {
     int d;
 };
 
-// Row t, features j .. j + N - 1, from G and U.
+// Row t, features j .. j + N - 1, from G and U; `top` grows with the largest |dG|, |dU|.
 template <typename E, bool BWD, int N>
 __device__ inline void gated_finish(const GatedArgs& a, int64_t t, int64_t j, const float (&G)[N],
-                                    const float (&U)[N], const float (&dh)[N]) {
+                                    const float (&U)[N], const float (&dh)[N], float factor, float& top) {
     const int64_t valid = a.f - j;
     if constexpr (!BWD) {
         if (valid <= 0) return;
@@ -80,6 +106,12 @@ __device__ inline void gated_finish(const GatedArgs& a, int64_t t, int64_t j, co
             act_both(G[r], a.act, &v, &s);
             dg[r] = r < valid ? dh[r] * U[r] * s : 0.0f;   // (0 in the padding, whatever G is)
             du[r] = r < valid ? dh[r] * v : 0.0f;
+            if constexpr (narrow_range<E>) {
+                top = fmaxf(top, __builtin_isfinite(dg[r]) ? fabsf(dg[r]) : 0.0f);
+                top = fmaxf(top, __builtin_isfinite(du[r]) ? fabsf(du[r]) : 0.0f);
+                dg[r] *= factor;
+                du[r] *= factor;
+            }
         }
         E* const row = static_cast<E*>(a.dgu) + t * a.ldg + j;
         store_n(row, dg, N);
@@ -101,6 +133,8 @@ template <typename Tl, bool BWD>
 __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
     typedef typename Tl::Mma::Elem E;
     __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+    const float factor = BWD && narrow_range<E> && a.factor ? *a.factor : 1.0f;
+    if (BWD && narrow_range<E> && a.factor && factor == 1.0f) return;
     int ti, tt;
     tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
     const int64_t f0 = (int64_t)ti * (Tl::ROWS / 2), t0 = (int64_t)tt * Tl::COLS;
@@ -143,6 +177,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
             }
         }
     }
+    float top = 0.0f;
 #pragma unroll
     for (int y = 0; y < Tl::UB; ++y) {
         rows.put(y);
@@ -152,7 +187,11 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
         rows.take(tl & 15, (p >> 1) * 4 + (p & 1) + 2, U);
 #pragma unroll
         for (int r = 0; r < 8; ++r) d[r] = BWD ? entry<E>(dh[BWD ? y : 0], r) : 0.0f;
-        if (tl < 16 && t < a.T) gated_finish<E, BWD>(a, t, j, G, U, d);
+        if (tl < 16 && t < a.T) gated_finish<E, BWD>(a, t, j, G, U, d, factor, top);
+    }
+    if constexpr (BWD && narrow_range<E>) {
+        top = wave_reduce(top, MaxNan());
+        if (lane == 0) a.top[(int64_t)blockIdx.x * (Tl::THREADS / 64) + wave] = top;
     }
 }
 
@@ -196,6 +235,8 @@ template <typename M, bool BWD, int Y, int U, bool SHIFT>
 __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
     typedef typename M::Elem E;
     extern __shared__ __attribute__((aligned(16))) char few_lds[];
+    const float factor = BWD && narrow_range<E> && a.factor ? *a.factor : 1.0f;
+    if (BWD && narrow_range<E> && a.factor && factor == 1.0f) return;
     const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, kq = lane >> 4;
@@ -302,7 +343,12 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
         float dh[4] = {};
         const int64_t j = j0 + kq * 4;
         if (BWD && t < a.T && j < a.f) load_n(static_cast<const E*>(a.dh) + t * a.lddh + j, dh, a.f - j);
-        if (t < a.T) gated_finish<E, BWD>(a, t, j, gv, uv, dh);
+        float top = 0.0f;
+        if (t < a.T) gated_finish<E, BWD>(a, t, j, gv, uv, dh, factor, top);
+        if constexpr (BWD && narrow_range<E>) {
+            top = wave_reduce(top, MaxNan());
+            if (lane == 0) a.top[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * Y + y] = top;
+        }
     }
 }
 
@@ -315,11 +361,16 @@ struct ProdArgs {
     int parts, part_chunks;        // the summed axis in parts of so many chunks
     float* partial;                // parts x end x dp, where there are several
     int64_t dp;
+    const float* undo;             // the outputs are taken times this, or NULL
 };
 
 template <typename E>
-__device__ inline void prod_store(const ProdArgs& a, int64_t t, int64_t i, const float (&v)[8]) {
+__device__ inline void prod_store(const ProdArgs& a, int64_t t, int64_t i, float undo, float (&v)[8]) {
     if (t >= a.end || (t >= a.split && t < a.split2)) return;
+    if constexpr (narrow_range<E>) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= undo;
+    }
     E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
                                : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
     store_n(row + i, v, a.d - i);
@@ -346,6 +397,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
     const auto rows =
         handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
     constexpr int PER = Tl::UA * 2;   // lanes a row
+    const float undo = narrow_range<E> && a.undo ? *a.undo : 1.0f;
     const int p = lane % PER;
     const int64_t i = i0 + Tl::a0(wave) + p * 8;
 #pragma unroll
@@ -361,7 +413,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
                 if (a.parts > 1)
                     store_n(a.partial + (part * a.end + t) * a.dp + i, v, 8);
                 else
-                    prod_store<E>(a, t, i, v);
+                    prod_store<E>(a, t, i, undo, v);
             }
         }
     }
@@ -380,7 +432,7 @@ __global__ __launch_bounds__(256) void k_prod_join(ProdArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += x.v[j];
     }
-    prod_store<E>(a, t, i, v);
+    prod_store<E>(a, t, i, narrow_range<E> && a.undo ? *a.undo : 1.0f, v);
 }
 
 // Up to three matrices of the same width copied into rows of cols_p, zeros behind;
@@ -430,8 +482,14 @@ static bool direct_rows(const void* p, int64_t ld, int64_t cols) {
 constexpr int64_t FEW_ROWS = 32;
 constexpr int64_t FEW_TILES = 4;
 
+// Values of GatedArgs.top that a launch writes at most (the kernels for few rows: one for 16 features of
+// 16 rows, in pairs; tiles: no more, a wave's part being 16 features of 32 rows or larger).  fp is a multiple
+// of 64.
+static int64_t gated_tops(int64_t T, int64_t fp) { return (T + 31) / 32 * 2 * (fp / 16); }
+
+// The launches return how many values of GatedArgs.top they write.
 template <typename M, bool BWD, int Y, int U>
-static void launch_gated_few(const FewArgs& f, const GatedArgs& a, hipStream_t st) {
+static int64_t launch_gated_few(const FewArgs& f, const GatedArgs& a, hipStream_t st) {
     // Words around the pieces of odd rows: the first row of each matrix begins on a word, and whole steps
     // end before the row does, so an entry before and one behind each piece are in the matrix.
     const bool shift = (f.ldx % 2 != 0 || f.ldw % 2 != 0) && f.d % 32 != 0 && (uintptr_t)f.x % 4 == 0 &&
@@ -444,6 +502,7 @@ static void launch_gated_few(const FewArgs& f, const GatedArgs& a, hipStream_t s
         hipLaunchKernelGGL((k_gated_few<M, BWD, Y, US, true>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
     else
         hipLaunchKernelGGL((k_gated_few<M, BWD, Y, U, false>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
+    return (int64_t)grid.x * grid.y * Y;
 }
 
 // Whether the kernel for few rows takes it: few rows, or few tiles with a long way to sum.
@@ -453,7 +512,7 @@ static bool gated_few_rows(int64_t T, int64_t f, int64_t d) {
 }
 
 template <typename M, bool BWD>
-static void launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
+static int64_t launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
     if (gated_few_rows(a.T, a.f, few.d))
         return a.T <= 16 ? launch_gated_few<M, BWD, 1, 4>(few, a, st)
                          : launch_gated_few<M, BWD, 2, 2>(few, a, st);
@@ -463,16 +522,13 @@ static void launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
         a.ni = (int)((f + Tl::ROWS / 2 - 1) / (Tl::ROWS / 2));
         a.nt = (int)((a.T + Tl::COLS - 1) / Tl::COLS);
         hipLaunchKernelGGL((k_gated<Tl, BWD>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
+        return (int64_t)a.ni * a.nt * (Tl::THREADS / 64);
     };
     const int tile = pick_tile(2 * f, a.T, op_cus(), true);
-    if (tile == 256)
-        go(BigTile<M>());
-    else if (tile == 128 && one_a_cu(128, 2 * f, a.T))
-        go(Tile<M, 128, 128, 2, 4, 3>());
-    else if (tile == 128)
-        go(Tile<M, 128, 128, 2, 4, 2>());
-    else
-        go(Tile<M, 64, 64, 2, 2, 4>());
+    if (tile == 256) return go(BigTile<M>());
+    if (tile == 128 && one_a_cu(128, 2 * f, a.T)) return go(Tile<M, 128, 128, 2, 4, 3>());
+    if (tile == 128) return go(Tile<M, 128, 128, 2, 4, 2>());
+    return go(Tile<M, 64, 64, 2, 2, 4>());
 }
 
 // How a product is cut: tile edge, and parts of the summed axis (of 4 chunks at least),
@@ -596,9 +652,9 @@ struct BackwardPlan {
     int64_t fp, ldg;
     bool rests_x, rests_w;
     ProdPlan dx, dw;
-    size_t dgu, partial;
+    size_t dgu, partial, top;   // bytes of the workspace; top: half precision, a GradScale before the values
 };
-static BackwardPlan backward_plan(int64_t T, int64_t d, int64_t f, bool dx, bool dw, int ncu) {
+static BackwardPlan backward_plan(int64_t T, int64_t d, int64_t f, bool half, bool dx, bool dw, int ncu) {
     BackwardPlan p{};
     p.fp = (f + 63) / 64 * 64;
     p.rests_w = dw && ((T <= 64 && f <= 4096) || d * f <= (1 << 17));
@@ -608,18 +664,27 @@ static BackwardPlan backward_plan(int64_t T, int64_t d, int64_t f, bool dx, bool
     if (dx) p.dx = prod_plan(d, T, (int)((p.rests_x ? 4 : 2) * p.fp / 64), ncu);
     if (dw) p.dw = prod_plan(d, 2 * p.fp, (int)((p.rests_w ? 2 : 1) * ((T + 63) / 64)), ncu);
     p.partial = std::max(p.dx.bytes, p.dw.bytes);
+    p.top = half ? up256(256 + (size_t)gated_tops(T, p.fp) * sizeof(float)) : 0;
     return p;
 }
 
 template <typename M>
-static void run_backward(const FewArgs& few, const GatedArgs& a, const BackwardPlan& p, int64_t d,
+static void run_backward(const FewArgs& few, GatedArgs a, const BackwardPlan& p, int64_t d,
                          void* dx, int64_t lddx, void* dw_gate, void* dw_up, int64_t lddw,
-                         void* partial, hipStream_t st) {
-    launch_gated<M, true>(few, a, st);
+                         char* top, void* partial, hipStream_t st) {
+    GradScale* const scale = reinterpret_cast<GradScale*>(top);
+    a.top = reinterpret_cast<float*>(top + 256);
+    const int64_t tops = launch_gated<M, true>(few, a, st);
+    if constexpr (narrow_range<typename M::Elem>) {
+        hipLaunchKernelGGL(k_grad_scale, dim3(1), dim3(1024), 0, st, a.top, tops, scale);
+        a.factor = &scale->factor;
+        launch_gated<M, true>(few, a, st);
+    }
     const int64_t ldg = 2 * a.ldg;   // in bytes
     const int64_t cols = (d + 7) / 8 * 8;   // (of x and the weights, as they are or padded)
     if (dx) {
         ProdArgs g{};
+        g.undo = narrow_range<typename M::Elem> ? &scale->undo : nullptr;
         g.a = operand(a.w.base, a.w.ld, cols, a.f);
         g.a.base2 = a.w.base2;
         g.a.split = (int)(a.fp / 64);
@@ -633,6 +698,7 @@ static void run_backward(const FewArgs& few, const GatedArgs& a, const BackwardP
     }
     if (dw_gate) {
         ProdArgs g{};
+        g.undo = narrow_range<typename M::Elem> ? &scale->undo : nullptr;
         g.a = operand(a.x.base, a.x.ld, cols, a.T);
         g.b = operand(a.dgu, ldg, 2 * a.fp, a.T);
         g.chunks = (int)((a.T + 63) / 64);
@@ -721,9 +787,10 @@ extern "C" bakron_status bakron_gated_mlp_backward(const void* dh, int64_t lddh,
     const bool many = !bk::gated_few_rows(T, f, d);
     const bk::PadPlan p = bk::pad_plan(x, ldx, w_gate, w_up, ldw, T, d, f, many || dw_gate, many || dx);
     const bk::BackwardPlan b =
-        bk::backward_plan(std::max<int64_t>(T, 1), d, f, dx != nullptr, dw_gate != nullptr, bk::op_cus());
+        bk::backward_plan(std::max<int64_t>(T, 1), d, f, dtype == BAKRON_F16, dx != nullptr, dw_gate != nullptr,
+                          bk::op_cus());
     bool query;
-    st = bk::op_workspace(who, work, work_bytes, p.xbytes + 2 * p.wbytes + b.dgu + b.partial, &query);
+    st = bk::op_workspace(who, work, work_bytes, p.xbytes + 2 * p.wbytes + b.dgu + b.top + b.partial, &query);
     if (st != BAKRON_OK || query) return st;
     if (!dw_gate != !dw_up) return bk::op_fail(who, "dw_gate and dw_up go together");
     if (!dx && !dw_gate) return bk::op_fail(who, "null pointer");
@@ -746,11 +813,12 @@ extern "C" bakron_status bakron_gated_mlp_backward(const void* dh, int64_t lddh,
     char* at = static_cast<char*>(work);
     bk::gated_operands(a, p, x, ldx, w_gate, w_up, ldw, d, &at, stream);
     a.dgu = at;
-    char* const partial = at + b.dgu;
+    char* const top = at + b.dgu;
+    char* const partial = top + b.top;
     const bk::FewArgs few{x, w_gate, w_up, ldx, ldw, (int)d};
     if (dtype == BAKRON_BF16)
-        bk::run_backward<bk::MmaBF16>(few, a, b, d, dx, lddx, dw_gate, dw_up, lddw, partial, stream);
+        bk::run_backward<bk::MmaBF16>(few, a, b, d, dx, lddx, dw_gate, dw_up, lddw, top, partial, stream);
     else
-        bk::run_backward<bk::MmaF16>(few, a, b, d, dx, lddx, dw_gate, dw_up, lddw, partial, stream);
+        bk::run_backward<bk::MmaF16>(few, a, b, d, dx, lddx, dw_gate, dw_up, lddw, top, partial, stream);
     return bk::op_launched(who);
 }

@@ -3,9 +3,11 @@ their range: the smallest and largest ones, a common offset, the tails of the ac
 
 Tolerances as in test_gpu_operators.py: bounds on the roundings that the header allows.
 """
+import math
+
 import pytest
 
-from test_gpu_operators import U32, _say, _t
+from test_gpu_operators import U32, _act64, _rand, _say, _slope64, _t, _tiny, _u
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -31,3 +33,126 @@ def test_norm_codes_of_subnormal_rows():
     want = (x.double() / torch.where(zero, 1.0, s)[:, None]).clamp(-127, 127)
     err = torch.where(zero[:, None], 0.0, q - want).abs()
     assert bool((err <= 0.5 + 127 * 4 * U32).all()), float(err.max())
+
+
+# ---------------------------------------------------------------- gated MLP, gradients in half precision
+def _backward_check(x, wg, wu, dh, act, want_dx=True, want_dw=True):
+    """Half-precision gradients against 64 bits.  Of dG and dU, what is kept is the nearest 11-bit number, and
+    of small ones no less than 2^-39 of the largest of all (11 bits of 2^15 go down to 2^-24; half a step)
+    or 2^-25, whichever is more where the largest is 1 or more."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    T, d = x.shape
+    f = wg.shape[0]
+    got = pk.gated_mlp_backward(*(t.to(DEV) for t in (dh, x, wg, wu)), act=act)
+    torch.cuda.synchronize()
+    x, wg, wu, dh = x.double(), wg.double(), wu.double(), dh.double()
+    G, U = x @ wg.t(), x @ wu.t()
+    eG = (d + 4) * U32 * (x.abs() @ wg.abs().t())
+    eU = (d + 4) * U32 * (x.abs() @ wu.abs().t())
+    A, S = _act64(G, act), _slope64(G, act)
+    eA = 1.13 * eG + 8 * U32 * (G.abs() + A.abs())
+    eS = eG + 16 * U32 * (1 + G.abs())
+    dG, dU = dh * U * S, dh * A
+    most = float(max(dG.abs().max(), dU.abs().max()))
+    lost = 2.0 ** -39 * most if most < 1 or most > 2.0 ** 15 else 2.0 ** -25
+    u = _u("f16")
+    eDG = dh.abs() * (eU * S.abs() + U.abs() * eS + eU * eS) + 4 * U32 * dG.abs()
+    eDG = eDG + u * (dG.abs() + eDG) + lost
+    eDU = dh.abs() * eA + 4 * U32 * dU.abs()
+    eDU = eDU + u * (dU.abs() + eDU) + lost
+
+    def check(g, want, err, size, terms, label):
+        e = err + (terms + 4) * U32 * size
+        e = e + u * (want.abs() + e) + _tiny("f16")
+        far = want.abs() > 65520 + e             # rounds to infinity
+        near = (want.abs() > 65504 - e) & ~far   # may or may not
+        g = g.cpu().double()
+        assert bool((g[far] == torch.sign(want[far]) * math.inf).all()), label
+        err = torch.where(far | near, 0.0, (g - want).abs())
+        assert bool((err <= e).all()), (label, float((err / e).max()))   # (NaN fails, too)
+    aG, aU = dG.abs() + eDG, dU.abs() + eDU
+    if want_dx:
+        check(got[0], dG @ wg + dU @ wu, eDG @ wg.abs() + eDU @ wu.abs(), aG @ wg.abs() + aU @ wu.abs(), 2 * f, "dx")
+    if want_dw:
+        check(got[1], dG.t() @ x, eDG.t() @ x.abs(), aG.t() @ x.abs(), T, "dw_gate")
+        check(got[2], dU.t() @ x, eDU.t() @ x.abs(), aU.t() @ x.abs(), T, "dw_up")
+    return got, (dG, dU, x, wg, wu)
+
+
+def _half_inputs(T, d, f, size, seed=21):
+    s = 1.0 / math.sqrt(d)
+    return (_rand((T, d), seed).half(), _rand((f, d), seed + 1, s).half(), _rand((f, d), seed + 2, s).half(),
+            _rand((T, f), seed + 3, size).half())
+
+
+@pytest.mark.parametrize("T,d,f", [(256, 512, 1376), (5, 96, 130), (40, 333, 70), (1500, 264, 2100)])
+@pytest.mark.parametrize("size", [1e-3, 1e-5, 3e-7])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_half_gradients_of_small_losses(T, d, f, size, act):
+    """dh as a loss that is a mean over many tokens has it, without a scale of its own."""
+    _say("half gradients, small", T, d, f, size, act)
+    torch = _t()
+    x, wg, wu, dh = _half_inputs(T, d, f, size)
+    got, (dG, dU, x, wg, wu) = _backward_check(x, wg, wu, dh, act)
+    # in norm: the rounding of dG and dU (each entry within u, 0.6 u at most in the mean square) and the result's own
+    # beside it; 1e-5 for fp32 sums
+    for g, want in ((got[0], dG @ wg + dU @ wu), (got[1], dG.t() @ x), (got[2], dU.t() @ x)):
+        once = (want.half().double() - want).norm()
+        assert float((g.cpu().double() - want).norm()) <= 1.05 * float(once) + (0.6 * _u("f16") + 1e-5) * float(want.norm())
+
+
+@pytest.mark.parametrize("T,d,f", [(200, 330, 500), (7, 96, 64)])
+def test_half_gradients_beyond_the_largest_number(T, d, f):
+    """dG beyond 65504 where small weights bring dx back into range."""
+    _say("half gradients, large", T, d, f)
+    torch = _t()
+    s = 1.0 / math.sqrt(d)
+    x, wu = _rand((T, d), 1, 4.0).half(), _rand((f, d), 2, s).half()
+    wg = _rand((f, d), 3, 1e-3 * s).half()
+    dh = (_rand((T, f), 4).sign() * 6e4).half()
+    got, _ = _backward_check(x, wg, wu, dh, "silu")
+    assert bool(torch.isfinite(got[0]).all()) and bool(torch.isfinite(got[2]).all())
+
+
+def test_half_gradients_spoiled_and_empty():
+    """NaN and infinities in dh spoil what they meet, and do not set the scale of the rest; all zeros give zeros."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("half gradients, spoiled")
+    x, wg, wu, dh = (t.to(DEV) for t in _half_inputs(70, 100, 90, 1e-5))
+    clean = pk.gated_mlp_backward(dh, x, wg, wu, need_dw=False)[0]
+    bad = dh.clone()
+    bad[3, 5], bad[69, 0] = math.nan, math.inf
+    got = pk.gated_mlp_backward(bad, x, wg, wu, need_dw=False)[0]
+    rows = torch.tensor([r for r in range(70) if r not in (3, 69)], device=DEV)
+    assert torch.equal(got[rows], clean[rows])
+    assert bool(got[3].isnan().all()) and not bool(got[69].isfinite().any())
+    for g in pk.gated_mlp_backward(torch.zeros_like(dh), x, wg, wu):
+        assert int(g.ne(0).sum()) == 0
+
+
+def test_half_gradients_replay_from_a_graph():
+    """One graph over inputs that need the second run, and do not, and need it again."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("half gradients, graph")
+    for T, d, f in ((9, 264, 136), (700, 264, 1000)):
+        x, wg, wu, _ = (t.to(DEV) for t in _half_inputs(T, d, f, 1.0))
+        dh = torch.zeros((T, f), dtype=torch.float16, device=DEV)
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            pk.gated_mlp_backward(dh, x, wg, wu)
+        st.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = pk.gated_mlp_backward(dh, x, wg, wu)
+        for k, size in enumerate((1e-5, 0.3, 1e-6, 2e4)):
+            dh.copy_((_rand((T, f), 30 + k) * size).half())
+            want = [t.clone() for t in pk.gated_mlp_backward(dh, x, wg, wu)]
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(out, want):
+                assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and int(a.ne(0).sum()) > 0, (k, T)   # (NaN, too)
