@@ -650,6 +650,8 @@ bakron_status bakron_gated_mlp_backward(const void *dh, int64_t lddh, const void
  * top alternatives, in one pass over the logits:
  *   lse_t = log sum_j exp(z_tj),   logprob_t = z_t,target - lse_t,
  *   entropy_t = -sum_j p_tj log p_tj,   p = exp(z - lse)
+ * Log probabilities are taken from the row's largest logit, so that a number
+ * added to the whole row costs them no precision.
  *   logits     device, T x V of dtype.  -inf masks a token.  A row of -inf
  *              throughout has lse -inf, entropy 0 and log probabilities -inf; a
  *              row with a NaN or +inf has NaN in every output but top_index
@@ -671,6 +673,7 @@ bakron_status bakron_token_logprobs(const void *logits, int64_t ld, int32_t dtyp
  * bakron_token_logprobs_backward -- the gradient with respect to the logits:
  *   d_tj = g_logprob_t (1[j = target_t] - p_tj) - g_entropy_t p_tj (log p_tj + entropy_t)
  * A target outside [0, V) has no first term; a row of -inf throughout has d = 0.
+ * p comes from lse in fp32: its rounding (2^-24 |lse|) is a relative error of p.
  *   lse, entropy  from bakron_token_logprobs (entropy may be NULL without
  *                 g_entropy)
  *   g_logprob, g_entropy  device, T floats, or NULL for 0; target may be NULL

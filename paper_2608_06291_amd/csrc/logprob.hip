@@ -2,7 +2,8 @@
 // gradient.
 //
 // For a row z:  m = max z,  s = sum exp(z - m),  s1 = sum exp(z - m) (z - m),
-//   lse = m + log s,   logprob = z_target - lse,   entropy = log s - s1 / s.
+//   lse = m + log s,   logprob = (z_target - m) - log s,   entropy = log s - s1 / s
+// (from lse itself a log probability would take lse's rounding, 5e-4 at logits around 1e4).
 // Parts of a row join by rescaling to the larger m:
 //   s = s_a e^(m_a - m) + s_b e^(m_b - m),
 //   s1 = (s1_a + (m_a - m) s_a) e^(m_a - m) + (s1_b + (m_b - m) s_b) e^(m_b - m).
@@ -77,7 +78,7 @@ __device__ inline void lp_store(const LpArgs& a, int64_t row, float m, float s, 
     const bool empty = m == -INFINITY;
     const float lse = empty ? -INFINITY : m + logf(s);
     if (a.lse) a.lse[row] = lse;
-    if (a.logprob) a.logprob[row] = !asked ? 0.0f : empty ? -INFINITY : zt - lse;
+    if (a.logprob) a.logprob[row] = !asked ? 0.0f : empty ? -INFINITY : (zt - m) - logf(s);
     if (a.entropy) a.entropy[row] = empty ? 0.0f : logf(s) - s1 / s;
 }
 
@@ -171,12 +172,12 @@ __global__ __launch_bounds__(LP_THREADS, 6) void k_logprob(LpArgs a) {
         }
     }
     if constexpr (TOP) {
-        const float base = m == -INFINITY ? 0.0f : m + logf(s);
+        const float log_s = m == -INFINITY ? 0.0f : logf(s);
         const int64_t part = row * a.parts + p;
         auto put = [&](int k, uint64_t v) {
             if (a.parts == 1) {
                 a.top_index[row * a.top + k] = lp_index(v);
-                a.top_logprob[row * a.top + k] = lp_unkey((uint32_t)(v >> 32)) - base;
+                a.top_logprob[row * a.top + k] = (lp_unkey((uint32_t)(v >> 32)) - ms) - log_s;
             } else {
                 a.cand[part * a.top + k] = v;
             }
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(64) void k_logprob_join(LpArgs a) {
     const float s1 = wave_reduce(fmaf(d, q.s, q.s1) * e, Add());
     if (lane == 0) lp_store(a, row, m, s, s1, zt, asked);
     if (a.top == 0) return;
-    const float base = m == -INFINITY ? 0.0f : m + logf(s);
+    const float log_s = m == -INFINITY ? 0.0f : logf(s);
     if (lane == 0) count = 0;
     __syncthreads();
     const int c = (a.top + a.parts - 1) / a.parts, q_th = (a.top + c - 1) / c;
@@ -319,7 +320,7 @@ __global__ __launch_bounds__(64) void k_logprob_join(LpArgs a) {
     const int n = count;
     auto put = [&](int k, uint64_t v) {
         a.top_index[row * a.top + k] = lp_index(v);
-        a.top_logprob[row * a.top + k] = lp_unkey((uint32_t)(v >> 32)) - base;
+        a.top_logprob[row * a.top + k] = (lp_unkey((uint32_t)(v >> 32)) - ms) - log_s;
     };
     if (n <= LP_JOIN) {
         for (int i = lane; i < n; i += 64) {

@@ -7,7 +7,7 @@ import math
 
 import pytest
 
-from test_gpu_operators import U32, _act64, _rand, _say, _slope64, _t, _tiny, _u
+from test_gpu_operators import U32, _act64, _rand, _say, _slope64, _t, _tiny, _u, _within
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -156,3 +156,29 @@ def test_half_gradients_replay_from_a_graph():
             torch.cuda.synchronize()
             for a, b in zip(out, want):
                 assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and int(a.ne(0).sum()) > 0, (k, T)   # (NaN, too)
+
+
+# ---------------------------------------------------------------- log probabilities
+@pytest.mark.parametrize("T,V,top", [(3, 1000, 5), (2, 60000, 20), (1, 131072, 1), (300, 5001, 3)])
+@pytest.mark.parametrize("offset", [1e3, -1e4])
+def test_token_logprobs_with_an_offset(T, V, top, offset):
+    """A constant added to a row changes nothing: log probabilities are as good as without it."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("logprob offset", T, V, top, offset)
+    z = (_rand((T, V), 5, 3.0) + offset).float()
+    # likely and unlikely targets
+    target = torch.where(torch.arange(T) % 3 > 0, z.argmax(1), torch.arange(T) % V)
+    z[torch.arange(T), target] += 10.0 * (torch.arange(T) % 2)
+    r = pk.token_logprobs(z.to(DEV), target.to(DEV), top=top)
+    zd = z.double()
+    m = zd.amax(1, keepdim=True)
+    logp = (zd - m) - (zd - m).exp().sum(1, keepdim=True).log()
+    lp = logp.gather(1, target[:, None])[:, 0]
+    # log of the sum: see _lp_tolerance; z - m is exact or rounded once
+    e = 260 * U32
+    _within(r.logprob, lp, e + 3 * U32 * lp.abs(), "logprob")
+    best = torch.sort(zd, dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(r.top_index.cpu(), best)
+    t = logp.gather(1, best)
+    _within(r.top_logprob, t, e + 3 * U32 * t.abs(), "top")
