@@ -196,6 +196,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
 }
 
 // 8 entries on their way; see SHIFT below.
+constexpr int FEW_STEPS = 2;
 template <bool SHIFT>
 struct FewPiece {
     u32x4 w;
@@ -223,15 +224,16 @@ struct FewPiece {
 };
 
 // Few rows (a decoding step): bound by reading the weights once.  A workgroup takes 16
-// features and Y units of 16 rows; its waves share the summed axis, blocks of U steps of 32 in
-// turn, every fragment straight from memory (at any alignment) into registers, two blocks asked
-// for at once.  The partial sums meet in LDS.
+// features and Y units of 16 rows; its waves share the summed axis, blocks of two steps of 32 in
+// turn, every fragment straight from memory (at any alignment) into registers, BLOCKS blocks asked
+// for at once (which wave sums what, and in which order, does not depend on it).  The partial sums
+// meet in LDS.
 //
 // SHIFT: rows of an odd number of entries, every other of them 2 bytes off a word.  16-byte reads
-// there are several times slower (4097 -> 11008, one row 79 us, 36 with this), so a lane
+// there are several times slower (4097 -> 11008, one row 79 us, 46 with this), so a lane
 // reads the words around its piece and shifts; the host makes sure that those words hold an
 // entry of the matrix (launch_gated).
-template <typename M, bool BWD, int Y, int U, bool SHIFT>
+template <typename M, bool BWD, int Y, int BLOCKS, bool SHIFT>
 __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
     typedef typename M::Elem E;
     extern __shared__ __attribute__((aligned(16))) char few_lds[];
@@ -248,6 +250,7 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
 #pragma unroll
     for (int y = 0; y < Y; ++y)
         x[y] = static_cast<const E*>(f.x) + min(t0 + y * 16 + r16, a.T - 1) * f.ldx + kq * 8;
+    constexpr int U = FEW_STEPS;
     const int nblocks = f.d / (32 * U), nsteps = f.d / 32;   // what is left goes to the last wave
 
     struct Block {
@@ -272,14 +275,13 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
             Up[y] = M::mma(__builtin_bit_cast(i32x4, u), b, Up[y]);
         }
     };
-    // two blocks of this wave are asked for at once
-    for (int c = wave; c < nblocks; c += waves * 2) {
-        Block b[2];
+    for (int c = wave; c < nblocks; c += waves * BLOCKS) {
+        Block b[BLOCKS];
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < BLOCKS; ++k)
             if (c + k * waves < nblocks) load(b[k], (c + k * waves) * (32 * U));
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < BLOCKS; ++k) {
             if (c + k * waves >= nblocks) break;
 #pragma unroll
             for (int i = 0; i < U; ++i) {
@@ -488,20 +490,19 @@ constexpr int64_t FEW_TILES = 4;
 static int64_t gated_tops(int64_t T, int64_t fp) { return (T + 31) / 32 * 2 * (fp / 16); }
 
 // The launches return how many values of GatedArgs.top they write.
-template <typename M, bool BWD, int Y, int U>
+template <typename M, bool BWD, int Y, int BLOCKS>
 static int64_t launch_gated_few(const FewArgs& f, const GatedArgs& a, hipStream_t st) {
     // Words around the pieces of odd rows: the first row of each matrix begins on a word, and whole steps
     // end before the row does, so an entry before and one behind each piece are in the matrix.
     const bool shift = (f.ldx % 2 != 0 || f.ldw % 2 != 0) && f.d % 32 != 0 && (uintptr_t)f.x % 4 == 0 &&
                        (uintptr_t)f.wg % 4 == 0 && (uintptr_t)f.wu % 4 == 0;
     const dim3 grid((unsigned)(((BWD ? a.fp : a.f) + 15) / 16), (unsigned)((a.T + Y * 16 - 1) / (Y * 16)));
-    constexpr int US = 2;   // (steps at a time with SHIFT, which takes more registers)
-    const int blocks = f.d / (32 * (shift ? US : U));   // as many waves as have work, 8 at most
+    const int blocks = f.d / (32 * FEW_STEPS);   // as many waves as have work, 8 at most
     const int waves = blocks >= 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
     if (shift)
-        hipLaunchKernelGGL((k_gated_few<M, BWD, Y, US, true>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
+        hipLaunchKernelGGL((k_gated_few<M, BWD, Y, 2, true>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
     else
-        hipLaunchKernelGGL((k_gated_few<M, BWD, Y, U, false>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
+        hipLaunchKernelGGL((k_gated_few<M, BWD, Y, BLOCKS, false>), grid, dim3(64 * waves), waves * Y * 2048, st, f, a);
     return (int64_t)grid.x * grid.y * Y;
 }
 

@@ -182,3 +182,25 @@ def test_token_logprobs_with_an_offset(T, V, top, offset):
     assert torch.equal(r.top_index.cpu(), best)
     t = logp.gather(1, best)
     _within(r.top_logprob, t, e + 3 * U32 * t.abs(), "top")
+
+
+# ---------------------------------------------------------------- order of sums
+@pytest.mark.parametrize("T", [1, 5, 16, 17, 30])
+@pytest.mark.parametrize("d", [129, 257, 513, 1001, 2049])
+def test_gated_mlp_sums_do_not_depend_on_alignment(T, d):
+    """The same values in rows an odd and an even number of entries apart: the same bits."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("mlp order", T, d)
+    f = 70
+    x, wg, wu, dh = _half_inputs(T, d, f, 0.3, seed=5)
+
+    def rows(t, ld):
+        buf = torch.zeros((t.shape[0], ld), dtype=t.dtype, device=DEV)
+        buf[:, :d] = t.to(DEV)
+        return buf[:, :d]
+    a, b = ([rows(t, ld) for t in (x, wg, wu)] for ld in (d | 1, (d + 8) // 8 * 8))
+    assert a[0].stride(0) % 2 == 1 or T == 1
+    assert torch.equal(pk.gated_mlp(*a), pk.gated_mlp(*b))
+    for p, q in zip(pk.gated_mlp_backward(dh.to(DEV), *a), pk.gated_mlp_backward(dh.to(DEV), *b)):
+        assert torch.equal(p, q)
