@@ -739,9 +739,10 @@ def linear(q, q_scale, w: PackedCodes, scale, group_size: int = 0, bias=None, ac
         raise ValueError("q needs rows padded to a multiple of 128 columns (as rmsnorm_quant leaves them)")
     g = int(group_size)
     groups = -(-n // g) if g > 0 else 1
+    # (the shape as well: as many scales in another order would give other products)
     if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.device != dev or \
-            scale.numel() != m * groups:
-        raise ValueError(f"scale must be contiguous fp32 with {m * groups} entries")
+            (scale.shape != (m, groups) and (groups > 1 or scale.shape != (m,))):
+        raise ValueError(f"scale must be contiguous fp32 of shape {(m, groups) if groups > 1 else (m,)} on {dev}")
     sp = _vector(q_scale, "q_scale", T, torch.float32, dev)
     if out is None:
         out = torch.empty(T, m, dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
