@@ -700,13 +700,18 @@ class PackedCodes(NamedTuple):
     width: int
 
 
-def pack_codes(codes, width: int = 4) -> PackedCodes:
+def pack_codes(codes, width: int = 4, check: bool = True) -> PackedCodes:
     """bakron_pack_codes: lays out codes (m x n int8, e.g. of solve) once per layer.
-    width 4 holds codes in [-8, 7]."""
+    width 4 holds codes in [-8, 7]; others are refused, which waits for the codes (not
+    with check=False, nor while the stream is being captured: their upper bits are then lost)."""
     torch = _torch or _import_torch()
     _check_dev(codes, "codes", torch.int8)
     if codes.dim() != 2:
         raise ValueError("codes must be m x n")
+    if width == 4 and check and codes.numel() and not torch.cuda.is_current_stream_capturing():
+        lo, hi = (int(v) for v in torch.aminmax(codes))
+        if lo < -8 or hi > 7:
+            raise ValueError(f"codes from {lo} to {hi} do not fit 4 bits: width 8 holds them")
     m, n = codes.shape
     padded = -(-n // PACK_COLUMNS) * PACK_COLUMNS
     data = torch.empty((m, padded * int(width) // 8), dtype=torch.uint8, device=codes.device)

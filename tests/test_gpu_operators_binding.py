@@ -36,3 +36,25 @@ def test_linear_takes_scales_in_their_shape_only():
     for bad in (one[None], one.view(2, 3)):
         with pytest.raises(ValueError):
             pk.linear(q, None, w, bad)
+
+
+def test_pack_refuses_codes_that_do_not_fit():
+    """4 bits hold -8 .. 7: what is beyond would lose its upper bits."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("pack, range")
+    for bad in (8, -9, 127, -128):
+        codes = torch.zeros((3, 40), dtype=torch.int8, device=DEV)
+        codes[2, 39] = bad
+        with pytest.raises(ValueError):
+            pk.pack_codes(codes)
+        assert pk.pack_codes(codes, check=False).data.shape == (3, 64)
+        assert int(pk.pack_codes(codes, 8).data.view(torch.int8)[2, 39]) == bad
+    codes[2, 38:] = torch.tensor([-8, 7], dtype=torch.int8)
+    assert int(pk.pack_codes(codes).data[2, 18]) == 0x80 and int(pk.pack_codes(codes).data[2, 19]) == 0x70
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()   # a capture cannot wait, and is not made to
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=side):
+        p = pk.pack_codes(codes)
+    g.replay()
+    assert torch.equal(p.data, pk.pack_codes(codes).data)
