@@ -411,6 +411,14 @@ def _raise_last(st):
         raise BakronError(st, load().bakron_last_error().decode())
 
 
+def _workspace(work, device):
+    """Address and bytes of a caller's workspace: kernels write there, so it has to be
+    memory of the device, without gaps."""
+    if not work.is_cuda or work.device != device or not work.is_contiguous():
+        raise ValueError(f"work must be contiguous on {device}")
+    return work.data_ptr(), ctypes.c_size_t(work.numel() * work.element_size())
+
+
 def _with_workspace(call, device):
     """Run a workspace-protocol entry point: query the size, allocate a torch
     buffer (256-byte aligned by the caching allocator), then call."""
@@ -449,8 +457,8 @@ def gram(X, w=None, s: float = 1.0, M=None, C=None, work=None):
     if work is None:
         _with_workspace(call, X.device)
     else:
-        size = ctypes.c_size_t(work.numel() * work.element_size())
-        _raise_last(call(_ptr(work), ctypes.byref(size)))
+        wp, size = _workspace(work, X.device)
+        _raise_last(call(ctypes.c_void_p(wp), ctypes.byref(size)))
     return C
 
 
@@ -640,7 +648,8 @@ def _run_op(fn, args, device, work=None, key=None, maybe_none=True):
             _raise_last(fn(*args, 256, ctypes.c_size_t(0), st))
             return
         work = torch.empty(need, dtype=torch.uint8, device=device)
-    _raise_last(fn(*args, work.data_ptr(), ctypes.c_size_t(work.numel() * work.element_size()), st))
+    wp, size = _workspace(work, device)
+    _raise_last(fn(*args, wp, size, st))
 
 
 class NormQuant(NamedTuple):

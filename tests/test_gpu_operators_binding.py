@@ -58,3 +58,22 @@ def test_pack_refuses_codes_that_do_not_fit():
         p = pk.pack_codes(codes)
     g.replay()
     assert torch.equal(p.data, pk.pack_codes(codes).data)
+
+
+def test_workspaces_have_to_be_device_memory():
+    """Kernels write to a workspace: host memory, or a tensor with gaps, is refused before any work."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("workspaces")
+    bf = dict(dtype=torch.bfloat16, device=DEV)
+    x, w, z = torch.zeros((70, 65), **bf), torch.zeros((300, 65), **bf), torch.zeros((1, 60000), device=DEV)
+    q, _, packed = _layer()
+    for work in (torch.empty(1 << 24, dtype=torch.uint8), torch.empty((1 << 12, 1 << 13), dtype=torch.uint8, device=DEV)[:, ::2]):
+        for call in (lambda: pk.gated_mlp(x, w, w, work=work), lambda: pk.token_logprobs(z, work=work),
+                     lambda: pk.gated_mlp_backward(torch.zeros((70, 300), **bf), x, w, w, work=work),
+                     lambda: pk.linear(q, None, packed, torch.ones(6, device=DEV), work=work),
+                     lambda: pk.gram(x.float(), work=work)):
+            with pytest.raises(ValueError):
+                call()
+    good = torch.empty(1 << 24, dtype=torch.uint8, device=DEV)
+    assert torch.equal(pk.gated_mlp(x, w, w, work=good), pk.gated_mlp(x, w, w))
