@@ -744,8 +744,9 @@ def linear(q, q_scale, w: PackedCodes, scale, group_size: int = 0, bias=None, ac
         raise ValueError(f"q has {n} columns, the codes {w.n}")
     padded = -(-n // PACK_COLUMNS) * PACK_COLUMNS
     m, row_bytes = w.data.shape
-    if row_bytes * 8 != padded * w.width or not w.data.is_contiguous() or w.data.device != dev:
-        raise ValueError("w.data must be m x padded row bytes, contiguous, on q's device")
+    if row_bytes * 8 != padded * w.width or not w.data.is_contiguous() or w.data.device != dev or \
+            w.data.dtype != torch.uint8:
+        raise ValueError("w.data must be m x padded row bytes (uint8), contiguous, on q's device")
     if T <= 1:
         # the one row may be a view of any stride: what counts is what follows it
         ldq = padded

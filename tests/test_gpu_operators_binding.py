@@ -77,3 +77,14 @@ def test_workspaces_have_to_be_device_memory():
                 call()
     good = torch.empty(1 << 24, dtype=torch.uint8, device=DEV)
     assert torch.equal(pk.gated_mlp(x, w, w, work=good), pk.gated_mlp(x, w, w))
+
+
+def test_linear_takes_packed_bytes_only():
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("packed bytes")
+    q, _, w = _layer()
+    one = torch.ones(6, device=DEV)
+    for data in (w.data.float(), w.data.to(torch.int16), w.data.cpu(), w.data[:, ::2], w.data[:, :64]):
+        with pytest.raises(ValueError):
+            pk.linear(q, None, w._replace(data=data), one)
