@@ -7,6 +7,7 @@ has not been built, every call raises instead of falling back to anything.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple
 
@@ -141,6 +142,21 @@ def status_string(status: int) -> str:
     return load().bakron_status_string(int(status)).decode()
 
 
+def _on_its_device(fn):
+    """The library launches on the current device: makes that of the first tensor the current
+    one for the call."""
+    @functools.wraps(fn)
+    def call(*args, **kwargs):
+        import torch
+        first = args[0] if args else next(iter(kwargs.values()), None)
+        device = getattr(first, "device", None)
+        if getattr(device, "type", None) != "cuda" or device.index == torch.cuda.current_device():
+            return fn(*args, **kwargs)
+        with torch.cuda.device(device):
+            return fn(*args, **kwargs)
+    return call
+
+
 def _stream(torch, device):
     return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
@@ -171,6 +187,7 @@ class Factors:
     def error(self) -> str:
         return load().bakron_factors_error(self._h).decode()
 
+    @_on_its_device
     def export(self, which: str):
         """Dense fp32 copy of L^A ('A') or L^B ('B') for testing."""
         import torch
@@ -206,6 +223,7 @@ class Factors:
         """The part of profile_read()["node"] that ran on fp32 MFMA (short nodes)."""
         return self._profile_stats()[3]
 
+    @_on_its_device
     def check(self) -> bool:
         """True if every solve on this handle since the last check completed
         all of its ordered waits (synchronises the current stream; a give-up
@@ -229,6 +247,7 @@ class Factors:
             pass
 
 
+@_on_its_device
 def factor(A, B, damp: float) -> Factors:
     """bakron_factor(A, B, damp) on the current stream.  B=None means I."""
     import torch
@@ -276,6 +295,7 @@ def _quantizer(bits, scale, m, n, alphabet, group_size, col_scale):
                       cp)
 
 
+@_on_its_device
 def solve(W, f: Factors, bits: int, scale, codes=None, V=None, pre=None, debug: bool = False,
           alphabet: str = "sym", group_size: int = 0, col_scale=None):
     """bakron_solve / bakron_solve_debug on the current stream.
@@ -311,6 +331,7 @@ def solve(W, f: Factors, bits: int, scale, codes=None, V=None, pre=None, debug: 
     return (codes, V, pre) if debug else (codes, V)
 
 
+@_on_its_device
 def solve_noalloc(W, f: Factors, bits: int, scale, codes=None, V=None, alphabet: str = "sym",
                   group_size: int = 0, col_scale=None):
     """bakron_solve_noalloc on the current stream: the solve with its workspace
@@ -336,6 +357,7 @@ def solve_noalloc(W, f: Factors, bits: int, scale, codes=None, V=None, alphabet:
     return codes, V
 
 
+@_on_its_device
 def solve_antidiag(W, f: Factors, bits: int, scale, codes=None, V=None, pre=None,
                    alphabet: str = "sym", group_size: int = 0, col_scale=None):
     """bakron_solve_antidiag (BaKron-antidiagonal, Alg. 3) on the current stream.
@@ -365,6 +387,7 @@ def solve_antidiag(W, f: Factors, bits: int, scale, codes=None, V=None, pre=None
     return (codes, V) if pre is None else (codes, V, pre)
 
 
+@_on_its_device
 def factor_blockdiag(A, B_blocks, damp: float) -> Factors:
     """bakron_factor_blockdiag: B = blockdiag of B_blocks (nblocks x hb x hb)."""
     import torch
@@ -384,6 +407,7 @@ def factor_blockdiag(A, B_blocks, damp: float) -> Factors:
     return Factors(h.value, n, nb * hb, A.device)
 
 
+@_on_its_device
 def mse_scales(W, bits: int, alphabet: str = "sym", group_size: int = 0, grid: int = 100,
                maxshrink: float = 0.5):
     """bakron_mse_scales on the current stream: m scales, or m x ceil(n/g)."""
@@ -433,6 +457,7 @@ def _with_workspace(call, device):
     return work
 
 
+@_on_its_device
 def gram(X, w=None, s: float = 1.0, M=None, C=None, work=None):
     """bakron_gram: C = s * (X^T diag(w) X) (.) M on the current stream.
     X: N x d fp32; w: N or None; M: d x d or None (may be C itself)."""
@@ -471,6 +496,7 @@ def gram_workspace_bytes(N: int, d: int) -> int:
     return int(need.value)
 
 
+@_on_its_device
 def sample_weights(X, c=None, w=None):
     """bakron_sample_weights: w_k = sum_i c_i X_ki^2 on the current stream."""
     import torch
@@ -489,6 +515,7 @@ def sample_weights(X, c=None, w=None):
     return w
 
 
+@_on_its_device
 def quadform_weights(X, M, w=None):
     """bakron_quadform_weights: w_k = x_k^T M x_k (M symmetric) on the current stream."""
     import torch
@@ -507,6 +534,7 @@ def quadform_weights(X, M, w=None):
     return w
 
 
+@_on_its_device
 def kron_factors(a, b, style: str = "kfac", iters: int = 1):
     """bakron_kron_factors (iters = 1) or bakron_kron_factors_iter (Shampoo
     with `iters` power steps): (A, B) of a global Hessian from paired vector
@@ -533,6 +561,7 @@ def kron_factors(a, b, style: str = "kfac", iters: int = 1):
     return A, B
 
 
+@_on_its_device
 def mlp_local_factors(x, g, D, style: str = "kfac", iters: int = 1):
     """bakron_mlp_local_factors: (A, B) of the MLP-local Hessian from inputs x
     (N x dm), features g or f (N x dff) and W_down D (dm x dff)."""
@@ -620,9 +649,14 @@ def _vector(t, name, n, dtype, device):
     return t.data_ptr()
 
 
-def _raw_stream(device):
-    """The current stream's handle (no Stream object: small calls are bound by the host)."""
-    return (_torch or _import_torch())._C._cuda_getCurrentRawStream(device.index)
+def _run(fn, args, device):
+    """Call an operator on its tensors' device, on the current stream there (by its raw handle:
+    small calls are bound by the host)."""
+    torch = _torch or _import_torch()
+    if torch._C._cuda_getDevice() != device.index:
+        with torch.cuda.device(device):
+            return _run(fn, args, device)
+    _raise_last(fn(*args, torch._C._cuda_getCurrentRawStream(device.index)))
 
 
 _work_sizes = {}
@@ -633,7 +667,10 @@ def _run_op(fn, args, device, work=None, key=None, maybe_none=True):
     holds everything its size depends on, so that it is asked for once; maybe_none: it may
     need none, so try that first."""
     torch = _torch or _import_torch()
-    st = _raw_stream(device)
+    if torch._C._cuda_getDevice() != device.index:
+        with torch.cuda.device(device):
+            return _run_op(fn, args, device, work, key, maybe_none)
+    st = torch._C._cuda_getCurrentRawStream(device.index)
     if work is None:
         need = _work_sizes.get(key) if key is not None else None
         if need is None:
@@ -695,9 +732,8 @@ def rmsnorm_quant(x, weight=None, residual=None, eps: float = 1e-5, normalise: b
         qp, cp = q.data_ptr(), scale.data_ptr()
         if ldq != d:
             q = q[:, :d]
-    _raise_last(lib.bakron_rmsnorm_quant(
-        xp, ldx, rp, ldr, code, T, d, wp, float(eps), 1 if normalise else 0, sp, lds, yp, ldy, qp, ldq,
-        cp, _raw_stream(dev)))
+    _run(lib.bakron_rmsnorm_quant,
+         (xp, ldx, rp, ldr, code, T, d, wp, float(eps), 1 if normalise else 0, sp, lds, yp, ldy, qp, ldq, cp), dev)
     return NormQuant(q, scale, hs, ys)
 
 
@@ -724,8 +760,7 @@ def pack_codes(codes, width: int = 4, check: bool = True) -> PackedCodes:
     m, n = codes.shape
     padded = -(-n // PACK_COLUMNS) * PACK_COLUMNS
     data = torch.empty((m, padded * int(width) // 8), dtype=torch.uint8, device=codes.device)
-    _raise_last(load().bakron_pack_codes(codes.data_ptr(), m, n, int(width), data.data_ptr(),
-                                         _raw_stream(codes.device)))
+    _run(load().bakron_pack_codes, (codes.data_ptr(), m, n, int(width), data.data_ptr()), codes.device)
     return PackedCodes(data, n, int(width))
 
 
@@ -876,9 +911,8 @@ def token_logprobs_backward(logits, target, lse, entropy=None, g_logprob=None, g
         out = torch.empty(T, V, dtype=logits.dtype, device=dev)
     dp, ldd = _rows_of(out, "out", (T, V), logits.dtype, dev)
     f32 = torch.float32
-    _raise_last(lib.bakron_token_logprobs_backward(
-        zp, ld, _dtype_code(logits.dtype), T, V, _vector(target, "target", T, torch.int64, dev),
-        _vector(lse, "lse", T, f32, dev), _vector(entropy, "entropy", T, f32, dev),
-        _vector(g_logprob, "g_logprob", T, f32, dev), _vector(g_entropy, "g_entropy", T, f32, dev), dp,
-        ldd, _raw_stream(dev)))
+    _run(lib.bakron_token_logprobs_backward,
+         (zp, ld, _dtype_code(logits.dtype), T, V, _vector(target, "target", T, torch.int64, dev),
+          _vector(lse, "lse", T, f32, dev), _vector(entropy, "entropy", T, f32, dev),
+          _vector(g_logprob, "g_logprob", T, f32, dev), _vector(g_entropy, "g_entropy", T, f32, dev), dp, ldd), dev)
     return out
