@@ -649,6 +649,15 @@ def _vector(t, name, n, dtype, device):
     return t.data_ptr()
 
 
+def _no_graph(name, instead, *tensors):
+    """Refuses tensors whose gradients somebody expects: these calls record no graph, and a loss
+    that came through one would silently have none."""
+    for t in tensors:
+        if t is not None and t.requires_grad and _torch.is_grad_enabled():
+            raise RuntimeError(f"{name} records no graph for backward(): call it under torch.no_grad() or with "
+                               f"detached tensors{instead}")
+
+
 def _run(fn, args, device):
     """Call an operator on its tensors' device, on the current stream there (by its raw handle:
     small calls are bound by the host)."""
@@ -705,9 +714,10 @@ def rmsnorm_quant(x, weight=None, residual=None, eps: float = 1e-5, normalise: b
     h / rms(h) (normalise=False: weight * h), q = rint(y / scale), scale = max |y| / 127
     per row.  x: T x d fp32, fp16 or bf16; weight: d fp32.  `sum` is returned where
     there is a residual, unless with_sum says otherwise; sum_out (e.g. residual
-    itself) receives it."""
+    itself) receives it.  Records no autograd graph."""
     torch = _torch or _import_torch()
     lib = load()
+    _no_graph("rmsnorm_quant", "", x, weight, residual, sum_out)
     xp, ldx = _rows_of(x, "x")
     T, d = x.shape
     code = _dtype_code(x.dtype)
@@ -769,9 +779,10 @@ def linear(q, q_scale, w: PackedCodes, scale, group_size: int = 0, bias=None, ac
     """bakron_linear on the current stream: act(q_scale * (q (scale * codes)^T) + bias),
     plus `other` (combine "add", the default where there is one) or times it ("mul").
     q, q_scale: as rmsnorm_quant returns them (T x n int8, T); scale: m, or m x
-    ceil(n / group_size).  Returns T x m of dtype (default bf16)."""
+    ceil(n / group_size).  Returns T x m of dtype (default bf16).  Records no autograd graph."""
     torch = _torch or _import_torch()
     lib = load()
+    _no_graph("linear", "", q_scale, scale, bias, other, out)
     qp, ldq = _rows_of(q, "q", None, torch.int8)
     dev = q.device
     T, n = q.shape
@@ -830,9 +841,11 @@ class MlpFeatures(NamedTuple):
 def gated_mlp(x, w_gate, w_up, act: str = "silu", features: bool = False, out=None, work=None):
     """bakron_gated_mlp on the current stream: act(x w_gate^T) * (x w_up^T) in one
     kernel.  x: T x d, w_gate, w_up: f x d, all fp16 or all bf16.  features=True
-    also returns act(G) and act'(G) * U in fp32."""
+    also returns act(G) and act'(G) * U in fp32.  Records no autograd graph: the gradients
+    come from gated_mlp_backward."""
     torch = _torch or _import_torch()
     lib = load()
+    _no_graph("gated_mlp", " and take the gradients from gated_mlp_backward", x, w_gate, w_up, out)
     xp, ldx, T, d, gp, up, ldw, f, code = _mlp_operands(x, w_gate, w_up)
     if out is None:
         out = torch.empty(T, f, dtype=x.dtype, device=x.device)
@@ -876,9 +889,11 @@ class TokenLogprobs(NamedTuple):
 def token_logprobs(logits, target=None, top: int = 0, work=None) -> TokenLogprobs:
     """bakron_token_logprobs on the current stream.  logits: T x V fp32, fp16 or
     bf16; target: T int64 (outside [0, V): ignored, 0) or None; top: number of
-    alternatives, at most 32."""
+    alternatives, at most 32.  Records no autograd graph: the gradients come from
+    token_logprobs_backward."""
     torch = _torch or _import_torch()
     lib = load()
+    _no_graph("token_logprobs", " and take the gradients from token_logprobs_backward", logits)
     zp, ld = _rows_of(logits, "logits")
     T, V = logits.shape
     dev = logits.device

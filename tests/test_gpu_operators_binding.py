@@ -88,3 +88,35 @@ def test_linear_takes_packed_bytes_only():
     for data in (w.data.float(), w.data.to(torch.int16), w.data.cpu(), w.data[:, ::2], w.data[:, :64]):
         with pytest.raises(ValueError):
             pk.linear(q, None, w._replace(data=data), one)
+
+
+def test_calls_that_would_lose_gradients_are_refused():
+    """The operators record no graph: with a tensor that asks for one they raise, they do not detach."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("graphs")
+    q, _, w = _layer()
+    bf = dict(dtype=torch.bfloat16, device=DEV)
+
+    def rand(*shape, **kw):
+        return torch.randn(shape, **(kw or bf))
+    x, wg, wu, z = rand(3, 64), rand(40, 64), rand(40, 64), rand(3, 500)
+    f32 = dict(device=DEV)
+    norm, scale, qs, bias, other = rand(64, **f32), rand(6, **f32), rand(3, **f32), rand(6), rand(3, 6)
+    calls = [(lambda: pk.rmsnorm_quant(x, norm, x), (x, norm)), (lambda: pk.gated_mlp(x, wg, wu), (x, wg, wu)),
+             (lambda: pk.linear(q, qs, w, scale, bias=bias, other=other), (qs, scale, bias, other)),
+             (lambda: pk.token_logprobs(z), (z,))]
+    for call, tensors in calls:
+        want = call()
+        for t in tensors:
+            t.requires_grad_(True)
+            with pytest.raises(RuntimeError, match="no_grad"):
+                call()
+            with torch.no_grad():
+                got = call()
+            t.requires_grad_(False)
+            for a, b in zip(*((v,) if isinstance(v, torch.Tensor) else v for v in (got, want))):
+                assert (a is None and b is None) or torch.equal(a, b)
+    # gradients as values, of parameters too
+    wg.requires_grad_(True)
+    assert all(not g.requires_grad for g in pk.gated_mlp_backward(rand(3, 40), x, wg, wu))
