@@ -446,22 +446,22 @@ struct PadArgs {
     int64_t cols, cols_p;
 };
 __global__ __launch_bounds__(256) void k_pad_rows(PadArgs a) {
-    int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= a.end[2]) return;
-    const int i = e < a.end[0] ? 0 : e < a.end[1] ? 1 : 2;
-    if (i > 0) e -= a.end[i - 1];
-    const int64_t per = a.cols_p / 8, r = e / per, c = e % per * 8;
-    const uint16_t* const src = i == 0 ? a.src[0] : i == 1 ? a.src[1] : a.src[2];
-    uint16_t* const dst = i == 0 ? a.dst[0] : i == 1 ? a.dst[1] : a.dst[2];
-    const uint16_t* const row = src + r * (i == 0 ? a.ld[0] : i == 1 ? a.ld[1] : a.ld[2]);
-    Pack<uint16_t, 8> v;
-    if (c + 8 <= a.cols) {
-        v = load_pack<uint16_t, 8>(row + c);
-    } else {
+    const int64_t per = a.cols_p / 8;
+    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < a.end[2]; n += (int64_t)gridDim.x * 256) {
+        const int i = n < a.end[0] ? 0 : n < a.end[1] ? 1 : 2;
+        const int64_t e = n - (i == 0 ? 0 : i == 1 ? a.end[0] : a.end[1]), r = e / per, c = e % per * 8;
+        const uint16_t* const src = i == 0 ? a.src[0] : i == 1 ? a.src[1] : a.src[2];
+        uint16_t* const dst = i == 0 ? a.dst[0] : i == 1 ? a.dst[1] : a.dst[2];
+        const uint16_t* const row = src + r * (i == 0 ? a.ld[0] : i == 1 ? a.ld[1] : a.ld[2]);
+        Pack<uint16_t, 8> v;
+        if (c + 8 <= a.cols) {
+            v = load_pack<uint16_t, 8>(row + c);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.v[j] = c + j < a.cols ? row[c + j] : (uint16_t)0;
+            for (int j = 0; j < 8; ++j) v.v[j] = c + j < a.cols ? row[c + j] : (uint16_t)0;
+        }
+        store_pack(dst + e * 8, v);
     }
-    store_pack(dst + e * 8, v);
 }
 
 __global__ __launch_bounds__(256) void k_zero_rows(uint16_t* p, int64_t ld, int64_t rows, int64_t cols) {
@@ -634,7 +634,7 @@ static void gated_operands(GatedArgs& a, const PadPlan& p, const void* x, int64_
     if (n > 0) {
         c.cols = d;
         c.cols_p = p.dp;
-        hipLaunchKernelGGL(k_pad_rows, grid256(pieces), dim3(256), 0, st, c);
+        hipLaunchKernelGGL(k_pad_rows, stride_grid(pieces), dim3(256), 0, st, c);
     }
     a.chunks = (int)((kbytes + CHUNK_BYTES - 1) / CHUNK_BYTES);
 }

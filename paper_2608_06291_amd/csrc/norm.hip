@@ -145,27 +145,28 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
     for (int c = a.d + tid; c < a.dpad; c += tpr) out[c] = 0;
 }
 
-// Codes to packed rows: a thread writes 16 bytes (32 codes of 4 bits, 16 of 8).
+// Codes to packed rows: a thread writes 16 bytes (32 codes of 4 bits, 16 of 8) at a time.
 template <int WIDTH>
 __global__ __launch_bounds__(256) void k_pack(const int8_t* __restrict__ codes, int64_t m, int64_t n,
                                               int64_t np, uint32_t* __restrict__ packed) {
     constexpr int PER = 128 / WIDTH;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, per_row = np / PER;
-    if (e >= m * per_row) return;
-    const int64_t i = e / per_row, c = e % per_row * PER;
-    const int8_t* const src = codes + i * n;
-    uint32_t out[4] = {0, 0, 0, 0};
+    const int64_t per_row = np / PER;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < m * per_row; e += (int64_t)gridDim.x * 256) {
+        const int64_t i = e / per_row, c = e % per_row * PER;
+        const int8_t* const src = codes + i * n;
+        uint32_t out[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const uint32_t v = c + j < n ? (uint32_t)(uint8_t)src[c + j] : 0u;
-        if (WIDTH == 8)
-            out[j / 4] |= v << (8 * (j % 4));
-        else
-            out[j / 8] |= (v & 15u) << (8 * (j % 4) + (j % 8 >= 4 ? 4 : 0));
+        for (int j = 0; j < PER; ++j) {
+            const uint32_t v = c + j < n ? (uint32_t)(uint8_t)src[c + j] : 0u;
+            if (WIDTH == 8)
+                out[j / 4] |= v << (8 * (j % 4));
+            else
+                out[j / 8] |= (v & 15u) << (8 * (j % 4) + (j % 8 >= 4 ? 4 : 0));
+        }
+        uint32_t* const dst = packed + e * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dst[j] = out[j];
     }
-    uint32_t* const dst = packed + e * 4;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) dst[j] = out[j];
 }
 
 template <typename E>
@@ -248,8 +249,7 @@ extern "C" bakron_status bakron_pack_codes(const int8_t* codes, int64_t m, int64
     if (!codes || !packed) return bk::op_fail(who, "null pointer");
     if ((uintptr_t)packed & 15) return bk::op_fail(who, "packed must be 16-byte aligned");
     const int64_t np = (n + BAKRON_PACK_COLUMNS - 1) / BAKRON_PACK_COLUMNS * BAKRON_PACK_COLUMNS;
-    const int64_t pieces = m * np * width / 128;
-    const dim3 grid((unsigned)((pieces + 255) / 256));
+    const dim3 grid = bk::stride_grid(m * np * width / 128);
     if (width == 4)
         hipLaunchKernelGGL(bk::k_pack<4>, grid, dim3(256), 0, stream, codes, m, n, np,
                            static_cast<uint32_t*>(packed));

@@ -156,6 +156,14 @@ constexpr int64_t OP_T_MAX = ((int64_t)1 << 31) - 1;
 // Threads of one launch (the runtime takes below 2^32).
 constexpr int64_t OP_LAUNCH_MAX = (int64_t)1 << 31;
 
+// The grid of a kernel that goes through n pieces, 256 threads a workgroup, in strides of the grid: any n,
+// where one piece a thread would pass what a launch takes.
+constexpr int64_t STRIDE_GROUPS = (int64_t)1 << 16;
+inline dim3 stride_grid(int64_t n) {
+    const int64_t groups = (n + 255) / 256;
+    return dim3((unsigned)(groups < STRIDE_GROUPS ? groups : STRIDE_GROUPS));
+}
+
 // CUs of the current device (asked for once a device).
 inline int op_cus() {
     static std::atomic<int> known[16];
