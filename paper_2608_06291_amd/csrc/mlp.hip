@@ -724,7 +724,7 @@ static void run_backward(const FewArgs& few, GatedArgs a, const BackwardPlan& p,
 
 static bakron_status mlp_sizes(const char* who, int64_t ldx, int64_t T, int64_t d, int64_t ldw,
                                int64_t f, int32_t dtype, int32_t act) {
-    if (T < 0 || d < 1 || f < 1 || d > ((int64_t)1 << 17) || f > ((int64_t)1 << 17))
+    if (T < 0 || T > bk::OP_T_MAX || d < 1 || f < 1 || d > ((int64_t)1 << 17) || f > ((int64_t)1 << 17))
         return bk::op_fail(who, "bad size");
     if (ldx < d || ldw < d) return bk::op_fail(who, "leading dimension below d");
     if (dtype != BAKRON_F16 && dtype != BAKRON_BF16) return bk::op_fail(who, "dtype must be 16-bit");
