@@ -544,7 +544,8 @@ typedef enum {
  *   y = normalise ? weight (.) h / sqrt(mean(h^2) + eps) : weight (.) h
  *   scale = max |y| / 127,   q = rint(y / scale)   (ties to even, within +-127)
  * A row of zeros, or one whose scale rounds to 0, has scale 0 and q 0; a row with a NaN or infinite y has scale
- * NaN and q 0.  The norm sees the unrounded h.
+ * NaN and q 0, and so has one whose mean of squares is beyond fp32 (|h| around
+ * 1.8e19).  The norm sees the unrounded h.
  *   x, residual   device, T x d of dtype (bakron_dtype); residual may be NULL
  *   weight        device, d floats, or NULL for 1.  A quantiser's per-column
  *                 factors (bakron_quantizer.col_scale) belong in here

@@ -35,7 +35,7 @@ struct NormArgs {
 template <typename E, int NV>
 __global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
     constexpr int VEC = 16 / sizeof(E);
-    __shared__ float red[2][16];
+    __shared__ float red[3][16];
     const int tid = threadIdx.x, tpr = blockDim.x, lane = tid & 63, wave = tid >> 6;
     const int waves = tpr >> 6;
     const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
@@ -98,7 +98,21 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a) {
     float r = 1.0f;
     if (a.normalise) {
         ssq = group_reduce(ssq, Add(), red[0], wave, lane, waves);
-        const float v = ssq / (float)a.d + a.eps;
+        float v = ssq / (float)a.d + a.eps;
+        if (v < 0x1p-120f) {   // (eps smaller still) squares that fp32 does not hold: again, of h 2^96
+            ssq = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    h[i][j] *= 0x1p96f;
+                    ssq = fmaf(h[i][j], h[i][j], ssq);
+                }
+            }
+            hx *= 0x1p96f;
+            ssq = group_reduce(fmaf(hx, hx, ssq), Add(), red[2], wave, lane, waves);
+            v = ssq / (float)a.d + a.eps * 0x1p96f * 0x1p96f;
+        }
         r = v == 0.0f ? 0.0f : 1.0f / sqrtf(v);
         if (!(v < INFINITY)) r = NAN;   // squares beyond fp32: not silently 0
     }

@@ -7,7 +7,7 @@ import math
 
 import pytest
 
-from test_gpu_operators import U32, _act64, _rand, _say, _slope64, _t, _tiny, _u, _within
+from test_gpu_operators import U32, _act64, _dtype, _rand, _say, _slope64, _t, _tiny, _u, _within
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -33,6 +33,25 @@ def test_norm_codes_of_subnormal_rows():
     want = (x.double() / torch.where(zero, 1.0, s)[:, None]).clamp(-127, 127)
     err = torch.where(zero[:, None], 0.0, q - want).abs()
     assert bool((err <= 0.5 + 127 * 4 * U32).all()), float(err.max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 1003, 20000])
+def test_norm_of_tiny_rows_without_eps(dtype, d):
+    """eps = 0: the mean of squares of rows down to the smallest numbers is not lost."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("norm tiny", dtype, d)
+    x = _rand((12, d), 3).clamp(-4, 4) * 2.0 ** torch.tensor([-10, -55, -59, -60, -61, -62, -63, -70, -75, -90, -110, -130])[:, None]
+    x = x.to(_dtype(dtype))
+    for w in (None, (1 + 0.1 * _rand((d,), 4)).float()):
+        r = pk.rmsnorm_quant(x.to(DEV), weight=None if w is None else w.to(DEV), eps=0.0, with_y=True)
+        h = x.double()
+        y = h / torch.sqrt((h * h).mean(1, keepdim=True)) * (1 if w is None else w.double())
+        # squares that are subnormal beside a mean of 2^-120 or more: a step of 2^-149 each
+        e = (d + 16) * U32 + 2.0 ** -29
+        _within(r.y, y, e * y.abs() + _u(dtype) * y.abs() * (1 + e) + _tiny(dtype), "y")
+        _within(r.scale, y.abs().amax(1) / 127, e * y.abs().amax(1) / 127, "scale")
 
 
 # ---------------------------------------------------------------- gated MLP, gradients in half precision
