@@ -46,7 +46,7 @@ __device__ inline void linear_store(const LinearArgs& a, int64_t t, int64_t i, f
                                     const float (&bias)[N], const float (&other)[N]) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        float v = act_value(z[j] + bias[j], a.act);
+        float v = act_value<sizeof(E) == 4>(z[j] + bias[j], a.act);
         if (a.combine == BAKRON_COMBINE_ADD) v += other[j];
         if (a.combine == BAKRON_COMBINE_MUL) v *= other[j];
         z[j] = v;

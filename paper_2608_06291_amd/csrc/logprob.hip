@@ -30,8 +30,6 @@ constexpr int LP_TOP = 32;            // alternatives at most
 constexpr int LP_CAND = 1024;         // candidates that are ranked by counting
 constexpr int LP_PARTS = 64;          // parts of a row at most
 constexpr int LP_JOIN = 256;          // candidates that the join ranks by counting
-constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LN2 = 0.69314718055994530942f;
 
 // What a part of a row leaves for the join.
 struct LpPart {
@@ -382,10 +380,10 @@ __global__ __launch_bounds__(256) void k_logprob_grad(LpGradArgs a) {
     const float gl = asked && a.g_logprob ? a.g_logprob[row] : 0.0f;
     const float gh = ENT ? a.g_entropy[row] : 0.0f, H = ENT ? a.entropy[row] : 0.0f;
     auto grad = [&](float x, int c) {
-        const float lp = x - lse;
-        const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
+        const float lp = max_nan(x - lse, -200.0f);   // (exp is 0 there; 0 * -inf stays out)
+        const float p = exp_of<sizeof(E) == 4>(lp);
         float g = gl;
-        if (ENT) g = fmaf(gh, max_nan(lp, -1e4f) + H, gl);   // (0 * -inf stays out)
+        if (ENT) g = fmaf(gh, lp + H, gl);
         const float v = -p * g;
         return c == t ? v + gl : v;
     };

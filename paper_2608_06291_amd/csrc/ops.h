@@ -120,6 +120,16 @@ __device__ inline float group_reduce(float v, Op op, float* red, int wave, int l
     return v;
 }
 
+// exp(x), |x| <= 200, from the hardware's exp2 (1 ulp).  x log2 e in fp32 alone leaves a relative error of
+// |x| 2^-24, which 16-bit results do not show; FINE: what the product lost and log2 e's next bits, too.
+constexpr float LOG2E = 1.44269504088896340736f, LOG2E_REST = 1.925963033500e-8f, LN2 = 0.69314718055994530942f;
+template <bool FINE>
+__device__ inline float exp_of(float x) {
+    const float t = x * LOG2E, e = __builtin_amdgcn_exp2f(t);
+    if constexpr (!FINE) return e;
+    return e * fmaf(fmaf(x, LOG2E_REST, fmaf(x, LOG2E, -t)), LN2, 1.0f);
+}
+
 inline bakron_status op_fail(const char* who, const char* what) {
     char buf[256];
     std::snprintf(buf, sizeof(buf), "%s: %s", who, what);

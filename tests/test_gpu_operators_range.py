@@ -7,7 +7,7 @@ import math
 
 import pytest
 
-from test_gpu_operators import U32, _act64, _dtype, _rand, _say, _slope64, _t, _tiny, _u, _within
+from test_gpu_operators import U32, _act64, _dtype, _gen, _rand, _say, _slope64, _t, _tiny, _u, _within
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -201,6 +201,54 @@ def test_token_logprobs_with_an_offset(T, V, top, offset):
     assert torch.equal(r.top_index.cpu(), best)
     t = logp.gather(1, best)
     _within(r.top_logprob, t, e + 3 * U32 * t.abs(), "top")
+
+
+def test_token_logprobs_gradient_of_unlikely_tokens():
+    """p of unlikely tokens in fp32, to the rounding of z - lse and a few more."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("logprob gradient, unlikely")
+    V = 4000
+    z = (-torch.rand((3, V), generator=_gen(1), dtype=torch.float64) * 80).float()
+    z[:, 0] = 0
+    lse = torch.logsumexp(z.double(), 1).float()
+    d = pk.token_logprobs_backward(z.to(DEV), torch.zeros(3, dtype=torch.int64, device=DEV), lse.to(DEV),
+                                   g_logprob=torch.full((3,), -1.0, device=DEV))
+    lp = z.double() - lse.double()[:, None]
+    p = lp.exp()
+    # z - lse rounded once (an error of the exponent, so relative in p), exp2 and its argument 4 units
+    tol = p * (U32 * lp.abs() * 1.01 + 4 * U32)
+    _within(d[:, 1:], p[:, 1:], tol[:, 1:], "p")
+
+
+# ---------------------------------------------------------------- activations
+def _activation_through_linear(z, act):
+    """act(z) in fp32 by a product whose sums are exact: z (n) multiples of 1/64 below 250 in size."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    k = (z * 64).round().to(torch.int64)
+    n, T = 256, z.numel()
+    q = torch.zeros((T, n), dtype=torch.int8)
+    left = k.clone()
+    for j in range(127):   # k as a sum of entries of at most 127
+        step = left.clamp(-127, 127)
+        q[:, j] = step.to(torch.int8)
+        left -= step
+    assert int(left.abs().sum()) == 0
+    codes = torch.ones((16, n), dtype=torch.int8, device=DEV)
+    y = pk.linear(q.to(DEV), None, pk.pack_codes(codes, 8), torch.full((16,), 1.0 / 64, device=DEV), act=act,
+                  dtype=torch.float32)
+    assert bool((y == y[:, :1]).all())
+    return y[:, 0]
+
+
+def test_silu_of_negative_numbers():
+    torch = _t()
+    _say("silu tail")
+    z = torch.arange(-85 * 64, 60 * 64, dtype=torch.float64) / 64
+    want = z * torch.sigmoid(z)
+    # exp2 of a two-part argument, sum, reciprocal, product: a unit or two each
+    _within(_activation_through_linear(z, "silu"), want, 8 * U32 * want.abs(), "silu")
 
 
 # ---------------------------------------------------------------- order of sums
