@@ -251,6 +251,15 @@ def test_silu_of_negative_numbers():
     _within(_activation_through_linear(z, "silu"), want, 8 * U32 * want.abs(), "silu")
 
 
+def test_gelu_of_negative_numbers():
+    torch = _t()
+    _say("gelu tail")
+    z = torch.arange(-12 * 64, 12 * 64, dtype=torch.float64) / 64
+    want = z * 0.5 * torch.special.erfc(-z * math.sqrt(0.5))   # (ndtr is 1 + erf: nothing is left of it at -9)
+    # a polynomial within 2e-7 relative to the tail, exp2 of a two-part argument, products
+    _within(_activation_through_linear(z, "gelu"), want, (2e-7 + 10 * U32) * want.abs(), "gelu")
+
+
 # ---------------------------------------------------------------- order of sums
 @pytest.mark.parametrize("T", [1, 5, 16, 17, 30])
 @pytest.mark.parametrize("d", [129, 257, 513, 1001, 2049])
