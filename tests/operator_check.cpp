@@ -1,7 +1,13 @@
 // CPU check of the host code of the operators around a quantised layer: the launches that
 // calls at the limits of their sizes make, recorded instead of made.  The kernels are
 // not run.  Prints one line a check; exit status = number of failing ones.
+//
+//   operator_check                    the checks
+//   operator_check tile I T           edge of the tiles of a product of I x T outputs on 256 CUs
+//   operator_check backward T D F     of the gradients: edge and parts for dx, edge and parts for dW
 #include <cstdio>
+#include <cstdlib>
+#include <cstring>
 #include <hip/hip_runtime.h>
 
 namespace {
@@ -42,7 +48,17 @@ void bk::set_last_error(const char*) {}
 
 static void* const P = reinterpret_cast<void*>(4096);
 
-int main() {
+int main(int argc, char** argv) {
+    if (argc == 4 && std::strcmp(argv[1], "tile") == 0) {
+        std::printf("%d\n", bk::pick_tile(std::atoll(argv[2]), std::atoll(argv[3]), 256, true));
+        return 0;
+    }
+    if (argc == 5 && std::strcmp(argv[1], "backward") == 0) {
+        const bk::BackwardPlan p =
+            bk::backward_plan(std::atoll(argv[2]), std::atoll(argv[3]), std::atoll(argv[4]), true, true, true, 256);
+        std::printf("%d %d %d %d\n", p.dx.tile, p.dx.parts, p.dw.tile, p.dw.parts);
+        return 0;
+    }
     const int before = fails;
     for (int width : {4, 8}) bakron_pack_codes(static_cast<int8_t*>(P), 1 << 20, 1 << 17, width, P, nullptr);
     size_t size = ~(size_t)0;

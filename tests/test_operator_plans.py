@@ -6,6 +6,8 @@ import subprocess
 
 import pytest
 
+from operator_sizes import BACKWARD, GATED, LINEAR_BIG
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 
@@ -27,3 +29,29 @@ def checker(tmp_path_factory):
 def test_launches_and_limits(checker):
     r = subprocess.run([checker], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0 and "fails 0" in r.stdout, r.stdout[-4000:]
+
+
+def _plan(checker, *args):
+    r = subprocess.run([checker, *map(str, args)], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0
+    return tuple(int(v) for v in r.stdout.split())
+
+
+def test_sizes_of_the_tile_tests_take_their_tiles(checker):
+    """test_gpu_operators_tiles.py tests the 256 x 256 tiles only while its sizes take them."""
+    for T, n, m in LINEAR_BIG:
+        assert _plan(checker, "tile", m, T) == (256,), (T, n, m)
+    for T, d, f in GATED:
+        assert _plan(checker, "tile", 2 * f, T) == (256,), (T, d, f)
+    # several chunks, odd numbers of them among these, the last not whole
+    assert {3, 5, 7} <= {-(-n // 128) for _, n, _ in LINEAR_BIG} and {5, 7} <= {-(-d // 64) for _, d, _ in GATED}
+    assert any(n % 128 for _, n, _ in LINEAR_BIG) and any(d % 64 for _, d, _ in GATED)
+    seen = set()
+    for T, d, f, _, _, dx, dw in BACKWARD:
+        p = _plan(checker, "backward", T, d, f)
+        assert (dx is None or p[:2] == dx) and (dw is None or p[2:] == dw), (T, d, f, p)
+        seen |= {("dx", *(dx or ())), ("dw", *(dw or ()))}
+    assert {("dx", 256, 1), ("dx", 256, 3), ("dw", 256, 1), ("dw", 256, 4)} <= seen
+    # the gated product of the first of them, too (its rows are padded to whole chunks)
+    T, _, f = BACKWARD[0][:3]
+    assert _plan(checker, "tile", 2 * (-(-f // 64) * 64), T) == (256,)
