@@ -115,26 +115,28 @@ __device__ inline uint32_t lds_address(char* p) {
 // 16 bytes a lane from p to LDS address `to` (the same in all lanes) + 16 * lane.  In
 // assembly because the compiler waits for every load of its own before a transposing LDS
 // read, which it cannot tell from the place being loaded; all waits are wait_loads().  It
-// writes no register.
+// writes no register but m0, which cannot be declared (the compiler keeps it for itself and need not
+// honour that): a kernel that loads this way must use m0 for nothing else, no builtin load to LDS
+// among it.  A test holds the built kernels to that.
 __device__ inline void load_lds(const char* p, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(
                      __builtin_amdgcn_readfirstlane(to)),
                  "v"(p)
-                 : "memory", "m0");
+                 : "memory");
 }
 // The same from base (the same in all lanes) + off.
 __device__ inline void load_lds(const char* base, uint32_t off, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(
                      __builtin_amdgcn_readfirstlane(to)),
                  "v"(off), "s"(base)
-                 : "memory", "m0");
+                 : "memory");
 }
 // 4 bytes a lane.
 __device__ inline void load_lds_word(const float* p, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(
                      __builtin_amdgcn_readfirstlane(to)),
                  "v"(p)
-                 : "memory", "m0");
+                 : "memory");
 }
 template <int N>
 __device__ inline void wait_loads() {   // all but the last N of this wave's
