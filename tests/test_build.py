@@ -1,10 +1,11 @@
-"""CPU check of the built library: m0, which the assembly loads to LDS write without being
-able to say so, is used for nothing else in their kernels."""
+"""CPU checks of the built library: what build() shows, and that m0, which the assembly loads to LDS
+write without being able to say so, is used for nothing else in their kernels."""
 import glob
 import os
 import re
 import struct
 import subprocess
+import types
 
 import pytest
 
@@ -56,3 +57,14 @@ def test_no_assembly_claims_a_reserved_register():
         for asm in re.findall(r"asm volatile\((.*?)\);", open(f).read(), flags=re.S):
             clobbers = asm.rsplit(":", 1)[-1]
             assert not re.search(r"\"(m0|exec|vcc|scc)\"", clobbers), (f, asm)
+
+
+def test_build_shows_warnings(monkeypatch, capsys, tmp_path):
+    from paper_2608_06291_amd import build
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "lib.so"))
+    monkeypatch.setattr(build.os, "replace", lambda a, b: None)
+    err = "a.hip:3: warning: something\nwarning: '-packed-fp32-ops' is not a recognized feature\n"
+    monkeypatch.setattr(build.subprocess, "run", lambda *a, **k: types.SimpleNamespace(returncode=0, stdout="", stderr=err))
+    build.build()
+    shown = capsys.readouterr().err
+    assert "warning: something" in shown and "packed" not in shown
