@@ -223,13 +223,7 @@ __global__ __launch_bounds__(LP_THREADS, 6) void k_logprob(LpArgs a) {
             ties = 1;
         }
         if (n <= LP_CAND) {
-            // every entry of the list has its own rank, whatever order it was filled in
-            for (int i = tid; i < n; i += LP_THREADS) {
-                const uint64_t v = cand[i];
-                int above = 0;
-                for (int k = 0; k < n; ++k) above += cand[k] > v;
-                if (above < a.top) put(above, v);
-            }
+            rank(n);
             // then the first entries equal to b, in the order of their indices
             for (int c0 = lo; ties && n < a.top && c0 < hi; c0 += LP_THREADS) {
                 const bool is = c0 + tid < hi && (float)z[c0 + tid] == b;

@@ -223,7 +223,6 @@ struct Source {
 template <typename M, int BM, int BN, int WM, int WN, int BUFS, bool ACOLS = false, bool BCOLS = false,
           int FLUSH = 0>
 struct Tile {
-    static constexpr bool BIG = false;
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int ROWS = BM, COLS = BN;
     static constexpr int TM = BM / WM, TN = BN / WN;      // a wave's part
@@ -414,7 +413,6 @@ struct Tile {
 // to 25 us a round.
 template <typename M, bool ACOLS = false, bool BCOLS = false>
 struct BigTile {
-    static constexpr bool BIG = true;
     static constexpr int THREADS = 512, ROWS = 256, COLS = 256;
     static constexpr int A_LDS = ROWS * M::A_BYTES, B_LDS = COLS * CHUNK_BYTES;
     static constexpr int A_HALF = A_LDS / 2, B_HALF = B_LDS / 2;
