@@ -4,14 +4,15 @@
 // The products of 8-bit values run on the integer matrix cores and are summed exactly:
 // |16 c q| <= 128 * 127 and n <= 2^17 keep the sum below 2^31.
 //
-// Many rows: the tiles of tile.h.  2048 x 8192 x 28672 in 4 bits 412 to 428 us, 2250 to 2330 TOPS (the library's
-// 8-bit product of 8192^3: 2202), 483 with SiLU and a factor, whose 117 MB are read and multiplied
-// while no tile is; 4096^3 62 us; with a scale for 128 columns 102 us, 1001 rows of
-// it 35: there each chunk's sums are scaled in fp32, two vector operations an accumulator
-// against two MFMAs, and both sets of sums halve the tile that fits.
-// Few rows: 1 x 4096 x 11008 in 4 bits with a scale for 128 columns 8.4 us, of which the codes'
-// 24 MB are 4.6 at the rate of a large copy; launch and three dependent trips to memory
-// are the rest.
+// Many rows: the tiles of tile.h.  2048 x 8192 x 28672 in 4 bits 389 to 428 us, 2250 to 2470 TOPS (the library's
+// 8-bit product of 8192^3: 2200), in 8 bits 387, with GELU 420 to 434, with SiLU and a factor, whose 117 MB
+// are read and multiplied while no tile is, 460 to 483; 4096^3 59 to 64 us, with a scale for 128 columns 93 to
+// 102.  1001 x 4096 x 4096 with such scales 36 us (for 64 columns 37; 8-bit codes 29, and 22 to 24 with one
+// scale a row): there each chunk's sums are scaled in fp32, two vector operations an
+// accumulator against two MFMAs, and both sets of sums halve the tile that fits.
+// Few rows: 1 x 4096 x 11008 in 4 bits with a scale for 128 columns 8.0 us (for 64 columns 9.9), of
+// which the codes' 24 MB are 4.6 at the rate of a large copy; launch and three dependent trips to
+// memory are the rest.  In 8 bits 10.8 (45 MB: 8.7), with a scale for 128 columns 12.1.
 #include "tile.h"
 
 namespace bk {

@@ -11,11 +11,14 @@
 // Top k without sorting: a workgroup holds its part of the row in registers, cuts
 // its threads into 32 groups and takes the k-th largest group maximum as a bound.
 // At least k entries are not below it, and of a row in random order only about
-// 32 (H_32 - H_(32-k)) (31 for k = 20) are, so the candidates are ranked by counting.
+// 32 (H_32 - H_(32-k)) (31 for k = 20) are, so the candidates are ranked by counting.  Where fewer than k
+// groups hold an entry there is no bound, and more than 1024 candidates are then gone through k times: 16-bit
+// rows (or parts of one) of 1025 to 128 (k - 1) tokens, fp32 ones to 64 (k - 1) (8192 x 2000 bf16: 230 us for
+// k = 20, 35 for 5).
 //
-// Bound by memory: 2048 x 131072 bf16 (537 MB) with 5 alternatives and masked rows 114 us, 4.7 TB/s,
-// without alternatives 96; the gradient of 4096 x 32768 (537 MB) 91 us, 5.9 TB/s (a large copy
-// here: 5.2).  What kept the first kernel at 328 us: loads behind branches, one after
+// Bound by memory: 2048 x 131072 bf16 (537 MB) with 5 alternatives and masked rows 107 to 114 us, 4.7 to 5.0
+// TB/s, without alternatives 96 to 103, in fp32 187; the gradient of 4096 x 32768 (537 MB) 91 us, 5.9 TB/s, in
+// fp32 178 (a large copy here: 5.2).  What kept the first kernel at 328 us: loads behind branches, one after
 // another, entries held in fp32 (twice the registers, half the workgroups), and the
 // masked rows' thousands of equal logits going through one counter.  One row of 131072 with 20
 // alternatives takes 12 us in two launches, latency.
@@ -240,7 +243,7 @@ __global__ __launch_bounds__(LP_THREADS, 6) void k_logprob(LpArgs a) {
             }
             for (int k = n + tid; k < a.top; k += LP_THREADS) put(k, 0);   // (part shorter than top)
         } else {
-            // a row in an order that defeats the bound (one group of threads far below the
+            // no bound, or a row in an order that defeats it (one group of threads far below the
             // others): the largest entry below the last one, top times
             uint64_t mine = 0, v = ~0ull;
             for (int k = 0; k < a.top; ++k) {

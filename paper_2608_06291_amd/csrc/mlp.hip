@@ -10,16 +10,17 @@
 // G and U are computed again in the backward pass (two of its six products, and 4 T f bytes less
 // to keep).  dG and dU are rounded to 16 bits, as the products that follow take them: one
 // rounding more than fp32 arithmetic, so dx and the weights' gradients are off by 2.4e-3 of their
-// norm in bf16 where a single rounding gives 1.7e-3, except where few entries make up a result
-// (backward_plan).
+// norm in bf16 where a single rounding gives 1.7e-3 (2.9e-4 and 2.1e-4 in half precision), except where
+// few entries make up a result (backward_plan).
 // In half precision their range counts, too: see GradScale.
 // The gradients' products read the weights, x, dG and dU as they lie (columns, see
 // tile.h), with no transposed copies.
 //
-// Measured (bf16, 4096 -> 11008): 8192 rows 1085 to 1220 us by the box, 1210 to 1364 TFLOP/s (the
-// library's product of that size: 1312), matrix cores 70% busy; backward of 4096 rows 1806 to
-// 1910 us: gated product 603, dx 522, dW 665; the first and last take 5.4 rounds of tiles in the
-// time of 6.  One row 34 us: the weights' 180 MB at 5.2 TB/s.
+// Measured (bf16, 4096 -> 11008): 8192 rows 1068 to 1220 us by the box, 1210 to 1384 TFLOP/s (the
+// library's product of that size: 1312 to 1363), matrix cores 68% busy, with the features, 8 bytes more an
+// entry, 1240 to 1290; backward of 4096 rows 1790 to 1910 us: gated product 584, dx 518 (matrix cores 66%
+// busy), dW 673 (53%), in half precision 617, 535, 679.  The first and last take 5.4 rounds of tiles in the
+// time of 6; of dW both operands come by transposing reads.  One row 35 us: the weights' 180 MB at 5.2 TB/s.
 #include "tile.h"
 
 namespace bk {
@@ -47,7 +48,8 @@ struct GatedArgs {
 // leaves the largest of them that is finite; where that is below 1 or beyond 65504 a second run of it takes
 // all of them times the power of two that puts the largest at 2^14 to 2^15, and the products that
 // follow undo it (in fp32).  Then no number down to 2^-29 of the largest loses a bit.  The second run is
-// launched in any case and ends at once where there is nothing to do: 5 us.
+// launched in any case and ends at once where there is nothing to do: 1111 x 1000 -> 2731 75.4 -> 79.2 us,
+// and 24 more where the run is needed.
 struct GradScale {
     float factor, undo;
 };

@@ -2,13 +2,14 @@
 //
 //   h = x + r,   y = w (.) h / sqrt(mean(h^2) + eps),   s = max |y| / 127,   q = rint(y / s)
 //
-// Every entry is read once and stays in registers over the two reductions of its
-// row (the sum of squares, then the largest |y|, which needs the first), so the
-// kernel moves what it must: x and r in, h and q out.  Bound by memory: 4096 x 8192 bf16
-// with a residual 40 us, 5.9 TB/s of 235 MB (a large copy here: 5.2); one row of 4096 3.5 us, all
-// latency.  A row per workgroup of one or two vectors a thread; loads are whole vectors at
-// clamped addresses, issued together (with a branch around each they went one after
-// the other: 47.5 us).
+// Every entry is read once and stays in registers over the two reductions of its row (the
+// sum of squares, then the largest |y|, which needs the first), so the kernel moves what it
+// must: x and r in, h and q out.  Bound by memory: 4096 x 8192 bf16 with a residual 40 us,
+// 5.9 TB/s of 235 MB (a large copy here: 5.2), 2048 x 8192 fp32 34 us; one row of 4096 3.6 us,
+// all latency.  A row per workgroup of one or two vectors a thread; loads are whole vectors
+// at clamped addresses, issued together (with a branch around each they went one after
+// the other: 47.5 us).  fp32 rows of more than 32768 entries take 64 of them a thread, and
+// about 50 registers go to memory and back: 1024 x 65536 220 us, 4.0 TB/s.
 #include "ops.h"
 
 namespace bk {
