@@ -825,6 +825,8 @@ def _mlp_operands(x, w_gate, w_up):
     gp, ldw = _rows_of(w_gate, "w_gate", None, x.dtype, x.device)
     f = w_gate.shape[0]
     up, ldu = _rows_of(w_up, "w_up", (f, d), x.dtype, x.device)
+    if f <= 1:
+        ldw = ldu = d   # (one row has no next one)
     if w_gate.shape[1] != d or ldu != ldw:
         raise ValueError("w_gate and w_up must be f x d with the same distance between rows")
     return xp, ldx, T, d, gp, up, ldw, f, _dtype_code(x.dtype)

@@ -120,3 +120,18 @@ def test_calls_that_would_lose_gradients_are_refused():
     # gradients as values, of parameters too
     wg.requires_grad_(True)
     assert all(not g.requires_grad for g in pk.gated_mlp_backward(rand(3, 40), x, wg, wu))
+
+
+def test_gated_mlp_of_one_feature_takes_any_distance():
+    """One row has no next one: views whose rows would lie at different distances are the same weights."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("one feature")
+    bf = dict(dtype=torch.bfloat16, device=DEV)
+    x, wide, dh = torch.randn((5, 64), **bf), torch.randn((3, 160), **bf), torch.randn((5, 1), **bf)
+    wg, wu = torch.randn((1, 64), **bf), wide[1:2, 8:72]
+    want = pk.gated_mlp(x, wg, wu.clone())
+    assert torch.equal(pk.gated_mlp(x, wg, wu), want) and torch.equal(pk.gated_mlp(x, wg, wide[::2][1:, 8:72]),
+                                                                      pk.gated_mlp(x, wg, wide[2:, 8:72].clone()))
+    for a, b in zip(pk.gated_mlp_backward(dh, x, wg, wu), pk.gated_mlp_backward(dh, x, wg, wu.clone())):
+        assert torch.equal(a, b)
