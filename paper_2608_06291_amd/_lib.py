@@ -1,8 +1,9 @@
 """ctypes binding for libbakron.so -- argument marshalling only.
 
 Every step of the solver runs in the library's HIP kernels; torch is used only
-for device memory (``data_ptr()``) and the current HIP stream.  If the library
-has not been built, every call raises instead of falling back to anything.
+for device memory (``data_ptr()``), the current HIP stream and the range check of
+pack_codes.  If the library has not been built, every call raises instead of falling
+back to anything.
 """
 from __future__ import annotations
 
