@@ -694,6 +694,133 @@ bakron_status bakron_token_logprobs_backward(const void *logits, int64_t ld, int
                                              const float *g_logprob, const float *g_entropy,
                                              void *d, int64_t ldd, hipStream_t stream);
 
+/*
+ * bakron_head_logprobs -- log probabilities of given tokens and entropies from the rows
+ * before the vocabulary matrix: bakron_token_logprobs of z = x w^T, without z
+ *   lse_t = log sum_j exp(z_tj),   logprob_t = z_t,target - lse_t,
+ *   entropy_t = -sum_j p_tj log p_tj,   p = exp(z - lse)
+ * z is summed in fp32 and not rounded.  Log probabilities are taken from the row's
+ * largest logit.
+ *   x        device, T x d of dtype BAKRON_F16 or BAKRON_BF16
+ *   w        device, V x d of dtype, the vocabulary matrix
+ *   target   device, T token numbers, or NULL (then logprob must be NULL).  One
+ *            outside [0, V) asks for nothing: logprob 0
+ *   logprob, entropy, lse   device outputs, T floats each, or NULL
+ * A row with a logit that is NaN or +inf has NaN in every output; one whose logits
+ * are all -inf has lse and log probability -inf and entropy 0.
+ * 1 <= d <= 2^17, 1 <= V <= 2^20; ceil(T / 64) ceil(max(d, V) / 64) < 2^23 (or
+ * BAKRON_EINVAL).  Workspace as above: 16 bytes a row for 32 to 256 tokens of the
+ * vocabulary, and padded copies of x and w where their rows are no 16-byte multiples
+ * at 16-byte addresses and T > 32.
+ */
+bakron_status bakron_head_logprobs(const void *x, int64_t ldx, int64_t T, int64_t d, const void *w,
+                                   int64_t ldw, int64_t V, int32_t dtype, const int64_t *target,
+                                   float *logprob, float *entropy, float *lse, void *work,
+                                   size_t *work_bytes, hipStream_t stream);
+
+/*
+ * bakron_head_logprobs_backward -- its gradients, from those with respect to the log
+ * probabilities and entropies (the logits are computed again, in pieces of the
+ * vocabulary):
+ *   dz_tj = g_logprob_t (1[j = target_t] - p_tj) - g_entropy_t p_tj (log p_tj + entropy_t)
+ *   dx = dz w,   dw = dz^T x
+ * A target outside [0, V) has no first term; a row whose logits are all -inf has dz = 0.
+ * dz is rounded to dtype for the products, in BAKRON_F16 times
+ * a power of two (undone at the end) by the largest |g_logprob| + 4 |g_entropy|; with the
+ * result's own rounding that leaves errors of about 2.4e-3 of a gradient's norm in
+ * BAKRON_BF16 and 2.9e-4 in BAKRON_F16 (with a hundred rows up to 3e-3 and 4e-4), where one
+ * rounding gives 1.7e-3 and 2.1e-4.  For T <= 64, where the errors may not average out, dz is kept as two numbers of dtype, and the
+ * result is as good as rounded once.
+ *   lse, entropy  from bakron_head_logprobs (entropy may be NULL without g_entropy)
+ *   g_logprob, g_entropy  device, T floats, or NULL for 0; target may be NULL
+ *                 without g_logprob
+ *   dx            device output, T x d of dtype, or NULL
+ *   dw            device output, V x d of dtype, or NULL.  T = 0 gives zeros
+ * Other arguments as bakron_head_logprobs.  The workspace holds dz of one piece (128 MB,
+ * or that of 256 tokens where it is more), T x d floats where there are several pieces, and padded copies.
+ */
+bakron_status bakron_head_logprobs_backward(const void *x, int64_t ldx, int64_t T, int64_t d,
+                                            const void *w, int64_t ldw, int64_t V, int32_t dtype,
+                                            const int64_t *target, const float *lse,
+                                            const float *entropy, const float *g_logprob,
+                                            const float *g_entropy, void *dx, int64_t lddx,
+                                            void *dw, int64_t lddw, void *work,
+                                            size_t *work_bytes, hipStream_t stream);
+
+/*
+ * bakron_layernorm -- residual addition and layer norm, or RMS norm, with the rows'
+ * statistics:
+ *   h = x + residual (rounded once to dtype)
+ *   y = weight (.) (h - mean) / sqrt(var + eps) + bias
+ * mean and var are those of the rounded h, so that `sum` is all that the backward pass
+ * needs of it.  Without centre, mean is 0 and var is mean(h^2).
+ *   x, residual    device, T x d of dtype (bakron_dtype); residual may be NULL
+ *   weight, bias   device, d floats, or NULL for 1 and 0
+ *   eps            finite, at least 1e-30
+ *   sum            device output of dtype, h, or NULL; may be x or residual with the same
+ *                  leading dimension
+ *   y              device output of dtype, y rounded once, or NULL
+ *   mean, rstd     device outputs, T floats: mean and 1 / sqrt(var + eps), or NULL; mean
+ *                  only with centre
+ * A row with a NaN or infinite h, or whose squares sum beyond fp32, has NaN in y and rstd.
+ * 1 <= d <= 65536.  One launch.
+ */
+bakron_status bakron_layernorm(const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                               int32_t dtype, int64_t T, int64_t d, const float *weight,
+                               const float *bias, float eps, int32_t centre, void *sum,
+                               int64_t lds, void *y, int64_t ldy, float *mean, float *rstd,
+                               hipStream_t stream);
+
+/*
+ * bakron_layernorm_backward -- its gradients from dy, the gradient with respect to y:
+ *   n = (x - mean) rstd,  g = weight (.) dy
+ *   dx = rstd (g - mean_j(g) - n mean_j(g n)) + d_sum      (no mean_j(g) without mean)
+ *   dweight = sum_t dy_t (.) n_t,   dbias = sum_t dy_t
+ *   x             device, T x d of dtype: the rows that the norm saw (its sum)
+ *   mean, rstd    from bakron_layernorm; mean NULL: the RMS norm
+ *   d_sum         device, T x d of dtype, the gradient that reaches those rows past the
+ *                 norm, or NULL
+ *   dx            device output, T x d of dtype, or NULL; may be d_sum with the same leading
+ *                 dimension
+ *   dweight, dbias  device outputs, d floats, or NULL.  T = 0 gives zeros
+ * 1 <= d <= 65536.  Workspace as above.
+ */
+bakron_status bakron_layernorm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx,
+                                        int32_t dtype, int64_t T, int64_t d, const float *weight,
+                                        const float *mean, const float *rstd, const void *d_sum,
+                                        int64_t ldds, void *dx, int64_t lddx, float *dweight,
+                                        float *dbias, void *work, size_t *work_bytes,
+                                        hipStream_t stream);
+
+/*
+ * bakron_embedding -- rows of a table: y_t = scale * table[tokens_t], rounded once.  A token
+ * outside [0, V) asks for nothing: zeros.
+ *   tokens  device, T token numbers
+ *   table   device, V x d of dtype (bakron_dtype)
+ *   y       device output, T x d of dtype
+ * T <= 2^20, 1 <= V <= 2^20, 1 <= d <= 65536; T ceil(d / 8192) (fp32: 4096) <= 2^23 (or
+ * BAKRON_EINVAL).  One launch.
+ */
+bakron_status bakron_embedding(const int64_t *tokens, int64_t T, const void *table, int64_t ldt,
+                               int32_t dtype, int64_t V, int64_t d, float scale, void *y,
+                               int64_t ldy, hipStream_t stream);
+
+/*
+ * bakron_embedding_backward -- the table's gradient:
+ *   dtable_v = base_v + scale * sum_{t: tokens_t = v} dy_t
+ * The sums run in fp32 over rising t and are rounded once.  Rows without a token are base, or zeros.
+ *   dy      device, T x d of dtype
+ *   base    device, V x d of dtype, or NULL for 0: e.g. the gradient of the same matrix at the
+ *           other end of the network
+ *   dtable  device output, V x d of dtype; may be base with the same leading dimension
+ * Sizes as bakron_embedding.  Workspace as above.
+ */
+bakron_status bakron_embedding_backward(const void *dy, int64_t lddy, const int64_t *tokens,
+                                        int64_t T, int32_t dtype, int64_t V, int64_t d,
+                                        float scale, const void *base, int64_t ldb, void *dtable,
+                                        int64_t ldo, void *work, size_t *work_bytes,
+                                        hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

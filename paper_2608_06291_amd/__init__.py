@@ -12,4 +12,6 @@ from ._lib import (BAKRON_EHIP, BAKRON_EINVAL, BAKRON_ENOMEM, BAKRON_ENOTSPD, BA
                    status_string,
                    MlpFeatures, NormQuant, PackedCodes, TokenLogprobs, gated_mlp,
                    gated_mlp_backward, linear, pack_codes, rmsnorm_quant, token_logprobs,
-                   token_logprobs_backward)
+                   token_logprobs_backward,
+                   LayerNorm, embedding, embedding_backward, head_logprobs, head_logprobs_backward,
+                   layernorm, layernorm_backward)

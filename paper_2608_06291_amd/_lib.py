@@ -25,7 +25,9 @@ EXPORTED = ("bakron_factor", "bakron_solve", "bakron_solve_debug", "bakron_facto
             "bakron_mse_scales", "bakron_factor_blockdiag", "bakron_quadform_weights",
             "bakron_kron_factors_iter", "bakron_mlp_local_factors_iter", "bakron_solve_noalloc",
             "bakron_rmsnorm_quant", "bakron_pack_codes", "bakron_linear", "bakron_gated_mlp",
-            "bakron_gated_mlp_backward", "bakron_token_logprobs", "bakron_token_logprobs_backward")
+            "bakron_gated_mlp_backward", "bakron_token_logprobs", "bakron_token_logprobs_backward",
+            "bakron_head_logprobs", "bakron_head_logprobs_backward", "bakron_layernorm",
+            "bakron_layernorm_backward", "bakron_embedding", "bakron_embedding_backward")
 
 ALPHABETS = {"sym": 0, "asym": 1}
 
@@ -132,7 +134,17 @@ def load(path: str = LIB_PATH):
             ("bakron_token_logprobs", [vp, i64, i32, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp, szp,
                                        vp]),
             ("bakron_token_logprobs_backward", [vp, i64, i32, i64, i64, vp, vp, vp, vp, vp, vp, i64,
-                                                vp])):
+                                                vp]),
+            ("bakron_head_logprobs", [vp, i64, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp, vp, szp, vp]),
+            ("bakron_head_logprobs_backward", [vp, i64, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp, vp, vp,
+                                               i64, vp, i64, vp, szp, vp]),
+            ("bakron_layernorm", [vp, i64, vp, i64, i32, i64, i64, vp, vp, f32, i32, vp, i64, vp, i64, vp, vp,
+                                  vp]),
+            ("bakron_layernorm_backward", [vp, i64, vp, i64, i32, i64, i64, vp, vp, vp, vp, i64, vp, i64, vp,
+                                           vp, vp, szp, vp]),
+            ("bakron_embedding", [vp, i64, vp, i64, i32, i64, i64, f32, vp, i64, vp]),
+            ("bakron_embedding_backward", [vp, i64, vp, i64, i32, i64, i64, f32, vp, i64, vp, i64, vp, szp,
+                                           vp])):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = args
     _lib = lib
@@ -933,4 +945,151 @@ def token_logprobs_backward(logits, target, lse, entropy=None, g_logprob=None, g
          (zp, ld, _dtype_code(logits.dtype), T, V, _vector(target, "target", T, torch.int64, dev),
           _vector(lse, "lse", T, f32, dev), _vector(entropy, "entropy", T, f32, dev),
           _vector(g_logprob, "g_logprob", T, f32, dev), _vector(g_entropy, "g_entropy", T, f32, dev), dp, ldd), dev)
+    return out
+
+
+# ---------------------------------------------------------------- the ends of the network and its norms
+def _head_operands(x, w):
+    xp, ldx = _rows_of(x, "x")
+    T, d = x.shape
+    wp, ldw = _rows_of(w, "w", None, x.dtype, x.device)
+    V = w.shape[0]
+    if w.shape[1] != d:
+        raise ValueError(f"w must have rows of {d} entries, got {tuple(w.shape)}")
+    return xp, ldx, T, d, wp, ldw, V, _dtype_code(x.dtype)
+
+
+def head_logprobs(x, w, target=None, work=None) -> TokenLogprobs:
+    """bakron_head_logprobs on the current stream: what token_logprobs gives for the logits x w^T,
+    which are never kept.  x: T x d fp16 or bf16 (the rows before the vocabulary matrix); w: V x d, the same
+    type; target: T int64 (outside [0, V): ignored, 0) or None.  Records no autograd graph: the
+    gradients come from head_logprobs_backward."""
+    torch = _torch or _import_torch()
+    lib = load()
+    _no_graph("head_logprobs", " and take the gradients from head_logprobs_backward", x, w)
+    xp, ldx, T, d, wp, ldw, V, code = _head_operands(x, w)
+    tp = _vector(target, "target", T, torch.int64, x.device)
+    logprob, entropy, lse = torch.empty(3, T, dtype=torch.float32, device=x.device).unbind(0)
+    _run_op(lib.bakron_head_logprobs,
+            (xp, ldx, T, d, wp, ldw, V, code, tp, None if tp is None else logprob.data_ptr(), entropy.data_ptr(),
+             lse.data_ptr()), x.device, work, maybe_none=False)
+    return TokenLogprobs(None if tp is None else logprob, entropy, lse)
+
+
+def head_logprobs_backward(x, w, target, lse, entropy=None, g_logprob=None, g_entropy=None, need_dx: bool = True,
+                           need_dw: bool = True, work=None):
+    """bakron_head_logprobs_backward: (dx, dw) from the gradients with respect to head_logprobs' logprob and
+    entropy (None for 0); None for what is not needed."""
+    torch = _torch or _import_torch()
+    lib = load()
+    xp, ldx, T, d, wp, ldw, V, code = _head_operands(x, w)
+    dev, f32 = x.device, torch.float32
+    dx = torch.empty(T, d, dtype=x.dtype, device=dev) if need_dx else None
+    dw = torch.empty(V, d, dtype=x.dtype, device=dev) if need_dw else None
+    _run_op(lib.bakron_head_logprobs_backward,
+            (xp, ldx, T, d, wp, ldw, V, code, _vector(target, "target", T, torch.int64, dev),
+             _vector(lse, "lse", T, f32, dev), _vector(entropy, "entropy", T, f32, dev),
+             _vector(g_logprob, "g_logprob", T, f32, dev), _vector(g_entropy, "g_entropy", T, f32, dev),
+             None if dx is None else dx.data_ptr(), d, None if dw is None else dw.data_ptr(), d), dev, work,
+            maybe_none=False)
+    return dx, dw
+
+
+class LayerNorm(NamedTuple):
+    """What layernorm returns: the normalised rows, their statistics (mean None for the RMS norm), and
+    x + residual where there is a residual."""
+    y: object
+    mean: object
+    rstd: object
+    sum: object = None
+
+
+def layernorm(x, weight=None, bias=None, residual=None, eps: float = 1e-5, centre: bool = True,
+              sum_out=None) -> LayerNorm:
+    """bakron_layernorm on the current stream: h = x + residual (rounded once), y = weight * (h - mean) /
+    sqrt(var + eps) + bias; centre=False: the RMS norm, mean 0.  x: T x d fp32, fp16 or bf16; weight, bias:
+    d fp32.  sum_out (e.g. residual itself) receives h.  Records no autograd graph: the gradients come from
+    layernorm_backward."""
+    torch = _torch or _import_torch()
+    lib = load()
+    _no_graph("layernorm", " and take the gradients from layernorm_backward", x, weight, bias, residual)
+    xp, ldx = _rows_of(x, "x")
+    T, d = x.shape
+    dev, dt = x.device, x.dtype
+    rp, ldr = _rows_of(residual, "residual", (T, d), dt, dev) if residual is not None else (None, d)
+    if sum_out is None and residual is not None:
+        sum_out = torch.empty(T, d, dtype=dt, device=dev)
+    sp, lds = _rows_of(sum_out, "sum_out", (T, d), dt, dev) if sum_out is not None else (None, d)
+    y = torch.empty(T, d, dtype=dt, device=dev)
+    mean = torch.empty(T, dtype=torch.float32, device=dev) if centre else None
+    rstd = torch.empty(T, dtype=torch.float32, device=dev)
+    _run(lib.bakron_layernorm,
+         (xp, ldx, rp, ldr, _dtype_code(dt), T, d, _vector(weight, "weight", d, torch.float32, dev),
+          _vector(bias, "bias", d, torch.float32, dev), float(eps), int(bool(centre)), sp, lds, y.data_ptr(), d,
+          None if mean is None else mean.data_ptr(), rstd.data_ptr()), dev)
+    return LayerNorm(y, mean, rstd, sum_out)
+
+
+def layernorm_backward(dy, x, weight, mean, rstd, d_sum=None, need_dx: bool = True, need_dweight: bool = True,
+                       need_dbias: bool = True, work=None):
+    """bakron_layernorm_backward: (dx, dweight, dbias) from dy, the gradient with respect to layernorm's y; None
+    for what is not needed.  x: the rows that the norm saw (layernorm's sum where there was a
+    residual); mean (None: the RMS norm), rstd: from layernorm; d_sum: the gradient that reaches those rows
+    past the norm, added to dx.  dweight and dbias: d fp32."""
+    torch = _torch or _import_torch()
+    lib = load()
+    xp, ldx = _rows_of(x, "x")
+    T, d = x.shape
+    dev, dt, f32 = x.device, x.dtype, torch.float32
+    gp, ldg = _rows_of(dy, "dy", (T, d), dt, dev)
+    sp, lds = _rows_of(d_sum, "d_sum", (T, d), dt, dev) if d_sum is not None else (None, d)
+    dx = torch.empty(T, d, dtype=dt, device=dev) if need_dx else None
+    dw = torch.empty(d, dtype=f32, device=dev) if need_dweight else None
+    db = torch.empty(d, dtype=f32, device=dev) if need_dbias else None
+    _run_op(lib.bakron_layernorm_backward,
+            (gp, ldg, xp, ldx, _dtype_code(dt), T, d, _vector(weight, "weight", d, f32, dev),
+             _vector(mean, "mean", T, f32, dev), _vector(rstd, "rstd", T, f32, dev), sp, lds,
+             None if dx is None else dx.data_ptr(), d, None if dw is None else dw.data_ptr(),
+             None if db is None else db.data_ptr()), dev, work,
+            ("layernorm_backward", T, d, dt, need_dx, need_dweight or need_dbias))
+    return dx, dw, db
+
+
+def embedding(tokens, table, scale: float = 1.0, out=None):
+    """bakron_embedding on the current stream: rows of table (V x d fp32, fp16 or bf16) for tokens (T int64;
+    outside [0, V): zeros), times scale, rounded once.  Records no autograd graph: the gradient comes
+    from embedding_backward."""
+    torch = _torch or _import_torch()
+    lib = load()
+    _no_graph("embedding", " and take the gradient from embedding_backward", table)
+    tp, ldt = _rows_of(table, "table")
+    V, d = table.shape
+    dev = table.device
+    if tokens.dim() != 1:
+        raise ValueError("tokens must have one dimension")
+    T = tokens.shape[0]
+    if out is None:
+        out = torch.empty(T, d, dtype=table.dtype, device=dev)
+    op, ldo = _rows_of(out, "out", (T, d), table.dtype, dev)
+    _run(lib.bakron_embedding, (_vector(tokens, "tokens", T, torch.int64, dev), T, tp, ldt, _dtype_code(table.dtype), V,
+                                d, float(scale), op, ldo), dev)
+    return out
+
+
+def embedding_backward(dy, tokens, rows: int, scale: float = 1.0, base=None, out=None, work=None):
+    """bakron_embedding_backward: the gradient of a table of `rows` rows from dy, the gradient with
+    respect to embedding's output, plus base (rows x d) where given, e.g. the same matrix's gradient at
+    the other end of the network; out may be base."""
+    torch = _torch or _import_torch()
+    lib = load()
+    gp, ldg = _rows_of(dy, "dy")
+    T, d = dy.shape
+    dev, dt, V = dy.device, dy.dtype, int(rows)
+    bp, ldb = _rows_of(base, "base", (V, d), dt, dev) if base is not None else (None, d)
+    if out is None:
+        out = torch.empty(V, d, dtype=dt, device=dev)
+    op, ldo = _rows_of(out, "out", (V, d), dt, dev)
+    _run_op(lib.bakron_embedding_backward,
+            (gp, ldg, _vector(tokens, "tokens", T, torch.int64, dev), T, _dtype_code(dt), V, d, float(scale), bp, ldb,
+             op, ldo), dev, work, ("embedding_backward", T, V, d, dt))
     return out

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["csrc/api.hip", "csrc/factor.hip", "csrc/solve.hip", "csrc/antidiag.hip",
            "csrc/hessian.hip", "csrc/quant.hip", "csrc/gptq.hip", "csrc/norm.hip", "csrc/linear.hip",
-           "csrc/mlp.hip", "csrc/logprob.hip"]
+           "csrc/mlp.hip", "csrc/logprob.hip", "csrc/head.hip", "csrc/layernorm.hip", "csrc/embedding.hip"]
 LIB = os.path.join(HERE, "libbakron.so")
 
 HIPCC_FLAGS = [

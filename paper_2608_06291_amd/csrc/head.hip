@@ -1,0 +1,678 @@
+// Log probabilities of given tokens from the rows before the vocabulary matrix, and their
+// gradient, without keeping the logits (16-bit floats, fp32 sums):
+//   z = x W^T,   lse = log sum exp z,   logprob = z_target - lse,   entropy = -sum p log p
+//   dz = g (1[target] - p) - g_H p (log p + entropy),   dx = dz W,   dW = dz^T x
+//
+// Forward: the tile product of tile.h with a softmax in its epilogue.  Every tile leaves, for each of its
+// rows of x, the largest logit m, s = sum exp(z - m) and s1 = sum exp(z - m) (z - m) over its part of the
+// vocabulary (16 bytes where the logits would take 4 bytes an entry); a second launch joins the parts.
+// Backward: the vocabulary goes in pieces.  Of a piece the logits are computed again, with dz in the
+// epilogue, rounded to 16 bits as operand of two products: dW of the piece, and dx, whose sums stay in
+// fp32 between the pieces.
+#include "product.h"
+
+namespace bk {
+
+// What a part of the vocabulary leaves of a row.
+struct HeadPart {
+    float m, s, s1, pad;
+};
+
+struct HeadArgs {
+    Operand x, w;
+    int64_t T;
+    int V;                     // rows of w (backward: of the piece)
+    int chunks, ni, nt;
+    const int64_t* target;
+    // forward
+    HeadPart* part;            // parts x T
+    float* at;                 // T: the target's logit, where there is one
+    // backward
+    const float *lse, *entropy, *g_logprob, *g_entropy;
+    int64_t v0, all;           // first token of the piece; tokens of all pieces
+    void* dz;                  // T rows: vp entries (zeros in the padding), then what their rounding took
+    int64_t vp, ldz;           // ldz: vp, or 2 vp with the rests
+    const float* factor;       // half precision: dz is taken times this
+};
+
+// What few rows need beside that: x and w as they are, in entries.
+struct HeadFew {
+    const void *x, *w;
+    int64_t ldx, ldw;
+    int d;
+};
+
+// Half precision: |dz| <= |g| + 4 |g_H| (p |log p + H| is below ln(V) / 4 + 1/2 <= 4 for V <= 2^20), so dz is taken
+// times the power of two that puts this bound at 2^13 to 2^14, undone at the end: none overflows, and
+// what is lost is below 2^-38 of the largest.
+struct HeadScale {
+    float factor, undo;
+};
+__global__ __launch_bounds__(1024) void k_head_scale(const float* __restrict__ g, const float* __restrict__ gh,
+                                                     int64_t T, HeadScale* out) {
+    __shared__ float red[16];
+    float m = 0.0f;
+    for (int64_t i = threadIdx.x; i < T; i += 1024) {
+        const float b = (g ? fabsf(g[i]) : 0.0f) + (gh ? 4.0f * fabsf(gh[i]) : 0.0f);
+        m = fmaxf(m, b < INFINITY ? b : 0.0f);
+    }
+    m = group_reduce(m, MaxNan(), red, threadIdx.x >> 6, threadIdx.x & 63, 16);
+    if (threadIdx.x != 0) return;
+    int e = 14;
+    if (m > 0.0f) frexpf(m, &e);   // m < 2^e
+    e = max(e, 14 - 126);          // (both powers are normal numbers)
+    *out = HeadScale{ldexpf(1.0f, 14 - e), ldexpf(1.0f, e - 14)};
+}
+
+// A row's part of the gradient.
+struct HeadRow {
+    float lse, g, gh, H;
+    int t;   // the target in the piece, or -1
+};
+__device__ inline HeadRow head_row(const HeadArgs& a, int64_t t) {
+    HeadRow r;
+    r.lse = a.lse[t];
+    const bool empty = r.lse == -INFINITY;
+    if (empty) r.lse = INFINITY;   // every p is then exp(-inf) = 0
+    const int64_t k = a.target ? a.target[t] : -1;
+    r.t = k >= a.v0 && k < a.v0 + a.V ? (int)(k - a.v0) : -1;
+    r.g = k >= 0 && k < a.all && a.g_logprob ? a.g_logprob[t] : 0.0f;
+    r.gh = a.g_entropy ? a.g_entropy[t] : 0.0f;
+    r.H = a.g_entropy ? a.entropy[t] : 0.0f;
+    if (empty) r.g = r.gh = 0.0f;
+    return r;
+}
+__device__ inline float head_grad(const HeadRow& r, float z, int i) {
+    const float lp = max_nan(z - r.lse, -200.0f);   // (exp is 0 there; 0 * -inf stays out)
+    const float v = -exp_of<false>(lp) * fmaf(r.gh, lp + r.H, r.g);
+    return i == r.t ? v + r.g : v;
+}
+// N entries from token i of the piece on; zeros past its end.
+template <typename E, int N>
+__device__ inline void head_store(const HeadArgs& a, const HeadRow& r, int64_t t, int i, float factor, float (&z)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        z[j] = i + j < a.V ? head_grad(r, z[j], i + j) : 0.0f;
+        if constexpr (narrow_range<E>) z[j] *= factor;
+    }
+    E* const row = static_cast<E*>(a.dz) + t * a.ldz + i;
+    store_n(row, z, N);
+    if (a.ldz > a.vp) {   // what the rounding took (nothing beside what is not finite)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float v = (float)(E)z[j];
+            z[j] = __builtin_isfinite(v) ? z[j] - v : 0.0f;
+        }
+        store_n(row + a.vp, z, N);
+    }
+}
+
+// Joins b to a.
+__device__ inline void head_join(HeadPart& a, const HeadPart& b) {
+    const float m = max_nan(a.m, b.m), ms = m == -INFINITY ? 0.0f : m;
+    const float da = max_nan(a.m - ms, -200.0f), db = max_nan(b.m - ms, -200.0f);
+    const float ea = exp_of<true>(da), eb = exp_of<true>(db);
+    a.s1 = fmaf(da, a.s, a.s1) * ea + fmaf(db, b.s, b.s1) * eb;
+    a.s = a.s * ea + b.s * eb;
+    a.m = m;
+}
+// Over lanes 16 and 32 apart: those that hold the same row of x.
+template <typename Op>
+__device__ inline float rows_reduce(float v, Op op) {
+    v = op(v, __shfl_xor(v, 16));
+    return op(v, __shfl_xor(v, 32));
+}
+// The part of one row that the four lanes of it hold, N logits each.
+template <int N>
+__device__ inline HeadPart head_part(const float (&z)[N]) {
+    float m = z[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) m = max_nan(m, z[j]);
+    m = rows_reduce(m, MaxNan());
+    const float ms = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float d = max_nan(z[j] - ms, -200.0f);   // (0 * -inf stays out of s1; exp is 0 there)
+        const float e = __builtin_amdgcn_exp2f(d * LOG2E);
+        s += e;
+        s1 = fmaf(e, d, s1);
+    }
+    return HeadPart{m, rows_reduce(s, Add()), rows_reduce(s1, Add()), 0.0f};
+}
+
+template <typename Tl, bool BWD>
+__global__ __launch_bounds__(Tl::THREADS) void k_head(HeadArgs a) {
+    typedef typename Tl::Mma::Elem E;
+    __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+    int ti, tt;
+    tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
+    const int i0 = ti * Tl::ROWS;
+    const int64_t t0 = (int64_t)tt * Tl::COLS;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    typename Tl::Accs acc = {};
+    Tl::run(lds, a.w, min(i0, a.V - 1), a.x, t0, 0, a.chunks, acc, [](int r) { return r; });
+
+    if constexpr (!BWD) {
+        constexpr int PART = Tl::UA * 16, WAVES_A = Tl::ROWS / PART;   // a wave's tokens; waves with the same rows
+        HeadPart* const parts = reinterpret_cast<HeadPart*>(lds);      // WAVES_A x COLS
+        const int r16 = lane & 15, first = i0 + Tl::a0(wave) + (lane >> 4) * 4;
+#pragma unroll
+        for (int y = 0; y < Tl::UB; ++y) {
+            float z[Tl::UA * 4];
+#pragma unroll
+            for (int x = 0; x < Tl::UA; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) z[x * 4 + r] = Tl::at(acc, x, y)[r];
+            if (i0 + Tl::ROWS > a.V) {
+#pragma unroll
+                for (int j = 0; j < Tl::UA * 4; ++j)
+                    if (first + j / 4 * 16 + j % 4 >= a.V) z[j] = -INFINITY;
+            }
+            const int col = Tl::b0(wave) + y * 16 + r16;
+            const HeadPart p = head_part(z);
+            if (lane < 16) parts[Tl::a0(wave) / PART * Tl::COLS + col] = p;
+            const int64_t t = t0 + col, k = a.target && t < a.T ? a.target[t] : -1;
+            const int64_t in = k < a.V ? k - first : -1;   // of this lane's 16 x UA tokens: 16 x + r
+            if (__any(in >= 0 && in < PART)) {
+#pragma unroll
+                for (int j = 0; j < Tl::UA * 4; ++j)
+                    if (in == j / 4 * 16 + j % 4) a.at[t] = z[j];
+            }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < Tl::COLS; c += Tl::THREADS) {
+            if (t0 + c >= a.T) break;
+            HeadPart p = parts[c];
+#pragma unroll
+            for (int w = 1; w < WAVES_A; ++w) head_join(p, parts[w * Tl::COLS + c]);
+            a.part[(int64_t)ti * a.T + t0 + c] = p;
+        }
+    } else {
+        HeadRow* const row = reinterpret_cast<HeadRow*>(lds + Tl::THREADS / 64 * (Tl::UA * 1024));
+        for (int c = threadIdx.x; c < Tl::COLS; c += Tl::THREADS)
+            if (t0 + c < a.T) row[c] = head_row(a, t0 + c);
+        __syncthreads();
+        const float factor = narrow_range<E> ? *a.factor : 1.0f;
+        const auto rows = handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
+        constexpr int PER = Tl::UA * 2, EACH = 64 / PER;   // lanes a row, rows at a time
+        const int p = lane % PER, i = i0 + Tl::a0(wave) + p * 8;
+#pragma unroll
+        for (int y = 0; y < Tl::UB; ++y) {
+            rows.put(y);
+#pragma unroll
+            for (int k = 0; k < 16 / EACH; ++k) {
+                const int tl = k * EACH + lane / PER, col = Tl::b0(wave) + y * 16 + tl;
+                float z[8];
+                rows.take(tl, p, z);
+                if (t0 + col < a.T && i < a.vp) head_store<E>(a, row[col], t0 + col, i, factor, z);
+            }
+        }
+    }
+}
+
+constexpr int HEAD_STEPS = 2;
+
+// Few rows (a decoding step): bound by reading w once.  A workgroup takes R units of 16 tokens and Y of 16
+// rows of x; its waves share the summed axis, blocks of two steps of 32 in turn, every
+// fragment straight from memory (at any alignment) into registers, BLOCKS blocks asked for at once.  The partial
+// sums meet in LDS.  SHIFT: see FewPiece.
+template <typename M, bool BWD, int R, int Y, int BLOCKS, bool SHIFT>
+__global__ __launch_bounds__(512) void k_head_few(HeadFew f, HeadArgs a) {
+    typedef typename M::Elem E;
+    extern __shared__ __attribute__((aligned(16))) char few_lds[];
+    const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, kq = lane >> 4;
+    const int i0 = (int)blockIdx.x * (R * 16);
+    const int64_t t0 = (int64_t)blockIdx.y * (Y * 16);
+    const E* w[R];
+    const E* x[Y];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        w[r] = static_cast<const E*>(f.w) + (int64_t)min(i0 + r * 16 + r16, a.V - 1) * f.ldw + kq * 8;
+#pragma unroll
+    for (int y = 0; y < Y; ++y)
+        x[y] = static_cast<const E*>(f.x) + min(t0 + y * 16 + r16, a.T - 1) * f.ldx + kq * 8;
+    constexpr int U = HEAD_STEPS;
+    const int nblocks = f.d / (32 * U), nsteps = f.d / 32;   // what is left goes one step a wave
+
+    struct Block {
+        FewPiece<SHIFT> w[U][R], x[U][Y];
+    };
+    auto load = [&](Block& b, int k) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < U; ++i) b.w[i][r].load(w[r] + k + i * 32);
+#pragma unroll
+        for (int y = 0; y < Y; ++y)
+#pragma unroll
+            for (int i = 0; i < U; ++i) b.x[i][y].load(x[y] + k + i * 32);
+    };
+    f32x4 acc[R][Y] = {};
+    auto add = [&](const u32x4 (&u)[R], const u32x4 (&v)[Y]) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int y = 0; y < Y; ++y)
+                acc[r][y] = M::mma(__builtin_bit_cast(i32x4, u[r]), __builtin_bit_cast(i32x4, v[y]), acc[r][y]);
+    };
+    for (int c = wave; c < nblocks; c += waves * BLOCKS) {
+        Block b[BLOCKS];
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k)
+            if (c + k * waves < nblocks) load(b[k], (c + k * waves) * (32 * U));
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k) {
+            if (c + k * waves >= nblocks) break;
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                u32x4 u[R], v[Y];
+#pragma unroll
+                for (int r = 0; r < R; ++r) u[r] = b[k].w[i][r].get(w[r]);
+#pragma unroll
+                for (int y = 0; y < Y; ++y) v[y] = b[k].x[i][y].get(x[y]);
+                add(u, v);
+            }
+        }
+    }
+    for (int s = nblocks * U + wave; s < nsteps; s += waves) {
+        u32x4 u[R], v[Y];
+#pragma unroll
+        for (int r = 0; r < R; ++r) u[r] = load_words(w[r] + s * 32);
+#pragma unroll
+        for (int y = 0; y < Y; ++y) v[y] = load_words(x[y] + s * 32);
+        add(u, v);
+    }
+    if (f.d % 32 != 0 && wave == (nsteps - nblocks * U) % waves) {
+        const int k = nsteps * 32, left = f.d - k - kq * 8;   // entries of this lane's pieces
+        u32x4 u[R], v[Y];
+#pragma unroll
+        for (int r = 0; r < R; ++r) u[r] = few_part(w[r] + k, left, f.d);
+#pragma unroll
+        for (int y = 0; y < Y; ++y) v[y] = few_part(x[y] + k, left, f.d);
+        add(u, v);
+    }
+#pragma unroll
+    for (int y = 0; y < Y; ++y)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            *reinterpret_cast<f32x4*>(few_lds + (((wave * Y + y) * R + r) * 64 + lane) * 16) = acc[r][y];
+    __syncthreads();
+    for (int y = wave; y < Y; y += waves) {   // a wave joins one unit of rows
+        float z[R * 4];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < waves; ++k)
+                sum += *reinterpret_cast<const f32x4*>(few_lds + (((k * Y + y) * R + r) * 64 + lane) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[r * 4 + j] = sum[j];
+        }
+        const int64_t t = t0 + y * 16 + r16;
+        const int first = i0 + kq * 4;
+        if constexpr (!BWD) {
+            const int64_t k = a.target && t < a.T ? a.target[t] : -1;
+#pragma unroll
+            for (int j = 0; j < R * 4; ++j) {
+                const int i = first + j / 4 * 16 + j % 4;
+                if (i >= a.V) z[j] = -INFINITY;
+                if (i == k && i < a.V) a.at[t] = z[j];
+            }
+            const HeadPart p = head_part(z);
+            if (lane < 16 && t < a.T) a.part[(int64_t)blockIdx.x * a.T + t] = p;
+        } else if (t < a.T) {
+            const HeadRow row = head_row(a, t);
+            const float factor = narrow_range<E> ? *a.factor : 1.0f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = z[r * 4 + j];
+                if (first + r * 16 < a.vp) head_store<E>(a, row, t, first + r * 16, factor, v);
+            }
+        }
+    }
+}
+
+// Joins the parts of the vocabulary: 256 / ROWS threads a row.
+struct HeadJoinArgs {
+    const HeadPart* part;
+    const float* at;
+    const int64_t* target;
+    int64_t T;
+    int V, parts;
+    float *logprob, *entropy, *lse;
+};
+template <int ROWS>
+__global__ __launch_bounds__(256) void k_head_join(HeadJoinArgs a) {
+    constexpr int PER = 256 / ROWS;
+    __shared__ HeadPart red[PER][ROWS];
+    const int c = threadIdx.x % ROWS, l = threadIdx.x / ROWS;
+    const int64_t t = (int64_t)blockIdx.x * ROWS + c, tr = min(t, a.T - 1);
+    HeadPart p{-INFINITY, 0.0f, 0.0f, 0.0f};
+    constexpr int AHEAD = 4;
+    for (int k = l; k < a.parts; k += PER * AHEAD) {
+        HeadPart q[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) q[j] = a.part[(int64_t)min(k + j * PER, a.parts - 1) * a.T + tr];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (k + j * PER < a.parts) head_join(p, q[j]);
+    }
+    red[l][c] = p;
+    for (int n = PER / 2; n > 0; n /= 2) {
+        __syncthreads();
+        if (l < n) head_join(red[l][c], red[l + n][c]);
+    }
+    if (l != 0 || t >= a.T) return;
+    p = red[0][c];
+    const bool empty = p.m == -INFINITY;
+    const float log_s = logf(p.s);
+    const int64_t k = a.target ? a.target[t] : -1;
+    const bool asked = k >= 0 && k < a.V;
+    if (a.lse) a.lse[t] = empty ? -INFINITY : p.m + log_s;
+    if (a.logprob) a.logprob[t] = !asked ? 0.0f : empty ? -INFINITY : (a.at[t] - p.m) - log_s;
+    if (a.entropy) a.entropy[t] = empty ? 0.0f : log_s - p.s1 / p.s;
+}
+
+// Rows up to which the product is taken as one of few rows; and with few tiles (by 64 x 64) a CU and a
+// long way to sum.
+constexpr int64_t HEAD_FEW_ROWS = 32, HEAD_FEW_TILES = 4;
+constexpr int HEAD_UNITS = 2;   // of 16 tokens a workgroup of that kernel
+
+static bool head_few_rows(int64_t T, int64_t V, int64_t d) {
+    if (T <= HEAD_FEW_ROWS) return true;
+    return ((V + 63) / 64) * ((T + 63) / 64) * HEAD_FEW_TILES <= op_cus() && d >= 512;
+}
+// Tokens that a workgroup takes, and so the parts of the vocabulary.
+static int head_edge(int64_t T, int64_t V, int64_t d) {
+    return head_few_rows(T, V, d) ? 16 * HEAD_UNITS : pick_tile(V, T, op_cus(), true);
+}
+
+template <typename M, bool BWD, int Y, int BLOCKS>
+static void launch_head_few(const HeadFew& f, const HeadArgs& a, hipStream_t st) {
+    constexpr int R = HEAD_UNITS;
+    // Words around the pieces of odd rows: each matrix begins on a word, and whole steps end before the row
+    // does, so an entry before and one behind each piece are in the matrix.
+    const bool shift = (f.ldx % 2 != 0 || f.ldw % 2 != 0) && f.d % 32 != 0 && (uintptr_t)f.x % 4 == 0 &&
+                       (uintptr_t)f.w % 4 == 0;
+    const int64_t n = BWD ? a.vp : a.V;
+    const dim3 grid((unsigned)((n + R * 16 - 1) / (R * 16)), (unsigned)((a.T + Y * 16 - 1) / (Y * 16)));
+    const int blocks = f.d / (32 * HEAD_STEPS);   // as many waves as have work, 8 at most
+    const int waves = blocks >= 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
+    if (shift)
+        hipLaunchKernelGGL((k_head_few<M, BWD, R, Y, 2, true>), grid, dim3(64 * waves), waves * Y * R * 1024, st, f, a);
+    else
+        hipLaunchKernelGGL((k_head_few<M, BWD, R, Y, BLOCKS, false>), grid, dim3(64 * waves), waves * Y * R * 1024, st,
+                           f, a);
+}
+
+// edge: head_edge of the call
+template <typename M, bool BWD>
+static void launch_head(const HeadFew& few, HeadArgs a, int edge, hipStream_t st) {
+    if (edge == 16 * HEAD_UNITS)
+        return a.T <= 16 ? launch_head_few<M, BWD, 1, 4>(few, a, st) : launch_head_few<M, BWD, 2, 2>(few, a, st);
+    const int64_t n = BWD ? a.vp : a.V;   // (the padding is written, too)
+    auto go = [&](auto tile) {
+        typedef decltype(tile) Tl;
+        a.ni = (int)((n + Tl::ROWS - 1) / Tl::ROWS);
+        a.nt = (int)((a.T + Tl::COLS - 1) / Tl::COLS);
+        hipLaunchKernelGGL((k_head<Tl, BWD>), dim3((unsigned)(a.ni * a.nt)), dim3(Tl::THREADS), 0, st, a);
+    };
+    if (edge == 256) return go(BigTile<M>());
+    if (edge == 128 && one_a_cu(128, n, a.T)) return go(Tile<M, 128, 128, 2, 4, 3>());
+    if (edge == 128) return go(Tile<M, 128, 128, 2, 4, 2>());
+    return go(Tile<M, 64, 64, 2, 2, 4>());
+}
+
+// x and w as operands, through padded copies where they cannot be staged as they are.
+struct HeadPad {
+    bool x, w;
+    int64_t dp;
+    size_t xbytes, wbytes;
+};
+static HeadPad head_pad(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t T, int64_t d, int64_t V,
+                        bool need_x, bool need_w) {
+    HeadPad p;
+    p.dp = (d + 63) / 64 * 64;
+    p.x = need_x && !direct_rows(x, ldx, d);
+    p.w = need_w && !direct_rows(w, ldw, d);
+    p.xbytes = p.x ? up256((size_t)T * p.dp * 2) : 0;
+    p.wbytes = p.w ? up256((size_t)V * p.dp * 2) : 0;
+    return p;
+}
+static void head_operands(HeadArgs& a, const HeadPad& p, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                          int64_t d, char* work, hipStream_t st) {
+    // (a copy's padding is zeros; without copies what lies past d reads as zeros)
+    const int64_t kbytes = p.x && p.w ? 2 * p.dp : 2 * ((d + 7) / 8 * 8);
+    a.x = operand(x, 2 * ldx, a.T, kbytes);
+    a.w = operand(w, 2 * ldw, a.V, kbytes);
+    a.chunks = (int)((kbytes + CHUNK_BYTES - 1) / CHUNK_BYTES);
+    PadArgs c{};
+    int n = 0;
+    int64_t pieces = 0;
+    auto copy = [&](const void* src, int64_t ld, int64_t rows, char* to) {
+        c.src[n] = static_cast<const uint16_t*>(src);
+        c.dst[n] = reinterpret_cast<uint16_t*>(to);
+        c.ld[n] = ld;
+        pieces += rows * (p.dp / 8);
+        for (int i = n; i < 3; ++i) c.end[i] = pieces;
+        ++n;
+    };
+    if (p.x) {
+        copy(x, ldx, a.T, work);
+        a.x = operand(work, 2 * p.dp, a.T, kbytes);
+    }
+    if (p.w) {
+        copy(w, ldw, a.V, work + p.xbytes);
+        a.w = operand(work + p.xbytes, 2 * p.dp, a.V, kbytes);
+    }
+    if (n == 0) return;
+    c.cols = d;
+    c.cols_p = p.dp;
+    hipLaunchKernelGGL(k_pad_rows, stride_grid(pieces), dim3(256), 0, st, c);
+}
+
+// The backward pass.  A piece of the vocabulary is as long as dz of it stays in the last-level cache (256 MB) with
+// the operands beside it.  As many tokens as there are in up to one chunk of rows do not average dz's
+// rounding out, so there the products go on over its rests, too.
+constexpr int64_t HEAD_PIECE_BYTES = (int64_t)128 << 20;
+struct HeadBackward {
+    int64_t vc, vp, ldz;   // tokens of a piece (all but the last), padded; row of dz
+    bool rests;
+    ProdPlan dx, dw;
+    size_t dz, partial, sums, scale;
+};
+static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bool dx, bool dw, int ncu) {
+    HeadBackward p{};
+    p.rests = T <= 64;
+    const int64_t most = std::max<int64_t>(HEAD_PIECE_BYTES / (T * (p.rests ? 4 : 2)) / 256, 1) * 256;
+    const int64_t pieces = (V + most - 1) / most;
+    p.vc = pieces == 1 ? V : ((V + pieces - 1) / pieces + 255) / 256 * 256;
+    p.vp = (p.vc + 63) / 64 * 64;
+    p.ldz = (p.rests ? 2 : 1) * p.vp;
+    p.dz = up256((size_t)T * p.ldz * 2);
+    if (dx) p.dx = prod_plan(d, T, (int)(p.ldz / 64), ncu);
+    if (dw) p.dw = prod_plan(d, p.vp, (int)((p.rests ? 2 : 1) * ((T + 63) / 64)), ncu);
+    p.partial = std::max(p.dx.bytes, p.dw.bytes);
+    p.sums = dx && p.vc < V ? up256((size_t)T * ((d + 7) / 8 * 8) * sizeof(float)) : 0;
+    p.scale = half ? 256 : 0;
+    return p;
+}
+
+template <typename M>
+static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, int64_t d, int64_t V, int edge,
+                              void* dx, int64_t lddx, void* dw, int64_t lddw, HeadScale* scale, void* partial,
+                              float* sums, hipStream_t st) {
+    typedef typename M::Elem E;
+    constexpr bool HALF = narrow_range<E>;
+    if (HALF) {
+        hipLaunchKernelGGL(k_head_scale, dim3(1), dim3(1024), 0, st, a.g_logprob, a.g_entropy, a.T, scale);
+        a.factor = &scale->factor;
+    }
+    const Operand w = a.w;
+    a.all = V;
+    const char* const few_w = static_cast<const char*>(few.w);
+    const int64_t cols = (d + 7) / 8 * 8;   // (of x and w, as they are or padded)
+    for (a.v0 = 0; a.v0 < V; a.v0 += p.vc) {
+        a.V = (int)std::min(p.vc, V - a.v0);
+        a.vp = ((int64_t)a.V + 63) / 64 * 64;   // (p.vp but for the last piece)
+        a.ldz = (p.rests ? 2 : 1) * a.vp;
+        a.w.base = w.base + a.v0 * w.ld;
+        a.w.n = a.V;
+        few.w = few_w + 2 * a.v0 * few.ldw;
+        launch_head<M, true>(few, a, edge, st);
+        ProdArgs g{};
+        g.undo = HALF ? &scale->undo : nullptr;
+        g.d = d;
+        if (dx) {
+            g.a = operand(a.w.base, w.ld, cols, a.V);
+            g.chunks = (int)(a.ldz / 64);
+            if (p.rests) {   // the same w again, beside the rests
+                g.a.base2 = g.a.base;
+                g.a.split = g.chunks / 2;
+            }
+            g.b = operand(a.dz, 2 * a.ldz, a.T, (int64_t)g.chunks * CHUNK_BYTES);
+            g.out = dx;
+            g.ldo = lddx;
+            g.split = g.split2 = g.end = a.T;
+            g.sums = sums;
+            g.first = a.v0 == 0;
+            g.last = a.v0 + a.V == V;
+            ProdPlan plan = p.dx;
+            if (a.vp != p.vp) {   // the last piece is shorter: no more parts than it has, none empty
+                plan.part_chunks = std::max(plan.part_chunks, 1);
+                plan.parts = std::min(plan.parts, (g.chunks + plan.part_chunks - 1) / plan.part_chunks);
+                if (plan.parts == 1) plan.part_chunks = g.chunks;
+            }
+            if (p.vc < V)
+                launch_prod<M, true, false, true>(g, plan, partial, st);
+            else
+                launch_prod<M, true, false>(g, plan, partial, st);
+        }
+        if (dw) {
+            g.a = operand(a.x.base, a.x.ld, cols, a.T);
+            g.b = operand(a.dz, 2 * a.ldz, a.vp, a.T);
+            g.chunks = (int)((a.T + 63) / 64);
+            if (p.rests) {
+                g.a.split = g.b.split = g.chunks;
+                g.a.base2 = g.a.base;
+                g.b.base2 = g.b.base + 2 * a.vp;
+                g.chunks *= 2;
+            }
+            g.out = static_cast<E*>(dw) + a.v0 * lddw;
+            g.ldo = lddw;
+            g.split = g.split2 = g.end = a.V;
+            launch_prod<M, true, true>(g, p.dw, partial, st);
+        }
+    }
+}
+
+}  // namespace bk
+
+static bakron_status head_sizes(const char* who, int64_t ldx, int64_t T, int64_t d, int64_t ldw, int64_t V,
+                                int32_t dtype) {
+    if (T < 0 || T > bk::OP_T_MAX || d < 1 || V < 1 || d > ((int64_t)1 << 17) || V > ((int64_t)1 << 20))
+        return bk::op_fail(who, "bad size");
+    if (ldx < d || ldw < d) return bk::op_fail(who, "leading dimension below d");
+    if (dtype != BAKRON_F16 && dtype != BAKRON_BF16) return bk::op_fail(who, "dtype must be 16-bit");
+    // (the widest launches: 64 x 64 blocks of 256 threads)
+    if ((T + 63) / 64 * ((std::max(d, V) + 63) / 64) > ((int64_t)1 << 23) - 1)
+        return bk::op_fail(who, "too many rows for one call");
+    return BAKRON_OK;
+}
+
+extern "C" bakron_status bakron_head_logprobs(const void* x, int64_t ldx, int64_t T, int64_t d, const void* w,
+                                              int64_t ldw, int64_t V, int32_t dtype, const int64_t* target,
+                                              float* logprob, float* entropy, float* lse, void* work,
+                                              size_t* work_bytes, hipStream_t stream) {
+    static const char who[] = "bakron_head_logprobs";
+    bk::set_last_error("");
+    bakron_status st = head_sizes(who, ldx, T, d, ldw, V, dtype);
+    if (st != BAKRON_OK) return st;
+    const int edge = bk::head_edge(T, V, d), parts = (int)((V + edge - 1) / edge);
+    const bool many = !bk::head_few_rows(T, V, d);
+    const bk::HeadPad p = bk::head_pad(x, ldx, w, ldw, T, d, V, many, many);
+    const size_t part = bk::up256((size_t)parts * T * sizeof(bk::HeadPart)), at = bk::up256((size_t)T * sizeof(float));
+    bool query;
+    st = bk::op_workspace(who, work, work_bytes, p.xbytes + p.wbytes + part + at, &query);
+    if (st != BAKRON_OK || query) return st;
+    if (logprob && !target) return bk::op_fail(who, "logprob needs targets");
+    if (T == 0) return BAKRON_OK;
+    if (!x || !w || (!logprob && !entropy && !lse)) return bk::op_fail(who, "null pointer");
+    char* const to = static_cast<char*>(work) + p.xbytes + p.wbytes;
+    bk::HeadArgs a{};
+    a.T = T;
+    a.V = (int)V;
+    a.target = logprob ? target : nullptr;
+    a.part = reinterpret_cast<bk::HeadPart*>(to);
+    a.at = reinterpret_cast<float*>(to + part);
+    bk::head_operands(a, p, x, ldx, w, ldw, d, static_cast<char*>(work), stream);
+    const bk::HeadFew few{x, w, ldx, ldw, (int)d};
+    if (dtype == BAKRON_BF16)
+        bk::launch_head<bk::MmaBF16, false>(few, a, edge, stream);
+    else
+        bk::launch_head<bk::MmaF16, false>(few, a, edge, stream);
+    const bk::HeadJoinArgs j{a.part, a.at, target, T, (int)V, parts, logprob, entropy, lse};
+    if (T <= 64)
+        hipLaunchKernelGGL(bk::k_head_join<1>, dim3((unsigned)T), dim3(256), 0, stream, j);
+    else
+        hipLaunchKernelGGL(bk::k_head_join<16>, dim3((unsigned)((T + 15) / 16)), dim3(256), 0, stream, j);
+    return bk::op_launched(who);
+}
+
+extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ldx, int64_t T, int64_t d,
+                                                       const void* w, int64_t ldw, int64_t V, int32_t dtype,
+                                                       const int64_t* target, const float* lse,
+                                                       const float* entropy, const float* g_logprob,
+                                                       const float* g_entropy, void* dx, int64_t lddx, void* dw,
+                                                       int64_t lddw, void* work, size_t* work_bytes,
+                                                       hipStream_t stream) {
+    static const char who[] = "bakron_head_logprobs_backward";
+    bk::set_last_error("");
+    bakron_status st = head_sizes(who, ldx, T, d, ldw, V, dtype);
+    if (st != BAKRON_OK) return st;
+    if ((dx && lddx < d) || (dw && lddw < d)) return bk::op_fail(who, "leading dimension below d");
+    const bk::HeadBackward b = bk::head_backward(std::max<int64_t>(T, 1), d, V, dtype == BAKRON_F16, dx != nullptr,
+                                                 dw != nullptr, bk::op_cus());
+    const bool many = !bk::head_few_rows(T, b.vc, d);
+    const bk::HeadPad p = bk::head_pad(x, ldx, w, ldw, T, d, V, many || dw, many || dx);
+    bool query;
+    st = bk::op_workspace(who, work, work_bytes, p.xbytes + p.wbytes + b.dz + b.partial + b.sums + b.scale, &query);
+    if (st != BAKRON_OK || query) return st;
+    if (!dx && !dw) return bk::op_fail(who, "null pointer");
+    if (g_logprob && !target) return bk::op_fail(who, "g_logprob needs targets");
+    if (g_entropy && !entropy) return bk::op_fail(who, "g_entropy needs the entropies");
+    if (T == 0 && !dw) return BAKRON_OK;
+    if (T == 0) {
+        hipLaunchKernelGGL(bk::k_zero_rows, dim3((unsigned)std::min<int64_t>(V, 65535)), dim3(256), 0, stream,
+                           static_cast<uint16_t*>(dw), lddw, V, d);
+        return bk::op_launched(who);
+    }
+    if (!x || !w || !lse) return bk::op_fail(who, "null pointer");
+    char* const to = static_cast<char*>(work) + p.xbytes + p.wbytes;
+    char* const partial = to + b.dz;
+    char* const sums = partial + b.partial;
+    bk::HeadScale* const scale = reinterpret_cast<bk::HeadScale*>(sums + b.sums);
+    bk::HeadArgs a{};
+    a.T = T;
+    a.V = (int)V;
+    a.target = g_logprob ? target : nullptr;
+    a.lse = lse;
+    a.entropy = entropy;
+    a.g_logprob = g_logprob;
+    a.g_entropy = g_entropy;
+    a.dz = to;
+    bk::head_operands(a, p, x, ldx, w, ldw, d, static_cast<char*>(work), stream);
+    const bk::HeadFew few{x, w, ldx, ldw, (int)d};
+    const int edge = bk::head_edge(T, b.vc, d);
+    if (dtype == BAKRON_BF16)
+        bk::run_head_backward<bk::MmaBF16>(few, a, b, d, V, edge, dx, lddx, dw, lddw, scale, partial,
+                                           reinterpret_cast<float*>(sums), stream);
+    else
+        bk::run_head_backward<bk::MmaF16>(few, a, b, d, V, edge, dx, lddx, dw, lddw, scale, partial,
+                                          reinterpret_cast<float*>(sums), stream);
+    return bk::op_launched(who);
+}

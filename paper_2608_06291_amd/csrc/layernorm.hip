@@ -1,0 +1,429 @@
+// Layer norm and RMS norm of a residual stream with the rows' statistics, and their gradients.
+//
+//   h = x + r (rounded once, as the stream holds it),   n = (h - mean) / sqrt(var + eps),   y = w (.) n + b
+//   g = w (.) dy,   dx = (g - mean(g) - n mean(g n)) / sqrt(var + eps) + d_sum
+//   dw = sum_t dy_t (.) n_t,   db = sum_t dy_t
+// with mean 0, var = mean(h^2) and no mean(g) for the RMS norm.
+//
+// Bound by memory: a row is read once and stays in registers over its reductions.
+#include "ops.h"
+
+namespace bk {
+
+struct LnArgs {
+    const void* x;
+    const void* res;
+    const float *w, *b;
+    void *sum, *y;
+    float *mean, *rstd;
+    int64_t ldx, ldr, lds, ldy, T;
+    int d, centre;
+    float eps;
+};
+
+// Two sums over `waves` waves of a workgroup at once; `red` as of group_reduce, twice as long.
+__device__ inline void group_sum2(float& a, float& b, float* red, int wave, int lane, int waves) {
+    a = wave_reduce(a, Add());
+    b = wave_reduce(b, Add());
+    if (waves == 1) return;
+    if (lane == 0) {
+        red[2 * wave] = a;
+        red[2 * wave + 1] = b;
+    }
+    __syncthreads();
+    a = red[0];
+    b = red[1];
+    for (int w = 1; w < waves; ++w) {
+        a += red[2 * w];
+        b += red[2 * w + 1];
+    }
+}
+
+// A row belongs to blockDim.x threads (one wave, with blockDim.y rows in the workgroup, or the
+// whole workgroup); thread t holds the whole vectors t, t + blockDim.x, .. of VEC entries, NV of them,
+// and one entry of what is left of the row.  Loads are whole vectors at clamped addresses, issued together.
+//
+// The mean's own rounding would be an error of every n where |mean| is far beyond the deviation, so the
+// entries less the rounded mean are summed as well, and what that leaves is taken off.
+template <typename E, int NV>
+__global__ __launch_bounds__(1024) void k_layernorm(LnArgs a) {
+    constexpr int VEC = 16 / sizeof(E);
+    __shared__ float red[3][32];
+    const int tid = threadIdx.x, tpr = blockDim.x, lane = tid & 63, wave = tid >> 6;
+    const int waves = tpr >> 6;
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (row >= a.T) return;   // (a whole wave, and never one of several in a row)
+    const E* const x = static_cast<const E*>(a.x) + row * a.ldx;
+    const E* const res = a.res ? static_cast<const E*>(a.res) + row * a.ldr : nullptr;
+    const int whole = a.d / VEC, left = whole * VEC + tid;
+
+    constexpr int STEP = NV * VEC <= 32 ? NV : 32 / VEC;   // vectors read at once
+    float h[NV][VEC], hx = 0.0f, s = 0.0f;
+#pragma unroll
+    for (int i0 = 0; i0 < NV; i0 += STEP) {
+        u32x4 rx[STEP], rr[STEP];
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) rx[i] = rr[i] = u32x4(0);
+        if (whole > 0) {   // (past the row its last vector, not used)
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) rx[i] = load_words(x + min((i0 + i) * tpr + tid, whole - 1) * VEC);
+            if (res) {
+#pragma unroll
+                for (int i = 0; i < STEP; ++i) rr[i] = load_words(res + min((i0 + i) * tpr + tid, whole - 1) * VEC);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+            const bool in = (i0 + i) * tpr + tid < whole;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                float v = entry<E>(rx[i], j);
+                if (res) v = (float)(E)(v + entry<E>(rr[i], j));
+                h[i0 + i][j] = in ? v : 0.0f;
+                s += h[i0 + i][j];
+            }
+        }
+    }
+    if (left < a.d) {
+        hx = (float)x[left];
+        if (res) hx = (float)(E)(hx + (float)res[left]);
+    }
+    s += hx;
+    auto store = [&](void* base, int64_t ld) {
+        E* const out = static_cast<E*>(base) + row * ld;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * tpr + tid;
+            Pack<E, VEC> p;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) p.v[j] = (E)h[i][j];
+            if (v < whole) store_pack(out + v * VEC, p);
+        }
+        if (left < a.d) out[left] = (E)hx;
+    };
+    if (a.sum) store(a.sum, a.lds);
+    const float inv_d = 1.0f / (float)a.d;
+    float mean = 0.0f, rest = 0.0f, sq = 0.0f;
+    if (a.centre) {
+        mean = group_reduce(s, Add(), red[0], wave, lane, waves) * inv_d;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool in = i * tpr + tid < whole;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) h[i][j] = in ? h[i][j] - mean : 0.0f;
+        }
+        hx = left < a.d ? hx - mean : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            rest += h[i][j];
+            sq = fmaf(h[i][j], h[i][j], sq);
+        }
+    rest += hx;
+    sq = fmaf(hx, hx, sq);
+    group_sum2(rest, sq, red[1], wave, lane, waves);
+    rest = a.centre ? rest * inv_d : 0.0f;
+    const float v = fmaxf(sq * inv_d - rest * rest, 0.0f) + a.eps;
+    const float r = v < INFINITY && sq < INFINITY ? 1.0f / sqrtf(v) : NAN;   // squares beyond fp32: not silently 0
+    if (tid == 0) {
+        if (a.mean) a.mean[row] = mean + rest;
+        if (a.rstd) a.rstd[row] = r;
+    }
+    if (!a.y) return;
+    const float off = -rest * r;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        Pack<float, VEC> w, b;
+        const int at = min(i * tpr + tid, whole - 1) * VEC;
+        if (a.w && whole > 0) w = load_pack<float, VEC>(a.w + at);
+        if (a.b && whole > 0) b = load_pack<float, VEC>(a.b + at);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            float n = fmaf(h[i][j], r, off);
+            if (a.w) n *= w.v[j];
+            if (a.b) n += b.v[j];
+            h[i][j] = n;
+        }
+    }
+    if (left < a.d) {
+        hx = fmaf(hx, r, off);
+        if (a.w) hx *= a.w[left];
+        if (a.b) hx += a.b[left];
+    }
+    store(a.y, a.ldy);
+}
+
+struct LnGradArgs {
+    const void *dy, *x, *ds;
+    const float *w, *mean, *rstd;
+    void* dx;
+    float *dw, *db;
+    float* part;   // slices x 2 x d
+    int64_t lddy, ldx, ldds, lddx, T;
+    int d, slices;
+};
+
+// dx, a row a group of threads as above.
+template <typename E, int NV>
+__global__ __launch_bounds__(1024) void k_layernorm_dx(LnGradArgs a) {
+    constexpr int VEC = 16 / sizeof(E);
+    __shared__ float red[32];
+    const int tid = threadIdx.x, tpr = blockDim.x, lane = tid & 63, wave = tid >> 6;
+    const int waves = tpr >> 6;
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (row >= a.T) return;
+    const E* const x = static_cast<const E*>(a.x) + row * a.ldx;
+    const E* const dy = static_cast<const E*>(a.dy) + row * a.lddy;
+    const int whole = a.d / VEC, left = whole * VEC + tid;
+    const float mean = a.mean ? a.mean[row] : 0.0f, r = a.rstd[row];
+    u32x4 rx[NV], rg[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) rx[i] = rg[i] = u32x4(0);
+    if (whole > 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            rx[i] = load_words(x + min(i * tpr + tid, whole - 1) * VEC);
+            rg[i] = load_words(dy + min(i * tpr + tid, whole - 1) * VEC);
+        }
+    }
+    float sg = 0.0f, sn = 0.0f;
+    auto weight = [&](int i) {
+        Pack<float, VEC> w;
+        if (a.w && whole > 0) return load_pack<float, VEC>(a.w + min(i * tpr + tid, whole - 1) * VEC);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) w.v[j] = 1.0f;
+        return w;
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i * tpr + tid >= whole) rg[i] = u32x4(0);
+        const auto w = weight(i);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float g = entry<E>(rg[i], j) * w.v[j], n = (entry<E>(rx[i], j) - mean) * r;
+            sg += g;
+            sn += i * tpr + tid < whole ? g * n : 0.0f;
+        }
+    }
+    float gx = 0.0f, nx = 0.0f;
+    if (left < a.d) {
+        gx = (float)dy[left] * (a.w ? a.w[left] : 1.0f);
+        nx = ((float)x[left] - mean) * r;
+    }
+    sg += gx;
+    sn = fmaf(gx, nx, sn);
+    group_sum2(sg, sn, red, wave, lane, waves);
+    sg = a.mean ? sg / (float)a.d : 0.0f;
+    sn /= (float)a.d;
+    E* const out = static_cast<E*>(a.dx) + row * a.lddx;
+    const E* const ds = a.ds ? static_cast<const E*>(a.ds) + row * a.ldds : nullptr;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = i * tpr + tid;
+        if (v >= whole) break;
+        const auto w = weight(i);
+        u32x4 rs = u32x4(0);
+        if (ds) rs = load_words(ds + v * VEC);
+        Pack<E, VEC> o;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float g = entry<E>(rg[i], j) * w.v[j], n = (entry<E>(rx[i], j) - mean) * r;
+            o.v[j] = (E)fmaf(g - sg - n * sn, r, entry<E>(rs, j));
+        }
+        store_pack(out + v * VEC, o);
+    }
+    if (left < a.d) out[left] = (E)fmaf(gx - sg - nx * sn, r, ds ? (float)ds[left] : 0.0f);
+}
+
+// Partial sums of dw and db over a slice of the rows: a thread has VEC columns, the four waves of a
+// workgroup the same columns and every fourth row, joined in LDS.
+template <typename E>
+__global__ __launch_bounds__(256) void k_layernorm_dw(LnGradArgs a) {
+    constexpr int VEC = 16 / sizeof(E);
+    __shared__ float red[3][2 * VEC][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = ((int)blockIdx.x * 64 + lane) * VEC;
+    const int64_t per = (a.T + a.slices - 1) / a.slices;
+    const int64_t lo = blockIdx.y * per, hi = min(a.T, lo + per);
+    float dw[VEC] = {}, db[VEC] = {};
+    if (c < a.d) {
+        for (int64_t t = lo + wave; t < hi; t += 4) {
+            const float mean = a.mean ? a.mean[t] : 0.0f, r = a.rstd[t];
+            const E* const x = static_cast<const E*>(a.x) + t * a.ldx + c;
+            const E* const dy = static_cast<const E*>(a.dy) + t * a.lddy + c;
+            float vx[VEC], vg[VEC];
+            if (c + VEC <= a.d) {
+                const u32x4 px = load_words(x), pg = load_words(dy);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    vx[j] = entry<E>(px, j);
+                    vg[j] = entry<E>(pg, j);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    vx[j] = c + j < a.d ? (float)x[j] : 0.0f;
+                    vg[j] = c + j < a.d ? (float)dy[j] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                dw[j] = fmaf(vg[j], (vx[j] - mean) * r, dw[j]);
+                db[j] += vg[j];
+            }
+        }
+    }
+    if (wave > 0) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            red[wave - 1][j][lane] = dw[j];
+            red[wave - 1][VEC + j][lane] = db[j];
+        }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    float* const part = a.part + (int64_t)blockIdx.y * 2 * a.d + c;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        if (c + j >= a.d) break;
+        part[j] = dw[j] + red[0][j][lane] + red[1][j][lane] + red[2][j][lane];
+        part[a.d + j] = db[j] + red[0][VEC + j][lane] + red[1][VEC + j][lane] + red[2][VEC + j][lane];
+    }
+}
+
+// Sums the slices, in their order.
+__global__ __launch_bounds__(256) void k_layernorm_join(LnGradArgs a) {
+    const int c = (int)blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.d) return;
+    float dw = 0.0f, db = 0.0f;
+    for (int s = 0; s < a.slices; ++s) {
+        dw += a.part[(int64_t)s * 2 * a.d + c];
+        db += a.part[((int64_t)s * 2 + 1) * a.d + c];
+    }
+    if (a.dw) a.dw[c] = dw;
+    if (a.db) a.db[c] = db;
+}
+
+// Threads a row, vectors a thread and rows a workgroup.
+struct LnGeom {
+    int tpr, nv, rows;
+};
+static LnGeom ln_geom(int64_t T, int64_t d, int vec, int nv_max) {
+    const int vecs = (int)((d + vec - 1) / vec);
+    LnGeom g{64, T < 1024 ? 1 : 2, 1};
+    while (g.tpr < 1024 && g.tpr * g.nv < vecs) g.tpr *= 2;
+    while (g.nv < nv_max && g.tpr * g.nv < vecs) g.nv *= 2;
+    if (g.tpr == 64) g.rows = 4;
+    return g;
+}
+
+template <typename E>
+static void launch_layernorm(const LnArgs& a, hipStream_t st) {
+    constexpr int VEC = 16 / sizeof(E), NV_MAX = 64 / VEC;
+    const LnGeom g = ln_geom(a.T, a.d, VEC, NV_MAX);
+    const dim3 grid((unsigned)((a.T + g.rows - 1) / g.rows)), block(g.tpr, g.rows);
+    switch (g.nv) {
+        case 1: hipLaunchKernelGGL((k_layernorm<E, 1>), grid, block, 0, st, a); break;
+        case 2: hipLaunchKernelGGL((k_layernorm<E, 2>), grid, block, 0, st, a); break;
+        case 4: hipLaunchKernelGGL((k_layernorm<E, 4>), grid, block, 0, st, a); break;
+        case 8: hipLaunchKernelGGL((k_layernorm<E, 8>), grid, block, 0, st, a); break;
+        default: hipLaunchKernelGGL((k_layernorm<E, NV_MAX>), grid, block, 0, st, a); break;
+    }
+}
+
+static int ln_slices(int64_t T, int64_t d, int esize) {
+    const int64_t blocks = (d * esize + 1023) / 1024;   // of columns
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / blocks + 1, (T + 15) / 16), 256));
+}
+
+template <typename E>
+static void launch_layernorm_grad(LnGradArgs a, hipStream_t st) {
+    constexpr int VEC = 16 / sizeof(E), NV_MAX = 64 / VEC;
+    if (a.dx) {
+        const LnGeom g = ln_geom(a.T, a.d, VEC, NV_MAX);
+        const dim3 grid((unsigned)((a.T + g.rows - 1) / g.rows)), block(g.tpr, g.rows);
+        switch (g.nv) {
+            case 1: hipLaunchKernelGGL((k_layernorm_dx<E, 1>), grid, block, 0, st, a); break;
+            case 2: hipLaunchKernelGGL((k_layernorm_dx<E, 2>), grid, block, 0, st, a); break;
+            case 4: hipLaunchKernelGGL((k_layernorm_dx<E, 4>), grid, block, 0, st, a); break;
+            case 8: hipLaunchKernelGGL((k_layernorm_dx<E, 8>), grid, block, 0, st, a); break;
+            default: hipLaunchKernelGGL((k_layernorm_dx<E, NV_MAX>), grid, block, 0, st, a); break;
+        }
+    }
+    if (a.dw || a.db) {
+        a.slices = ln_slices(a.T, a.d, sizeof(E));
+        const dim3 grid((unsigned)((a.d + 64 * VEC - 1) / (64 * VEC)), (unsigned)a.slices);
+        hipLaunchKernelGGL(k_layernorm_dw<E>, grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL(k_layernorm_join, dim3((unsigned)((a.d + 255) / 256)), dim3(256), 0, st, a);
+    }
+}
+
+}  // namespace bk
+
+static bakron_status layernorm_sizes(const char* who, int32_t dtype, int64_t T, int64_t d) {
+    if (T < 0 || T > bk::OP_T_MAX || d < 1 || d > 65536) return bk::op_fail(who, "bad size");
+    if (dtype != BAKRON_F32 && dtype != BAKRON_F16 && dtype != BAKRON_BF16) return bk::op_fail(who, "bad dtype");
+    const int vec = dtype == BAKRON_F32 ? 4 : 8;
+    if (T > bk::OP_LAUNCH_MAX / bk::ln_geom(T, d, vec, 64 / vec).tpr)
+        return bk::op_fail(who, "too many rows for one call");
+    return BAKRON_OK;
+}
+
+extern "C" bakron_status bakron_layernorm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int32_t dtype,
+                                          int64_t T, int64_t d, const float* weight, const float* bias, float eps,
+                                          int32_t centre, void* sum, int64_t lds, void* y, int64_t ldy, float* mean,
+                                          float* rstd, hipStream_t stream) {
+    static const char who[] = "bakron_layernorm";
+    bk::set_last_error("");
+    const bakron_status st = layernorm_sizes(who, dtype, T, d);
+    if (st != BAKRON_OK) return st;
+    if (!(eps >= 1e-30f) || !std::isfinite(eps)) return bk::op_fail(who, "bad eps");
+    if (ldx < d || (residual && ldr < d) || (sum && lds < d) || (y && ldy < d))
+        return bk::op_fail(who, "leading dimension below d");
+    if ((sum && sum == x && lds != ldx) || (sum && sum == residual && lds != ldr))
+        return bk::op_fail(who, "sum in place needs the same leading dimension");
+    if (mean && !centre) return bk::op_fail(who, "mean goes with centre");
+    if (T == 0) return BAKRON_OK;
+    if (!x || (!sum && !y && !mean && !rstd)) return bk::op_fail(who, "null pointer");
+    const bk::LnArgs a{x, residual, weight, bias, sum, y, mean, rstd, ldx, ldr, lds, ldy, T, (int)d, centre != 0, eps};
+    if (dtype == BAKRON_F32)
+        bk::launch_layernorm<float>(a, stream);
+    else if (dtype == BAKRON_F16)
+        bk::launch_layernorm<bk::f16_t>(a, stream);
+    else
+        bk::launch_layernorm<bk::bf16_t>(a, stream);
+    return bk::op_launched(who);
+}
+
+extern "C" bakron_status bakron_layernorm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                                   int32_t dtype, int64_t T, int64_t d, const float* weight,
+                                                   const float* mean, const float* rstd, const void* d_sum,
+                                                   int64_t ldds, void* dx, int64_t lddx, float* dweight, float* dbias,
+                                                   void* work, size_t* work_bytes, hipStream_t stream) {
+    static const char who[] = "bakron_layernorm_backward";
+    bk::set_last_error("");
+    bakron_status st = layernorm_sizes(who, dtype, T, d);
+    if (st != BAKRON_OK) return st;
+    const int esize = dtype == BAKRON_F32 ? 4 : 2;
+    const size_t need = dweight || dbias ? (size_t)bk::ln_slices(T, d, esize) * 2 * d * sizeof(float) : 0;
+    bool query;
+    st = bk::op_workspace(who, work, work_bytes, need, &query);
+    if (st != BAKRON_OK || query) return st;
+    if (lddy < d || ldx < d || (d_sum && ldds < d) || (dx && lddx < d))
+        return bk::op_fail(who, "leading dimension below d");
+    if (dx && dx == d_sum && lddx != ldds)
+        return bk::op_fail(who, "dx in place needs the same leading dimension");
+    if (!dx && !dweight && !dbias) return bk::op_fail(who, "null pointer");
+    if (T > 0 && (!dy || !x || !rstd)) return bk::op_fail(who, "null pointer");
+    bk::LnGradArgs a{dy, x, d_sum, weight, mean, rstd, T > 0 ? dx : nullptr, dweight, dbias, static_cast<float*>(work),
+                     lddy, ldx, ldds, lddx, T, (int)d, 0};
+    if (dtype == BAKRON_F32)
+        bk::launch_layernorm_grad<float>(a, stream);
+    else if (dtype == BAKRON_F16)
+        bk::launch_layernorm_grad<bk::f16_t>(a, stream);
+    else
+        bk::launch_layernorm_grad<bk::bf16_t>(a, stream);
+    return bk::op_launched(who);
+}

@@ -21,7 +21,7 @@
 // entry, 1240 to 1290; backward of 4096 rows 1790 to 1910 us: gated product 584, dx 518 (matrix cores 66%
 // busy), dW 673 (53%), in half precision 617, 535, 679.  The first and last take 5.4 rounds of tiles in the
 // time of 6; of dW both operands come by transposing reads.  One row 35 us: the weights' 180 MB at 5.2 TB/s.
-#include "tile.h"
+#include "product.h"
 
 namespace bk {
 
@@ -53,8 +53,6 @@ struct GatedArgs {
 struct GradScale {
     float factor, undo;
 };
-template <typename E>
-constexpr bool narrow_range = std::is_same<E, f16_t>::value;
 __global__ __launch_bounds__(1024) void k_grad_scale(const float* __restrict__ top, int64_t n, GradScale* out) {
     __shared__ float red[16];
     float m = 0.0f;
@@ -197,33 +195,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_gated(GatedArgs a) {
     }
 }
 
-// 8 entries on their way; see SHIFT below.
 constexpr int FEW_STEPS = 2;
-template <bool SHIFT>
-struct FewPiece {
-    u32x4 w;
-    uint32_t next;
-    template <typename E>
-    __device__ inline void load(const E* p) {
-        if constexpr (SHIFT) {
-            const uintptr_t at = (uintptr_t)p & ~(uintptr_t)3;
-            __builtin_memcpy(&w, (const void*)at, 16);
-            __builtin_memcpy(&next, (const void*)(at + ((uintptr_t)p & 2 ? 16 : 12)), 4);
-        } else {
-            w = load_words(p);
-        }
-    }
-    // `row`: any address of the same row's parity
-    template <typename E>
-    __device__ inline u32x4 get(const E* row) const {
-        if constexpr (SHIFT) {
-            if ((uintptr_t)row & 2)
-                return u32x4{__builtin_amdgcn_alignbit(w[1], w[0], 16), __builtin_amdgcn_alignbit(w[2], w[1], 16),
-                             __builtin_amdgcn_alignbit(w[3], w[2], 16), __builtin_amdgcn_alignbit(next, w[3], 16)};
-        }
-        return w;
-    }
-};
 
 // Few rows (a decoding step): bound by reading the weights once.  A workgroup takes 16
 // features and Y units of 16 rows; its waves share the summed axis, blocks of two steps of 32 in
@@ -303,26 +275,7 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
     }
     if (f.d % 32 != 0 && wave == (nsteps - nblocks * U) % waves) {
         const int k = nsteps * 32, left = f.d - k - kq * 8;   // entries of this lane's pieces
-        // 8 entries from p + k, zeros past the row: its last 8 entries moved down
-        auto part = [&](const E* p) {
-            u32x4 r = u32x4(0);
-            if (left >= 8) {
-                r = load_words(p + k);
-            } else if (left > 0 && f.d >= 8) {
-                unsigned __int128 v;
-                const u32x4 last = load_words(p + k + left - 8);
-                __builtin_memcpy(&v, &last, 16);
-                v >>= 16 * (8 - left);
-                __builtin_memcpy(&r, &v, 16);
-            } else if (left > 0) {
-                uint16_t v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[e] = e < left ? __builtin_bit_cast(uint16_t, p[k + e]) : (uint16_t)0;
-                __builtin_memcpy(&r, v, 16);
-            }
-            return r;
-        };
+        auto part = [&](const E* p) { return few_part(p + k, left, f.d); };
         u32x4 v[Y];
 #pragma unroll
         for (int y = 0; y < Y; ++y) v[y] = part(x[y]);
@@ -354,129 +307,6 @@ __global__ __launch_bounds__(512) void k_gated_few(FewArgs f, GatedArgs a) {
             if (lane == 0) a.top[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * Y + y] = top;
         }
     }
-}
-
-struct ProdArgs {
-    Operand a, b;                  // D[i][t] = sum_k a[i][k] b[t][k]
-    int chunks, ni, nt;
-    int64_t d;                     // columns of the output
-    void *out, *out2;              // rows t < split of out; split2 <= t < end, of out2
-    int64_t ldo, split, split2, end;
-    int parts, part_chunks;        // the summed axis in parts of so many chunks
-    float* partial;                // parts x end x dp, where there are several
-    int64_t dp;
-    const float* undo;             // the outputs are taken times this, or NULL
-};
-
-template <typename E>
-__device__ inline void prod_store(const ProdArgs& a, int64_t t, int64_t i, float undo, float (&v)[8]) {
-    if (t >= a.end || (t >= a.split && t < a.split2)) return;
-    if constexpr (narrow_range<E>) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= undo;
-    }
-    E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
-                               : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
-    store_n(row + i, v, a.d - i);
-}
-
-template <typename Tl>
-__global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
-    typedef typename Tl::Mma::Elem E;
-    __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
-    int ti, tt, part = 0, chunks = a.chunks;
-    if (a.parts > 1) {
-        part = blockIdx.x % (uint32_t)a.parts;
-        tile_of(blockIdx.x / (uint32_t)a.parts, a.ni, a.nt, 8, &ti, &tt);
-        chunks = min(a.part_chunks, a.chunks - part * a.part_chunks);
-    } else {
-        tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
-    }
-    const int64_t i0 = (int64_t)ti * Tl::ROWS, t0 = (int64_t)tt * Tl::COLS;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-
-    typename Tl::Accs acc = {};
-    Tl::run(lds, a.a, i0, a.b, t0, part * a.part_chunks, chunks, acc, [](int r) { return r; });
-
-    const auto rows =
-        handover<Tl>(lds, wave, lane, [&](int x, int y) { return Tl::at(acc, x, y); });
-    constexpr int PER = Tl::UA * 2;   // lanes a row
-    const float undo = narrow_range<E> && a.undo ? *a.undo : 1.0f;
-    const int p = lane % PER;
-    const int64_t i = i0 + Tl::a0(wave) + p * 8;
-#pragma unroll
-    for (int y = 0; y < Tl::UB; ++y) {
-        rows.put(y);
-#pragma unroll
-        for (int k = 0; k < 16 * PER / 64; ++k) {
-            const int tl = k * (64 / PER) + lane / PER;
-            const int64_t t = t0 + Tl::b0(wave) + y * 16 + tl;
-            float v[8];
-            rows.take(tl, p, v);
-            if (i < a.d && t < a.end) {
-                if (a.parts > 1)
-                    store_n(a.partial + (part * a.end + t) * a.dp + i, v, 8);
-                else
-                    prod_store<E>(a, t, i, undo, v);
-            }
-        }
-    }
-}
-
-// Sums the parts, in their order.
-template <typename E>
-__global__ __launch_bounds__(256) void k_prod_join(ProdArgs a) {
-    const int64_t per = a.dp / 8, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= a.end * per) return;
-    const int64_t t = e / per, i = e % per * 8;
-    if (i >= a.d) return;
-    float v[8] = {};
-    for (int p = 0; p < a.parts; ++p) {
-        const auto x = load_pack<float, 8>(a.partial + (p * a.end + t) * a.dp + i);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += x.v[j];
-    }
-    prod_store<E>(a, t, i, narrow_range<E> && a.undo ? *a.undo : 1.0f, v);
-}
-
-// Up to three matrices of the same width copied into rows of cols_p, zeros behind;
-// 16-bit entries.
-struct PadArgs {
-    const uint16_t* src[3];
-    uint16_t* dst[3];
-    int64_t ld[3], end[3];   // end: 8-entry pieces up to and with this one
-    int64_t cols, cols_p;
-};
-__global__ __launch_bounds__(256) void k_pad_rows(PadArgs a) {
-    const int64_t per = a.cols_p / 8;
-    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < a.end[2]; n += (int64_t)gridDim.x * 256) {
-        const int i = n < a.end[0] ? 0 : n < a.end[1] ? 1 : 2;
-        const int64_t e = n - (i == 0 ? 0 : i == 1 ? a.end[0] : a.end[1]), r = e / per, c = e % per * 8;
-        const uint16_t* const src = i == 0 ? a.src[0] : i == 1 ? a.src[1] : a.src[2];
-        uint16_t* const dst = i == 0 ? a.dst[0] : i == 1 ? a.dst[1] : a.dst[2];
-        const uint16_t* const row = src + r * (i == 0 ? a.ld[0] : i == 1 ? a.ld[1] : a.ld[2]);
-        Pack<uint16_t, 8> v;
-        if (c + 8 <= a.cols) {
-            v = load_pack<uint16_t, 8>(row + c);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v.v[j] = c + j < a.cols ? row[c + j] : (uint16_t)0;
-        }
-        store_pack(dst + e * 8, v);
-    }
-}
-
-__global__ __launch_bounds__(256) void k_zero_rows(uint16_t* p, int64_t ld, int64_t rows, int64_t cols) {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int64_t c = threadIdx.x; c < cols; c += 256) p[r * ld + c] = 0;
-}
-
-static inline size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
-static inline dim3 grid256(int64_t n) { return dim3((unsigned)((n + 255) / 256)); }
-
-// Whether rows can be staged as they are: 16-byte pieces at 16-byte addresses.
-static bool direct_rows(const void* p, int64_t ld, int64_t cols) {
-    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && 2 * ld < TILE_LD_MAX;
 }
 
 // Rows up to which the gated product is taken as one of few rows: 4096 -> 11008, 32 rows 52 us
@@ -532,59 +362,6 @@ static int64_t launch_gated(const FewArgs& few, GatedArgs a, hipStream_t st) {
     if (tile == 128 && one_a_cu(128, 2 * f, a.T)) return go(Tile<M, 128, 128, 2, 4, 3>());
     if (tile == 128) return go(Tile<M, 128, 128, 2, 4, 2>());
     return go(Tile<M, 64, 64, 2, 2, 4>());
-}
-
-// How a product is cut: tile edge, and parts of the summed axis (of 4 chunks at least),
-// by the least time: 1.55 us for a chunk's round of 256 x 256, the partial sums written and read
-// at 4 TB/s, 4 us for the launch that joins them.
-struct ProdPlan {
-    int tile, parts, part_chunks;
-    size_t bytes;   // of the partial sums
-};
-static ProdPlan prod_plan(int64_t i, int64_t t, int chunks, int ncu) {
-    ProdPlan best{64, 1, chunks, 0};
-    double least = 1e30;
-    for (int tile : {256, 128, 64}) {
-        const int64_t tiles = ((i + tile - 1) / tile) * ((t + tile - 1) / tile);
-        for (int parts = 1; parts <= 32 && (parts == 1 || chunks / parts >= 4); ++parts) {
-            const int each = (chunks + parts - 1) / parts, n = (chunks + each - 1) / each;
-            if (n != parts) continue;
-            const double us = tile_rounds(tile, tiles * n, ncu) * (each * 1.55 + 6.0) +
-                              (n > 1 ? 8.0 * n * i * t / 4e6 + 4.0 : 0.0);
-            if (us < least) {
-                least = us;
-                best = ProdPlan{tile, n, each, 0};
-            }
-        }
-    }
-    if (best.parts > 1)
-        best.bytes = up256((size_t)best.parts * t * ((i + 7) / 8 * 8) * sizeof(float));
-    return best;
-}
-
-template <typename M, bool ACOLS, bool BCOLS>
-static void launch_prod(ProdArgs a, const ProdPlan& p, void* partial, hipStream_t st) {
-    a.parts = p.parts;
-    a.part_chunks = p.part_chunks;
-    a.partial = static_cast<float*>(partial);
-    a.dp = (a.d + 7) / 8 * 8;
-    auto go = [&](auto tile) {
-        typedef decltype(tile) Tl;
-        a.ni = (int)((a.a.n + Tl::ROWS - 1) / Tl::ROWS);
-        a.nt = (int)((a.b.n + Tl::COLS - 1) / Tl::COLS);
-        hipLaunchKernelGGL((k_prod<Tl>), dim3((unsigned)(a.ni * a.nt * a.parts)), dim3(Tl::THREADS), 0, st,
-                           a);
-    };
-    if (p.tile == 256)
-        go(BigTile<M, ACOLS, BCOLS>());
-    else if (p.tile == 128 && one_a_cu(128, a.a.n, a.b.n, p.parts))
-        go(Tile<M, 128, 128, 2, 4, 3, ACOLS, BCOLS>());
-    else if (p.tile == 128)
-        go(Tile<M, 128, 128, 2, 4, 2, ACOLS, BCOLS>());
-    else
-        go(Tile<M, 64, 64, 2, 2, 4, ACOLS, BCOLS>());
-    if (a.parts > 1)
-        hipLaunchKernelGGL(k_prod_join<typename M::Elem>, grid256(a.end * (a.dp / 8)), dim3(256), 0, st, a);
 }
 
 // Padded copies of operands that cannot be staged as they are.
