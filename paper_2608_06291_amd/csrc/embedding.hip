@@ -4,7 +4,11 @@
 // A token outside [0, V) asks for nothing: its row of y is zeros, its dy counts nowhere.
 //
 // Forward: bound by memory.  Backward: the positions are sorted by token (equal ones in rising
-// order), so that each row of the table has one range of them, summed in that order by whoever writes the row.
+// order), so that each row of the table has one range of them.  Texts repeat a few tokens hundreds of times, so it is
+// chunks of 16 sorted positions that are summed, not ranges: a range inside a chunk gives its row at once, the
+// sums of longer ones are joined by whoever writes the row, in their order, beside the rows of no token.
+#include <algorithm>
+
 #include "ops.h"
 
 namespace bk {
@@ -52,42 +56,147 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
     if (left < hi) out[left] = asked ? (E)((float)row[left] * a.scale) : (E)0.0f;
 }
 
-// Sorting by counting: a position's place is the number of positions with a smaller token, or the same one
-// before it.  64 positions a workgroup, whose 16 waves share the comparisons.  Tokens outside [0, V)
-// sort behind all others.
-constexpr int SORT_WAVES = 16;
+// Positions sorted by token, equal tokens in rising order; tokens outside [0, V) behind all others.
 struct SortArgs {
     const int64_t* token;
     int64_t T, V;
-    int32_t *key, *pos;   // sorted tokens (V for those outside) and their positions
+    int32_t *key, *pos;        // sorted tokens (V for those outside) and their positions
+    // by digits
+    int32_t *key_in, *pos_in;  // what a pass reads (the first one: tokens)
+    int32_t* count;            // SORT_BINS x blocks
+    int blocks, shift;
 };
-__device__ inline uint32_t embed_key(int64_t token, int64_t V) {
-    return token >= 0 && token < V ? (uint32_t)token : (uint32_t)V;
+__device__ inline int32_t embed_key(int64_t token, int64_t V) {
+    return token >= 0 && token < V ? (int32_t)token : (int32_t)V;
 }
+
+// Up to SORT_BY_COUNT positions: a position's place is the number of positions with a smaller token, or the
+// same one before it.  A workgroup takes 32 positions, its 32 half waves share what they are compared with.
+// One launch; the work grows with T^2.
+constexpr int SORT_WAVES = 16;
 __global__ __launch_bounds__(64 * SORT_WAVES) void k_embed_sort(SortArgs a) {
-    __shared__ uint32_t keys[SORT_WAVES][64];
-    __shared__ int count[SORT_WAVES][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t t = (int64_t)blockIdx.x * 64 + lane;
-    const uint32_t mine = embed_key(t < a.T ? a.token[t] : -1, a.V);
+    __shared__ __attribute__((aligned(16))) int32_t keys[SORT_WAVES][64];
+    __shared__ int count[2 * SORT_WAVES][32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l = lane & 31;
+    const int64_t t0 = (int64_t)blockIdx.x * 32, t = t0 + l;
+    const int32_t mine = embed_key(t < a.T ? a.token[t] : -1, a.V);
     int below = 0;
-    // 64 keys of the others a wave at a time, read back one by one by all lanes
+    // 64 keys a wave at a time, 32 for each half; its own 32 positions' among them by (key, position)
+    int64_t next = wave * 64 + lane < a.T ? a.token[wave * 64 + lane] : -1;
     for (int64_t o0 = wave * 64; o0 < a.T; o0 += 64 * SORT_WAVES) {
-        keys[wave][lane] = o0 + lane < a.T ? embed_key(a.token[o0 + lane], a.V) : 0xffffffffu;
+        const int64_t o = o0 + lane, n = o + 64 * SORT_WAVES;
+        const int64_t token = next;
+        if (n < a.T) next = a.token[n];
         __builtin_amdgcn_wave_barrier();
-#pragma unroll 16
-        for (int k = 0; k < 64; ++k) {
-            const uint32_t o = keys[wave][k];
-            below += o < mine || (o == mine && o0 + k < t);
+        keys[wave][lane] = o < a.T ? embed_key(token, a.V) : 0x7fffffff;
+        __builtin_amdgcn_wave_barrier();
+        const int64_t first = o0 + half * 32;
+        const int32_t* const k = &keys[wave][half * 32];
+        // (keys below, or equal ones, of earlier positions: below `mine + 1`)
+        const int32_t bound = first < t0 ? mine + 1 : mine;
+        typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            const i32x4_t o4 = *reinterpret_cast<const i32x4_t*>(k + j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) below += o4[i] < bound;
         }
+        if (first == t0)
+            for (int j = 0; j < 32; ++j) below += k[j] == mine && j < l;
+    }
+    count[2 * wave + half][l] = below;
+    __syncthreads();
+    if (threadIdx.x >= 32 || t >= a.T) return;
+    for (int w = 1; w < 2 * SORT_WAVES; ++w) below += count[w][l];
+    a.key[below] = mine;
+    a.pos[below] = (int32_t)t;
+}
+constexpr int64_t SORT_BY_COUNT = 16384;
+
+// More of them: by two digits of 11 bits, each pass in three launches: the blocks' counts of each digit, their
+// running sum over (digit, block), and every position to its place.
+constexpr int SORT_BITS = 11, SORT_BINS = 1 << SORT_BITS, SORT_EACH = 4, SORT_BLOCK = 1024 * SORT_EACH;
+__device__ inline int32_t sort_key(const SortArgs& a, int64_t at) {
+    return a.key_in ? a.key_in[at] : embed_key(a.token[at], a.V);
+}
+__global__ __launch_bounds__(1024) void k_sort_count(SortArgs a) {
+    __shared__ int32_t bins[SORT_BINS];
+    for (int i = threadIdx.x; i < SORT_BINS; i += 1024) bins[i] = 0;
+    __syncthreads();
+    const int64_t lo = (int64_t)blockIdx.x * SORT_BLOCK;
+#pragma unroll
+    for (int i = 0; i < SORT_EACH; ++i) {
+        const int64_t at = lo + i * 1024 + threadIdx.x;
+        if (at < a.T) atomicAdd(&bins[(sort_key(a, at) >> a.shift) & (SORT_BINS - 1)], 1);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < SORT_BINS; i += 1024) a.count[(int64_t)i * a.blocks + blockIdx.x] = bins[i];
+}
+// One workgroup: each thread takes SORT_BINS / 1024 digits.
+__global__ __launch_bounds__(1024) void k_sort_scan(SortArgs a) {
+    __shared__ int32_t sums[1024];
+    const int64_t each = (int64_t)(SORT_BINS / 1024) * a.blocks;
+    int32_t* const c = a.count + threadIdx.x * each;
+    int32_t sum = 0;
+    for (int64_t i = 0; i < each; ++i) sum += c[i];
+    sums[threadIdx.x] = sum;
+    for (int n = 1; n < 1024; n *= 2) {
+        __syncthreads();
+        const int32_t v = (int)threadIdx.x >= n ? sums[threadIdx.x - n] : 0;
+        __syncthreads();
+        sums[threadIdx.x] += v;
+    }
+    int32_t at = sums[threadIdx.x] - sum;
+    for (int64_t i = 0; i < each; ++i) {
+        const int32_t n = c[i];
+        c[i] = at;
+        at += n;
+    }
+}
+// A wave takes 64 SORT_EACH positions in a row, 64 at a time; those of equal digits find each other by ballots.
+__global__ __launch_bounds__(1024) void k_sort_place(SortArgs a) {
+    __shared__ uint16_t bins[16][SORT_BINS];   // a wave's counts, then what lies before it in the block
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i = threadIdx.x; i < 16 * SORT_BINS; i += 1024) (&bins[0][0])[i] = 0;
+    __syncthreads();
+    const int64_t lo = (int64_t)blockIdx.x * SORT_BLOCK + wave * (64 * SORT_EACH);
+    int32_t key[SORT_EACH], rank[SORT_EACH];
+#pragma unroll
+    for (int i = 0; i < SORT_EACH; ++i) {
+        const int64_t at = lo + i * 64 + lane;
+        key[i] = at < a.T ? sort_key(a, at) : 0;
+        const int digit = (key[i] >> a.shift) & (SORT_BINS - 1);
+        uint64_t same = __ballot(at < a.T);
+#pragma unroll
+        for (int b = 0; b < SORT_BITS; ++b) {
+            const uint64_t one = __ballot((digit >> b) & 1);
+            same &= (digit >> b) & 1 ? one : ~one;
+        }
+        const int before = __popcll(same & ((1ull << lane) - 1));
+        rank[i] = bins[wave][digit] + before;   // (read by all before the last of them writes)
+        __builtin_amdgcn_wave_barrier();
+        if (at < a.T && (same >> lane) == 1) bins[wave][digit] = (uint16_t)(rank[i] + 1);
         __builtin_amdgcn_wave_barrier();
     }
-    count[wave][lane] = below;
     __syncthreads();
-    if (wave > 0 || t >= a.T) return;
-    for (int w = 1; w < SORT_WAVES; ++w) below += count[w][lane];
-    a.key[below] = (int32_t)mine;
-    a.pos[below] = (int32_t)t;
+    for (int i = threadIdx.x; i < SORT_BINS; i += 1024) {
+        int sum = 0;
+        for (int w = 0; w < 16; ++w) {
+            const int n = bins[w][i];
+            bins[w][i] = (uint16_t)sum;
+            sum += n;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < SORT_EACH; ++i) {
+        const int64_t at = lo + i * 64 + lane;
+        if (at >= a.T) break;
+        const int digit = (key[i] >> a.shift) & (SORT_BINS - 1);
+        const int64_t to = a.count[(int64_t)digit * a.blocks + blockIdx.x] + bins[wave][digit] + rank[i];
+        a.key[to] = key[i];
+        a.pos[to] = a.pos_in ? a.pos_in[at] : (int32_t)at;
+    }
 }
 
 struct EmbedGradArgs {
@@ -95,60 +204,150 @@ struct EmbedGradArgs {
     const void* base;
     void* out;
     const int32_t *key, *pos;
-    int64_t lddy, ldb, ldo, T, V;
-    int d, pieces;
+    int32_t* start;            // V + 1: where each token's sorted positions begin
+    float* part;               // what a chunk leaves of the range it begins in, and of the one it ends in: chunks x 2 x dp
+    int64_t lddy, ldb, ldo, T, V, dp;
+    int d, chunk_blocks, lanes;   // threads a row
     float scale;
 };
+// Sorted positions of a chunk.
+constexpr int EMBED_CHUNK = 16;
 
-// The first of n sorted keys that is not below v, found by a wave: 64 probes a step.
-__device__ inline int64_t lower_bound(const int32_t* key, int64_t n, int32_t v, int lane) {
-    int64_t lo = 0, hi = n;   // the answer is in [lo, hi]
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-        const uint64_t below = __ballot(at < hi && key[at] < v);
-        const int c = __popcll(below);   // probes 0 .. c - 1 are below v
-        if (c == 0) return lo;
-        hi = min(hi, lo + c * step);
-        lo = lo + (c - 1) * step + 1;
+// A row is read and written in whole vectors (WHOLE: d is a multiple of them), or its last entries one by one: `n` of
+// them are left from this vector on.
+template <typename E, bool WHOLE>
+__device__ inline u32x4 embed_load(const E* p, int n) {
+    constexpr int VEC = 16 / sizeof(E);
+    if (WHOLE || n >= VEC) return load_words(p);
+    E v[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) v[j] = j < n ? p[j] : (E)0.0f;
+    u32x4 r;
+    __builtin_memcpy(&r, v, 16);
+    return r;
+}
+// Base + scale * s.
+template <typename E, bool WHOLE>
+__device__ inline void embed_write(const EmbedGradArgs& a, int64_t v, int c, int n, const float (&s)[16 / sizeof(E)]) {
+    constexpr int VEC = 16 / sizeof(E);
+    float o[VEC] = {};
+    if (a.base) {
+        const u32x4 b = embed_load<E, WHOLE>(static_cast<const E*>(a.base) + v * a.ldb + c, n);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o[j] = entry<E>(b, j);
     }
-    return lo;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) o[j] = fmaf(s[j], a.scale, o[j]);
+    store_n(static_cast<E*>(a.out) + v * a.ldo + c, o, WHOLE ? VEC : n);
 }
 
-// A wave takes one vector a lane of one row of the table.
-template <typename E>
+// A chunk of the sorted positions is summed by `lanes` threads, a vector of the row each.  Where a token's whole range
+// lies in the chunk its row is written; of one that goes on from the chunk before, or into the next, the sum is
+// left for the row's writer.  The workgroups behind those of the chunks find where each token's range begins.
+template <typename E, bool WHOLE>
+__global__ __launch_bounds__(256) void k_embed_chunks(EmbedGradArgs a) {
+    constexpr int VEC = 16 / sizeof(E);
+    if ((int)blockIdx.x >= a.chunk_blocks) {
+        const int64_t v = (int64_t)((int)blockIdx.x - a.chunk_blocks) * 256 + threadIdx.x;
+        if (blockIdx.y > 0 || v > a.V) return;
+        int lo = 0, hi = (int)a.T;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (a.key[mid] < (int32_t)v)
+                lo = mid + 1;
+            else
+                hi = mid;
+        }
+        a.start[v] = lo;
+        return;
+    }
+    const int64_t chunk = (int64_t)blockIdx.x * (256 / a.lanes) + threadIdx.x / a.lanes;
+    const int64_t lo = chunk * EMBED_CHUNK;
+    const int c = ((int)blockIdx.y * a.lanes + (int)(threadIdx.x % a.lanes)) * VEC, n = a.d - c;
+    if (lo >= a.T || n <= 0) return;
+    const E* const dy = static_cast<const E*>(a.dy) + c;
+    const int count = (int)min(a.T - lo, (int64_t)EMBED_CHUNK);
+    // (whole chunks of both: the arrays are padded, and what lies past T is not used)
+    const auto key = load_pack<int32_t, EMBED_CHUNK>(a.key + lo), pos = load_pack<int32_t, EMBED_CHUNK>(a.pos + lo);
+    int32_t token = key.v[0];
+    const int32_t before = lo > 0 ? a.key[lo - 1] : -1, behind = lo + count < a.T ? a.key[lo + count] : -1;
+    u32x4 x[EMBED_CHUNK];
+#pragma unroll
+    for (int i = 0; i < EMBED_CHUNK; ++i)   // (all asked for at once)
+        x[i] = embed_load<E, WHOLE>(dy + (i < count ? pos.v[i] : pos.v[0]) * a.lddy, n);
+    bool begins = before != token;
+    float s[VEC] = {};
+    // (tokens outside the table are the last ones: V)
+    auto flush = [&](bool ends) {
+        if (begins && ends)
+            embed_write<E, WHOLE>(a, token, c, n, s);
+        else
+            store_n(a.part + (chunk * 2 + (begins ? 1 : 0)) * a.dp + c, s, VEC);
+    };
+#pragma unroll
+    for (int i = 0; i < EMBED_CHUNK; ++i) {
+        if (i > 0 && i < count && key.v[i] != token) {   // the token's range ends before this position
+            if (token < a.V) flush(true);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) s[j] = 0.0f;
+            token = key.v[i];
+            begins = true;
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) s[j] += i < count ? entry<E>(x[i], j) : 0.0f;
+    }
+    if (token < a.V) flush(token != behind);
+}
+
+// The rows that are left.  Those whose range spans chunks: first, as they take longest, by one workgroup for each
+// chunk in which such a range begins (256 vectors of the row a workgroup).  Those of no token: `lanes` lanes of a
+// wave take EMBED_ROWS of them, NV vectors a lane (blockIdx.y: which part of a longer row).
+constexpr int EMBED_ROWS = 4;
+template <typename E, int NV, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed_grad(EmbedGradArgs a) {
     constexpr int VEC = 16 / sizeof(E);
-    const int lane = threadIdx.x & 63;
-    const int64_t v = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (v >= a.V) return;
-    const int c = ((int)blockIdx.y * 64 + lane) * VEC;
-    const int64_t lo = lower_bound(a.key, a.T, (int32_t)v, lane), hi = lower_bound(a.key, a.T, (int32_t)v + 1, lane);
-    if (c >= a.d) return;
-    const int n = min(VEC, a.d - c);
-    float s[VEC] = {};
-    for (int64_t k = lo; k < hi; ++k) {
-        const E* const p = static_cast<const E*>(a.dy) + a.pos[k] * a.lddy + c;
-        if (n == VEC) {
-            const u32x4 x = load_words(p);
+    if ((int)blockIdx.x < a.chunk_blocks) {
+        const int64_t next = ((int64_t)blockIdx.x + 1) * EMBED_CHUNK;
+        const int32_t token = a.key[next];
+        if (token != a.key[next - 1] || token >= a.V) return;
+        const int lo = a.start[token], first = lo / EMBED_CHUNK, end = (a.start[token + 1] - 1) / EMBED_CHUNK;
+        if (first != (int)blockIdx.x) return;
+        for (int c = ((int)blockIdx.y * 256 + threadIdx.x) * VEC; c < a.d; c += gridDim.y * 256 * VEC) {
+            constexpr int AHEAD = 8;
+            const float* const part = a.part + c;
+            float s[VEC];
+            const auto p = load_pack<float, VEC>(part + ((int64_t)first * 2 + 1) * a.dp);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) s[j] += entry<E>(x, j);
-        } else {
+            for (int j = 0; j < VEC; ++j) s[j] = p.v[j];
+            for (int k = first + 1; k <= end; k += AHEAD) {
+                Pack<float, VEC> x[AHEAD];
 #pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (j < n) s[j] += (float)p[j];
+                for (int m = 0; m < AHEAD; ++m) x[m] = load_pack<float, VEC>(part + (int64_t)min(k + m, end) * 2 * a.dp);
+#pragma unroll
+                for (int m = 0; m < AHEAD; ++m)
+                    if (k + m <= end) {
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) s[j] += x[m].v[j];
+                    }
+            }
+            embed_write<E, WHOLE>(a, token, c, a.d - c, s);
         }
+        return;
     }
-    E* const out = static_cast<E*>(a.out) + v * a.ldo + c;
-    const E* const base = a.base ? static_cast<const E*>(a.base) + v * a.ldb + c : nullptr;
-    Pack<E, VEC> o;
+    const int64_t v0 = ((int64_t)((int)blockIdx.x - a.chunk_blocks) * (256 / a.lanes) + threadIdx.x / a.lanes) * EMBED_ROWS;
+    const int step = a.lanes * VEC, c = (int)blockIdx.y * NV * step + (int)(threadIdx.x % a.lanes) * VEC, n = a.d - c;
+    if (v0 >= a.V || n <= 0) return;
+    int start[EMBED_ROWS + 1];   // (all asked for at once; past the table its end: no rows)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) o.v[j] = (E)fmaf(s[j], a.scale, base && j < n ? (float)base[j] : 0.0f);
-    if (n == VEC) {
-        store_pack(out, o);
-    } else {
+    for (int r = 0; r <= EMBED_ROWS; ++r) start[r] = a.start[min(v0 + r, a.V)];
+    const float none[VEC] = {};
 #pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            if (j < n) out[j] = o.v[j];
+    for (int r = 0; r < EMBED_ROWS; ++r) {
+        if (v0 + r >= a.V) break;
+        if (start[r] < start[r + 1]) continue;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * step < n) embed_write<E, WHOLE>(a, v0 + r, c + i * step, n - i * step, none);
     }
 }
 
@@ -158,11 +357,79 @@ static void launch_embed(EmbedArgs a, hipStream_t st) {
     a.pieces = (a.d + len - 1) / len;
     hipLaunchKernelGGL(k_embed<E>, dim3((unsigned)(a.T * a.pieces)), dim3(256), 0, st, a);
 }
-template <typename E>
+// The workspace of the gradient.
+struct EmbedWork {
+    size_t keys, count, start, part;   // of one array of keys or positions (four of them where they are sorted by digits)
+    int blocks;
+    int64_t dp;
+    size_t bytes() const { return (blocks ? 4 : 2) * keys + count + start + part; }
+};
+static size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
+static EmbedWork embed_work(int64_t T, int64_t V, int64_t d) {
+    EmbedWork w{};
+    w.start = up256((size_t)(V + 1) * sizeof(int32_t));
+    w.keys = up256((size_t)T * sizeof(int32_t));
+    w.dp = (d + 7) / 8 * 8;
+    w.part = up256((size_t)((T + EMBED_CHUNK - 1) / EMBED_CHUNK) * 2 * w.dp * sizeof(float));
+    if (T > SORT_BY_COUNT) {
+        w.blocks = (int)((T + SORT_BLOCK - 1) / SORT_BLOCK);
+        w.count = up256((size_t)SORT_BINS * w.blocks * sizeof(int32_t));
+    }
+    return w;
+}
+
+// Leaves the sorted keys and positions at work and work + w.keys.
+static void launch_sort(const EmbedWork& w, const int64_t* tokens, int64_t T, int64_t V, char* work, hipStream_t st) {
+    auto at = [&](size_t o) { return reinterpret_cast<int32_t*>(work + o); };
+    SortArgs a{tokens, T, V, at(0), at(w.keys), nullptr, nullptr, nullptr, w.blocks, 0};
+    if (w.blocks == 0) {
+        hipLaunchKernelGGL(k_embed_sort, dim3((unsigned)((T + 31) / 32)), dim3(64 * SORT_WAVES), 0, st, a);
+        return;
+    }
+    a.count = at(4 * w.keys);
+    for (int pass = 0; pass < 2; ++pass) {
+        a.shift = pass * SORT_BITS;
+        a.key = at(pass ? 0 : 2 * w.keys);
+        a.pos = at(pass ? w.keys : 3 * w.keys);
+        a.key_in = pass ? at(2 * w.keys) : nullptr;
+        a.pos_in = pass ? at(3 * w.keys) : nullptr;
+        const dim3 grid((unsigned)w.blocks), block(1024);
+        hipLaunchKernelGGL(k_sort_count, grid, block, 0, st, a);
+        hipLaunchKernelGGL(k_sort_scan, dim3(1), block, 0, st, a);
+        hipLaunchKernelGGL(k_sort_place, grid, block, 0, st, a);
+    }
+}
+
+template <typename E, bool WHOLE>
 static void launch_embed_grad(EmbedGradArgs a, hipStream_t st) {
-    const int len = 64 * 16 / (int)sizeof(E);
-    a.pieces = (a.d + len - 1) / len;
-    hipLaunchKernelGGL(k_embed_grad<E>, dim3((unsigned)((a.V + 3) / 4), (unsigned)a.pieces), dim3(256), 0, st, a);
+    const int vecs = (a.d * (int)sizeof(E) + 15) / 16;
+    auto lanes = [&](int most) {
+        a.lanes = 1;
+        while (a.lanes < most && a.lanes < vecs) a.lanes *= 2;
+    };
+    lanes(256);
+    const int64_t chunks = (a.T + EMBED_CHUNK - 1) / EMBED_CHUNK;
+    a.chunk_blocks = (int)((chunks * a.lanes + 255) / 256);
+    hipLaunchKernelGGL((k_embed_chunks<E, WHOLE>),
+                       dim3((unsigned)(a.chunk_blocks + (a.V + 256) / 256), (unsigned)((vecs + a.lanes - 1) / a.lanes)),
+                       dim3(256), 0, st, a);
+    lanes(64);
+    a.chunk_blocks = (int)std::max<int64_t>(chunks - 1, 0);
+    const int nv = vecs <= 64 ? 1 : vecs <= 128 ? 2 : 4, each = 256 / a.lanes * EMBED_ROWS;
+    const dim3 grid((unsigned)(a.chunk_blocks + (a.V + each - 1) / each), (unsigned)((vecs + a.lanes * nv - 1) / (a.lanes * nv)));
+    if (nv == 1)
+        hipLaunchKernelGGL((k_embed_grad<E, 1, WHOLE>), grid, dim3(256), 0, st, a);
+    else if (nv == 2)
+        hipLaunchKernelGGL((k_embed_grad<E, 2, WHOLE>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_embed_grad<E, 4, WHOLE>), grid, dim3(256), 0, st, a);
+}
+template <typename E>
+static void launch_embed_grad(const EmbedGradArgs& a, hipStream_t st) {
+    if (a.d % (16 / (int)sizeof(E)) == 0)
+        launch_embed_grad<E, true>(a, st);
+    else
+        launch_embed_grad<E, false>(a, st);
 }
 
 }  // namespace bk
@@ -205,19 +472,19 @@ extern "C" bakron_status bakron_embedding_backward(const void* dy, int64_t lddy,
     bk::set_last_error("");
     bakron_status st = embed_sizes(who, dtype, T, V, d);
     if (st != BAKRON_OK) return st;
-    const size_t keys = ((size_t)T * sizeof(int32_t) + 255) / 256 * 256;
+    const bk::EmbedWork w = bk::embed_work(T, V, d);
     bool query;
-    st = bk::op_workspace(who, work, work_bytes, 2 * keys, &query);
+    st = bk::op_workspace(who, work, work_bytes, w.bytes(), &query);
     if (st != BAKRON_OK || query) return st;
     if (lddy < d || ldo < d || (base && ldb < d)) return bk::op_fail(who, "leading dimension below d");
     if (base && base == dtable && ldb != ldo) return bk::op_fail(who, "base in place needs the same leading dimension");
     if (!dtable || (T > 0 && (!dy || !tokens))) return bk::op_fail(who, "null pointer");
-    int32_t* const key = static_cast<int32_t*>(work);
-    int32_t* const pos = reinterpret_cast<int32_t*>(static_cast<char*>(work) + keys);
-    if (T > 0)
-        hipLaunchKernelGGL(bk::k_embed_sort, dim3((unsigned)((T + 63) / 64)), dim3(64 * bk::SORT_WAVES), 0, stream,
-                           bk::SortArgs{tokens, T, V, key, pos});
-    const bk::EmbedGradArgs a{dy, base, dtable, key, pos, lddy, ldb, ldo, T, V, (int)d, 0, scale};
+    char* const at = static_cast<char*>(work);
+    if (T > 0) bk::launch_sort(w, tokens, T, V, at, stream);
+    char* const part = at + w.bytes() - w.part;
+    const bk::EmbedGradArgs a{dy, base, dtable, reinterpret_cast<int32_t*>(at), reinterpret_cast<int32_t*>(at + w.keys),
+                              reinterpret_cast<int32_t*>(part - w.start), reinterpret_cast<float*>(part), lddy, ldb, ldo,
+                              T, V, w.dp, (int)d, 0, 0, scale};
     if (dtype == BAKRON_F32)
         bk::launch_embed_grad<float>(a, stream);
     else if (dtype == BAKRON_F16)

@@ -6,6 +6,8 @@
 // with mean 0, var = mean(h^2) and no mean(g) for the RMS norm.
 //
 // Bound by memory: a row is read once and stays in registers over its reductions.
+#include <algorithm>
+
 #include "ops.h"
 
 namespace bk {
@@ -160,7 +162,7 @@ struct LnGradArgs {
     const float *w, *mean, *rstd;
     void* dx;
     float *dw, *db;
-    float* part;   // slices x 2 x d
+    float* part;   // slices x 2 x dp, dp: d rounded up to a multiple of 8
     int64_t lddy, ldx, ldds, lddx, T;
     int d, slices;
 };
@@ -284,26 +286,187 @@ __global__ __launch_bounds__(256) void k_layernorm_dw(LnGradArgs a) {
     }
     __syncthreads();
     if (wave > 0) return;
-    float* const part = a.part + (int64_t)blockIdx.y * 2 * a.d + c;
+    const int64_t dp = (a.d + 7) / 8 * 8;
+    float* const part = a.part + blockIdx.y * 2 * dp + c;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
         if (c + j >= a.d) break;
         part[j] = dw[j] + red[0][j][lane] + red[1][j][lane] + red[2][j][lane];
-        part[a.d + j] = db[j] + red[0][VEC + j][lane] + red[1][VEC + j][lane] + red[2][VEC + j][lane];
+        part[dp + j] = db[j] + red[0][VEC + j][lane] + red[1][VEC + j][lane] + red[2][VEC + j][lane];
     }
 }
 
-// Sums the slices, in their order.
-__global__ __launch_bounds__(256) void k_layernorm_join(LnGradArgs a) {
-    const int c = (int)blockIdx.x * 256 + threadIdx.x;
-    if (c >= a.d) return;
-    float dw = 0.0f, db = 0.0f;
-    for (int s = 0; s < a.slices; ++s) {
-        dw += a.part[(int64_t)s * 2 * a.d + c];
-        db += a.part[((int64_t)s * 2 + 1) * a.d + c];
+// Sums the slices: a lane has one column of dw or db, the 16 waves every 16th slice each, joined in their order.
+__global__ __launch_bounds__(1024) void k_layernorm_join(LnGradArgs a) {
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int dp = (a.d + 7) / 8 * 8, c = (int)blockIdx.x * 64 + lane;
+    float sum = 0.0f;
+    if (c < 2 * dp) {
+        constexpr int AHEAD = 8;
+        for (int s = wave; s < a.slices; s += 16 * AHEAD) {
+            float v[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) v[i] = a.part[(int64_t)min(s + 16 * i, a.slices - 1) * 2 * dp + c];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) sum += s + 16 * i < a.slices ? v[i] : 0.0f;
+        }
     }
-    if (a.dw) a.dw[c] = dw;
-    if (a.db) a.db[c] = db;
+    red[wave][lane] = sum;
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < 16; ++w) sum += red[w][lane];
+    if (c < a.d && a.dw) a.dw[c] = sum;
+    if (c >= dp && c < dp + a.d && a.db) a.db[c - dp] = sum;
+}
+
+// Both at once, for rows that a workgroup's registers hold with the columns' sums beside them: a workgroup takes
+// every G-th block of rows (a row a group of tpr threads), the next rows on their way while one is summed, and
+// keeps sum dy n and sum dy of its columns.  x and dy are read once.  What is left of a row (less than a
+// vector) goes one entry a thread.
+template <typename E, int NV>
+__global__ __launch_bounds__(1024) void k_layernorm_grad(LnGradArgs a) {
+    constexpr int VEC = 16 / sizeof(E);
+    extern __shared__ __attribute__((aligned(16))) float sums[];   // rows of the workgroup beyond one: their columns' sums
+    __shared__ __attribute__((aligned(16))) float red[2][32];
+    const int tid = threadIdx.x, tpr = blockDim.x, lane = tid & 63, wave = tid >> 6;
+    const int waves = tpr >> 6, ys = blockDim.y;
+    const int whole = a.d / VEC, left = whole * VEC + tid;
+    const bool more = left < a.d;
+    float dw[NV][VEC] = {}, db[NV][VEC] = {}, dwx = 0.0f, dbx = 0.0f;
+    const float inv_d = 1.0f / (float)a.d;
+
+    struct Row {
+        u32x4 x[NV], g[NV];
+        float xl, gl, mean, r;
+    };
+    auto load = [&](Row& row, int64_t t) {
+        const E* const x = static_cast<const E*>(a.x) + t * a.ldx;
+        const E* const dy = static_cast<const E*>(a.dy) + t * a.lddy;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            row.x[i] = row.g[i] = u32x4(0);
+            if (whole > 0) {
+                row.x[i] = load_words(x + min(i * tpr + tid, whole - 1) * VEC);
+                row.g[i] = load_words(dy + min(i * tpr + tid, whole - 1) * VEC);
+            }
+        }
+        row.xl = more ? (float)x[left] : 0.0f;
+        row.gl = more ? (float)dy[left] : 0.0f;
+        row.mean = a.mean ? a.mean[t] : 0.0f;
+        row.r = a.rstd[t];
+    };
+    Pack<float, VEC> w[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) w[i].v[j] = 1.0f;
+        if (a.w && whole > 0) w[i] = load_pack<float, VEC>(a.w + min(i * tpr + tid, whole - 1) * VEC);
+    }
+    const float wl = a.w && more ? a.w[left] : 1.0f;
+
+    const int64_t step = (int64_t)gridDim.x * ys;
+    int64_t t = (int64_t)blockIdx.x * ys + threadIdx.y;
+    Row cur, next;
+    if (t < a.T) load(next, t);
+    int turn = 0;
+    // (with several rows a workgroup each is one wave: no barrier in here)
+    for (; t < a.T; t += step, turn ^= 1) {
+        cur = next;
+        u32x4 rs[NV];
+        float rsl = 0.0f;
+        if (a.dx && a.ds) {
+            const E* const ds = static_cast<const E*>(a.ds) + t * a.ldds;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                rs[i] = u32x4(0);
+                if (whole > 0) rs[i] = load_words(ds + min(i * tpr + tid, whole - 1) * VEC);
+            }
+            if (more) rsl = (float)ds[left];
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) rs[i] = u32x4(0);
+        }
+        if (t + step < a.T) load(next, t + step);
+        float sg = 0.0f, sn = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (i * tpr + tid < whole) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float dy = entry<E>(cur.g[i], j), g = dy * w[i].v[j];
+                    const float n = (entry<E>(cur.x[i], j) - cur.mean) * cur.r;
+                    sg += g;
+                    sn = fmaf(g, n, sn);
+                    dw[i][j] = fmaf(dy, n, dw[i][j]);
+                    db[i][j] += dy;
+                }
+            }
+        }
+        const float gl = cur.gl * wl, nl = more ? (cur.xl - cur.mean) * cur.r : 0.0f;
+        sg += gl;
+        sn = fmaf(gl, nl, sn);
+        dwx = fmaf(cur.gl, nl, dwx);
+        dbx += cur.gl;
+        if (!a.dx) continue;
+        group_sum2(sg, sn, red[turn], wave, lane, waves);
+        sg = a.mean ? sg * inv_d : 0.0f;
+        sn *= inv_d;
+        E* const out = static_cast<E*>(a.dx) + t * a.lddx;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * tpr + tid;
+            Pack<E, VEC> o;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float g = entry<E>(cur.g[i], j) * w[i].v[j], n = (entry<E>(cur.x[i], j) - cur.mean) * cur.r;
+                o.v[j] = (E)fmaf(g - sg - n * sn, cur.r, entry<E>(rs[i], j));
+            }
+            if (v < whole) store_pack(out + v * VEC, o);
+        }
+        if (more) out[left] = (E)fmaf(gl - sg - nl * sn, cur.r, rsl);
+    }
+    // the rows of a workgroup, in their order
+    const int64_t dp = (a.d + 7) / 8 * 8;
+    float* const part = a.part + (int64_t)blockIdx.x * 2 * dp;
+    for (int y = 1; y < ys; ++y) {
+        if ((int)threadIdx.y == y) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    sums[(i * VEC + j) * 64 + lane] = dw[i][j];
+                    sums[(NV * VEC + i * VEC + j) * 64 + lane] = db[i][j];
+                }
+            sums[2 * NV * VEC * 64 + lane] = dwx;
+            sums[2 * NV * VEC * 64 + 64 + lane] = dbx;
+        }
+        __syncthreads();
+        if (threadIdx.y == 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    dw[i][j] += sums[(i * VEC + j) * 64 + lane];
+                    db[i][j] += sums[(NV * VEC + i * VEC + j) * 64 + lane];
+                }
+            dwx += sums[2 * NV * VEC * 64 + lane];
+            dbx += sums[2 * NV * VEC * 64 + 64 + lane];
+        }
+        __syncthreads();
+    }
+    if (threadIdx.y != 0) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = i * tpr + tid;
+        if (v >= whole) break;
+        store_n(part + v * VEC, dw[i], VEC);
+        store_n(part + dp + v * VEC, db[i], VEC);
+    }
+    if (more) {
+        part[left] = dwx;
+        part[dp + left] = dbx;
+    }
 }
 
 // Threads a row, vectors a thread and rows a workgroup.
@@ -333,7 +496,17 @@ static void launch_layernorm(const LnArgs& a, hipStream_t st) {
     }
 }
 
+// The gradients together, where a row is at most two vectors a thread of 1024; else dx, then dw and db from x and
+// dy read once more.  Slices of the rows: together, one a CU, more where each still has 16 blocks of rows, because a
+// slice's sums are as much to write and read as two rows; else so many that every CU has two workgroups.
+static bool ln_together(int64_t d, int esize) { return d * esize <= 2 * 16 * 1024; }
 static int ln_slices(int64_t T, int64_t d, int esize) {
+    if (ln_together(d, esize)) {
+        const LnGeom g = ln_geom(1 << 20, d, 16 / esize, 2);
+        const int64_t blocks = (T + g.rows - 1) / g.rows, cus = op_cus();
+        const int64_t most = cus * std::max(1, 512 / (g.tpr * g.rows));   // so many have room
+        return (int)std::max<int64_t>(1, std::min({blocks, most, std::max(cus, blocks / 16)}));
+    }
     const int64_t blocks = (d * esize + 1023) / 1024;   // of columns
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / blocks + 1, (T + 15) / 16), 256));
 }
@@ -341,7 +514,17 @@ static int ln_slices(int64_t T, int64_t d, int esize) {
 template <typename E>
 static void launch_layernorm_grad(LnGradArgs a, hipStream_t st) {
     constexpr int VEC = 16 / sizeof(E), NV_MAX = 64 / VEC;
-    if (a.dx) {
+    const bool columns = a.dw || a.db;
+    if (columns) a.slices = ln_slices(a.T, a.d, sizeof(E));
+    if (columns && ln_together(a.d, sizeof(E))) {
+        const LnGeom g = ln_geom(1 << 20, a.d, VEC, 2);
+        const dim3 grid((unsigned)a.slices), block(g.tpr, g.rows);
+        const int lds = g.rows > 1 ? (2 * g.nv * VEC + 2) * 64 * (int)sizeof(float) : 0;
+        if (g.nv == 1)
+            hipLaunchKernelGGL((k_layernorm_grad<E, 1>), grid, block, lds, st, a);
+        else
+            hipLaunchKernelGGL((k_layernorm_grad<E, 2>), grid, block, lds, st, a);
+    } else if (a.dx) {
         const LnGeom g = ln_geom(a.T, a.d, VEC, NV_MAX);
         const dim3 grid((unsigned)((a.T + g.rows - 1) / g.rows)), block(g.tpr, g.rows);
         switch (g.nv) {
@@ -352,12 +535,12 @@ static void launch_layernorm_grad(LnGradArgs a, hipStream_t st) {
             default: hipLaunchKernelGGL((k_layernorm_dx<E, NV_MAX>), grid, block, 0, st, a); break;
         }
     }
-    if (a.dw || a.db) {
-        a.slices = ln_slices(a.T, a.d, sizeof(E));
+    if (!columns) return;
+    if (!ln_together(a.d, sizeof(E))) {
         const dim3 grid((unsigned)((a.d + 64 * VEC - 1) / (64 * VEC)), (unsigned)a.slices);
         hipLaunchKernelGGL(k_layernorm_dw<E>, grid, dim3(256), 0, st, a);
-        hipLaunchKernelGGL(k_layernorm_join, dim3((unsigned)((a.d + 255) / 256)), dim3(256), 0, st, a);
     }
+    hipLaunchKernelGGL(k_layernorm_join, dim3((unsigned)((2 * ((a.d + 7) / 8 * 8) + 63) / 64)), dim3(1024), 0, st, a);
 }
 
 }  // namespace bk
@@ -407,7 +590,7 @@ extern "C" bakron_status bakron_layernorm_backward(const void* dy, int64_t lddy,
     bakron_status st = layernorm_sizes(who, dtype, T, d);
     if (st != BAKRON_OK) return st;
     const int esize = dtype == BAKRON_F32 ? 4 : 2;
-    const size_t need = dweight || dbias ? (size_t)bk::ln_slices(T, d, esize) * 2 * d * sizeof(float) : 0;
+    const size_t need = dweight || dbias ? (size_t)bk::ln_slices(T, d, esize) * 2 * ((d + 7) / 8 * 8) * sizeof(float) : 0;
     bool query;
     st = bk::op_workspace(who, work, work_bytes, need, &query);
     if (st != BAKRON_OK || query) return st;

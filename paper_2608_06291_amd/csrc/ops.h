@@ -31,6 +31,32 @@ __device__ inline void store_pack(E* p, const Pack<E, N>& r) {
     __builtin_memcpy(p, &r, sizeof(r));
 }
 
+// N consecutive entries, `valid` of them inside the row.
+template <typename E, int N>
+__device__ inline void store_n(E* p, const float (&v)[N], int64_t valid) {
+    if (valid >= N) {
+        Pack<E, N> o;
+#pragma unroll
+        for (int j = 0; j < N; ++j) o.v[j] = (E)v[j];
+        store_pack(p, o);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < valid) p[j] = (E)v[j];
+    }
+}
+template <typename E, int N>
+__device__ inline void load_n(const E* p, float (&v)[N], int64_t valid) {
+    if (valid >= N) {
+        const auto o = load_pack<E, N>(p);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = (float)o.v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = j < valid ? (float)p[j] : 0.0f;
+    }
+}
+
 // A 16-byte vector of E as four registers: whole until an entry is asked for, so that
 // neither a branch around a load nor a second use makes the compiler take it apart.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -680,32 +680,6 @@ inline bool one_a_cu(int tile, int64_t i, int64_t t, int parts = 1) {
     return ((i + tile - 1) / tile) * ((t + tile - 1) / tile) * parts <= op_cus();
 }
 
-// N consecutive entries, `valid` of them inside the row.
-template <typename E, int N>
-__device__ inline void store_n(E* p, const float (&v)[N], int64_t valid) {
-    if (valid >= N) {
-        Pack<E, N> o;
-#pragma unroll
-        for (int j = 0; j < N; ++j) o.v[j] = (E)v[j];
-        store_pack(p, o);
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (j < valid) p[j] = (E)v[j];
-    }
-}
-template <typename E, int N>
-__device__ inline void load_n(const E* p, float (&v)[N], int64_t valid) {
-    if (valid >= N) {
-        const auto o = load_pack<E, N>(p);
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = (float)o.v[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = j < valid ? (float)p[j] : 0.0f;
-    }
-}
-
 // Activations and their slopes in fp32, from the hardware's exp2 and reciprocal (1 ulp each).  FINE is for a
 // product that stays in 32 bits, whose sums are exact: the exponent in two parts (exp_of), so that the tails of
 // negative z are good to a few units (2048 x 8192 x 28672 with SiLU 425 -> 439 us).  Elsewhere what z itself is off by,
