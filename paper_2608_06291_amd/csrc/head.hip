@@ -475,6 +475,33 @@ static void head_operands(HeadArgs& a, const HeadPad& p, const void* x, int64_t 
     hipLaunchKernelGGL(k_pad_rows, stride_grid(pieces), dim3(256), 0, st, c);
 }
 
+// x (T x cols, rows of 16-byte pieces) as columns: cols rows of tp entries, zeros from T on.  64 x 64 a workgroup.
+__global__ __launch_bounds__(256) void k_transpose(const char* x, int64_t ld, int64_t T, int cols, uint16_t* out,
+                                                   int64_t tp) {
+    __shared__ uint16_t tile[64][66];
+    const int64_t t0 = (int64_t)blockIdx.x * 64;
+    const int c0 = (int)blockIdx.y * 64;
+    const int p = threadIdx.x & 7, r = threadIdx.x >> 3;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int64_t t = t0 + i * 32 + r;
+        u32x4 v = u32x4(0);
+        if (t < T && c0 + p * 8 < cols) v = load_words(reinterpret_cast<const uint16_t*>(x + t * ld) + c0 + p * 8);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) tile[i * 32 + r][p * 8 + j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = c0 + i * 32 + r;
+        if (c >= cols) break;
+        Pack<uint16_t, 8> v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v.v[j] = tile[p * 8 + j][i * 32 + r];
+        store_pack(out + c * tp + t0 + p * 8, v);
+    }
+}
+
 // The backward pass.  A piece of the vocabulary is as long as dz of it stays in the last-level cache (256 MB) with
 // the operands beside it.  As many tokens as there are in up to one chunk of rows do not average dz's
 // rounding out, so there the products go on over its rests, too.
@@ -482,8 +509,9 @@ constexpr int64_t HEAD_PIECE_BYTES = (int64_t)128 << 20;
 struct HeadBackward {
     int64_t vc, vp, ldz;   // tokens of a piece (all but the last), padded; row of dz
     bool rests;
+    int64_t tp;            // x is taken as columns, of so many entries; or 0
     ProdPlan dx, dw;
-    size_t dz, partial, sums, scale;
+    size_t dz, partial, sums, scale, xt;
 };
 static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bool dx, bool dw, int ncu) {
     HeadBackward p{};
@@ -499,13 +527,15 @@ static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bo
     p.partial = std::max(p.dx.bytes, p.dw.bytes);
     p.sums = dx && p.vc < V ? up256((size_t)T * ((d + 7) / 8 * 8) * sizeof(float)) : 0;
     p.scale = half ? 256 : 0;
+    p.tp = dw && T >= 512 && V >= 8192 ? (T + 63) / 64 * 64 : 0;
+    p.xt = up256((size_t)((d + 7) / 8 * 8) * p.tp * 2);
     return p;
 }
 
 template <typename M>
 static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, int64_t d, int64_t V, int edge,
                               void* dx, int64_t lddx, void* dw, int64_t lddw, HeadScale* scale, void* partial,
-                              float* sums, hipStream_t st) {
+                              float* sums, uint16_t* xt, hipStream_t st) {
     typedef typename M::Elem E;
     constexpr bool HALF = narrow_range<E>;
     if (HALF) {
@@ -516,6 +546,9 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
     a.all = V;
     const char* const few_w = static_cast<const char*>(few.w);
     const int64_t cols = (d + 7) / 8 * 8;   // (of x and w, as they are or padded)
+    if (p.tp)
+        hipLaunchKernelGGL(k_transpose, dim3((unsigned)(p.tp / 64), (unsigned)((cols + 63) / 64)), dim3(256), 0, st,
+                           a.x.base, a.x.ld, a.T, (int)cols, xt, p.tp);
     for (a.v0 = 0; a.v0 < V; a.v0 += p.vc) {
         a.V = (int)std::min(p.vc, V - a.v0);
         a.vp = ((int64_t)a.V + 63) / 64 * 64;   // (p.vp but for the last piece)
@@ -565,7 +598,12 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
             g.out = static_cast<E*>(dw) + a.v0 * lddw;
             g.ldo = lddw;
             g.split = g.split2 = g.end = a.V;
-            launch_prod<M, true, true>(g, p.dw, partial, st);
+            if (p.tp) {
+                g.a = operand(xt, 2 * p.tp, cols, 2 * p.tp);
+                launch_prod<M, false, true>(g, p.dw, partial, st);
+            } else {
+                launch_prod<M, true, true>(g, p.dw, partial, st);
+            }
         }
     }
 }
@@ -640,7 +678,7 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     const bool many = !bk::head_few_rows(T, b.vc, d);
     const bk::HeadPad p = bk::head_pad(x, ldx, w, ldw, T, d, V, many || dw, many || dx);
     bool query;
-    st = bk::op_workspace(who, work, work_bytes, p.xbytes + p.wbytes + b.dz + b.partial + b.sums + b.scale, &query);
+    st = bk::op_workspace(who, work, work_bytes, p.xbytes + p.wbytes + b.dz + b.partial + b.sums + b.scale + b.xt, &query);
     if (st != BAKRON_OK || query) return st;
     if (!dx && !dw) return bk::op_fail(who, "null pointer");
     if (g_logprob && !target) return bk::op_fail(who, "g_logprob needs targets");
@@ -656,6 +694,7 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     char* const partial = to + b.dz;
     char* const sums = partial + b.partial;
     bk::HeadScale* const scale = reinterpret_cast<bk::HeadScale*>(sums + b.sums);
+    uint16_t* const xt = reinterpret_cast<uint16_t*>(sums + b.sums + b.scale);
     bk::HeadArgs a{};
     a.T = T;
     a.V = (int)V;
@@ -670,9 +709,9 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     const int edge = bk::head_edge(T, b.vc, d);
     if (dtype == BAKRON_BF16)
         bk::run_head_backward<bk::MmaBF16>(few, a, b, d, V, edge, dx, lddx, dw, lddw, scale, partial,
-                                           reinterpret_cast<float*>(sums), stream);
+                                           reinterpret_cast<float*>(sums), xt, stream);
     else
         bk::run_head_backward<bk::MmaF16>(few, a, b, d, V, edge, dx, lddx, dw, lddw, scale, partial,
-                                          reinterpret_cast<float*>(sums), stream);
+                                          reinterpret_cast<float*>(sums), xt, stream);
     return bk::op_launched(who);
 }
