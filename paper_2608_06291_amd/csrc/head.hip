@@ -380,20 +380,26 @@ __global__ __launch_bounds__(256) void k_head_join(HeadJoinArgs a) {
 // Rows up to which the product is taken as one of few rows; and with few tiles (by 64 x 64) a CU and a
 // long way to sum.
 constexpr int64_t HEAD_FEW_ROWS = 32, HEAD_FEW_TILES = 4;
-constexpr int HEAD_UNITS = 2;   // of 16 tokens a workgroup of that kernel
-
 static bool head_few_rows(int64_t T, int64_t V, int64_t d) {
     if (T <= HEAD_FEW_ROWS) return true;
     return ((V + 63) / 64) * ((T + 63) / 64) * HEAD_FEW_TILES <= op_cus() && d >= 512;
 }
+// Units of 16 tokens that a workgroup of that kernel takes.  More of them share the rows of x: 32 x 4096 x 131072 with
+// one unit 362 us, two 263, four 218, 16 rows of 2048 136, 108, 102.  With fewer rows x costs nothing, and long rows of w
+// come faster when few are read side by side: one row of 4096 175, 208, 201, four of 2048 102, 95, 102.  But every
+// CU should have a workgroup.
+static int head_units(int64_t T, int64_t V, int64_t d) {
+    int units = T > 8 ? 4 : d >= 4096 ? 1 : 2;
+    while (units > 1 && (V + 16 * units - 1) / (16 * units) * ((T + 31) / 32) < op_cus()) units /= 2;
+    return units;
+}
 // Tokens that a workgroup takes, and so the parts of the vocabulary.
 static int head_edge(int64_t T, int64_t V, int64_t d) {
-    return head_few_rows(T, V, d) ? 16 * HEAD_UNITS : pick_tile(V, T, op_cus(), true);
+    return head_few_rows(T, V, d) ? 16 * head_units(T, V, d) : pick_tile(V, T, op_cus(), true);
 }
 
-template <typename M, bool BWD, int Y, int BLOCKS>
+template <typename M, bool BWD, int R, int Y, int BLOCKS>
 static void launch_head_few(const HeadFew& f, const HeadArgs& a, hipStream_t st) {
-    constexpr int R = HEAD_UNITS;
     // Words around the pieces of odd rows: each matrix begins on a word, and whole steps end before the row
     // does, so an entry before and one behind each piece are in the matrix.
     const bool shift = (f.ldx % 2 != 0 || f.ldw % 2 != 0) && f.d % 32 != 0 && (uintptr_t)f.x % 4 == 0 &&
@@ -403,17 +409,21 @@ static void launch_head_few(const HeadFew& f, const HeadArgs& a, hipStream_t st)
     const int blocks = f.d / (32 * HEAD_STEPS);   // as many waves as have work, 8 at most
     const int waves = blocks >= 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
     if (shift)
-        hipLaunchKernelGGL((k_head_few<M, BWD, R, Y, 2, true>), grid, dim3(64 * waves), waves * Y * R * 1024, st, f, a);
+        hipLaunchKernelGGL((k_head_few<M, BWD, R, Y, BLOCKS, true>), grid, dim3(64 * waves), waves * Y * R * 1024, st, f, a);
     else
         hipLaunchKernelGGL((k_head_few<M, BWD, R, Y, BLOCKS, false>), grid, dim3(64 * waves), waves * Y * R * 1024, st,
                            f, a);
 }
 
-// edge: head_edge of the call
+// few_rows, edge: head_few_rows and head_edge of the call
 template <typename M, bool BWD>
-static void launch_head(const HeadFew& few, HeadArgs a, int edge, hipStream_t st) {
-    if (edge == 16 * HEAD_UNITS)
-        return a.T <= 16 ? launch_head_few<M, BWD, 1, 4>(few, a, st) : launch_head_few<M, BWD, 2, 2>(few, a, st);
+static void launch_head(const HeadFew& few, HeadArgs a, bool few_rows, int edge, hipStream_t st) {
+    if (few_rows) {
+        const bool one = a.T <= 16;
+        if (edge == 16) return one ? launch_head_few<M, BWD, 1, 1, 4>(few, a, st) : launch_head_few<M, BWD, 1, 2, 2>(few, a, st);
+        if (edge == 32) return one ? launch_head_few<M, BWD, 2, 1, 4>(few, a, st) : launch_head_few<M, BWD, 2, 2, 2>(few, a, st);
+        return one ? launch_head_few<M, BWD, 4, 1, 2>(few, a, st) : launch_head_few<M, BWD, 4, 2, 1>(few, a, st);
+    }
     const int64_t n = BWD ? a.vp : a.V;   // (the padding is written, too)
     auto go = [&](auto tile) {
         typedef decltype(tile) Tl;
@@ -533,8 +543,8 @@ static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bo
 }
 
 template <typename M>
-static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, int64_t d, int64_t V, int edge,
-                              void* dx, int64_t lddx, void* dw, int64_t lddw, HeadScale* scale, void* partial,
+static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, int64_t d, int64_t V,
+                              bool few_rows, int edge, void* dx, int64_t lddx, void* dw, int64_t lddw, HeadScale* scale, void* partial,
                               float* sums, uint16_t* xt, hipStream_t st) {
     typedef typename M::Elem E;
     constexpr bool HALF = narrow_range<E>;
@@ -556,7 +566,7 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
         a.w.base = w.base + a.v0 * w.ld;
         a.w.n = a.V;
         few.w = few_w + 2 * a.v0 * few.ldw;
-        launch_head<M, true>(few, a, edge, st);
+        launch_head<M, true>(few, a, few_rows, edge, st);
         ProdArgs g{};
         g.undo = HALF ? &scale->undo : nullptr;
         g.d = d;
@@ -650,9 +660,9 @@ extern "C" bakron_status bakron_head_logprobs(const void* x, int64_t ldx, int64_
     bk::head_operands(a, p, x, ldx, w, ldw, d, static_cast<char*>(work), stream);
     const bk::HeadFew few{x, w, ldx, ldw, (int)d};
     if (dtype == BAKRON_BF16)
-        bk::launch_head<bk::MmaBF16, false>(few, a, edge, stream);
+        bk::launch_head<bk::MmaBF16, false>(few, a, !many, edge, stream);
     else
-        bk::launch_head<bk::MmaF16, false>(few, a, edge, stream);
+        bk::launch_head<bk::MmaF16, false>(few, a, !many, edge, stream);
     const bk::HeadJoinArgs j{a.part, a.at, target, T, (int)V, parts, logprob, entropy, lse};
     if (T <= 64)
         hipLaunchKernelGGL(bk::k_head_join<1>, dim3((unsigned)T), dim3(256), 0, stream, j);
@@ -708,10 +718,10 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     const bk::HeadFew few{x, w, ldx, ldw, (int)d};
     const int edge = bk::head_edge(T, b.vc, d);
     if (dtype == BAKRON_BF16)
-        bk::run_head_backward<bk::MmaBF16>(few, a, b, d, V, edge, dx, lddx, dw, lddw, scale, partial,
+        bk::run_head_backward<bk::MmaBF16>(few, a, b, d, V, !many, edge, dx, lddx, dw, lddw, scale, partial,
                                            reinterpret_cast<float*>(sums), xt, stream);
     else
-        bk::run_head_backward<bk::MmaF16>(few, a, b, d, V, edge, dx, lddx, dw, lddw, scale, partial,
+        bk::run_head_backward<bk::MmaF16>(few, a, b, d, V, !many, edge, dx, lddx, dw, lddw, scale, partial,
                                           reinterpret_cast<float*>(sums), xt, stream);
     return bk::op_launched(who);
 }
