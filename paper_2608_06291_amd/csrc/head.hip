@@ -33,6 +33,7 @@ struct HeadArgs {
     void* dz;                  // T rows: vp entries (zeros in the padding), then what their rounding took
     int64_t vp, ldz;           // ldz: vp, or 2 vp with the rests
     const float* factor;       // half precision: dz is taken times this
+    void* dzt;                 // few rows: dz once more, a token a row: 16 or 32 rows of x, then the rests
 };
 
 // What few rows need beside that: x and w as they are, in entries.
@@ -89,12 +90,15 @@ __device__ inline float head_grad(const HeadRow& r, float z, int i) {
 }
 // N entries from token i of the piece on; zeros past its end.
 template <typename E, int N>
-__device__ inline void head_store(const HeadArgs& a, const HeadRow& r, int64_t t, int i, float factor, float (&z)[N]) {
+__device__ inline void head_grads(const HeadArgs& a, const HeadRow& r, int i, float factor, float (&z)[N]) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         z[j] = i + j < a.V ? head_grad(r, z[j], i + j) : 0.0f;
         if constexpr (narrow_range<E>) z[j] *= factor;
     }
+}
+template <typename E, int N>
+__device__ inline void head_store(const HeadArgs& a, int64_t t, int i, float (&z)[N]) {
     E* const row = static_cast<E*>(a.dz) + t * a.ldz + i;
     store_n(row, z, N);
     if (a.ldz > a.vp) {   // what the rounding took (nothing beside what is not finite)
@@ -104,6 +108,18 @@ __device__ inline void head_store(const HeadArgs& a, const HeadRow& r, int64_t t
             z[j] = __builtin_isfinite(v) ? z[j] - v : 0.0f;
         }
         store_n(row + a.vp, z, N);
+    }
+}
+
+// Few rows: the same four entries in the order of dzt, zeros for rows of x past T.
+template <typename E, int Y>
+__device__ inline void head_store_few(const HeadArgs& a, int64_t t, int i, const float (&z)[4]) {
+    E* const p = static_cast<E*>(a.dzt) + (int64_t)i * (32 * Y) + t;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float v = (float)(E)z[j];
+        p[j * (32 * Y)] = (E)z[j];
+        p[j * (32 * Y) + 16 * Y] = (E)(__builtin_isfinite(v) ? z[j] - v : 0.0f);
     }
 }
 
@@ -205,7 +221,10 @@ __global__ __launch_bounds__(Tl::THREADS) void k_head(HeadArgs a) {
                 const int tl = k * EACH + lane / PER, col = Tl::b0(wave) + y * 16 + tl;
                 float z[8];
                 rows.take(tl, p, z);
-                if (t0 + col < a.T && i < a.vp) head_store<E>(a, row[col], t0 + col, i, factor, z);
+                if (t0 + col < a.T && i < a.vp) {
+                    head_grads<E>(a, row[col], i, factor, z);
+                    head_store<E>(a, t0 + col, i, z);
+                }
             }
         }
     }
@@ -322,16 +341,205 @@ __global__ __launch_bounds__(512) void k_head_few(HeadFew f, HeadArgs a) {
             }
             const HeadPart p = head_part(z);
             if (lane < 16 && t < a.T) a.part[(int64_t)blockIdx.x * a.T + t] = p;
-        } else if (t < a.T) {
-            const HeadRow row = head_row(a, t);
+        } else {
+            HeadRow row{};
+            if (t < a.T) row = head_row(a, t);
             const float factor = narrow_range<E> ? *a.factor : 1.0f;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float v[4];
+                const int i = first + r * 16;
+                if (i >= a.vp) break;
+                float v[4] = {};
+                if (t < a.T) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = z[r * 4 + j];
-                if (first + r * 16 < a.vp) head_store<E>(a, row, t, first + r * 16, factor, v);
+                    for (int j = 0; j < 4; ++j) v[j] = z[r * 4 + j];
+                    head_grads<E>(a, row, i, factor, v);
+                }
+                if (a.dzt) head_store_few<E, Y>(a, t, i, v);
+                if (t < a.T) head_store<E>(a, t, i, v);
             }
+        }
+    }
+}
+
+// The products of few rows, bound by memory as dz is: w read once, dW written once.
+struct HeadFewProd {
+    const void *x, *w, *dz, *dzt;
+    int64_t ldx, ldw, ldz, vp, T;
+    int V, d, steps;           // steps of the vocabulary a wave (dW) or a workgroup (dx) takes
+    void* dw;
+    int64_t lddw;
+    float* partial;            // dx: parts x T x dp
+    int64_t dp;
+    const float* undo;
+};
+
+// dW: a wave holds 128 columns of x, of all rows, as 8 operands and goes through `steps` units of 16 tokens.
+// The results go through LDS, so that a store writes 256 bytes of each of four rows, and past the caches, which dW would
+// only sweep: 32768 x 4096 from one row, with dz, 97 us (through the caches 124; 64 bytes of 16 rows as the lanes hold them
+// 161).
+// A summed axis of 32 holds the rows of x and, up to 16 of them, the same again for dz's rests.
+template <typename M, int Y>
+__global__ __launch_bounds__(256) void k_head_few_dw(HeadFewProd a) {
+    typedef typename M::Elem E;
+    __shared__ __attribute__((aligned(16))) E rows[4][16][136];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
+    const int c0 = (int)blockIdx.x * 128;
+    const int64_t first = ((int64_t)blockIdx.y * 4 + wave) * a.steps * 16;
+    if (first >= a.V) return;
+    i32x4 x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int c = c0 + u * 16 + r16;
+        uint16_t v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int t = (kq * 8 + j) & (16 * Y - 1);
+            const uint16_t e = static_cast<const uint16_t*>(a.x)[min((int64_t)t, a.T - 1) * a.ldx + min(c, a.d - 1)];
+            v[j] = t < a.T && c < a.d ? e : (uint16_t)0;
+        }
+        __builtin_memcpy(&x[u], v, 16);
+    }
+    const float undo = narrow_range<E> ? *a.undo : 1.0f;
+    const char* const dzt = static_cast<const char*>(a.dzt) + (first + r16) * (64 * Y) + kq * 16;
+    const int n = (int)min((int64_t)a.steps, (a.V - first + 15) / 16), c = c0 + r16 * 8;
+    i32x4 b[Y], next[Y];
+    auto load = [&](int k) {   // (dz has rows of zeros up to a multiple of 64)
+#pragma unroll
+        for (int s = 0; s < Y; ++s) next[s] = *reinterpret_cast<const i32x4*>(dzt + (int64_t)k * (16 * 64 * Y) + s * 64);
+    };
+    load(0);
+    for (int k = 0; k < n; ++k) {
+#pragma unroll
+        for (int s = 0; s < Y; ++s) b[s] = next[s];
+        if (k + 1 < n) load(k + 1);
+        __builtin_amdgcn_wave_barrier();   // (what was put there is stored)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            f32x4 acc = M::mma(x[u], b[0], f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+            if constexpr (Y == 2) acc = M::mma(x[u], b[Y - 1], acc);
+            Pack<E, 4> o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o.v[j] = (E)(narrow_range<E> ? acc[j] * undo : acc[j]);
+            __builtin_memcpy(&rows[wave][r16][u * 16 + kq * 4], &o, 8);
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t v = first + k * 16 + r * 4 + kq;
+            const u32x4 o = *reinterpret_cast<const u32x4*>(&rows[wave][r * 4 + kq][r16 * 8]);
+            if (v >= a.V || c >= a.d) continue;
+            E* const out = static_cast<E*>(a.dw) + v * a.lddw + c;
+            if (c + 8 <= a.d) {
+                store_words_past(out, o);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < a.d) out[j] = (E)entry<E>(o, j);
+            }
+        }
+    }
+}
+
+// Sums dx's parts: a lane has one entry of a row, the 16 waves every 16th part each, joined in their order.
+template <typename E>
+__global__ __launch_bounds__(1024) void k_head_few_join(HeadFewProd a, E* dx, int64_t lddx) {
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t e = (int64_t)blockIdx.x * 64 + lane, all = a.T * a.dp;
+    const int parts = ((a.V + 31) / 32 + a.steps - 1) / a.steps;
+    float sum = 0.0f;
+    if (e < all) {
+        constexpr int AHEAD = 4;
+        for (int p = wave; p < parts; p += 16 * AHEAD) {
+            float v[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) v[i] = a.partial[min(p + 16 * i, parts - 1) * all + e];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) sum += p + 16 * i < parts ? v[i] : 0.0f;
+        }
+    }
+    red[wave][lane] = sum;
+    __syncthreads();
+    if (wave > 0 || e >= all || e % a.dp >= a.d) return;
+    for (int w = 1; w < 16; ++w) sum += red[w][lane];
+    dx[e / a.dp * lddx + e % a.dp] = (E)(narrow_range<E> ? sum * *a.undo : sum);
+}
+
+// dx: a wave takes 128 columns of w, 8 a lane, and 32 tokens a step; the 8 x 8 entries of a lane turn into 8 operands
+// with the tokens along (one permutation of two registers a pair), operand m having column 8 i + m as its row i.
+// The waves of a workgroup share its steps and meet in LDS, the workgroups' parts in a second launch.
+template <typename M, int Y>
+__global__ __launch_bounds__(256) void k_head_few_dx(HeadFewProd a) {
+    typedef typename M::Elem E;
+    __shared__ __attribute__((aligned(16))) f32x4 sums[3][8 * Y][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
+    // (past the row its last 8 columns, twice the same results)
+    const int c = min((int)blockIdx.x * 128 + r16 * 8, a.d - 8);
+    const int all = (a.V + 31) / 32, s0 = (int)blockIdx.y * a.steps, s1 = min(all, s0 + a.steps);
+    const E* const w = static_cast<const E*>(a.w) + c;
+    const E* dz[Y];
+#pragma unroll
+    for (int y = 0; y < Y; ++y) dz[y] = static_cast<const E*>(a.dz) + min((int64_t)(y * 16 + r16), a.T - 1) * a.ldz + kq * 8;
+    f32x4 acc[8][Y] = {};
+    struct Step {
+        u32x4 w[8];
+        i32x4 hi[Y], rest[Y];
+    };
+    auto load = [&](Step& p, int s) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p.w[j] = load_words(w + (int64_t)min(s * 32 + kq * 8 + j, a.V - 1) * a.ldw);
+#pragma unroll
+        for (int y = 0; y < Y; ++y) {
+            p.hi[y] = *reinterpret_cast<const i32x4*>(dz[y] + s * 32);
+            p.rest[y] = *reinterpret_cast<const i32x4*>(dz[y] + a.vp + s * 32);
+        }
+    };
+    Step cur, next;
+    if (s0 + wave < s1) load(next, s0 + wave);
+    for (int s = s0 + wave; s < s1; s += 4) {
+        cur = next;
+        if (s + 4 < s1) load(next, s + 4);
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+            i32x4 f;
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+                f[p] = (int32_t)__builtin_amdgcn_perm(cur.w[2 * p + 1][m >> 1], cur.w[2 * p][m >> 1],
+                                                      m & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int y = 0; y < Y; ++y) {
+                acc[m][y] = M::mma(f, cur.hi[y], acc[m][y]);
+                acc[m][y] = M::mma(f, cur.rest[y], acc[m][y]);
+            }
+        }
+    }
+    if (wave > 0) {
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+#pragma unroll
+            for (int y = 0; y < Y; ++y) sums[wave - 1][m * Y + y][lane] = acc[m][y];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int m = 0; m < 8; ++m)
+#pragma unroll
+        for (int y = 0; y < Y; ++y)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) acc[m][y] += sums[k][m * Y + y][lane];
+#pragma unroll
+    for (int y = 0; y < Y; ++y) {
+        const int64_t t = y * 16 + r16;
+        if (t >= a.T) break;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int col = (int)blockIdx.x * 128 + (kq * 4 + r) * 8;
+            if (col >= a.d) break;
+            float o[8];
+#pragma unroll
+            for (int m = 0; m < 8; ++m) o[m] = acc[m][y][r];
+            store_n(a.partial + ((int64_t)blockIdx.y * a.T + t) * a.dp + min(col, a.d - 8), o, 8);
         }
     }
 }
@@ -518,10 +726,11 @@ __global__ __launch_bounds__(256) void k_transpose(const char* x, int64_t ld, in
 constexpr int64_t HEAD_PIECE_BYTES = (int64_t)128 << 20;
 struct HeadBackward {
     int64_t vc, vp, ldz;   // tokens of a piece (all but the last), padded; row of dz
-    bool rests;
+    bool rests, few;       // few: the kernels for few rows; dx in `parts` of `steps` x 32 tokens
+    int parts, steps;
     int64_t tp;            // x is taken as columns, of so many entries; or 0
     ProdPlan dx, dw;
-    size_t dz, partial, sums, scale, xt;
+    size_t dz, dzt, partial, sums, scale, xt;
 };
 static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bool dx, bool dw, int ncu) {
     HeadBackward p{};
@@ -532,14 +741,46 @@ static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bo
     p.vp = (p.vc + 63) / 64 * 64;
     p.ldz = (p.rests ? 2 : 1) * p.vp;
     p.dz = up256((size_t)T * p.ldz * 2);
+    p.scale = half ? 256 : 0;
+    p.few = T <= HEAD_FEW_ROWS && d >= 8;   // (of one piece: 2^20 tokens at most)
+    if (p.few) {
+        const int slabs = (int)((d + 127) / 128), all = (int)((V + 31) / 32);
+        p.steps = std::max((all * slabs + 4 * ncu - 1) / (4 * ncu), 8);
+        p.parts = (all + p.steps - 1) / p.steps;
+        p.dzt = dw ? up256((size_t)p.vp * (T <= 16 ? 64 : 128)) : 0;
+        p.partial = dx ? up256((size_t)p.parts * T * ((d + 7) / 8 * 8) * sizeof(float)) : 0;
+        return p;
+    }
     if (dx) p.dx = prod_plan(d, T, (int)(p.ldz / 64), ncu);
     if (dw) p.dw = prod_plan(d, p.vp, (int)((p.rests ? 2 : 1) * ((T + 63) / 64)), ncu);
     p.partial = std::max(p.dx.bytes, p.dw.bytes);
     p.sums = dx && p.vc < V ? up256((size_t)T * ((d + 7) / 8 * 8) * sizeof(float)) : 0;
-    p.scale = half ? 256 : 0;
     p.tp = dw && T >= 512 && V >= 8192 ? (T + 63) / 64 * 64 : 0;
     p.xt = up256((size_t)((d + 7) / 8 * 8) * p.tp * 2);
     return p;
+}
+
+template <typename M, int Y>
+static void run_head_few(const HeadFew& few, HeadArgs a, const HeadBackward& p, int64_t d, int edge, void* dx, int64_t lddx,
+                         void* dw, int64_t lddw, HeadScale* scale, float* partial, hipStream_t st) {
+    typedef typename M::Elem E;
+    a.vp = p.vp;
+    a.ldz = p.ldz;
+    launch_head<M, true>(few, a, true, edge, st);
+    HeadFewProd g{few.x, few.w, a.dz, a.dzt, few.ldx, few.ldw, p.ldz, p.vp, a.T, a.V, (int)d, p.steps, dw, lddw, partial,
+                  (d + 7) / 8 * 8, narrow_range<E> ? &scale->undo : nullptr};
+    const unsigned slabs = (unsigned)((d + 127) / 128);
+    if (dx) {
+        hipLaunchKernelGGL((k_head_few_dx<M, Y>), dim3(slabs, (unsigned)p.parts), dim3(256), 0, st, g);
+        hipLaunchKernelGGL(k_head_few_join<E>, dim3((unsigned)((a.T * g.dp + 63) / 64)), dim3(1024), 0, st, g,
+                           static_cast<E*>(dx), lddx);
+    }
+    if (dw) {
+        const int64_t units = (a.V + 15) / 16;
+        g.steps = (int)std::max<int64_t>(1, std::min<int64_t>(16, units * slabs / (16 * op_cus())));
+        hipLaunchKernelGGL((k_head_few_dw<M, Y>), dim3(slabs, (unsigned)((units + 4 * g.steps - 1) / (4 * g.steps))), dim3(256), 0,
+                           st, g);
+    }
 }
 
 template <typename M>
@@ -552,8 +793,15 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
         hipLaunchKernelGGL(k_head_scale, dim3(1), dim3(1024), 0, st, a.g_logprob, a.g_entropy, a.T, scale);
         a.factor = &scale->factor;
     }
-    const Operand w = a.w;
     a.all = V;
+    if (p.few) {
+        if (a.T <= 16)
+            run_head_few<M, 1>(few, a, p, d, edge, dx, lddx, dw, lddw, scale, static_cast<float*>(partial), st);
+        else
+            run_head_few<M, 2>(few, a, p, d, edge, dx, lddx, dw, lddw, scale, static_cast<float*>(partial), st);
+        return;
+    }
+    const Operand w = a.w;
     const char* const few_w = static_cast<const char*>(few.w);
     const int64_t cols = (d + 7) / 8 * 8;   // (of x and w, as they are or padded)
     if (p.tp)
@@ -686,9 +934,10 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     const bk::HeadBackward b = bk::head_backward(std::max<int64_t>(T, 1), d, V, dtype == BAKRON_F16, dx != nullptr,
                                                  dw != nullptr, bk::op_cus());
     const bool many = !bk::head_few_rows(T, b.vc, d);
-    const bk::HeadPad p = bk::head_pad(x, ldx, w, ldw, T, d, V, many || dw, many || dx);
+    const bk::HeadPad p = bk::head_pad(x, ldx, w, ldw, T, d, V, many || (dw && !b.few), many || (dx && !b.few));
     bool query;
-    st = bk::op_workspace(who, work, work_bytes, p.xbytes + p.wbytes + b.dz + b.partial + b.sums + b.scale + b.xt, &query);
+    st = bk::op_workspace(who, work, work_bytes, p.xbytes + p.wbytes + b.dz + b.dzt + b.partial + b.sums + b.scale + b.xt,
+                          &query);
     if (st != BAKRON_OK || query) return st;
     if (!dx && !dw) return bk::op_fail(who, "null pointer");
     if (g_logprob && !target) return bk::op_fail(who, "g_logprob needs targets");
@@ -701,7 +950,7 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     }
     if (!x || !w || !lse) return bk::op_fail(who, "null pointer");
     char* const to = static_cast<char*>(work) + p.xbytes + p.wbytes;
-    char* const partial = to + b.dz;
+    char* const partial = to + b.dz + b.dzt;
     char* const sums = partial + b.partial;
     bk::HeadScale* const scale = reinterpret_cast<bk::HeadScale*>(sums + b.sums);
     uint16_t* const xt = reinterpret_cast<uint16_t*>(sums + b.sums + b.scale);
@@ -714,6 +963,7 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     a.g_logprob = g_logprob;
     a.g_entropy = g_entropy;
     a.dz = to;
+    a.dzt = b.dzt ? to + b.dz : nullptr;
     bk::head_operands(a, p, x, ldx, w, ldw, d, static_cast<char*>(work), stream);
     const bk::HeadFew few{x, w, ldx, ldw, (int)d};
     const int edge = bk::head_edge(T, b.vc, d);

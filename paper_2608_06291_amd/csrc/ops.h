@@ -76,6 +76,12 @@ __device__ inline float entry(const u32x4& u, int j) {
         return (float)__builtin_bit_cast(f16_t, (uint16_t)(u[j >> 1] >> (16 * (j & 1))));
     }
 }
+// 16 bytes to an address of any even alignment, not kept in the caches.
+typedef uint32_t u32x4_loose __attribute__((ext_vector_type(4), aligned(2)));
+template <typename E>
+__device__ inline void store_words_past(E* p, const u32x4& u) {
+    __builtin_nontemporal_store(u, reinterpret_cast<u32x4_loose*>(p));
+}
 // -infinity in every entry.
 template <typename E>
 __device__ inline uint32_t minus_infinity() {
