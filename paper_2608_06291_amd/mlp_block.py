@@ -8,7 +8,7 @@ the solver:
   * calibration: `gated_mlp` gives h and the features of the MLP-local Hessians of W_up
     and W_gate (App. A); the loss's gradient at the logits (`token_logprobs_backward`)
     gives b, the gradient at the block's output, for the global Hessian of W_down;
-    `gated_mlp_backward` takes b on to the layers before;
+    `gated_mlp_backward` and `layernorm_backward` take b on to the layers before;
   * rounding: `mse_scales`, `factor`, `solve` for each matrix, `pack_codes`;
   * serving: `rmsnorm_quant` makes 8-bit rows, `linear` multiplies them with the codes, the
     activation, the gate's product and the residual in its epilogue;
@@ -41,13 +41,17 @@ class GatedMLP:
         return out, y, h
 
     def backward(self, x, y, b):
-        """(dx, dw_gate, dw_up) from b, the gradient with respect to the block's output.  The
-        norm's gradient, a small part of the work, is torch's."""
-        dy, dw_gate, dw_up = _lib.gated_mlp_backward(b @ self.w_down, y, self.w_gate, self.w_up, act=self.act)
-        xf, g = x.float(), dy.float() * self.norm
-        r = (xf.square().mean(1, keepdim=True) + self.eps).rsqrt()
-        dx = r * (g - xf * (r * r) * (g * xf).mean(1, keepdim=True))
-        return (b.float() + dx).to(x.dtype), dw_gate, dw_up
+        """(dx, dw_gate, dw_up) from b, the gradient with respect to the block's output."""
+        return self.gradients(x, y, b)[:3]
+
+    def gradients(self, x, y, b, need_dw: bool = True):
+        """(dx, dw_gate, dw_up, dnorm) from b, the gradient with respect to the block's output; dnorm in fp32.
+        need_dw=False: the matrices stay as they are (None)."""
+        dy, dw_gate, dw_up = _lib.gated_mlp_backward(b @ self.w_down, y, self.w_gate, self.w_up, act=self.act,
+                                                     need_dw=need_dw)
+        rstd = _lib.layernorm(x, eps=self.eps, centre=False).rstd
+        dx, dnorm, _ = _lib.layernorm_backward(dy, x, self.norm, None, rstd, d_sum=b, need_dbias=False)
+        return dx, dw_gate, dw_up, dnorm
 
 
 @dataclass
