@@ -708,8 +708,8 @@ bakron_status bakron_token_logprobs_backward(const void *logits, int64_t ld, int
  *   logprob, entropy, lse   device outputs, T floats each, or NULL
  * A row with a logit that is NaN or +inf has NaN in every output; one whose logits
  * are all -inf has lse and log probability -inf and entropy 0.
- * 1 <= d <= 2^17, 1 <= V <= 2^20; ceil(T / 64) ceil(max(d, V) / 64) < 2^23 (or
- * BAKRON_EINVAL).  Workspace as above: 16 bytes a row for 32 to 256 tokens of the
+ * 1 <= d <= 2^17, 1 <= V <= 2^20, T <= 2^27, ceil(T / 64) ceil(max(d, V) / 64) < 2^23
+ * (or BAKRON_EINVAL).  Workspace as above: 16 bytes a row for 32 to 256 tokens of the
  * vocabulary, and padded copies of x and w where their rows are no 16-byte multiples
  * at 16-byte addresses and T > 32.
  */

@@ -755,7 +755,7 @@ static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bo
     if (dw) p.dw = prod_plan(d, p.vp, (int)((p.rests ? 2 : 1) * ((T + 63) / 64)), ncu);
     p.partial = std::max(p.dx.bytes, p.dw.bytes);
     p.sums = dx && p.vc < V ? up256((size_t)T * ((d + 7) / 8 * 8) * sizeof(float)) : 0;
-    p.tp = dw && T >= 512 && V >= 8192 ? (T + 63) / 64 * 64 : 0;
+    p.tp = dw && T >= 512 && V >= 8192 && 2 * (T + 63) < TILE_LD_MAX ? (T + 63) / 64 * 64 : 0;
     p.xt = up256((size_t)((d + 7) / 8 * 8) * p.tp * 2);
     return p;
 }
@@ -874,8 +874,8 @@ static bakron_status head_sizes(const char* who, int64_t ldx, int64_t T, int64_t
         return bk::op_fail(who, "bad size");
     if (ldx < d || ldw < d) return bk::op_fail(who, "leading dimension below d");
     if (dtype != BAKRON_F16 && dtype != BAKRON_BF16) return bk::op_fail(who, "dtype must be 16-bit");
-    // (the widest launches: 64 x 64 blocks of 256 threads)
-    if ((T + 63) / 64 * ((std::max(d, V) + 63) / 64) > ((int64_t)1 << 23) - 1)
+    // (the widest launches: 64 x 64 blocks of 256 threads, and 16 threads a row)
+    if (T > bk::OP_LAUNCH_MAX / 16 || (T + 63) / 64 * ((std::max(d, V) + 63) / 64) > ((int64_t)1 << 23) - 1)
         return bk::op_fail(who, "too many rows for one call");
     return BAKRON_OK;
 }

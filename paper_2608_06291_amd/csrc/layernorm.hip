@@ -600,6 +600,7 @@ extern "C" bakron_status bakron_layernorm_backward(const void* dy, int64_t lddy,
         return bk::op_fail(who, "dx in place needs the same leading dimension");
     if (!dx && !dweight && !dbias) return bk::op_fail(who, "null pointer");
     if (T > 0 && (!dy || !x || !rstd)) return bk::op_fail(who, "null pointer");
+    if (T == 0 && !dweight && !dbias) return BAKRON_OK;
     bk::LnGradArgs a{dy, x, d_sum, weight, mean, rstd, T > 0 ? dx : nullptr, dweight, dbias, static_cast<float*>(work),
                      lddy, ldx, ldds, lddx, T, (int)d, 0};
     if (dtype == BAKRON_F32)

@@ -10,6 +10,8 @@ import math
 
 import pytest
 
+from network_ends_sizes import HEAD, HEAD_LARGE
+
 pytestmark = pytest.mark.gpu
 
 U32 = 2.0 ** -24
@@ -309,12 +311,6 @@ def test_layernorm_backward_against_differences(centre):
 
 
 # ---------------------------------------------------------------- vocabulary loss
-# T, d, V, pad, shift: few rows, few tiles, each tile; odd rows; a vocabulary below and above a tile
-HEAD = [(1, 1, 1, 0, 0), (1, 4096, 1000, 0, 0), (2, 64, 33, 0, 0), (5, 7, 3, 0, 0), (17, 131, 257, 1, 1), (16, 1001, 700, 0, 0),
-        (33, 1024, 100, 0, 0), (33, 72, 1000, 8, 8), (70, 130, 65, 3, 1), (200, 264, 2000, 0, 0), (129, 520, 4100, 0, 0),
-        (600, 72, 9001, 0, 0), (300, 1000, 515, 0, 2), (64, 96, 300, 0, 0), (65, 96, 300, 0, 0)]
-
-
 def _head_inputs(T, d, V, dtype, seed=0):
     torch = _t()
     dt = _dtype(dtype)
@@ -412,3 +408,50 @@ def test_head_logprobs_backward(dtype, entropy, T, d, V, pad, shift):
     assert only[1] is None and torch.equal(only[0], dx)
     only = pk.head_logprobs_backward(*args, need_dx=False)
     assert only[0] is None and torch.equal(only[1], dw)
+
+
+@pytest.mark.parametrize("dtype", ("f16", "bf16"))
+@pytest.mark.parametrize("T,d,V,pad,shift", HEAD_LARGE)
+def test_head_large(dtype, T, d, V, pad, shift):
+    """Forward and backward against 64 bits on the GPU (its products in 64 bits are torch's)."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("head large", dtype, T, d, V, pad, shift)
+    x, w, tok = _head_inputs(T, d, V, dtype)
+    xs, ws, tk = _strided(x, pad, shift), _strided(w, pad, shift), tok.to(DEV)
+    xd, wd = x.to(DEV).double(), w.to(DEV).double()
+    z = xd @ wd.t()
+    lse = torch.logsumexp(z, 1)
+    logp = z - lse[:, None]
+    H = torch.special.entr(logp.exp()).sum(1)
+    asked = (tk >= 0) & (tk < V)
+    at = torch.where(asked, logp.gather(1, tk.clamp(0, V - 1)[:, None])[:, 0], 0.0)
+    got = pk.head_logprobs(xs, ws, tk)
+    ez = float((d + 1) * U32 * (xd.abs().amax() * wd.abs().sum(1).amax()))   # (bounds of test_head_logprobs, the largest row's)
+    es = 2 * ez + (V + 40) * U32 + 4 * U32 * (1 + H)
+    span = (z.amax(1) - z.amin(1)) + 1
+    for g, want, tol in ((got.lse, lse, ez + es + 2 * U32 * (lse.abs() + 1)), (got.entropy, H, 4 * es * span + 8 * U32 * (span + 1)),
+                         (got.logprob, at, torch.where(asked, 2 * ez + es + 4 * U32 * (at.abs() + lse.abs() + 1), 0.0))):
+        _within(g, want.cpu(), tol.cpu(), "forward")
+    del z
+    gl = (-torch.rand((T,), generator=torch.Generator().manual_seed(9)) / T).to(DEV)
+    dx, dw = pk.head_logprobs_backward(xs, ws, tk, lse.float(), g_logprob=gl)
+    again = pk.head_logprobs_backward(xs, ws, tk, lse.float(), g_logprob=gl)
+    assert torch.equal(dx, again[0]) and torch.equal(dw, again[1])
+    dz = logp.exp_().mul_(-torch.where(asked, gl.double(), 0.0)[:, None])
+    # p's own error, of a logit's, of lse's rounding and of exp's, counts in full where 1 - p is small
+    edz = dz.abs() * (2 * ez + 2 * U32 * (lse.abs()[:, None] + 30) + 8 * U32)
+    dz[asked, tk[asked]] += gl.double()[asked]
+    u = _u(dtype)
+    for got, want in ((dx, dz @ wd), (dw, dz.t().contiguous() @ xd)):
+        far = float((got.double() - want).norm())
+        own = 0.44 * u * (1 + 2 / math.sqrt(want.numel()))             # (as in test_head_logprobs_backward)
+        of_dz = 0.44 * u * (1 + 2 / math.sqrt(T / 4))
+        assert far <= (math.hypot(own, of_dz) + 1e-6) * float(want.norm()) + _tiny(dtype) * math.sqrt(want.numel()), far
+        # and no row is wrong: entrywise, a rounding of each term and of the result
+        size = dz.abs() @ wd.abs() if got is dx else dz.abs().t().contiguous() @ xd.abs()
+        of_p = edz @ wd.abs() if got is dx else edz.t().contiguous() @ xd.abs()
+        low = float(gl.abs().max()) * 2.0 ** -37 * max(T, V) * float(xd.abs().max()) if dtype == "f16" else 0.0
+        tol = 1.01 * (u * size + of_p + 2 * max(T, V) * U32 * size) + u * want.abs() + _tiny(dtype) + low
+        bad = (got.double() - want).abs() > tol
+        assert not bool(bad.any()), (got is dx, int(bad.sum()), float(((got.double() - want).abs() / tol).max()))
