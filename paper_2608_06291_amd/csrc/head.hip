@@ -730,6 +730,7 @@ struct HeadBackward {
     int parts, steps;
     int64_t tp;            // x is taken as columns, of so many entries; or 0
     ProdPlan dx, dw;
+    bool both;             // both products in one launch, where both are asked for
     size_t dz, dzt, partial, sums, scale, xt;
 };
 static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bool dx, bool dw, int ncu) {
@@ -751,11 +752,23 @@ static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bo
         p.partial = dx ? up256((size_t)p.parts * T * ((d + 7) / 8 * 8) * sizeof(float)) : 0;
         return p;
     }
-    if (dx) p.dx = prod_plan(d, T, (int)(p.ldz / 64), ncu);
-    if (dw) p.dw = prod_plan(d, p.vp, (int)((p.rests ? 2 : 1) * ((T + 63) / 64)), ncu);
-    p.partial = std::max(p.dx.bytes, p.dw.bytes);
+    // (the same sums whether both are asked for or one)
+    const int chunks_x = (int)(p.ldz / 64), chunks_w = (int)((p.rests ? 2 : 1) * ((T + 63) / 64));
+    p.dx = prod_plan(d, T, chunks_x, ncu);
+    p.dw = prod_plan(d, p.vp, chunks_w, ncu);
+    if (p.vc == V) {
+        const TwoPlans two = two_plans(d, T, chunks_x, d, p.vp, chunks_w, ncu);
+        p.both = two.us < p.dx.us + p.dw.us + 4.0;
+        if (p.both) {
+            p.dx = two.a;
+            p.dw = two.b;
+        }
+    }
+    if (!dx) p.dx.bytes = 0;
+    if (!dw) p.dw.bytes = 0;
+    p.partial = p.both ? p.dx.bytes + p.dw.bytes : std::max(p.dx.bytes, p.dw.bytes);
     p.sums = dx && p.vc < V ? up256((size_t)T * ((d + 7) / 8 * 8) * sizeof(float)) : 0;
-    p.tp = dw && T >= 512 && V >= 8192 && 2 * (T + 63) < TILE_LD_MAX ? (T + 63) / 64 * 64 : 0;
+    p.tp = dw && !p.both && T >= 512 && V >= 8192 && 2 * (T + 63) < TILE_LD_MAX ? (T + 63) / 64 * 64 : 0;
     p.xt = up256((size_t)((d + 7) / 8 * 8) * p.tp * 2);
     return p;
 }
@@ -815,53 +828,58 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
         a.w.n = a.V;
         few.w = few_w + 2 * a.v0 * few.ldw;
         launch_head<M, true>(few, a, few_rows, edge, st);
-        ProdArgs g{};
-        g.undo = HALF ? &scale->undo : nullptr;
-        g.d = d;
+        ProdArgs gx{}, gw{};
+        gx.undo = gw.undo = HALF ? &scale->undo : nullptr;
+        gx.d = gw.d = d;
         if (dx) {
-            g.a = operand(a.w.base, w.ld, cols, a.V);
-            g.chunks = (int)(a.ldz / 64);
+            gx.a = operand(a.w.base, w.ld, cols, a.V);
+            gx.chunks = (int)(a.ldz / 64);
             if (p.rests) {   // the same w again, beside the rests
-                g.a.base2 = g.a.base;
-                g.a.split = g.chunks / 2;
+                gx.a.base2 = gx.a.base;
+                gx.a.split = gx.chunks / 2;
             }
-            g.b = operand(a.dz, 2 * a.ldz, a.T, (int64_t)g.chunks * CHUNK_BYTES);
-            g.out = dx;
-            g.ldo = lddx;
-            g.split = g.split2 = g.end = a.T;
-            g.sums = sums;
-            g.first = a.v0 == 0;
-            g.last = a.v0 + a.V == V;
-            ProdPlan plan = p.dx;
-            if (a.vp != p.vp) {   // the last piece is shorter: no more parts than it has, none empty
-                plan.part_chunks = std::max(plan.part_chunks, 1);
-                plan.parts = std::min(plan.parts, (g.chunks + plan.part_chunks - 1) / plan.part_chunks);
-                if (plan.parts == 1) plan.part_chunks = g.chunks;
-            }
-            if (p.vc < V)
-                launch_prod<M, true, false, true>(g, plan, partial, st);
-            else
-                launch_prod<M, true, false>(g, plan, partial, st);
+            gx.b = operand(a.dz, 2 * a.ldz, a.T, (int64_t)gx.chunks * CHUNK_BYTES);
+            gx.out = dx;
+            gx.ldo = lddx;
+            gx.split = gx.split2 = gx.end = a.T;
+            gx.sums = sums;
+            gx.first = a.v0 == 0;
+            gx.last = a.v0 + a.V == V;
         }
         if (dw) {
-            g.a = operand(a.x.base, a.x.ld, cols, a.T);
-            g.b = operand(a.dz, 2 * a.ldz, a.vp, a.T);
-            g.chunks = (int)((a.T + 63) / 64);
+            gw.a = operand(a.x.base, a.x.ld, cols, a.T);
+            gw.b = operand(a.dz, 2 * a.ldz, a.vp, a.T);
+            gw.chunks = (int)((a.T + 63) / 64);
             if (p.rests) {
-                g.a.split = g.b.split = g.chunks;
-                g.a.base2 = g.a.base;
-                g.b.base2 = g.b.base + 2 * a.vp;
-                g.chunks *= 2;
+                gw.a.split = gw.b.split = gw.chunks;
+                gw.a.base2 = gw.a.base;
+                gw.b.base2 = gw.b.base + 2 * a.vp;
+                gw.chunks *= 2;
             }
-            g.out = static_cast<E*>(dw) + a.v0 * lddw;
-            g.ldo = lddw;
-            g.split = g.split2 = g.end = a.V;
-            if (p.tp) {
-                g.a = operand(xt, 2 * p.tp, cols, 2 * p.tp);
-                launch_prod<M, false, true>(g, p.dw, partial, st);
-            } else {
-                launch_prod<M, true, true>(g, p.dw, partial, st);
+            gw.out = static_cast<E*>(dw) + a.v0 * lddw;
+            gw.ldo = lddw;
+            gw.split = gw.split2 = gw.end = a.V;
+        }
+        if (p.both && dx && dw) {
+            launch_two<M>(gx, gw, p.dx, p.dw, static_cast<char*>(partial), st);
+            return;
+        }
+        if (dx) {
+            ProdPlan plan = p.dx;
+            if (a.vp != p.vp) {   // the last piece is shorter: no more parts than it has, none empty
+                plan.parts = std::min(plan.parts, (gx.chunks + plan.part_chunks - 1) / plan.part_chunks);
+                if (plan.parts == 1) plan.part_chunks = gx.chunks;
             }
+            if (p.vc < V)
+                launch_prod<M, true, false, true>(gx, plan, partial, st);
+            else
+                launch_prod<M, true, false>(gx, plan, partial, st);
+        }
+        if (dw && p.tp) {
+            gw.a = operand(xt, 2 * p.tp, cols, 2 * p.tp);
+            launch_prod<M, false, true>(gw, p.dw, partial, st);
+        } else if (dw) {
+            launch_prod<M, true, true>(gw, p.dw, partial, st);
         }
     }
 }

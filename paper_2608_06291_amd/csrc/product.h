@@ -96,17 +96,17 @@ __device__ inline void prod_store(const ProdArgs& a, int64_t t, int64_t i, float
     store_n(row + i, v, a.d - i);
 }
 
+// Workgroup `block` of a product.
 template <typename Tl, bool ACC>
-__global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
+__device__ inline void prod_tile(const ProdArgs& a, int block, char* lds) {
     typedef typename Tl::Mma::Elem E;
-    __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
     int ti, tt, part = 0, chunks = a.chunks;
     if (a.parts > 1) {
-        part = blockIdx.x % (uint32_t)a.parts;
-        tile_of(blockIdx.x / (uint32_t)a.parts, a.ni, a.nt, 8, &ti, &tt);
+        part = block % (uint32_t)a.parts;
+        tile_of(block / (uint32_t)a.parts, a.ni, a.nt, 8, &ti, &tt);
         chunks = min(a.part_chunks, a.chunks - part * a.part_chunks);
     } else {
-        tile_of(blockIdx.x, a.ni, a.nt, 8, &ti, &tt);
+        tile_of(block, a.ni, a.nt, 8, &ti, &tt);
     }
     const int64_t i0 = (int64_t)ti * Tl::ROWS, t0 = (int64_t)tt * Tl::COLS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -137,6 +137,22 @@ __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
             }
         }
     }
+}
+
+template <typename Tl, bool ACC>
+__global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+    prod_tile<Tl, ACC>(a, (int)blockIdx.x, lds);
+}
+// Two products in one launch: the first `first` workgroups are the one's.
+template <typename Ta, typename Tb>
+__global__ __launch_bounds__(Ta::THREADS) void k_prod_two(ProdArgs a, ProdArgs b, int first) {
+    static_assert(Ta::THREADS == Tb::THREADS && Ta::LDS == Tb::LDS, "tiles of one size");
+    __shared__ __attribute__((aligned(1024))) char lds[Ta::LDS];
+    if ((int)blockIdx.x < first)
+        prod_tile<Ta, false>(a, (int)blockIdx.x, lds);
+    else
+        prod_tile<Tb, false>(b, (int)blockIdx.x - first, lds);
 }
 
 // Sums the parts, in their order.
@@ -201,9 +217,10 @@ static bool direct_rows(const void* p, int64_t ld, int64_t cols) {
 struct ProdPlan {
     int tile, parts, part_chunks;
     size_t bytes;   // of the partial sums
+    double us;
 };
 static ProdPlan prod_plan(int64_t i, int64_t t, int chunks, int ncu) {
-    ProdPlan best{64, 1, chunks, 0};
+    ProdPlan best{64, 1, chunks, 0, 0.0};
     double least = 1e30;
     for (int tile : {256, 128, 64}) {
         const int64_t tiles = ((i + tile - 1) / tile) * ((t + tile - 1) / tile);
@@ -214,13 +231,81 @@ static ProdPlan prod_plan(int64_t i, int64_t t, int chunks, int ncu) {
                               (n > 1 ? 8.0 * n * i * t / 4e6 + 4.0 : 0.0);
             if (us < least) {
                 least = us;
-                best = ProdPlan{tile, n, each, 0};
+                best = ProdPlan{tile, n, each, 0, us};
             }
         }
     }
     if (best.parts > 1)
         best.bytes = up256((size_t)best.parts * t * ((i + 7) / 8 * 8) * sizeof(float));
     return best;
+}
+
+// Both of two products that need not wait for each other in one launch, by the same model: one launch (4 us) less,
+// and CUs that the one leaves idle go to the other.  Tiles of 128 or 64, the same for both.
+struct TwoPlans {
+    ProdPlan a, b;
+    double us;
+};
+static TwoPlans two_plans(int64_t ia, int64_t ta, int chunks_a, int64_t ib, int64_t tb, int chunks_b, int ncu) {
+    TwoPlans best{};
+    best.us = 1e30;
+    auto tiles = [](int64_t i, int64_t t, int tile) { return ((i + tile - 1) / tile) * ((t + tile - 1) / tile); };
+    auto join = [](int n, int64_t i, int64_t t) { return n > 1 ? 8.0 * n * i * t / 4e6 + 4.0 : 0.0; };
+    auto cut = [](int chunks, int parts, int* each) {   // whether the parts come out as so many
+        *each = (chunks + parts - 1) / parts;
+        return (parts == 1 || chunks / parts >= 4) && (chunks + *each - 1) / *each == parts;
+    };
+    for (int tile : {128, 64}) {
+        const int64_t na = tiles(ia, ta, tile), nb = tiles(ib, tb, tile);
+        for (int pa = 1, ea; pa <= 32; ++pa) {
+            if (!cut(chunks_a, pa, &ea)) continue;
+            for (int pb = 1, eb; pb <= 32; ++pb) {
+                if (!cut(chunks_b, pb, &eb)) continue;
+                const int64_t n = na * pa + nb * pb;
+                // as long as all of them take, and as the longest does (those of a come first)
+                const double mean = (double)(na * chunks_a + nb * chunks_b) / n;
+                const double all = tile_rounds(tile, n, ncu) * (mean * 1.55 + 6.0);
+                const double longest = tile_rounds(tile, std::min<int64_t>(n, 2 * ncu), ncu) * (std::max(ea, eb) * 1.55 + 6.0);
+                const double us = std::max(all, longest) + join(pa, ia, ta) + join(pb, ib, tb);
+                if (us < best.us) best = TwoPlans{{tile, pa, ea, 0, 0.0}, {tile, pb, eb, 0, 0.0}, us};
+            }
+        }
+    }
+    auto bytes = [](const ProdPlan& p, int64_t i, int64_t t) {
+        return p.parts > 1 ? up256((size_t)p.parts * t * ((i + 7) / 8 * 8) * sizeof(float)) : 0;
+    };
+    best.a.bytes = bytes(best.a, ia, ta);
+    best.b.bytes = bytes(best.b, ib, tb);
+    return best;
+}
+// a by columns of its first operand, b by columns of both.
+template <typename M>
+static void launch_two(ProdArgs a, ProdArgs b, const ProdPlan& pa, const ProdPlan& pb, char* partial, hipStream_t st) {
+    auto set = [](ProdArgs& g, const ProdPlan& q, char* partial) {
+        g.parts = q.parts;
+        g.part_chunks = q.part_chunks;
+        g.partial = reinterpret_cast<float*>(partial);
+        g.dp = (g.d + 7) / 8 * 8;
+        g.ni = (int)((g.a.n + q.tile - 1) / q.tile);
+        g.nt = (int)((g.b.n + q.tile - 1) / q.tile);
+    };
+    set(a, pa, partial);
+    set(b, pb, partial + pa.bytes);
+    const int first = a.ni * a.nt * a.parts, n = first + b.ni * b.nt * b.parts;
+    auto go = [&](auto ta, auto tb) {
+        typedef decltype(ta) Ta;
+        typedef decltype(tb) Tb;
+        hipLaunchKernelGGL((k_prod_two<Ta, Tb>), dim3((unsigned)n), dim3(Ta::THREADS), 0, st, a, b, first);
+    };
+    if (pa.tile == 128 && n <= op_cus())
+        go(Tile<M, 128, 128, 2, 4, 3, true, false>(), Tile<M, 128, 128, 2, 4, 3, true, true>());
+    else if (pa.tile == 128)
+        go(Tile<M, 128, 128, 2, 4, 2, true, false>(), Tile<M, 128, 128, 2, 4, 2, true, true>());
+    else
+        go(Tile<M, 64, 64, 2, 2, 4, true, false>(), Tile<M, 64, 64, 2, 2, 4, true, true>());
+    for (const ProdArgs* g : {&a, &b})
+        if (g->parts > 1)
+            hipLaunchKernelGGL((k_prod_join<typename M::Elem, false>), grid256(g->end * (g->dp / 8)), dim3(256), 0, st, *g);
 }
 
 template <typename M, bool ACOLS, bool BCOLS, bool ACC = false>
