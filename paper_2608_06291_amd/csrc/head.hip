@@ -49,6 +49,12 @@ struct HeadFew {
 struct HeadScale {
     float factor, undo;
 };
+__device__ inline HeadScale head_scale(float m) {
+    int e = 14;
+    if (m > 0.0f) frexpf(m, &e);   // m < 2^e
+    e = max(e, 14 - 126);          // (both powers are normal numbers)
+    return HeadScale{ldexpf(1.0f, 14 - e), ldexpf(1.0f, e - 14)};
+}
 __global__ __launch_bounds__(1024) void k_head_scale(const float* __restrict__ g, const float* __restrict__ gh,
                                                      int64_t T, HeadScale* out) {
     __shared__ float red[16];
@@ -59,10 +65,14 @@ __global__ __launch_bounds__(1024) void k_head_scale(const float* __restrict__ g
     }
     m = group_reduce(m, MaxNan(), red, threadIdx.x >> 6, threadIdx.x & 63, 16);
     if (threadIdx.x != 0) return;
-    int e = 14;
-    if (m > 0.0f) frexpf(m, &e);   // m < 2^e
-    e = max(e, 14 - 126);          // (both powers are normal numbers)
-    *out = HeadScale{ldexpf(1.0f, 14 - e), ldexpf(1.0f, e - 14)};
+    *out = head_scale(m);
+}
+
+// The same by every workgroup itself, for up to 64 rows (all lanes of the wave): one launch less.
+__device__ inline HeadScale head_scale_few(const float* g, const float* gh, int64_t T, int lane) {
+    float b = 0.0f;
+    if (lane < T) b = (g ? fabsf(g[lane]) : 0.0f) + (gh ? 4.0f * fabsf(gh[lane]) : 0.0f);
+    return head_scale(wave_reduce(b < INFINITY ? b : 0.0f, MaxNan()));
 }
 
 // A row's part of the gradient.
@@ -344,7 +354,9 @@ __global__ __launch_bounds__(512) void k_head_few(HeadFew f, HeadArgs a) {
         } else {
             HeadRow row{};
             if (t < a.T) row = head_row(a, t);
-            const float factor = narrow_range<E> ? *a.factor : 1.0f;
+            float factor = 1.0f;
+            if constexpr (narrow_range<E>)
+                factor = a.factor ? *a.factor : head_scale_few(a.g_logprob, a.g_entropy, a.T, lane).factor;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int i = first + r * 16;
@@ -366,26 +378,28 @@ __global__ __launch_bounds__(512) void k_head_few(HeadFew f, HeadArgs a) {
 struct HeadFewProd {
     const void *x, *w, *dz, *dzt;
     int64_t ldx, ldw, ldz, vp, T;
-    int V, d, steps;           // steps of the vocabulary a wave (dW) or a workgroup (dx) takes
+    int V, d;
+    int parts, steps;          // dx: parts of the vocabulary (0: not asked for), of so many steps of 32 tokens
+    int units;                 // dW: units of 16 tokens a wave takes
     void* dw;
     int64_t lddw;
     float* partial;            // dx: parts x T x dp
     int64_t dp;
-    const float* undo;
+    const float *g, *gh;
 };
 
-// dW: a wave holds 128 columns of x, of all rows, as 8 operands and goes through `steps` units of 16 tokens.
+// dW: a wave holds 128 columns of x, of all rows, as 8 operands and goes through `units` units of 16 tokens.
 // The results go through LDS, so that a store writes 256 bytes of each of four rows, and past the caches, which dW would
 // only sweep: 32768 x 4096 from one row, with dz, 97 us (through the caches 124; 64 bytes of 16 rows as the lanes hold them
 // 161).
 // A summed axis of 32 holds the rows of x and, up to 16 of them, the same again for dz's rests.
 template <typename M, int Y>
-__global__ __launch_bounds__(256) void k_head_few_dw(HeadFewProd a) {
+__device__ inline void head_few_dw(const HeadFewProd& a, int group, char* lds) {
     typedef typename M::Elem E;
-    __shared__ __attribute__((aligned(16))) E rows[4][16][136];
+    E (*const rows)[16][136] = reinterpret_cast<E (*)[16][136]>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
     const int c0 = (int)blockIdx.x * 128;
-    const int64_t first = ((int64_t)blockIdx.y * 4 + wave) * a.steps * 16;
+    const int64_t first = ((int64_t)group * 4 + wave) * a.units * 16;
     if (first >= a.V) return;
     i32x4 x[8];
 #pragma unroll
@@ -400,9 +414,9 @@ __global__ __launch_bounds__(256) void k_head_few_dw(HeadFewProd a) {
         }
         __builtin_memcpy(&x[u], v, 16);
     }
-    const float undo = narrow_range<E> ? *a.undo : 1.0f;
+    const float undo = narrow_range<E> ? head_scale_few(a.g, a.gh, a.T, lane).undo : 1.0f;
     const char* const dzt = static_cast<const char*>(a.dzt) + (first + r16) * (64 * Y) + kq * 16;
-    const int n = (int)min((int64_t)a.steps, (a.V - first + 15) / 16), c = c0 + r16 * 8;
+    const int n = (int)min((int64_t)a.units, (a.V - first + 15) / 16), c = c0 + r16 * 8;
     i32x4 b[Y], next[Y];
     auto load = [&](int k) {   // (dz has rows of zeros up to a multiple of 64)
 #pragma unroll
@@ -447,36 +461,37 @@ __global__ __launch_bounds__(1024) void k_head_few_join(HeadFewProd a, E* dx, in
     __shared__ float red[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t e = (int64_t)blockIdx.x * 64 + lane, all = a.T * a.dp;
-    const int parts = ((a.V + 31) / 32 + a.steps - 1) / a.steps;
     float sum = 0.0f;
     if (e < all) {
         constexpr int AHEAD = 4;
-        for (int p = wave; p < parts; p += 16 * AHEAD) {
+        for (int p = wave; p < a.parts; p += 16 * AHEAD) {
             float v[AHEAD];
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) v[i] = a.partial[min(p + 16 * i, parts - 1) * all + e];
+            for (int i = 0; i < AHEAD; ++i) v[i] = a.partial[min(p + 16 * i, a.parts - 1) * all + e];
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) sum += p + 16 * i < parts ? v[i] : 0.0f;
+            for (int i = 0; i < AHEAD; ++i) sum += p + 16 * i < a.parts ? v[i] : 0.0f;
         }
     }
     red[wave][lane] = sum;
     __syncthreads();
-    if (wave > 0 || e >= all || e % a.dp >= a.d) return;
+    if (wave > 0) return;
     for (int w = 1; w < 16; ++w) sum += red[w][lane];
-    dx[e / a.dp * lddx + e % a.dp] = (E)(narrow_range<E> ? sum * *a.undo : sum);
+    if constexpr (narrow_range<E>) sum *= head_scale_few(a.g, a.gh, a.T, lane).undo;
+    if (e >= all || e % a.dp >= a.d) return;
+    dx[e / a.dp * lddx + e % a.dp] = (E)sum;
 }
 
 // dx: a wave takes 128 columns of w, 8 a lane, and 32 tokens a step; the 8 x 8 entries of a lane turn into 8 operands
 // with the tokens along (one permutation of two registers a pair), operand m having column 8 i + m as its row i.
 // The waves of a workgroup share its steps and meet in LDS, the workgroups' parts in a second launch.
 template <typename M, int Y>
-__global__ __launch_bounds__(256) void k_head_few_dx(HeadFewProd a) {
+__device__ inline void head_few_dx(const HeadFewProd& a, int part, char* lds) {
     typedef typename M::Elem E;
-    __shared__ __attribute__((aligned(16))) f32x4 sums[3][8 * Y][64];
+    f32x4 (*const sums)[8 * Y][64] = reinterpret_cast<f32x4 (*)[8 * Y][64]>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
     // (past the row its last 8 columns, twice the same results)
     const int c = min((int)blockIdx.x * 128 + r16 * 8, a.d - 8);
-    const int all = (a.V + 31) / 32, s0 = (int)blockIdx.y * a.steps, s1 = min(all, s0 + a.steps);
+    const int all = (a.V + 31) / 32, s0 = part * a.steps, s1 = min(all, s0 + a.steps);
     const E* const w = static_cast<const E*>(a.w) + c;
     const E* dz[Y];
 #pragma unroll
@@ -539,9 +554,21 @@ __global__ __launch_bounds__(256) void k_head_few_dx(HeadFewProd a) {
             float o[8];
 #pragma unroll
             for (int m = 0; m < 8; ++m) o[m] = acc[m][y][r];
-            store_n(a.partial + ((int64_t)blockIdx.y * a.T + t) * a.dp + min(col, a.d - 8), o, 8);
+            store_n(a.partial + ((int64_t)part * a.T + t) * a.dp + min(col, a.d - 8), o, 8);
         }
     }
+}
+
+// DX and DW: both in one launch, the first `parts` rows of workgroups being dx's.
+template <typename M, int Y, bool DX, bool DW>
+__global__ __launch_bounds__(256) void k_head_few_prod(HeadFewProd a) {
+    constexpr int LDS_X = 3 * 8 * Y * 64 * 16, LDS_W = 4 * 16 * 136 * 2;
+    __shared__ __attribute__((aligned(16))) char lds[!DX ? LDS_W : !DW || LDS_X > LDS_W ? LDS_X : LDS_W];
+    const int group = (int)blockIdx.y - (DX ? a.parts : 0);
+    if (DX && group < 0)
+        head_few_dx<M, Y>(a, (int)blockIdx.y, lds);
+    else if (DW)
+        head_few_dw<M, Y>(a, group, lds);
 }
 
 // Joins the parts of the vocabulary: 256 / ROWS threads a row.
@@ -742,8 +769,8 @@ static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bo
     p.vp = (p.vc + 63) / 64 * 64;
     p.ldz = (p.rests ? 2 : 1) * p.vp;
     p.dz = up256((size_t)T * p.ldz * 2);
-    p.scale = half ? 256 : 0;
     p.few = T <= HEAD_FEW_ROWS && d >= 8;   // (of one piece: 2^20 tokens at most)
+    p.scale = half && !p.few ? 256 : 0;
     if (p.few) {
         const int slabs = (int)((d + 127) / 128), all = (int)((V + 31) / 32);
         p.steps = std::max((all * slabs + 4 * ncu - 1) / (4 * ncu), 8);
@@ -775,25 +802,28 @@ static HeadBackward head_backward(int64_t T, int64_t d, int64_t V, bool half, bo
 
 template <typename M, int Y>
 static void run_head_few(const HeadFew& few, HeadArgs a, const HeadBackward& p, int64_t d, int edge, void* dx, int64_t lddx,
-                         void* dw, int64_t lddw, HeadScale* scale, float* partial, hipStream_t st) {
+                         void* dw, int64_t lddw, float* partial, hipStream_t st) {
     typedef typename M::Elem E;
     a.vp = p.vp;
     a.ldz = p.ldz;
     launch_head<M, true>(few, a, true, edge, st);
-    HeadFewProd g{few.x, few.w, a.dz, a.dzt, few.ldx, few.ldw, p.ldz, p.vp, a.T, a.V, (int)d, p.steps, dw, lddw, partial,
-                  (d + 7) / 8 * 8, narrow_range<E> ? &scale->undo : nullptr};
-    const unsigned slabs = (unsigned)((d + 127) / 128);
-    if (dx) {
-        hipLaunchKernelGGL((k_head_few_dx<M, Y>), dim3(slabs, (unsigned)p.parts), dim3(256), 0, st, g);
+    const int64_t slabs = (d + 127) / 128, units = (a.V + 15) / 16;
+    HeadFewProd g{few.x, few.w, a.dz, a.dzt, few.ldx, few.ldw, p.ldz, p.vp, a.T, a.V, (int)d, dx ? p.parts : 0, p.steps,
+                  (int)std::max<int64_t>(1, std::min<int64_t>(16, units * slabs / (16 * op_cus()))), dw, lddw, partial,
+                  (d + 7) / 8 * 8, a.g_logprob, a.g_entropy};
+    const int64_t groups = dw ? (units + 4 * g.units - 1) / (4 * g.units) : 0;
+    // (of 32 rows dx's LDS would keep half of dW's workgroups out: 32 x 4096 x 32768 174 us, in one launch 204; 16 x 1024 x
+    // 4096 24.0, in one launch 19.6)
+    const dim3 block(256), gx((unsigned)slabs, (unsigned)p.parts), gw((unsigned)slabs, (unsigned)groups);
+    if (Y == 1 && dx && dw) {
+        hipLaunchKernelGGL((k_head_few_prod<M, 1, true, true>), dim3(gx.x, gx.y + gw.y), block, 0, st, g);
+    } else {
+        if (dx) hipLaunchKernelGGL((k_head_few_prod<M, Y, true, false>), gx, block, 0, st, g);
+        if (dw) hipLaunchKernelGGL((k_head_few_prod<M, Y, false, true>), gw, block, 0, st, g);
+    }
+    if (dx)
         hipLaunchKernelGGL(k_head_few_join<E>, dim3((unsigned)((a.T * g.dp + 63) / 64)), dim3(1024), 0, st, g,
                            static_cast<E*>(dx), lddx);
-    }
-    if (dw) {
-        const int64_t units = (a.V + 15) / 16;
-        g.steps = (int)std::max<int64_t>(1, std::min<int64_t>(16, units * slabs / (16 * op_cus())));
-        hipLaunchKernelGGL((k_head_few_dw<M, Y>), dim3(slabs, (unsigned)((units + 4 * g.steps - 1) / (4 * g.steps))), dim3(256), 0,
-                           st, g);
-    }
 }
 
 template <typename M>
@@ -802,16 +832,16 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
                               float* sums, uint16_t* xt, hipStream_t st) {
     typedef typename M::Elem E;
     constexpr bool HALF = narrow_range<E>;
-    if (HALF) {
+    if (HALF && !p.few) {
         hipLaunchKernelGGL(k_head_scale, dim3(1), dim3(1024), 0, st, a.g_logprob, a.g_entropy, a.T, scale);
         a.factor = &scale->factor;
     }
     a.all = V;
     if (p.few) {
         if (a.T <= 16)
-            run_head_few<M, 1>(few, a, p, d, edge, dx, lddx, dw, lddw, scale, static_cast<float*>(partial), st);
+            run_head_few<M, 1>(few, a, p, d, edge, dx, lddx, dw, lddw, static_cast<float*>(partial), st);
         else
-            run_head_few<M, 2>(few, a, p, d, edge, dx, lddx, dw, lddw, scale, static_cast<float*>(partial), st);
+            run_head_few<M, 2>(few, a, p, d, edge, dx, lddx, dw, lddw, static_cast<float*>(partial), st);
         return;
     }
     const Operand w = a.w;
