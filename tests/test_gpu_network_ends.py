@@ -72,7 +72,8 @@ def _within(got, want, tol, label):
 
 # ---------------------------------------------------------------- embedding
 EMBED = [(1, 1, 1, 0, 0), (1, 4096, 1000, 0, 0), (5, 7, 3, 0, 0), (200, 127, 50, 3, 1), (1000, 520, 90, 8, 0),
-         (3000, 64, 20000, 0, 0), (130, 8193, 33, 1, 3), (4097, 96, 2, 0, 0), (70, 1028, 5, 0, 0)]
+         (3000, 64, 20000, 0, 0), (130, 8193, 33, 1, 3), (4097, 96, 2, 0, 0), (70, 1028, 5, 0, 0),
+         (256, 40, 2000, 0, 0), (257, 40, 2000, 0, 0), (255, 640, 7, 0, 0), (300, 1100, 11, 0, 0), (65, 3, 5000, 0, 0)]
 
 
 def _tokens(T, V, seed):
