@@ -959,6 +959,11 @@ def _head_operands(x, w):
     return xp, ldx, T, d, wp, ldw, V, _dtype_code(x.dtype)
 
 
+def _head_key(name, device, xp, ldx, T, d, wp, ldw, V, *more):
+    """What the workspace of a head call depends on: sizes, and whether rows can be staged as they are."""
+    return (name, device.index, T, d, V, (xp | 2 * ldx) & 15 == 0, (wp | 2 * ldw) & 15 == 0, ldx >> 22 or ldw >> 22, *more)
+
+
 def head_logprobs(x, w, target=None, work=None) -> TokenLogprobs:
     """bakron_head_logprobs on the current stream: what token_logprobs gives for the logits x w^T,
     which are never kept.  x: T x d fp16 or bf16 (the rows before the vocabulary matrix); w: V x d, the same
@@ -972,7 +977,7 @@ def head_logprobs(x, w, target=None, work=None) -> TokenLogprobs:
     logprob, entropy, lse = torch.empty(3, T, dtype=torch.float32, device=x.device).unbind(0)
     _run_op(lib.bakron_head_logprobs,
             (xp, ldx, T, d, wp, ldw, V, code, tp, None if tp is None else logprob.data_ptr(), entropy.data_ptr(),
-             lse.data_ptr()), x.device, work, maybe_none=False)
+             lse.data_ptr()), x.device, work, _head_key("head_logprobs", x.device, xp, ldx, T, d, wp, ldw, V))
     return TokenLogprobs(None if tp is None else logprob, entropy, lse)
 
 
@@ -991,7 +996,7 @@ def head_logprobs_backward(x, w, target, lse, entropy=None, g_logprob=None, g_en
              _vector(lse, "lse", T, f32, dev), _vector(entropy, "entropy", T, f32, dev),
              _vector(g_logprob, "g_logprob", T, f32, dev), _vector(g_entropy, "g_entropy", T, f32, dev),
              None if dx is None else dx.data_ptr(), d, None if dw is None else dw.data_ptr(), d), dev, work,
-            maybe_none=False)
+            _head_key("head_logprobs_backward", dev, xp, ldx, T, d, wp, ldw, V, code, need_dx, need_dw))
     return dx, dw
 
 

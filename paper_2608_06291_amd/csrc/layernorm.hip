@@ -164,12 +164,12 @@ struct LnGradArgs {
     float *dw, *db;
     float* part;   // slices x 2 x dp, dp: d rounded up to a multiple of 8
     int64_t lddy, ldx, ldds, lddx, T;
-    int d, slices;
+    int d, slices, dx_blocks;
 };
 
 // dx, a row a group of threads as above.
 template <typename E, int NV>
-__global__ __launch_bounds__(1024) void k_layernorm_dx(LnGradArgs a) {
+__device__ inline void layernorm_dx(const LnGradArgs& a) {
     constexpr int VEC = 16 / sizeof(E);
     __shared__ float red[32];
     const int tid = threadIdx.x, tpr = blockDim.x, lane = tid & 63, wave = tid >> 6;
@@ -238,6 +238,60 @@ __global__ __launch_bounds__(1024) void k_layernorm_dx(LnGradArgs a) {
     }
     if (left < a.d) out[left] = (E)fmaf(gx - sg - nx * sn, r, ds ? (float)ds[left] : 0.0f);
 }
+
+template <typename E, int NV>
+__global__ __launch_bounds__(1024) void k_layernorm_dx(LnGradArgs a) {
+    layernorm_dx<E, NV>(a);
+}
+// Few rows: dx by the first dx_blocks workgroups, dw and db by the others, a vector of columns a thread and all rows.
+// Neither needs the other, nor a join: 1 x 4096 f16 13.8 us a call in two launches with a workspace, 9.6 so.
+template <typename E, int NV>
+__global__ __launch_bounds__(1024) void k_layernorm_few(LnGradArgs a) {
+    constexpr int VEC = 16 / sizeof(E), AHEAD = 4;
+    if ((int)blockIdx.x < a.dx_blocks) return layernorm_dx<E, NV>(a);
+    const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
+    const int c = (((int)blockIdx.x - a.dx_blocks) * threads + tid) * VEC;
+    if (c >= a.d) return;
+    float dw[VEC] = {}, db[VEC] = {};
+    const int T = (int)a.T;
+    if (c + VEC <= a.d) {
+        for (int t0 = 0; t0 < T; t0 += AHEAD) {
+            u32x4 x[AHEAD], g[AHEAD];
+            float mean[AHEAD], r[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int64_t t = min(t0 + i, T - 1);
+                x[i] = load_words(static_cast<const E*>(a.x) + t * a.ldx + c);
+                g[i] = load_words(static_cast<const E*>(a.dy) + t * a.lddy + c);
+                mean[i] = a.mean ? a.mean[t] : 0.0f;
+                r[i] = a.rstd[t];
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (t0 + i < T) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float dy = entry<E>(g[i], j);
+                        dw[j] = fmaf(dy, (entry<E>(x[i], j) - mean[i]) * r[i], dw[j]);
+                        db[j] += dy;
+                    }
+                }
+        }
+    } else {
+        for (int64_t t = 0; t < T; ++t)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (c + j < a.d) {
+                    const float dy = (float)static_cast<const E*>(a.dy)[t * a.lddy + c + j];
+                    const float x = (float)static_cast<const E*>(a.x)[t * a.ldx + c + j];
+                    dw[j] = fmaf(dy, (x - (a.mean ? a.mean[t] : 0.0f)) * a.rstd[t], dw[j]);
+                    db[j] += dy;
+                }
+    }
+    if (a.dw) store_n(a.dw + c, dw, a.d - c);
+    if (a.db) store_n(a.db + c, db, a.d - c);
+}
+constexpr int64_t LN_FEW_ROWS = 32;
 
 // Partial sums of dw and db over a slice of the rows: a thread has VEC columns, the four waves of a
 // workgroup the same columns and every fourth row, joined in LDS.
@@ -516,6 +570,20 @@ static void launch_layernorm_grad(LnGradArgs a, hipStream_t st) {
     constexpr int VEC = 16 / sizeof(E), NV_MAX = 64 / VEC;
     const bool columns = a.dw || a.db;
     if (columns) a.slices = ln_slices(a.T, a.d, sizeof(E));
+    if (columns && a.T <= LN_FEW_ROWS) {
+        const LnGeom g = ln_geom(a.T, a.d, VEC, NV_MAX);
+        const int each = g.tpr * g.rows * VEC;   // columns a workgroup
+        a.dx_blocks = a.dx ? (int)((a.T + g.rows - 1) / g.rows) : 0;
+        const dim3 grid((unsigned)(a.dx_blocks + (a.d + each - 1) / each)), block(g.tpr, g.rows);
+        switch (g.nv) {
+            case 1: hipLaunchKernelGGL((k_layernorm_few<E, 1>), grid, block, 0, st, a); break;
+            case 2: hipLaunchKernelGGL((k_layernorm_few<E, 2>), grid, block, 0, st, a); break;
+            case 4: hipLaunchKernelGGL((k_layernorm_few<E, 4>), grid, block, 0, st, a); break;
+            case 8: hipLaunchKernelGGL((k_layernorm_few<E, 8>), grid, block, 0, st, a); break;
+            default: hipLaunchKernelGGL((k_layernorm_few<E, NV_MAX>), grid, block, 0, st, a); break;
+        }
+        return;
+    }
     if (columns && ln_together(a.d, sizeof(E))) {
         const LnGeom g = ln_geom(1 << 20, a.d, VEC, 2);
         const dim3 grid((unsigned)a.slices), block(g.tpr, g.rows);
@@ -590,7 +658,7 @@ extern "C" bakron_status bakron_layernorm_backward(const void* dy, int64_t lddy,
     bakron_status st = layernorm_sizes(who, dtype, T, d);
     if (st != BAKRON_OK) return st;
     const int esize = dtype == BAKRON_F32 ? 4 : 2;
-    const size_t need = dweight || dbias ? (size_t)bk::ln_slices(T, d, esize) * 2 * ((d + 7) / 8 * 8) * sizeof(float) : 0;
+    const size_t need = (dweight || dbias) && T > bk::LN_FEW_ROWS ? (size_t)bk::ln_slices(T, d, esize) * 2 * ((d + 7) / 8 * 8) * sizeof(float) : 0;
     bool query;
     st = bk::op_workspace(who, work, work_bytes, need, &query);
     if (st != BAKRON_OK || query) return st;
@@ -602,7 +670,7 @@ extern "C" bakron_status bakron_layernorm_backward(const void* dy, int64_t lddy,
     if (T > 0 && (!dy || !x || !rstd)) return bk::op_fail(who, "null pointer");
     if (T == 0 && !dweight && !dbias) return BAKRON_OK;
     bk::LnGradArgs a{dy, x, d_sum, weight, mean, rstd, T > 0 ? dx : nullptr, dweight, dbias, static_cast<float*>(work),
-                     lddy, ldx, ldds, lddx, T, (int)d, 0};
+                     lddy, ldx, ldds, lddx, T, (int)d, 0, 0};
     if (dtype == BAKRON_F32)
         bk::launch_layernorm_grad<float>(a, stream);
     else if (dtype == BAKRON_F16)

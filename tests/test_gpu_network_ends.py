@@ -150,7 +150,8 @@ def test_embedding_backward(dtype, T, d, V, pad, shift):
 # ---------------------------------------------------------------- layer norm
 NORM = [(1, 1, False, 0, 0), (1, 4096, True, 0, 0), (3, 127, True, 0, 0), (5, 128, False, 3, 1), (130, 1000, True, 0, 0),
         (2, 8191, True, 1, 3), (1030, 520, True, 8, 0), (1100, 2049, False, 0, 0), (1, 32768, True, 0, 0),
-        (2, 65536, False, 0, 0), (257, 7, True, 0, 0), (40, 16384, True, 0, 0)]
+        (2, 65536, False, 0, 0), (257, 7, True, 0, 0), (40, 16384, True, 0, 0),
+        (32, 1001, True, 0, 0), (33, 1001, True, 0, 0), (31, 70, True, 3, 1)]
 
 
 @pytest.mark.parametrize("centre", [True, False])

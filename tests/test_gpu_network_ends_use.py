@@ -395,3 +395,20 @@ def test_head_beyond_32_bits(T, d, V):
         p = torch.exp(z - lp.lse.double()[:, None]) - (tok[:, None] == torch.arange(V, device=DEV)[v][None]).double()
         want = p.t().contiguous() @ x[:, d - 64:].double()
         assert float((dw[v, d - 64:].double() - want).norm()) <= 0.85 * 2.0 ** -8 * float(want.norm()), v
+
+
+def test_workspaces_of_calls_that_differ_in_alignment_only():
+    """The binding keeps the sizes that it has asked for: rows that have to be copied need more."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("kept sizes")
+    T, d, V = 100, 128, 3000
+    x, w, tok, _, _, gl = _inputs(T, d, V)
+    want = pk.head_logprobs(x, w, tok)
+    grads = pk.head_logprobs_backward(x, w, tok, want.lse, g_logprob=gl)
+    for px, pw in ((0, 1), (1, 0), (8, 8), (3, 3), (0, 0)):
+        xs, ws = (torch.empty((n, d + p), dtype=x.dtype, device=DEV)[:, p // 2:p // 2 + d] for n, p in ((T, px), (V, pw)))
+        xs.copy_(x), ws.copy_(w)
+        assert all(torch.equal(a, b) for a, b in zip(pk.head_logprobs(xs, ws, tok)[:3], want[:3]))
+        got = pk.head_logprobs_backward(xs, ws, tok, want.lse, g_logprob=gl)
+        assert all(torch.equal(a, b) for a, b in zip(got, grads))

@@ -63,7 +63,7 @@ def test_layernorm_refuses(lib, change):  # noqa: F811
 @pytest.mark.parametrize("change", SIZES + [
     dict(d=65537, ldx=1 << 17, lddy=1 << 17, ldds=1 << 17, lddx=1 << 17), dict(lddy=63), dict(ldx=63), dict(ldds=63), dict(lddx=63),
     dict(ds=P, ldds=65), dict(dx=None), dict(T=1, dy=None), dict(T=1, x=None), dict(T=1, rstd=None), dict(T=1 << 26),
-    dict(T=5, dw=P, size=_size(10)), dict(T=5, db=P, work=ctypes.c_void_p(4104))])
+    dict(T=50, dw=P, size=_size(10)), dict(T=50, db=P, work=ctypes.c_void_p(4104))])
 def test_layernorm_backward_refuses(lib, change):  # noqa: F811
     base = dict(LNB_OK, size=_size(BIG))
     assert _call(lib.bakron_layernorm_backward, LNB, base) == 0
@@ -100,7 +100,7 @@ def test_workspace_sizes(lib, name):  # noqa: F811
     for T in (1, 40, 700, 20000):
         need = ctypes.c_size_t(0)
         assert _call(fn, names, dict(base, T=T, work=None, size=ctypes.byref(need))) == 0
-        if name == "bakron_embedding_backward" and T <= 256:
+        if T <= {"bakron_embedding_backward": 256, "bakron_layernorm_backward": 32}.get(name, 0):
             assert need.value == 0
             continue
         assert need.value > 0
