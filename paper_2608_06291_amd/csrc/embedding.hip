@@ -56,6 +56,8 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
     if (left < hi) out[left] = asked ? (E)((float)row[left] * a.scale) : (E)0.0f;
 }
 
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+
 // Positions sorted by token, equal tokens in rising order; tokens outside [0, V) behind all others.
 struct SortArgs {
     const int64_t* token;
@@ -94,7 +96,6 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void k_embed_sort(SortArgs a) {
         const int32_t* const k = &keys[wave][half * 32];
         // (keys below, or equal ones, of earlier positions: below `mine + 1`)
         const int32_t bound = first < t0 ? mine + 1 : mine;
-        typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
             const i32x4_t o4 = *reinterpret_cast<const i32x4_t*>(k + j);
@@ -132,25 +133,37 @@ __global__ __launch_bounds__(1024) void k_sort_count(SortArgs a) {
     __syncthreads();
     for (int i = threadIdx.x; i < SORT_BINS; i += 1024) a.count[(int64_t)i * a.blocks + blockIdx.x] = bins[i];
 }
-// One workgroup: each thread takes SORT_BINS / 1024 digits.
+// One workgroup goes through the counts, four a thread at a time.
 __global__ __launch_bounds__(1024) void k_sort_scan(SortArgs a) {
-    __shared__ int32_t sums[1024];
-    const int64_t each = (int64_t)(SORT_BINS / 1024) * a.blocks;
-    int32_t* const c = a.count + threadIdx.x * each;
-    int32_t sum = 0;
-    for (int64_t i = 0; i < each; ++i) sum += c[i];
-    sums[threadIdx.x] = sum;
-    for (int n = 1; n < 1024; n *= 2) {
+    __shared__ int32_t sums[2][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t n = (int64_t)SORT_BINS * a.blocks;   // (a multiple of 2048)
+    int32_t before = 0;
+    const i32x4_t none = {0, 0, 0, 0};
+    auto at = [&](int64_t i) { return reinterpret_cast<i32x4_t*>(a.count) + i; };
+    i32x4_t next = threadIdx.x < n / 4 ? *at(threadIdx.x) : none;
+    int turn = 0;
+    for (int64_t i = threadIdx.x; i - threadIdx.x < n / 4; i += 1024, turn ^= 1) {
+        i32x4_t c = next;
+        next = i + 1024 < n / 4 ? *at(i + 1024) : none;
+        const int32_t own = c[0] + c[1] + c[2] + c[3];
+        int32_t sum = own;
+#pragma unroll
+        for (int k = 1; k < 64; k *= 2) {
+            const int32_t v = __shfl_up(sum, k);
+            if (lane >= k) sum += v;
+        }
+        if (lane == 63) sums[turn][wave] = sum;
         __syncthreads();
-        const int32_t v = (int)threadIdx.x >= n ? sums[threadIdx.x - n] : 0;
-        __syncthreads();
-        sums[threadIdx.x] += v;
-    }
-    int32_t at = sums[threadIdx.x] - sum;
-    for (int64_t i = 0; i < each; ++i) {
-        const int32_t n = c[i];
-        c[i] = at;
-        at += n;
+        int32_t first = before + sum - own;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            const int32_t v = sums[turn][w];
+            if (w < wave) first += v;
+            before += v;
+        }
+        const i32x4_t o = {first, first + c[0], first + c[0] + c[1], first + c[0] + c[1] + c[2]};
+        if (i < n / 4) *at(i) = o;
     }
 }
 // A wave takes 64 SORT_EACH positions in a row, 64 at a time; those of equal digits find each other by ballots.
@@ -208,10 +221,16 @@ struct EmbedGradArgs {
     float* part;               // what a chunk leaves of the range it begins in, and of the one it ends in: chunks x 2 x dp
     int64_t lddy, ldb, ldo, T, V, dp;
     int d, chunk_blocks, lanes;   // threads a row
+    int past;                  // the gradient is written past the caches
     float scale;
 };
 // Sorted positions of a chunk.
 constexpr int EMBED_CHUNK = 16;
+
+// A gradient that the last-level cache (256 MB) would not hold with anything beside it is written past the caches:
+// 8192 x 4096 into 32768 rows (268 MB) 82 -> 72 us, 65536 x 1024 into 131072 rows 167 -> 144.  A smaller one is left to
+// whoever reads it next.
+constexpr int64_t EMBED_PAST = (int64_t)128 << 20;
 
 // A row is read and written in whole vectors (WHOLE: d is a multiple of them), or its last entries one by one: `n` of
 // them are left from this vector on.
@@ -238,7 +257,17 @@ __device__ inline void embed_write(const EmbedGradArgs& a, int64_t v, int c, int
     }
 #pragma unroll
     for (int j = 0; j < VEC; ++j) o[j] = fmaf(s[j], a.scale, o[j]);
-    store_n(static_cast<E*>(a.out) + v * a.ldo + c, o, WHOLE ? VEC : n);
+    E* const out = static_cast<E*>(a.out) + v * a.ldo + c;
+    if (a.past && (WHOLE || n >= VEC)) {
+        Pack<E, VEC> p;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) p.v[j] = (E)o[j];
+        u32x4 u;
+        __builtin_memcpy(&u, &p, 16);
+        store_words_past(out, u);
+    } else {
+        store_n(out, o, WHOLE ? VEC : n);
+    }
 }
 
 // A chunk of the sorted positions is summed by `lanes` threads, a vector of the row each.  Where a token's whole range
@@ -553,7 +582,7 @@ extern "C" bakron_status bakron_embedding_backward(const void* dy, int64_t lddy,
     char* const part = at + w.bytes() - w.part;
     const bk::EmbedGradArgs a{dy, base, dtable, reinterpret_cast<int32_t*>(at), reinterpret_cast<int32_t*>(at + w.keys),
                               reinterpret_cast<int32_t*>(part - w.start), reinterpret_cast<float*>(part), lddy, ldb, ldo,
-                              T, V, w.dp, (int)d, 0, 0, scale};
+                              T, V, w.dp, (int)d, 0, 0, V * d * (dtype == BAKRON_F32 ? 4 : 2) >= bk::EMBED_PAST, scale};
     if (dtype == BAKRON_F32)
         bk::launch_embed_grad<float>(a, tokens, stream);
     else if (dtype == BAKRON_F16)
