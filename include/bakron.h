@@ -783,7 +783,7 @@ bakron_status bakron_layernorm(const void *x, int64_t ldx, const void *residual,
  *   dx            device output, T x d of dtype, or NULL; may be d_sum with the same leading
  *                 dimension
  *   dweight, dbias  device outputs, d floats, or NULL.  T = 0 gives zeros
- * 1 <= d <= 65536.  Workspace as above.
+ * 1 <= d <= 65536.  Workspace as above (none for T <= 32, or without dweight and dbias).
  */
 bakron_status bakron_layernorm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx,
                                         int32_t dtype, int64_t T, int64_t d, const float *weight,
@@ -808,12 +808,14 @@ bakron_status bakron_embedding(const int64_t *tokens, int64_t T, const void *tab
 /*
  * bakron_embedding_backward -- the table's gradient:
  *   dtable_v = base_v + scale * sum_{t: tokens_t = v} dy_t
- * The sums run in fp32 over rising t and are rounded once.  Rows without a token are base, or zeros.
+ * The sums are fp32 and rounded once; their order depends on the tokens alone (sums over at most
+ * 16 rising t, added up in rising order).  Rows without a token are base, or zeros.
  *   dy      device, T x d of dtype
  *   base    device, V x d of dtype, or NULL for 0: e.g. the gradient of the same matrix at the
  *           other end of the network
  *   dtable  device output, V x d of dtype; may be base with the same leading dimension
- * Sizes as bakron_embedding.  Workspace as above.
+ * T <= 2^20, 1 <= V <= 2^20, 1 <= d <= 65536.  Workspace as above (none for T <= 256: one launch,
+ * and three beyond, eight beyond 16384).
  */
 bakron_status bakron_embedding_backward(const void *dy, int64_t lddy, const int64_t *tokens,
                                         int64_t T, int32_t dtype, int64_t V, int64_t d,
