@@ -711,7 +711,7 @@ bakron_status bakron_token_logprobs_backward(const void *logits, int64_t ld, int
  * 1 <= d <= 2^17, 1 <= V <= 2^20, T <= 2^27, ceil(T / 64) ceil(max(d, V) / 64) < 2^23
  * (or BAKRON_EINVAL).  Workspace as above: 16 bytes a row for 32 to 256 tokens of the
  * vocabulary, and padded copies of x and w where their rows are no 16-byte multiples
- * at 16-byte addresses and T > 32.
+ * at 16-byte addresses (not for T <= 8, nor for T <= 32 with d no multiple of 8).
  */
 bakron_status bakron_head_logprobs(const void *x, int64_t ldx, int64_t T, int64_t d, const void *w,
                                    int64_t ldw, int64_t V, int32_t dtype, const int64_t *target,

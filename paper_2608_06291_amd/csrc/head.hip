@@ -620,12 +620,16 @@ __global__ __launch_bounds__(256) void k_head_join(HeadJoinArgs a) {
     if (a.entropy) a.entropy[t] = empty ? 0.0f : log_s - p.s1 / p.s;
 }
 
-// Rows up to which the product is taken as one of few rows; and with few tiles (by 64 x 64) a CU and a
-// long way to sum.
+// Whether the logits are taken by the kernel for few rows.  Up to 8 rows always (4096 x 32768, one row 50 us, in tiles 58);
+// up to 32 where there are fewer tiles (by 64 x 64) than CUs (32 x 2048 x 8192 15.8 us, in tiles 18.1; but 32 x 4096 x 131072
+// 221 against 182), and where tiles would need padded copies of all rows, by their length (so that the order of
+// sums depends on sizes alone).  More rows with fewer tiles still and a long way to sum: 100 x 2048 x 1000 (32) 19.1 and in tiles 20;
+// 300 x 4096 x 2000 (160) 54 against 32.
 constexpr int64_t HEAD_FEW_ROWS = 32, HEAD_FEW_TILES = 4;
 static bool head_few_rows(int64_t T, int64_t V, int64_t d) {
-    if (T <= HEAD_FEW_ROWS) return true;
-    return ((V + 63) / 64) * ((T + 63) / 64) * HEAD_FEW_TILES <= op_cus() && d >= 512;
+    const int64_t tiles = ((V + 63) / 64) * ((T + 63) / 64);
+    if (T <= HEAD_FEW_ROWS) return T <= 8 || d % 8 != 0 || tiles < op_cus();
+    return tiles * HEAD_FEW_TILES <= op_cus() && d >= 512;
 }
 // Units of 16 tokens that a workgroup of that kernel takes.  More of them share the rows of x: 32 x 4096 x 131072 with
 // one unit 362 us, two 263, four 218, 16 rows of 2048 136, 108, 102.  With fewer rows x costs nothing, and long rows of w
@@ -992,7 +996,7 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     if ((dx && lddx < d) || (dw && lddw < d)) return bk::op_fail(who, "leading dimension below d");
     const bk::HeadBackward b = bk::head_backward(std::max<int64_t>(T, 1), d, V, dtype == BAKRON_F16, dx != nullptr,
                                                  dw != nullptr, bk::op_cus());
-    const bool many = !bk::head_few_rows(T, b.vc, d);
+    const bool many = !b.few && !bk::head_few_rows(T, b.vc, d);
     const bk::HeadPad p = bk::head_pad(x, ldx, w, ldw, T, d, V, many || (dw && !b.few), many || (dx && !b.few));
     bool query;
     st = bk::op_workspace(who, work, work_bytes, p.xbytes + p.wbytes + b.dz + b.dzt + b.partial + b.sums + b.scale + b.xt,
@@ -1025,7 +1029,7 @@ extern "C" bakron_status bakron_head_logprobs_backward(const void* x, int64_t ld
     a.dzt = b.dzt ? to + b.dz : nullptr;
     bk::head_operands(a, p, x, ldx, w, ldw, d, static_cast<char*>(work), stream);
     const bk::HeadFew few{x, w, ldx, ldw, (int)d};
-    const int edge = bk::head_edge(T, b.vc, d);
+    const int edge = b.few ? 16 * bk::head_units(T, V, d) : bk::head_edge(T, b.vc, d);
     if (dtype == BAKRON_BF16)
         bk::run_head_backward<bk::MmaBF16>(few, a, b, d, V, !many, edge, dx, lddx, dw, lddw, scale, partial,
                                            reinterpret_cast<float*>(sums), xt, stream);
