@@ -21,41 +21,41 @@ struct EmbedArgs {
     const void* table;
     void* y;
     int64_t ldt, ldy, T, V;
-    int d, pieces;   // of a row
+    int d, pieces, lanes;   // pieces of a row; threads a row
     float scale;
 };
 
 constexpr int EMBED_NV = 4;   // vectors a thread has in flight
 
-// A workgroup of 256 threads takes one piece of one row.
+// `lanes` threads take one piece of one row; of short rows a workgroup takes several.
 template <typename E>
 __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
-    constexpr int VEC = 16 / sizeof(E), LEN = 256 * EMBED_NV * VEC;
-    const int64_t t = blockIdx.x / (uint32_t)a.pieces;
-    const int lo = (int)(blockIdx.x % (uint32_t)a.pieces) * LEN;
-    const int hi = min(a.d, lo + LEN), whole = (hi - lo) / VEC;
+    constexpr int VEC = 16 / sizeof(E);
+    const int len = a.lanes * EMBED_NV * VEC, lane = (int)threadIdx.x % a.lanes;
+    const int64_t t = (int64_t)(blockIdx.x / (uint32_t)a.pieces) * (256 / a.lanes) + threadIdx.x / a.lanes;
+    if (t >= a.T) return;
+    const int lo = (int)(blockIdx.x % (uint32_t)a.pieces) * len;
+    const int hi = min(a.d, lo + len), whole = (hi - lo) / VEC;
     const int64_t k = a.token[t];
     const bool asked = k >= 0 && k < a.V;
     const E* const row = static_cast<const E*>(a.table) + (asked ? k : 0) * a.ldt;
     E* const out = static_cast<E*>(a.y) + t * a.ldy;
     u32x4 r[EMBED_NV];
 #pragma unroll
-    for (int i = 0; i < EMBED_NV; ++i) r[i] = u32x4(0);
-    if (asked && whole > 0) {
-#pragma unroll
-        for (int i = 0; i < EMBED_NV; ++i)
-            r[i] = load_words(row + lo + min(i * 256 + (int)threadIdx.x, whole - 1) * VEC);
+    for (int i = 0; i < EMBED_NV; ++i) {
+        r[i] = u32x4(0);
+        if (asked && i * a.lanes < whole) r[i] = load_words(row + lo + min(i * a.lanes + lane, whole - 1) * VEC);
     }
 #pragma unroll
     for (int i = 0; i < EMBED_NV; ++i) {
-        const int v = i * 256 + (int)threadIdx.x;
+        const int v = i * a.lanes + lane;
         if (v >= whole) break;
         Pack<E, VEC> o;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) o.v[j] = asked ? (E)(entry<E>(r[i], j) * a.scale) : (E)0.0f;
         store_pack(out + lo + v * VEC, o);
     }
-    const int left = lo + whole * VEC + (int)threadIdx.x;
+    const int left = lo + whole * VEC + lane;
     if (left < hi) out[left] = asked ? (E)((float)row[left] * a.scale) : (E)0.0f;
 }
 
@@ -446,9 +446,12 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGradArgs a, const int64_
 
 template <typename E>
 static void launch_embed(EmbedArgs a, hipStream_t st) {
-    const int len = 256 * EMBED_NV * 16 / (int)sizeof(E);
+    constexpr int VEC = 16 / (int)sizeof(E);
+    a.lanes = VEC;   // (what is left of a row, less than a vector, goes one entry a thread)
+    while (a.lanes < 256 && a.lanes * VEC < a.d) a.lanes *= 2;
+    const int len = a.lanes * EMBED_NV * VEC, rows = 256 / a.lanes;
     a.pieces = (a.d + len - 1) / len;
-    hipLaunchKernelGGL(k_embed<E>, dim3((unsigned)(a.T * a.pieces)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_embed<E>, dim3((unsigned)((a.T + rows - 1) / rows * a.pieces)), dim3(256), 0, st, a);
 }
 // The workspace of the gradient.
 struct EmbedWork {
@@ -556,7 +559,7 @@ extern "C" bakron_status bakron_embedding(const int64_t* tokens, int64_t T, cons
     if (T > bk::OP_LAUNCH_MAX / 256 / ((d + len - 1) / len)) return bk::op_fail(who, "too many rows for one call");
     if (T == 0) return BAKRON_OK;
     if (!tokens || !table || !y) return bk::op_fail(who, "null pointer");
-    const bk::EmbedArgs a{tokens, table, y, ldt, ldy, T, V, (int)d, 0, scale};
+    const bk::EmbedArgs a{tokens, table, y, ldt, ldy, T, V, (int)d, 0, 0, scale};
     if (dtype == BAKRON_F32)
         bk::launch_embed<float>(a, stream);
     else if (dtype == BAKRON_F16)

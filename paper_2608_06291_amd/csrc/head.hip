@@ -76,7 +76,7 @@ __global__ __launch_bounds__(1024) void k_head_scale(const float* __restrict__ g
     *out = head_scale(m);
 }
 
-// The same by every workgroup itself, for up to 64 rows (all lanes of the wave): one launch less.
+// The same by every wave itself, for up to 64 rows (all its lanes have to be active): one launch less.
 __device__ inline HeadScale head_scale_few(const float* g, const float* gh, int64_t T, int lane) {
     float b = 0.0f;
     if (lane < T) b = (g ? fabsf(g[lane]) : 0.0f) + (gh ? 4.0f * fabsf(gh[lane]) : 0.0f);
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_head(HeadArgs a) {
             const HeadPart p = head_part(z);
             if (lane < 16) parts[Tl::a0(wave) / PART * Tl::COLS + col] = p;
             const int64_t t = t0 + col, k = a.target && t < a.T ? a.target[t] : -1;
-            const int64_t in = k < a.V ? k - first : -1;   // of this lane's 16 x UA tokens: 16 x + r
+            const int64_t in = k >= 0 && k < a.V ? k - first : -1;   // this lane's tokens: 16 x + r
             if (__any(in >= 0 && in < PART)) {
 #pragma unroll
                 for (int j = 0; j < Tl::UA * 4; ++j)
