@@ -16,7 +16,8 @@
 // 10130 to 10520 us, 1255 to 1302 TFLOP/s (a piece: logits and dz 435, dx 404, dW 447), of the second 1350 to 1395.  dz's and dW's
 // stores overlap nothing (one workgroup a CU, all at the end of a round): 20 and 8% of those kernels' time.
 // Few rows are bound by reading w: one row of 4096 x 32768 42 us (6.3 TB/s of 268 MB) and 5 for the join, 32 rows of 4096 x
-// 131072 215; gradients of one row 135 us (w twice, dW once: 805 MB, 6.0 TB/s), of 32 175.
+// 131072 182; gradients of one row of 4096 x 32768 135 us (w twice, dW once: 805 MB, 6.0 TB/s), of 32 175, of 64 224, of
+// 256 284.
 #include "product.h"
 
 namespace bk {
@@ -765,7 +766,11 @@ __global__ __launch_bounds__(256) void k_transpose(const char* x, int64_t ld, in
 //
 // dW's product reads x and dz by columns (transposing reads).  For many pieces and rows x is transposed once instead, which
 // costs 17 us there: 10350 -> 10130 us, 2048 x 4096 x 32768 1372 -> 1349.
-constexpr int64_t HEAD_PIECE_BYTES = (int64_t)128 << 20;
+//
+// A dW that the last-level cache would not hold with anything beside it is written past it, or w would be swept out of it
+// and what follows wait for it to be written: 65 x 4096 x 32768 254 -> 190 us, 256 rows 326 -> 287, 100 x 2048 x 100000 418 ->
+// 352, 2048 rows and more no difference.
+constexpr int64_t HEAD_PIECE_BYTES = (int64_t)128 << 20, HEAD_PAST = (int64_t)128 << 20;
 struct HeadBackward {
     int64_t vc, vp, ldz;   // tokens of a piece (all but the last), padded; row of dz
     bool rests, few;       // few: the kernels for few rows; dx in `parts` of `steps` x 32 tokens
@@ -920,12 +925,15 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
             else
                 launch_prod<M, true, false>(gx, plan, partial, st);
         }
-        if (dw && p.tp) {
-            gw.a = operand(xt, 2 * p.tp, cols, 2 * p.tp);
-            launch_prod<M, false, true>(gw, p.dw, partial, st);
-        } else if (dw) {
-            launch_prod<M, true, true>(gw, p.dw, partial, st);
-        }
+        if (!dw) continue;
+        const bool past = 2 * V * d >= HEAD_PAST;
+        if (p.tp) gw.a = operand(xt, 2 * p.tp, cols, 2 * p.tp);
+        if (p.tp)
+            past ? launch_prod<M, false, true, false, true>(gw, p.dw, partial, st)
+                 : launch_prod<M, false, true>(gw, p.dw, partial, st);
+        else
+            past ? launch_prod<M, true, true, false, true>(gw, p.dw, partial, st)
+                 : launch_prod<M, true, true>(gw, p.dw, partial, st);
     }
 }
 

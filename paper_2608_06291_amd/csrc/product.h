@@ -75,7 +75,8 @@ struct ProdArgs {
     bool first, last;
 };
 
-template <typename E, bool ACC>
+// PAST: whole vectors are stored past the caches.
+template <typename E, bool ACC, bool PAST = false>
 __device__ inline void prod_store(const ProdArgs& a, int64_t t, int64_t i, float undo, float (&v)[8]) {
     if (t >= a.end || (t >= a.split && t < a.split2)) return;
     if constexpr (ACC) {
@@ -93,11 +94,20 @@ __device__ inline void prod_store(const ProdArgs& a, int64_t t, int64_t i, float
     }
     E* const row = t < a.split ? static_cast<E*>(a.out) + t * a.ldo
                                : static_cast<E*>(a.out2) + (t - a.split2) * a.ldo;
-    store_n(row + i, v, a.d - i);
+    if (PAST && a.d - i >= 8) {
+        Pack<E, 8> o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o.v[j] = (E)v[j];
+        u32x4 u;
+        __builtin_memcpy(&u, &o, 16);
+        store_words_past(row + i, u);
+    } else {
+        store_n(row + i, v, a.d - i);
+    }
 }
 
 // Workgroup `block` of a product.
-template <typename Tl, bool ACC>
+template <typename Tl, bool ACC, bool PAST>
 __device__ inline void prod_tile(const ProdArgs& a, int block, char* lds) {
     typedef typename Tl::Mma::Elem E;
     int ti, tt, part = 0, chunks = a.chunks;
@@ -133,16 +143,16 @@ __device__ inline void prod_tile(const ProdArgs& a, int block, char* lds) {
                 if (a.parts > 1)
                     store_n(a.partial + (part * a.end + t) * a.dp + i, v, 8);
                 else
-                    prod_store<E, ACC>(a, t, i, undo, v);
+                    prod_store<E, ACC, PAST>(a, t, i, undo, v);
             }
         }
     }
 }
 
-template <typename Tl, bool ACC>
+template <typename Tl, bool ACC, bool PAST>
 __global__ __launch_bounds__(Tl::THREADS) void k_prod(ProdArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
-    prod_tile<Tl, ACC>(a, (int)blockIdx.x, lds);
+    prod_tile<Tl, ACC, PAST>(a, (int)blockIdx.x, lds);
 }
 // Two products in one launch: the first `first` workgroups are the one's.
 template <typename Ta, typename Tb>
@@ -150,9 +160,9 @@ __global__ __launch_bounds__(Ta::THREADS) void k_prod_two(ProdArgs a, ProdArgs b
     static_assert(Ta::THREADS == Tb::THREADS && Ta::LDS == Tb::LDS, "tiles of one size");
     __shared__ __attribute__((aligned(1024))) char lds[Ta::LDS];
     if ((int)blockIdx.x < first)
-        prod_tile<Ta, false>(a, (int)blockIdx.x, lds);
+        prod_tile<Ta, false, false>(a, (int)blockIdx.x, lds);
     else
-        prod_tile<Tb, false>(b, (int)blockIdx.x - first, lds);
+        prod_tile<Tb, false, false>(b, (int)blockIdx.x - first, lds);
 }
 
 // Sums the parts, in their order.
@@ -308,7 +318,7 @@ static void launch_two(ProdArgs a, ProdArgs b, const ProdPlan& pa, const ProdPla
             hipLaunchKernelGGL((k_prod_join<typename M::Elem, false>), grid256(g->end * (g->dp / 8)), dim3(256), 0, st, *g);
 }
 
-template <typename M, bool ACOLS, bool BCOLS, bool ACC = false>
+template <typename M, bool ACOLS, bool BCOLS, bool ACC = false, bool PAST = false>
 static void launch_prod(ProdArgs a, const ProdPlan& p, void* partial, hipStream_t st) {
     a.parts = p.parts;
     a.part_chunks = p.part_chunks;
@@ -318,7 +328,7 @@ static void launch_prod(ProdArgs a, const ProdPlan& p, void* partial, hipStream_
         typedef decltype(tile) Tl;
         a.ni = (int)((a.a.n + Tl::ROWS - 1) / Tl::ROWS);
         a.nt = (int)((a.b.n + Tl::COLS - 1) / Tl::COLS);
-        hipLaunchKernelGGL((k_prod<Tl, ACC>), dim3((unsigned)(a.ni * a.nt * a.parts)), dim3(Tl::THREADS), 0, st,
+        hipLaunchKernelGGL((k_prod<Tl, ACC, PAST>), dim3((unsigned)(a.ni * a.nt * a.parts)), dim3(Tl::THREADS), 0, st,
                            a);
     };
     if (p.tile == 256)
