@@ -23,6 +23,12 @@ from dataclasses import dataclass, field
 from . import _lib
 
 
+def _rows(t):
+    """t without a graph, in rows that the operators read."""
+    t = t.detach()
+    return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
+
+
 @dataclass
 class GatedMLP:
     """The block in 16-bit floats.  norm: d fp32; w_gate, w_up: f x d; w_down: d x f."""
@@ -46,7 +52,8 @@ class GatedMLP:
 
     def gradients(self, x, y, b, need_dw: bool = True):
         """(dx, dw_gate, dw_up, dnorm) from b, the gradient with respect to the block's output; dnorm in fp32.
-        need_dw=False: the matrices stay as they are (None)."""
+        need_dw=False: the matrices stay as they are (None).  x and b may be of any strides."""
+        x, b = _rows(x), _rows(b)
         dy, dw_gate, dw_up = _lib.gated_mlp_backward(b @ self.w_down, y, self.w_gate, self.w_up, act=self.act,
                                                      need_dw=need_dw)
         rstd = _lib.layernorm(x, eps=self.eps, centre=False).rstd

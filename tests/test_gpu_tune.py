@@ -78,3 +78,21 @@ def test_step_and_command():
     net.step(r["text"], r["target"], 0.25)
     assert torch.equal(net.table, (before[0].float() - 0.25 * g["table"].float()).to(before[0].dtype))
     assert torch.equal(net.block.norm, before[1] - 0.25 * g["norm"]) and torch.equal(net.final, before[2] - 0.25 * g["final"])
+
+
+def test_block_gradients_of_any_layout():
+    """Transposed, broadcast and graph-bearing rows give what contiguous ones do."""
+    import torch
+    net = _network(90, 72, 104, 3)
+    gen = torch.Generator().manual_seed(4)
+    x, b = ((torch.randn((40, 72), generator=gen) * 0.5).to(torch.bfloat16).to("cuda:0") for _ in range(2))
+    y = net.block.forward(x)[1]
+    want = net.block.gradients(x, y, b)
+    flat = b[:1].expand(40, 72)
+    want_flat = net.block.gradients(x, y, flat.contiguous())
+    turned = lambda t: t.t().contiguous().t()
+    for got, ref in ((net.block.gradients(turned(x), y, turned(b)), want), (net.block.gradients(x, y, flat), want_flat),
+                     (net.block.gradients(x.clone().requires_grad_(), y, b), want)):
+        for g, r in zip(got, ref):
+            assert torch.equal(g, r) and not g.requires_grad
+    assert all(torch.equal(g, r) for g, r in zip(net.block.backward(turned(x), y, turned(b)), want[:3]))
