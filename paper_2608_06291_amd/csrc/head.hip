@@ -425,19 +425,20 @@ struct HeadFewProd {
     float* partial;            // dx: parts x T x dp
     int64_t dp;
     const float *g, *gh;
+    int slabs, rows;           // of 128 columns; parts of dx and groups of dW
 };
 
 // dW: a wave holds 128 columns of x, of all rows, as 8 operands and goes through `units` units of 16 tokens.
-// The results go through LDS, so that a store writes 256 bytes of each of four rows, and past the caches, which dW would
-// only sweep: 32768 x 4096 from one row, with dz, 97 us (through the caches 124; 64 bytes of 16 rows as the lanes hold them
-// 161).
+// The results go through LDS, so that a store writes 256 bytes of each of four rows, and past the caches where dW would
+// only sweep them (PAST): 32768 x 4096 from one row, with dz, 97 us (through the caches 124; 64 bytes of 16 rows as the lanes
+// hold them 161).
 // A summed axis of 32 holds the rows of x and, up to 16 of them, the same again for dz's rests.
-template <typename M, int Y>
-__device__ inline void head_few_dw(const HeadFewProd& a, int group, char* lds) {
+template <typename M, int Y, bool PAST>
+__device__ inline void head_few_dw(const HeadFewProd& a, int slab, int group, char* lds) {
     typedef typename M::Elem E;
     E (*const rows)[16][136] = reinterpret_cast<E (*)[16][136]>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
-    const int c0 = (int)blockIdx.x * 128;
+    const int c0 = slab * 128;
     const int64_t first = ((int64_t)group * 4 + wave) * a.units * 16;
     if (first >= a.V) return;
     i32x4 x[8];
@@ -484,7 +485,10 @@ __device__ inline void head_few_dw(const HeadFewProd& a, int group, char* lds) {
             if (v >= a.V || c >= a.d) continue;
             E* const out = static_cast<E*>(a.dw) + v * a.lddw + c;
             if (c + 8 <= a.d) {
-                store_words_past(out, o);
+                if constexpr (PAST)
+                    store_words_past(out, o);
+                else
+                    __builtin_memcpy(out, &o, 16);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -524,12 +528,12 @@ __global__ __launch_bounds__(1024) void k_head_few_join(HeadFewProd a, E* dx, in
 // with the tokens along (one permutation of two registers a pair), operand m having column 8 i + m as its row i.
 // The waves of a workgroup share its steps and meet in LDS, the workgroups' parts in a second launch.
 template <typename M, int Y>
-__device__ inline void head_few_dx(const HeadFewProd& a, int part, char* lds) {
+__device__ inline void head_few_dx(const HeadFewProd& a, int slab, int part, char* lds) {
     typedef typename M::Elem E;
     f32x4 (*const sums)[8 * Y][64] = reinterpret_cast<f32x4 (*)[8 * Y][64]>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
     // (past the row its last 8 columns, twice the same results)
-    const int c = min((int)blockIdx.x * 128 + r16 * 8, a.d - 8);
+    const int c = min(slab * 128 + r16 * 8, a.d - 8);
     const int all = (a.V + 31) / 32, s0 = part * a.steps, s1 = min(all, s0 + a.steps);
     const E* const w = static_cast<const E*>(a.w) + c;
     const E* dz[Y];
@@ -588,7 +592,7 @@ __device__ inline void head_few_dx(const HeadFewProd& a, int part, char* lds) {
         if (t >= a.T) break;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int col = (int)blockIdx.x * 128 + (kq * 4 + r) * 8;
+            const int col = slab * 128 + (kq * 4 + r) * 8;
             if (col >= a.d) break;
             float o[8];
 #pragma unroll
@@ -598,16 +602,20 @@ __device__ inline void head_few_dx(const HeadFewProd& a, int part, char* lds) {
     }
 }
 
-// DX and DW: both in one launch, the first `parts` rows of workgroups being dx's.
-template <typename M, int Y, bool DX, bool DW>
+// DX and DW: both in one launch, the parts of dx first.  Every eighth workgroup runs on the same XCD: those have
+// all slabs of a part or group, so that a line of W or dW that two slabs share is fetched, or joined, in one L2 (gradients
+// of 1 x 1001 x 70000 130 -> 111 us, 32 x 1024 x 70000 131 -> 121).
+template <typename M, int Y, bool DX, bool DW, bool PAST>
 __global__ __launch_bounds__(256) void k_head_few_prod(HeadFewProd a) {
     constexpr int LDS_X = 3 * 8 * Y * 64 * 16, LDS_W = 4 * 16 * 136 * 2;
     __shared__ __attribute__((aligned(16))) char lds[!DX ? LDS_W : !DW || LDS_X > LDS_W ? LDS_X : LDS_W];
-    const int group = (int)blockIdx.y - (DX ? a.parts : 0);
-    if (DX && group < 0)
-        head_few_dx<M, Y>(a, (int)blockIdx.y, lds);
+    const uint32_t at = blockIdx.x / 8;
+    const int slab = (int)(at % (uint32_t)a.slabs), row = (int)(at / (uint32_t)a.slabs * 8 + blockIdx.x % 8);
+    if (row >= a.rows) return;
+    if (DX && row < a.parts)
+        head_few_dx<M, Y>(a, slab, row, lds);
     else if (DW)
-        head_few_dw<M, Y>(a, group, lds);
+        head_few_dw<M, Y, PAST>(a, slab, row - (DX ? a.parts : 0), lds);
 }
 
 // Joins the parts of the vocabulary: 256 / ROWS threads a row.
@@ -799,7 +807,8 @@ __global__ __launch_bounds__(256) void k_transpose(const char* x, int64_t ld, in
 //
 // A dW that the last-level cache would not hold with anything beside it is written past it, or w would be swept out of it
 // and what follows wait for it to be written: 65 x 4096 x 32768 254 -> 190 us, 256 rows 326 -> 287, 100 x 2048 x 100000 418 ->
-// 352, 2048 rows and more no difference.
+// 352, 2048 rows and more no difference.  Not where its rows share lines, which the caches join (1 x 1001 x 70000 130 us, past
+// them 161).
 constexpr int64_t HEAD_PIECE_BYTES = (int64_t)128 << 20, HEAD_PAST = (int64_t)128 << 20;
 struct HeadBackward {
     int64_t vc, vp, ldz;   // tokens of a piece (all but the last), padded; row of dz
@@ -860,16 +869,20 @@ static void run_head_few(const HeadFew& few, HeadArgs a, const HeadBackward& p, 
     const int64_t slabs = (d + 127) / 128, units = (a.V + 15) / 16;
     HeadFewProd g{few.x, few.w, a.dz, a.dzt, few.ldx, few.ldw, p.ldz, p.vp, a.T, a.V, (int)d, dx ? p.parts : 0, p.steps,
                   (int)std::max<int64_t>(1, std::min<int64_t>(16, units * slabs / (16 * op_cus()))), dw, lddw, partial,
-                  (d + 7) / 8 * 8, a.g_logprob, a.g_entropy};
+                  (d + 7) / 8 * 8, a.g_logprob, a.g_entropy, (int)slabs, 0};
     const int64_t groups = dw ? (units + 4 * g.units - 1) / (4 * g.units) : 0;
     // (of 32 rows dx's LDS would keep half of dW's workgroups out: 32 x 4096 x 32768 174 us, in one launch 204; 16 x 1024 x
     // 4096 24.0, in one launch 19.6)
-    const dim3 block(256), gx((unsigned)slabs, (unsigned)p.parts), gw((unsigned)slabs, (unsigned)groups);
+    const bool past = 2 * a.V * d >= HEAD_PAST && ((uintptr_t)dw & 15) == 0 && lddw % 8 == 0;
+    auto go = [&](auto kernel, int64_t rows) {
+        g.rows = (int)rows;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 7) / 8 * 8 * slabs)), dim3(256), 0, st, g);
+    };
     if (Y == 1 && dx && dw) {
-        hipLaunchKernelGGL((k_head_few_prod<M, 1, true, true>), dim3(gx.x, gx.y + gw.y), block, 0, st, g);
+        go(past ? k_head_few_prod<M, 1, true, true, true> : k_head_few_prod<M, 1, true, true, false>, p.parts + groups);
     } else {
-        if (dx) hipLaunchKernelGGL((k_head_few_prod<M, Y, true, false>), gx, block, 0, st, g);
-        if (dw) hipLaunchKernelGGL((k_head_few_prod<M, Y, false, true>), gw, block, 0, st, g);
+        if (dx) go(k_head_few_prod<M, Y, true, false, false>, p.parts);
+        if (dw) go(past ? k_head_few_prod<M, Y, false, true, true> : k_head_few_prod<M, Y, false, true, false>, groups);
     }
     if (dx)
         hipLaunchKernelGGL(k_head_few_join<E>, dim3((unsigned)((a.T * g.dp + 63) / 64)), dim3(1024), 0, st, g,
@@ -957,7 +970,7 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
                 launch_prod<M, true, false>(gx, plan, partial, st);
         }
         if (!dw) continue;
-        const bool past = 2 * V * d >= HEAD_PAST;
+        const bool past = 2 * V * d >= HEAD_PAST && ((uintptr_t)dw & 15) == 0 && lddw % 8 == 0;
         if (p.tp) gw.a = operand(xt, 2 * p.tp, cols, 2 * p.tp);
         if (p.tp)
             past ? launch_prod<M, false, true, false, true>(gw, p.dw, partial, st)
