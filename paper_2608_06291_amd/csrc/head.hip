@@ -281,6 +281,38 @@ __global__ __launch_bounds__(Tl::THREADS) void k_head(HeadArgs a) {
 
 constexpr int HEAD_STEPS = 2;
 
+// Pieces of U steps of 32 entries of a row on their way, a lane's 8 of each (those of the same row 16 lanes apart).
+// SHIFT: see FewPiece; the word behind a piece is the first one of the lane 16 further on, and behind the last
+// lane's that of the first lane's next step; only the last step's are loaded (1 x 1001 x 70000 55 us with all words loaded,
+// 46; 32 rows 65 and 60; but 16 x 3539 x 17120 60 and 66, waiting for LDS).
+template <int U, bool SHIFT>
+struct HeadPieces {
+    u32x4 w[U];
+    uint32_t next;
+    template <typename E>
+    __device__ inline void load(const E* p) {
+#pragma unroll
+        for (int i = 0; i < U - 1; ++i) {
+            if constexpr (SHIFT)
+                __builtin_memcpy(&w[i], (const void*)((uintptr_t)(p + i * 32) & ~(uintptr_t)3), 16);
+            else
+                w[i] = load_words(p + i * 32);
+        }
+        FewPiece<SHIFT> last;
+        last.load(p + (U - 1) * 32);
+        w[U - 1] = last.w;
+        if constexpr (SHIFT) next = last.next;
+    }
+    template <typename E>
+    __device__ inline u32x4 get(int i, const E* row, int lane) const {
+        if constexpr (!SHIFT) return w[i];
+        FewPiece<SHIFT> p;
+        p.w = w[i];
+        p.next = i == U - 1 ? next : (uint32_t)__shfl((int)(lane < 16 ? w[min(i + 1, U - 1)][0] : w[i][0]), (lane + 16) & 63);
+        return p.get(row);
+    }
+};
+
 // Few rows (a decoding step): bound by reading w once.  A workgroup takes R units of 16 tokens and Y of 16
 // rows of x; its waves share the summed axis, blocks of two steps of 32 in turn, every
 // fragment straight from memory (at any alignment) into registers, BLOCKS blocks asked for at once.  The partial
@@ -306,17 +338,13 @@ __global__ __launch_bounds__(512) void k_head_few(HeadFew f, HeadArgs a) {
     const int nblocks = f.d / (32 * U), nsteps = f.d / 32;   // what is left goes one step a wave
 
     struct Block {
-        FewPiece<SHIFT> w[U][R], x[U][Y];
+        HeadPieces<U, SHIFT> w[R], x[Y];
     };
     auto load = [&](Block& b, int k) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r) b.w[r].load(w[r] + k);
 #pragma unroll
-            for (int i = 0; i < U; ++i) b.w[i][r].load(w[r] + k + i * 32);
-#pragma unroll
-        for (int y = 0; y < Y; ++y)
-#pragma unroll
-            for (int i = 0; i < U; ++i) b.x[i][y].load(x[y] + k + i * 32);
+        for (int y = 0; y < Y; ++y) b.x[y].load(x[y] + k);
     };
     f32x4 acc[R][Y] = {};
     auto add = [&](const u32x4 (&u)[R], const u32x4 (&v)[Y]) {
@@ -338,9 +366,9 @@ __global__ __launch_bounds__(512) void k_head_few(HeadFew f, HeadArgs a) {
             for (int i = 0; i < U; ++i) {
                 u32x4 u[R], v[Y];
 #pragma unroll
-                for (int r = 0; r < R; ++r) u[r] = b[k].w[i][r].get(w[r]);
+                for (int r = 0; r < R; ++r) u[r] = b[k].w[r].get(i, w[r], lane);
 #pragma unroll
-                for (int y = 0; y < Y; ++y) v[y] = b[k].x[i][y].get(x[y]);
+                for (int y = 0; y < Y; ++y) v[y] = b[k].x[y].get(i, x[y], lane);
                 add(u, v);
             }
         }
