@@ -224,6 +224,7 @@ struct EmbedGradArgs {
     float* part;               // what a chunk leaves of the range it begins in, and of the one it ends in: chunks x 2 x dp
     int64_t lddy, ldb, ldo, T, V, dp;
     int d, chunk_blocks, lanes;   // threads a row
+    int rows, slabs;           // k_embed_grad, k_embed_few: workgroups along the rows, and along one
     int past;                  // the gradient is written past the caches
     float scale;
 };
@@ -233,7 +234,8 @@ constexpr int EMBED_CHUNK = 16;
 // A gradient that the last-level cache (256 MB) would not hold with anything beside it is written past the caches:
 // 8192 x 4096 into 32768 rows (268 MB) 82 -> 72 us, 65536 x 1024 into 131072 rows 167 -> 144.  A smaller one is left to
 // whoever reads it next, and one of few positions, which reads nothing that it could sweep (200 positions 37 us, past
-// the caches 44).
+// the caches 44).  Rows that share lines are left to the caches, which join them (300 x 3571 fp32 into 35552 125 us, past
+// them 138).
 constexpr int64_t EMBED_PAST = (int64_t)128 << 20;
 
 // A row is read and written in whole vectors (WHOLE: d is a multiple of them), or its last entries one by one: `n` of
@@ -272,6 +274,29 @@ __device__ inline void embed_write(const EmbedGradArgs& a, int64_t v, int c, int
     } else {
         store_n(out, o, WHOLE ? VEC : n);
     }
+}
+
+// A row of zeros where there is no base: whole vectors at addresses that are multiples of theirs, what lies before and
+// behind an entry a lane (13 x 3571 into 35552 rows 73
+// us, at any alignment, and 68).  c: the first of a thread's NV vectors, `step` entries apart
+// (and rows of VEC vectors at least, so that each entry has its lane).
+template <typename E, int NV>
+__device__ inline void embed_zero(const EmbedGradArgs& a, int64_t v, int c, int step) {
+    constexpr int VEC = 16 / sizeof(E);
+    E* const row = static_cast<E*>(a.out) + v * a.ldo;
+    const int before = (int)(-(uintptr_t)row & 15) / (int)sizeof(E), behind = (a.d - before) % VEC;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        E* const p = row + before + c + i * step;
+        if (before + c + i * step + VEC > a.d) continue;
+        if (a.past)
+            store_words_past(p, u32x4(0));
+        else
+            *reinterpret_cast<u32x4*>(p) = u32x4(0);
+    }
+    const int lane = c / VEC;
+    if (lane < before) row[lane] = (E)0.0f;
+    if (lane < behind) row[a.d - behind + lane] = (E)0.0f;
 }
 
 // A chunk of the sorted positions is summed by `lanes` threads, a vector of the row each.  Where a token's whole range
@@ -332,20 +357,31 @@ __global__ __launch_bounds__(256) void k_embed_chunks(EmbedGradArgs a) {
     if (token < a.V) flush(token != behind);
 }
 
+// Which rows and which part of them a workgroup takes.  Every eighth workgroup runs on the same XCD: those have all parts
+// of a row, so that a line that two parts share is joined in one L2 (13 x 3571 into 35552 rows 68 us, parts in turn, and 53).
+__device__ inline bool embed_block(const EmbedGradArgs& a, int& row, int& slab) {
+    const uint32_t at = blockIdx.x / 8;
+    slab = (int)(at % (uint32_t)a.slabs);
+    row = (int)(at / (uint32_t)a.slabs * 8 + blockIdx.x % 8);
+    return row < a.rows;
+}
+
 // The rows that are left.  Those whose range spans chunks: first, as they take longest, by one workgroup for each
 // chunk in which such a range begins (256 vectors of the row a workgroup).  Those of no token: `lanes` lanes of a
-// wave take EMBED_ROWS of them, NV vectors a lane (blockIdx.y: which part of a longer row).
+// wave take EMBED_ROWS of them, NV vectors a lane (of a longer row a part).
 constexpr int EMBED_ROWS = 4;
 template <typename E, int NV, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed_grad(EmbedGradArgs a) {
     constexpr int VEC = 16 / sizeof(E);
-    if ((int)blockIdx.x < a.chunk_blocks) {
-        const int64_t next = ((int64_t)blockIdx.x + 1) * EMBED_CHUNK;
+    int block, slab;
+    if (!embed_block(a, block, slab)) return;
+    if (block < a.chunk_blocks) {
+        const int64_t next = ((int64_t)block + 1) * EMBED_CHUNK;
         const int32_t token = a.key[next];
         if (token != a.key[next - 1] || token >= a.V) return;
         const int lo = a.start[token], first = lo / EMBED_CHUNK, end = (a.start[token + 1] - 1) / EMBED_CHUNK;
-        if (first != (int)blockIdx.x) return;
-        for (int c = ((int)blockIdx.y * 256 + threadIdx.x) * VEC; c < a.d; c += gridDim.y * 256 * VEC) {
+        if (first != block) return;
+        for (int c = (slab * 256 + (int)threadIdx.x) * VEC; c < a.d; c += a.slabs * 256 * VEC) {
             constexpr int AHEAD = 8;
             const float* const part = a.part + c;
             float s[VEC];
@@ -367,8 +403,8 @@ __global__ __launch_bounds__(256) void k_embed_grad(EmbedGradArgs a) {
         }
         return;
     }
-    const int64_t v0 = ((int64_t)((int)blockIdx.x - a.chunk_blocks) * (256 / a.lanes) + threadIdx.x / a.lanes) * EMBED_ROWS;
-    const int step = a.lanes * VEC, c = (int)blockIdx.y * NV * step + (int)(threadIdx.x % a.lanes) * VEC, n = a.d - c;
+    const int64_t v0 = ((int64_t)(block - a.chunk_blocks) * (256 / a.lanes) + threadIdx.x / a.lanes) * EMBED_ROWS;
+    const int step = a.lanes * VEC, c = slab * NV * step + (int)(threadIdx.x % a.lanes) * VEC, n = a.d - c;
     if (v0 >= a.V || n <= 0) return;
     int start[EMBED_ROWS + 1];   // (all asked for at once; past the table its end: no rows)
 #pragma unroll
@@ -378,6 +414,10 @@ __global__ __launch_bounds__(256) void k_embed_grad(EmbedGradArgs a) {
     for (int r = 0; r < EMBED_ROWS; ++r) {
         if (v0 + r >= a.V) break;
         if (start[r] < start[r + 1]) continue;
+        if (!a.base && a.d >= VEC * VEC) {
+            embed_zero<E, NV>(a, v0 + r, c, step);
+            continue;
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (i * step < n) embed_write<E, WHOLE>(a, v0 + r, c + i * step, n - i * step, none);
@@ -391,14 +431,17 @@ template <typename E, int NV, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed_few(EmbedGradArgs a, const int64_t* __restrict__ tokens) {
     constexpr int VEC = 16 / sizeof(E), WORDS = EMBED_FEW / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = 64 / a.lanes, group = lane / a.lanes;
+    static_assert(WORDS == 4, "words of a row's positions");
+    int block, slab;
+    if (!embed_block(a, block, slab)) return;
     int32_t key[WORDS];
 #pragma unroll
     for (int k = 0; k < WORDS; ++k) {
         const int t = k * 64 + lane;
         key[k] = t < a.T ? embed_key(tokens[t], a.V) : -1;
     }
-    const int step = a.lanes * VEC, c = (int)blockIdx.y * NV * step + lane % a.lanes * VEC, n = a.d - c;
-    const int64_t v0 = ((int64_t)blockIdx.x * 4 + wave) * (groups * EMBED_ROWS);
+    const int step = a.lanes * VEC, c = slab * NV * step + lane % a.lanes * VEC, n = a.d - c;
+    const int64_t v0 = ((int64_t)block * 4 + wave) * (groups * EMBED_ROWS);
     const E* const dy = static_cast<const E*>(a.dy) + c;
     for (int r = 0; r < EMBED_ROWS; ++r) {
         const int64_t first = v0 + r * groups, v = first + group;
@@ -411,6 +454,10 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGradArgs a, const int64_
                 if (g == group) hit[k] = is;
             }
         if (v >= a.V || n <= 0) continue;
+        if ((hit[0] | hit[1] | hit[2] | hit[3]) == 0 && !a.base && a.d >= VEC * VEC) {
+            embed_zero<E, NV>(a, v, c, step);
+            continue;
+        }
         float s[NV][VEC] = {};
 #pragma unroll
         for (int k = 0; k < WORDS; ++k)
@@ -515,7 +562,9 @@ static void launch_embed_grad(EmbedGradArgs a, const int64_t* tokens, hipStream_
     }
     lanes(64);
     const int each = 256 / a.lanes * EMBED_ROWS;
-    const dim3 grid((unsigned)(a.chunk_blocks + (a.V + each - 1) / each), (unsigned)((vecs + a.lanes * nv - 1) / (a.lanes * nv)));
+    a.rows = (int)(a.chunk_blocks + (a.V + each - 1) / each);
+    a.slabs = (vecs + a.lanes * nv - 1) / (a.lanes * nv);
+    const dim3 grid((unsigned)((a.rows + 7) / 8 * 8 * a.slabs));
     auto go = [&](auto few, auto many) {
         if (a.T <= EMBED_FEW)
             hipLaunchKernelGGL(few, grid, dim3(256), 0, st, a, tokens);
@@ -587,9 +636,11 @@ extern "C" bakron_status bakron_embedding_backward(const void* dy, int64_t lddy,
     char* const at = static_cast<char*>(work);
     if (T > bk::EMBED_FEW) bk::launch_sort(w, tokens, T, V, at, stream);
     char* const part = at + w.bytes() - w.part;
+    const int64_t esize = dtype == BAKRON_F32 ? 4 : 2;
+    const bool past = T > bk::EMBED_FEW && V * d * esize >= bk::EMBED_PAST && (((uintptr_t)dtable | ldo * esize) & 15) == 0;
     const bk::EmbedGradArgs a{dy, base, dtable, reinterpret_cast<int32_t*>(at), reinterpret_cast<int32_t*>(at + w.keys),
                               reinterpret_cast<int32_t*>(part - w.start), reinterpret_cast<float*>(part), lddy, ldb, ldo,
-                              T, V, w.dp, (int)d, 0, 0, T > bk::EMBED_FEW && V * d * (dtype == BAKRON_F32 ? 4 : 2) >= bk::EMBED_PAST, scale};
+                              T, V, w.dp, (int)d, 0, 0, 0, 0, past, scale};
     if (dtype == BAKRON_F32)
         bk::launch_embed_grad<float>(a, tokens, stream);
     else if (dtype == BAKRON_F16)

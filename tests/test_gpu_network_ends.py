@@ -147,6 +147,25 @@ def test_embedding_backward(dtype, T, d, V, pad, shift):
     assert torch.equal(pk.embedding_backward(x[:0], none[:0], V, base=base.to(DEV)).cpu(), base)
 
 
+@pytest.mark.parametrize("dtype", NAMES)
+@pytest.mark.parametrize("T", [5, 300])
+@pytest.mark.parametrize("d,V,pad,shift", [(1, 70, 0, 1), (7, 70, 1, 0), (33, 90, 0, 3), (63, 90, 2, 1), (17, 50, 0, 1), (64, 40, 8, 0), (64, 40, 1, 1), (201, 60, 0, 5),
+                                           (2051, 25, 4, 2), (4100, 19, 0, 0), (4100, 17000, 12, 8), (4096, 17000, 16, 16)])
+def test_embedding_backward_into_rows(dtype, T, d, V, pad, shift):
+    """The gradient in rows of a wider buffer at any alignment: rows of no token are zeros, nothing else is written."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("embedding backward into rows", dtype, T, d, V, pad, shift)
+    dt = _dtype(dtype)
+    dy, tok = _rand((T, d), 1).to(dt).to(DEV), _tokens(T, V, 2).clamp(max=V // 2).to(DEV)   # (half of the rows without one)
+    want = pk.embedding_backward(dy, tok, V, base=torch.zeros(V, d, dtype=dt, device=DEV))
+    buf = torch.full((shift + V * (d + pad) + 64,), 9.0, dtype=dt, device=DEV)
+    out = buf[shift:shift + V * (d + pad)].view(V, d + pad)
+    pk.embedding_backward(dy, tok, V, out=out[:, :d])
+    assert torch.equal(out[:, :d], want) and not bool(out[V // 2 + 1:, :d].any())
+    assert bool((buf[:shift] == 9).all()) and bool((buf[shift + V * (d + pad):] == 9).all()) and bool((out[:, d:] == 9).all())
+
+
 # ---------------------------------------------------------------- layer norm
 NORM = [(1, 1, False, 0, 0), (1, 4096, True, 0, 0), (3, 127, True, 0, 0), (5, 128, False, 3, 1), (130, 1000, True, 0, 0),
         (2, 8191, True, 1, 3), (1030, 520, True, 8, 0), (1100, 2049, False, 0, 0), (1, 32768, True, 0, 0),
