@@ -453,7 +453,7 @@ struct HeadFewProd {
     float* partial;            // dx: parts x T x dp
     int64_t dp;
     const float *g, *gh;
-    int slabs, rows;           // of 128 columns; parts of dx and groups of dW
+    int slabs, rows, each;     // of 128 columns; parts of dx and groups of dW, so many of them in turn
 };
 
 // dW: a wave holds 128 columns of x, of all rows, as 8 operands and goes through `units` units of 16 tokens.
@@ -630,15 +630,15 @@ __device__ inline void head_few_dx(const HeadFewProd& a, int slab, int part, cha
     }
 }
 
-// DX and DW: both in one launch, the parts of dx first.  Every eighth workgroup runs on the same XCD: those have
-// all slabs of a part or group, so that a line of W or dW that two slabs share is fetched, or joined, in one L2 (gradients
-// of 1 x 1001 x 70000 130 -> 111 us, 32 x 1024 x 70000 131 -> 121).
+// DX and DW: both in one launch, the parts of dx first.  Every eighth workgroup runs on the same XCD: with each = 8 those
+// have all slabs of a part or group, so that a line of W or dW that two slabs share is fetched, or joined, in one L2 (gradients
+// of 1 x 1001 x 70000 120 -> 102 us, 32 x 1024 x 70000 132 -> 121; but 1 x 4096 x 32768 140 -> 152).
 template <typename M, int Y, bool DX, bool DW, bool PAST>
 __global__ __launch_bounds__(256) void k_head_few_prod(HeadFewProd a) {
     constexpr int LDS_X = 3 * 8 * Y * 64 * 16, LDS_W = 4 * 16 * 136 * 2;
     __shared__ __attribute__((aligned(16))) char lds[!DX ? LDS_W : !DW || LDS_X > LDS_W ? LDS_X : LDS_W];
-    const uint32_t at = blockIdx.x / 8;
-    const int slab = (int)(at % (uint32_t)a.slabs), row = (int)(at / (uint32_t)a.slabs * 8 + blockIdx.x % 8);
+    const uint32_t each = (uint32_t)a.each, at = blockIdx.x / each;
+    const int slab = (int)(at % (uint32_t)a.slabs), row = (int)(at / (uint32_t)a.slabs * each + blockIdx.x % each);
     if (row >= a.rows) return;
     if (DX && row < a.parts)
         head_few_dx<M, Y>(a, slab, row, lds);
@@ -897,14 +897,17 @@ static void run_head_few(const HeadFew& few, HeadArgs a, const HeadBackward& p, 
     const int64_t slabs = (d + 127) / 128, units = (a.V + 15) / 16;
     HeadFewProd g{few.x, few.w, a.dz, a.dzt, few.ldx, few.ldw, p.ldz, p.vp, a.T, a.V, (int)d, dx ? p.parts : 0, p.steps,
                   (int)std::max<int64_t>(1, std::min<int64_t>(16, units * slabs / (16 * op_cus()))), dw, lddw, partial,
-                  (d + 7) / 8 * 8, a.g_logprob, a.g_entropy, (int)slabs, 0};
+                  (d + 7) / 8 * 8, a.g_logprob, a.g_entropy, (int)slabs, 0, 8};
     const int64_t groups = dw ? (units + 4 * g.units - 1) / (4 * g.units) : 0;
     // (of 32 rows dx's LDS would keep half of dW's workgroups out: 32 x 4096 x 32768 174 us, in one launch 204; 16 x 1024 x
     // 4096 24.0, in one launch 19.6)
     const bool past = 2 * a.V * d >= HEAD_PAST && ((uintptr_t)dw & 15) == 0 && lddw % 8 == 0;
+    // long rows whose slabs share no line: slab by slab (of 2048 entries and more the same or better, of 1024 5 to 9% slower)
+    const bool apart = (((dx ? (uintptr_t)few.w | few.ldw * 2 : 0) | (dw ? (uintptr_t)dw | lddw * 2 : 0)) & 127) == 0;
+    if (apart && slabs > 16) g.each = 1;
     auto go = [&](auto kernel, int64_t rows) {
         g.rows = (int)rows;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 7) / 8 * 8 * slabs)), dim3(256), 0, st, g);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + g.each - 1) / g.each * g.each * slabs)), dim3(256), 0, st, g);
     };
     if (Y == 1 && dx && dw) {
         go(past ? k_head_few_prod<M, 1, true, true, true> : k_head_few_prod<M, 1, true, true, false>, p.parts + groups);
