@@ -27,12 +27,13 @@ struct EmbedArgs {
 
 constexpr int EMBED_NV = 4;   // vectors a thread has in flight
 
-// `lanes` threads take one piece of one row; of short rows a workgroup takes several.
-template <typename E>
+// `lanes` threads take one piece of one row; of short rows a workgroup takes several.  LONG: 256 lanes, known when it
+// is built (8192 x 4096 22 us with tokens that change, 24 without).
+template <typename E, bool LONG>
 __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
     constexpr int VEC = 16 / sizeof(E);
-    const int len = a.lanes * EMBED_NV * VEC, lane = (int)threadIdx.x % a.lanes;
-    const int64_t t = (int64_t)(blockIdx.x / (uint32_t)a.pieces) * (256 / a.lanes) + threadIdx.x / a.lanes;
+    const int lanes = LONG ? 256 : a.lanes, len = lanes * EMBED_NV * VEC, lane = (int)threadIdx.x % lanes;
+    const int64_t t = (int64_t)(blockIdx.x / (uint32_t)a.pieces) * (256 / lanes) + threadIdx.x / lanes;
     if (t >= a.T) return;
     const int lo = (int)(blockIdx.x % (uint32_t)a.pieces) * len;
     const int hi = min(a.d, lo + len), whole = (hi - lo) / VEC;
@@ -44,11 +45,11 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
 #pragma unroll
     for (int i = 0; i < EMBED_NV; ++i) {
         r[i] = u32x4(0);
-        if (asked && i * a.lanes < whole) r[i] = load_words(row + lo + min(i * a.lanes + lane, whole - 1) * VEC);
+        if (asked && i * lanes < whole) r[i] = load_words(row + lo + min(i * lanes + lane, whole - 1) * VEC);
     }
 #pragma unroll
     for (int i = 0; i < EMBED_NV; ++i) {
-        const int v = i * a.lanes + lane;
+        const int v = i * lanes + lane;
         if (v >= whole) break;
         Pack<E, VEC> o;
 #pragma unroll
@@ -498,7 +499,11 @@ static void launch_embed(EmbedArgs a, hipStream_t st) {
     while (a.lanes < 256 && a.lanes * VEC < a.d) a.lanes *= 2;
     const int len = a.lanes * EMBED_NV * VEC, rows = 256 / a.lanes;
     a.pieces = (a.d + len - 1) / len;
-    hipLaunchKernelGGL(k_embed<E>, dim3((unsigned)((a.T + rows - 1) / rows * a.pieces)), dim3(256), 0, st, a);
+    const dim3 grid((unsigned)((a.T + rows - 1) / rows * a.pieces));
+    if (rows == 1)
+        hipLaunchKernelGGL((k_embed<E, true>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_embed<E, false>), grid, dim3(256), 0, st, a);
 }
 // The workspace of the gradient.
 struct EmbedWork {
