@@ -726,7 +726,9 @@ bakron_status bakron_head_logprobs(const void *x, int64_t ldx, int64_t T, int64_
  *   dx = dz w,   dw = dz^T x
  * A target outside [0, V) has no first term; a row whose logits are all -inf has dz = 0.
  * dz is rounded to dtype for the products, in BAKRON_F16 times
- * a power of two (undone at the end) by the largest |g_logprob| + 4 |g_entropy|; with the
+ * a power of two (undone at the end) by the largest |g_logprob| + 4 |g_entropy| of the rows
+ * that ask for them (without g_logprob where the target lies outside [0, V); not of rows whose
+ * logits are all -inf); with the
  * result's own rounding that leaves errors of about 2.4e-3 of a gradient's norm in
  * BAKRON_BF16 and 2.9e-4 in BAKRON_F16 (with a hundred rows up to 3e-3 and 4e-4), where one
  * rounding gives 1.7e-3 and 2.1e-4.  For T <= 64, where the errors may not average out, dz is kept as two numbers of dtype, and the

@@ -27,6 +27,27 @@ struct HeadPart {
     float m, s, s1, pad;
 };
 
+// What comes in at the rows.
+struct HeadIn {
+    const int64_t* target;
+    const float *lse, *g, *gh;
+    int64_t all;   // tokens of all pieces
+
+    // Of row t: whether no logit is finite, and the gradient of its log probability, where it has a target.
+    __device__ bool empty(int64_t t) const { return lse[t] == -INFINITY; }
+    __device__ float logprob(int64_t t) const {
+        if (!target || !g) return 0.0f;
+        const float v = g[t];
+        const int64_t k = target[t];
+        return k >= 0 && k < all ? v : 0.0f;
+    }
+    // The bound of row t's |dz|; 0 where it asks for nothing, whatever came in there.
+    __device__ float bound(int64_t t) const {
+        const float b = fabsf(logprob(t)) + (gh ? 4.0f * fabsf(gh[t]) : 0.0f);
+        return b < INFINITY && !empty(t) ? b : 0.0f;
+    }
+};
+
 struct HeadScale;
 struct HeadArgs {
     Operand x, w;
@@ -40,6 +61,7 @@ struct HeadArgs {
     // backward
     const float *lse, *entropy, *g_logprob, *g_entropy;
     int64_t v0, all;           // first token of the piece; tokens of all pieces
+    __host__ __device__ HeadIn in() const { return HeadIn{target, lse, g_logprob, g_entropy, all}; }
     void* dz;                  // T rows: vp entries (zeros in the padding), then what their rounding took
     int64_t vp, ldz;           // ldz: vp, or 2 vp with the rests
     const float* factor;       // half precision: dz is taken times this, or NULL: by the kernel itself,
@@ -66,40 +88,31 @@ __device__ inline HeadScale head_scale(float m) {
     e = max(e, 14 - 126);          // (both powers are normal numbers)
     return HeadScale{ldexpf(1.0f, 14 - e), ldexpf(1.0f, e - 14)};
 }
-__global__ __launch_bounds__(1024) void k_head_scale(const float* __restrict__ g, const float* __restrict__ gh,
-                                                     int64_t T, HeadScale* out) {
+__global__ __launch_bounds__(1024) void k_head_scale(HeadIn in, int64_t T, HeadScale* out) {
     __shared__ float red[16];
     float m = 0.0f;
-    for (int64_t i = threadIdx.x; i < T; i += 1024) {
-        const float b = (g ? fabsf(g[i]) : 0.0f) + (gh ? 4.0f * fabsf(gh[i]) : 0.0f);
-        m = fmaxf(m, b < INFINITY ? b : 0.0f);
-    }
+    for (int64_t i = threadIdx.x; i < T; i += 1024) m = fmaxf(m, in.bound(i));
     m = group_reduce(m, MaxNan(), red, threadIdx.x >> 6, threadIdx.x & 63, 16);
     if (threadIdx.x != 0) return;
     *out = head_scale(m);
 }
 
 // The same by every wave itself, for up to 64 rows (all its lanes have to be active): one launch less.
-__device__ inline HeadScale head_scale_few(const float* g, const float* gh, int64_t T, int lane) {
-    float b = 0.0f;
-    if (lane < T) b = (g ? fabsf(g[lane]) : 0.0f) + (gh ? 4.0f * fabsf(gh[lane]) : 0.0f);
-    return head_scale(wave_reduce(b < INFINITY ? b : 0.0f, MaxNan()));
+__device__ inline HeadScale head_scale_few(const HeadIn& in, int64_t T, int lane) {
+    return head_scale(wave_reduce(lane < T ? in.bound(lane) : 0.0f, MaxNan()));
 }
 
 // The same for up to HEAD_SCALE_ROWS rows: a launch less, for a scan by every workgroup (gradients of 200 x 1000 x 5003
 // 43 -> 39 us, 500 x 1000 x 5000 51 -> 47; with 1024 rows 1024 x 512 x 32000 152 -> 156).
-__device__ inline HeadScale head_scale_rows(const float* g, const float* gh, int T, int lane) {
+__device__ inline HeadScale head_scale_rows(const HeadIn& in, int T, int lane) {
     constexpr int AHEAD = 4;
     float m = 0.0f;
     for (int t0 = 0; t0 < T; t0 += 64 * AHEAD) {
         float b[AHEAD];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {   // (past the last row it once more)
-            const int t = min(t0 + i * 64 + lane, T - 1);
-            b[i] = (g ? fabsf(g[t]) : 0.0f) + (gh ? 4.0f * fabsf(gh[t]) : 0.0f);
-        }
+        for (int i = 0; i < AHEAD; ++i) b[i] = in.bound(min(t0 + i * 64 + lane, T - 1));   // (past the last row it once more)
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) m = fmaxf(m, b[i] < INFINITY ? b[i] : 0.0f);
+        for (int i = 0; i < AHEAD; ++i) m = fmaxf(m, b[i]);
     }
     return head_scale(wave_reduce(m, MaxNan()));
 }
@@ -113,11 +126,11 @@ struct HeadRow {
 __device__ inline HeadRow head_row(const HeadArgs& a, int64_t t) {
     HeadRow r;
     r.lse = a.lse[t];
-    const bool empty = r.lse == -INFINITY;
+    const bool empty = a.in().empty(t);
     if (empty) r.lse = INFINITY;   // every p is then exp(-inf) = 0
     const int64_t k = a.target ? a.target[t] : -1;
     r.t = k >= a.v0 && k < a.v0 + a.V ? (int)(k - a.v0) : -1;
-    r.g = k >= 0 && k < a.all && a.g_logprob ? a.g_logprob[t] : 0.0f;
+    r.g = a.in().logprob(t);
     r.gh = a.g_entropy ? a.g_entropy[t] : 0.0f;
     r.H = a.g_entropy ? a.entropy[t] : 0.0f;
     if (empty) r.g = r.gh = 0.0f;
@@ -253,7 +266,7 @@ __global__ __launch_bounds__(Tl::THREADS) void k_head(HeadArgs a) {
             if (a.factor) {
                 factor = *a.factor;
             } else {
-                const HeadScale own = head_scale_rows(a.g_logprob, a.g_entropy, (int)a.T, lane);
+                const HeadScale own = head_scale_rows(a.in(), (int)a.T, lane);
                 factor = own.factor;
                 if (blockIdx.x == 0 && threadIdx.x == 0) *a.scale = own;
             }
@@ -423,7 +436,7 @@ __global__ __launch_bounds__(512) void k_head_few(HeadFew f, HeadArgs a) {
             if (t < a.T) row = head_row(a, t);
             float factor = 1.0f;
             if constexpr (narrow_range<E>)
-                factor = a.factor ? *a.factor : head_scale_few(a.g_logprob, a.g_entropy, a.T, lane).factor;
+                factor = a.factor ? *a.factor : head_scale_few(a.in(), a.T, lane).factor;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int i = first + r * 16;
@@ -452,7 +465,7 @@ struct HeadFewProd {
     int64_t lddw;
     float* partial;            // dx: parts x T x dp
     int64_t dp;
-    const float *g, *gh;
+    HeadIn in;
     int slabs, rows, each;     // of 128 columns; parts of dx and groups of dW, so many of them in turn
 };
 
@@ -482,7 +495,7 @@ __device__ inline void head_few_dw(const HeadFewProd& a, int slab, int group, ch
         }
         __builtin_memcpy(&x[u], v, 16);
     }
-    const float undo = narrow_range<E> ? head_scale_few(a.g, a.gh, a.T, lane).undo : 1.0f;
+    const float undo = narrow_range<E> ? head_scale_few(a.in, a.T, lane).undo : 1.0f;
     const char* const dzt = static_cast<const char*>(a.dzt) + (first + r16) * (64 * Y) + kq * 16;
     const int n = (int)min((int64_t)a.units, (a.V - first + 15) / 16), c = c0 + r16 * 8;
     i32x4 b[Y], next[Y];
@@ -547,7 +560,7 @@ __global__ __launch_bounds__(1024) void k_head_few_join(HeadFewProd a, E* dx, in
     __syncthreads();
     if (wave > 0) return;
     for (int w = 1; w < 16; ++w) sum += red[w][lane];
-    if constexpr (narrow_range<E>) sum *= head_scale_few(a.g, a.gh, a.T, lane).undo;
+    if constexpr (narrow_range<E>) sum *= head_scale_few(a.in, a.T, lane).undo;
     if (e >= all || e % a.dp >= a.d) return;
     dx[e / a.dp * lddx + e % a.dp] = (E)sum;
 }
@@ -897,7 +910,7 @@ static void run_head_few(const HeadFew& few, HeadArgs a, const HeadBackward& p, 
     const int64_t slabs = (d + 127) / 128, units = (a.V + 15) / 16;
     HeadFewProd g{few.x, few.w, a.dz, a.dzt, few.ldx, few.ldw, p.ldz, p.vp, a.T, a.V, (int)d, dx ? p.parts : 0, p.steps,
                   (int)std::max<int64_t>(1, std::min<int64_t>(16, units * slabs / (16 * op_cus()))), dw, lddw, partial,
-                  (d + 7) / 8 * 8, a.g_logprob, a.g_entropy, (int)slabs, 0, 8};
+                  (d + 7) / 8 * 8, a.in(), (int)slabs, 0, 8};
     const int64_t groups = dw ? (units + 4 * g.units - 1) / (4 * g.units) : 0;
     // (of 32 rows dx's LDS would keep half of dW's workgroups out: 32 x 4096 x 32768 174 us, in one launch 204; 16 x 1024 x
     // 4096 24.0, in one launch 19.6)
@@ -927,11 +940,11 @@ static void run_head_backward(HeadFew few, HeadArgs a, const HeadBackward& p, in
     typedef typename M::Elem E;
     constexpr bool HALF = narrow_range<E>;
     a.scale = scale;
+    a.all = V;
     if (HALF && !p.few && (few_rows || a.T > HEAD_SCALE_ROWS)) {
-        hipLaunchKernelGGL(k_head_scale, dim3(1), dim3(1024), 0, st, a.g_logprob, a.g_entropy, a.T, scale);
+        hipLaunchKernelGGL(k_head_scale, dim3(1), dim3(1024), 0, st, a.in(), a.T, scale);
         a.factor = &scale->factor;
     }
-    a.all = V;
     if (p.few) {
         if (a.T <= 16)
             run_head_few<M, 1>(few, a, p, d, edge, dx, lddx, dw, lddw, static_cast<float*>(partial), st);
