@@ -29,6 +29,14 @@ def _rows(t):
     return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
 
 
+def _rstd(x, eps):
+    """1 / sqrt(mean(x^2) + eps) of the rows, as rmsnorm_quant takes them: any eps, 0 for a row of zeros without one."""
+    if eps >= 1e-30:
+        return _lib.layernorm(x, eps=eps, centre=False).rstd
+    v = x.double().square().mean(1) + eps   # (layernorm takes no eps below that)
+    return v.rsqrt().masked_fill(v == 0, 0.0).float()
+
+
 @dataclass
 class GatedMLP:
     """The block in 16-bit floats.  norm: d fp32; w_gate, w_up: f x d; w_down: d x f."""
@@ -56,8 +64,7 @@ class GatedMLP:
         x, b = _rows(x), _rows(b)
         dy, dw_gate, dw_up = _lib.gated_mlp_backward(b @ self.w_down, y, self.w_gate, self.w_up, act=self.act,
                                                      need_dw=need_dw)
-        rstd = _lib.layernorm(x, eps=self.eps, centre=False).rstd
-        dx, dnorm, _ = _lib.layernorm_backward(dy, x, self.norm, None, rstd, d_sum=b, need_dbias=False)
+        dx, dnorm, _ = _lib.layernorm_backward(dy, x, self.norm, None, _rstd(x, self.eps), d_sum=b, need_dbias=False)
         return dx, dw_gate, dw_up, dnorm
 
 

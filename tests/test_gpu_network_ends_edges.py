@@ -45,3 +45,55 @@ def test_rows_that_ask_for_nothing_do_not_scale(dtype, T, d, V):
     # without gradients of log probabilities the targets ask for nothing either way
     got = [pk.head_logprobs_backward(x, w, t, lse, H, None, gh) for t in (tok, None)]
     assert all(torch.equal(p, q) for p, q in zip(*got))
+
+
+def _block(d, f, eps, dtype="bf16", seed=0):
+    from paper_2608_06291_amd import mlp_block
+    torch = _t()
+    dt = _dtype(dtype)
+    w = [(_rand(s, seed + k) * s[1] ** -0.5).to(dt).to(DEV) for k, s in enumerate(((f, d), (f, d), (d, f)))]
+    return mlp_block.GatedMLP((1 + 0.1 * _rand((d,), seed + 5)).float().to(DEV), *w, eps=eps)
+
+
+def _block_gradients(blk, x, b, dy):
+    """(dx, bound of its error, dnorm, bound) of the block's norm from dy, in 64 bits."""
+    torch = _t()
+    xd, g, bd, norm = x.cpu().double(), dy.cpu().double(), b.cpu().double(), blk.norm.cpu().double()
+    T, d = xd.shape
+    ms = xd.square().mean(1, keepdim=True) + float(torch.tensor(blk.eps, dtype=torch.float32))
+    r = torch.where(ms > 0, ms.rsqrt(), 0.0)
+    n, gw = xd * r, g * norm
+    mn = (gw * n).mean(1, keepdim=True)
+    dx, dnorm = r * (gw - n * mn) + bd, (g * n).sum(0)
+    # rstd: its sum's d roundings, halved by the root, and four more; n two more; g one; the mean d + 6 of its terms' sizes
+    er = (d / 2 + 4) * U32
+    en = (er + 2.1 * U32) * n.abs()
+    size = gw.abs() + (n * mn).abs()
+    e = r * (U32 * gw.abs() + en * mn.abs() + n.abs() * ((d + 6) * U32 + er + 3 * U32) * (gw * n).abs().mean(1, keepdim=True)
+             + (4 * U32 + er) * size) + 2 * U32 * dx.abs()
+    return dx, e, dnorm, ((T + 4) * U32 + er) * (g * n).abs().sum(0) + 2.0 ** -149
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f16"))
+@pytest.mark.parametrize("eps", [0.0, 1e-35, 1e-5])
+@pytest.mark.parametrize("T,d,f", [(1, 64, 96), (40, 72, 104), (300, 130, 70)])
+def test_block_gradients_of_any_eps(eps, dtype, T, d, f):
+    """A block whose forward pass runs has its gradients, also with no eps and a row of zeros (which it leaves as they are)."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("block", dtype, eps, T, d, f)
+    blk = _block(d, f, eps, dtype)
+    x, b = (_rand((T, d), k).to(_dtype(dtype)).to(DEV) for k in (1, 2))
+    if T > 2:
+        x[2] = 0
+    out, y, h = blk.forward(x)
+    assert bool(torch.isfinite(out).all())
+    dx, dw_gate, dw_up, dnorm = blk.gradients(x, y, b)
+    dy = pk.gated_mlp_backward(b @ blk.w_down, y, blk.w_gate, blk.w_up, act=blk.act)
+    assert torch.equal(dw_gate, dy[1]) and torch.equal(dw_up, dy[2])
+    want, e, wnorm, en = _block_gradients(blk, x, b, dy[0])
+    for got, w, lim in ((dx, want, e + _u(dtype) * (want.abs() + e) + _tiny(dtype)), (dnorm, wnorm, en)):
+        assert bool(((got.cpu().double() - w).abs() <= lim).all()), float(((got.cpu().double() - w).abs() / lim).max())
+    if T > 2 and eps == 0.0:
+        assert torch.equal(dx[2], b[2])
+    assert all(torch.equal(p, q) for p, q in zip(blk.backward(x, y, b), (dx, dw_gate, dw_up)))
