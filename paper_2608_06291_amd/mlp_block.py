@@ -60,12 +60,15 @@ class GatedMLP:
 
     def gradients(self, x, y, b, need_dw: bool = True):
         """(dx, dw_gate, dw_up, dnorm) from b, the gradient with respect to the block's output; dnorm in fp32.
-        need_dw=False: the matrices stay as they are (None).  x and b may be of any strides."""
+        need_dw=False: the matrices stay as they are (None).  x and b may be of any strides, x of another type than
+        the block's (dx has it)."""
         x, b = _rows(x), _rows(b)
         dy, dw_gate, dw_up = _lib.gated_mlp_backward(b @ self.w_down, y, self.w_gate, self.w_up, act=self.act,
                                                      need_dw=need_dw)
-        dx, dnorm, _ = _lib.layernorm_backward(dy, x, self.norm, None, _rstd(x, self.eps), d_sum=b, need_dbias=False)
-        return dx, dw_gate, dw_up, dnorm
+        rows = (dy, x, b) if x.dtype == dy.dtype else (dy.float(), x.float(), b.float())
+        dx, dnorm, _ = _lib.layernorm_backward(rows[0], rows[1], self.norm, None, _rstd(rows[1], self.eps),
+                                               d_sum=rows[2], need_dbias=False)
+        return dx.to(x.dtype), dw_gate, dw_up, dnorm
 
 
 @dataclass

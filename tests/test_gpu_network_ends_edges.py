@@ -97,3 +97,24 @@ def test_block_gradients_of_any_eps(eps, dtype, T, d, f):
     if T > 2 and eps == 0.0:
         assert torch.equal(dx[2], b[2])
     assert all(torch.equal(p, q) for p, q in zip(blk.backward(x, y, b), (dx, dw_gate, dw_up)))
+
+
+@pytest.mark.parametrize("stream", ("f32", "f16", "bf16"))
+@pytest.mark.parametrize("dtype", ("bf16", "f16"))
+def test_block_gradients_of_a_stream_of_another_type(dtype, stream):
+    """x of any type beside a block in 16 bits: dx in x's type, rounded once."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("block, stream", dtype, stream)
+    T, d, f = 70, 130, 72
+    blk = _block(d, f, 1e-5, dtype)
+    x, b = _rand((T, d), 1).to(_dtype(stream)).to(DEV), _rand((T, d), 2).to(_dtype(dtype)).to(DEV)
+    y = blk.forward(x.to(_dtype(dtype)))[1]
+    dx, dw_gate, dw_up, dnorm = blk.gradients(x, y, b)
+    assert dx.dtype == x.dtype and dw_gate.dtype == b.dtype and dnorm.dtype == torch.float32
+    dy = pk.gated_mlp_backward(b @ blk.w_down, y, blk.w_gate, blk.w_up, act=blk.act)[0]
+    want, e, wnorm, en = _block_gradients(blk, x, b, dy)
+    e = e + U32 * (want.abs() + e) if stream != dtype else e   # (32 bits on the way)
+    for got, w, lim in ((dx, want, e + _u(stream) * (want.abs() + e) + _tiny(stream)), (dnorm, wnorm, en)):
+        assert bool(((got.cpu().double() - w).abs() <= lim).all()), float(((got.cpu().double() - w).abs() / lim).max())
+    assert torch.equal(blk.backward(x, y, b)[0], dx)
