@@ -961,7 +961,8 @@ def _head_operands(x, w):
 
 def _head_key(name, device, xp, ldx, T, d, wp, ldw, V, *more):
     """What the workspace of a head call depends on: sizes, and whether rows can be staged as they are."""
-    return (name, device.index, T, d, V, (xp | 2 * ldx) & 15 == 0, (wp | 2 * ldw) & 15 == 0, ldx >> 22 or ldw >> 22, *more)
+    return (name, device.index, T, d, V, (xp | 2 * ldx) & 15 == 0 and ldx < 1 << 22, (wp | 2 * ldw) & 15 == 0 and ldw < 1 << 22,
+            *more)
 
 
 def head_logprobs(x, w, target=None, work=None) -> TokenLogprobs:

@@ -1,0 +1,28 @@
+"""What the binding of the operators at the ends of a network keeps, and what it refuses before it looks at devices:
+needs no GPU."""
+import ctypes
+
+import pytest
+
+from test_network_ends_refusals import HEAD, HEAD_OK, HEADB, HEADB_OK
+from test_operators_refusals import P, _call, lib  # noqa: F401
+
+
+@pytest.mark.parametrize("name", ["bakron_head_logprobs", "bakron_head_logprobs_backward"])
+def test_kept_sizes_of_head_calls(lib, name):  # noqa: F811
+    """Calls that need workspaces of different sizes have different keys: each matrix alone and both with rows far apart, off
+    an aligned start, at distances that are no multiples of 16 bytes."""
+    import torch
+    import paper_2608_06291_amd as pk
+    names, base = (HEAD, HEAD_OK) if name == "bakron_head_logprobs" else (HEADB, dict(HEADB_OK, dw=P))
+    dev, T, d, V = torch.device("cuda", 0), 40, 64, 5000
+    sizes = {}
+    far = ((4096, 64), (4096, 1 << 22), (4096, (1 << 22) + 8), (4098, 64), (4096, 65), (4096, 1 << 30))
+    for xp, ldx in far:
+        for wp, ldw in far:
+            need = ctypes.c_size_t(0)
+            assert _call(getattr(lib, name), names, dict(base, T=T, d=d, V=V, x=ctypes.c_void_p(xp), ldx=ldx, w=ctypes.c_void_p(wp), ldw=ldw, work=None,
+                                                         size=ctypes.byref(need))) == 0
+            key = pk._lib._head_key(name, dev, xp, ldx, T, d, wp, ldw, V)
+            assert sizes.setdefault(key, need.value) == need.value, (xp, ldx, wp, ldw)
+    assert len(set(sizes.values())) == 4   # (none copied, x, w, both)
