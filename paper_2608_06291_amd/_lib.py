@@ -1057,7 +1057,7 @@ def layernorm_backward(dy, x, weight, mean, rstd, d_sum=None, need_dx: bool = Tr
              _vector(mean, "mean", T, f32, dev), _vector(rstd, "rstd", T, f32, dev), sp, lds,
              None if dx is None else dx.data_ptr(), d, None if dw is None else dw.data_ptr(),
              None if db is None else db.data_ptr()), dev, work,
-            ("layernorm_backward", T, d, dt, need_dx, need_dweight or need_dbias))
+            ("layernorm_backward", dev.index, T, d, dt, need_dx, need_dweight or need_dbias))
     return dx, dw, db
 
 

@@ -26,3 +26,32 @@ def test_kept_sizes_of_head_calls(lib, name):  # noqa: F811
             key = pk._lib._head_key(name, dev, xp, ldx, T, d, wp, ldw, V)
             assert sizes.setdefault(key, need.value) == need.value, (xp, ldx, wp, ldw)
     assert len(set(sizes.values())) == 4   # (none copied, x, w, both)
+
+
+class _Rows:
+    """As much of a tensor as the binding looks at."""
+
+    def __init__(self, device, *shape):
+        import torch
+        self.shape, self.dtype, self.device, self.requires_grad = shape, torch.bfloat16, device, False
+
+
+def test_kept_sizes_of_norm_gradients(monkeypatch):
+    """The size depends on the CUs of the device: each device has its own."""
+    import torch
+    import paper_2608_06291_amd as pk
+    keys = []
+    monkeypatch.setattr(pk._lib, "_rows_of", lambda t, *more: (4096, t.shape[1]))
+    monkeypatch.setattr(pk._lib, "_vector", lambda *more: 4096)
+    monkeypatch.setattr(pk._lib, "_run_op", lambda fn, args, device, work=None, key=None: keys.append(key))
+
+    class Torch:
+        def __getattr__(self, name):
+            return (lambda *shape, **more: _Rows(more["device"], *shape)) if name == "empty" else getattr(torch, name)
+    monkeypatch.setattr(_Rows, "data_ptr", lambda self: 4096, raising=False)
+    pk._lib._import_torch()
+    monkeypatch.setattr(pk._lib, "_torch", Torch())
+    for index in (0, 1):
+        x = _Rows(torch.device("cuda", index), 50, 8)
+        pk.layernorm_backward(x, x, None, None, None)
+    assert len(keys) == 2 and keys[0] != keys[1]
