@@ -1018,7 +1018,7 @@ def layernorm(x, weight=None, bias=None, residual=None, eps: float = 1e-5, centr
     layernorm_backward."""
     torch = _torch or _import_torch()
     lib = load()
-    _no_graph("layernorm", " and take the gradients from layernorm_backward", x, weight, bias, residual)
+    _no_graph("layernorm", " and take the gradients from layernorm_backward", x, weight, bias, residual, sum_out)
     xp, ldx = _rows_of(x, "x")
     T, d = x.shape
     dev, dt = x.device, x.dtype
@@ -1067,7 +1067,7 @@ def embedding(tokens, table, scale: float = 1.0, out=None):
     from embedding_backward."""
     torch = _torch or _import_torch()
     lib = load()
-    _no_graph("embedding", " and take the gradient from embedding_backward", table)
+    _no_graph("embedding", " and take the gradient from embedding_backward", table, out)
     tp, ldt = _rows_of(table, "table")
     V, d = table.shape
     dev = table.device
@@ -1088,6 +1088,7 @@ def embedding_backward(dy, tokens, rows: int, scale: float = 1.0, base=None, out
     the other end of the network; out may be base."""
     torch = _torch or _import_torch()
     lib = load()
+    _no_graph("embedding_backward", "", out)
     gp, ldg = _rows_of(dy, "dy")
     T, d = dy.shape
     dev, dt, V = dy.device, dy.dtype, int(rows)

@@ -55,3 +55,17 @@ def test_kept_sizes_of_norm_gradients(monkeypatch):
         x = _Rows(torch.device("cuda", index), 50, 8)
         pk.layernorm_backward(x, x, None, None, None)
     assert len(keys) == 2 and keys[0] != keys[1]
+
+
+def test_outputs_that_require_gradients():
+    """An output that autograd follows is not overwritten silently."""
+    import torch
+    import paper_2608_06291_amd as pk
+    x, tok = torch.zeros((2, 4)), torch.zeros(2, dtype=torch.int64)
+    out, table = torch.zeros((2, 4), requires_grad=True), torch.zeros((3, 4), requires_grad=True)
+    for call in (lambda: pk.layernorm(x, sum_out=out), lambda: pk.layernorm(x, residual=x, sum_out=out), lambda: pk.embedding(tok, x, out=out),
+                 lambda: pk.embedding_backward(x, tok, 3, out=table), lambda: pk.embedding_backward(x, tok, 3, base=table, out=table)):
+        with pytest.raises(RuntimeError, match="no_grad"):
+            call()
+        with torch.no_grad(), pytest.raises(TypeError, match="CUDA"):   # (taken, but for the device)
+            call()
