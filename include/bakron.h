@@ -782,8 +782,8 @@ bakron_status bakron_layernorm(const void *x, int64_t ldx, const void *residual,
  *   mean, rstd    from bakron_layernorm; mean NULL: the RMS norm
  *   d_sum         device, T x d of dtype, the gradient that reaches those rows past the
  *                 norm, or NULL
- *   dx            device output, T x d of dtype, or NULL; may be d_sum with the same leading
- *                 dimension
+ *   dx            device output, T x d of dtype, or NULL; may be d_sum, dy or x with the same
+ *                 leading dimension
  *   dweight, dbias  device outputs, d floats, or NULL.  T = 0 gives zeros
  * 1 <= d <= 65536.  Workspace as above (none for T <= 32, or without dweight and dbias).
  */

@@ -573,6 +573,14 @@ template <typename E>
 static void launch_layernorm_grad(LnGradArgs a, hipStream_t st) {
     constexpr int VEC = 16 / sizeof(E), NV_MAX = 64 / VEC;
     const bool columns = a.dw || a.db;
+    // dx in the place of dy or x: where others than the row's own threads read them, the columns' sums come first
+    if (columns && a.dx && (a.dx == a.dy || a.dx == a.x) && (a.T <= LN_FEW_ROWS || !ln_together(a.d, sizeof(E)))) {
+        LnGradArgs c = a;
+        c.dx = nullptr;
+        a.dw = a.db = nullptr;
+        launch_layernorm_grad<E>(c, st);
+        return launch_layernorm_grad<E>(a, st);
+    }
     if (columns) a.slices = ln_slices(a.T, a.d, sizeof(E));
     if (columns && a.T <= LN_FEW_ROWS) {
         const LnGeom g = ln_geom(a.T, a.d, VEC, NV_MAX);
@@ -668,7 +676,7 @@ extern "C" bakron_status bakron_layernorm_backward(const void* dy, int64_t lddy,
     if (st != BAKRON_OK || query) return st;
     if (lddy < d || ldx < d || (d_sum && ldds < d) || (dx && lddx < d))
         return bk::op_fail(who, "leading dimension below d");
-    if (dx && dx == d_sum && lddx != ldds)
+    if (dx && ((dx == d_sum && lddx != ldds) || (dx == dy && lddx != lddy) || (dx == x && lddx != ldx)))
         return bk::op_fail(who, "dx in place needs the same leading dimension");
     if (!dx && !dweight && !dbias) return bk::op_fail(who, "null pointer");
     if (T > 0 && (!dy || !x || !rstd)) return bk::op_fail(who, "null pointer");

@@ -118,3 +118,35 @@ def test_block_gradients_of_a_stream_of_another_type(dtype, stream):
     for got, w, lim in ((dx, want, e + _u(stream) * (want.abs() + e) + _tiny(stream)), (dnorm, wnorm, en)):
         assert bool(((got.cpu().double() - w).abs() <= lim).all()), float(((got.cpu().double() - w).abs() / lim).max())
     assert torch.equal(blk.backward(x, y, b)[0], dx)
+
+
+@pytest.mark.parametrize("columns", [True, False])
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+@pytest.mark.parametrize("T,d", [(1, 64), (5, 131), (32, 1001), (33, 1001), (300, 1001), (3000, 72), (40, 20000), (300, 20001)])
+def test_norm_gradients_in_place(dtype, T, d, columns):
+    """dx in the place of dy, of x and of d_sum (through the C entry): the same results as beside them."""
+    import ctypes
+
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("layernorm backward in place", dtype, T, d, columns)
+    lib, dt = pk.load(), _dtype(dtype)
+    st = torch.cuda.current_stream().cuda_stream
+    x, dy, ds = (_rand((T, d), k).to(dt).to(DEV) for k in (1, 2, 3))
+    w = (1 + 0.1 * _rand((d,), 4)).float().to(DEV)
+    f = pk.layernorm(x, w)
+    want = pk.layernorm_backward(dy, x, w, f.mean, f.rstd, d_sum=ds, need_dweight=columns, need_dbias=columns)
+    for place in range(3):
+        rows = [t.clone() for t in (dy, x, ds)]
+        sums = torch.full((2, d), 9.0, device=DEV)
+        args = [rows[0].data_ptr(), d, rows[1].data_ptr(), d, {"f32": 0, "bf16": 2}[dtype], T, d, w.data_ptr(), f.mean.data_ptr(), f.rstd.data_ptr(),
+                rows[2].data_ptr(), d, rows[place].data_ptr(), d, *(sums[k].data_ptr() if columns else None for k in range(2))]
+        size = ctypes.c_size_t(0)
+        assert lib.bakron_layernorm_backward(*args, None, ctypes.byref(size), st) == 0
+        work = torch.empty(size.value + 256, dtype=torch.uint8, device=DEV)
+        assert lib.bakron_layernorm_backward(*args, work.data_ptr(), ctypes.byref(size), st) == 0
+        torch.cuda.synchronize()
+        for k, t in enumerate((dy, x, ds)):
+            assert torch.equal(rows[k], want[0] if k == place else t), (place, k)
+        if columns:
+            assert torch.equal(sums[0], want[1]) and torch.equal(sums[1], want[2]), place

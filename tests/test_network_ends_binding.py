@@ -4,8 +4,8 @@ import ctypes
 
 import pytest
 
-from test_network_ends_refusals import HEAD, HEAD_OK, HEADB, HEADB_OK
-from test_operators_refusals import P, _call, lib  # noqa: F401
+from test_network_ends_refusals import HEAD, HEAD_OK, HEADB, HEADB_OK, LNB, LNB_OK
+from test_operators_refusals import P, _call, _size, lib  # noqa: F401
 
 
 @pytest.mark.parametrize("name", ["bakron_head_logprobs", "bakron_head_logprobs_backward"])
@@ -69,3 +69,12 @@ def test_outputs_that_require_gradients():
             call()
         with torch.no_grad(), pytest.raises(TypeError, match="CUDA"):   # (taken, but for the device)
             call()
+
+
+@pytest.mark.parametrize("name,ld", [("dy", "lddy"), ("x", "ldx"), ("ds", "ldds")])
+def test_norm_gradients_in_place_need_the_same_rows(lib, name, ld):  # noqa: F811
+    base = dict(LNB_OK, size=_size(1 << 50), dy=ctypes.c_void_p(16384), x=ctypes.c_void_p(32768), ds=ctypes.c_void_p(65536), dw=P)
+    base["dx"] = base[name]
+    assert _call(lib.bakron_layernorm_backward, LNB, dict(base, T=0, dw=None)) == 0
+    assert _call(lib.bakron_layernorm_backward, LNB, base, **{ld: 72}) == 1
+    assert b"in place" in lib.bakron_last_error()
