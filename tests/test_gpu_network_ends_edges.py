@@ -150,3 +150,85 @@ def test_norm_gradients_in_place(dtype, T, d, columns):
             assert torch.equal(rows[k], want[0] if k == place else t), (place, k)
         if columns:
             assert torch.equal(sums[0], want[1]) and torch.equal(sums[1], want[2]), place
+
+
+def _walk(x, w, z):
+    """Errors of fp32 logits as a random walk: each of d roundings is off by U32 of a partial sum at most, which lies between 0
+    and z but for a few times the root of the sum of squares; independent ones add up to the root of their number.  Six times
+    that, for the largest of many."""
+    return 6 * x.shape[1] ** 0.5 * U32 * ((x.square() @ w.square().t()).sqrt() + z.abs())
+
+
+@pytest.mark.parametrize("dtype", ("f16", "bf16"))
+@pytest.mark.parametrize("T,d,V,pad,shift", HEAD + HEAD_LARGE)
+def test_head_statistics_as_good_as_their_sums(dtype, T, d, V, pad, shift):
+    """lse, log probability and entropy within what roundings leave on the average, far below their own sizes: the bounds of the
+    worst case would let whole nats of the entropy pass for long rows."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("head statistics", dtype, T, d, V, pad, shift)
+    x, w, tok = _head_inputs(T, d, V, dtype)
+    xs, ws, tk = _strided(x, pad, shift), _strided(w, pad, shift), tok.to(DEV)
+    got = pk.head_logprobs(xs, ws, tk)
+    wd = w.to(DEV).double()
+    for rows in torch.arange(T, device=DEV).split(1024):
+        xd, t = x.to(DEV)[rows].double(), tk[rows]
+        z = xd @ wd.t()
+        ez = _walk(xd, wd, z)
+        top = z.amax(1)
+        lse = torch.logsumexp(z, 1)
+        logp = z.sub_(lse[:, None])
+        p = logp.exp()
+        H = torch.special.entr(p).sum(1)
+        # what the logits' errors make of lse and of the entropy, to the first order (the second is their square)
+        of_lse, of_H = (p * ez).sum(1), (p * (logp + H[:, None]).abs() * ez).sum(1)
+        asked = (t >= 0) & (t < V)
+        k = t.clamp(0, V - 1)[:, None]
+        at, ez_at = logp.gather(1, k)[:, 0], ez.gather(1, k)[:, 0]
+        # the sums of V positive terms, a walk as well (four times the root of V), with 40 levels of joins and exp's 4 U32 and
+        # those of its argument's rounding
+        mean = (p * (top[:, None] - lse[:, None] - logp)).sum(1)           # sum p (m - z)
+        es = (4 * V ** 0.5 + 40 + 4 * (1 + mean)) * U32
+        second = (p * ez.square()).sum(1)
+        for g, want, tol in ((got.lse, lse, of_lse + second + es + 2 * U32 * (lse.abs() + 1)),
+                             (got.logprob, torch.where(asked, at, 0.0),
+                              torch.where(asked, ez_at + of_lse + second + es + 4 * U32 * (at.abs() + 1), 0.0)),
+                             (got.entropy, H, of_H + (2 + H) * second + es * (2 + mean) + 8 * U32 * (1 + mean + H))):
+            far = (g[rows].double() - want).abs()
+            assert bool((far <= tol).all()), float((far / tol.clamp(min=1e-300)).max())
+        if V > 1000:
+            # the bound says something of each row: 1% of its entropy, or of one nat where the entropy is less (it goes to 0 with
+            # 1 - p of the row's token, the roundings of log s and of the mean, at 4 sqrt(V) U32 > 7e-6, do not)
+            assert bool((tol < 0.01 * H.clamp(min=1.0)).all()), float(tol.max())
+        del z, logp, p, ez
+
+
+@pytest.mark.parametrize("dtype", ("f16", "bf16"))
+@pytest.mark.parametrize("T,d,V", [(2100, 520, 33000), (70, 1001, 67201), (2048, 1024, 16384), (600, 72, 9001)])
+def test_head_large_gradients_of_entropies(dtype, T, d, V):
+    """Gradients of log probabilities and entropies together, and of entropies alone, over tiles, pieces and parts."""
+    import paper_2608_06291_amd as pk
+    torch = _t()
+    _say("head large, entropy", dtype, T, d, V)
+    x, w, tok = (t.to(DEV) for t in _head_inputs(T, d, V, dtype))
+    lp = pk.head_logprobs(x, w, tok)
+    xd, wd = x.double(), w.double()
+    logp = torch.log_softmax(xd @ wd.t(), 1)
+    p = logp.exp()
+    H = torch.special.entr(p).sum(1)
+    g = torch.Generator().manual_seed(9)
+    gl, gh = (((torch.rand((T,), generator=g) - 0.5) / T).to(DEV) for _ in range(2))
+    asked = (tok >= 0) & (tok < V)
+    for a in (gl, None):
+        dz = -p * (gh.double()[:, None] * (logp + H[:, None]))
+        if a is not None:
+            ga = torch.where(asked, a.double(), 0.0)
+            dz -= p * ga[:, None]
+            dz[asked, tok[asked]] += ga[asked]
+        u = _u(dtype)
+        for got, want in zip(pk.head_logprobs_backward(x, w, tok, lp.lse, lp.entropy, a, gh), (dz @ wd, dz.t().contiguous() @ xd)):
+            far = float((got.double() - want).norm())
+            # one rounding of the result and one of dz, 0.43 u of a root mean square each, of as many numbers as there are
+            # entries and rows (one in four of which counts); statistics in fp32 are 1e-3 of that
+            own, of_dz = (0.44 * u * (1 + 2 / math.sqrt(n)) for n in (want.numel(), T / 4))
+            assert far <= (math.hypot(own, of_dz) + 1e-5) * float(want.norm()) + _tiny(dtype) * math.sqrt(want.numel()), far / float(want.norm())
