@@ -557,10 +557,11 @@ static void launch_layernorm(const LnArgs& a, hipStream_t st) {
 // The gradients together, where a row is at most two vectors a thread of 1024; else dx, then dw and db from x and
 // dy read once more.  Slices of the rows: together, one a CU, more where each still has 16 blocks of rows, because a
 // slice's sums are as much to write and read as two rows; else so many that every CU has two workgroups.
-static bool ln_together(int64_t d, int esize) { return d * esize <= 2 * 16 * 1024; }
+constexpr int LN_GRAD_NV = 2;   // vectors a thread
+static bool ln_together(int64_t d, int esize) { return d * esize <= LN_GRAD_NV * 16 * 1024; }
 static int ln_slices(int64_t T, int64_t d, int esize) {
     if (ln_together(d, esize)) {
-        const LnGeom g = ln_geom(1 << 20, d, 16 / esize, 2);
+        const LnGeom g = ln_geom(1 << 20, d, 16 / esize, LN_GRAD_NV);
         const int64_t blocks = (T + g.rows - 1) / g.rows, cus = op_cus();
         const int64_t most = cus * std::max(1, 512 / (g.tpr * g.rows));   // so many have room
         return (int)std::max<int64_t>(1, std::min({blocks, most, std::max(cus, blocks / 16)}));
@@ -597,13 +598,10 @@ static void launch_layernorm_grad(LnGradArgs a, hipStream_t st) {
         return;
     }
     if (columns && ln_together(a.d, sizeof(E))) {
-        const LnGeom g = ln_geom(1 << 20, a.d, VEC, 2);
+        const LnGeom g = ln_geom(1 << 20, a.d, VEC, LN_GRAD_NV);
         const dim3 grid((unsigned)a.slices), block(g.tpr, g.rows);
         const int lds = g.rows > 1 ? (2 * g.nv * VEC + 2) * 64 * (int)sizeof(float) : 0;
-        if (g.nv == 1)
-            hipLaunchKernelGGL((k_layernorm_grad<E, 1>), grid, block, lds, st, a);
-        else
-            hipLaunchKernelGGL((k_layernorm_grad<E, 2>), grid, block, lds, st, a);
+        hipLaunchKernelGGL((k_layernorm_grad<E, LN_GRAD_NV>), grid, block, lds, st, a);
     } else if (a.dx) {
         const LnGeom g = ln_geom(a.T, a.d, VEC, NV_MAX);
         const dim3 grid((unsigned)((a.T + g.rows - 1) / g.rows)), block(g.tpr, g.rows);
