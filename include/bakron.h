@@ -709,7 +709,7 @@ bakron_status bakron_token_logprobs_backward(const void *logits, int64_t ld, int
  * A row with a logit that is NaN or +inf has NaN in every output; one whose logits
  * are all -inf has lse and log probability -inf and entropy 0.
  * 1 <= d <= 2^17, 1 <= V <= 2^20, T <= 2^27, ceil(T / 64) ceil(max(d, V) / 64) < 2^23
- * (or BAKRON_EINVAL).  Workspace as above: 16 bytes a row for 32 to 256 tokens of the
+ * (or BAKRON_EINVAL).  Workspace as above: 16 bytes a row for 16 to 256 tokens of the
  * vocabulary, and padded copies of x and w where their rows are no 16-byte multiples
  * at 16-byte addresses (not for T <= 8, nor for T <= 32 with d no multiple of 8).
  */
@@ -725,14 +725,13 @@ bakron_status bakron_head_logprobs(const void *x, int64_t ldx, int64_t T, int64_
  *   dz_tj = g_logprob_t (1[j = target_t] - p_tj) - g_entropy_t p_tj (log p_tj + entropy_t)
  *   dx = dz w,   dw = dz^T x
  * A target outside [0, V) has no first term; a row whose logits are all -inf has dz = 0.
- * dz is rounded to dtype for the products, in BAKRON_F16 times
- * a power of two (undone at the end) by the largest |g_logprob| + 4 |g_entropy| of the rows
- * that ask for them (without g_logprob where the target lies outside [0, V); not of rows whose
- * logits are all -inf); with the
- * result's own rounding that leaves errors of about 2.4e-3 of a gradient's norm in
- * BAKRON_BF16 and 2.9e-4 in BAKRON_F16 (with a hundred rows up to 3e-3 and 4e-4), where one
- * rounding gives 1.7e-3 and 2.1e-4.  For T <= 64, where the errors may not average out, dz is kept as two numbers of dtype, and the
- * result is as good as rounded once.
+ * dz is rounded to dtype for the products, in BAKRON_F16 times a power of two (undone at the
+ * end) by the largest |g_logprob| + 4 |g_entropy| of the rows that ask for them (without
+ * g_logprob where the target lies outside [0, V); not of rows whose logits are all -inf).  With
+ * the result's own rounding that leaves errors of about 2.4e-3 of a gradient's norm in
+ * BAKRON_BF16 and 3.3e-4 in BAKRON_F16 (with a hundred rows up to 3e-3 and 4e-4), where one
+ * rounding gives 1.7e-3 and 2.1e-4.  For T <= 64, where the errors may not average out, dz is
+ * kept as two numbers of dtype, and the result is as good as rounded once.
  *   lse, entropy  from bakron_head_logprobs (entropy may be NULL without g_entropy)
  *   g_logprob, g_entropy  device, T floats, or NULL for 0; target may be NULL
  *                 without g_logprob
@@ -800,7 +799,7 @@ bakron_status bakron_layernorm_backward(const void *dy, int64_t lddy, const void
  *   tokens  device, T token numbers
  *   table   device, V x d of dtype (bakron_dtype)
  *   y       device output, T x d of dtype
- * T <= 2^20, 1 <= V <= 2^20, 1 <= d <= 65536; T ceil(d / 8192) (fp32: 4096) <= 2^23 (or
+ * T <= 2^20 as in the gradient, 1 <= V <= 2^20, 1 <= d <= 65536; T ceil(d / 8192) (fp32: 4096) <= 2^23 (or
  * BAKRON_EINVAL).  One launch.
  */
 bakron_status bakron_embedding(const int64_t *tokens, int64_t T, const void *table, int64_t ldt,
@@ -810,8 +809,9 @@ bakron_status bakron_embedding(const int64_t *tokens, int64_t T, const void *tab
 /*
  * bakron_embedding_backward -- the table's gradient:
  *   dtable_v = base_v + scale * sum_{t: tokens_t = v} dy_t
- * The sums are fp32 and rounded once; their order depends on the tokens alone (sums over at most
- * 16 rising t, added up in rising order).  Rows without a token are base, or zeros.
+ * The sums are fp32 and rounded once; their order depends on the tokens alone: rising t up to T = 256,
+ * beyond sums over at most 16 rising t, added up in rising order.  Rows without a token are
+ * base, or zeros.
  *   dy      device, T x d of dtype
  *   base    device, V x d of dtype, or NULL for 0: e.g. the gradient of the same matrix at the
  *           other end of the network

@@ -594,7 +594,8 @@ static void launch_embed_grad(const EmbedGradArgs& a, const int64_t* tokens, hip
 }  // namespace bk
 
 static bakron_status embed_sizes(const char* who, int32_t dtype, int64_t T, int64_t V, int64_t d) {
-    // (rows and pieces of a launch; positions are sorted as 32-bit numbers, all against all)
+    // (rows and pieces of a launch; tokens and positions of the gradient are sorted as 32-bit numbers, tokens by two digits of
+    // 11 bits; the forward pass takes as many as its gradient does)
     if (T < 0 || T > ((int64_t)1 << 20) || V < 1 || V > ((int64_t)1 << 20) || d < 1 || d > 65536)
         return bk::op_fail(who, "bad size");
     if (dtype != BAKRON_F32 && dtype != BAKRON_F16 && dtype != BAKRON_BF16) return bk::op_fail(who, "bad dtype");

@@ -5,7 +5,8 @@
 //
 // Forward: the tile product of tile.h with a softmax in its epilogue.  Every tile leaves, for each of its
 // rows of x, the largest logit m, s = sum exp(z - m) and s1 = sum exp(z - m) (z - m) over its part of the
-// vocabulary (16 bytes for 64 to 256 tokens, where the logits would take 4 bytes each); a second launch joins the parts:
+// vocabulary (16 bytes for 64 to 256 tokens, of few rows 16 to 64, where the logits would take 4 bytes each); a second
+// launch joins the parts:
 //   s = s_a e^(m_a - m) + s_b e^(m_b - m),   s1 = (s1_a + (m_a - m) s_a) e^(m_a - m) + the same of b.
 // Backward: the vocabulary goes in pieces.  Of a piece the logits are computed again, with dz in the
 // epilogue, rounded to 16 bits as operand of two products: dW of the piece, and dx, whose sums stay in
@@ -14,7 +15,7 @@
 // Measured (bf16): 4096 x 4096 x 131072 3270 to 3370 us forward, 1345 TFLOP/s (the library's product of that size,
 // without the softmax: 3050; matrix cores 67% busy, bound by power), 2048 x 4096 x 32768 391; gradients of the first
 // 10130 to 10520 us, 1255 to 1302 TFLOP/s (a piece: logits and dz 435, dx 404, dW 447), of the second 1350 to 1395.  dz's and dW's
-// stores overlap nothing (one workgroup a CU, all at the end of a round): 20 and 8% of those kernels' time.
+// stores overlap nothing (one workgroup a CU, all at the end of a round).
 // Few rows are bound by reading w: one row of 4096 x 32768 42 us (6.3 TB/s of 268 MB) and 5 for the join, 32 rows of 4096 x
 // 131072 182; gradients of one row of 4096 x 32768 135 us (w twice, dW once: 805 MB, 6.0 TB/s), of 32 175, of 64 224, of
 // 256 284.
@@ -840,8 +841,13 @@ __global__ __launch_bounds__(256) void k_transpose(const char* x, int64_t ld, in
 }
 
 // The backward pass.  A piece of the vocabulary is as long as dz of it stays in the last-level cache (256 MB) with
-// the operands beside it (4096 x 4096 x 131072 in pieces of 128 MB 10130 us, of 512 MB 10330).  The rows of one chunk or less
-// do not average dz's rounding out, so there the products go on over its rests, too.
+// the operands beside it (4096 x 4096 x 131072 in pieces of 128 MB 10130 us, of 512 MB 10330).
+//
+// dz's rounding to 16 bits is as large in a gradient as the result's own: 2.2e-3 to 2.4e-3 of its norm where the result's
+// alone is 1.7e-3 (half precision 3.3e-4 and 2.1e-4).  The rows of one chunk or less (T <= 64) do not average it out, a few
+// of them can lose more, and reading W is what they take: there the products go on over dz's rests, too.  Beyond,
+// the rests would be half as much work again: 4096 x 4096 x 131072 10260 us and with rests 16990, 2048 x 4096 x 32768 1357 and
+// 2226, 256 rows 282 and 384, 200 x 1000 x 5003 32 and 37 (half precision 35 and 40).
 //
 // dW's product reads x and dz by columns (transposing reads).  For many pieces and rows x is transposed once instead, which
 // costs 17 us there: 10350 -> 10130 us, 2048 x 4096 x 32768 1372 -> 1349.
@@ -849,7 +855,8 @@ __global__ __launch_bounds__(256) void k_transpose(const char* x, int64_t ld, in
 // A dW that the last-level cache would not hold with anything beside it is written past it, or w would be swept out of it
 // and what follows wait for it to be written: 65 x 4096 x 32768 254 -> 190 us, 256 rows 326 -> 287, 100 x 2048 x 100000 418 ->
 // 352, 2048 rows and more no difference.  Not where its rows share lines, which the caches join (1 x 1001 x 70000 130 us, past
-// them 161).
+// them 161), nor by the launch of both products, which is the faster one through the caches, too (128 x 4096 x 16384 97 us, two
+// launches past them 104; 65 rows 95 and 103, 256 142 and 146; 65 x 2048 x 32768 90 and 100; 256 x 1024 x 65536 144 and 152).
 constexpr int64_t HEAD_PIECE_BYTES = (int64_t)128 << 20, HEAD_PAST = (int64_t)128 << 20;
 struct HeadBackward {
     int64_t vc, vp, ldz;   // tokens of a piece (all but the last), padded; row of dz
