@@ -843,7 +843,7 @@ __global__ __launch_bounds__(256) void k_transpose(const char* x, int64_t ld, in
 // The backward pass.  A piece of the vocabulary is as long as dz of it stays in the last-level cache (256 MB) with
 // the operands beside it (4096 x 4096 x 131072 in pieces of 128 MB 10130 us, of 512 MB 10330).
 //
-// dz's rounding to 16 bits is as large in a gradient as the result's own: 2.2e-3 to 2.4e-3 of its norm where the result's
+// dz's rounding to 16 bits is as large in a gradient as the result's own: 2.2e-3 to 2.5e-3 of its norm where the result's
 // alone is 1.7e-3 (half precision 3.3e-4 and 2.1e-4).  The rows of one chunk or less (T <= 64) do not average it out, a few
 // of them can lose more, and reading W is what they take: there the products go on over dz's rests, too.  Beyond,
 // the rests would be half as much work again: 4096 x 4096 x 131072 10260 us and with rests 16990, 2048 x 4096 x 32768 1357 and
