@@ -62,12 +62,12 @@ struct HeadArgs {
     // backward
     const float *lse, *entropy, *g_logprob, *g_entropy;
     int64_t v0, all;           // first token of the piece; tokens of all pieces
-    __host__ __device__ HeadIn in() const { return HeadIn{target, lse, g_logprob, g_entropy, all}; }
     void* dz;                  // T rows: vp entries (zeros in the padding), then what their rounding took
     int64_t vp, ldz;           // ldz: vp, or 2 vp with the rests
     const float* factor;       // half precision: dz is taken times this, or NULL: by the kernel itself,
     HeadScale* scale;          // whose first workgroup leaves it here
     void* dzt;                 // few rows: dz once more, a token a row: 16 or 32 rows of x, then the rests
+    __host__ __device__ HeadIn in() const { return HeadIn{target, lse, g_logprob, g_entropy, all}; }
 };
 
 // What few rows need beside that: x and w as they are, in entries.
