@@ -846,7 +846,7 @@ __global__ __launch_bounds__(256) void k_transpose(const char* x, int64_t ld, in
 // dz's rounding to 16 bits is as large in a gradient as the result's own: 2.2e-3 to 2.5e-3 of its norm where the result's
 // alone is 1.7e-3 (half precision 3.3e-4 and 2.1e-4).  The rows of one chunk or less (T <= 64) do not average it out, a few
 // of them can lose more, and reading W is what they take: there the products go on over dz's rests, too.  Beyond,
-// the rests would be half as much work again: 4096 x 4096 x 131072 10260 us and with rests 16990, 2048 x 4096 x 32768 1357 and
+// the rests would be two thirds more work (five products for three): 4096 x 4096 x 131072 10260 us and with rests 16990, 2048 x 4096 x 32768 1357 and
 // 2226, 256 rows 282 and 384, 200 x 1000 x 5003 32 and 37 (half precision 35 and 40).
 //
 // dW's product reads x and dz by columns (transposing reads).  For many pieces and rows x is transposed once instead, which
